@@ -336,6 +336,103 @@ int revffn_op_attention_bwd_noalloc(int32_t dtype, int32_t kernel_mode, const vo
                                     void *dq, void *dk, void *dv, int32_t B, int32_t S,
                                     int32_t H, int32_t dh, int32_t causal, void *hip_stream);
 
+/* ---- attention over key ranges, rotary positions, layer norm ------------------------------------------------------
+ * The parts of an attention layer in which pre-trained models and training batches differ from the block above: packed
+ * documents, prefixes, windows, capped scores, a distance bias, shared key heads, other rotary layouts, and LayerNorm.
+ * None of the calls needs a context; they allocate nothing, only enqueue work on hip_stream and can be captured into a HIP
+ * graph.  Device pointers belong to the device that is current at the call, and so does hip_stream.  Scratch memory comes
+ * from the caller (16-byte aligned): it needs no initial contents and keeps none for a later call, and two calls that may
+ * overlap need two.  A returned REVFFN_EINVAL / ESHAPE / ENULL means that nothing has been enqueued.
+ * Arithmetic and sums are float32; with REVFFN_BF16 the attention probabilities and score gradients are rounded to bfloat16 as
+ * operands of the matrix cores, and results are rounded once.  No atomics: same inputs, same bits.
+ *
+ * Which keys a query sees.  Query row i sees the key rows lo[i] <= j < hi[i] (clamped to 0 .. Tk; lo >= hi: none).  Documents
+ * that lie one behind the other, causal order, a prefix that everybody sees and a sliding window are all such ranges;
+ * revffn_op_attention_ranges writes them, or the caller does.  A query that sees nothing gets o = 0, lse = -inf and dq = 0;
+ * a key that nobody sees gets dk = dv = 0.  What lies outside a query's range never reaches its results, not even an
+ * infinity or a NaN (a tile that holds one is then worked out again row by row, which is slow). */
+typedef struct revffn_attn_mask {
+  const int32_t *lo, *hi;  /* device [Tq]                                                            */
+  const int32_t *at;       /* device [Tq]: the key row at which query i stands (only the distance bias reads it); NULL = i */
+  const int32_t *used;     /* device [2] or NULL: query rows and key rows in use, clamped to Tq and Tk; result rows from
+                              there on are left as they were.  NULL = all                            */
+} revffn_attn_mask;
+
+typedef struct revffn_attn_desc {
+  int32_t dtype;           /* REVFFN_F32 or REVFFN_BF16: q, k, v, o and the gradients                */
+  int32_t kernel_mode;     /* 0 = automatic, 1 = the row-by-row kernels (any shape, slow), 2 = matrix-core kernels only */
+  int32_t H, Hkv, dh;      /* query heads; key heads (divides H: query head h reads key head h / (H / Hkv)); head width 1..512 */
+  int32_t Tq, Tk;          /* rows of q, o and of k, v (Tk may be 0)                                 */
+  int64_t ldq, ldk, ldv, ldo; /* row strides in elements of q, dq / k, dk / v, dv / o, d_o (head hh in columns hh*dh ..);
+                              0 = dense (H*dh, Hkv*dh)                                               */
+  float scale;             /* of q . k; 0 = 1 / sqrt(dh)                                             */
+  float softcap;           /* > 0: scores become softcap * tanh(score / softcap); 0 = not            */
+  const float *slopes;     /* device [H] or NULL: slopes[hh] * |at[i] - j| is subtracted from the (capped) score; no gradient */
+} revffn_attn_desc;
+
+/* Ranges of n_docs documents that lie one behind the other in the rows of q and of k.  cu_q, cu_k: device [n_docs + 1] first
+ * row of each document and the end of the last; cu_q NULL: documents of Tq / n_docs rows; cu_k NULL: as cu_q (both NULL:
+ * Tk / n_docs rows).  A document's queries are the last of its rows: query r of n, with m keys, stands at key m - n + r.
+ * causal: it sees the keys up to its own; with prefix (device [n_docs] or NULL) also the first prefix[doc] ones whatever
+ * their order; with window > 0 the last `window` of them only (0 = no window; prefix and window exclude each other, and
+ * both need causal).  Rows before cu_q[0] and from cu_q[n_docs] on see nothing.  at and used may be NULL.  Row
+ * numbers out of range are clamped. */
+int revffn_op_attention_ranges(const int32_t *cu_q, const int32_t *cu_k, const int32_t *prefix, int32_t n_docs,
+                               int32_t causal, int32_t window, int32_t Tq, int32_t Tk, int32_t *lo, int32_t *hi,
+                               int32_t *at, int32_t *used, void *hip_stream);
+
+/* o = softmax(scores) v over each query's range; lse[H, Tq] = log of the sum of exponentials (NULL if not wanted; the
+ * backward pass needs it).  q, k, v are not changed and overlap no result.  work: revffn_op_attention_masked_workspace
+ * bytes.  A call of few query rows, a single token each for instance, is split along its keys and joined.
+ * The backward pass takes o and lse of the forward pass with the same desc and mask, and d_o; dq, dk, dv are overwritten.
+ * dk and dv are summed over the query heads that share a key head.
+ * REVFFN_EINVAL: a bad field, work_bytes too small.  REVFFN_ESHAPE: a row stride below the row's width, or more rows
+ * times heads than a launch can have (2^26).  REVFFN_EUNSUPPORTED: kernel_mode 2 and a shape that the matrix-core kernels
+ * don't take (float32: dh a multiple of 4 up to 128; bfloat16: of 8; strides and pointers aligned to 16 bytes). */
+size_t revffn_op_attention_masked_workspace(const revffn_attn_desc *desc, int32_t backward);
+int revffn_op_attention_masked_fwd(const revffn_attn_desc *desc, const revffn_attn_mask *mask, const void *q, const void *k,
+                                   const void *v, void *o, float *lse, void *work, size_t work_bytes, void *hip_stream);
+int revffn_op_attention_masked_bwd(const revffn_attn_desc *desc, const revffn_attn_mask *mask, const void *q, const void *k,
+                                   const void *v, const void *o, const void *d_o, const float *lse, void *dq, void *dk,
+                                   void *dv, void *work, size_t work_bytes, void *hip_stream);
+
+/* Rotary positions.  Pair i of the first `dims` columns of a head is turned by the angle pos * f_i and multiplied by
+ * magnitude; the other columns are copied.  f_i = theta^(-2 i / dims), scaled for contexts longer than the trained one:
+ *   1 linear: f_i / factor;   2 base: theta * factor^(dims / (dims - 2)) in theta's place;
+ *   3 wavelength (arXiv 2309.00071, by parts): g f_i + (1 - g) f_i / factor, where g rises from 0 to 1 as the turns that
+ *     pair i makes over `original` positions rise from few_turns to many_turns.
+ * Angles are worked out in float64 and reduced there, so far positions lose nothing. */
+typedef struct revffn_rotary {
+  int32_t dims;            /* even, 2..min(dh, 256)                                                   */
+  int32_t interleaved;     /* 0: pairs (c, c + dims/2), as the block's own rotation;  1: pairs (2c, 2c + 1) */
+  int32_t scaling;         /* 0 none, 1 linear, 2 base, 3 wavelength                                  */
+  int32_t original;        /* scaling 3: positions the model was trained on                           */
+  float theta, factor;     /* > 0; factor is read with scaling 1..3                                   */
+  float few_turns, many_turns;  /* scaling 3: 0 <= few < many                                         */
+  float magnitude;         /* 0 = 1                                                                   */
+} revffn_rotary;
+/* The dims / 2 angles per position, to a HOST array (no GPU work). */
+int revffn_op_rotary_frequencies(const revffn_rotary *r, double *freqs);
+/* x, y: T rows (fewer than 2^24) of H heads of dh (<= 1024, H * dh <= 2^22) columns, row strides ldx, ldy in elements; y = x (with ldy = ldx) turns in place,
+ * otherwise they must not share elements.  pos: device [T], or NULL: row t is at position t % S.  transposed: the turn by
+ * -angle, which is the gradient (and, at magnitude 1, the inverse) of the other. */
+int revffn_op_rotary(int32_t dtype, const revffn_rotary *r, const void *x, void *y, const int32_t *pos, int32_t T,
+                     int32_t S, int32_t H, int32_t dh, int64_t ldx, int64_t ldy, int32_t transposed, void *hip_stream);
+
+/* LayerNorm of `rows` rows (fewer than 2^22) of `cols` (<= 2^24) columns: y = (x - mean) * rstd * gain + bias, rstd = 1 / sqrt(variance + eps).  gain and
+ * bias (dtype, [cols]) may be NULL (1 and 0).  mean, rstd (float32 [rows]) may be NULL; the backward pass needs them.  y may be
+ * x with the same stride.  Backward: dx, and the sums dgain, dbias over the rows (either may be NULL: not wanted), in
+ * dtype, or float32 with grads_f32; dx may be dy with the same stride.  All are overwritten.  work: revffn_op_layernorm_workspace bytes,
+ * read only if dgain or dbias is wanted.  rows = 0 is allowed (dgain = dbias = 0). */
+size_t revffn_op_layernorm_workspace(int32_t rows, int32_t cols);
+int revffn_op_layernorm_fwd(int32_t dtype, const void *x, const void *gain, const void *bias, void *y, float *mean,
+                            float *rstd, int32_t rows, int32_t cols, int64_t ldx, int64_t ldy, float eps,
+                            void *hip_stream);
+int revffn_op_layernorm_bwd(int32_t dtype, const void *dy, const void *x, const void *gain, const float *mean,
+                            const float *rstd, void *dx, void *dgain, void *dbias, int32_t rows, int32_t cols,
+                            int64_t lddy, int64_t ldx, int64_t lddx, int32_t grads_f32, void *work, size_t work_bytes,
+                            void *hip_stream);
+
 /* Host-only check hook (no GPU work): where the MFMA GEMM's XCD-aware launch places its workgroups.
  * Workgroups reach the 8 XCDs round-robin by linear id; the kernel maps workgroup `i` back to a tile so that
  * each XCD works on tiles that share operands.  This call runs the same index function on the host for every

@@ -11,7 +11,10 @@ from .binding import (Config, Weights, Grads, Context, load_library, library_pat
                       revffn_get_branch, revffn_strerror, RevffnError, EXPORTED_SYMBOLS,
                       WEIGHT_FIELDS, revffn_op_gemm, revffn_op_attention_fwd, revffn_op_attention_bwd,
                       revffn_op_attention_bwd_noalloc, revffn_op_tile_placement,
-                      Merged, MERGED_FIELDS, revffn_merge_adapters, revffn_forward_merged, revffn_inverse_merged)
+                      Merged, MERGED_FIELDS, revffn_merge_adapters, revffn_forward_merged, revffn_inverse_merged,
+                      AttnDesc, AttnMask, Rotary, revffn_op_attention_ranges, revffn_op_attention_masked_workspace,
+                      revffn_op_attention_masked_fwd, revffn_op_attention_masked_bwd, revffn_op_rotary_frequencies,
+                      revffn_op_rotary, revffn_op_layernorm_workspace, revffn_op_layernorm_fwd, revffn_op_layernorm_bwd)
 
 __all__ = ["Config", "Weights", "Grads", "Context", "load_library", "library_path",
            "revffn_forward", "revffn_inverse", "revffn_backward", "revffn_backward_stored", "revffn_inverse_backward",
@@ -20,4 +23,7 @@ __all__ = ["Config", "Weights", "Grads", "Context", "load_library", "library_pat
            "revffn_strerror", "RevffnError", "EXPORTED_SYMBOLS", "WEIGHT_FIELDS", "revffn_op_gemm",
            "revffn_op_attention_fwd", "revffn_op_attention_bwd", "revffn_op_attention_bwd_noalloc",
            "revffn_op_tile_placement", "Merged", "MERGED_FIELDS", "revffn_merge_adapters", "revffn_forward_merged",
-           "revffn_inverse_merged"]
+           "revffn_inverse_merged", "AttnDesc", "AttnMask", "Rotary", "revffn_op_attention_ranges",
+           "revffn_op_attention_masked_workspace", "revffn_op_attention_masked_fwd", "revffn_op_attention_masked_bwd",
+           "revffn_op_rotary_frequencies", "revffn_op_rotary", "revffn_op_layernorm_workspace", "revffn_op_layernorm_fwd",
+           "revffn_op_layernorm_bwd"]

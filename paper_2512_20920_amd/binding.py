@@ -15,6 +15,9 @@ EXPORTED_SYMBOLS = (
     "revffn_set_kernel_mode", "revffn_set_helper_streams", "revffn_strerror", "revffn_profile_enable", "revffn_profile_read",
     "revffn_profile_kernel_name", "revffn_op_gemm", "revffn_op_attention_fwd", "revffn_op_attention_bwd",
     "revffn_op_attention_bwd_noalloc", "revffn_op_tile_placement",
+    "revffn_op_attention_ranges", "revffn_op_attention_masked_workspace", "revffn_op_attention_masked_fwd",
+    "revffn_op_attention_masked_bwd", "revffn_op_rotary_frequencies", "revffn_op_rotary", "revffn_op_layernorm_workspace",
+    "revffn_op_layernorm_fwd", "revffn_op_layernorm_bwd",
 )
 
 WEIGHT_FIELDS = (
@@ -49,6 +52,32 @@ MERGED_FIELDS = ("wq", "wk", "wv", "wo", "w_gate_up", "w_down", "ws_gate_up", "w
 
 class Merged(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in MERGED_FIELDS]
+
+
+class AttnDesc(ctypes.Structure):
+    """revffn_attn_desc; slopes: a float32 tensor (kept alive by this object), an address or None."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "kernel_mode", "H", "Hkv", "dh", "Tq", "Tk")] + [
+        (n, ctypes.c_int64) for n in ("ldq", "ldk", "ldv", "ldo")] + [
+        ("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("slopes", ctypes.c_void_p)]
+
+    def __init__(self, slopes=None, **fields):
+        super().__init__(slopes=_ptr(slopes), **fields)
+        self.kept = slopes
+
+
+class AttnMask(ctypes.Structure):
+    """revffn_attn_mask; int32 tensors (kept alive by this object), addresses or None."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("lo", "hi", "at", "used")]
+
+    def __init__(self, lo, hi, at=None, used=None):
+        super().__init__(_ptr(lo), _ptr(hi), _ptr(at), _ptr(used))
+        self.kept = (lo, hi, at, used)
+
+
+class Rotary(ctypes.Structure):
+    """revffn_rotary."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("dims", "interleaved", "scaling", "original")] + [
+        (n, ctypes.c_float) for n in ("theta", "factor", "few_turns", "many_turns", "magnitude")]
 
 
 def library_path():
@@ -102,6 +131,18 @@ def load_library():
                                             i32, i32, i32, i32, i32, vp]
     lib.revffn_op_attention_bwd_noalloc.argtypes = [i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp,
                                                     i32, i32, i32, i32, i32, vp]
+    desc, mask, rot, size = ctypes.POINTER(AttnDesc), ctypes.POINTER(AttnMask), ctypes.POINTER(Rotary), ctypes.c_size_t
+    lib.revffn_op_attention_ranges.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp]
+    lib.revffn_op_attention_masked_workspace.argtypes = [desc, i32]
+    lib.revffn_op_attention_masked_workspace.restype = size
+    lib.revffn_op_attention_masked_fwd.argtypes = [desc, mask, vp, vp, vp, vp, vp, vp, size, vp]
+    lib.revffn_op_attention_masked_bwd.argtypes = [desc, mask, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, size, vp]
+    lib.revffn_op_rotary_frequencies.argtypes = [rot, vp]
+    lib.revffn_op_rotary.argtypes = [i32, rot, vp, vp, vp, i32, i32, i32, i32, i64, i64, i32, vp]
+    lib.revffn_op_layernorm_workspace.argtypes = [i32, i32]
+    lib.revffn_op_layernorm_workspace.restype = size
+    lib.revffn_op_layernorm_fwd.argtypes = [i32, vp, vp, vp, vp, vp, vp, i32, i32, i64, i64, ctypes.c_float, vp]
+    lib.revffn_op_layernorm_bwd.argtypes = [i32, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i64, i64, i64, i32, vp, size, vp]
     lib.revffn_profile_enable.argtypes = [vp, i32]
     lib.revffn_profile_read.argtypes = [vp, i32, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int64),
                                         ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double)]
@@ -110,8 +151,8 @@ def load_library():
     lib.revffn_strerror.restype = ctypes.c_char_p
     lib.revffn_strerror.argtypes = [ctypes.c_int]
     for name in EXPORTED_SYMBOLS:
-        if name not in ("revffn_workspace_bytes", "revffn_destroy", "revffn_strerror",
-                        "revffn_profile_kernel_name"):
+        if name not in ("revffn_workspace_bytes", "revffn_destroy", "revffn_strerror", "revffn_profile_kernel_name",
+                        "revffn_op_attention_masked_workspace", "revffn_op_layernorm_workspace"):
             getattr(lib, name).restype = ctypes.c_int
     _LIB = lib
     return lib
@@ -364,3 +405,84 @@ def revffn_inverse_merged(ctx, weights, merged, y1, y2, x1, x2, B, S, ld, residu
     w, m = _w(weights), _m(merged)
     _check(ctx.lib.revffn_inverse_merged(ctx.handle, ctypes.byref(w), ctypes.byref(m), _ptr(y1), _ptr(y2), _ptr(x1),
                                          _ptr(x2), B, S, ld, _ptr(residual), _stream(stream)))
+
+
+# ---- attention over key ranges, rotary positions, layer norm ----------------------------------------------------------
+def _check_tensors(dtype, typed, others=(), ints=(), work=None):
+    """Tensors must lie on the current device and have the element type that the call reads: `typed` the one of `dtype`,
+    `others` float32, `ints` int32; work may have any.  Raw addresses and None pass."""
+    import torch
+    device = torch.cuda.current_device() if torch.cuda.is_initialized() or torch.cuda.is_available() else -2
+    for group, want in ((typed, torch.bfloat16 if dtype == 1 else torch.float32), (others, torch.float32), (ints, torch.int32),
+                        ((work,), None)):
+        for t in group:
+            if t is None or isinstance(t, int):
+                continue
+            if t.get_device() != device:
+                raise RevffnError(f"a tensor on {t.device}, which is not the current device")
+            if want is not None and t.dtype != want:
+                raise RevffnError(f"a tensor of {t.dtype} where {want} is read")
+
+
+def _work(work):
+    """(address, bytes) of a workspace tensor or None."""
+    if work is None:
+        return None, 0
+    return work.data_ptr(), work.numel() * work.element_size()
+
+
+def revffn_op_attention_ranges(cu_q, cu_k, prefix, n_docs, causal, window, Tq, Tk, lo, hi, at=None, used=None, stream=None):
+    _check_tensors(0, (), ints=(cu_q, cu_k, prefix, lo, hi, at, used))
+    _check(load_library().revffn_op_attention_ranges(_ptr(cu_q), _ptr(cu_k), _ptr(prefix), n_docs, int(causal), window, Tq, Tk,
+                                                     _ptr(lo), _ptr(hi), _ptr(at), _ptr(used), _stream(stream)))
+
+
+def revffn_op_attention_masked_workspace(desc, backward):
+    """Bytes of scratch memory for a forward pass, or for both (0 also for a desc that the calls refuse)."""
+    return load_library().revffn_op_attention_masked_workspace(ctypes.byref(desc), int(backward))
+
+
+def revffn_op_attention_masked_fwd(desc, mask, q, k, v, o, lse, work=None, stream=None):
+    _check_tensors(desc.dtype, (q, k, v, o), (lse, desc.kept), mask.kept, work)
+    w, n = _work(work)
+    _check(load_library().revffn_op_attention_masked_fwd(ctypes.byref(desc), ctypes.byref(mask), _ptr(q), _ptr(k), _ptr(v), _ptr(o),
+                                                         _ptr(lse), w, n, _stream(stream)))
+
+
+def revffn_op_attention_masked_bwd(desc, mask, q, k, v, o, d_o, lse, dq, dk, dv, work=None, stream=None):
+    _check_tensors(desc.dtype, (q, k, v, o, d_o, dq, dk, dv), (lse, desc.kept), mask.kept, work)
+    w, n = _work(work)
+    _check(load_library().revffn_op_attention_masked_bwd(ctypes.byref(desc), ctypes.byref(mask), _ptr(q), _ptr(k), _ptr(v), _ptr(o),
+                                                         _ptr(d_o), _ptr(lse), _ptr(dq), _ptr(dk), _ptr(dv), w, n, _stream(stream)))
+
+
+def revffn_op_rotary_frequencies(rotary):
+    """Host-only: the angle per position of each pair, a float64 numpy array of dims / 2."""
+    import numpy as np
+    f = np.zeros(max(rotary.dims // 2, 1))
+    _check(load_library().revffn_op_rotary_frequencies(ctypes.byref(rotary), f.ctypes.data))
+    return f
+
+
+def revffn_op_rotary(dtype, rotary, x, y, pos, T, S, H, dh, ldx, ldy, transposed=False, stream=None):
+    _check_tensors(dtype, (x, y), ints=(pos,))
+    _check(load_library().revffn_op_rotary(dtype, ctypes.byref(rotary), _ptr(x), _ptr(y), _ptr(pos), T, S, H, dh, ldx, ldy,
+                                           int(transposed), _stream(stream)))
+
+
+def revffn_op_layernorm_workspace(rows, cols):
+    return load_library().revffn_op_layernorm_workspace(rows, cols)
+
+
+def revffn_op_layernorm_fwd(dtype, x, gain, bias, y, mean, rstd, rows, cols, ldx, ldy, eps, stream=None):
+    _check_tensors(dtype, (x, gain, bias, y), (mean, rstd))
+    _check(load_library().revffn_op_layernorm_fwd(dtype, _ptr(x), _ptr(gain), _ptr(bias), _ptr(y), _ptr(mean), _ptr(rstd), rows, cols,
+                                                  ldx, ldy, eps, _stream(stream)))
+
+
+def revffn_op_layernorm_bwd(dtype, dy, x, gain, mean, rstd, dx, dgain, dbias, rows, cols, lddy, ldx, lddx, grads_f32=False, work=None,
+                            stream=None):
+    _check_tensors(dtype, (dy, x, gain, dx) + (() if grads_f32 else (dgain, dbias)), (mean, rstd) + ((dgain, dbias) if grads_f32 else ()), work=work)
+    w, n = _work(work)
+    _check(load_library().revffn_op_layernorm_bwd(dtype, _ptr(dy), _ptr(x), _ptr(gain), _ptr(mean), _ptr(rstd), _ptr(dx), _ptr(dgain),
+                                                  _ptr(dbias), rows, cols, lddy, ldx, lddx, int(grads_f32), w, n, _stream(stream)))

@@ -342,3 +342,43 @@ int launch_attn_fwd_flash(const void* q, const void* k, const void* v, void* o, 
 int launch_attn_bwd_flash(const void* q, const void* k, const void* v, const void* o, const void* d_o,
                           const float* lse, float* dvec, void* dq, void* dk, void* dv,
                           int B, int S, int H, int dh, int causal, hipStream_t s);
+
+// ---- attention over key ranges (attn_range*.hip) ---------------------------------------------------------------
+// Query row i sees the key rows lo[i] <= j < hi[i].  q, o, d_o, dq: [Tq, H heads of dh], k, v, dk, dv: [Tk, Hkv heads of dh], row
+// strides ld*; lse, dvec: [H, Tq].  Scores: z = scale q.k, capped (cap > 0): cap tanh(z / cap), less slopes[h] |at[i] - j|.
+struct RangeAttn {
+  const void *q, *k, *v, *o, *d_o;
+  void *out, *dq, *dk, *dv;              // out: o of the forward pass
+  float *lse, *dvec;
+  const int *lo, *hi, *at, *used;
+  const float* slopes;
+  int dt, H, Hkv, G, dh, Tq, Tk;         // G = H / Hkv
+  i64 ldq, ldk, ldv, ldo;
+  float scale, cap;
+};
+void launch_attn_ranges(const int* cu_q, const int* cu_k, const int* prefix, int n_docs, int causal, int window, int Tq, int Tk,
+                        int* lo, int* hi, int* at, int* used, hipStream_t s);
+// row by row: any head width up to 512, any alignment
+void launch_range_fwd_rows(const RangeAttn& a, hipStream_t s);
+void launch_range_bwd_rows(const RangeAttn& a, hipStream_t s);
+
+// ---- rotary positions, layer norm ---------------------------------------------------------------------------
+#define ROTARY_MAX_DIMS 256
+struct RotaryArgs {
+  const void* x; void* y; const int* pos;
+  int dt, T, S, H, dh, dims, interleaved;
+  i64 ldx, ldy;
+  float mag, sign;
+  double freq[ROTARY_MAX_DIMS / 2];      // angle per position of each pair, in turns (1 = 2 pi)
+};
+void launch_rotary(const RotaryArgs& a, hipStream_t s);
+struct LayerNorm {
+  const void *x, *gain, *bias, *dy; void *y, *dx, *dgain, *dbias;
+  float *mean, *rstd, *partial;
+  int dt, rows, cols, grads_f32;
+  i64 ldx, ldy, lddy, lddx;
+  float eps;
+};
+size_t layernorm_partial_floats(int rows, int cols);
+void launch_layernorm_fwd(const LayerNorm& a, hipStream_t s);
+void launch_layernorm_bwd(const LayerNorm& a, hipStream_t s);

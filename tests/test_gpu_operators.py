@@ -1,0 +1,322 @@
+"""The operators for attention layers through the C ABI, each against float64 with bounds from the arithmetic."""
+import numpy as np
+import pytest
+import torch
+
+import operators_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+if torch.cuda.is_available():
+    import paper_2512_20920_amd as R
+
+TORCH = {"bf16": torch.bfloat16, "f32": torch.float32}
+NAN = float("nan")
+
+
+def _rand(rng, shape, dtype, scale=1.0):
+    return torch.from_numpy((scale * rng.standard_normal(shape)).astype(np.float32)).to(TORCH[dtype])
+
+
+def _np(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def _ints(a):
+    return torch.from_numpy(np.asarray(a)).to("cuda", torch.int32)
+
+
+class Attention:
+    """One call's tensors; q, k, v may be parts of wider rows, and rows past `used` hold NaN."""
+
+    def __init__(self, dtype, H, Hkv, dh, Tq, Tk, seed=0, pad=0, extra_rows=0, scale=1.0):
+        rng = np.random.default_rng(seed + 31 * Tq + 7 * Tk + dh + H)
+        self.dtype, self.H, self.Hkv, self.dh, self.Tq, self.Tk = dtype, H, Hkv, dh, Tq, Tk
+        self.rows_q, self.rows_k = Tq + extra_rows, Tk + extra_rows
+
+        def rows(n, used, heads, sc=1.0, fill=NAN):
+            wide = torch.full((n, heads * dh + pad), fill, dtype=TORCH[dtype], device="cuda")
+            wide[:used, : heads * dh] = _rand(rng, (used, heads * dh), dtype, sc).cuda()
+            return wide
+        self.q, self.k, self.v = rows(self.rows_q, Tq, H, scale), rows(self.rows_k, Tk, Hkv, scale), rows(self.rows_k, Tk, Hkv)
+        self.do = rows(self.rows_q, Tq, H)
+        self.o, self.dq = torch.full_like(self.q, NAN), torch.full_like(self.q, NAN)
+        self.dk, self.dv = torch.full_like(self.k, NAN), torch.full_like(self.v, NAN)
+        self.lse = torch.full((H, self.rows_q), NAN, dtype=torch.float32, device="cuda")
+
+    def part(self, name):
+        """[rows in use, heads, dh] of a tensor in float64."""
+        n, heads = (self.Tk, self.Hkv) if name in ("k", "v", "dk", "dv") else (self.Tq, self.H)
+        return _np(getattr(self, name)[:n, : heads * self.dh].reshape(n, heads, self.dh))
+
+    def run(self, lo, hi, at=None, mode=0, backward=True, cap=0.0, slopes=None, scale=0.0, used=False, stream=None):
+        self.slopes = None if slopes is None else torch.tensor(slopes, dtype=torch.float32, device="cuda")
+        wide = lambda t: t.stride(0)
+        self.desc = R.AttnDesc(dtype=1 if self.dtype == "bf16" else 0, kernel_mode=mode, H=self.H, Hkv=self.Hkv, dh=self.dh, Tq=self.rows_q,
+                               Tk=self.rows_k, ldq=wide(self.q), ldk=wide(self.k), ldv=wide(self.v), ldo=wide(self.o), scale=scale, softcap=cap,
+                               slopes=self.slopes)
+        full = lambda a, n: _ints(np.concatenate([a, np.zeros(n - len(a), int)]))
+        self.mask = R.AttnMask(full(lo, self.rows_q), full(hi, self.rows_q), None if at is None else full(at, self.rows_q),
+                               _ints([self.Tq, self.Tk]) if used else None)
+        n = R.revffn_op_attention_masked_workspace(self.desc, backward)
+        self.work = torch.full((max(n, 16),), 255, dtype=torch.uint8, device="cuda")        # NaN patterns throughout
+        R.revffn_op_attention_masked_fwd(self.desc, self.mask, self.q, self.k, self.v, self.o, self.lse, self.work, stream=stream)
+        if backward:
+            R.revffn_op_attention_masked_bwd(self.desc, self.mask, self.q, self.k, self.v, self.o, self.do, self.lse, self.dq, self.dk, self.dv,
+                                             self.work, stream=stream)
+        torch.cuda.synchronize()
+
+    def check(self, lo, hi, at=None, backward=True, cap=0.0, slopes=None, scale=None):
+        sl = None if slopes is None else np.asarray(slopes, np.float32).astype(np.float64)
+        want = ref.attention(self.part("q"), self.part("k"), self.part("v"), lo, hi, at, scale, cap, sl,
+                             self.part("do") if backward else None, self.dtype)
+        got = {"o": self.part("o"), "lse": _np(self.lse[:, : self.Tq])}
+        if backward:
+            got |= {"dq": self.part("dq"), "dk": self.part("dk"), "dv": self.part("dv")}
+        worst = {name: ref.outside(got[name], *want[name]) for name in got}
+        assert max(worst.values()) <= 1.0, worst
+
+
+def _slopes(H):
+    return 2.0 ** (-8.0 * (np.arange(H) + 1) / H)
+
+
+# name: heads, key heads, width, query documents, key documents (None: the same), options
+SHAPES = {
+    "one_token": (2, 2, 64, [1], None, {}),
+    "one_key_each": (4, 2, 128, [1, 1, 1], None, {}),
+    "packed": (4, 2, 128, [37, 1, 130, 64, 5, 0, 66], None, {}),
+    "packed_both_ways": (3, 3, 64, [70, 3, 150], None, dict(causal=False)),
+    "long": (2, 1, 128, [517], None, {}),
+    "window": (4, 1, 64, [300, 77], None, dict(window=33)),
+    "window_of_one": (2, 2, 64, [100], None, dict(window=1)),
+    "prefix": (2, 2, 128, [200, 90], None, dict(prefix=[77, 200])),
+    "capped": (4, 4, 64, [140, 61], None, dict(cap=5.0)),
+    "biased": (4, 2, 128, [140, 61], None, dict(bias=True)),
+    "capped_biased_prefix": (6, 2, 64, [129, 200], None, dict(cap=30.0, bias=True, prefix=[100, 0])),
+    "behind_a_cache": (4, 2, 64, [40, 7, 129], [300, 7, 500], dict(bias=True)),
+    "more_queries_than_keys": (2, 1, 64, [50, 20], [20, 20], {}),
+    "no_keys": (2, 1, 64, [20, 30], [0, 30], dict(causal=False)),
+    "width_32": (2, 1, 32, [70, 65], None, {}),
+    "width_80": (3, 1, 80, [70, 65], None, dict(cap=20.0)),
+    "width_96": (2, 2, 96, [150], None, {}),
+    "width_120": (2, 1, 120, [33, 100], None, {}),
+    "width_odd": (2, 1, 33, [40, 35], None, dict(bias=True)),
+    "width_256": (2, 1, 256, [40, 35], None, {}),
+    "width_500": (1, 1, 500, [70], None, {}),
+    "many_heads_to_one": (16, 1, 64, [65, 64], None, {}),
+}
+
+
+def _case(name):
+    H, Hkv, dh, q_lens, k_lens, opt = SHAPES[name]
+    opt = dict(opt)
+    cap, slopes = opt.pop("cap", 0.0), _slopes(H) if opt.pop("bias", False) else None
+    lo, hi, at = ref.ranges(q_lens, k_lens, **opt)
+    return H, Hkv, dh, sum(q_lens), sum(k_lens or q_lens), lo, hi, at, dict(cap=cap, slopes=slopes)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("mode", [0, 1])
+@pytest.mark.parametrize("name", list(SHAPES))
+def test_attention(name, mode, dtype):
+    H, Hkv, dh, Tq, Tk, lo, hi, at, opt = _case(name)
+    a = Attention(dtype, H, Hkv, dh, Tq, Tk)
+    a.run(lo, hi, at, mode, **opt)
+    a.check(lo, hi, at, **opt)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pad,mode", [(8, 0), (64, 0), (3, 0), (3, 1)])
+def test_attention_strides_and_rows_behind_the_last_document(pad, mode, dtype):
+    """q, k, v inside wider rows; the rows behind the last document hold NaN and their results stay as they were."""
+    H, Hkv, dh, Tq, Tk, lo, hi, at, opt = _case("packed")
+    a = Attention(dtype, H, Hkv, dh, Tq, Tk, pad=pad, extra_rows=70)
+    a.run(lo, hi, at, mode, used=True, **opt)
+    a.check(lo, hi, at, **opt)
+    for t, n, heads in ((a.o, Tq, H), (a.dq, Tq, H), (a.dk, Tk, Hkv), (a.dv, Tk, Hkv)):
+        assert torch.isnan(t[n:]).all() and torch.isnan(t[:, heads * dh:]).all()
+    assert torch.isnan(a.lse[:, Tq:]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("mode", [0, 1])
+def test_attention_any_ranges(mode, dtype):
+    """Ranges that no documents make, out of bounds ones among them, and queries that see nothing."""
+    rng = np.random.default_rng(5)
+    n, m = 203, 331
+    lo, hi = rng.integers(-50, m, n), rng.integers(0, m + 50, n)
+    lo[7], hi[7], lo[8], hi[8] = 5, 5, 2 ** 31 - 1, -2 ** 31
+    hi[64:96] = lo[64:96]                                   # a whole tile of queries without keys
+    cl, ch = np.maximum(lo, 0), np.minimum(hi, m)
+    a = Attention(dtype, 4, 2, 64, n, m)
+    a.run(lo, hi, np.arange(n), mode)
+    a.check(cl, ch)
+    none = cl >= ch
+    assert none.sum() > 32 and (a.part("o")[none] == 0).all() and (a.part("dq")[none] == 0).all()
+    assert torch.isneginf(a.lse[:, torch.from_numpy(none).cuda()]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("mode", [0, 1])
+@pytest.mark.parametrize("value", [NAN, float("inf"), float("-inf")])
+def test_attention_values_that_are_not_finite_stay_where_they_are(value, mode, dtype):
+    """One document's rows hold NaN or infinities, in each tensor by turns: the other documents' results are what they are
+    without, in every tile that two documents share."""
+    lens = [45, 30, 70, 100]
+    lo, hi, at = ref.ranges(lens)
+    inside = np.zeros(sum(lens), bool)
+    inside[45:75] = True
+    for where in ("q", "k", "v", "do"):
+        a = Attention(dtype, 2, 1, 64, sum(lens), sum(lens))
+        clean = Attention(dtype, 2, 1, 64, sum(lens), sum(lens))
+        getattr(a, where)[50] = value
+        a.run(lo, hi, at, mode)
+        clean.run(lo, hi, at, mode)
+        clean.check(lo, hi, at)
+        for name in ("o", "dq", "dk", "dv"):
+            got, want = a.part(name)[~inside], clean.part(name)[~inside]
+            # (a tile worked out again adds in another order: both are within the bounds, so at most two of them apart)
+            bound = ref.attention(clean.part("q"), clean.part("k"), clean.part("v"), lo, hi, at, do=clean.part("do"), dtype=dtype)[name][1][~inside]
+            assert ref.outside(got, want, 2 * bound) <= 1.0, (where, name)
+        row = a.part("o")[50]
+        if where in ("k", "v"):
+            assert not np.isfinite(row).all()               # and who sees it, gets it
+
+
+def test_attention_ranges():
+    for q_lens, k_lens, kw in [([3, 0, 5, 1], None, {}), ([3, 0, 5, 1], None, dict(causal=False)), ([1, 1], [700, 3], {}),
+                               ([4, 9], [2, 20], dict(prefix=[1, 30])), ([300, 9], None, dict(window=7))]:
+        n, m = sum(q_lens), sum(k_lens or q_lens)
+        lo, hi, at = ref.ranges(q_lens, k_lens, Tq=n + 5, **kw)
+        new = lambda k: torch.full((k,), -7, dtype=torch.int32, device="cuda")
+        dl, dh, da, du = new(n + 5), new(n + 5), new(n + 5), new(2)
+        cum = lambda l: _ints(np.cumsum([0] + l))
+        R.revffn_op_attention_ranges(cum(q_lens), None if k_lens is None else cum(k_lens), _ints(kw["prefix"]) if "prefix" in kw else None, len(q_lens),
+                                     kw.get("causal", True), kw.get("window", 0), n + 5, m + 9, dl, dh, da, du)
+        torch.cuda.synchronize()
+        assert dl.tolist() == list(lo) and dh.tolist() == list(hi) and du.tolist() == [n, m]
+        assert da[:n].tolist() == list(at[:n])
+    # equal documents without a table, with and without one for the keys
+    lo, hi, at = ref.ranges([4, 4, 4], [7, 7, 7])
+    dl, dh = torch.empty(12, dtype=torch.int32, device="cuda"), torch.empty(12, dtype=torch.int32, device="cuda")
+    for cu_k in (None, _ints([0, 7, 14, 21])):
+        R.revffn_op_attention_ranges(None, cu_k, None, 3, True, 0, 12, 21, dl, dh)
+        torch.cuda.synchronize()
+        assert dl.tolist() == list(lo) and dh.tolist() == list(hi)
+    # rows out of bounds in the table: everything clamped
+    R.revffn_op_attention_ranges(_ints([-3, 6, 40]), _ints([-9, 5, 2 ** 31 - 1]), None, 2, False, 0, 12, 21, dl, dh)
+    torch.cuda.synchronize()
+    assert dl.min() >= 0 and dh.max() <= 21
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+# T, H, dh, dims, extra columns in a row, scaling
+@pytest.mark.parametrize("T,H,dh,dims,extra,scaling", [(1, 1, 2, 2, 0, 0), (5, 3, 64, 64, 0, 1), (70, 20, 128, 64, 32, 2), (33, 4, 128, 128, 64, 3),
+                                                        (9, 3, 80, 20, 1, 3), (4, 2, 33, 30, 0, 0), (3, 2, 1000, 6, 3, 0), (2000, 2, 256, 256, 0, 2),
+                                                        (17, 5, 24, 24, 0, 0), (3000, 7, 20, 12, 0, 1)])
+def test_rotary(T, H, dh, dims, extra, scaling, interleaved, dtype):
+    if scaling == 2 and dims == 2:
+        scaling = 0
+    rng = np.random.default_rng(T + dh + dims)
+    r = R.Rotary(dims=dims, interleaved=interleaved, scaling=scaling, original=512, theta=10000.0, factor=4.0, few_turns=1.0, many_turns=32.0,
+                 magnitude=1.25 if scaling == 3 else 0.0)
+    freq = R.revffn_op_rotary_frequencies(r)
+    i = np.arange(dims // 2)
+    want = 10000.0 ** (-2.0 * i / dims)
+    if scaling == 1:
+        want = want / 4
+    if scaling == 2:
+        want = (10000.0 * 4.0 ** (dims / (dims - 2))) ** (-2.0 * i / dims)
+    if scaling == 3:
+        g = np.clip((512 * want / (2 * np.pi) - 1) / 31, 0, 1)
+        want = g * want + (1 - g) * want / 4
+    assert np.allclose(freq, want, rtol=1e-12, atol=0)
+    mag = 1.25 if scaling == 3 else 1.0
+    rows = _rand(rng, (T, H * dh + extra), dtype).cuda()
+    x = _np(rows[:, : H * dh]).reshape(T, H, dh)
+    pos = rng.integers(0, 1_000_000, T)
+    pos[0] = -5
+    u, w = HALF_STEP[dtype], 2.0 ** -24
+    for transposed in (False, True):
+        for p, dev in ((pos, _ints(pos)), (np.arange(T) % 7, None)):
+            y = torch.full((T, H * dh + 2 * extra), NAN, dtype=TORCH[dtype], device="cuda")
+            R.revffn_op_rotary(1 if dtype == "bf16" else 0, r, rows, y, dev, T, 7, H, dh, H * dh + extra, H * dh + 2 * extra, transposed)
+            again = rows.clone()
+            R.revffn_op_rotary(1 if dtype == "bf16" else 0, r, again, again, dev, T, 7, H, dh, H * dh + extra, H * dh + extra, transposed)
+            torch.cuda.synchronize()
+            ref_y = ref.rotary(x, p, freq, interleaved, mag, transposed)
+            # a sine or cosine is off by 2 ulp of 1, products and their sum by half a step each; both columns are at most the pair's length
+            pair = mag * np.abs(x).max(initial=0.0) * 1.5
+            got = _np(y[:, : H * dh]).reshape(T, H, dh)
+            assert ref.outside(got, ref_y, 8 * w * pair + u * np.abs(ref_y)) <= 1.0
+            assert (got[..., dims:] == x[..., dims:]).all() and torch.isnan(y[:, H * dh:]).all()
+            assert torch.equal(again[:, : H * dh], y[:, : H * dh]) and torch.equal(again[:, H * dh:], rows[:, H * dh:])
+
+
+HALF_STEP = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols,pad", [(1, 1, 0), (3, 7, 0), (5, 64, 0), (130, 500, 0), (9, 513, 0), (70, 1024, 8), (40, 1025, 3), (33, 2048, 0), (2100, 256, 0),
+                                           (21, 2056, 0), (6, 4100, 4), (7, 8192, 0), (5, 8200, 1), (3, 32768, 0), (9, 32776, 0), (3, 40001, 0)])
+@pytest.mark.parametrize("params", ["both", "none", "gain_f32"])
+def test_layernorm(rows, cols, pad, params, dtype):
+    rng = np.random.default_rng(rows + cols)
+    wide = lambda sc, shift=0.0: (_rand(rng, (rows, cols + pad), dtype, sc).cuda() + shift).to(TORCH[dtype])
+    x, dy = wide(1.5, 0.7), wide(1.0)
+    gain = None if params == "none" else (1 + 0.2 * _rand(rng, cols, "f32")).to(TORCH[dtype]).cuda()
+    bias = _rand(rng, cols, dtype).cuda() if params == "both" else None
+    new = lambda: torch.full((rows, cols + pad), NAN, dtype=TORCH[dtype], device="cuda")
+    y, dx, mean, rstd = new(), new(), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    gt = torch.float32 if params == "gain_f32" else TORCH[dtype]
+    dgain = torch.full((cols,), NAN, dtype=gt, device="cuda") if params != "none" else None
+    dbias = torch.full((cols,), NAN, dtype=gt, device="cuda") if params == "both" else None
+    work = torch.full((R.revffn_op_layernorm_workspace(rows, cols),), 255, dtype=torch.uint8, device="cuda")
+    dt, ld = (1 if dtype == "bf16" else 0), cols + pad
+    R.revffn_op_layernorm_fwd(dt, x, gain, bias, y, mean, rstd, rows, cols, ld, ld, 1e-5)
+    R.revffn_op_layernorm_bwd(dt, dy, x, gain, mean, rstd, dx, dgain, dbias, rows, cols, ld, ld, ld, params == "gain_f32", work)
+    torch.cuda.synchronize()
+    xn, dyn = _np(x[:, :cols]), _np(dy[:, :cols])
+    g, b = (None if t is None else _np(t) for t in (gain, bias))
+    ry, rm, rr, rdx, rdg, rdb = ref.layernorm(xn, g, b, 1e-5, dyn)
+    u, e = HALF_STEP[dtype], 2.0 ** -24
+    gm = 1.0 if g is None else np.abs(g)
+    # a float32 sum of n terms in any order is off by n e of the sum of their sizes; it is taken over at most 64 terms per thread and a tree behind
+    n = min(cols, 64) + 16
+    e_mean = n * e * np.abs(xn).mean(1)
+    e_r = (n + 8) * e + e_mean * rr                                       # relative, of rstd (at mean +- e_mean the variance is e_mean^2 larger)
+    xh = np.abs((xn - rm[:, None]) * rr[:, None])
+    e_xh = (e_mean * rr)[:, None] + (e_r[:, None] + 2 * e) * xh
+    assert ref.outside(_np(mean), rm, e_mean + e * np.abs(rm)) <= 1.0
+    assert ref.outside(_np(rstd), rr, e_r * rr) <= 1.0
+    assert ref.outside(_np(y[:, :cols]), ry, e_xh * gm + 2 * e * (xh * gm + (0 if b is None else np.abs(b))) + u * np.abs(ry)) <= 1.0
+    d = np.abs(dyn) * gm
+    m1, m2 = d.mean(1, keepdims=True), (d * xh).mean(1, keepdims=True)
+    e_dx = rr[:, None] * (4 * e * d + n * e * m1 + xh * ((n + 4) * e * m2 + (d * e_xh).mean(1, keepdims=True)) + e_xh * m2) + (e_r[:, None] + 4 * e) * (
+        rr[:, None] * (d + m1 + xh * m2))
+    assert ref.outside(_np(dx[:, :cols]), rdx, e_dx + u * np.abs(rdx)) <= 1.0
+    ug = 2.0 ** -24 if params == "gain_f32" else u
+    if dgain is not None:
+        assert ref.outside(_np(dgain), rdg, ((rows + 16) * e * np.abs(dyn) * xh + np.abs(dyn) * e_xh).sum(0) + ug * np.abs(rdg)) <= 1.0
+    if dbias is not None:
+        assert ref.outside(_np(dbias), rdb, (rows + 16) * e * np.abs(dyn).sum(0) + ug * np.abs(rdb)) <= 1.0
+    if pad:
+        assert torch.isnan(y[:, cols:]).all() and torch.isnan(dx[:, cols:]).all()
+    # in place: the same bits
+    x2, dy2 = x.clone(), dy.clone()
+    R.revffn_op_layernorm_bwd(dt, dy2, x2, gain, mean, rstd, dy2, None, None, rows, cols, ld, ld, ld)
+    R.revffn_op_layernorm_fwd(dt, x2, gain, bias, x2, None, None, rows, cols, ld, ld, 1e-5)
+    torch.cuda.synchronize()
+    assert torch.equal(x2[:, :cols], y[:, :cols]) and torch.equal(dy2[:, :cols], dx[:, :cols])
+
+
+def test_layernorm_without_rows():
+    t, f = torch.empty(8, device="cuda"), torch.empty(8, device="cuda")
+    g, b = torch.full((8,), NAN, device="cuda"), torch.full((8,), NAN, device="cuda")
+    work = torch.empty(R.revffn_op_layernorm_workspace(0, 8), dtype=torch.uint8, device="cuda")
+    R.revffn_op_layernorm_fwd(0, t, None, None, f, None, None, 0, 8, 8, 8, 1e-5)
+    R.revffn_op_layernorm_bwd(0, t, t, None, f, f, f, g, b, 0, 8, 8, 8, 8, False, work)
+    torch.cuda.synchronize()
+    assert (g == 0).all() and (b == 0).all()
