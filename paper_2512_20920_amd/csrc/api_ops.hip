@@ -11,11 +11,15 @@ namespace {
 // a launch's grid times its 256 threads has to stay below 2^32
 bool grid_fits(i64 workgroups) { return workgroups < ((i64)1 << 24); }
 
-struct Scratch { float* dvec; size_t bytes; };
+struct Scratch { float* dvec; void* blocks; float* sums; size_t bytes; };
 Scratch lay_out(const RangeAttn& a, bool backward, void* work) {
-  Scratch w = {nullptr, 0};
+  Scratch w = {nullptr, nullptr, nullptr, 0};
   auto take = [&](size_t n) { void* p = work ? (char*)work + w.bytes : nullptr; w.bytes += (n + 255) / 256 * 256; return p; };
-  if (backward) w.dvec = (float*)take((size_t)a.H * a.Tq * 4);
+  if (backward) {
+    w.dvec = (float*)take((size_t)a.H * a.Tq * 4);
+    w.blocks = take(((size_t)a.Tq + 63) / 64 * 16);
+    w.sums = (float*)take(range_flash_sum_floats(a) * 4);
+  }
   return w;
 }
 
@@ -97,8 +101,9 @@ int revffn_op_attention_masked_fwd(const revffn_attn_desc* desc, const revffn_at
   if (w.bytes && !work) return REVFFN_ENULL;
   if (w.bytes > work_bytes || ((uintptr_t)work & 15)) return REVFFN_EINVAL;
   a.q = q; a.k = k; a.v = v; a.out = o; a.lse = lse;
-  if (desc->kernel_mode == 2) return REVFFN_EUNSUPPORTED;
-  launch_range_fwd_rows(a, (hipStream_t)stream);
+  if (desc->kernel_mode != 1 && range_flash_takes(a, false)) launch_range_fwd_flash(a, (hipStream_t)stream);
+  else if (desc->kernel_mode == 2) return REVFFN_EUNSUPPORTED;
+  else launch_range_fwd_rows(a, (hipStream_t)stream);
   return 0;
 }
 
@@ -113,8 +118,9 @@ int revffn_op_attention_masked_bwd(const revffn_attn_desc* desc, const revffn_at
   if (w.bytes && !work) return REVFFN_ENULL;
   if (w.bytes > work_bytes || ((uintptr_t)work & 15)) return REVFFN_EINVAL;
   a.q = q; a.k = k; a.v = v; a.o = o; a.d_o = d_o; a.lse = (float*)lse; a.dq = dq; a.dk = dk; a.dv = dv; a.dvec = w.dvec;
-  if (desc->kernel_mode == 2) return REVFFN_EUNSUPPORTED;
-  launch_range_bwd_rows(a, (hipStream_t)stream);
+  if (desc->kernel_mode != 1 && range_flash_takes(a, true)) launch_range_bwd_flash(a, w.blocks, w.sums, (hipStream_t)stream);
+  else if (desc->kernel_mode == 2) return REVFFN_EUNSUPPORTED;
+  else launch_range_bwd_rows(a, (hipStream_t)stream);
   return 0;
 }
 

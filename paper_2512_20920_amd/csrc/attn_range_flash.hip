@@ -1,0 +1,642 @@
+// Attention over key ranges on the matrix cores: bf16, heads of up to 128 columns (a multiple of 8).
+#include "attn_range_tiles.h"
+
+// Which tile a workgroup takes (1-D grid of tiles x heads).  Heads are the fastest index, and those that share a key head follow each
+// other 8 apart where there are 8 key heads or more, so that they run on the same XCD (id & 7) and find its keys in that L2.
+__device__ __forceinline__ void place(const RangeAttn& a, int* tile, int* h) {
+  const int row = (int)blockIdx.x / a.H, r = (int)blockIdx.x - row * a.H;
+  *tile = row;
+  *h = (r % a.Hkv) * a.G + r / a.Hkv;
+}
+
+// The key ranges of 128 queries, as every wave of a workgroup sees them: its own lane's query, all queries' (two per lane)
+struct QueryRanges {
+  int2 r0, r1;             // of queries q0 + lane, q0 + 64 + lane (none: lo = INT_MAX, hi = 0)
+  int first, end;          // over all of them
+  // where the first tile of 64 keys starts, at or after kv, that some query sees; `end`: there is none
+  __device__ __forceinline__ int live_from(int kv) const {
+    if (kv >= end) return end;
+    if (__any((r0.x < kv + 64 && r0.y > kv) || (r1.x < kv + 64 && r1.y > kv))) return kv;
+    const int a = r0.y > kv ? r0.x : INT_MAX, b = r1.y > kv ? r1.x : INT_MAX;
+    return min(wave_imin(min(a, b)), end);
+  }
+};
+__device__ __forceinline__ QueryRanges query_ranges(const RangeAttn& a, int q0, int rows, int keys, int lane) {
+  QueryRanges q;
+  const int2 none = make_int2(INT_MAX, 0);
+  q.r0 = q0 + lane < rows ? key_range(a, q0 + lane, keys) : none;
+  q.r1 = q0 + 64 + lane < rows ? key_range(a, q0 + 64 + lane, keys) : none;
+  if (q.r0.x == q.r0.y) q.r0 = none;
+  if (q.r1.x == q.r1.y) q.r1 = none;
+  q.first = wave_imin(min(q.r0.x, q.r1.x));
+  q.end = wave_imax(max(q.r0.y, q.r1.y));
+  return q;
+}
+
+// ------------------------------------------------------------------------------------
+// Forward.  Workgroup = 128 queries of one head, wave = 32 queries; keys and values streamed in tiles of 64 from the first key
+// that some query sees to the last, tiles that none sees left out; K two tiles ahead and V one.  An iteration is two phases with a
+// barrier behind each: in the first a wave takes the maximum and half of the exponentials and reads the next tile's key
+// fragments, in the second it multiplies those and P V of this tile, with the other half of the exponentials between.
+// ------------------------------------------------------------------------------------
+template <int DHP, bool MOD>
+__global__ void __launch_bounds__(256, 2) range_fwd_k(RangeAttn a) {
+  typedef Tiles<DHP> T;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem_raw[];      // K, V, K, V
+  int qt, h;
+  place(a, &qt, &h);
+  qt = (a.Tq + 127) / 128 - 1 - qt;                 // late query tiles tend to be the long ones
+  const int rows = rows_in_use(a), keys = keys_in_use(a), q0 = qt * 128;
+  if (q0 >= rows) return;
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
+  const int myq = q0 + wv * 32 + (lane & 31), kh = h / a.G;
+  const QueryRanges qr = query_ranges(a, q0, rows, keys, lane);
+  const int2 mine = myq < rows ? key_range(a, myq, keys) : make_int2(INT_MIN, INT_MAX);    // (a row that is not there needs no mask)
+  const int all_from = wave_imax(mine.x), all_to = wave_imin(mine.y);                      // every query sees the keys between
+  const ScoreForm sf = score_form(a, h);
+  const int at = MOD && sf.biased ? (a.at ? a.at[min(myq, rows - 1)] : myq) : 0;
+  bf16* o = (bf16*)a.out + (i64)myq * a.ldo + (i64)h * a.dh;
+
+  bf16x8 qf[T::KK];
+  T::load_frags((const bf16*)a.q + (i64)myq * a.ldq + (i64)h * a.dh, myq < rows, a.dh, g, qf);
+  const HeadRows rk = {(const unsigned char*)a.k + (i64)kh * a.dh * 2, a.ldk * 2, a.dh * 2}, rv = {(const unsigned char*)a.v + (i64)kh * a.dh * 2, a.ldv * 2, a.dh * 2};
+  const unsigned lds0 = lds_address(smem_raw) + (unsigned)wv * (T::BYTES / 4);
+  auto issue = [&](const HeadRows& r, int kv, unsigned stage) {             // 16 of the tile's rows
+    T::load16(rows_buffer(r, kv, min(64, qr.end - kv)), (unsigned)r.ldb, r.width, wv * 16, lds0 + stage * T::BYTES, lane);
+  };
+  const unsigned rbase = T::row_base(lane), cbase = T::col_base(lane);
+  f32x16 oacc[T::DT] = {}, s[2];
+  bf16x8 kf[2 * T::KK], pf[4];
+  float m = -INFINITY, l = 0.f;
+  bool partly = false;                              // some tile was not seen whole: what the rest of it holds was multiplied by zero
+  auto read_k = [&](unsigned stage, int from) {     // half of K of a tile
+    const unsigned char* cK = smem_raw + stage * T::BYTES;
+#pragma unroll
+    for (int kk = from; kk < from + T::KK / 2; kk++)
+#pragma unroll
+      for (int j = 0; j < 2; j++) kf[kk * 2 + j] = *(const bf16x8*)(cK + j * 32 * T::ROW + (rbase ^ (unsigned)(kk * 32)));
+  };
+  auto times_q = [&]() {
+    s[0] = f32x16{};
+    s[1] = f32x16{};
+#pragma unroll
+    for (int kk = 0; kk < T::KK; kk++)
+#pragma unroll
+      for (int j = 0; j < 2; j++) s[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk * 2 + j], qf[kk], s[j], 0, 0, 0);
+  };
+  // scores to their final form in units of log2 (MOD), and those of keys that are not seen to -infinity
+  auto finish = [&](int kv) {
+    if constexpr (MOD) {
+      const float d0 = (float)((i64)at - kv - g * 4);
+#pragma unroll
+      for (int j = 0; j < 2; j++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) {
+          float x = sf.capped ? fast_tanh_2(s[j][e] * sf.x2) * sf.cap2 : s[j][e] * sf.f;
+          if (sf.biased) x = fmaf(-sf.slope2, fabsf(d0 - (float)(j * 32 + (e >> 2) * 8 + (e & 3))), x);
+          s[j][e] = x;
+        }
+    }
+    if (kv < all_from || kv + 64 > all_to) {
+      partly = true;
+      const int lo = max(mine.x, kv) - kv - g * 4;
+      const unsigned n = (unsigned)max(min(mine.y, kv + 64) - max(mine.x, kv), 0);
+#pragma unroll
+      for (int j = 0; j < 2; j++)
+#pragma unroll
+        for (int e = 0; e < 16; e++)
+          if ((unsigned)(j * 32 + (e >> 2) * 8 + (e & 3) - lo) >= n) s[j][e] = -INFINITY;
+    }
+  };
+  const float unit = MOD ? 1.f : sf.f;              // (without MOD the scale is positive and goes into the exponential)
+  float ms = 0.f;
+  auto exponentials = [&](f32x16 x, int half) {
+    float rs[2] = {};
+#pragma unroll
+    for (int e = 0; e < 16; e++) {
+      x[e] = fast_exp2(MOD ? x[e] - ms : fmaf(x[e], unit, -ms));
+      rs[e & 1] += x[e];
+    }
+    l += rs[0] + rs[1];
+    pf[half * 2] = acc_to_frag(x, 0);
+    pf[half * 2 + 1] = acc_to_frag(x, 1);
+  };
+  if (qr.first < qr.end) {
+    int kv = qr.first, kv1 = qr.live_from(kv + 64), kv2;                    // this tile, the next one, the one after
+    issue(rk, kv, 0); issue(rk, kv1, 2); issue(rv, kv, 1);
+    T::arrived(qf);
+    wait_vmcnt<2 * T::LOADS>();                     // the first keys
+    phase_end();
+    read_k(0, 0);
+    read_k(0, T::KK / 2);
+    times_q();
+    wait_vmcnt<T::LOADS>();                         // K of the next tile is there, V of this one may be on its way
+    phase_end();
+    // the keys read in the phase before and the values just read make room
+    auto softmax = [&](unsigned st) {
+      kv2 = qr.live_from(kv1 + 64);
+      issue(rk, kv2, st);
+      issue(rv, kv1, st ^ 2u ^ 1u);
+      read_k(st ^ 2u, 0);
+      finish(kv);
+      float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int e = 0; e < 32; e += 2) mx[(e >> 1) & 3] = fmaxf(fmaxf(mx[(e >> 1) & 3], s[e >> 4][e & 15]), s[e >> 4][(e & 15) + 1]);
+      const float mn = fmaxf(m, both_halves_max(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]))) * unit);
+      if (__any(mn > m)) {                          // the accumulator is rescaled only when some query of the wave has raised its maximum
+        const float alpha = fast_exp2(m - (mn == -INFINITY ? 0.f : mn));
+        l *= alpha;
+#pragma unroll
+        for (int d = 0; d < T::DT; d++) oacc[d] *= alpha;
+        m = mn;
+      }
+      read_k(st ^ 2u, T::KK / 2);
+      ms = m == -INFINITY ? 0.f : m;
+      exponentials(s[0], 0);
+      wait_vmcnt<2 * T::LOADS>();                   // V of this tile is there
+      phase_end();
+    };
+    unsigned st = 0;
+    while (kv1 < qr.end) {
+      softmax(st);
+      __builtin_amdgcn_s_setprio(1);
+      const f32x16 rest = s[1];
+      const unsigned char* cV = smem_raw + (st + 1) * T::BYTES;
+      bf16x8 vf[T::DT];
+      times_q();
+      exponentials(rest, 1);
+      T::read_cols(vf, cV, cbase, 0);
+      if constexpr (DHP == 128) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+#pragma unroll
+        for (int j = 0; j < 14; j++) {
+          __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
+          if (j >= 6) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      T::template cols_times<64>(oacc, cV, cbase, pf, vf);                  // O^T[dh, q] += V^T[dh, kv] P^T[kv, q]
+      __builtin_amdgcn_s_setprio(0);
+      wait_vmcnt<T::LOADS>();                       // K of the tile after the next is there
+      phase_end();
+      st ^= 2u;
+      kv = kv1;
+      kv1 = kv2;
+    }
+    softmax(st);
+    exponentials(s[1], 1);
+    const unsigned char* cV = smem_raw + (st + 1) * T::BYTES;
+    bf16x8 vf[T::DT];
+    T::read_cols(vf, cV, cbase, 0);
+    T::template cols_times<64>(oacc, cV, cbase, pf, vf);
+    wait_vmcnt<0>();                                // the zero-filled loads past the last tile
+    phase_end();
+  }
+  if (partly && !T::finite(oacc)) {                 // a value that is not finite: seen, or only in a tile with seen ones?
+    for (int r = 0; r < 32 && q0 + wv * 32 + r < rows; r++) range_row_fwd<bf16>(a, q0 + wv * 32 + r, h, keys, (float*)smem_raw + wv * 2 * DHP);
+    return;
+  }
+  l = both_halves_sum(l);
+  if (myq < rows) {
+    T::store(o, oacc, l == 0.f ? 0.f : 1.0f / l, a.dh, g);
+    if (g == 0 && a.lse) a.lse[(i64)h * a.Tq + myq] = l == 0.f ? -INFINITY : (m + __log2f(l)) * LN2;
+  }
+}
+
+// ------------------------------------------------------------------------------------
+// Backward, part 1: dQ, D = <o, dO> of the rows, and per block of 64 queries which keys some and all of them see, for part 2.
+//   S^T = K Q^T,  P^T = exp(S^T - lse),  dP^T = V dO^T,  dS^T = P^T (dP^T - D),  dQ^T += K^T dS^T,  times scale at the end.
+// The forward kernel's tiles and phases; the keys of a tile are read once more in the phase after, so they have three stages.
+// ------------------------------------------------------------------------------------
+// block of 64 queries: the first key that some query sees and one past the last (none: INT_MAX, 0), and between which keys all see
+typedef int4 BlockSeen;
+
+template <int DHP, bool MOD>
+__global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen* __restrict__ blocks) {
+  typedef Tiles<DHP> T;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem_raw[];      // K, K, K, V, V
+  int qt, h;
+  place(a, &qt, &h);
+  qt = (a.Tq + 127) / 128 - 1 - qt;
+  const int rows = rows_in_use(a), keys = keys_in_use(a), q0 = qt * 128;
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
+  const QueryRanges qr = query_ranges(a, q0, rows, keys, lane);
+  if (h == 0 && wv < 2) {                           // (a row in use that sees nothing leaves no key that all see)
+    const int2 r = wv ? qr.r1 : qr.r0;
+    const bool in = q0 + wv * 64 + lane < rows, sees = r.x < r.y;
+    const int4 b = make_int4(wave_imin(r.x), wave_imax(r.y), wave_imax(sees ? r.x : in ? INT_MAX : INT_MIN), wave_imin(sees ? r.y : in ? 0 : INT_MAX));
+    if (lane == 0 && q0 + wv * 64 < a.Tq) blocks[qt * 2 + wv] = b;
+  }
+  if (q0 >= rows) return;
+  const int myq = q0 + wv * 32 + (lane & 31), kh = h / a.G;
+  const int2 mine = myq < rows ? key_range(a, myq, keys) : make_int2(INT_MIN, INT_MAX);
+  const int all_from = wave_imax(mine.x), all_to = wave_imin(mine.y);
+  const ScoreForm sf = score_form(a, h);
+  const int at = MOD && sf.biased ? (a.at ? a.at[min(myq, rows - 1)] : myq) : 0;
+
+  bf16x8 qf[T::KK], dof[T::KK];
+  T::load_frags((const bf16*)a.q + (i64)myq * a.ldq + (i64)h * a.dh, myq < rows, a.dh, g, qf);
+  T::load_frags((const bf16*)a.d_o + (i64)myq * a.ldo + (i64)h * a.dh, myq < rows, a.dh, g, dof);
+  float mylse = myq < rows ? a.lse[(i64)h * a.Tq + myq] * LOG2E : 0.f;
+  if (mylse == -INFINITY) mylse = 0.f;              // (sees nothing: every score is -infinity)
+  float myD = 0.f;
+  {
+    bf16x8 of[T::KK];
+    T::load_frags((const bf16*)a.o + (i64)myq * a.ldo + (i64)h * a.dh, myq < rows, a.dh, g, of);
+#pragma unroll
+    for (int kk = 0; kk < T::KK; kk++)
+#pragma unroll
+      for (int u = 0; u < 8; u++) myD = fmaf((float)of[kk][u], (float)dof[kk][u], myD);
+    myD = both_halves_sum(myD);
+    if (g == 0 && myq < rows) a.dvec[(i64)h * a.Tq + myq] = myD;
+  }
+  if (mine.x == mine.y) myD = 0.f;
+  const HeadRows rk = {(const unsigned char*)a.k + (i64)kh * a.dh * 2, a.ldk * 2, a.dh * 2}, rv = {(const unsigned char*)a.v + (i64)kh * a.dh * 2, a.ldv * 2, a.dh * 2};
+  const unsigned lds0 = lds_address(smem_raw) + (unsigned)wv * (T::BYTES / 4);
+  auto issue = [&](const HeadRows& r, int kv, unsigned stage) {
+    T::load16(rows_buffer(r, kv, min(64, qr.end - kv)), (unsigned)r.ldb, r.width, wv * 16, lds0 + stage * T::BYTES, lane);
+  };
+  const unsigned rbase = T::row_base(lane), cbase = T::col_base(lane);
+  f32x16 acc[T::DT] = {}, s[2], dp[2];
+  bf16x8 dsf[4], first[T::DT];
+  bf16x8 fr[2][4];
+  bool partly = false;
+  auto read_kv = [&](bf16x8 (&f)[4], unsigned sk, unsigned sv, int kk) {
+    const unsigned char *cK = smem_raw + sk * T::BYTES, *cV = smem_raw + sv * T::BYTES;
+    const unsigned w = rbase ^ (unsigned)(kk * 32);
+    f[0] = *(const bf16x8*)(cK + w);
+    f[1] = *(const bf16x8*)(cV + w);
+    f[2] = *(const bf16x8*)(cK + 32 * T::ROW + w);
+    f[3] = *(const bf16x8*)(cV + 32 * T::ROW + w);
+  };
+  auto times_q = [&](unsigned sk, unsigned sv) {    // (after read_kv(fr[0], .., 0))
+#pragma unroll
+    for (int j = 0; j < 2; j++) { s[j] = f32x16{}; dp[j] = f32x16{}; }
+#pragma unroll
+    for (int kk = 0; kk < T::KK; kk++) {
+      if (kk < T::KK - 1) read_kv(fr[(kk + 1) & 1], sk, sv, kk + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < 2; j++) {
+        s[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[kk & 1][j * 2], qf[kk], s[j], 0, 0, 0);
+        dp[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[kk & 1][j * 2 + 1], dof[kk], dp[j], 0, 0, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  auto gradients = [&](int kv) {                    // dS in place of S
+    const float d0 = (float)((i64)at - kv - g * 4);
+#pragma unroll
+    for (int j = 0; j < 2; j++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) {
+        float x, keep = 1.f;
+        if constexpr (MOD) {
+          x = s[j][e] * sf.f;
+          if (sf.capped) {
+            const float t = fast_tanh_2(s[j][e] * sf.x2);
+            x = t * sf.cap2;
+            keep = 1.f - t * t;
+          }
+          if (sf.biased) x = fmaf(-sf.slope2, fabsf(d0 - (float)(j * 32 + (e >> 2) * 8 + (e & 3))), x);
+          x -= mylse;
+        } else x = fmaf(s[j][e], sf.f, -mylse);
+        s[j][e] = fast_exp2(x) * (dp[j][e] - myD) * keep;
+      }
+    if (kv < all_from || kv + 64 > all_to) {
+      partly = true;
+      const int lo = max(mine.x, kv) - kv - g * 4;
+      const unsigned n = (unsigned)max(min(mine.y, kv + 64) - max(mine.x, kv), 0);
+#pragma unroll
+      for (int j = 0; j < 2; j++)
+#pragma unroll
+        for (int e = 0; e < 16; e++)
+          if ((unsigned)(j * 32 + (e >> 2) * 8 + (e & 3) - lo) >= n) s[j][e] = 0.f;
+    }
+#pragma unroll
+    for (int c = 0; c < 4; c++) dsf[c] = acc_to_frag(s[c >> 1], c & 1);
+  };
+  if (qr.first < qr.end) {
+    int kv = qr.first, kv1 = qr.live_from(kv + 64), kv2;
+    issue(rk, kv, 0); issue(rv, kv, 3); issue(rk, kv1, 1); issue(rv, kv1, 4);
+    T::arrived(qf);
+    T::arrived(dof);
+    asm volatile("" : "+v"(mylse), "+v"(myD));
+    wait_vmcnt<2 * T::LOADS>();
+    phase_end();
+    unsigned before = 2, now = 0, sv = 3;           // places of K of the last tile and this one, of V of this one
+    read_kv(fr[0], 0, 3, 0);
+    times_q(0, 3);
+    phase_end();
+    // the values just read and the keys read for the second time make room
+    auto probabilities = [&]() {
+      kv2 = qr.live_from(kv1 + 64);
+      issue(rk, kv2, before);
+      issue(rv, kv2, sv);
+      gradients(kv);
+      T::read_cols(first, smem_raw + now * T::BYTES, cbase, 0);
+      const unsigned next = 3u - before - now;
+      before = now;
+      now = next;
+      sv = 7u - sv;
+      wait_vmcnt<2 * T::LOADS>();                   // K and V of the next tile are there
+      phase_end();
+    };
+    while (kv1 < qr.end) {
+      probabilities();
+      __builtin_amdgcn_s_setprio(1);
+      read_kv(fr[0], now, sv, 0);
+      T::template cols_times<64>(acc, smem_raw + before * T::BYTES, cbase, dsf, first);
+      times_q(now, sv);
+      __builtin_amdgcn_s_setprio(0);
+      phase_end();
+      kv = kv1;
+      kv1 = kv2;
+    }
+    probabilities();
+    T::template cols_times<64>(acc, smem_raw + before * T::BYTES, cbase, dsf, first);
+    wait_vmcnt<0>();                                // the zero-filled loads past the last tile
+    phase_end();
+  }
+  if (partly && !T::finite(acc)) {
+    for (int r = 0; r < 32 && q0 + wv * 32 + r < rows; r++) range_row_dq<bf16>(a, q0 + wv * 32 + r, h, keys, (float*)smem_raw + wv * 2 * DHP);
+    return;
+  }
+  if (myq < rows) T::store((bf16*)a.dq + (i64)myq * a.ldq + (i64)h * a.dh, acc, a.scale, a.dh, g);
+}
+
+// ------------------------------------------------------------------------------------
+// Backward, part 2: dK and dV.  Workgroup = 128 keys of one key head, wave = 32 keys (one per lane column).  It goes over the blocks of
+// 64 queries that see some of its keys, and in each over the query heads that share the key head:
+//   S = Q K^T,  P = exp(S - lse),  dP = dO V^T,  dS = P (dP - D),  dV^T += dO^T P,  dK^T += Q^T dS, times scale at the end.
+// parts > 1: workgroup `part` of a tile takes every parts-th of those (block, head) pairs and leaves its sums in float32 for the
+// kernel below.
+// ------------------------------------------------------------------------------------
+template <int DHP> constexpr unsigned DKV_STAGE = 2 * Tiles<DHP>::BYTES + 5 * 256;      // Q, dO, lse, D, lo, hi, at
+template <int DHP, bool MOD>
+__global__ void __launch_bounds__(256, 2) range_bwd_dkv_k(RangeAttn a, const BlockSeen* __restrict__ blocks, float* __restrict__ sums, int parts) {
+  typedef Tiles<DHP> T;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem_raw[];      // 2 stages
+  const int per = a.Hkv * parts, kt = (int)blockIdx.x / per, r0 = (int)blockIdx.x - kt * per, kh = r0 % a.Hkv, part = r0 / a.Hkv;
+  const int rows = rows_in_use(a), keys = keys_in_use(a), k0 = kt * 128;
+  if (k0 >= keys) return;
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
+  const int kw = k0 + wv * 32, mykv = kw + (lane & 31);
+
+  bf16x8 kf[T::KK], vf[T::KK];
+  T::load_frags((const bf16*)a.k + (i64)mykv * a.ldk + (i64)kh * a.dh, mykv < keys, a.dh, g, kf);
+  T::load_frags((const bf16*)a.v + (i64)mykv * a.ldv + (i64)kh * a.dh, mykv < keys, a.dh, g, vf);
+  // blocks that see some of the workgroup's keys, from the first to the last
+  const int nb = (rows + 63) / 64;
+  const int2* seen2 = (const int2*)blocks;
+  int b0 = INT_MAX, b1 = -1;
+#pragma unroll 4
+  for (int b = lane; b < nb; b += 64) {
+    const int2 t = seen2[2 * (i64)b];
+    if (t.x < k0 + 128 && t.y > k0) { b0 = min(b0, b); b1 = b; }
+  }
+  b0 = wave_imin(b0);
+  b1 = wave_imax(b1);
+  unsigned long long live = 0;
+  int base = b0 - 64, pair = -1, blk = -1, hg = a.G - 1;
+  auto next = [&]() {                               // the next (block, head) of this part; blk = -1: none
+    do {
+      if (++hg == a.G) {
+        hg = 0;
+        while (!live) {
+          base += 64;
+          if (base > b1 || b1 < 0) { blk = -1; return; }
+          const int b = base + lane;
+          const int2 t = b <= b1 ? seen2[2 * (i64)b] : make_int2(INT_MAX, 0);
+          live = __ballot(t.x < k0 + 128 && t.y > k0);
+        }
+        blk = base + __builtin_ctzll(live);
+        live &= live - 1;
+      }
+      pair++;
+    } while (pair % parts != part);
+  };
+  f32x16 dkacc[T::DT] = {}, dvacc[T::DT] = {};
+  const unsigned lds0 = lds_address(smem_raw);
+  auto issue = [&](int b, int head, int stage) {
+    const unsigned dst = lds0 + (unsigned)stage * DKV_STAGE<DHP>;
+    const int h = kh * a.G + head, n = min(64, rows - b * 64);
+    const HeadRows rq = {(const unsigned char*)a.q + (i64)h * a.dh * 2, a.ldq * 2, a.dh * 2}, ro = {(const unsigned char*)a.d_o + (i64)h * a.dh * 2, a.ldo * 2, a.dh * 2};
+    T::load16(rows_buffer(rq, b * 64, n), (unsigned)rq.ldb, rq.width, wv * 16, dst + wv * (T::BYTES / 4), lane);
+    T::load16(rows_buffer(ro, b * 64, n), (unsigned)ro.ldb, ro.width, wv * 16, dst + T::BYTES + wv * (T::BYTES / 4), lane);
+    const unsigned words = dst + 2 * T::BYTES, off = (unsigned)lane * 4u;
+    if (wv == 0) load_lds_b32(words_buffer(a.lse + (i64)h * a.Tq, b * 64, n), words, off);
+    if (wv == 1) load_lds_b32(words_buffer(a.dvec + (i64)h * a.Tq, b * 64, n), words + 256u, off);
+    if (wv == 2) load_lds_b32(words_buffer(a.lo, b * 64, n), words + 512u, off);
+    if (wv == 3) load_lds_b32(words_buffer(a.hi, b * 64, n), words + 768u, off);
+    if (MOD && wv == 0 && a.slopes && a.at) load_lds_b32(words_buffer(a.at, b * 64, n), words + 1024u, off);
+  };
+  const unsigned rbase = T::row_base(lane), cbase = T::col_base(lane);
+  bool partly = false;
+  next();
+  if (blk >= 0) issue(blk, hg, 0);
+  T::arrived(kf);
+  T::arrived(vf);
+  wait_vmcnt<0>();
+  __syncthreads();
+  int cur = 0;
+  while (blk >= 0) {
+    const int b = blk, h = kh * a.G + hg;
+    const int4 seen = blocks[b];
+    next();
+    if (blk >= 0) issue(blk, hg, cur ^ 1);
+    if (seen.x < kw + 32 && seen.y > kw) {          // some query of the block sees some key of this wave
+      const bool whole = seen.z <= kw && seen.w >= kw + 32;
+      if (!whole) partly = true;
+      const ScoreForm sf = score_form(a, h);
+      const unsigned char *cQ = smem_raw + cur * DKV_STAGE<DHP>, *cO = cQ + T::BYTES;
+      const float *cL = (const float*)(cO + T::BYTES), *cD = cL + 64;
+      const int *cLo = (const int*)(cD + 64), *cHi = cLo + 64, *cAt = cHi + 64;
+#pragma unroll 1
+      for (int j = 0; j < 2; j++) {
+        unsigned rb = rbase + (unsigned)(j * 32 * T::ROW), cb = cbase;
+        asm volatile("" : "+v"(rb), "+v"(cb));
+        f32x16 s = {}, dp = {};
+        bf16x8 f[2][2];
+        auto read_rows = [&](bf16x8 (&x)[2], int kk) {
+          x[0] = *(const bf16x8*)(cQ + (rb ^ (unsigned)(kk * 32)));
+          x[1] = *(const bf16x8*)(cO + (rb ^ (unsigned)(kk * 32)));
+        };
+        read_rows(f[0], 0);
+#pragma unroll
+        for (int kk = 0; kk < T::KK; kk++) {
+          if (kk < T::KK - 1) read_rows(f[(kk + 1) & 1], kk + 1);
+          __builtin_amdgcn_sched_barrier(0);
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[kk & 1][0], kf[kk], s, 0, 0, 0);
+          dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[kk & 1][1], vf[kk], dp, 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        // element e is query j * 32 + (e >> 2) * 8 + g * 4 + (e & 3) of the block
+#pragma unroll
+        for (int eb = 0; eb < 4; eb++) {
+          const int q4 = j * 32 + eb * 8 + g * 4;
+          const float4 l4 = *(const float4*)(cL + q4), d4 = *(const float4*)(cD + q4);
+          const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, dv[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+          for (int i = 0; i < 4; i++) {
+            const int e = eb * 4 + i;
+            float x, keep = 1.f;
+            if constexpr (MOD) {
+              x = s[e] * sf.f;
+              if (sf.capped) {
+                const float t = fast_tanh_2(s[e] * sf.x2);
+                x = t * sf.cap2;
+                keep = 1.f - t * t;
+              }
+              if (sf.biased) x = fmaf(-sf.slope2, fabsf((float)((i64)(a.at ? cAt[q4 + i] : b * 64 + q4 + i) - mykv)), x);
+              x = fmaf(lv[i], -LOG2E, x);
+            } else x = fmaf(s[e], sf.f, -lv[i] * LOG2E);
+            s[e] = fast_exp2(x);
+            dp[e] = s[e] * (dp[e] - dv[i]) * keep;
+          }
+        }
+        if (!whole) {
+#pragma unroll
+          for (int eb = 0; eb < 4; eb++) {
+            const int q4 = j * 32 + eb * 8 + g * 4;
+            const int4 l4 = *(const int4*)(cLo + q4), h4 = *(const int4*)(cHi + q4);
+            const int lo[4] = {l4.x, l4.y, l4.z, l4.w}, hi[4] = {h4.x, h4.y, h4.z, h4.w};
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+              if (mykv < lo[i] || mykv >= hi[i]) s[eb * 4 + i] = dp[eb * 4 + i] = 0.f;
+          }
+        }
+        bf16x8 pf[2], dsf[2];
+#pragma unroll
+        for (int c = 0; c < 2; c++) { pf[c] = acc_to_frag(s, c); dsf[c] = acc_to_frag(dp, c); }
+        // dO^T P and Q^T dS by turns, 16 queries each, the next fragments read while these are multiplied
+        bf16x8 x[2][T::DT];
+        T::read_cols(x[0], cO + j * 32 * T::ROW, cb, 0);
+#pragma unroll
+        for (int c = 0; c < 4; c++) {
+          if (c < 3) T::read_cols(x[(c + 1) & 1], (c & 1 ? cO : cQ) + j * 32 * T::ROW, cb, (c + 1) >> 1);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int d = 0; d < T::DT; d++) {
+            if (c & 1) dkacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[c & 1][d], dsf[c >> 1], dkacc[d], 0, 0, 0);
+            else dvacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[c & 1][d], pf[c >> 1], dvacc[d], 0, 0, 0);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+    // this wave's part of the next tile has landed, and its reads of this one have returned
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __syncthreads();
+    cur ^= 1;
+  }
+  if (parts > 1) {
+    if (mykv >= keys) return;
+    float* out = sums + ((((i64)part * 2) * a.Tk + mykv) * a.Hkv + kh) * DHP;
+    const i64 dv = (i64)a.Tk * a.Hkv * DHP;
+#pragma unroll
+    for (int d = 0; d < T::DT; d++)
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        const int c = d * 32 + e * 8 + g * 4;
+        *(float4*)(out + c) = make_float4(dkacc[d][e * 4], dkacc[d][e * 4 + 1], dkacc[d][e * 4 + 2], dkacc[d][e * 4 + 3]);
+        *(float4*)(out + dv + c) = make_float4(dvacc[d][e * 4], dvacc[d][e * 4 + 1], dvacc[d][e * 4 + 2], dvacc[d][e * 4 + 3]);
+      }
+    return;
+  }
+  if (partly && (!T::finite(dkacc) || !T::finite(dvacc))) {
+    for (int r = 0; r < 32 && kw + r < keys; r++) range_row_dkv<bf16>(a, kw + r, kh, rows, keys, (float*)smem_raw + wv * 2 * DHP);
+    return;
+  }
+  if (mykv < keys) {
+    T::store((bf16*)a.dk + (i64)mykv * a.ldk + (i64)kh * a.dh, dkacc, a.scale, a.dh, g);
+    T::store((bf16*)a.dv + (i64)mykv * a.ldv + (i64)kh * a.dh, dvacc, 1.0f, a.dh, g);
+  }
+}
+// the sum of the parts, one wave per key row and head: 2 columns per lane (DHP = 64: one)
+template <int DHP> __global__ void __launch_bounds__(256) range_dkv_sum_k(RangeAttn a, const float* __restrict__ sums, int parts) {
+  __shared__ float lds[4][2 * DHP];
+  constexpr int C = DHP / 64;
+  const int rows = rows_in_use(a), keys = keys_in_use(a), lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const i64 n = (i64)blockIdx.x * 4 + wv;
+  const int j = (int)(n / a.Hkv), kh = (int)(n - (i64)j * a.Hkv);
+  if (j >= keys) return;
+  float k[C] = {}, v[C] = {};
+  const i64 half = (i64)a.Tk * a.Hkv * DHP;
+  const float* p = sums + n * DHP + lane * C;
+#pragma unroll 4
+  for (int i = 0; i < parts; i++)
+#pragma unroll
+    for (int c = 0; c < C; c++) { k[c] += p[(i64)i * 2 * half + c]; v[c] += p[(i64)i * 2 * half + half + c]; }
+  float z = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; c++) z = __builtin_fmaf(k[c], 0.f, __builtin_fmaf(v[c], 0.f, z));
+  if (!__all(z == 0.f)) {                           // a value that is not finite: seen, or only in a tile with seen ones?
+    range_row_dkv<bf16>(a, j, kh, rows, keys, lds[wv]);
+    return;
+  }
+  bf16 *dk = (bf16*)a.dk + (i64)j * a.ldk + (i64)kh * a.dh, *dv = (bf16*)a.dv + (i64)j * a.ldv + (i64)kh * a.dh;
+#pragma unroll
+  for (int c = 0; c < C; c++)
+    if (lane * C + c < a.dh) { dk[lane * C + c] = (bf16)(k[c] * a.scale); dv[lane * C + c] = (bf16)v[c]; }
+}
+
+// ---- launchers ----
+static bool takes(const RangeAttn& a, bool back) {
+  if (a.dt != 1 || a.dh > 128 || a.dh % 8) return false;
+  uintptr_t p = (uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v;
+  p |= back ? (uintptr_t)a.o | (uintptr_t)a.d_o | (uintptr_t)a.dq | (uintptr_t)a.dk | (uintptr_t)a.dv : (uintptr_t)a.out;
+  const i64 l = a.ldq | a.ldk | a.ldv | a.ldo;
+  // 64 rows of a tile are addressed with 31-bit byte offsets
+  return !(p & 15) && !(l & 7) && a.ldq < (1 << 24) && a.ldk < (1 << 24) && a.ldv < (1 << 24) && a.ldo < (1 << 24);
+}
+bool range_flash_takes(const RangeAttn& a, bool back) { return takes(a, back); }
+static bool modified(const RangeAttn& a) { return a.cap > 0.f || a.slopes || a.scale < 0.f; }
+
+template <class K> static void set_lds(std::atomic<unsigned long long>& mask, K kernel, unsigned bytes) {
+  if (attr_needed(mask)) {
+    (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    attr_done(mask);
+  }
+}
+template <int DHP, bool MOD> static void fwd(const RangeAttn& a, hipStream_t s) {
+  static std::atomic<unsigned long long> mask{0};
+  constexpr unsigned smem = 4 * Tiles<DHP>::BYTES;
+  set_lds(mask, range_fwd_k<DHP, MOD>, smem);
+  hipLaunchKernelGGL((range_fwd_k<DHP, MOD>), dim3((unsigned)((i64)cdiv(a.Tq, 128) * a.H)), dim3(256), smem, s, a);
+}
+// Parts of a key tile's (query block, head) pairs in dK/dV: enough workgroups for two per CU, where the heads that share a key
+// head make many pairs.
+static int dkv_parts(const RangeAttn& a) {
+  const i64 workgroups = (i64)cdiv(a.Tk, 128) * a.Hkv;
+  int n = 1;
+  while (n < 8 && n < a.G && workgroups * n < 512) n *= 2;
+  return n;
+}
+size_t range_flash_sum_floats(const RangeAttn& a) {
+  const int n = dkv_parts(a);
+  return n > 1 ? (size_t)n * 2 * a.Tk * a.Hkv * (a.dh <= 64 ? 64 : 128) : 0;
+}
+template <int DHP, bool MOD> static void bwd(const RangeAttn& a, void* blocks, float* sums, hipStream_t s) {
+  static std::atomic<unsigned long long> mask_q{0}, mask_kv{0};
+  constexpr unsigned sq = 5 * Tiles<DHP>::BYTES, skv = 2 * DKV_STAGE<DHP>;
+  set_lds(mask_q, range_bwd_dq_k<DHP, MOD>, sq);
+  set_lds(mask_kv, range_bwd_dkv_k<DHP, MOD>, skv);
+  if (a.Tq > 0) hipLaunchKernelGGL((range_bwd_dq_k<DHP, MOD>), dim3((unsigned)((i64)cdiv(a.Tq, 128) * a.H)), dim3(256), sq, s, a, (BlockSeen*)blocks);
+  if (a.Tk <= 0) return;
+  const int parts = dkv_parts(a);
+  hipLaunchKernelGGL((range_bwd_dkv_k<DHP, MOD>), dim3((unsigned)((i64)cdiv(a.Tk, 128) * a.Hkv * parts)), dim3(256), skv, s, a, (const BlockSeen*)blocks, sums, parts);
+  if (parts > 1) hipLaunchKernelGGL(range_dkv_sum_k<DHP>, dim3((unsigned)cdiv((i64)a.Tk * a.Hkv, 4)), dim3(256), 0, s, a, sums, parts);
+}
+void launch_range_fwd_flash(const RangeAttn& a, hipStream_t s) {
+  if (a.Tq <= 0) return;
+  if (a.dh <= 64) { if (modified(a)) fwd<64, true>(a, s); else fwd<64, false>(a, s); }
+  else if (modified(a)) fwd<128, true>(a, s);
+  else fwd<128, false>(a, s);
+}
+void launch_range_bwd_flash(const RangeAttn& a, void* blocks, float* sums, hipStream_t s) {
+  if (a.dh <= 64) { if (modified(a)) bwd<64, true>(a, blocks, sums, s); else bwd<64, false>(a, blocks, sums, s); }
+  else if (modified(a)) bwd<128, true>(a, blocks, sums, s);
+  else bwd<128, false>(a, blocks, sums, s);
+}

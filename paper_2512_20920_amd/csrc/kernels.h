@@ -362,6 +362,13 @@ void launch_attn_ranges(const int* cu_q, const int* cu_k, const int* prefix, int
 void launch_range_fwd_rows(const RangeAttn& a, hipStream_t s);
 void launch_range_bwd_rows(const RangeAttn& a, hipStream_t s);
 
+// on the matrix cores, bf16, heads of up to 128 columns, where range_flash_takes the call.  blocks: 16 bytes per 64 query rows; sums:
+// range_flash_sum_floats floats
+bool range_flash_takes(const RangeAttn& a, bool back);
+size_t range_flash_sum_floats(const RangeAttn& a);
+void launch_range_fwd_flash(const RangeAttn& a, hipStream_t s);
+void launch_range_bwd_flash(const RangeAttn& a, void* blocks, float* sums, hipStream_t s);
+
 // ---- rotary positions, layer norm ---------------------------------------------------------------------------
 #define ROTARY_MAX_DIMS 256
 struct RotaryArgs {
