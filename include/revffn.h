@@ -360,7 +360,9 @@ typedef struct revffn_attn_mask {
 
 typedef struct revffn_attn_desc {
   int32_t dtype;           /* REVFFN_F32 or REVFFN_BF16: q, k, v, o and the gradients                */
-  int32_t kernel_mode;     /* 0 = automatic, 1 = the row-by-row kernels (any shape, slow), 2 = matrix-core kernels only */
+  int32_t kernel_mode;     /* 0 = automatic, 1 = the row-by-row kernels (any shape, slow), 2 = matrix-core kernels only;
+                              + 256 / + 512 = the form for few rows / for many (bfloat16) whatever the size, so that a test
+                              can reach both at small sizes                                          */
   int32_t H, Hkv, dh;      /* query heads; key heads (divides H: query head h reads key head h / (H / Hkv)); head width 1..512 */
   int32_t Tq, Tk;          /* rows of q, o and of k, v (Tk may be 0)                                 */
   int64_t ldq, ldk, ldv, ldo; /* row strides in elements of q, dq / k, dk / v, dv / o, d_o (head hh in columns hh*dh ..);

@@ -11,21 +11,21 @@ namespace {
 // a launch's grid times its 256 threads has to stay below 2^32
 bool grid_fits(i64 workgroups) { return workgroups < ((i64)1 << 24); }
 
-struct Scratch { float* dvec; void* blocks; float* sums; size_t bytes; };
+struct Scratch { float *parts, *dvec; void* blocks; float* sums; size_t bytes; };
 Scratch lay_out(const RangeAttn& a, bool backward, void* work) {
-  Scratch w = {nullptr, nullptr, nullptr, 0};
+  Scratch w = {nullptr, nullptr, nullptr, nullptr, 0};
   auto take = [&](size_t n) { void* p = work ? (char*)work + w.bytes : nullptr; w.bytes += (n + 255) / 256 * 256; return p; };
   if (backward) {
     w.dvec = (float*)take((size_t)a.H * a.Tq * 4);
     w.blocks = take(((size_t)a.Tq + 63) / 64 * 16);
-    w.sums = (float*)take(range_flash_sum_floats(a) * 4);
-  }
+    if (a.dt == 1 && a.dh <= 128) w.sums = (float*)take(range_flash_sum_floats(a) * 4);
+  } else if (a.dh <= 128) w.parts = (float*)take(range_few_floats(a) * 4);
   return w;
 }
 
 int check_desc(const revffn_attn_desc* d, RangeAttn* a) {
   if (!d) return REVFFN_ENULL;
-  if ((d->dtype != 0 && d->dtype != 1) || d->kernel_mode < 0 || d->kernel_mode > 2 || d->H < 1 || d->Hkv < 1 || d->H % d->Hkv ||
+  if ((d->dtype != 0 && d->dtype != 1) || d->kernel_mode < 0 || (d->kernel_mode & 0xff) > 2 || d->kernel_mode >> 8 > 2 || d->H < 1 || d->Hkv < 1 || d->H % d->Hkv ||
       d->H > 65536 || d->dh < 1 || d->dh > 512 || d->Tq < 0 || d->Tk < 0 || !(fabsf(d->scale) < INFINITY) || !(d->softcap >= 0.f) ||
       !(d->softcap < INFINITY))
     return REVFFN_EINVAL;
@@ -101,8 +101,12 @@ int revffn_op_attention_masked_fwd(const revffn_attn_desc* desc, const revffn_at
   if (w.bytes && !work) return REVFFN_ENULL;
   if (w.bytes > work_bytes || ((uintptr_t)work & 15)) return REVFFN_EINVAL;
   a.q = q; a.k = k; a.v = v; a.out = o; a.lse = lse;
-  if (desc->kernel_mode != 1 && range_flash_takes(a, false)) launch_range_fwd_flash(a, (hipStream_t)stream);
-  else if (desc->kernel_mode == 2) return REVFFN_EUNSUPPORTED;
+  const int mode = desc->kernel_mode & 0xff, form = desc->kernel_mode >> 8;
+  if (mode != 1 && range_flash_takes(a, false)) {
+    if (form ? form == 1 : range_flash_few(a)) launch_range_fwd_flash_few(a, w.parts, (hipStream_t)stream);
+    else launch_range_fwd_flash(a, (hipStream_t)stream);
+  } else if (mode != 1 && range_f32_takes(a, false)) launch_range_fwd_f32(a, w.parts, (hipStream_t)stream);
+  else if (mode == 2) return REVFFN_EUNSUPPORTED;
   else launch_range_fwd_rows(a, (hipStream_t)stream);
   return 0;
 }
@@ -118,8 +122,10 @@ int revffn_op_attention_masked_bwd(const revffn_attn_desc* desc, const revffn_at
   if (w.bytes && !work) return REVFFN_ENULL;
   if (w.bytes > work_bytes || ((uintptr_t)work & 15)) return REVFFN_EINVAL;
   a.q = q; a.k = k; a.v = v; a.o = o; a.d_o = d_o; a.lse = (float*)lse; a.dq = dq; a.dk = dk; a.dv = dv; a.dvec = w.dvec;
-  if (desc->kernel_mode != 1 && range_flash_takes(a, true)) launch_range_bwd_flash(a, w.blocks, w.sums, (hipStream_t)stream);
-  else if (desc->kernel_mode == 2) return REVFFN_EUNSUPPORTED;
+  const int mode = desc->kernel_mode & 0xff;
+  if (mode != 1 && range_flash_takes(a, true)) launch_range_bwd_flash(a, w.blocks, w.sums, (hipStream_t)stream);
+  else if (mode != 1 && range_f32_takes(a, true)) launch_range_bwd_f32(a, w.blocks, (hipStream_t)stream);
+  else if (mode == 2) return REVFFN_EUNSUPPORTED;
   else launch_range_bwd_rows(a, (hipStream_t)stream);
   return 0;
 }

@@ -7,6 +7,19 @@
 #define LN2 0.6931471805599453f
 #define RANGE_MAX_DH 512
 
+// ---- integers over the 64 lanes, as the sums and maxima of floats ----
+template <int CTRL, int ROW_MASK> __device__ __forceinline__ int dpp_i(int keep, int v) { return __builtin_amdgcn_update_dpp(keep, v, CTRL, ROW_MASK, 0xf, false); }
+__device__ __forceinline__ int wave_imax(int v) {
+  v = max(v, dpp_i<0x111, 0xf>(v, v));
+  v = max(v, dpp_i<0x112, 0xf>(v, v));
+  v = max(v, dpp_i<0x114, 0xf>(v, v));
+  v = max(v, dpp_i<0x118, 0xf>(v, v));
+  v = max(v, dpp_i<0x142, 0xa>(v, v));
+  v = max(v, dpp_i<0x143, 0xc>(v, v));
+  return __builtin_amdgcn_readlane(v, 63);
+}
+__device__ __forceinline__ int wave_imin(int v) { return -1 - wave_imax(-1 - v); }
+
 __device__ __forceinline__ int rows_in_use(const RangeAttn& a) { return a.used ? min(max(a.used[0], 0), a.Tq) : a.Tq; }
 __device__ __forceinline__ int keys_in_use(const RangeAttn& a) { return a.used ? min(max(a.used[1], 0), a.Tk) : a.Tk; }
 // clamped; lo = hi = 0 if there is none

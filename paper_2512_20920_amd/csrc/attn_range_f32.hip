@@ -1,0 +1,292 @@
+// Attention over key ranges in float32 on the matrix cores (v_mfma_f32_32x32x2_f32), heads of up to 128 columns (a multiple of 4).
+//
+// Transposed score tiles: in S^T[key, row] = K Q^T a lane owns one row, element e of the result is key (e >> 2) * 8 + (lane >> 5)
+// * 4 + (e & 3), and that is what the second product wants as its operand: instruction e contracts over the two keys that
+// the two halves of the wave hold in element e.  So probabilities stay in the registers they were computed in, at full
+// precision, and keys and values are read from memory as operands directly: K 16 bytes of its own row per lane, V a row of 32
+// consecutive columns per half.  32 rows (keys) per workgroup, tiles of 32 shared out to the waves.
+#include "attn_range_few.h"
+
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+
+#define NW 4
+
+__device__ __forceinline__ int elem_row(int e, int half) { return (e >> 2) * 8 + half * 4 + (e & 3); }
+__device__ __forceinline__ float half_sum(float v) { return v + __shfl_xor(v, 32, WAVE); }
+// this lane's half of a row as an operand of a product over the width: columns 8 c + 4 half .. + 3
+template <int DHP> __device__ __forceinline__ void load_row(const float* row, bool ok, int dh, int half, float f, float (&r)[DHP / 2]) {
+#pragma unroll
+  for (int c = 0; c < DHP / 8; c++) {
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (ok && c * 8 + half * 4 < dh) v = *(const f32x4*)(row + c * 8 + half * 4);
+#pragma unroll
+    for (int i = 0; i < 4; i++) r[c * 4 + i] = v[i] * f;
+  }
+}
+template <int DHP> __device__ __forceinline__ f32x16 scores(const float* row, int dh, int half, const float (&r)[DHP / 2]) {
+  f32x16 a = {};
+#pragma unroll
+  for (int c = 0; c < DHP / 8; c++) {
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (c * 8 + half * 4 < dh) v = *(const f32x4*)(row + c * 8 + half * 4);
+#pragma unroll
+    for (int i = 0; i < 4; i++) a = __builtin_amdgcn_mfma_f32_32x32x2f32(v[i], r[c * 4 + i], a, 0, 0, 0);
+  }
+  return a;
+}
+// acc^T[column, lane] += X^T[column, row] p[row, lane] over the 32 rows of X from r0 on (rows past the last one are that one: p is
+// zero there); all loads in flight before the first product
+template <int DHP> __device__ __forceinline__ void accumulate(f32x16 (&acc)[DHP / 32], const float* x, i64 ld, int dh, int r0, int last, const f32x16& p, int lane) {
+  constexpr int DT = DHP / 32;
+  float v[16][DT];
+#pragma unroll
+  for (int e = 0; e < 16; e++) {
+    const float* row = x + (i64)min(r0 + elem_row(e, lane >> 5), last) * ld + (lane & 31);
+#pragma unroll
+    for (int i = 0; i < DT; i++) v[e][i] = (lane & 31) + i * 32 < dh ? row[i * 32] : 0.f;
+  }
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int e = 0; e < 16; e++)
+#pragma unroll
+    for (int i = 0; i < DT; i++) acc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[e][i], p[e], acc[i], 0, 0, 0);
+}
+// a wave's accumulators to LDS, [column][32 rows]
+template <int DHP> __device__ __forceinline__ void spill(float* t, const f32x16 (&acc)[DHP / 32], int lane) {
+#pragma unroll
+  for (int i = 0; i < DHP / 32; i++)
+#pragma unroll
+    for (int e = 0; e < 16; e++) t[(i * 32 + elem_row(e, lane >> 5)) * 32 + (lane & 31)] = acc[i][e];
+}
+// the sum of the waves' tiles for row threadIdx.x & 31, DHP / 8 columns of it; whether all of it is finite
+template <int DHP> __device__ __forceinline__ bool store_sum(const float* sm, float* row, bool ok, int dh, float f) {
+  constexpr int C = DHP * 32 / (NW * 64);
+  const int r = threadIdx.x & 31, c0 = (int)(threadIdx.x >> 5) * C;
+  float z = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; c += 4) {
+    f32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      float t = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW; w++) t += sm[(w * DHP + c0 + c + i) * 32 + r];
+      z = fmaf(t, 0.f, z);
+      v[i] = t * f;
+    }
+    if (ok && c0 + c < dh) *(f32x4*)(row + c0 + c) = v;
+  }
+  return !ok || z == 0.f;
+}
+
+template <int DHP> __global__ void __launch_bounds__(NW * 64) range_fwd_f32_k(RangeAttn a, FewShape f) {
+  extern __shared__ float sm[];                      // NW results [DHP][32], statistics
+  int tile, split, head, t0;
+  few_place(a, f, (int)blockIdx.x, &tile, &split, &head);
+  const int rows = rows_in_use(a), keys = keys_in_use(a);
+  if (tile * f.qpt >= rows) return;
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, kh = head % a.Hkv;
+  const FewRow row = few_row(a, f, tile, head, lane & 31, rows);
+  const FewKeys fk = few_keys(a, f, row, split, keys, &t0);
+  const float slope = a.slopes ? a.slopes[row.h] : 0.f;
+  const int at = row.ok && a.at ? a.at[row.i] : row.i;
+  const float *k = (const float*)a.k + (i64)kh * a.dh, *v = (const float*)a.v + (i64)kh * a.dh;
+  float qf[DHP / 2];
+  load_row<DHP>((const float*)a.q + (i64)row.i * a.ldq + (i64)row.h * a.dh, row.ok, a.dh, half, a.scale, qf);
+  f32x16 acc[DHP / 32] = {};
+  float m = -INFINITY, l = 0.f;
+  for (int t = fk.live_from(t0 + wv, NW); t < fk.t1; t = fk.live_from(t + NW, NW)) {
+    const int kv = fk.first + t * 32;
+    f32x16 s = scores<DHP>(k + (i64)min(kv + (lane & 31), fk.end - 1) * a.ldk, a.dh, half, qf);
+    float mx = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 16; e++) {
+      const int j = kv + elem_row(e, half);
+      float keep;
+      s[e] = j >= fk.r.x && j < fk.r.y ? range_score(s[e], a.cap, slope, at, j, &keep) : -INFINITY;
+      mx = fmaxf(mx, s[e]);
+    }
+    mx = fmaxf(mx, __shfl_xor(mx, 32, WAVE));
+    const float mn = fmaxf(m, mx), ms = mn == -INFINITY ? 0.f : mn, alpha = expf(m - ms);
+    float rs = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; e++) { s[e] = expf(s[e] - ms); rs += s[e]; }
+    l = l * alpha + rs;
+    m = mn;
+#pragma unroll
+    for (int i = 0; i < DHP / 32; i++) acc[i] *= alpha;
+    accumulate<DHP>(acc, v, a.ldv, a.dh, kv, fk.end - 1, s, lane);
+  }
+  l = half_sum(l);
+  float* stats = sm + NW * DHP * 32;
+  spill<DHP>(sm + wv * DHP * 32, acc, lane);
+  if (half == 0) { stats[wv * 64 + lane] = m * LOG2E; stats[wv * 64 + 32 + lane] = l; }
+  __syncthreads();
+  few_finish<float, DHP, NW>(a, f, tile, split, head, rows, keys, sm, stats, sm);
+}
+
+// dQ of 32 rows, and D = <o, dO>.  The last workgroups of the launch (from `tiles` on) note instead, a wave per block of 64 queries, the first key that
+// some of them see and one past the last.
+template <int DHP> __global__ void __launch_bounds__(NW * 64) range_dq_f32_k(RangeAttn a, FewShape f, int tiles, int2* __restrict__ blocks) {
+  extern __shared__ float sm[];
+  const int rows = rows_in_use(a), keys = keys_in_use(a);
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+  if ((int)blockIdx.x >= tiles) {
+    const int b = ((int)blockIdx.x - tiles) * NW + wv, i = b * 64 + lane;
+    int2 r = i < rows ? key_range(a, i, keys) : make_int2(0, 0);
+    if (r.x == r.y) r = make_int2(INT_MAX, 0);
+    r = make_int2(wave_imin(r.x), wave_imax(r.y));
+    if (lane == 0 && b * 64 < a.Tq) blocks[b] = r;
+    return;
+  }
+  int tile, split, head, t0;
+  few_place(a, f, (int)blockIdx.x, &tile, &split, &head);
+  if (tile * f.qpt >= rows) return;
+  const int kh = head % a.Hkv;
+  const FewRow row = few_row(a, f, tile, head, lane & 31, rows);
+  const FewKeys fk = few_keys(a, f, row, 0, keys, &t0);
+  const float slope = a.slopes ? a.slopes[row.h] : 0.f;
+  const int at = row.ok && a.at ? a.at[row.i] : row.i;
+  const float *k = (const float*)a.k + (i64)kh * a.dh, *v = (const float*)a.v + (i64)kh * a.dh;
+  const i64 orow = (i64)row.i * a.ldo + (i64)row.h * a.dh, qrow = (i64)row.i * a.ldq + (i64)row.h * a.dh, srow = (i64)row.h * a.Tq + row.i;
+  float qf[DHP / 2], dof[DHP / 2], D = 0.f;
+  load_row<DHP>((const float*)a.d_o + orow, row.ok, a.dh, half, 1.f, dof);
+  load_row<DHP>((const float*)a.o + orow, row.ok, a.dh, half, 1.f, qf);
+#pragma unroll
+  for (int c = 0; c < DHP / 2; c++) D = fmaf(qf[c], dof[c], D);
+  D = half_sum(D);
+  if (wv == 0 && half == 0 && row.ok) a.dvec[srow] = D;
+  load_row<DHP>((const float*)a.q + qrow, row.ok, a.dh, half, a.scale, qf);
+  const float L = row.ok ? a.lse[srow] : -INFINITY;
+  f32x16 acc[DHP / 32] = {};
+  for (int t = fk.live_from(t0 + wv, NW); t < fk.t1; t = fk.live_from(t + NW, NW)) {
+    const int kv = fk.first + t * 32, jc = min(kv + (lane & 31), fk.end - 1);
+    f32x16 s = scores<DHP>(k + (i64)jc * a.ldk, a.dh, half, qf);
+    const f32x16 dp = scores<DHP>(v + (i64)jc * a.ldv, a.dh, half, dof);
+#pragma unroll
+    for (int e = 0; e < 16; e++) {
+      const int j = kv + elem_row(e, half);
+      float keep;
+      const float x = range_score(s[e], a.cap, slope, at, j, &keep);
+      s[e] = j >= fk.r.x && j < fk.r.y && L != -INFINITY ? expf(x - L) * (dp[e] - D) * keep : 0.f;
+    }
+    accumulate<DHP>(acc, k, a.ldk, a.dh, kv, fk.end - 1, s, lane);
+  }
+  spill<DHP>(sm + wv * DHP * 32, acc, lane);
+  __syncthreads();
+  const FewRow mine = few_row(a, f, tile, head, threadIdx.x & 31, rows);
+  const bool fine = store_sum<DHP>(sm, (float*)a.dq + (i64)mine.i * a.ldq + (i64)mine.h * a.dh, mine.ok, a.dh, a.scale);
+  if (__syncthreads_or(!fine))
+    for (int x = wv; x < 32; x += NW) {
+      const FewRow again = few_row(a, f, tile, head, x, rows);
+      if (again.ok) range_row_dq<float>(a, again.i, again.h, keys, sm + wv * 2 * DHP);
+    }
+}
+
+// dK, dV of 32 keys of a key head: the waves share out the blocks of 32 queries that see some of them, of every head that shares it.
+template <int DHP> __global__ void __launch_bounds__(NW * 64) range_dkv_f32_k(RangeAttn a, const int2* __restrict__ blocks) {
+  extern __shared__ float sm[];                      // NW results [DHP][32], then 5 x 32 words per wave
+  const int kt = (int)blockIdx.x / a.Hkv, kh = (int)blockIdx.x - kt * a.Hkv, k0 = kt * 32;
+  const int rows = rows_in_use(a), keys = keys_in_use(a);
+  if (k0 >= keys) return;
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, myk = k0 + (lane & 31);
+  float* words = sm + NW * DHP * 32 + wv * 160;
+  float kf[DHP / 2], vf[DHP / 2];
+  load_row<DHP>((const float*)a.k + (i64)myk * a.ldk + (i64)kh * a.dh, myk < keys, a.dh, half, a.scale, kf);
+  load_row<DHP>((const float*)a.v + (i64)myk * a.ldv + (i64)kh * a.dh, myk < keys, a.dh, half, 1.f, vf);
+  f32x16 dka[DHP / 32] = {}, dva[DHP / 32] = {};
+  const int nb = (rows + 63) / 64;
+  int turn = 0;
+  for (int b0 = 0; b0 < nb; b0 += 64) {
+    const int2 r = b0 + lane < nb ? blocks[b0 + lane] : make_int2(INT_MAX, 0);
+    unsigned long long live = __ballot(r.x < k0 + 32 && r.y > k0);
+    while (live) {
+      const int b = b0 + __builtin_ctzll(live);
+      live &= live - 1;
+      for (int n = 0; n < 2 * a.G; n++, turn++) {
+        const int q0 = b * 64 + (n & 1) * 32, h = kh * a.G + (n >> 1), i = q0 + (lane & 31);
+        if (turn % NW != wv || q0 >= rows) continue;
+        const int2 see = i < rows ? key_range(a, i, keys) : make_int2(0, 0);
+        if (!__any(see.x < k0 + 32 && see.y > k0)) continue;
+        const int ic = min(i, rows - 1);
+        wave_lds_fence();
+        if (half == 0) {
+          words[lane] = a.lse[(i64)h * a.Tq + ic];
+          words[32 + lane] = a.dvec[(i64)h * a.Tq + ic];
+          ((int*)words)[64 + lane] = a.at ? a.at[ic] : ic;
+        } else {
+          ((int*)words)[96 + lane - 32] = see.x;
+          ((int*)words)[128 + lane - 32] = see.y;
+        }
+        wave_lds_fence();
+        const float *q = (const float*)a.q + (i64)h * a.dh, *d_o = (const float*)a.d_o + (i64)h * a.dh;
+        f32x16 s = scores<DHP>(q + (i64)ic * a.ldq, a.dh, half, kf);
+        f32x16 dp = scores<DHP>(d_o + (i64)ic * a.ldo, a.dh, half, vf);
+        const float slope = a.slopes ? a.slopes[h] : 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; e++) {
+          const int x = elem_row(e, half);
+          const float L = words[x];
+          const bool sees = myk >= ((const int*)words)[96 + x] && myk < ((const int*)words)[128 + x] && L != -INFINITY;
+          float keep;
+          const float p = expf(range_score(s[e], a.cap, slope, ((const int*)words)[64 + x], myk, &keep) - L);
+          dp[e] = sees ? p * (dp[e] - words[32 + x]) * keep : 0.f;
+          s[e] = sees ? p : 0.f;
+        }
+        accumulate<DHP>(dva, d_o, a.ldo, a.dh, q0, rows - 1, s, lane);
+        accumulate<DHP>(dka, q, a.ldq, a.dh, q0, rows - 1, dp, lane);
+      }
+    }
+  }
+  const int r = k0 + (int)(threadIdx.x & 31);
+  spill<DHP>(sm + wv * DHP * 32, dka, lane);
+  __syncthreads();
+  bool fine = store_sum<DHP>(sm, (float*)a.dk + (i64)r * a.ldk + (i64)kh * a.dh, r < keys, a.dh, a.scale);
+  __syncthreads();
+  spill<DHP>(sm + wv * DHP * 32, dva, lane);
+  __syncthreads();
+  fine &= store_sum<DHP>(sm, (float*)a.dv + (i64)r * a.ldv + (i64)kh * a.dh, r < keys, a.dh, 1.f);
+  if (__syncthreads_or(!fine))
+    for (int x = wv; x < 32 && k0 + x < keys; x += NW) range_row_dkv<float>(a, k0 + x, kh, rows, keys, sm + wv * 2 * DHP);
+}
+
+// rows are read 4 elements at a time
+bool range_f32_takes(const RangeAttn& a, bool back) {
+  if (a.dt != 0 || a.dh > 128 || a.dh % 4) return false;
+  uintptr_t p = (uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v;
+  p |= back ? (uintptr_t)a.o | (uintptr_t)a.d_o | (uintptr_t)a.dq | (uintptr_t)a.dk | (uintptr_t)a.dv : (uintptr_t)a.out;
+  return !(p & 15) && !((a.ldq | a.ldk | a.ldv | a.ldo) & 3);
+}
+template <class K> static void set_lds(std::atomic<unsigned long long>& mask, K kernel, size_t bytes) {
+  if (attr_needed(mask)) {
+    (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    attr_done(mask);
+  }
+}
+template <int DHP> static void fwd(const RangeAttn& a, float* work, hipStream_t s) {
+  constexpr size_t smem = (size_t)(NW * DHP * 32 + NW * 64) * 4;
+  static std::atomic<unsigned long long> mask{0};
+  set_lds(mask, range_fwd_f32_k<DHP>, smem);
+  const FewShape f = few_shape(a, work);
+  hipLaunchKernelGGL(range_fwd_f32_k<DHP>, dim3((unsigned)((i64)f.tiles * f.splits * a.Hkv * f.hb)), dim3(NW * 64), smem, s, a, f);
+  if (f.splits > 1) hipLaunchKernelGGL((range_join_k<float, DHP>), dim3((unsigned)cdiv((i64)a.Tq * a.H, 4)), dim3(256), 0, s, a, f);
+}
+template <int DHP> static void bwd(const RangeAttn& a, void* blocks, hipStream_t s) {
+  constexpr size_t smem = (size_t)NW * DHP * 32 * 4, smem_kv = smem + NW * 160 * 4;
+  static std::atomic<unsigned long long> mask_q{0}, mask_kv{0};
+  set_lds(mask_q, range_dq_f32_k<DHP>, smem);
+  set_lds(mask_kv, range_dkv_f32_k<DHP>, smem_kv);
+  FewShape f = few_shape(a, nullptr);
+  f.splits = 1;
+  const int tiles = f.tiles * a.Hkv * f.hb;
+  if (a.Tq > 0) hipLaunchKernelGGL(range_dq_f32_k<DHP>, dim3((unsigned)(tiles + cdiv(a.Tq, 64 * NW))), dim3(NW * 64), smem, s, a, f, tiles, (int2*)blocks);
+  if (a.Tk > 0) hipLaunchKernelGGL(range_dkv_f32_k<DHP>, dim3((unsigned)((i64)cdiv(a.Tk, 32) * a.Hkv)), dim3(NW * 64), smem_kv, s, a, (const int2*)blocks);
+}
+void launch_range_fwd_f32(const RangeAttn& a, float* work, hipStream_t s) {
+  if (a.Tq <= 0) return;
+  if (a.dh <= 64) fwd<64>(a, work, s); else fwd<128>(a, work, s);
+}
+void launch_range_bwd_f32(const RangeAttn& a, void* blocks, hipStream_t s) {
+  if (a.dh <= 64) bwd<64>(a, blocks, s); else bwd<128>(a, blocks, s);
+}

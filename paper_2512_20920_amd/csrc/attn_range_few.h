@@ -1,0 +1,162 @@
+// The forms of attention over key ranges for few rows: a workgroup takes 32 rows, which are queries of all (at most 32) heads that share
+// a key head, so that its keys are read once for all of them, and its four waves share the keys out in tiles of 32.  The keys may
+// be split further over several workgroups, whose results a second launch joins.
+#pragma once
+#include "attn_range.h"
+
+struct FewShape {
+  int gp, hb;              // heads of a workgroup, head blocks per key head (more than one: more than 32 heads to a key head)
+  int qpt, tiles;          // queries of a workgroup, tiles of them
+  int splits;              // of the keys
+  float2* stats;           // splits > 1: [query row, head][split] maximum (units of log2) and sum
+  float* part;             //             [query row, head][split][DHP] unnormalised result
+};
+struct FewRow { int i, h; bool ok; };
+__device__ __forceinline__ FewRow few_row(const RangeAttn& a, const FewShape& f, int tile, int head, int r, int rows) {
+  const int kh = head % a.Hkv, hb = head / a.Hkv, q = r / f.gp, hg = hb * f.gp + r - q * f.gp;
+  FewRow x;
+  x.i = tile * f.qpt + q;
+  x.ok = q < f.qpt && hg < a.G && x.i < rows;
+  x.h = kh * a.G + min(hg, a.G - 1);
+  return x;
+}
+// workgroup id -> tile, split, head block (fastest: consecutive workgroups go to different XCDs, a key head stays with one)
+__device__ __forceinline__ void few_place(const RangeAttn& a, const FewShape& f, int id, int* tile, int* split, int* head) {
+  const int heads = a.Hkv * f.hb, row = id / heads;
+  *head = id - row * heads;
+  *tile = row / f.splits;
+  *split = row - *tile * f.splits;
+}
+// the keys that the 32 rows see, in tiles of 32 from the first one on
+struct FewKeys {
+  int2 r;                  // of this lane's row (lane & 31); lo = INT_MAX, hi = 0: none
+  int first, end, t1;      // t1: one past this workgroup's last tile
+  // the first tile from t on, in steps of `step`, that some row sees; t1 or more: there is none
+  __device__ __forceinline__ int live_from(int t, int step) const {
+    while (t < t1) {
+      const int kv = first + t * 32;
+      if (__any(r.x < kv + 32 && r.y > kv)) return t;
+      const int v = wave_imin(r.y > kv ? r.x : INT_MAX);      // the next key that anybody sees
+      if (v == INT_MAX) return t1;
+      t += max(1, ((v - first) / 32 - t + step - 1) / step) * step;
+    }
+    return t;
+  }
+};
+__device__ __forceinline__ FewKeys few_keys(const RangeAttn& a, const FewShape& f, const FewRow& row, int split, int keys, int* t0) {
+  FewKeys k;
+  k.r = row.ok ? key_range(a, row.i, keys) : make_int2(0, 0);
+  if (k.r.x == k.r.y) k.r = make_int2(INT_MAX, 0);
+  k.first = wave_imin(k.r.x);
+  k.end = wave_imax(k.r.y);
+  const int n = k.first < k.end ? (k.end - k.first + 31) / 32 : 0, per = (n + f.splits - 1) / f.splits;
+  *t0 = min(split * per, n);
+  k.t1 = min(*t0 + per, n);
+  return k;
+}
+
+// The waves' partial results, [column][32 rows] in LDS each, with their maxima (units of log2) and sums, to the row's result or to this split's
+// part of it.  slow: 2 dh floats of LDS per wave for rows that are worked out again.
+template <class T, int DHP, int NW>
+__device__ __forceinline__ void few_finish(const RangeAttn& a, const FewShape& f, int tile, int split, int head, int rows, int keys,
+                                           const float* part, const float* stats, float* slow) {
+  constexpr int C = DHP * 32 / (NW * 64);            // columns per thread
+  const int r = threadIdx.x & 31, c0 = (int)(threadIdx.x >> 5) * C;
+  const FewRow row = few_row(a, f, tile, head, r, rows);
+  float M = -INFINITY, w[NW], tot = 0.f, v[C];
+#pragma unroll
+  for (int j = 0; j < NW; j++) M = fmaxf(M, stats[j * 64 + r]);
+  const float Ms = M == -INFINITY ? 0.f : M;
+#pragma unroll
+  for (int j = 0; j < NW; j++) { w[j] = exp2f(stats[j * 64 + r] - Ms); tot += w[j] * stats[j * 64 + 32 + r]; }
+#pragma unroll
+  for (int c = 0; c < C; c++) {
+    v[c] = 0.f;
+#pragma unroll
+    for (int j = 0; j < NW; j++) v[c] = fmaf(w[j], part[(j * DHP + c0 + c) * 32 + r], v[c]);
+  }
+  if (f.splits > 1) {
+    if (!row.ok) return;
+    const i64 at = ((i64)row.i * a.H + row.h) * f.splits + split;
+    if (threadIdx.x < 32) f.stats[at] = make_float2(M, tot);
+    if (tot == 0.f) return;                          // (nothing seen: the second launch leaves it out)
+#pragma unroll
+    for (int c = 0; c < C; c += 4) *(float4*)(f.part + at * DHP + c0 + c) = make_float4(v[c], v[c + 1], v[c + 2], v[c + 3]);
+    return;
+  }
+  const float inv = tot == 0.f ? 0.f : 1.f / tot;
+  float z = 0.f;
+  T* o = (T*)a.out + (i64)row.i * a.ldo + (i64)row.h * a.dh;
+#pragma unroll
+  for (int c = 0; c < C; c += 4) {
+    typedef __attribute__((ext_vector_type(4))) T V4;
+    V4 x;
+#pragma unroll
+    for (int i = 0; i < 4; i++) { z = fmaf(v[c + i], 0.f, z); x[i] = from_f<T>(v[c + i] * inv); }
+    if (row.ok && c0 + c < a.dh) *(V4*)(o + c0 + c) = x;
+  }
+  if (threadIdx.x < 32 && row.ok && a.lse) a.lse[(i64)row.h * a.Tq + row.i] = tot == 0.f ? -INFINITY : (M + log2f(tot)) * LN2;
+  // a value that is not finite: seen by its row, or only multiplied by zero in a tile that it sees a part of?
+  if (__syncthreads_or(row.ok && z != 0.f))
+    for (int x = (int)(threadIdx.x >> 6); x < 32; x += NW) {
+      const FewRow again = few_row(a, f, tile, head, x, rows);
+      if (again.ok) range_row_fwd<T>(a, again.i, again.h, keys, slow + (threadIdx.x >> 6) * 2 * DHP);
+    }
+}
+// joins the splits: one wave per (query row, head), DHP / 64 columns per lane; at most 64 splits
+template <class T, int DHP> __global__ void __launch_bounds__(256) range_join_k(RangeAttn a, FewShape f) {
+  __shared__ float slow[4][2 * DHP];
+  constexpr int C = DHP / 64;
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, rows = rows_in_use(a);
+  const i64 n = (i64)blockIdx.x * 4 + wv;
+  const int i = (int)(n / a.H), h = (int)(n - (i64)i * a.H);
+  if (i >= rows) return;
+  const float2 st = lane < f.splits ? f.stats[n * f.splits + lane] : make_float2(-INFINITY, 0.f);
+  const float M = wave_max(st.x), Ms = M == -INFINITY ? 0.f : M;
+  const float w = st.y == 0.f ? 0.f : exp2f(st.x - Ms);
+  const float tot = wave_sum(w * st.y);
+  float v[C] = {};
+  const float* p = f.part + n * f.splits * DHP + lane * C;
+  const unsigned long long live = __ballot(st.y != 0.f);
+#pragma unroll 8
+  for (int s = 0; s < f.splits; s++)
+    if ((live >> s) & 1) {
+      const float ws = __shfl(w, s, WAVE);
+#pragma unroll
+      for (int c = 0; c < C; c++) v[c] = fmaf(ws, p[s * DHP + c], v[c]);
+    }
+  float z = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; c++) z = fmaf(v[c], 0.f, z);
+  if (!__all(z == 0.f)) {
+    range_row_fwd<T>(a, i, h, keys_in_use(a), slow[wv]);
+    return;
+  }
+  const float inv = tot == 0.f ? 0.f : 1.f / tot;
+  T* o = (T*)a.out + (i64)i * a.ldo + (i64)h * a.dh;
+#pragma unroll
+  for (int c = 0; c < C; c++) if (lane * C + c < a.dh) o[lane * C + c] = from_f<T>(v[c] * inv);
+  if (lane == 0 && a.lse) a.lse[(i64)h * a.Tq + i] = tot == 0.f ? -INFINITY : (M + log2f(tot)) * LN2;
+}
+
+// workgroups that fill the chip twice, of 128 keys (a tile per wave) at least
+inline FewShape few_shape(const RangeAttn& a, float* work) {
+  FewShape f;
+  f.gp = a.G < 32 ? a.G : 32;
+  f.hb = (a.G + f.gp - 1) / f.gp;
+  f.qpt = 32 / f.gp;
+  f.tiles = cdiv(a.Tq, f.qpt);
+  const i64 workgroups = (i64)f.tiles * a.Hkv * f.hb, most = cdiv(a.Tk, 128);
+  i64 n = workgroups ? 512 / workgroups : 1;
+  if (n > most) n = most;
+  if (n > 64) n = 64;
+  f.splits = n < 1 ? 1 : (int)n;
+  f.stats = (float2*)work;
+  f.part = work ? work + 2 * (i64)a.Tq * a.H * f.splits : nullptr;
+  if ((2 * (i64)a.Tq * a.H * f.splits) % 4) f.part += 2;     // (16-byte aligned)
+  return f;
+}
+inline size_t few_floats(const RangeAttn& a) {
+  const FewShape f = few_shape(a, nullptr);
+  return f.splits > 1 ? (size_t)a.Tq * a.H * f.splits * (2 + (a.dh <= 64 ? 64 : 128)) + 2 : 0;
+}

@@ -1,5 +1,6 @@
 // Attention over key ranges on the matrix cores: bf16, heads of up to 128 columns (a multiple of 8).
 #include "attn_range_tiles.h"
+#include "attn_range_few.h"
 
 // Which tile a workgroup takes (1-D grid of tiles x heads).  Heads are the fastest index, and those that share a key head follow each
 // other 8 apart where there are 8 key heads or more, so that they run on the same XCD (id & 7) and find its keys in that L2.
@@ -202,6 +203,108 @@ __global__ void __launch_bounds__(256, 2) range_fwd_k(RangeAttn a) {
     T::store(o, oacc, l == 0.f ? 0.f : 1.0f / l, a.dh, g);
     if (g == 0 && a.lse) a.lse[(i64)h * a.Tq + myq] = l == 0.f ? -INFINITY : (m + __log2f(l)) * LN2;
   }
+}
+
+// ------------------------------------------------------------------------------------
+// Forward for few rows: 32 rows per workgroup, tiles of 32 keys shared out to the waves, each in LDS of its own that no other wave
+// touches, so nothing waits at a barrier until the partial results meet.  A single token's query against a long run of keys
+// reads every key and value once, for all heads that share them: that reading bounds it.
+// ------------------------------------------------------------------------------------
+template <int DHP> constexpr unsigned FEW_SMEM = 4 * Tiles<DHP>::BYTES + 4 * 256;       // the waves' K and V (then their results), statistics
+template <int DHP, bool MOD>
+__global__ void __launch_bounds__(256, 2) range_fwd_few_k(RangeAttn a, FewShape f) {
+  typedef Tiles<DHP> T;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem_raw[];
+  int tile, split, head, t0;
+  few_place(a, f, (int)blockIdx.x, &tile, &split, &head);
+  const int rows = rows_in_use(a), keys = keys_in_use(a);
+  if (tile * f.qpt >= rows) return;
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, kh = head % a.Hkv;
+  const FewRow row = few_row(a, f, tile, head, lane & 31, rows);
+  const FewKeys fk = few_keys(a, f, row, split, keys, &t0);
+  const ScoreForm sf = score_form(a, row.h);
+  const int at = MOD && sf.biased && row.ok ? (a.at ? a.at[row.i] : row.i) : 0;
+  const HeadRows rk = {(const unsigned char*)a.k + (i64)kh * a.dh * 2, a.ldk * 2, a.dh * 2}, rv = {(const unsigned char*)a.v + (i64)kh * a.dh * 2, a.ldv * 2, a.dh * 2};
+  unsigned char* tK = smem_raw + wv * T::BYTES;      // 32 rows of K, 32 of V
+  const unsigned aK = lds_address(smem_raw) + (unsigned)wv * T::BYTES, aV = aK + T::BYTES / 2;
+  auto issue = [&](const HeadRows& r, int t, unsigned dst) {
+    const int kv = t < fk.t1 ? fk.first + t * 32 : 0, n = t < fk.t1 ? min(32, fk.end - kv) : 0;
+    const __amdgpu_buffer_rsrc_t rs = rows_buffer(r, kv, n);
+    T::load16(rs, (unsigned)r.ldb, r.width, 0, dst, lane);
+    T::load16(rs, (unsigned)r.ldb, r.width, 16, dst + 16 * T::ROW, lane);
+  };
+  int t = fk.live_from(t0 + wv, 4);
+  issue(rk, t, aK);
+  issue(rv, t, aV);
+  bf16x8 qf[T::KK];
+  T::load_frags((const bf16*)a.q + (i64)row.i * a.ldq + (i64)row.h * a.dh, row.ok, a.dh, g, qf);
+  T::arrived(qf);
+  const unsigned rbase = T::row_base(lane), cbase = T::col_base(lane);
+  f32x16 acc[T::DT] = {};
+  float m = -INFINITY, l = 0.f;
+  wait_vmcnt<0>();
+  while (t < fk.t1) {
+    const int kv = fk.first + t * 32, next = fk.live_from(t + 4, 4);
+    wait_vmcnt<2 * T::LOADS>();                     // K; V may be on its way
+    bf16x8 x[T::KK];
+#pragma unroll
+    for (int kk = 0; kk < T::KK; kk++) x[kk] = *(const bf16x8*)(tK + (rbase ^ (unsigned)(kk * 32)));
+    __builtin_amdgcn_sched_barrier(0);
+    f32x16 s = {};
+#pragma unroll
+    for (int kk = 0; kk < T::KK; kk++) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[kk], qf[kk], s, 0, 0, 0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    issue(rk, next, aK);
+    const float d0 = (float)((i64)at - kv - g * 4);
+    const int lo = max(fk.r.x, kv) - kv - g * 4;
+    const unsigned n = (unsigned)max(min(fk.r.y, kv + 32) - max(fk.r.x, kv), 0);
+    float mx = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 16; e++) {
+      const int c = (e >> 2) * 8 + (e & 3);
+      float y;
+      if constexpr (MOD) {
+        y = sf.capped ? fast_tanh_2(s[e] * sf.x2) * sf.cap2 : s[e] * sf.f;
+        if (sf.biased) y = fmaf(-sf.slope2, fabsf(d0 - (float)c), y);
+      } else y = s[e] * sf.f;
+      if ((unsigned)(c - lo) >= n) y = -INFINITY;
+      s[e] = y;
+      mx = fmaxf(mx, y);
+    }
+    const float mn = fmaxf(m, both_halves_max(mx)), ms = mn == -INFINITY ? 0.f : mn;
+    float rs = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; e++) { s[e] = fast_exp2(s[e] - ms); rs += s[e]; }
+    if (__any(mn > m)) {
+      const float alpha = fast_exp2(m - ms);
+      l *= alpha;
+#pragma unroll
+      for (int d = 0; d < T::DT; d++) acc[d] *= alpha;
+    }
+    l += rs;
+    m = mn;
+    bf16x8 pf[2], vf[T::DT];
+    pf[0] = acc_to_frag(s, 0);
+    pf[1] = acc_to_frag(s, 1);
+    wait_vmcnt<2 * T::LOADS>();                     // V; the next K may be on its way
+    T::read_cols(vf, tK + T::BYTES / 2, cbase, 0);
+    T::template cols_times<32>(acc, tK + T::BYTES / 2, cbase, pf, vf);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    issue(rv, next, aV);
+    t = next;
+  }
+  wait_vmcnt<0>();                                  // the zero-filled loads past the last tile
+  l = both_halves_sum(l);
+  float *stats = (float*)(smem_raw + 4 * T::BYTES), *mine = (float*)tK;
+#pragma unroll
+  for (int d = 0; d < T::DT; d++)
+#pragma unroll
+    for (int e = 0; e < 16; e++) mine[(d * 32 + (e >> 2) * 8 + g * 4 + (e & 3)) * 32 + (lane & 31)] = acc[d][e];
+  if (g == 0) { stats[wv * 64 + lane] = m; stats[wv * 64 + 32 + lane] = l; }
+  __syncthreads();
+  few_finish<bf16, DHP, 4>(a, f, tile, split, head, rows, keys, (const float*)smem_raw, stats, (float*)smem_raw);
 }
 
 // ------------------------------------------------------------------------------------
@@ -629,6 +732,21 @@ template <int DHP, bool MOD> static void bwd(const RangeAttn& a, void* blocks, f
   hipLaunchKernelGGL((range_bwd_dkv_k<DHP, MOD>), dim3((unsigned)((i64)cdiv(a.Tk, 128) * a.Hkv * parts)), dim3(256), skv, s, a, (const BlockSeen*)blocks, sums, parts);
   if (parts > 1) hipLaunchKernelGGL(range_dkv_sum_k<DHP>, dim3((unsigned)cdiv((i64)a.Tk * a.Hkv, 4)), dim3(256), 0, s, a, sums, parts);
 }
+template <int DHP, bool MOD> static void fwd_few(const RangeAttn& a, float* work, hipStream_t s) {
+  static std::atomic<unsigned long long> mask{0};
+  set_lds(mask, range_fwd_few_k<DHP, MOD>, FEW_SMEM<DHP>);
+  const FewShape f = few_shape(a, work);
+  hipLaunchKernelGGL((range_fwd_few_k<DHP, MOD>), dim3((unsigned)((i64)f.tiles * f.splits * a.Hkv * f.hb)), dim3(256), FEW_SMEM<DHP>, s, a, f);
+  if (f.splits > 1) hipLaunchKernelGGL((range_join_k<bf16, DHP>), dim3((unsigned)cdiv((i64)a.Tq * a.H, 4)), dim3(256), 0, s, a, f);
+}
+bool range_flash_few(const RangeAttn& a) { return (i64)a.Tq * a.H <= 16 * 1024; }
+void launch_range_fwd_flash_few(const RangeAttn& a, float* work, hipStream_t s) {
+  if (a.Tq <= 0) return;
+  if (a.dh <= 64) { if (modified(a)) fwd_few<64, true>(a, work, s); else fwd_few<64, false>(a, work, s); }
+  else if (modified(a)) fwd_few<128, true>(a, work, s);
+  else fwd_few<128, false>(a, work, s);
+}
+size_t range_few_floats(const RangeAttn& a) { return few_floats(a); }
 void launch_range_fwd_flash(const RangeAttn& a, hipStream_t s) {
   if (a.Tq <= 0) return;
   if (a.dh <= 64) { if (modified(a)) fwd<64, true>(a, s); else fwd<64, false>(a, s); }

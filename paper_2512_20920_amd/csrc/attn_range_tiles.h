@@ -27,19 +27,6 @@ __device__ __forceinline__ bf16x8 acc_to_frag(const f32x16& a, int c) {
   return r;
 }
 
-// ---- integers over the 64 lanes, as the sums and maxima of floats ----
-template <int CTRL, int ROW_MASK> __device__ __forceinline__ int dpp_i(int keep, int v) { return __builtin_amdgcn_update_dpp(keep, v, CTRL, ROW_MASK, 0xf, false); }
-__device__ __forceinline__ int wave_imax(int v) {
-  v = max(v, dpp_i<0x111, 0xf>(v, v));
-  v = max(v, dpp_i<0x112, 0xf>(v, v));
-  v = max(v, dpp_i<0x114, 0xf>(v, v));
-  v = max(v, dpp_i<0x118, 0xf>(v, v));
-  v = max(v, dpp_i<0x142, 0xa>(v, v));
-  v = max(v, dpp_i<0x143, 0xc>(v, v));
-  return __builtin_amdgcn_readlane(v, 63);
-}
-__device__ __forceinline__ int wave_imin(int v) { return -1 - wave_imax(-1 - v); }
-
 // ---- tiles ----
 template <int DHP> __device__ __forceinline__ int swz(int r) {
   return DHP == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);

@@ -105,6 +105,12 @@ SHAPES = {
     "width_256": (2, 1, 256, [40, 35], None, {}),
     "width_500": (1, 1, 500, [70], None, {}),
     "many_heads_to_one": (16, 1, 64, [65, 64], None, {}),
+    "forty_heads_to_one": (40, 1, 64, [3, 30], [3, 300], {}),
+    "three_heads_to_one": (6, 2, 128, [30, 11], [70, 11], {}),
+    "next_tokens": (8, 2, 128, [1] * 9, [212, 37, 1001, 450, 1, 777, 128, 0, 1500], {}),
+    "next_tokens_capped": (4, 4, 64, [1] * 40, [(37 * i) % 111 for i in range(40)], dict(cap=10.0, bias=True)),
+    "next_token_of_one": (2, 1, 80, [1], [2500], dict(bias=True)),
+    "few_new_tokens": (4, 2, 128, [3, 4, 1], [900, 4, 33], {}),
 }
 
 
@@ -116,8 +122,7 @@ def _case(name):
     return H, Hkv, dh, sum(q_lens), sum(k_lens or q_lens), lo, hi, at, dict(cap=cap, slopes=slopes)
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("mode", [0, 1])
+@pytest.mark.parametrize("dtype,mode", [("bf16", 1), ("bf16", 256), ("bf16", 512), ("f32", 0), ("f32", 1)])
 @pytest.mark.parametrize("name", list(SHAPES))
 def test_attention(name, mode, dtype):
     H, Hkv, dh, Tq, Tk, lo, hi, at, opt = _case(name)
@@ -139,8 +144,7 @@ def test_attention_strides_and_rows_behind_the_last_document(pad, mode, dtype):
     assert torch.isnan(a.lse[:, Tq:]).all()
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("mode", [0, 1])
+@pytest.mark.parametrize("dtype,mode", [("bf16", 1), ("bf16", 256), ("bf16", 512), ("f32", 0), ("f32", 1)])
 def test_attention_any_ranges(mode, dtype):
     """Ranges that no documents make, out of bounds ones among them, and queries that see nothing."""
     rng = np.random.default_rng(5)
@@ -157,8 +161,7 @@ def test_attention_any_ranges(mode, dtype):
     assert torch.isneginf(a.lse[:, torch.from_numpy(none).cuda()]).all()
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("mode", [0, 1])
+@pytest.mark.parametrize("dtype,mode", [("bf16", 1), ("bf16", 256), ("bf16", 512), ("f32", 0), ("f32", 1)])
 @pytest.mark.parametrize("value", [NAN, float("inf"), float("-inf")])
 def test_attention_values_that_are_not_finite_stay_where_they_are(value, mode, dtype):
     """One document's rows hold NaN or infinities, in each tensor by turns: the other documents' results are what they are
@@ -182,6 +185,18 @@ def test_attention_values_that_are_not_finite_stay_where_they_are(value, mode, d
         row = a.part("o")[50]
         if where in ("k", "v"):
             assert not np.isfinite(row).all()               # and who sees it, gets it
+
+
+@pytest.mark.parametrize("dtype,mode", [("bf16", 256), ("bf16", 512), ("f32", 0)])
+def test_attention_far_apart(mode, dtype):
+    """Queries next to each other whose keys lie far apart: what nobody sees between is left out."""
+    n, m = 70, 40000
+    lo = np.where(np.arange(n) % 2 == 0, 3, m - 130)
+    lo[40:] = 20000 + np.arange(30)
+    hi = lo + 1 + np.arange(n) % 97
+    a = Attention(dtype, 2, 1, 64, n, m)
+    a.run(lo, hi, None, mode)
+    a.check(lo, hi)
 
 
 def test_attention_ranges():
