@@ -352,9 +352,7 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen*
 #pragma unroll
       for (int u = 0; u < 8; u++) myD = fmaf((float)of[kk][u], (float)dof[kk][u], myD);
     myD = both_halves_sum(myD);
-    if (g == 0 && myq < rows) a.dvec[(i64)h * a.Tq + myq] = myD;
   }
-  if (mine.x == mine.y) myD = 0.f;
   const HeadRows rk = {(const unsigned char*)a.k + (i64)kh * a.dh * 2, a.ldk * 2, a.dh * 2}, rv = {(const unsigned char*)a.v + (i64)kh * a.dh * 2, a.ldv * 2, a.dh * 2};
   const unsigned lds0 = lds_address(smem_raw) + (unsigned)wv * (T::BYTES / 4);
   auto issue = [&](const HeadRows& r, int kv, unsigned stage) {
@@ -388,34 +386,50 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen*
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  auto gradients = [&](int kv) {                    // dS in place of S
+  // dS in place of S.  D = <o, dO> carries the rounding of o, which for a query of few keys counts as much as all other roundings: where
+  // one tile holds all keys of a query, its D is summed from the tile's own products instead, D = sum P dP.
+  auto gradients = [&](int kv) {
+    const bool masked = kv < all_from || kv + 64 > all_to, alone = mine.x >= kv && mine.y <= kv + 64;
+    if (masked) partly = true;
     const float d0 = (float)((i64)at - kv - g * 4);
+    const int lo = max(mine.x, kv) - kv - g * 4;
+    const unsigned n = (unsigned)max(min(mine.y, kv + 64) - max(mine.x, kv), 0);
+    auto prob = [&](int j, int e, float* keep) {
+      *keep = 1.f;
+      if constexpr (!MOD) return fast_exp2(fmaf(s[j][e], sf.f, -mylse));
+      float x = s[j][e] * sf.f;
+      if (sf.capped) {
+        const float t = fast_tanh_2(s[j][e] * sf.x2);
+        x = t * sf.cap2;
+        *keep = 1.f - t * t;
+      }
+      if (sf.biased) x = fmaf(-sf.slope2, fabsf(d0 - (float)(j * 32 + (e >> 2) * 8 + (e & 3))), x);
+      return fast_exp2(x - mylse);
+    };
+    auto seen = [&](int j, int e) { return (unsigned)(j * 32 + (e >> 2) * 8 + (e & 3) - lo) < n; };
+    if (__any(alone)) {
+      float sum = 0.f, keep;
+#pragma unroll
+      for (int j = 0; j < 2; j++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) sum += seen(j, e) ? prob(j, e, &keep) * dp[j][e] : 0.f;
+      sum = both_halves_sum(sum);
+      if (alone) myD = sum;
+    }
 #pragma unroll
     for (int j = 0; j < 2; j++)
 #pragma unroll
       for (int e = 0; e < 16; e++) {
-        float x, keep = 1.f;
-        if constexpr (MOD) {
-          x = s[j][e] * sf.f;
-          if (sf.capped) {
-            const float t = fast_tanh_2(s[j][e] * sf.x2);
-            x = t * sf.cap2;
-            keep = 1.f - t * t;
-          }
-          if (sf.biased) x = fmaf(-sf.slope2, fabsf(d0 - (float)(j * 32 + (e >> 2) * 8 + (e & 3))), x);
-          x -= mylse;
-        } else x = fmaf(s[j][e], sf.f, -mylse);
-        s[j][e] = fast_exp2(x) * (dp[j][e] - myD) * keep;
+        float keep;
+        const float p = prob(j, e, &keep);
+        s[j][e] = p * (dp[j][e] - myD) * keep;
       }
-    if (kv < all_from || kv + 64 > all_to) {
-      partly = true;
-      const int lo = max(mine.x, kv) - kv - g * 4;
-      const unsigned n = (unsigned)max(min(mine.y, kv + 64) - max(mine.x, kv), 0);
+    if (masked) {
 #pragma unroll
       for (int j = 0; j < 2; j++)
 #pragma unroll
         for (int e = 0; e < 16; e++)
-          if ((unsigned)(j * 32 + (e >> 2) * 8 + (e & 3) - lo) >= n) s[j][e] = 0.f;
+          if (!seen(j, e)) s[j][e] = 0.f;
     }
 #pragma unroll
     for (int c = 0; c < 4; c++) dsf[c] = acc_to_frag(s[c >> 1], c & 1);
@@ -462,6 +476,7 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen*
     wait_vmcnt<0>();                                // the zero-filled loads past the last tile
     phase_end();
   }
+  if (g == 0 && myq < rows) a.dvec[(i64)h * a.Tq + myq] = myD;
   if (partly && !T::finite(acc)) {
     for (int r = 0; r < 32 && q0 + wv * 32 + r < rows; r++) range_row_dq<bf16>(a, q0 + wv * 32 + r, h, keys, (float*)smem_raw + wv * 2 * DHP);
     return;
