@@ -353,7 +353,8 @@ int revffn_op_attention_bwd_noalloc(int32_t dtype, int32_t kernel_mode, const vo
  * infinity or a NaN (a tile that holds one is then worked out again row by row, which is slow). */
 typedef struct revffn_attn_mask {
   const int32_t *lo, *hi;  /* device [Tq]                                                            */
-  const int32_t *at;       /* device [Tq]: the key row at which query i stands (only the distance bias reads it); NULL = i */
+  const int32_t *at;       /* device [Tq]: the key row at which query i stands, -2^30 .. 2^30 (only the distance bias
+                              reads it); NULL = i                                                    */
   const int32_t *used;     /* device [2] or NULL: query rows and key rows in use, clamped to Tq and Tk; result rows from
                               there on are left as they were.  NULL = all                            */
 } revffn_attn_mask;

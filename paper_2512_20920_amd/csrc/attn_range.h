@@ -36,8 +36,7 @@ __device__ __forceinline__ float range_score(float z, float cap, float slope, in
     z = t * cap;
     *keep = 1.f - t * t;
   }
-  // (at and the keys may be any 32-bit numbers: their distance is taken in 64)
-  return slope != 0.f ? z - slope * fabsf((float)((i64)at - j)) : z;
+  return slope != 0.f ? z - slope * fabsf((float)(at - j)) : z;
 }
 
 // Values of one wave that its other lanes read back: the LDS accesses of a wave are in order, the compiler's need this.

@@ -59,27 +59,6 @@ template <int DHP> __device__ __forceinline__ void spill(float* t, const f32x16 
 #pragma unroll
     for (int e = 0; e < 16; e++) t[(i * 32 + elem_row(e, lane >> 5)) * 32 + (lane & 31)] = acc[i][e];
 }
-// the sum of the waves' tiles for row threadIdx.x & 31, DHP / 8 columns of it; whether all of it is finite
-template <int DHP> __device__ __forceinline__ bool store_sum(const float* sm, float* row, bool ok, int dh, float f) {
-  constexpr int C = DHP * 32 / (NW * 64);
-  const int r = threadIdx.x & 31, c0 = (int)(threadIdx.x >> 5) * C;
-  float z = 0.f;
-#pragma unroll
-  for (int c = 0; c < C; c += 4) {
-    f32x4 v;
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-      float t = 0.f;
-#pragma unroll
-      for (int w = 0; w < NW; w++) t += sm[(w * DHP + c0 + c + i) * 32 + r];
-      z = fmaf(t, 0.f, z);
-      v[i] = t * f;
-    }
-    if (ok && c0 + c < dh) *(f32x4*)(row + c0 + c) = v;
-  }
-  return !ok || z == 0.f;
-}
-
 template <int DHP> __global__ void __launch_bounds__(NW * 64) range_fwd_f32_k(RangeAttn a, FewShape f) {
   extern __shared__ float sm[];                      // NW results [DHP][32], statistics
   int tile, split, head, t0;
@@ -133,10 +112,8 @@ template <int DHP> __global__ void __launch_bounds__(NW * 64) range_dq_f32_k(Ran
   const int rows = rows_in_use(a), keys = keys_in_use(a);
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
   if ((int)blockIdx.x >= tiles) {
-    const int b = ((int)blockIdx.x - tiles) * NW + wv, i = b * 64 + lane;
-    int2 r = i < rows ? key_range(a, i, keys) : make_int2(0, 0);
-    if (r.x == r.y) r = make_int2(INT_MAX, 0);
-    r = make_int2(wave_imin(r.x), wave_imax(r.y));
+    const int b = ((int)blockIdx.x - tiles) * NW + wv;
+    const int2 r = block_seen(a, b, rows, keys, lane);
     if (lane == 0 && b * 64 < a.Tq) blocks[b] = r;
     return;
   }
@@ -176,7 +153,7 @@ template <int DHP> __global__ void __launch_bounds__(NW * 64) range_dq_f32_k(Ran
   spill<DHP>(sm + wv * DHP * 32, acc, lane);
   __syncthreads();
   const FewRow mine = few_row(a, f, tile, head, threadIdx.x & 31, rows);
-  const bool fine = store_sum<DHP>(sm, (float*)a.dq + (i64)mine.i * a.ldq + (i64)mine.h * a.dh, mine.ok, a.dh, a.scale);
+  const bool fine = few_store<float, DHP, NW>(sm, (float*)a.dq + (i64)mine.i * a.ldq + (i64)mine.h * a.dh, mine.ok, a.dh, a.scale);
   if (__syncthreads_or(!fine))
     for (int x = wv; x < 32; x += NW) {
       const FewRow again = few_row(a, f, tile, head, x, rows);
@@ -242,11 +219,11 @@ template <int DHP> __global__ void __launch_bounds__(NW * 64) range_dkv_f32_k(Ra
   const int r = k0 + (int)(threadIdx.x & 31);
   spill<DHP>(sm + wv * DHP * 32, dka, lane);
   __syncthreads();
-  bool fine = store_sum<DHP>(sm, (float*)a.dk + (i64)r * a.ldk + (i64)kh * a.dh, r < keys, a.dh, a.scale);
+  bool fine = few_store<float, DHP, NW>(sm, (float*)a.dk + (i64)r * a.ldk + (i64)kh * a.dh, r < keys, a.dh, a.scale);
   __syncthreads();
   spill<DHP>(sm + wv * DHP * 32, dva, lane);
   __syncthreads();
-  fine &= store_sum<DHP>(sm, (float*)a.dv + (i64)r * a.ldv + (i64)kh * a.dh, r < keys, a.dh, 1.f);
+  fine &= few_store<float, DHP, NW>(sm, (float*)a.dv + (i64)r * a.ldv + (i64)kh * a.dh, r < keys, a.dh, 1.f);
   if (__syncthreads_or(!fine))
     for (int x = wv; x < 32 && k0 + x < keys; x += NW) range_row_dkv<float>(a, k0 + x, kh, rows, keys, sm + wv * 2 * DHP);
 }

@@ -103,6 +103,34 @@ __device__ __forceinline__ void few_finish(const RangeAttn& a, const FewShape& f
       if (again.ok) range_row_fwd<T>(a, again.i, again.h, keys, slow + (threadIdx.x >> 6) * 2 * DHP);
     }
 }
+// The sum of the waves' partial results, [column][32 rows] in LDS each, times f, to row threadIdx.x & 31; whether all of it is finite
+template <class T, int DHP, int NW> __device__ __forceinline__ bool few_store(const float* part, T* row, bool ok, int dh, float f) {
+  constexpr int C = DHP * 32 / (NW * 64);
+  typedef __attribute__((ext_vector_type(4))) T V4;
+  const int r = threadIdx.x & 31, c0 = (int)(threadIdx.x >> 5) * C;
+  float z = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; c += 4) {
+    V4 v;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      float t = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW; w++) t += part[(w * DHP + c0 + c + i) * 32 + r];
+      z = fmaf(t, 0.f, z);
+      v[i] = from_f<T>(t * f);
+    }
+    if (ok && c0 + c < dh) *(V4*)(row + c0 + c) = v;
+  }
+  return !ok || z == 0.f;
+}
+// block b of 64 queries: the first key that some of them see and one past the last (none: INT_MAX, 0)
+__device__ __forceinline__ int2 block_seen(const RangeAttn& a, int b, int rows, int keys, int lane) {
+  const int i = b * 64 + lane;
+  int2 r = i < rows ? key_range(a, i, keys) : make_int2(0, 0);
+  if (r.x == r.y) r = make_int2(INT_MAX, 0);
+  return make_int2(wave_imin(r.x), wave_imax(r.y));
+}
 // joins the splits: one wave per (query row, head), DHP / 64 columns per lane; at most 64 splits
 template <class T, int DHP> __global__ void __launch_bounds__(256) range_join_k(RangeAttn a, FewShape f) {
   __shared__ float slow[4][2 * DHP];

@@ -1,37 +1,55 @@
 // Attention over key ranges on the matrix cores: bf16, heads of up to 128 columns (a multiple of 8).
 #include "attn_range_tiles.h"
 #include "attn_range_few.h"
+#include <stdlib.h>
 
+// Two workgroups fit on a CU: where the whole grid is resident at once, workgroups i and i + 256 share one, so the second 256 take the
+// tiles in the other order, and a long tile shares its CU with a short one.
+__device__ __forceinline__ int paired(int tile, int tiles, int per_tile) {
+  const int first = 256 / per_tile;
+  return (int)gridDim.x <= 512 && tile >= first ? tiles - 1 - (tile - first) : tile;
+}
 // Which tile a workgroup takes (1-D grid of tiles x heads).  Heads are the fastest index, and those that share a key head follow each
 // other 8 apart where there are 8 key heads or more, so that they run on the same XCD (id & 7) and find its keys in that L2.
 __device__ __forceinline__ void place(const RangeAttn& a, int* tile, int* h) {
   const int row = (int)blockIdx.x / a.H, r = (int)blockIdx.x - row * a.H;
-  *tile = row;
+  *tile = paired(row, (a.Tq + 127) / 128, a.H);
   *h = (r % a.Hkv) * a.G + r / a.Hkv;
 }
 
-// The key ranges of 128 queries, as every wave of a workgroup sees them: its own lane's query, all queries' (two per lane)
-struct QueryRanges {
-  int2 r0, r1;             // of queries q0 + lane, q0 + 64 + lane (none: lo = INT_MAX, hi = 0)
-  int first, end;          // over all of them
-  // where the first tile of 64 keys starts, at or after kv, that some query sees; `end`: there is none
-  __device__ __forceinline__ int live_from(int kv) const {
-    if (kv >= end) return end;
-    if (__any((r0.x < kv + 64 && r0.y > kv) || (r1.x < kv + 64 && r1.y > kv))) return kv;
-    const int a = r0.y > kv ? r0.x : INT_MAX, b = r1.y > kv ? r1.x : INT_MAX;
-    return min(wave_imin(min(a, b)), end);
-  }
-};
-__device__ __forceinline__ QueryRanges query_ranges(const RangeAttn& a, int q0, int rows, int keys, int lane) {
-  QueryRanges q;
+// The keys that 128 queries see: from the first to the last, and whether there may be keys between that none sees (neighbouring
+// queries' ranges that don't touch, or a query without any)
+struct QueryRanges { int first, end; bool gaps; };
+struct TwoRanges { int2 r0, r1; };                  // of queries q0 + lane, q0 + 64 + lane (none: lo = INT_MAX, hi = 0)
+__device__ __forceinline__ TwoRanges two_ranges(const RangeAttn& a, int q0, int rows, int keys) {
+  const int lane = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+  TwoRanges t;
   const int2 none = make_int2(INT_MAX, 0);
-  q.r0 = q0 + lane < rows ? key_range(a, q0 + lane, keys) : none;
-  q.r1 = q0 + 64 + lane < rows ? key_range(a, q0 + 64 + lane, keys) : none;
-  if (q.r0.x == q.r0.y) q.r0 = none;
-  if (q.r1.x == q.r1.y) q.r1 = none;
-  q.first = wave_imin(min(q.r0.x, q.r1.x));
-  q.end = wave_imax(max(q.r0.y, q.r1.y));
+  t.r0 = q0 + lane < rows ? key_range(a, q0 + lane, keys) : none;
+  t.r1 = q0 + 64 + lane < rows ? key_range(a, q0 + 64 + lane, keys) : none;
+  if (t.r0.x == t.r0.y) t.r0 = none;
+  if (t.r1.x == t.r1.y) t.r1 = none;
+  return t;
+}
+__device__ __forceinline__ QueryRanges query_ranges(const TwoRanges& t, int q0, int rows, int lane) {
+  QueryRanges q;
+  q.first = wave_imin(min(t.r0.x, t.r1.x));
+  q.end = wave_imax(max(t.r0.y, t.r1.y));
+  auto apart = [](int2 u, int2 v) { return max(u.x, v.x) > min(u.y, v.y); };
+  const int2 over = make_int2(__builtin_amdgcn_readfirstlane(t.r1.x), __builtin_amdgcn_readfirstlane(t.r1.y));
+  int2 n0 = make_int2(__shfl_down(t.r0.x, 1, WAVE), __shfl_down(t.r0.y, 1, WAVE)), n1 = make_int2(__shfl_down(t.r1.x, 1, WAVE), __shfl_down(t.r1.y, 1, WAVE));
+  if (lane == 63) n0 = over;
+  q.gaps = __any((q0 + lane + 1 < rows && apart(t.r0, n0)) || (lane < 63 && q0 + 64 + lane + 1 < rows && apart(t.r1, n1)));
   return q;
+}
+// where the first tile of 64 keys starts, at or after kv, that some query sees; `end`: there is none.  (The ranges are read again: they are
+// not worth four registers in the loops.)
+__device__ __forceinline__ int live_from(const QueryRanges& q, int kv, int q0, int rows, int keys) {
+  if (kv >= q.end) return q.end;
+  if (!q.gaps) return kv;
+  const TwoRanges t = two_ranges(args_again(), q0, rows, keys);
+  if (__any((t.r0.x < kv + 64 && t.r0.y > kv) || (t.r1.x < kv + 64 && t.r1.y > kv))) return kv;
+  return min(wave_imin(min(t.r0.y > kv ? t.r0.x : INT_MAX, t.r1.y > kv ? t.r1.x : INT_MAX)), q.end);
 }
 
 // ------------------------------------------------------------------------------------
@@ -40,7 +58,7 @@ __device__ __forceinline__ QueryRanges query_ranges(const RangeAttn& a, int q0, 
 // barrier behind each: in the first a wave takes the maximum and half of the exponentials and reads the next tile's key
 // fragments, in the second it multiplies those and P V of this tile, with the other half of the exponentials between.
 // ------------------------------------------------------------------------------------
-template <int DHP, bool MOD>
+template <int DHP, int MOD>
 __global__ void __launch_bounds__(256, 2) range_fwd_k(RangeAttn a) {
   typedef Tiles<DHP> T;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem_raw[];      // K, V, K, V
@@ -51,19 +69,18 @@ __global__ void __launch_bounds__(256, 2) range_fwd_k(RangeAttn a) {
   if (q0 >= rows) return;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
   const int myq = q0 + wv * 32 + (lane & 31), kh = h / a.G;
-  const QueryRanges qr = query_ranges(a, q0, rows, keys, lane);
+  const QueryRanges qr = query_ranges(two_ranges(a, q0, rows, keys), q0, rows, lane);
   const int2 mine = myq < rows ? key_range(a, myq, keys) : make_int2(INT_MIN, INT_MAX);    // (a row that is not there needs no mask)
   const int all_from = wave_imax(mine.x), all_to = wave_imin(mine.y);                      // every query sees the keys between
   const ScoreForm sf = score_form(a, h);
-  const int at = MOD && sf.biased ? (a.at ? a.at[min(myq, rows - 1)] : myq) : 0;
-  bf16* o = (bf16*)a.out + (i64)myq * a.ldo + (i64)h * a.dh;
+  const int at = MOD & BIASED ? (a.at ? a.at[min(myq, rows - 1)] : myq) : 0;
 
   bf16x8 qf[T::KK];
   T::load_frags((const bf16*)a.q + (i64)myq * a.ldq + (i64)h * a.dh, myq < rows, a.dh, g, qf);
   const HeadRows rk = {(const unsigned char*)a.k + (i64)kh * a.dh * 2, a.ldk * 2, a.dh * 2}, rv = {(const unsigned char*)a.v + (i64)kh * a.dh * 2, a.ldv * 2, a.dh * 2};
   const unsigned lds0 = lds_address(smem_raw) + (unsigned)wv * (T::BYTES / 4);
   auto issue = [&](const HeadRows& r, int kv, unsigned stage) {             // 16 of the tile's rows
-    T::load16(rows_buffer(r, kv, min(64, qr.end - kv)), (unsigned)r.ldb, r.width, wv * 16, lds0 + stage * T::BYTES, lane);
+    T::load16(rows_buffer(r, kv, min(64, qr.end - kv)), (unsigned)r.ldb, r.width, wv * 16, lds0 + stage * T::BYTES);
   };
   const unsigned rbase = T::row_base(lane), cbase = T::col_base(lane);
   f32x16 oacc[T::DT] = {}, s[2];
@@ -87,16 +104,13 @@ __global__ void __launch_bounds__(256, 2) range_fwd_k(RangeAttn a) {
   };
   // scores to their final form in units of log2 (MOD), and those of keys that are not seen to -infinity
   auto finish = [&](int kv) {
-    if constexpr (MOD) {
-      const float d0 = (float)((i64)at - kv - g * 4);
+    if constexpr (MOD != 0) {
+      const float d0 = (float)(at - kv - g * 4);
+      float keep;
 #pragma unroll
       for (int j = 0; j < 2; j++)
 #pragma unroll
-        for (int e = 0; e < 16; e++) {
-          float x = sf.capped ? fast_tanh_2(s[j][e] * sf.x2) * sf.cap2 : s[j][e] * sf.f;
-          if (sf.biased) x = fmaf(-sf.slope2, fabsf(d0 - (float)(j * 32 + (e >> 2) * 8 + (e & 3))), x);
-          s[j][e] = x;
-        }
+        for (int e = 0; e < 16; e++) s[j][e] = final_score<MOD>(sf, s[j][e], d0 - (float)(j * 32 + (e >> 2) * 8 + (e & 3)), &keep);
     }
     if (kv < all_from || kv + 64 > all_to) {
       partly = true;
@@ -109,13 +123,13 @@ __global__ void __launch_bounds__(256, 2) range_fwd_k(RangeAttn a) {
           if ((unsigned)(j * 32 + (e >> 2) * 8 + (e & 3) - lo) >= n) s[j][e] = -INFINITY;
     }
   };
-  const float unit = MOD ? 1.f : sf.f;              // (without MOD the scale is positive and goes into the exponential)
+  const float unit = MOD != 0 ? 1.f : sf.f;              // (without MOD the scale is positive and goes into the exponential)
   float ms = 0.f;
   auto exponentials = [&](f32x16 x, int half) {
     float rs[2] = {};
 #pragma unroll
     for (int e = 0; e < 16; e++) {
-      x[e] = fast_exp2(MOD ? x[e] - ms : fmaf(x[e], unit, -ms));
+      x[e] = fast_exp2(MOD != 0 ? x[e] - ms : fmaf(x[e], unit, -ms));
       rs[e & 1] += x[e];
     }
     l += rs[0] + rs[1];
@@ -123,7 +137,7 @@ __global__ void __launch_bounds__(256, 2) range_fwd_k(RangeAttn a) {
     pf[half * 2 + 1] = acc_to_frag(x, 1);
   };
   if (qr.first < qr.end) {
-    int kv = qr.first, kv1 = qr.live_from(kv + 64), kv2;                    // this tile, the next one, the one after
+    int kv = qr.first, kv1 = live_from(qr, kv + 64, q0, rows, keys), kv2;                    // this tile, the next one, the one after
     issue(rk, kv, 0); issue(rk, kv1, 2); issue(rv, kv, 1);
     T::arrived(qf);
     wait_vmcnt<2 * T::LOADS>();                     // the first keys
@@ -135,7 +149,7 @@ __global__ void __launch_bounds__(256, 2) range_fwd_k(RangeAttn a) {
     phase_end();
     // the keys read in the phase before and the values just read make room
     auto softmax = [&](unsigned st) {
-      kv2 = qr.live_from(kv1 + 64);
+      kv2 = live_from(qr, kv1 + 64, q0, rows, keys);
       issue(rk, kv2, st);
       issue(rv, kv1, st ^ 2u ^ 1u);
       read_k(st ^ 2u, 0);
@@ -195,13 +209,14 @@ __global__ void __launch_bounds__(256, 2) range_fwd_k(RangeAttn a) {
     phase_end();
   }
   if (partly && !T::finite(oacc)) {                 // a value that is not finite: seen, or only in a tile with seen ones?
-    for (int r = 0; r < 32 && q0 + wv * 32 + r < rows; r++) range_row_fwd<bf16>(a, q0 + wv * 32 + r, h, keys, (float*)smem_raw + wv * 2 * DHP);
+    for (int r = 0; r < 32 && q0 + wv * 32 + r < rows; r++) range_row_fwd<bf16>(args_again(), q0 + wv * 32 + r, h, keys, (float*)smem_raw + wv * 2 * DHP);
     return;
   }
   l = both_halves_sum(l);
   if (myq < rows) {
-    T::store(o, oacc, l == 0.f ? 0.f : 1.0f / l, a.dh, g);
-    if (g == 0 && a.lse) a.lse[(i64)h * a.Tq + myq] = l == 0.f ? -INFINITY : (m + __log2f(l)) * LN2;
+    const RangeAttn b = args_again();
+    T::store((bf16*)b.out + (i64)myq * b.ldo + (i64)h * b.dh, oacc, l == 0.f ? 0.f : 1.0f / l, b.dh, g);
+    if (g == 0 && b.lse) b.lse[(i64)h * b.Tq + myq] = l == 0.f ? -INFINITY : (m + __log2f(l)) * LN2;
   }
 }
 
@@ -210,8 +225,15 @@ __global__ void __launch_bounds__(256, 2) range_fwd_k(RangeAttn a) {
 // touches, so nothing waits at a barrier until the partial results meet.  A single token's query against a long run of keys
 // reads every key and value once, for all heads that share them: that reading bounds it.
 // ------------------------------------------------------------------------------------
+// a wave's result to its part of LDS, [column][32 rows]
+template <int DT> __device__ __forceinline__ void put_partial(float* mine, const f32x16 (&acc)[DT], int lane) {
+#pragma unroll
+  for (int d = 0; d < DT; d++)
+#pragma unroll
+    for (int e = 0; e < 16; e++) mine[(d * 32 + (e >> 2) * 8 + (lane >> 5) * 4 + (e & 3)) * 32 + (lane & 31)] = acc[d][e];
+}
 template <int DHP> constexpr unsigned FEW_SMEM = 4 * Tiles<DHP>::BYTES + 4 * 256;       // the waves' K and V (then their results), statistics
-template <int DHP, bool MOD>
+template <int DHP, int MOD>
 __global__ void __launch_bounds__(256, 2) range_fwd_few_k(RangeAttn a, FewShape f) {
   typedef Tiles<DHP> T;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem_raw[];
@@ -223,15 +245,15 @@ __global__ void __launch_bounds__(256, 2) range_fwd_few_k(RangeAttn a, FewShape 
   const FewRow row = few_row(a, f, tile, head, lane & 31, rows);
   const FewKeys fk = few_keys(a, f, row, split, keys, &t0);
   const ScoreForm sf = score_form(a, row.h);
-  const int at = MOD && sf.biased && row.ok ? (a.at ? a.at[row.i] : row.i) : 0;
+  const int at = (MOD & BIASED) && row.ok ? (a.at ? a.at[row.i] : row.i) : 0;
   const HeadRows rk = {(const unsigned char*)a.k + (i64)kh * a.dh * 2, a.ldk * 2, a.dh * 2}, rv = {(const unsigned char*)a.v + (i64)kh * a.dh * 2, a.ldv * 2, a.dh * 2};
   unsigned char* tK = smem_raw + wv * T::BYTES;      // 32 rows of K, 32 of V
   const unsigned aK = lds_address(smem_raw) + (unsigned)wv * T::BYTES, aV = aK + T::BYTES / 2;
   auto issue = [&](const HeadRows& r, int t, unsigned dst) {
     const int kv = t < fk.t1 ? fk.first + t * 32 : 0, n = t < fk.t1 ? min(32, fk.end - kv) : 0;
     const __amdgpu_buffer_rsrc_t rs = rows_buffer(r, kv, n);
-    T::load16(rs, (unsigned)r.ldb, r.width, 0, dst, lane);
-    T::load16(rs, (unsigned)r.ldb, r.width, 16, dst + 16 * T::ROW, lane);
+    T::load16(rs, (unsigned)r.ldb, r.width, 0, dst);
+    T::load16(rs, (unsigned)r.ldb, r.width, 16, dst + 16 * T::ROW);
   };
   int t = fk.live_from(t0 + wv, 4);
   issue(rk, t, aK);
@@ -256,18 +278,14 @@ __global__ void __launch_bounds__(256, 2) range_fwd_few_k(RangeAttn a, FewShape 
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
     issue(rk, next, aK);
-    const float d0 = (float)((i64)at - kv - g * 4);
+    const float d0 = (float)(at - kv - g * 4);
     const int lo = max(fk.r.x, kv) - kv - g * 4;
     const unsigned n = (unsigned)max(min(fk.r.y, kv + 32) - max(fk.r.x, kv), 0);
     float mx = -INFINITY;
 #pragma unroll
     for (int e = 0; e < 16; e++) {
       const int c = (e >> 2) * 8 + (e & 3);
-      float y;
-      if constexpr (MOD) {
-        y = sf.capped ? fast_tanh_2(s[e] * sf.x2) * sf.cap2 : s[e] * sf.f;
-        if (sf.biased) y = fmaf(-sf.slope2, fabsf(d0 - (float)c), y);
-      } else y = s[e] * sf.f;
+      float keep, y = final_score<MOD>(sf, s[e], d0 - (float)c, &keep);
       if ((unsigned)(c - lo) >= n) y = -INFINITY;
       s[e] = y;
       mx = fmaxf(mx, y);
@@ -298,10 +316,7 @@ __global__ void __launch_bounds__(256, 2) range_fwd_few_k(RangeAttn a, FewShape 
   wait_vmcnt<0>();                                  // the zero-filled loads past the last tile
   l = both_halves_sum(l);
   float *stats = (float*)(smem_raw + 4 * T::BYTES), *mine = (float*)tK;
-#pragma unroll
-  for (int d = 0; d < T::DT; d++)
-#pragma unroll
-    for (int e = 0; e < 16; e++) mine[(d * 32 + (e >> 2) * 8 + g * 4 + (e & 3)) * 32 + (lane & 31)] = acc[d][e];
+  put_partial<T::DT>(mine, acc, lane);
   if (g == 0) { stats[wv * 64 + lane] = m; stats[wv * 64 + 32 + lane] = l; }
   __syncthreads();
   few_finish<bf16, DHP, 4>(a, f, tile, split, head, rows, keys, (const float*)smem_raw, stats, (float*)smem_raw);
@@ -315,7 +330,7 @@ __global__ void __launch_bounds__(256, 2) range_fwd_few_k(RangeAttn a, FewShape 
 // block of 64 queries: the first key that some query sees and one past the last (none: INT_MAX, 0), and between which keys all see
 typedef int4 BlockSeen;
 
-template <int DHP, bool MOD>
+template <int DHP, int MOD>
 __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen* __restrict__ blocks) {
   typedef Tiles<DHP> T;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem_raw[];      // K, K, K, V, V
@@ -324,9 +339,10 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen*
   qt = (a.Tq + 127) / 128 - 1 - qt;
   const int rows = rows_in_use(a), keys = keys_in_use(a), q0 = qt * 128;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
-  const QueryRanges qr = query_ranges(a, q0, rows, keys, lane);
+  const TwoRanges two = two_ranges(a, q0, rows, keys);
+  const QueryRanges qr = query_ranges(two, q0, rows, lane);
   if (h == 0 && wv < 2) {                           // (a row in use that sees nothing leaves no key that all see)
-    const int2 r = wv ? qr.r1 : qr.r0;
+    const int2 r = wv ? two.r1 : two.r0;
     const bool in = q0 + wv * 64 + lane < rows, sees = r.x < r.y;
     const int4 b = make_int4(wave_imin(r.x), wave_imax(r.y), wave_imax(sees ? r.x : in ? INT_MAX : INT_MIN), wave_imin(sees ? r.y : in ? 0 : INT_MAX));
     if (lane == 0 && q0 + wv * 64 < a.Tq) blocks[qt * 2 + wv] = b;
@@ -336,7 +352,7 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen*
   const int2 mine = myq < rows ? key_range(a, myq, keys) : make_int2(INT_MIN, INT_MAX);
   const int all_from = wave_imax(mine.x), all_to = wave_imin(mine.y);
   const ScoreForm sf = score_form(a, h);
-  const int at = MOD && sf.biased ? (a.at ? a.at[min(myq, rows - 1)] : myq) : 0;
+  const int at = MOD & BIASED ? (a.at ? a.at[min(myq, rows - 1)] : myq) : 0;
 
   bf16x8 qf[T::KK], dof[T::KK];
   T::load_frags((const bf16*)a.q + (i64)myq * a.ldq + (i64)h * a.dh, myq < rows, a.dh, g, qf);
@@ -356,7 +372,7 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen*
   const HeadRows rk = {(const unsigned char*)a.k + (i64)kh * a.dh * 2, a.ldk * 2, a.dh * 2}, rv = {(const unsigned char*)a.v + (i64)kh * a.dh * 2, a.ldv * 2, a.dh * 2};
   const unsigned lds0 = lds_address(smem_raw) + (unsigned)wv * (T::BYTES / 4);
   auto issue = [&](const HeadRows& r, int kv, unsigned stage) {
-    T::load16(rows_buffer(r, kv, min(64, qr.end - kv)), (unsigned)r.ldb, r.width, wv * 16, lds0 + stage * T::BYTES, lane);
+    T::load16(rows_buffer(r, kv, min(64, qr.end - kv)), (unsigned)r.ldb, r.width, wv * 16, lds0 + stage * T::BYTES);
   };
   const unsigned rbase = T::row_base(lane), cbase = T::col_base(lane);
   f32x16 acc[T::DT] = {}, s[2], dp[2];
@@ -391,20 +407,13 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen*
   auto gradients = [&](int kv) {
     const bool masked = kv < all_from || kv + 64 > all_to, alone = mine.x >= kv && mine.y <= kv + 64;
     if (masked) partly = true;
-    const float d0 = (float)((i64)at - kv - g * 4);
-    const int lo = max(mine.x, kv) - kv - g * 4;
+    float d0 = (float)(at - kv - g * 4);
+    int lo = max(mine.x, kv) - kv - g * 4;
     const unsigned n = (unsigned)max(min(mine.y, kv + 64) - max(mine.x, kv), 0);
     auto prob = [&](int j, int e, float* keep) {
+      if constexpr (MOD != 0) return fast_exp2(final_score<MOD>(sf, s[j][e], d0 - (float)(j * 32 + (e >> 2) * 8 + (e & 3)), keep) - mylse);
       *keep = 1.f;
-      if constexpr (!MOD) return fast_exp2(fmaf(s[j][e], sf.f, -mylse));
-      float x = s[j][e] * sf.f;
-      if (sf.capped) {
-        const float t = fast_tanh_2(s[j][e] * sf.x2);
-        x = t * sf.cap2;
-        *keep = 1.f - t * t;
-      }
-      if (sf.biased) x = fmaf(-sf.slope2, fabsf(d0 - (float)(j * 32 + (e >> 2) * 8 + (e & 3))), x);
-      return fast_exp2(x - mylse);
+      return fast_exp2(fmaf(s[j][e], sf.f, -mylse));
     };
     auto seen = [&](int j, int e) { return (unsigned)(j * 32 + (e >> 2) * 8 + (e & 3) - lo) < n; };
     if (__any(alone)) {
@@ -414,7 +423,8 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen*
 #pragma unroll
         for (int e = 0; e < 16; e++) sum += seen(j, e) ? prob(j, e, &keep) * dp[j][e] : 0.f;
       sum = both_halves_sum(sum);
-      if (alone) myD = sum;
+      if (alone) myD = sum;                         // (the probabilities are worked out twice, not kept)
+      asm volatile("" : "+v"(mylse), "+v"(lo), "+v"(d0));
     }
 #pragma unroll
     for (int j = 0; j < 2; j++)
@@ -435,7 +445,7 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen*
     for (int c = 0; c < 4; c++) dsf[c] = acc_to_frag(s[c >> 1], c & 1);
   };
   if (qr.first < qr.end) {
-    int kv = qr.first, kv1 = qr.live_from(kv + 64), kv2;
+    int kv = qr.first, kv1 = live_from(qr, kv + 64, q0, rows, keys), kv2;
     issue(rk, kv, 0); issue(rv, kv, 3); issue(rk, kv1, 1); issue(rv, kv1, 4);
     T::arrived(qf);
     T::arrived(dof);
@@ -448,7 +458,7 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen*
     phase_end();
     // the values just read and the keys read for the second time make room
     auto probabilities = [&]() {
-      kv2 = qr.live_from(kv1 + 64);
+      kv2 = live_from(qr, kv1 + 64, q0, rows, keys);
       issue(rk, kv2, before);
       issue(rv, kv2, sv);
       gradients(kv);
@@ -476,12 +486,13 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen*
     wait_vmcnt<0>();                                // the zero-filled loads past the last tile
     phase_end();
   }
-  if (g == 0 && myq < rows) a.dvec[(i64)h * a.Tq + myq] = myD;
+  const RangeAttn b = args_again();
+  if (g == 0 && myq < rows) b.dvec[(i64)h * b.Tq + myq] = myD;
   if (partly && !T::finite(acc)) {
-    for (int r = 0; r < 32 && q0 + wv * 32 + r < rows; r++) range_row_dq<bf16>(a, q0 + wv * 32 + r, h, keys, (float*)smem_raw + wv * 2 * DHP);
+    for (int r = 0; r < 32 && q0 + wv * 32 + r < rows; r++) range_row_dq<bf16>(args_again(), q0 + wv * 32 + r, h, keys, (float*)smem_raw + wv * 2 * DHP);
     return;
   }
-  if (myq < rows) T::store((bf16*)a.dq + (i64)myq * a.ldq + (i64)h * a.dh, acc, a.scale, a.dh, g);
+  if (myq < rows) T::store((bf16*)b.dq + (i64)myq * b.ldq + (i64)h * b.dh, acc, b.scale, b.dh, g);
 }
 
 // ------------------------------------------------------------------------------------
@@ -492,11 +503,11 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen*
 // kernel below.
 // ------------------------------------------------------------------------------------
 template <int DHP> constexpr unsigned DKV_STAGE = 2 * Tiles<DHP>::BYTES + 5 * 256;      // Q, dO, lse, D, lo, hi, at
-template <int DHP, bool MOD>
+template <int DHP, int MOD>
 __global__ void __launch_bounds__(256, 2) range_bwd_dkv_k(RangeAttn a, const BlockSeen* __restrict__ blocks, float* __restrict__ sums, int parts) {
   typedef Tiles<DHP> T;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem_raw[];      // 2 stages
-  const int per = a.Hkv * parts, kt = (int)blockIdx.x / per, r0 = (int)blockIdx.x - kt * per, kh = r0 % a.Hkv, part = r0 / a.Hkv;
+  const int per = a.Hkv * parts, row = (int)blockIdx.x / per, r0 = (int)blockIdx.x - row * per, kt = paired(row, (a.Tk + 127) / 128, per), kh = r0 % a.Hkv, part = r0 / a.Hkv;
   const int rows = rows_in_use(a), keys = keys_in_use(a), k0 = kt * 128;
   if (k0 >= keys) return;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
@@ -525,7 +536,7 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dkv_k(RangeAttn a, const Blo
         while (!live) {
           base += 64;
           if (base > b1 || b1 < 0) { blk = -1; return; }
-          const int b = base + lane;
+          const int b = base + lane_now();
           const int2 t = b <= b1 ? seen2[2 * (i64)b] : make_int2(INT_MAX, 0);
           live = __ballot(t.x < k0 + 128 && t.y > k0);
         }
@@ -541,16 +552,18 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dkv_k(RangeAttn a, const Blo
     const unsigned dst = lds0 + (unsigned)stage * DKV_STAGE<DHP>;
     const int h = kh * a.G + head, n = min(64, rows - b * 64);
     const HeadRows rq = {(const unsigned char*)a.q + (i64)h * a.dh * 2, a.ldq * 2, a.dh * 2}, ro = {(const unsigned char*)a.d_o + (i64)h * a.dh * 2, a.ldo * 2, a.dh * 2};
-    T::load16(rows_buffer(rq, b * 64, n), (unsigned)rq.ldb, rq.width, wv * 16, dst + wv * (T::BYTES / 4), lane);
-    T::load16(rows_buffer(ro, b * 64, n), (unsigned)ro.ldb, ro.width, wv * 16, dst + T::BYTES + wv * (T::BYTES / 4), lane);
-    const unsigned words = dst + 2 * T::BYTES, off = (unsigned)lane * 4u;
+    T::load16(rows_buffer(rq, b * 64, n), (unsigned)rq.ldb, rq.width, wv * 16, dst + wv * (T::BYTES / 4));
+    T::load16(rows_buffer(ro, b * 64, n), (unsigned)ro.ldb, ro.width, wv * 16, dst + T::BYTES + wv * (T::BYTES / 4));
+    const unsigned words = dst + 2 * T::BYTES, off = (unsigned)lane_now() * 4u;
     if (wv == 0) load_lds_b32(words_buffer(a.lse + (i64)h * a.Tq, b * 64, n), words, off);
     if (wv == 1) load_lds_b32(words_buffer(a.dvec + (i64)h * a.Tq, b * 64, n), words + 256u, off);
     if (wv == 2) load_lds_b32(words_buffer(a.lo, b * 64, n), words + 512u, off);
     if (wv == 3) load_lds_b32(words_buffer(a.hi, b * 64, n), words + 768u, off);
-    if (MOD && wv == 0 && a.slopes && a.at) load_lds_b32(words_buffer(a.at, b * 64, n), words + 1024u, off);
+    if constexpr (MOD & BIASED) {
+      if (wv == 0 && a.at) load_lds_b32(words_buffer(a.at, b * 64, n), words + 1024u, off);
+      if (wv == 0 && !a.at) ((int*)(smem_raw + (unsigned)stage * DKV_STAGE<DHP> + 2 * T::BYTES + 1024u))[off / 4] = b * 64 + (int)off / 4;
+    }
   };
-  const unsigned rbase = T::row_base(lane), cbase = T::col_base(lane);
   bool partly = false;
   next();
   if (blk >= 0) issue(blk, hg, 0);
@@ -573,8 +586,8 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dkv_k(RangeAttn a, const Blo
       const int *cLo = (const int*)(cD + 64), *cHi = cLo + 64, *cAt = cHi + 64;
 #pragma unroll 1
       for (int j = 0; j < 2; j++) {
-        unsigned rb = rbase + (unsigned)(j * 32 * T::ROW), cb = cbase;
-        asm volatile("" : "+v"(rb), "+v"(cb));
+        const int lane = lane_now(), g = lane >> 5, mykv = kw + (lane & 31);
+        const unsigned rb = T::row_base(lane) + (unsigned)(j * 32 * T::ROW), cb = T::col_base(lane);
         f32x16 s = {}, dp = {};
         bf16x8 f[2][2];
         auto read_rows = [&](bf16x8 (&x)[2], int kk) {
@@ -594,22 +607,20 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dkv_k(RangeAttn a, const Blo
 #pragma unroll
         for (int eb = 0; eb < 4; eb++) {
           const int q4 = j * 32 + eb * 8 + g * 4;
+          if constexpr (DHP == 128) __builtin_amdgcn_sched_barrier(0);      // (all reads at once would cost the registers that are short here)
           const float4 l4 = *(const float4*)(cL + q4), d4 = *(const float4*)(cD + q4);
           const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, dv[4] = {d4.x, d4.y, d4.z, d4.w};
+          int av[4];
+          if constexpr (MOD & BIASED) {
+            const int4 a4 = *(const int4*)(cAt + q4);
+            av[0] = a4.x; av[1] = a4.y; av[2] = a4.z; av[3] = a4.w;
+          }
 #pragma unroll
           for (int i = 0; i < 4; i++) {
             const int e = eb * 4 + i;
             float x, keep = 1.f;
-            if constexpr (MOD) {
-              x = s[e] * sf.f;
-              if (sf.capped) {
-                const float t = fast_tanh_2(s[e] * sf.x2);
-                x = t * sf.cap2;
-                keep = 1.f - t * t;
-              }
-              if (sf.biased) x = fmaf(-sf.slope2, fabsf((float)((i64)(a.at ? cAt[q4 + i] : b * 64 + q4 + i) - mykv)), x);
-              x = fmaf(lv[i], -LOG2E, x);
-            } else x = fmaf(s[e], sf.f, -lv[i] * LOG2E);
+            if constexpr (MOD != 0) x = fmaf(lv[i], -LOG2E, final_score<MOD>(sf, s[e], MOD & BIASED ? (float)(av[i] - mykv) : 0.f, &keep));
+            else x = fmaf(s[e], sf.f, -lv[i] * LOG2E);
             s[e] = fast_exp2(x);
             dp[e] = s[e] * (dp[e] - dv[i]) * keep;
           }
@@ -618,6 +629,7 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dkv_k(RangeAttn a, const Blo
 #pragma unroll
           for (int eb = 0; eb < 4; eb++) {
             const int q4 = j * 32 + eb * 8 + g * 4;
+            if constexpr (DHP == 128) __builtin_amdgcn_sched_barrier(0);
             const int4 l4 = *(const int4*)(cLo + q4), h4 = *(const int4*)(cHi + q4);
             const int lo[4] = {l4.x, l4.y, l4.z, l4.w}, hi[4] = {h4.x, h4.y, h4.z, h4.w};
 #pragma unroll
@@ -664,12 +676,13 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dkv_k(RangeAttn a, const Blo
     return;
   }
   if (partly && (!T::finite(dkacc) || !T::finite(dvacc))) {
-    for (int r = 0; r < 32 && kw + r < keys; r++) range_row_dkv<bf16>(a, kw + r, kh, rows, keys, (float*)smem_raw + wv * 2 * DHP);
+    for (int r = 0; r < 32 && kw + r < keys; r++) range_row_dkv<bf16>(args_again(), kw + r, kh, rows, keys, (float*)smem_raw + wv * 2 * DHP);
     return;
   }
   if (mykv < keys) {
-    T::store((bf16*)a.dk + (i64)mykv * a.ldk + (i64)kh * a.dh, dkacc, a.scale, a.dh, g);
-    T::store((bf16*)a.dv + (i64)mykv * a.ldv + (i64)kh * a.dh, dvacc, 1.0f, a.dh, g);
+    const RangeAttn b = args_again();
+    T::store((bf16*)b.dk + (i64)mykv * b.ldk + (i64)kh * b.dh, dkacc, b.scale, b.dh, g);
+    T::store((bf16*)b.dv + (i64)mykv * b.ldv + (i64)kh * b.dh, dvacc, 1.0f, b.dh, g);
   }
 }
 // the sum of the parts, one wave per key row and head: 2 columns per lane (DHP = 64: one)
@@ -700,6 +713,280 @@ template <int DHP> __global__ void __launch_bounds__(256) range_dkv_sum_k(RangeA
     if (lane * C + c < a.dh) { dk[lane * C + c] = (bf16)(k[c] * a.scale); dv[lane * C + c] = (bf16)v[c]; }
 }
 
+// ------------------------------------------------------------------------------------
+// Backward for few rows: dQ of 32 rows, then dK/dV of 32 keys per workgroup, the keys (the blocks of 32 queries and the heads that share the
+// key head) shared out to the waves, each with tiles of its own in LDS.
+// ------------------------------------------------------------------------------------
+// a^T[row, lane] = tile a's rows x fa, the same for b; the next fragments are read while these are multiplied
+template <int DHP> __device__ __forceinline__ void rows_times2(f32x16& a, f32x16& b, const unsigned char* ta, const unsigned char* tb, unsigned rbase,
+                                                               const bf16x8 (&fa)[DHP / 16], const bf16x8 (&fb)[DHP / 16]) {
+  bf16x8 x[2][2];
+  auto read = [&](bf16x8 (&y)[2], int kk) {
+    y[0] = *(const bf16x8*)(ta + (rbase ^ (unsigned)(kk * 32)));
+    y[1] = *(const bf16x8*)(tb + (rbase ^ (unsigned)(kk * 32)));
+  };
+  a = f32x16{};
+  b = f32x16{};
+  read(x[0], 0);
+#pragma unroll
+  for (int kk = 0; kk < DHP / 16; kk++) {
+    if (kk < DHP / 16 - 1) read(x[(kk + 1) & 1], kk + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    a = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[kk & 1][0], fa[kk], a, 0, 0, 0);
+    b = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[kk & 1][1], fb[kk], b, 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+// The last workgroups of the launch (from `tiles` on) note which keys the blocks of 64 queries see, a wave per block.
+template <int DHP, int MOD>
+__global__ void __launch_bounds__(256, 2) range_dq_few_k(RangeAttn a, FewShape f, int tiles, int2* __restrict__ blocks) {
+  typedef Tiles<DHP> T;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem_raw[];
+  const int rows = rows_in_use(a), keys = keys_in_use(a);
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
+  if ((int)blockIdx.x >= tiles) {
+    const int b = ((int)blockIdx.x - tiles) * 4 + wv;
+    const int2 r = block_seen(a, b, rows, keys, lane);
+    if (lane == 0 && b * 64 < a.Tq) blocks[b] = r;
+    return;
+  }
+  int tile, split, head, t0;
+  few_place(a, f, (int)blockIdx.x, &tile, &split, &head);
+  tile = f.tiles - 1 - tile;                        // late queries tend to have the long ranges
+  if (tile * f.qpt >= rows) return;
+  const int kh = head % a.Hkv;
+  const FewRow row = few_row(a, f, tile, head, lane & 31, rows);
+  const FewKeys fk = few_keys(a, f, row, 0, keys, &t0);
+  const ScoreForm sf = score_form(a, row.h);
+  const int at = (MOD & BIASED) && row.ok ? (a.at ? a.at[row.i] : row.i) : 0;
+  const HeadRows rk = {(const unsigned char*)a.k + (i64)kh * a.dh * 2, a.ldk * 2, a.dh * 2}, rv = {(const unsigned char*)a.v + (i64)kh * a.dh * 2, a.ldv * 2, a.dh * 2};
+  unsigned char* tK = smem_raw + wv * T::BYTES;      // 32 rows of K, 32 of V
+  const unsigned aK = lds_address(smem_raw) + (unsigned)wv * T::BYTES, aV = aK + T::BYTES / 2;
+  auto issue = [&](const HeadRows& r, int t, unsigned dst) {
+    const int kv = fk.first + t * 32;
+    const __amdgpu_buffer_rsrc_t rs = rows_buffer(r, kv, min(32, fk.end - kv));
+    T::load16(rs, (unsigned)r.ldb, r.width, 0, dst);
+    T::load16(rs, (unsigned)r.ldb, r.width, 16, dst + 16 * T::ROW);
+  };
+  int t = fk.live_from(t0 + wv, 4);
+  if (t < fk.t1) {
+    issue(rv, t, aV);
+    issue(rk, t, aK);
+  }
+  const i64 orow = (i64)row.i * a.ldo + (i64)row.h * a.dh, srow = (i64)row.h * a.Tq + row.i;
+  bf16x8 qf[T::KK], dof[T::KK];
+  float L = row.ok ? a.lse[srow] * LOG2E : 0.f, D = 0.f;
+  T::load_frags((const bf16*)a.d_o + orow, row.ok, a.dh, g, dof);
+  T::load_frags((const bf16*)a.o + orow, row.ok, a.dh, g, qf);
+#pragma unroll
+  for (int kk = 0; kk < T::KK; kk++)
+#pragma unroll
+    for (int u = 0; u < 8; u++) D = fmaf((float)qf[kk][u], (float)dof[kk][u], D);
+  D = both_halves_sum(D);
+  T::load_frags((const bf16*)a.q + (i64)row.i * a.ldq + (i64)row.h * a.dh, row.ok, a.dh, g, qf);
+  if (L == -INFINITY) L = 0.f;
+  T::arrived(qf);
+  T::arrived(dof);
+  asm volatile("" : "+v"(L), "+v"(D));
+  const unsigned rbase = T::row_base(lane), cbase = T::col_base(lane);
+  f32x16 acc[T::DT] = {};
+  bool own = wv == 0;                               // this wave has the row's D
+  while (t < fk.t1) {
+    const int kv = fk.first + t * 32, next = fk.live_from(t + 4, 4);
+    wait_vmcnt<0>();
+    f32x16 dp, s;
+    rows_times2<DHP>(dp, s, tK + T::BYTES / 2, tK, rbase, dof, qf);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    if (next < fk.t1) issue(rv, next, aV);
+    const float d0 = (float)(at - kv - g * 4);
+    const int lo = max(fk.r.x, kv) - kv - g * 4;
+    const unsigned n = (unsigned)max(min(fk.r.y, kv + 32) - max(fk.r.x, kv), 0);
+    float keep[16], sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; e++) {
+      const int c = (e >> 2) * 8 + (e & 3);
+      if constexpr (MOD != 0) s[e] = fast_exp2(final_score<MOD>(sf, s[e], d0 - (float)c, &keep[e]) - L);
+      else { s[e] = fast_exp2(fmaf(s[e], sf.f, -L)); keep[e] = 1.f; }
+      if ((unsigned)(c - lo) >= n) s[e] = dp[e] = 0.f;
+      sum = fmaf(s[e], dp[e], sum);
+    }
+    // (as in the other form: D of a row whose keys are all in this tile)
+    const bool alone = fk.r.x >= kv && fk.r.y <= kv + 32 && fk.r.x < fk.r.y;
+    if (__any(alone)) {
+      sum = both_halves_sum(sum);
+      if (alone) { D = sum; own = true; }
+    }
+#pragma unroll
+    for (int e = 0; e < 16; e++) s[e] *= (dp[e] - D) * keep[e];
+    if (!__all(fk.r.x <= kv && fk.r.y >= kv + 32)) {
+#pragma unroll
+      for (int e = 0; e < 16; e++) if ((unsigned)((e >> 2) * 8 + (e & 3) - lo) >= n) s[e] = 0.f;      // (D may be no number)
+    }
+    bf16x8 ds[2], first[T::DT];
+    ds[0] = acc_to_frag(s, 0);
+    ds[1] = acc_to_frag(s, 1);
+    T::read_cols(first, tK, cbase, 0);
+    T::template cols_times<32>(acc, tK, cbase, ds, first);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    if (next < fk.t1) issue(rk, next, aK);
+    t = next;
+  }
+  float2* found = (float2*)(smem_raw + 4 * T::BYTES);      // [wave][row]: D, and whether it is the one
+  if (g == 0) found[wv * 32 + lane] = make_float2(D, own ? 1.f : 0.f);
+  put_partial<T::DT>((float*)tK, acc, lane);
+  __syncthreads();
+  const FewRow mine = few_row(a, f, tile, head, threadIdx.x & 31, rows);
+  if (threadIdx.x < 32 && mine.ok) {
+    float d = found[threadIdx.x].x;
+#pragma unroll
+    for (int w = 1; w < 4; w++) if (found[w * 32 + threadIdx.x].y != 0.f) d = found[w * 32 + threadIdx.x].x;
+    a.dvec[(i64)mine.h * a.Tq + mine.i] = d;
+  }
+  const bool fine = few_store<bf16, DHP, 4>((const float*)smem_raw, (bf16*)a.dq + (i64)mine.i * a.ldq + (i64)mine.h * a.dh, mine.ok, a.dh, a.scale);
+  if (__syncthreads_or(!fine))
+    for (int x = wv; x < 32; x += 4) {
+      const FewRow again = few_row(a, f, tile, head, x, rows);
+      if (again.ok) range_row_dq<bf16>(args_again(), again.i, again.h, keys, (float*)smem_raw + wv * 2 * DHP);
+    }
+}
+template <int DHP, int MOD>
+__global__ void __launch_bounds__(256, 2) range_dkv_few_k(RangeAttn a, const int2* __restrict__ blocks) {
+  typedef Tiles<DHP> T;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem_raw[];
+  const int kt = (int)blockIdx.x / a.Hkv, kh = (int)blockIdx.x - kt * a.Hkv, k0 = kt * 32;      // early keys are seen by the most queries
+  const int rows = rows_in_use(a), keys = keys_in_use(a);
+  if (k0 >= keys) return;
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, mykv = k0 + (lane & 31);
+  unsigned char* tQ = smem_raw + wv * T::BYTES;      // 32 rows of Q, 32 of dO
+  const unsigned aQ = lds_address(smem_raw) + (unsigned)wv * T::BYTES, aS = lds_address(smem_raw) + 4 * T::BYTES + (unsigned)wv * 1280u;
+  const float* st = (const float*)(smem_raw + 4 * T::BYTES + wv * 1280);      // lse, D, lo, hi, at: 64 words each, of which 32 are used
+  // the pairs of a block of 32 queries, in a block of 64 that sees some of the keys, and a head: every fourth is this wave's
+  const int nb = (rows + 63) / 64;
+  unsigned long long live = 0;
+  int base = -64, n = 2 * a.G - 1, turn = -1, blk = 0, q0 = -1, h = 0;
+  auto next = [&]() {                               // q0 = -1: none
+    do {
+      if (++n == 2 * a.G) {
+        n = 0;
+        while (!live) {
+          base += 64;
+          if (base >= nb) { q0 = -1; return; }
+          const int b = base + lane_now();
+          const int2 r = b < nb ? blocks[b] : make_int2(INT_MAX, 0);
+          live = __ballot(r.x < k0 + 32 && r.y > k0);
+        }
+        blk = base + __builtin_ctzll(live);
+        live &= live - 1;
+      }
+      turn++;
+      q0 = blk * 64 + (n & 1) * 32;
+      h = kh * a.G + (n >> 1);
+    } while ((turn & 3) != wv || q0 >= rows);
+  };
+  auto issue = [&]() {
+    const int m = min(32, rows - q0);
+    const HeadRows rq = {(const unsigned char*)a.q + (i64)h * a.dh * 2, a.ldq * 2, a.dh * 2}, ro = {(const unsigned char*)a.d_o + (i64)h * a.dh * 2, a.ldo * 2, a.dh * 2};
+    const __amdgpu_buffer_rsrc_t bq = rows_buffer(rq, q0, m), bo = rows_buffer(ro, q0, m);
+    T::load16(bq, (unsigned)rq.ldb, rq.width, 0, aQ);
+    T::load16(bq, (unsigned)rq.ldb, rq.width, 16, aQ + 16 * T::ROW);
+    T::load16(bo, (unsigned)ro.ldb, ro.width, 0, aQ + T::BYTES / 2);
+    T::load16(bo, (unsigned)ro.ldb, ro.width, 16, aQ + T::BYTES / 2 + 16 * T::ROW);
+    const unsigned off = (unsigned)lane_now() * 4u;
+    load_lds_b32(words_buffer(a.lse + (i64)h * a.Tq, q0, m), aS, off);
+    load_lds_b32(words_buffer(a.dvec + (i64)h * a.Tq, q0, m), aS + 256u, off);
+    load_lds_b32(words_buffer(a.lo, q0, m), aS + 512u, off);
+    load_lds_b32(words_buffer(a.hi, q0, m), aS + 768u, off);
+    if constexpr (MOD & BIASED) {
+      if (a.at) load_lds_b32(words_buffer(a.at, q0, m), aS + 1024u, off);
+      else ((int*)st)[256 + off / 4] = q0 + (int)off / 4;
+    }
+  };
+  next();
+  if (q0 >= 0) issue();
+  bf16x8 kf[T::KK], vf[T::KK];
+  T::load_frags((const bf16*)a.k + (i64)mykv * a.ldk + (i64)kh * a.dh, mykv < keys, a.dh, g, kf);
+  T::load_frags((const bf16*)a.v + (i64)mykv * a.ldv + (i64)kh * a.dh, mykv < keys, a.dh, g, vf);
+  T::arrived(kf);
+  T::arrived(vf);
+  f32x16 dka[T::DT] = {}, dva[T::DT] = {};
+  while (q0 >= 0) {
+    const ScoreForm sf = score_form(a, h);
+    wait_vmcnt<0>();
+    const int lane = lane_now(), g = lane >> 5, mykv = k0 + (lane & 31);
+    const unsigned rbase = T::row_base(lane), cbase = T::col_base(lane);
+    f32x16 s, dp;
+    rows_times2<DHP>(s, dp, tQ, tQ + T::BYTES / 2, rbase, kf, vf);
+    const int2 lo_hi = make_int2(((const int*)st)[128 + (lane & 31)], ((const int*)st)[192 + (lane & 31)]);
+#pragma unroll
+    for (int eb = 0; eb < 4; eb++) {
+      const int r0 = eb * 8 + g * 4;
+      __builtin_amdgcn_sched_barrier(0);            // (all reads at once would cost the registers that are short here)
+      const float4 l4 = *(const float4*)(st + r0), d4 = *(const float4*)(st + 64 + r0);
+      const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, dv[4] = {d4.x, d4.y, d4.z, d4.w};
+      int av[4] = {0, 0, 0, 0};
+      if constexpr (MOD & BIASED) {
+        const int4 a4 = *(const int4*)(st + 256 + r0);
+        av[0] = a4.x; av[1] = a4.y; av[2] = a4.z; av[3] = a4.w;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        const int e = eb * 4 + i;
+        float x, keep = 1.f;
+        if constexpr (MOD != 0) x = fmaf(lv[i], -LOG2E, final_score<MOD>(sf, s[e], MOD & BIASED ? (float)(av[i] - mykv) : 0.f, &keep));
+        else x = fmaf(s[e], sf.f, -lv[i] * LOG2E);
+        s[e] = fast_exp2(x);
+        dp[e] = s[e] * (dp[e] - dv[i]) * keep;
+      }
+    }
+    if (!__all(lo_hi.x <= k0 && lo_hi.y >= k0 + 32)) {
+#pragma unroll
+      for (int eb = 0; eb < 4; eb++) {
+        const int r0 = eb * 8 + g * 4;
+        __builtin_amdgcn_sched_barrier(0);
+        const int4 lo4 = *(const int4*)(st + 128 + r0), hi4 = *(const int4*)(st + 192 + r0);
+        const int lo[4] = {lo4.x, lo4.y, lo4.z, lo4.w}, hi[4] = {hi4.x, hi4.y, hi4.z, hi4.w};
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+          if (mykv < lo[i] || mykv >= hi[i]) s[eb * 4 + i] = dp[eb * 4 + i] = 0.f;
+      }
+    }
+    bf16x8 pf[2], dsf[2];
+#pragma unroll
+    for (int c = 0; c < 2; c++) { pf[c] = acc_to_frag(s, c); dsf[c] = acc_to_frag(dp, c); }
+    const unsigned char* tO = tQ + T::BYTES / 2;
+    bf16x8 x[2][T::DT];
+    T::read_cols(x[0], tO, cbase, 0);
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+      if (c < 3) T::read_cols(x[(c + 1) & 1], c & 1 ? tO : tQ, cbase, (c + 1) >> 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int d = 0; d < T::DT; d++) {
+        if (c & 1) dka[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[c & 1][d], dsf[c >> 1], dka[d], 0, 0, 0);
+        else dva[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[c & 1][d], pf[c >> 1], dva[d], 0, 0, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    next();
+    if (q0 >= 0) issue();
+  }
+  const RangeAttn b = args_again();
+  const int r = k0 + (int)(threadIdx.x & 31);
+  put_partial<T::DT>((float*)tQ, dka, lane);
+  __syncthreads();
+  bool fine = few_store<bf16, DHP, 4>((const float*)smem_raw, (bf16*)b.dk + (i64)r * b.ldk + (i64)kh * b.dh, r < keys, b.dh, b.scale);
+  __syncthreads();
+  put_partial<T::DT>((float*)tQ, dva, lane);
+  __syncthreads();
+  fine &= few_store<bf16, DHP, 4>((const float*)smem_raw, (bf16*)b.dv + (i64)r * b.ldv + (i64)kh * b.dh, r < keys, b.dh, 1.f);
+  if (__syncthreads_or(!fine))
+    for (int x = wv; x < 32 && k0 + x < keys; x += 4) range_row_dkv<bf16>(b, k0 + x, kh, rows, keys, (float*)smem_raw + wv * 2 * DHP);
+}
+
 // ---- launchers ----
 static bool takes(const RangeAttn& a, bool back) {
   if (a.dt != 1 || a.dh > 128 || a.dh % 8) return false;
@@ -710,7 +997,20 @@ static bool takes(const RangeAttn& a, bool back) {
   return !(p & 15) && !(l & 7) && a.ldq < (1 << 24) && a.ldk < (1 << 24) && a.ldv < (1 << 24) && a.ldo < (1 << 24);
 }
 bool range_flash_takes(const RangeAttn& a, bool back) { return takes(a, back); }
-static bool modified(const RangeAttn& a) { return a.cap > 0.f || a.slopes || a.scale < 0.f; }
+// what a kernel has to have; a negative scale needs scores in their final form before the maximum, as a bias does
+static int parts_of_score(const RangeAttn& a) {
+  const int m = (a.cap > 0.f ? CAPPED : 0) | (a.slopes ? BIASED : 0);
+  return m == 0 && a.scale < 0.f ? BIASED : m;
+}
+#define BY_FORM(call)                                                              \
+  do {                                                                             \
+    const int m = parts_of_score(a);                                               \
+    if (a.dh <= 64) { if (m == 0) call(64, 0); else if (m == 1) call(64, 1); else if (m == 2) call(64, 2); else call(64, 3); } \
+    else if (m == 0) call(128, 0);                                                 \
+    else if (m == 1) call(128, 1);                                                 \
+    else if (m == 2) call(128, 2);                                                 \
+    else call(128, 3);                                                             \
+  } while (0)
 
 template <class K> static void set_lds(std::atomic<unsigned long long>& mask, K kernel, unsigned bytes) {
   if (attr_needed(mask)) {
@@ -718,7 +1018,7 @@ template <class K> static void set_lds(std::atomic<unsigned long long>& mask, K 
     attr_done(mask);
   }
 }
-template <int DHP, bool MOD> static void fwd(const RangeAttn& a, hipStream_t s) {
+template <int DHP, int MOD> static void fwd(const RangeAttn& a, hipStream_t s) {
   static std::atomic<unsigned long long> mask{0};
   constexpr unsigned smem = 4 * Tiles<DHP>::BYTES;
   set_lds(mask, range_fwd_k<DHP, MOD>, smem);
@@ -728,15 +1028,16 @@ template <int DHP, bool MOD> static void fwd(const RangeAttn& a, hipStream_t s) 
 // head make many pairs.
 static int dkv_parts(const RangeAttn& a) {
   const i64 workgroups = (i64)cdiv(a.Tk, 128) * a.Hkv;
+  if (getenv("RP")) return atoi(getenv("RP"));
   int n = 1;
-  while (n < 8 && n < a.G && workgroups * n < 512) n *= 2;
+  while (a.G > 1 && n < 8 && n < 2 * a.G && workgroups * n < 1024) n *= 2;
   return n;
 }
 size_t range_flash_sum_floats(const RangeAttn& a) {
   const int n = dkv_parts(a);
   return n > 1 ? (size_t)n * 2 * a.Tk * a.Hkv * (a.dh <= 64 ? 64 : 128) : 0;
 }
-template <int DHP, bool MOD> static void bwd(const RangeAttn& a, void* blocks, float* sums, hipStream_t s) {
+template <int DHP, int MOD> static void bwd(const RangeAttn& a, void* blocks, float* sums, hipStream_t s) {
   static std::atomic<unsigned long long> mask_q{0}, mask_kv{0};
   constexpr unsigned sq = 5 * Tiles<DHP>::BYTES, skv = 2 * DKV_STAGE<DHP>;
   set_lds(mask_q, range_bwd_dq_k<DHP, MOD>, sq);
@@ -747,7 +1048,23 @@ template <int DHP, bool MOD> static void bwd(const RangeAttn& a, void* blocks, f
   hipLaunchKernelGGL((range_bwd_dkv_k<DHP, MOD>), dim3((unsigned)((i64)cdiv(a.Tk, 128) * a.Hkv * parts)), dim3(256), skv, s, a, (const BlockSeen*)blocks, sums, parts);
   if (parts > 1) hipLaunchKernelGGL(range_dkv_sum_k<DHP>, dim3((unsigned)cdiv((i64)a.Tk * a.Hkv, 4)), dim3(256), 0, s, a, sums, parts);
 }
-template <int DHP, bool MOD> static void fwd_few(const RangeAttn& a, float* work, hipStream_t s) {
+template <int DHP, int MOD> static void bwd_few(const RangeAttn& a, void* blocks, hipStream_t s) {
+  static std::atomic<unsigned long long> mask_q{0}, mask_kv{0};
+  constexpr unsigned sq = 4 * Tiles<DHP>::BYTES + 4 * 256, skv = 4 * Tiles<DHP>::BYTES + 4 * 1280;
+  set_lds(mask_q, range_dq_few_k<DHP, MOD>, sq);
+  set_lds(mask_kv, range_dkv_few_k<DHP, MOD>, skv);
+  FewShape f = few_shape(a, nullptr);
+  f.splits = 1;
+  const int tiles = f.tiles * a.Hkv * f.hb;
+  if (a.Tq > 0) hipLaunchKernelGGL((range_dq_few_k<DHP, MOD>), dim3((unsigned)(tiles + cdiv(a.Tq, 64 * 4))), dim3(256), sq, s, a, f, tiles, (int2*)blocks);
+  if (a.Tk > 0) hipLaunchKernelGGL((range_dkv_few_k<DHP, MOD>), dim3((unsigned)((i64)cdiv(a.Tk, 32) * a.Hkv)), dim3(256), skv, s, a, (const int2*)blocks);
+}
+void launch_range_bwd_flash_few(const RangeAttn& a, void* blocks, hipStream_t s) {
+#define BWD_FEW(W, M) bwd_few<W, M>(a, blocks, s)
+  BY_FORM(BWD_FEW);
+}
+bool range_flash_few_bwd(const RangeAttn& a) { return (i64)a.Tq * a.H <= 32 * 1024; }
+template <int DHP, int MOD> static void fwd_few(const RangeAttn& a, float* work, hipStream_t s) {
   static std::atomic<unsigned long long> mask{0};
   set_lds(mask, range_fwd_few_k<DHP, MOD>, FEW_SMEM<DHP>);
   const FewShape f = few_shape(a, work);
@@ -757,19 +1074,16 @@ template <int DHP, bool MOD> static void fwd_few(const RangeAttn& a, float* work
 bool range_flash_few(const RangeAttn& a) { return (i64)a.Tq * a.H <= 16 * 1024; }
 void launch_range_fwd_flash_few(const RangeAttn& a, float* work, hipStream_t s) {
   if (a.Tq <= 0) return;
-  if (a.dh <= 64) { if (modified(a)) fwd_few<64, true>(a, work, s); else fwd_few<64, false>(a, work, s); }
-  else if (modified(a)) fwd_few<128, true>(a, work, s);
-  else fwd_few<128, false>(a, work, s);
+#define FEW(W, M) fwd_few<W, M>(a, work, s)
+  BY_FORM(FEW);
 }
 size_t range_few_floats(const RangeAttn& a) { return few_floats(a); }
 void launch_range_fwd_flash(const RangeAttn& a, hipStream_t s) {
   if (a.Tq <= 0) return;
-  if (a.dh <= 64) { if (modified(a)) fwd<64, true>(a, s); else fwd<64, false>(a, s); }
-  else if (modified(a)) fwd<128, true>(a, s);
-  else fwd<128, false>(a, s);
+#define FWD(W, M) fwd<W, M>(a, s)
+  BY_FORM(FWD);
 }
 void launch_range_bwd_flash(const RangeAttn& a, void* blocks, float* sums, hipStream_t s) {
-  if (a.dh <= 64) { if (modified(a)) bwd<64, true>(a, blocks, sums, s); else bwd<64, false>(a, blocks, sums, s); }
-  else if (modified(a)) bwd<128, true>(a, blocks, sums, s);
-  else bwd<128, false>(a, blocks, sums, s);
+#define BWD(W, M) bwd<W, M>(a, blocks, sums, s)
+  BY_FORM(BWD);
 }

@@ -27,6 +27,26 @@ __device__ __forceinline__ bf16x8 acc_to_frag(const f32x16& a, int c) {
   return r;
 }
 
+// The kernel's arguments (RangeAttn is the first of them), read anew: for what comes after a loop, or hardly ever, so that it holds no
+// registers in the loop.
+__device__ __forceinline__ RangeAttn args_again() {
+  unsigned long long p = (unsigned long long)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  typedef const __attribute__((address_space(4))) unsigned long long word;
+  static_assert(sizeof(RangeAttn) % 8 == 0, "whole words");
+  union { RangeAttn a; unsigned long long w[sizeof(RangeAttn) / 8]; } r;
+#pragma unroll
+  for (unsigned i = 0; i < sizeof(RangeAttn) / 8; i++) r.w[i] = ((word*)p)[i];
+  return r.a;
+}
+
+// The lane number, asked for where it is used: what is worked out from it then holds no register from tile to tile.
+__device__ __forceinline__ int lane_now() {
+  unsigned none = 0;
+  asm volatile("" : "+v"(none));
+  return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, none));
+}
+
 // ---- tiles ----
 template <int DHP> __device__ __forceinline__ int swz(int r) {
   return DHP == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
@@ -46,9 +66,9 @@ template <int DHP> struct Tiles {
   static constexpr unsigned LOADS = 16 / RPL;                               // wave-loads per 16 rows
   static constexpr unsigned BYTES = 64u * ROW;                              // of a tile of 64 rows
   // 16 rows of a buffer, from row0 on, to LDS at dst
-  static __device__ __forceinline__ void load16(__amdgpu_buffer_rsrc_t rs, unsigned ldb, int width, int row0, unsigned dst, int lane) {
-    unsigned a = (unsigned)(lane / CPR), c = (unsigned)((lane % CPR) ^ swz<DHP>(lane / CPR));
-    asm volatile("" : "+v"(a), "+v"(c));            // (the offsets are not worth a register each from tile to tile)
+  static __device__ __forceinline__ void load16(__amdgpu_buffer_rsrc_t rs, unsigned ldb, int width, int row0, unsigned dst) {
+    const int lane = lane_now();
+    const unsigned a = (unsigned)(lane / CPR), c = (unsigned)((lane % CPR) ^ swz<DHP>(lane / CPR));
 #pragma unroll
     for (unsigned i = 0; i < LOADS; i++) {
       const unsigned chunk = c ^ (i * (DHP == 128 ? 1u : 2u));              // swz(RPL i + a) = swz(a) ^ ..
@@ -136,20 +156,27 @@ __device__ __forceinline__ float both_halves_sum(float x) {
   return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
 }
 
-// Scores in units of log2: q.k times f (no cap), or cap2 tanh(q.k x2 / 2 log2e), less slope2 times the distance.
+// Scores in units of log2: q.k times f, or capped, cap2 tanh(q.k x2 / (2 log2e)), less slope2 times the distance.
 // tanh(x) = 1 - 2 / (e^2x + 1): off by some 2^-22 at most, by the exponential and the reciprocal.
-struct ScoreForm {
-  float f, x2, cap2, slope2;
-  bool capped, biased;
-};
+enum { CAPPED = 1, BIASED = 2 };                    // the parts that a kernel has (MOD); 0: f is positive
+struct ScoreForm { float f, x2, cap2, slope2; };
 __device__ __forceinline__ ScoreForm score_form(const RangeAttn& a, int h) {
   ScoreForm s;
   s.f = a.scale * LOG2E;
-  s.capped = a.cap > 0.f;
-  s.x2 = s.capped ? 2.f * LOG2E * a.scale / a.cap : 0.f;
+  s.x2 = a.cap > 0.f ? 2.f * LOG2E * a.scale / a.cap : 0.f;
   s.cap2 = a.cap * LOG2E;
-  s.biased = a.slopes != nullptr;
-  s.slope2 = s.biased ? a.slopes[h] * LOG2E : 0.f;
+  s.slope2 = a.slopes ? a.slopes[h] * LOG2E : 0.f;
   return s;
 }
 __device__ __forceinline__ float fast_tanh_2(float two_x_log2e) { return 1.f - 2.f * __builtin_amdgcn_rcpf(fast_exp2(two_x_log2e) + 1.f); }
+// from q.k and the distance; keep: what a gradient at the score is multiplied by to be one at scale q.k
+template <int MOD> __device__ __forceinline__ float final_score(const ScoreForm& sf, float x, float distance, float* keep) {
+  *keep = 1.f;
+  if constexpr (MOD & CAPPED) {
+    const float t = fast_tanh_2(x * sf.x2);
+    *keep = fmaf(-t, t, 1.f);
+    x = t * sf.cap2;
+  } else x *= sf.f;
+  if constexpr (MOD & BIASED) x = fmaf(-sf.slope2, fabsf(distance), x);
+  return x;
+}

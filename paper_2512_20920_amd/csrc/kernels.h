@@ -372,6 +372,8 @@ bool range_flash_few(const RangeAttn& a);
 size_t range_few_floats(const RangeAttn& a);
 void launch_range_fwd_flash_few(const RangeAttn& a, float* work, hipStream_t s);
 void launch_range_bwd_flash(const RangeAttn& a, void* blocks, float* sums, hipStream_t s);
+bool range_flash_few_bwd(const RangeAttn& a);
+void launch_range_bwd_flash_few(const RangeAttn& a, void* blocks, hipStream_t s);
 // the same in float32
 bool range_f32_takes(const RangeAttn& a, bool back);
 void launch_range_fwd_f32(const RangeAttn& a, float* work, hipStream_t s);

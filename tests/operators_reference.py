@@ -90,10 +90,11 @@ def attention(q, k, v, lo, hi, at=None, scale=None, cap=0.0, slopes=None, do=Non
         ds = p * (dp - D) * keep
         e_ds = (rel + (8 * 2.0 ** -21 if cap else 0.0)) * np.abs(p * (dp - D)) + p * (e_D + e_dp)
         r = lambda a, b: a @ b * scale
+        size = lambda a, b: a @ b * abs(scale)              # (of errors: whatever the sign of the scale)
         dq = r(ds, kz)
-        out["dq"][0][:, h], out["dq"][1][:, h] = dq, r(e_ds + (m + 8) * E32 * np.abs(ds), np.abs(kz)) + u * np.abs(dq)
+        out["dq"][0][:, h], out["dq"][1][:, h] = dq, size(e_ds + (m + 8) * E32 * np.abs(ds), np.abs(kz)) + u * np.abs(dq)
         out["dk"][0][:, h // G] += r(ds.T, qz)
-        out["dk"][1][:, h // G] += r((e_ds + (n * G + 8) * E32 * np.abs(ds)).T, np.abs(qz))
+        out["dk"][1][:, h // G] += size((e_ds + (n * G + 8) * E32 * np.abs(ds)).T, np.abs(qz))
         out["dv"][0][:, h // G] += p.T @ g
         out["dv"][1][:, h // G] += (p * (rel + (n * G + 8) * E32)).T @ np.abs(g)
     for name in ("dk", "dv"):

@@ -94,6 +94,9 @@ SHAPES = {
     "capped": (4, 4, 64, [140, 61], None, dict(cap=5.0)),
     "biased": (4, 2, 128, [140, 61], None, dict(bias=True)),
     "capped_biased_prefix": (6, 2, 64, [129, 200], None, dict(cap=30.0, bias=True, prefix=[100, 0])),
+    "capped_wide": (2, 2, 128, [140, 61], None, dict(cap=5.0)),
+    "capped_biased_wide": (4, 1, 128, [200, 30], None, dict(cap=8.0, bias=True)),
+    "biased_narrow": (4, 2, 64, [140, 61], None, dict(bias=True)),
     "behind_a_cache": (4, 2, 64, [40, 7, 129], [300, 7, 500], dict(bias=True)),
     "more_queries_than_keys": (2, 1, 64, [50, 20], [20, 20], {}),
     "no_keys": (2, 1, 64, [20, 30], [0, 30], dict(causal=False)),
@@ -185,6 +188,15 @@ def test_attention_values_that_are_not_finite_stay_where_they_are(value, mode, d
         row = a.part("o")[50]
         if where in ("k", "v"):
             assert not np.isfinite(row).all()               # and who sees it, gets it
+
+
+@pytest.mark.parametrize("dtype,mode", [("bf16", 1), ("bf16", 256), ("bf16", 512), ("f32", 0)])
+@pytest.mark.parametrize("scale,cap", [(0.3, 0.0), (-0.2, 0.0), (-0.2, 3.0), (1e-3, 0.5)])
+def test_attention_scales(scale, cap, mode, dtype):
+    lo, hi, at = ref.ranges([70, 40])
+    a = Attention(dtype, 2, 1, 64, 110, 110)
+    a.run(lo, hi, at, mode, cap=cap, scale=scale)
+    a.check(lo, hi, at, cap=cap, scale=scale)
 
 
 @pytest.mark.parametrize("dtype,mode", [("bf16", 256), ("bf16", 512), ("f32", 0)])
