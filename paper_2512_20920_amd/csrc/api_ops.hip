@@ -102,10 +102,8 @@ int revffn_op_attention_masked_fwd(const revffn_attn_desc* desc, const revffn_at
   if (w.bytes > work_bytes || ((uintptr_t)work & 15)) return REVFFN_EINVAL;
   a.q = q; a.k = k; a.v = v; a.out = o; a.lse = lse;
   const int mode = desc->kernel_mode & 0xff, form = desc->kernel_mode >> 8;
-  if (mode != 1 && range_flash_takes(a, false)) {
-    if (form ? form == 1 : range_flash_few(a)) launch_range_fwd_flash_few(a, w.parts, (hipStream_t)stream);
-    else launch_range_fwd_flash(a, (hipStream_t)stream);
-  } else if (mode != 1 && range_f32_takes(a, false)) launch_range_fwd_f32(a, w.parts, (hipStream_t)stream);
+  if (mode != 1 && range_flash_takes(a, false)) launch_range_fwd_flash(a, w.parts, form, (hipStream_t)stream);
+  else if (mode != 1 && range_f32_takes(a, false)) launch_range_fwd_f32(a, w.parts, (hipStream_t)stream);
   else if (mode == 2) return REVFFN_EUNSUPPORTED;
   else launch_range_fwd_rows(a, (hipStream_t)stream);
   return 0;
@@ -123,10 +121,8 @@ int revffn_op_attention_masked_bwd(const revffn_attn_desc* desc, const revffn_at
   if (w.bytes > work_bytes || ((uintptr_t)work & 15)) return REVFFN_EINVAL;
   a.q = q; a.k = k; a.v = v; a.o = o; a.d_o = d_o; a.lse = (float*)lse; a.dq = dq; a.dk = dk; a.dv = dv; a.dvec = w.dvec;
   const int mode = desc->kernel_mode & 0xff, form = desc->kernel_mode >> 8;
-  if (mode != 1 && range_flash_takes(a, true)) {
-    if (form ? form == 1 : range_flash_few_bwd(a)) launch_range_bwd_flash_few(a, w.blocks, (hipStream_t)stream);
-    else launch_range_bwd_flash(a, w.blocks, w.sums, (hipStream_t)stream);
-  } else if (mode != 1 && range_f32_takes(a, true)) launch_range_bwd_f32(a, w.blocks, (hipStream_t)stream);
+  if (mode != 1 && range_flash_takes(a, true)) launch_range_bwd_flash(a, w.blocks, w.sums, form, (hipStream_t)stream);
+  else if (mode != 1 && range_f32_takes(a, true)) launch_range_bwd_f32(a, w.blocks, (hipStream_t)stream);
   else if (mode == 2) return REVFFN_EUNSUPPORTED;
   else launch_range_bwd_rows(a, (hipStream_t)stream);
   return 0;

@@ -107,13 +107,13 @@ template <int DHP> __global__ void __launch_bounds__(NW * 64) range_fwd_f32_k(Ra
 
 // dQ of 32 rows, and D = <o, dO>.  The last workgroups of the launch (from `tiles` on) note instead, a wave per block of 64 queries, the first key that
 // some of them see and one past the last.
-template <int DHP> __global__ void __launch_bounds__(NW * 64) range_dq_f32_k(RangeAttn a, FewShape f, int tiles, int2* __restrict__ blocks) {
+template <int DHP> __global__ void __launch_bounds__(NW * 64) range_dq_f32_k(RangeAttn a, FewShape f, int tiles, BlockSeen* __restrict__ blocks) {
   extern __shared__ float sm[];
   const int rows = rows_in_use(a), keys = keys_in_use(a);
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
   if ((int)blockIdx.x >= tiles) {
     const int b = ((int)blockIdx.x - tiles) * NW + wv;
-    const int2 r = block_seen(a, b, rows, keys, lane);
+    const BlockSeen r = block_seen(a, b, rows, keys, lane);
     if (lane == 0 && b * 64 < a.Tq) blocks[b] = r;
     return;
   }
@@ -162,7 +162,7 @@ template <int DHP> __global__ void __launch_bounds__(NW * 64) range_dq_f32_k(Ran
 }
 
 // dK, dV of 32 keys of a key head: the waves share out the blocks of 32 queries that see some of them, of every head that shares it.
-template <int DHP> __global__ void __launch_bounds__(NW * 64) range_dkv_f32_k(RangeAttn a, const int2* __restrict__ blocks) {
+template <int DHP> __global__ void __launch_bounds__(NW * 64) range_dkv_f32_k(RangeAttn a, const BlockSeen* __restrict__ blocks) {
   extern __shared__ float sm[];                      // NW results [DHP][32], then 5 x 32 words per wave
   const int kt = (int)blockIdx.x / a.Hkv, kh = (int)blockIdx.x - kt * a.Hkv, k0 = kt * 32;
   const int rows = rows_in_use(a), keys = keys_in_use(a);
@@ -176,7 +176,7 @@ template <int DHP> __global__ void __launch_bounds__(NW * 64) range_dkv_f32_k(Ra
   const int nb = (rows + 63) / 64;
   int turn = 0;
   for (int b0 = 0; b0 < nb; b0 += 64) {
-    const int2 r = b0 + lane < nb ? blocks[b0 + lane] : make_int2(INT_MAX, 0);
+    const int2 r = b0 + lane < nb ? *(const int2*)(blocks + b0 + lane) : make_int2(INT_MAX, 0);
     unsigned long long live = __ballot(r.x < k0 + 32 && r.y > k0);
     while (live) {
       const int b = b0 + __builtin_ctzll(live);
@@ -247,7 +247,7 @@ template <int DHP> static void fwd(const RangeAttn& a, float* work, hipStream_t 
   set_lds(mask, range_fwd_f32_k<DHP>, smem);
   const FewShape f = few_shape(a, work);
   hipLaunchKernelGGL(range_fwd_f32_k<DHP>, dim3((unsigned)((i64)f.tiles * f.splits * a.Hkv * f.hb)), dim3(NW * 64), smem, s, a, f);
-  if (f.splits > 1) hipLaunchKernelGGL((range_join_k<float, DHP>), dim3((unsigned)cdiv((i64)a.Tq * a.H, 4)), dim3(256), 0, s, a, f);
+  join_splits<float, DHP>(a, f, s);
 }
 template <int DHP> static void bwd(const RangeAttn& a, void* blocks, hipStream_t s) {
   constexpr size_t smem = (size_t)NW * DHP * 32 * 4, smem_kv = smem + NW * 160 * 4;
@@ -257,8 +257,8 @@ template <int DHP> static void bwd(const RangeAttn& a, void* blocks, hipStream_t
   FewShape f = few_shape(a, nullptr);
   f.splits = 1;
   const int tiles = f.tiles * a.Hkv * f.hb;
-  if (a.Tq > 0) hipLaunchKernelGGL(range_dq_f32_k<DHP>, dim3((unsigned)(tiles + cdiv(a.Tq, 64 * NW))), dim3(NW * 64), smem, s, a, f, tiles, (int2*)blocks);
-  if (a.Tk > 0) hipLaunchKernelGGL(range_dkv_f32_k<DHP>, dim3((unsigned)((i64)cdiv(a.Tk, 32) * a.Hkv)), dim3(NW * 64), smem_kv, s, a, (const int2*)blocks);
+  if (a.Tq > 0) hipLaunchKernelGGL(range_dq_f32_k<DHP>, dim3((unsigned)(tiles + cdiv(a.Tq, 64 * NW))), dim3(NW * 64), smem, s, a, f, tiles, (BlockSeen*)blocks);
+  if (a.Tk > 0) hipLaunchKernelGGL(range_dkv_f32_k<DHP>, dim3((unsigned)((i64)cdiv(a.Tk, 32) * a.Hkv)), dim3(NW * 64), smem_kv, s, a, (const BlockSeen*)blocks);
 }
 void launch_range_fwd_f32(const RangeAttn& a, float* work, hipStream_t s) {
   if (a.Tq <= 0) return;

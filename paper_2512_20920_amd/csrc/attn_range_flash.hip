@@ -1,7 +1,6 @@
 // Attention over key ranges on the matrix cores: bf16, heads of up to 128 columns (a multiple of 8).
 #include "attn_range_tiles.h"
 #include "attn_range_few.h"
-#include <stdlib.h>
 
 // Two workgroups fit on a CU: where the whole grid is resident at once, workgroups i and i + 256 share one, so the second 256 take the
 // tiles in the other order, and a long tile shares its CU with a short one.
@@ -327,9 +326,6 @@ __global__ void __launch_bounds__(256, 2) range_fwd_few_k(RangeAttn a, FewShape 
 //   S^T = K Q^T,  P^T = exp(S^T - lse),  dP^T = V dO^T,  dS^T = P^T (dP^T - D),  dQ^T += K^T dS^T,  times scale at the end.
 // The forward kernel's tiles and phases; the keys of a tile are read once more in the phase after, so they have three stages.
 // ------------------------------------------------------------------------------------
-// block of 64 queries: the first key that some query sees and one past the last (none: INT_MAX, 0), and between which keys all see
-typedef int4 BlockSeen;
-
 template <int DHP, int MOD>
 __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen* __restrict__ blocks) {
   typedef Tiles<DHP> T;
@@ -339,12 +335,9 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen*
   qt = (a.Tq + 127) / 128 - 1 - qt;
   const int rows = rows_in_use(a), keys = keys_in_use(a), q0 = qt * 128;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
-  const TwoRanges two = two_ranges(a, q0, rows, keys);
-  const QueryRanges qr = query_ranges(two, q0, rows, lane);
-  if (h == 0 && wv < 2) {                           // (a row in use that sees nothing leaves no key that all see)
-    const int2 r = wv ? two.r1 : two.r0;
-    const bool in = q0 + wv * 64 + lane < rows, sees = r.x < r.y;
-    const int4 b = make_int4(wave_imin(r.x), wave_imax(r.y), wave_imax(sees ? r.x : in ? INT_MAX : INT_MIN), wave_imin(sees ? r.y : in ? 0 : INT_MAX));
+  const QueryRanges qr = query_ranges(two_ranges(a, q0, rows, keys), q0, rows, lane);
+  if (h == 0 && wv < 2) {
+    const BlockSeen b = block_seen(a, qt * 2 + wv, rows, keys, lane);
     if (lane == 0 && q0 + wv * 64 < a.Tq) blocks[qt * 2 + wv] = b;
   }
   if (q0 >= rows) return;
@@ -739,14 +732,14 @@ template <int DHP> __device__ __forceinline__ void rows_times2(f32x16& a, f32x16
 }
 // The last workgroups of the launch (from `tiles` on) note which keys the blocks of 64 queries see, a wave per block.
 template <int DHP, int MOD>
-__global__ void __launch_bounds__(256, 2) range_dq_few_k(RangeAttn a, FewShape f, int tiles, int2* __restrict__ blocks) {
+__global__ void __launch_bounds__(256, 2) range_dq_few_k(RangeAttn a, FewShape f, int tiles, BlockSeen* __restrict__ blocks) {
   typedef Tiles<DHP> T;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem_raw[];
   const int rows = rows_in_use(a), keys = keys_in_use(a);
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
   if ((int)blockIdx.x >= tiles) {
     const int b = ((int)blockIdx.x - tiles) * 4 + wv;
-    const int2 r = block_seen(a, b, rows, keys, lane);
+    const BlockSeen r = block_seen(a, b, rows, keys, lane);
     if (lane == 0 && b * 64 < a.Tq) blocks[b] = r;
     return;
   }
@@ -852,17 +845,18 @@ __global__ void __launch_bounds__(256, 2) range_dq_few_k(RangeAttn a, FewShape f
     }
 }
 template <int DHP, int MOD>
-__global__ void __launch_bounds__(256, 2) range_dkv_few_k(RangeAttn a, const int2* __restrict__ blocks) {
+__global__ void __launch_bounds__(256, 2) range_dkv_few_k(RangeAttn a, const BlockSeen* __restrict__ blocks, float* __restrict__ sums, int parts) {
   typedef Tiles<DHP> T;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem_raw[];
-  const int kt = (int)blockIdx.x / a.Hkv, kh = (int)blockIdx.x - kt * a.Hkv, k0 = kt * 32;      // early keys are seen by the most queries
+  const int per = a.Hkv * parts, kt = (int)blockIdx.x / per, r0 = (int)blockIdx.x - kt * per, kh = r0 % a.Hkv, part = r0 / a.Hkv;
+  const int k0 = kt * 32;                           // early keys are seen by the most queries
   const int rows = rows_in_use(a), keys = keys_in_use(a);
   if (k0 >= keys) return;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, mykv = k0 + (lane & 31);
   unsigned char* tQ = smem_raw + wv * T::BYTES;      // 32 rows of Q, 32 of dO
   const unsigned aQ = lds_address(smem_raw) + (unsigned)wv * T::BYTES, aS = lds_address(smem_raw) + 4 * T::BYTES + (unsigned)wv * 1280u;
   const float* st = (const float*)(smem_raw + 4 * T::BYTES + wv * 1280);      // lse, D, lo, hi, at: 64 words each, of which 32 are used
-  // the pairs of a block of 32 queries, in a block of 64 that sees some of the keys, and a head: every fourth is this wave's
+  // the pairs of a block of 32 queries, in a block of 64 that sees some of the keys, and a head, dealt out to the waves of all parts
   const int nb = (rows + 63) / 64;
   unsigned long long live = 0;
   int base = -64, n = 2 * a.G - 1, turn = -1, blk = 0, q0 = -1, h = 0;
@@ -874,7 +868,7 @@ __global__ void __launch_bounds__(256, 2) range_dkv_few_k(RangeAttn a, const int
           base += 64;
           if (base >= nb) { q0 = -1; return; }
           const int b = base + lane_now();
-          const int2 r = b < nb ? blocks[b] : make_int2(INT_MAX, 0);
+          const int2 r = b < nb ? *(const int2*)(blocks + b) : make_int2(INT_MAX, 0);
           live = __ballot(r.x < k0 + 32 && r.y > k0);
         }
         blk = base + __builtin_ctzll(live);
@@ -883,7 +877,7 @@ __global__ void __launch_bounds__(256, 2) range_dkv_few_k(RangeAttn a, const int
       turn++;
       q0 = blk * 64 + (n & 1) * 32;
       h = kh * a.G + (n >> 1);
-    } while ((turn & 3) != wv || q0 >= rows);
+    } while (turn % (4 * parts) != part * 4 + wv || q0 >= rows);
   };
   auto issue = [&]() {
     const int m = min(32, rows - q0);
@@ -976,6 +970,17 @@ __global__ void __launch_bounds__(256, 2) range_dkv_few_k(RangeAttn a, const int
   }
   const RangeAttn b = args_again();
   const int r = k0 + (int)(threadIdx.x & 31);
+  if (parts > 1) {
+    float* row = sums + ((((i64)part * 2) * b.Tk + r) * b.Hkv + kh) * DHP;
+    put_partial<T::DT>((float*)tQ, dka, lane);
+    __syncthreads();
+    (void)few_store<float, DHP, 4>((const float*)smem_raw, row, r < keys, DHP, 1.f);
+    __syncthreads();
+    put_partial<T::DT>((float*)tQ, dva, lane);
+    __syncthreads();
+    (void)few_store<float, DHP, 4>((const float*)smem_raw, row + (i64)b.Tk * b.Hkv * DHP, r < keys, DHP, 1.f);
+    return;
+  }
   put_partial<T::DT>((float*)tQ, dka, lane);
   __syncthreads();
   bool fine = few_store<bf16, DHP, 4>((const float*)smem_raw, (bf16*)b.dk + (i64)r * b.ldk + (i64)kh * b.dh, r < keys, b.dh, b.scale);
@@ -1018,72 +1023,89 @@ template <class K> static void set_lds(std::atomic<unsigned long long>& mask, K 
     attr_done(mask);
   }
 }
-template <int DHP, int MOD> static void fwd(const RangeAttn& a, hipStream_t s) {
-  static std::atomic<unsigned long long> mask{0};
-  constexpr unsigned smem = 4 * Tiles<DHP>::BYTES;
-  set_lds(mask, range_fwd_k<DHP, MOD>, smem);
-  hipLaunchKernelGGL((range_fwd_k<DHP, MOD>), dim3((unsigned)((i64)cdiv(a.Tq, 128) * a.H)), dim3(256), smem, s, a);
-}
-// Parts of a key tile's (query block, head) pairs in dK/dV: enough workgroups for two per CU, where the heads that share a key
-// head make many pairs.
+// Parts of a key tile's (query block, head) pairs in dK/dV, for 128 keys per workgroup and for 32: workgroups enough to fill the chip twice, where
+// several heads that share a key head make the pairs many (and the float32 sums that a part costs few).
 static int dkv_parts(const RangeAttn& a) {
   const i64 workgroups = (i64)cdiv(a.Tk, 128) * a.Hkv;
-  if (getenv("RP")) return atoi(getenv("RP"));
   int n = 1;
   while (a.G > 1 && n < 8 && n < 2 * a.G && workgroups * n < 1024) n *= 2;
   return n;
 }
+static int dkv_parts_few(const RangeAttn& a) {
+  const i64 workgroups = (i64)cdiv(a.Tk, 32) * a.Hkv;
+  int n = 1;
+  while (n < 8 && n < a.G && workgroups * n < 1024) n *= 2;
+  return n;
+}
 size_t range_flash_sum_floats(const RangeAttn& a) {
-  const int n = dkv_parts(a);
+  const int n = dkv_parts(a) > dkv_parts_few(a) ? dkv_parts(a) : dkv_parts_few(a);
   return n > 1 ? (size_t)n * 2 * a.Tk * a.Hkv * (a.dh <= 64 ? 64 : 128) : 0;
 }
-template <int DHP, int MOD> static void bwd(const RangeAttn& a, void* blocks, float* sums, hipStream_t s) {
-  static std::atomic<unsigned long long> mask_q{0}, mask_kv{0};
-  constexpr unsigned sq = 5 * Tiles<DHP>::BYTES, skv = 2 * DKV_STAGE<DHP>;
-  set_lds(mask_q, range_bwd_dq_k<DHP, MOD>, sq);
-  set_lds(mask_kv, range_bwd_dkv_k<DHP, MOD>, skv);
-  if (a.Tq > 0) hipLaunchKernelGGL((range_bwd_dq_k<DHP, MOD>), dim3((unsigned)((i64)cdiv(a.Tq, 128) * a.H)), dim3(256), sq, s, a, (BlockSeen*)blocks);
-  if (a.Tk <= 0) return;
-  const int parts = dkv_parts(a);
-  hipLaunchKernelGGL((range_bwd_dkv_k<DHP, MOD>), dim3((unsigned)((i64)cdiv(a.Tk, 128) * a.Hkv * parts)), dim3(256), skv, s, a, (const BlockSeen*)blocks, sums, parts);
+template <int DHP> static void sum_parts(const RangeAttn& a, const float* sums, int parts, hipStream_t s) {
   if (parts > 1) hipLaunchKernelGGL(range_dkv_sum_k<DHP>, dim3((unsigned)cdiv((i64)a.Tk * a.Hkv, 4)), dim3(256), 0, s, a, sums, parts);
 }
-template <int DHP, int MOD> static void bwd_few(const RangeAttn& a, void* blocks, hipStream_t s) {
-  static std::atomic<unsigned long long> mask_q{0}, mask_kv{0};
-  constexpr unsigned sq = 4 * Tiles<DHP>::BYTES + 4 * 256, skv = 4 * Tiles<DHP>::BYTES + 4 * 1280;
-  set_lds(mask_q, range_dq_few_k<DHP, MOD>, sq);
-  set_lds(mask_kv, range_dkv_few_k<DHP, MOD>, skv);
-  FewShape f = few_shape(a, nullptr);
-  f.splits = 1;
-  const int tiles = f.tiles * a.Hkv * f.hb;
-  if (a.Tq > 0) hipLaunchKernelGGL((range_dq_few_k<DHP, MOD>), dim3((unsigned)(tiles + cdiv(a.Tq, 64 * 4))), dim3(256), sq, s, a, f, tiles, (int2*)blocks);
-  if (a.Tk > 0) hipLaunchKernelGGL((range_dkv_few_k<DHP, MOD>), dim3((unsigned)((i64)cdiv(a.Tk, 32) * a.Hkv)), dim3(256), skv, s, a, (const int2*)blocks);
+// Which form each kernel takes; form: 0 by the rules, 1 for few rows, 2 for many.  us, many -> few:
+//   forward, query rows x heads   packed documents, 2048 x 16 of 128 (longest 730): 31.6 -> 27.0   2048 x 16, one document: 57.0 -> 57.4
+//     2111 x 12 of 64, behind 4014 keys: 50.4 -> 35.8   4000 x 8 of 64: 47.4 -> 36.4   4096 x 16, 8 documents: 29.0 -> 49.4
+//   dQ   the same: 40.2 -> 33.4, 69.9 -> 61.8   4000 x 8 of 64: 54.3 -> 32.4   2000 x 32 of 64: 59.1 -> 50.7   4096 x 16 of 128: 37.5 -> 59.6
+//   dK/dV 2048 x 16 of 128: 58.0 -> 39.3, 99.5 -> 73.2   4095 x 16 (8 key heads) of 64: 85 -> 75   4096 x 16 of 128: 47.8 -> 66
+// At 32 k rows x heads the form for many has one workgroup per CU.
+static bool few_fwd(const RangeAttn& a, int form) { return form ? form == 1 : (i64)a.Tq * a.H <= 32 * 1024; }
+static bool few_dq(const RangeAttn& a, int form) { return form ? form == 1 : (i64)a.Tq * a.H <= (a.dh <= 64 ? 64 : 32) * 1024; }
+static bool few_dkv(const RangeAttn& a, int form) { return form ? form == 1 : (i64)a.Tk * a.Hkv <= 32 * 1024 && (i64)a.Tk * a.H <= 64 * 1024; }
+
+template <int DHP, int MOD> static void bwd(const RangeAttn& a, void* blocks, float* sums, int form, hipStream_t s) {
+  const bool fq = few_dq(a, form), fkv = few_dkv(a, form);
+  if (a.Tq > 0 && fq) {
+    static std::atomic<unsigned long long> mask{0};
+    constexpr unsigned smem = 4 * Tiles<DHP>::BYTES + 4 * 256;
+    set_lds(mask, range_dq_few_k<DHP, MOD>, smem);
+    FewShape f = few_shape(a, nullptr);
+    f.splits = 1;
+    const int tiles = f.tiles * a.Hkv * f.hb;
+    hipLaunchKernelGGL((range_dq_few_k<DHP, MOD>), dim3((unsigned)(tiles + cdiv(a.Tq, 64 * 4))), dim3(256), smem, s, a, f, tiles, (BlockSeen*)blocks);
+  } else if (a.Tq > 0) {
+    static std::atomic<unsigned long long> mask{0};
+    constexpr unsigned smem = 5 * Tiles<DHP>::BYTES;
+    set_lds(mask, range_bwd_dq_k<DHP, MOD>, smem);
+    hipLaunchKernelGGL((range_bwd_dq_k<DHP, MOD>), dim3((unsigned)((i64)cdiv(a.Tq, 128) * a.H)), dim3(256), smem, s, a, (BlockSeen*)blocks);
+  }
+  if (a.Tk <= 0) return;
+  const int parts = fkv ? dkv_parts_few(a) : dkv_parts(a);
+  if (fkv) {
+    static std::atomic<unsigned long long> mask{0};
+    constexpr unsigned smem = 4 * Tiles<DHP>::BYTES + 4 * 1280;
+    set_lds(mask, range_dkv_few_k<DHP, MOD>, smem);
+    hipLaunchKernelGGL((range_dkv_few_k<DHP, MOD>), dim3((unsigned)((i64)cdiv(a.Tk, 32) * a.Hkv * parts)), dim3(256), smem, s, a, (const BlockSeen*)blocks, sums, parts);
+  } else {
+    static std::atomic<unsigned long long> mask{0};
+    constexpr unsigned smem = 2 * DKV_STAGE<DHP>;
+    set_lds(mask, range_bwd_dkv_k<DHP, MOD>, smem);
+    hipLaunchKernelGGL((range_bwd_dkv_k<DHP, MOD>), dim3((unsigned)((i64)cdiv(a.Tk, 128) * a.Hkv * parts)), dim3(256), smem, s, a, (const BlockSeen*)blocks, sums, parts);
+  }
+  sum_parts<DHP>(a, sums, parts, s);
 }
-void launch_range_bwd_flash_few(const RangeAttn& a, void* blocks, hipStream_t s) {
-#define BWD_FEW(W, M) bwd_few<W, M>(a, blocks, s)
-  BY_FORM(BWD_FEW);
-}
-bool range_flash_few_bwd(const RangeAttn& a) { return (i64)a.Tq * a.H <= 32 * 1024; }
-template <int DHP, int MOD> static void fwd_few(const RangeAttn& a, float* work, hipStream_t s) {
+template <int DHP, int MOD> static void fwd(const RangeAttn& a, float* work, int form, hipStream_t s) {
   static std::atomic<unsigned long long> mask{0};
-  set_lds(mask, range_fwd_few_k<DHP, MOD>, FEW_SMEM<DHP>);
-  const FewShape f = few_shape(a, work);
-  hipLaunchKernelGGL((range_fwd_few_k<DHP, MOD>), dim3((unsigned)((i64)f.tiles * f.splits * a.Hkv * f.hb)), dim3(256), FEW_SMEM<DHP>, s, a, f);
-  if (f.splits > 1) hipLaunchKernelGGL((range_join_k<bf16, DHP>), dim3((unsigned)cdiv((i64)a.Tq * a.H, 4)), dim3(256), 0, s, a, f);
-}
-bool range_flash_few(const RangeAttn& a) { return (i64)a.Tq * a.H <= 16 * 1024; }
-void launch_range_fwd_flash_few(const RangeAttn& a, float* work, hipStream_t s) {
-  if (a.Tq <= 0) return;
-#define FEW(W, M) fwd_few<W, M>(a, work, s)
-  BY_FORM(FEW);
+  if (few_fwd(a, form)) {
+    set_lds(mask, range_fwd_few_k<DHP, MOD>, FEW_SMEM<DHP>);
+    const FewShape f = few_shape(a, work);
+    hipLaunchKernelGGL((range_fwd_few_k<DHP, MOD>), dim3((unsigned)((i64)f.tiles * f.splits * a.Hkv * f.hb)), dim3(256), FEW_SMEM<DHP>, s, a, f);
+    join_splits<bf16, DHP>(a, f, s);
+    return;
+  }
+  static std::atomic<unsigned long long> mask_many{0};
+  constexpr unsigned smem = 4 * Tiles<DHP>::BYTES;
+  set_lds(mask_many, range_fwd_k<DHP, MOD>, smem);
+  hipLaunchKernelGGL((range_fwd_k<DHP, MOD>), dim3((unsigned)((i64)cdiv(a.Tq, 128) * a.H)), dim3(256), smem, s, a);
 }
 size_t range_few_floats(const RangeAttn& a) { return few_floats(a); }
-void launch_range_fwd_flash(const RangeAttn& a, hipStream_t s) {
+void launch_range_fwd_flash(const RangeAttn& a, float* work, int form, hipStream_t s) {
   if (a.Tq <= 0) return;
-#define FWD(W, M) fwd<W, M>(a, s)
+#define FWD(W, M) fwd<W, M>(a, work, form, s)
   BY_FORM(FWD);
 }
-void launch_range_bwd_flash(const RangeAttn& a, void* blocks, float* sums, hipStream_t s) {
-#define BWD(W, M) bwd<W, M>(a, blocks, sums, s)
+void launch_range_bwd_flash(const RangeAttn& a, void* blocks, float* sums, int form, hipStream_t s) {
+#define BWD(W, M) bwd<W, M>(a, blocks, sums, form, s)
   BY_FORM(BWD);
 }

@@ -2,12 +2,21 @@
 // with float32 arithmetic.  It serves what the matrix-core kernels don't take.  Also the ranges themselves.
 #include "attn_range.h"
 
-// One thread per query row; a document's rows are found by bisection of cu_q.  A few loads per row: its launch bounds it.
+// One thread per query row; a document's rows are found by bisection of cu_q, of which LDS holds as much as fits, so that one load's
+// latency is paid and not one per step (7 documents, 2048 rows: 4.8 us without).
+#define CU_LDS 2048
 __global__ void __launch_bounds__(256) attn_ranges_k(const int* __restrict__ cu_q, const int* __restrict__ cu_k, const int* __restrict__ prefix,
                                                      int n_docs, int causal, int window, int Tq, int Tk, int* __restrict__ lo, int* __restrict__ hi,
                                                      int* __restrict__ at, int* __restrict__ used) {
   const i64 i = (i64)blockIdx.x * 256 + threadIdx.x;
+  __shared__ int table[CU_LDS];
   const int *cq = cu_q, *ck = cu_k ? cu_k : cu_q;
+  if (cu_q && n_docs < CU_LDS) {
+    for (int d = threadIdx.x; d <= n_docs; d += 256) table[d] = cu_q[d];
+    __syncthreads();
+    cq = table;
+    if (!cu_k) ck = table;
+  }
   if (i == 0 && used) {
     used[0] = cq ? min(max(cq[n_docs], 0), Tq) : Tq;
     used[1] = ck ? min(max(ck[n_docs], 0), Tk) : Tk;

@@ -366,14 +366,10 @@ void launch_range_bwd_rows(const RangeAttn& a, hipStream_t s);
 // range_flash_sum_floats floats
 bool range_flash_takes(const RangeAttn& a, bool back);
 size_t range_flash_sum_floats(const RangeAttn& a);
-void launch_range_fwd_flash(const RangeAttn& a, hipStream_t s);
-// the form for few rows, which splits the keys; work: range_few_floats floats
-bool range_flash_few(const RangeAttn& a);
-size_t range_few_floats(const RangeAttn& a);
-void launch_range_fwd_flash_few(const RangeAttn& a, float* work, hipStream_t s);
-void launch_range_bwd_flash(const RangeAttn& a, void* blocks, float* sums, hipStream_t s);
-bool range_flash_few_bwd(const RangeAttn& a);
-void launch_range_bwd_flash_few(const RangeAttn& a, void* blocks, hipStream_t s);
+size_t range_few_floats(const RangeAttn& a);        // (work of both forward passes, which may split the keys)
+// form: 0 by size, 1 the one for few rows, 2 the one for many
+void launch_range_fwd_flash(const RangeAttn& a, float* work, int form, hipStream_t s);
+void launch_range_bwd_flash(const RangeAttn& a, void* blocks, float* sums, int form, hipStream_t s);
 // the same in float32
 bool range_f32_takes(const RangeAttn& a, bool back);
 void launch_range_fwd_f32(const RangeAttn& a, float* work, hipStream_t s);
