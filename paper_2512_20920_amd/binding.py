@@ -408,33 +408,56 @@ def revffn_inverse_merged(ctx, weights, merged, y1, y2, x1, x2, B, S, ld, residu
 
 
 # ---- attention over key ranges, rotary positions, layer norm ----------------------------------------------------------
-def _check_tensors(dtype, typed, others=(), ints=(), work=None):
-    """Tensors must lie on the current device and have the element type that the call reads: `typed` the one of `dtype`,
-    `others` float32, `ints` int32; work may have any.  Raw addresses and None pass."""
-    import torch
-    device = torch.cuda.current_device() if torch.cuda.is_initialized() or torch.cuda.is_available() else -2
-    for group, want in ((typed, torch.bfloat16 if dtype == 1 else torch.float32), (others, torch.float32), (ints, torch.int32),
-                        ((work,), None)):
-        for t in group:
-            if t is None or isinstance(t, int):
-                continue
-            if t.get_device() != device:
-                raise RevffnError(f"a tensor on {t.device}, which is not the current device")
-            if want is not None and t.dtype != want:
-                raise RevffnError(f"a tensor of {t.dtype} where {want} is read")
+_torch = None
 
 
-def _work(work):
+def _device():
+    """torch and the current device.  (Small calls are bound by what the host does for them, so these functions look things up once.)"""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch, _torch.cuda.current_device() if _torch.cuda.is_available() else -2
+
+
+def _refuse(t, want):
+    if want is not None and t.dtype is not want:
+        raise RevffnError(f"a tensor of {t.dtype} where {want} is read")
+    raise RevffnError(f"a tensor on {t.device}, which is not the current device")
+
+
+def _addresses(device, want, *tensors):
+    """Addresses of tensors, which must lie on the current device and have the element type that the call reads (want = None: any).
+    Raw addresses and None pass."""
+    out = []
+    for t in tensors:
+        if t is None or type(t) is int:
+            out.append(t)
+        elif t.get_device() != device or (t.dtype is not want and want is not None):
+            _refuse(t, want)
+        else:
+            out.append(t.data_ptr())
+    return out
+
+
+def _on(stream, torch, device):
+    """The stream's handle; None: the current one of the current device."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device)
+    return stream if isinstance(stream, int) else stream.cuda_stream
+
+
+def _work(device, work):
     """(address, bytes) of a workspace tensor or None."""
     if work is None:
         return None, 0
-    return work.data_ptr(), work.numel() * work.element_size()
+    return _addresses(device, None, work)[0], work.numel() * work.element_size()
 
 
 def revffn_op_attention_ranges(cu_q, cu_k, prefix, n_docs, causal, window, Tq, Tk, lo, hi, at=None, used=None, stream=None):
-    _check_tensors(0, (), ints=(cu_q, cu_k, prefix, lo, hi, at, used))
-    _check(load_library().revffn_op_attention_ranges(_ptr(cu_q), _ptr(cu_k), _ptr(prefix), n_docs, int(causal), window, Tq, Tk,
-                                                     _ptr(lo), _ptr(hi), _ptr(at), _ptr(used), _stream(stream)))
+    torch, dev = _device()
+    q, k, p, l, h, a, u = _addresses(dev, torch.int32, cu_q, cu_k, prefix, lo, hi, at, used)
+    _check(load_library().revffn_op_attention_ranges(q, k, p, n_docs, int(causal), window, Tq, Tk, l, h, a, u, _on(stream, torch, dev)))
 
 
 def revffn_op_attention_masked_workspace(desc, backward):
@@ -442,18 +465,27 @@ def revffn_op_attention_masked_workspace(desc, backward):
     return load_library().revffn_op_attention_masked_workspace(ctypes.byref(desc), int(backward))
 
 
+def _element(torch, dtype):
+    return torch.bfloat16 if dtype == 1 else torch.float32
+
+
+def _attention_operands(desc, mask, *typed):
+    torch, dev = _device()
+    _addresses(dev, torch.float32, desc.kept)
+    _addresses(dev, torch.int32, *mask.kept)
+    return torch, dev, _addresses(dev, _element(torch, desc.dtype), *typed)
+
+
 def revffn_op_attention_masked_fwd(desc, mask, q, k, v, o, lse, work=None, stream=None):
-    _check_tensors(desc.dtype, (q, k, v, o), (lse, desc.kept), mask.kept, work)
-    w, n = _work(work)
-    _check(load_library().revffn_op_attention_masked_fwd(ctypes.byref(desc), ctypes.byref(mask), _ptr(q), _ptr(k), _ptr(v), _ptr(o),
-                                                         _ptr(lse), w, n, _stream(stream)))
+    torch, dev, p = _attention_operands(desc, mask, q, k, v, o)
+    _check(load_library().revffn_op_attention_masked_fwd(ctypes.byref(desc), ctypes.byref(mask), *p, *_addresses(dev, torch.float32, lse),
+                                                         *_work(dev, work), _on(stream, torch, dev)))
 
 
 def revffn_op_attention_masked_bwd(desc, mask, q, k, v, o, d_o, lse, dq, dk, dv, work=None, stream=None):
-    _check_tensors(desc.dtype, (q, k, v, o, d_o, dq, dk, dv), (lse, desc.kept), mask.kept, work)
-    w, n = _work(work)
-    _check(load_library().revffn_op_attention_masked_bwd(ctypes.byref(desc), ctypes.byref(mask), _ptr(q), _ptr(k), _ptr(v), _ptr(o),
-                                                         _ptr(d_o), _ptr(lse), _ptr(dq), _ptr(dk), _ptr(dv), w, n, _stream(stream)))
+    torch, dev, p = _attention_operands(desc, mask, q, k, v, o, d_o, dq, dk, dv)
+    _check(load_library().revffn_op_attention_masked_bwd(ctypes.byref(desc), ctypes.byref(mask), *p[:5], *_addresses(dev, torch.float32, lse),
+                                                         *p[5:], *_work(dev, work), _on(stream, torch, dev)))
 
 
 def revffn_op_rotary_frequencies(rotary):
@@ -465,9 +497,10 @@ def revffn_op_rotary_frequencies(rotary):
 
 
 def revffn_op_rotary(dtype, rotary, x, y, pos, T, S, H, dh, ldx, ldy, transposed=False, stream=None):
-    _check_tensors(dtype, (x, y), ints=(pos,))
-    _check(load_library().revffn_op_rotary(dtype, ctypes.byref(rotary), _ptr(x), _ptr(y), _ptr(pos), T, S, H, dh, ldx, ldy,
-                                           int(transposed), _stream(stream)))
+    torch, dev = _device()
+    px, py = _addresses(dev, _element(torch, dtype), x, y)
+    _check(load_library().revffn_op_rotary(dtype, ctypes.byref(rotary), px, py, *_addresses(dev, torch.int32, pos), T, S, H, dh, ldx, ldy,
+                                           int(transposed), _on(stream, torch, dev)))
 
 
 def revffn_op_layernorm_workspace(rows, cols):
@@ -475,14 +508,16 @@ def revffn_op_layernorm_workspace(rows, cols):
 
 
 def revffn_op_layernorm_fwd(dtype, x, gain, bias, y, mean, rstd, rows, cols, ldx, ldy, eps, stream=None):
-    _check_tensors(dtype, (x, gain, bias, y), (mean, rstd))
-    _check(load_library().revffn_op_layernorm_fwd(dtype, _ptr(x), _ptr(gain), _ptr(bias), _ptr(y), _ptr(mean), _ptr(rstd), rows, cols,
-                                                  ldx, ldy, eps, _stream(stream)))
+    torch, dev = _device()
+    _check(load_library().revffn_op_layernorm_fwd(dtype, *_addresses(dev, _element(torch, dtype), x, gain, bias, y),
+                                                  *_addresses(dev, torch.float32, mean, rstd), rows, cols, ldx, ldy, eps,
+                                                  _on(stream, torch, dev)))
 
 
 def revffn_op_layernorm_bwd(dtype, dy, x, gain, mean, rstd, dx, dgain, dbias, rows, cols, lddy, ldx, lddx, grads_f32=False, work=None,
                             stream=None):
-    _check_tensors(dtype, (dy, x, gain, dx) + (() if grads_f32 else (dgain, dbias)), (mean, rstd) + ((dgain, dbias) if grads_f32 else ()), work=work)
-    w, n = _work(work)
-    _check(load_library().revffn_op_layernorm_bwd(dtype, _ptr(dy), _ptr(x), _ptr(gain), _ptr(mean), _ptr(rstd), _ptr(dx), _ptr(dgain),
-                                                  _ptr(dbias), rows, cols, lddy, ldx, lddx, int(grads_f32), w, n, _stream(stream)))
+    torch, dev = _device()
+    dyp, xp, gp, dxp = _addresses(dev, _element(torch, dtype), dy, x, gain, dx)
+    grads = _addresses(dev, torch.float32 if grads_f32 else _element(torch, dtype), dgain, dbias)
+    _check(load_library().revffn_op_layernorm_bwd(dtype, dyp, xp, gp, *_addresses(dev, torch.float32, mean, rstd), dxp, *grads, rows, cols,
+                                                  lddy, ldx, lddx, int(grads_f32), *_work(dev, work), _on(stream, torch, dev)))

@@ -134,22 +134,22 @@ __device__ __forceinline__ BlockSeen block_seen(const RangeAttn& a, int b, int r
   const bool sees = r.x < r.y;
   return make_int4(wave_imin(sees ? r.x : INT_MAX), wave_imax(r.y), wave_imax(sees ? r.x : in ? INT_MAX : INT_MIN), wave_imin(sees ? r.y : in ? 0 : INT_MAX));
 }
-// Joins the splits (at most 64): a workgroup per (query row, head), each wave a quarter of them, all their loads in flight at once; DHP / 64
-// columns per lane.  (One wave per row, eight splits in flight: 64 splits of 160 rows 10.8 us.)
-template <class T, int DHP> __global__ void __launch_bounds__(256) range_join_k(RangeAttn a, FewShape f) {
-  __shared__ float sums[4][DHP], slow[2 * DHP];
+// Joins the splits of a (query row, head), W waves each a share of them (16 at most), all their loads in flight at once; DHP / 64
+// columns per lane.  (One wave for all, eight splits in flight: 64 splits of 160 rows 10.8 us, 4.8 like this.)
+template <class T, int DHP, int W> __global__ void __launch_bounds__(256) range_join_k(RangeAttn a, FewShape f) {
+  __shared__ float sums[4][DHP], slow[4][2 * DHP];
   constexpr int C = DHP / 64;
-  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rows = rows_in_use(a);
-  const i64 n = blockIdx.x;
-  const int i = (int)blockIdx.x / a.H, h = (int)blockIdx.x - i * a.H;
-  if (i >= rows) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wv = W == 4 ? wave : 0, rows = rows_in_use(a);
+  const i64 n = W == 4 ? (i64)blockIdx.x : (i64)blockIdx.x * 4 + wave;
+  const int i = (int)(n / a.H), h = (int)(n - (i64)i * a.H);
+  if (i >= rows) return;                             // (W = 4: all waves, W = 1: no barrier)
   const float2 st = lane < f.splits ? f.stats[n * f.splits + lane] : make_float2(-INFINITY, 0.f);
   const unsigned long long live = __ballot(st.y != 0.f);
   const float* p = f.part + n * f.splits * DHP + lane * C;
   float x[16][C];
 #pragma unroll
   for (int k = 0; k < 16; k++) {
-    const int s = k * 4 + wv;
+    const int s = k * W + wv;
 #pragma unroll
     for (int c = 0; c < C; c++) x[k][c] = (live >> s) & 1 ? p[s * DHP + c] : 0.f;
   }
@@ -159,23 +159,26 @@ template <class T, int DHP> __global__ void __launch_bounds__(256) range_join_k(
   float v[C] = {};
 #pragma unroll
   for (int k = 0; k < 16; k++) {
-    const float ws = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), k * 4 + wv));
+    const float ws = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), k * W + wv));
 #pragma unroll
     for (int c = 0; c < C; c++) v[c] = fmaf(ws, x[k][c], v[c]);
   }
+  if constexpr (W == 4) {
 #pragma unroll
-  for (int c = 0; c < C; c++) sums[wv][lane * C + c] = v[c];
-  __syncthreads();
-  if (wv) return;
+    for (int c = 0; c < C; c++) sums[wv][lane * C + c] = v[c];
+    __syncthreads();
+    if (wv) return;
+#pragma unroll
+    for (int c = 0; c < C; c++) {
+      const int k = lane * C + c;
+      v[c] = (sums[0][k] + sums[1][k]) + (sums[2][k] + sums[3][k]);
+    }
+  }
   float z = 0.f;
 #pragma unroll
-  for (int c = 0; c < C; c++) {
-    const int k = lane * C + c;
-    v[c] = (sums[0][k] + sums[1][k]) + (sums[2][k] + sums[3][k]);
-    z = fmaf(v[c], 0.f, z);
-  }
+  for (int c = 0; c < C; c++) z = fmaf(v[c], 0.f, z);
   if (!__all(z == 0.f)) {
-    range_row_fwd<T>(a, i, h, keys_in_use(a), slow);
+    range_row_fwd<T>(a, i, h, keys_in_use(a), slow[wave]);
     return;
   }
   const float inv = tot == 0.f ? 0.f : 1.f / tot;
@@ -185,7 +188,9 @@ template <class T, int DHP> __global__ void __launch_bounds__(256) range_join_k(
   if (lane == 0 && a.lse) a.lse[(i64)h * a.Tq + i] = tot == 0.f ? -INFINITY : (M + log2f(tot)) * LN2;
 }
 template <class T, int DHP> static void join_splits(const RangeAttn& a, const FewShape& f, hipStream_t s) {
-  if (f.splits > 1) hipLaunchKernelGGL((range_join_k<T, DHP>), dim3((unsigned)((i64)a.Tq * a.H)), dim3(256), 0, s, a, f);
+  const i64 n = (i64)a.Tq * a.H;
+  if (f.splits > 16) hipLaunchKernelGGL((range_join_k<T, DHP, 4>), dim3((unsigned)n), dim3(256), 0, s, a, f);
+  else if (f.splits > 1) hipLaunchKernelGGL((range_join_k<T, DHP, 1>), dim3((unsigned)cdiv(n, 4)), dim3(256), 0, s, a, f);
 }
 
 // workgroups that fill the chip twice, of 128 keys (a tile per wave) at least

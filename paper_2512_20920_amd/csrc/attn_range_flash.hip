@@ -1052,7 +1052,7 @@ template <int DHP> static void sum_parts(const RangeAttn& a, const float* sums, 
 // At 32 k rows x heads the form for many has one workgroup per CU.
 static bool few_fwd(const RangeAttn& a, int form) { return form ? form == 1 : (i64)a.Tq * a.H <= 32 * 1024; }
 static bool few_dq(const RangeAttn& a, int form) { return form ? form == 1 : (i64)a.Tq * a.H <= (a.dh <= 64 ? 64 : 32) * 1024; }
-static bool few_dkv(const RangeAttn& a, int form) { return form ? form == 1 : (i64)a.Tk * a.Hkv <= 32 * 1024 && (i64)a.Tk * a.H <= 64 * 1024; }
+static bool few_dkv(const RangeAttn& a, int form) { return form ? form == 1 : (a.G <= 2 || (i64)a.Tk * a.Hkv <= 4 * 1024) && (i64)a.Tk * a.H <= (a.G == 1 ? 32 : 64) * 1024; }
 
 template <int DHP, int MOD> static void bwd(const RangeAttn& a, void* blocks, float* sums, int form, hipStream_t s) {
   const bool fq = few_dq(a, form), fkv = few_dkv(a, form);

@@ -49,6 +49,33 @@ template <bool ALIGNED> __device__ __forceinline__ void store8(float* p, int lef
   }
 }
 
+// 8 columns as they are in memory: the next row's are on their way while a row is worked on
+template <class T, bool ALIGNED> struct Raw8;
+template <> struct Raw8<bf16, true> {
+  bf16x8_v v;
+  __device__ __forceinline__ void load(const bf16* p, int) { v = *(const bf16x8_v*)p; }
+  __device__ __forceinline__ void get(float (&r)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; i++) r[i] = (float)v[i];
+  }
+};
+template <> struct Raw8<float, true> {
+  float4 u, v;
+  __device__ __forceinline__ void load(const float* p, int) { u = *(const float4*)p; v = *(const float4*)(p + 4); }
+  __device__ __forceinline__ void get(float (&r)[8]) const { r[0] = u.x; r[1] = u.y; r[2] = u.z; r[3] = u.w; r[4] = v.x; r[5] = v.y; r[6] = v.z; r[7] = v.w; }
+};
+template <class T> struct Raw8<T, false> {
+  T v[8];
+  __device__ __forceinline__ void load(const T* p, int left) {
+#pragma unroll
+    for (int i = 0; i < 8; i++) v[i] = i < left ? p[i] : (T)0.f;
+  }
+  __device__ __forceinline__ void get(float (&r)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; i++) r[i] = (float)v[i];
+  }
+};
+
 // the sum over the WAVES waves that work on a row, in every thread of them; red: 2 * WAVES floats, which two sums use by turns
 template <int WAVES> __device__ __forceinline__ float row_sum(float v, float* red) {
   v = wave_sum(v);
@@ -152,10 +179,31 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) layernorm_bwd_k
   const float n = (float)cols;
   float dg[C][8] = {}, db[C][8] = {};
   int turn = 0;
-  for (i64 row = (i64)blockIdx.x * ROWS + (ROWS == 4 ? wv : 0); row < a.rows; row += (i64)gridDim.x * ROWS) {
+  i64 row = (i64)blockIdx.x * ROWS + (ROWS == 4 ? wv : 0);
+  const i64 step = (i64)gridDim.x * ROWS;
+  Raw8<T, ALIGNED> rx[C], rd[C];
+  float mean_next = 0.f, rstd_next = 0.f;
+  auto fetch = [&](i64 r) {
+    if (r >= a.rows) return;
+    mean_next = a.mean[r];
+    rstd_next = a.rstd[r];
+    if constexpr (CH > 0) {
+      const T *x = (const T*)a.x + r * a.ldx, *dy = (const T*)a.dy + r * a.lddy;
+#pragma unroll
+      for (int k = 0; k < C; k++) {
+        const int c = (tid + k * NT) * 8;
+        if (c < cols) {
+          rx[k].load(x + c, cols - c);
+          rd[k].load(dy + c, cols - c);
+        }
+      }
+    }
+  };
+  fetch(row);
+  for (; row < a.rows; row += step) {
     const T *x = (const T*)a.x + row * a.ldx, *dy = (const T*)a.dy + row * a.lddy;
     T* dx = (T*)a.dx + row * a.lddx;
-    const float mean = a.mean[row], rstd = a.rstd[row];
+    const float mean = mean_next, rstd = rstd_next;
     float s = 0.f, q = 0.f;
     if constexpr (CH > 0) {
       float xh[CH][8], d[CH][8];
@@ -163,10 +211,11 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) layernorm_bwd_k
       for (int k = 0; k < CH; k++) {
         const int c = (tid + k * NT) * 8;
         if (c < cols) {
-          load8<ALIGNED>(x + c, cols - c, xh[k]);
-          load8<ALIGNED>(dy + c, cols - c, d[k]);
+          rx[k].get(xh[k]);
+          rd[k].get(d[k]);
         }
       }
+      fetch(row + step);
 #pragma unroll
       for (int k = 0; k < CH; k++) {
         const int c = (tid + k * NT) * 8;
@@ -222,6 +271,7 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) layernorm_bwd_k
         for (int i = 0; i < 8; i++) d[i] = rstd * (d[i] - s - v[i] * q);
         store8<ALIGNED>(dx + c, cols - c, d);
       }
+      fetch(row + step);
     }
     turn ^= 2;                                       // (a slow wave may still read the last row's sums)
   }
@@ -273,25 +323,25 @@ template <class T> __global__ void __launch_bounds__(256) layernorm_params_k(Lay
   const float* p = &part[w][0][threadIdx.x & 63];
   a.partial[((i64)blockIdx.y * 2 + w) * a.cols + c] = (p[0] + p[64]) + (p[128] + p[192]);
 }
-// 64 columns of one of the two sums per workgroup, 4 threads to a column, each a quarter of the partial sums
+// 16 columns of one of the two sums per workgroup, 16 threads to a column, each every 16th of the partial sums
 template <class T> __global__ void __launch_bounds__(256) layernorm_reduce_k(const float* __restrict__ partial, int n, int cols, T* dgain, T* dbias) {
-  __shared__ float part[4][64];
-  const int c = (int)blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
+  __shared__ float part[16][17];
+  const int tc = threadIdx.x & 15, w = threadIdx.x >> 4, c = (int)blockIdx.x * 16 + tc;
   T* out = blockIdx.y ? dbias : dgain;
   if (!out) return;
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  float s = 0.f;
   if (c < cols) {
     const float* p = partial + (i64)blockIdx.y * cols + c;
-    const int per = (n + 3) / 4, end = min(n, (w + 1) * per);
-    int i = w * per;
-    for (; i + 3 < end; i += 4)
-#pragma unroll
-      for (int u = 0; u < 4; u++) s[u] += p[(i64)(i + u) * 2 * cols];
-    for (; i < end; i++) s[0] += p[(i64)i * 2 * cols];
+#pragma unroll 8
+    for (int i = w; i < n; i += 16) s += p[(i64)i * 2 * cols];
   }
-  part[w][threadIdx.x & 63] = (s[0] + s[1]) + (s[2] + s[3]);
+  part[w][tc] = s;
   __syncthreads();
-  if (w == 0 && c < cols) out[c] = from_f<T>((part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]));
+  if (w == 0 && c < cols) {
+#pragma unroll
+    for (int i = 1; i < 16; i++) s += part[i][tc];
+    out[c] = from_f<T>(s);
+  }
 }
 
 // partial sums: one per workgroup of the backward kernel
@@ -355,7 +405,7 @@ void launch_layernorm_bwd(const LayerNorm& a, hipStream_t s) {
     else n = al ? bwd<bf16, true>(a, params, s) : bwd<bf16, false>(a, params, s);
   }
   if (!params) return;
-  const dim3 grid(cdiv(a.cols, 64), 2);
+  const dim3 grid(cdiv(a.cols, 16), 2);
   if (a.dt == 0 || a.grads_f32) hipLaunchKernelGGL(layernorm_reduce_k<float>, grid, dim3(256), 0, s, a.partial, n, a.cols, (float*)a.dgain, (float*)a.dbias);
   else hipLaunchKernelGGL(layernorm_reduce_k<bf16>, grid, dim3(256), 0, s, a.partial, n, a.cols, (bf16*)a.dgain, (bf16*)a.dbias);
 }
