@@ -18,7 +18,7 @@ Scratch lay_out(const RangeAttn& a, bool backward, void* work) {
   if (backward) {
     w.dvec = (float*)take((size_t)a.H * a.Tq * 4);
     w.blocks = take(((size_t)a.Tq + 63) / 64 * 16);
-    if (a.dt == 1 && a.dh <= 128) w.sums = (float*)take(range_flash_sum_floats(a) * 4);
+    if (a.dh <= 128) w.sums = (float*)take((a.dt == 1 ? range_flash_sum_floats(a) : range_f32_sum_floats(a)) * 4);
   } else if (a.dh <= 128) w.parts = (float*)take(range_few_floats(a) * 4);
   return w;
 }
@@ -122,7 +122,7 @@ int revffn_op_attention_masked_bwd(const revffn_attn_desc* desc, const revffn_at
   a.q = q; a.k = k; a.v = v; a.o = o; a.d_o = d_o; a.lse = (float*)lse; a.dq = dq; a.dk = dk; a.dv = dv; a.dvec = w.dvec;
   const int mode = desc->kernel_mode & 0xff, form = desc->kernel_mode >> 8;
   if (mode != 1 && range_flash_takes(a, true)) launch_range_bwd_flash(a, w.blocks, w.sums, form, (hipStream_t)stream);
-  else if (mode != 1 && range_f32_takes(a, true)) launch_range_bwd_f32(a, w.blocks, (hipStream_t)stream);
+  else if (mode != 1 && range_f32_takes(a, true)) launch_range_bwd_f32(a, w.blocks, w.sums, (hipStream_t)stream);
   else if (mode == 2) return REVFFN_EUNSUPPORTED;
   else launch_range_bwd_rows(a, (hipStream_t)stream);
   return 0;

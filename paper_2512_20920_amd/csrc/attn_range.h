@@ -29,9 +29,9 @@ __device__ __forceinline__ int2 key_range(const RangeAttn& a, int i, int keys) {
   return r;
 }
 // the score from z = scale q.k, and what a gradient at the score is multiplied by to be one at z
-__device__ __forceinline__ float range_score(float z, float cap, float slope, int at, int j, float* keep) {
+template <bool CAPPED = true> __device__ __forceinline__ float range_score(float z, float cap, float slope, int at, int j, float* keep) {
   *keep = 1.f;
-  if (cap > 0.f) {
+  if (CAPPED && cap > 0.f) {
     const float t = tanhf(z / cap);
     z = t * cap;
     *keep = 1.f - t * t;

@@ -10,7 +10,6 @@
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 
-#define NW 4
 
 __device__ __forceinline__ int elem_row(int e, int half) { return (e >> 2) * 8 + half * 4 + (e & 3); }
 __device__ __forceinline__ float half_sum(float v) { return v + __shfl_xor(v, 32, WAVE); }
@@ -59,7 +58,8 @@ template <int DHP> __device__ __forceinline__ void spill(float* t, const f32x16 
 #pragma unroll
     for (int e = 0; e < 16; e++) t[(i * 32 + elem_row(e, lane >> 5)) * 32 + (lane & 31)] = acc[i][e];
 }
-template <int DHP> __global__ void __launch_bounds__(NW * 64) range_fwd_f32_k(RangeAttn a, FewShape f) {
+// CAP: with the tanh, whose code the other calls would fetch for nothing
+template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) range_fwd_f32_k(RangeAttn a, FewShape f) {
   extern __shared__ float sm[];                      // NW results [DHP][32], statistics
   int tile, split, head, t0;
   few_place(a, f, (int)blockIdx.x, &tile, &split, &head);
@@ -83,7 +83,7 @@ template <int DHP> __global__ void __launch_bounds__(NW * 64) range_fwd_f32_k(Ra
     for (int e = 0; e < 16; e++) {
       const int j = kv + elem_row(e, half);
       float keep;
-      s[e] = j >= fk.r.x && j < fk.r.y ? range_score(s[e], a.cap, slope, at, j, &keep) : -INFINITY;
+      s[e] = j >= fk.r.x && j < fk.r.y ? range_score<CAP>(s[e], a.cap, slope, at, j, &keep) : -INFINITY;
       mx = fmaxf(mx, s[e]);
     }
     mx = fmaxf(mx, __shfl_xor(mx, 32, WAVE));
@@ -107,7 +107,7 @@ template <int DHP> __global__ void __launch_bounds__(NW * 64) range_fwd_f32_k(Ra
 
 // dQ of 32 rows, and D = <o, dO>.  The last workgroups of the launch (from `tiles` on) note instead, a wave per block of 64 queries, the first key that
 // some of them see and one past the last.
-template <int DHP> __global__ void __launch_bounds__(NW * 64) range_dq_f32_k(RangeAttn a, FewShape f, int tiles, BlockSeen* __restrict__ blocks) {
+template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) range_dq_f32_k(RangeAttn a, FewShape f, int tiles, BlockSeen* __restrict__ blocks) {
   extern __shared__ float sm[];
   const int rows = rows_in_use(a), keys = keys_in_use(a);
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
@@ -145,7 +145,7 @@ template <int DHP> __global__ void __launch_bounds__(NW * 64) range_dq_f32_k(Ran
     for (int e = 0; e < 16; e++) {
       const int j = kv + elem_row(e, half);
       float keep;
-      const float x = range_score(s[e], a.cap, slope, at, j, &keep);
+      const float x = range_score<CAP>(s[e], a.cap, slope, at, j, &keep);
       s[e] = j >= fk.r.x && j < fk.r.y && L != -INFINITY ? expf(x - L) * (dp[e] - D) * keep : 0.f;
     }
     accumulate<DHP>(acc, k, a.ldk, a.dh, kv, fk.end - 1, s, lane);
@@ -162,9 +162,9 @@ template <int DHP> __global__ void __launch_bounds__(NW * 64) range_dq_f32_k(Ran
 }
 
 // dK, dV of 32 keys of a key head: the waves share out the blocks of 32 queries that see some of them, of every head that shares it.
-template <int DHP> __global__ void __launch_bounds__(NW * 64) range_dkv_f32_k(RangeAttn a, const BlockSeen* __restrict__ blocks) {
+template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) range_dkv_f32_k(RangeAttn a, const BlockSeen* __restrict__ blocks, float* __restrict__ sums, int parts) {
   extern __shared__ float sm[];                      // NW results [DHP][32], then 5 x 32 words per wave
-  const int kt = (int)blockIdx.x / a.Hkv, kh = (int)blockIdx.x - kt * a.Hkv, k0 = kt * 32;
+  const int per = a.Hkv * parts, kt = (int)blockIdx.x / per, r0 = (int)blockIdx.x - kt * per, kh = r0 % a.Hkv, part = r0 / a.Hkv, k0 = kt * 32;
   const int rows = rows_in_use(a), keys = keys_in_use(a);
   if (k0 >= keys) return;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, myk = k0 + (lane & 31);
@@ -183,7 +183,7 @@ template <int DHP> __global__ void __launch_bounds__(NW * 64) range_dkv_f32_k(Ra
       live &= live - 1;
       for (int n = 0; n < 2 * a.G; n++, turn++) {
         const int q0 = b * 64 + (n & 1) * 32, h = kh * a.G + (n >> 1), i = q0 + (lane & 31);
-        if (turn % NW != wv || q0 >= rows) continue;
+        if (turn % (NW * parts) != part * NW + wv || q0 >= rows) continue;
         const int2 see = i < rows ? key_range(a, i, keys) : make_int2(0, 0);
         if (!__any(see.x < k0 + 32 && see.y > k0)) continue;
         const int ic = min(i, rows - 1);
@@ -207,7 +207,7 @@ template <int DHP> __global__ void __launch_bounds__(NW * 64) range_dkv_f32_k(Ra
           const float L = words[x];
           const bool sees = myk >= ((const int*)words)[96 + x] && myk < ((const int*)words)[128 + x] && L != -INFINITY;
           float keep;
-          const float p = expf(range_score(s[e], a.cap, slope, ((const int*)words)[64 + x], myk, &keep) - L);
+          const float p = expf(range_score<CAP>(s[e], a.cap, slope, ((const int*)words)[64 + x], myk, &keep) - L);
           dp[e] = sees ? p * (dp[e] - words[32 + x]) * keep : 0.f;
           s[e] = sees ? p : 0.f;
         }
@@ -217,6 +217,17 @@ template <int DHP> __global__ void __launch_bounds__(NW * 64) range_dkv_f32_k(Ra
     }
   }
   const int r = k0 + (int)(threadIdx.x & 31);
+  if (parts > 1) {
+    float* row = sums + ((((i64)part * 2) * a.Tk + r) * a.Hkv + kh) * DHP;
+    spill<DHP>(sm + wv * DHP * 32, dka, lane);
+    __syncthreads();
+    (void)few_store<float, DHP, NW>(sm, row, r < keys, DHP, 1.f);
+    __syncthreads();
+    spill<DHP>(sm + wv * DHP * 32, dva, lane);
+    __syncthreads();
+    (void)few_store<float, DHP, NW>(sm, row + (i64)a.Tk * a.Hkv * DHP, r < keys, DHP, 1.f);
+    return;
+  }
   spill<DHP>(sm + wv * DHP * 32, dka, lane);
   __syncthreads();
   bool fine = few_store<float, DHP, NW>(sm, (float*)a.dk + (i64)r * a.ldk + (i64)kh * a.dh, r < keys, a.dh, a.scale);
@@ -241,29 +252,55 @@ template <class K> static void set_lds(std::atomic<unsigned long long>& mask, K 
     attr_done(mask);
   }
 }
-template <int DHP> static void fwd(const RangeAttn& a, float* work, hipStream_t s) {
+template <int DHP, int NW, bool CAP> static void fwd(const RangeAttn& a, float* work, hipStream_t s) {
   constexpr size_t smem = (size_t)(NW * DHP * 32 + NW * 64) * 4;
   static std::atomic<unsigned long long> mask{0};
-  set_lds(mask, range_fwd_f32_k<DHP>, smem);
+  set_lds(mask, range_fwd_f32_k<DHP, NW, CAP>, smem);
   const FewShape f = few_shape(a, work);
-  hipLaunchKernelGGL(range_fwd_f32_k<DHP>, dim3((unsigned)((i64)f.tiles * f.splits * a.Hkv * f.hb)), dim3(NW * 64), smem, s, a, f);
+  hipLaunchKernelGGL((range_fwd_f32_k<DHP, NW, CAP>), dim3((unsigned)((i64)f.tiles * f.splits * a.Hkv * f.hb)), dim3(NW * 64), smem, s, a, f);
   join_splits<float, DHP>(a, f, s);
 }
-template <int DHP> static void bwd(const RangeAttn& a, void* blocks, hipStream_t s) {
+// dK/dV: the pairs of a block of 32 queries and a head in parts, where the workgroups leave CUs idle
+static int dkv_parts(const RangeAttn& a) {
+  const i64 workgroups = (i64)cdiv(a.Tk, 32) * a.Hkv, pairs = (i64)cdiv(a.Tq, 32) * a.G;
+  const int waves = few_waves(a);
+  int n = 1;
+  while (n < 8 && workgroups * n * 2 * waves <= 2048 && pairs >= 2 * n * waves) n *= 2;
+  return n;
+}
+size_t range_f32_sum_floats(const RangeAttn& a) {
+  const int n = dkv_parts(a);
+  return n > 1 ? (size_t)n * 2 * a.Tk * a.Hkv * (a.dh <= 64 ? 64 : 128) : 0;
+}
+template <int DHP, int NW, bool CAP> static void bwd(const RangeAttn& a, void* blocks, float* sums, hipStream_t s) {
   constexpr size_t smem = (size_t)NW * DHP * 32 * 4, smem_kv = smem + NW * 160 * 4;
   static std::atomic<unsigned long long> mask_q{0}, mask_kv{0};
-  set_lds(mask_q, range_dq_f32_k<DHP>, smem);
-  set_lds(mask_kv, range_dkv_f32_k<DHP>, smem_kv);
+  set_lds(mask_q, range_dq_f32_k<DHP, NW, CAP>, smem);
+  set_lds(mask_kv, range_dkv_f32_k<DHP, NW, CAP>, smem_kv);
   FewShape f = few_shape(a, nullptr);
   f.splits = 1;
   const int tiles = f.tiles * a.Hkv * f.hb;
-  if (a.Tq > 0) hipLaunchKernelGGL(range_dq_f32_k<DHP>, dim3((unsigned)(tiles + cdiv(a.Tq, 64 * NW))), dim3(NW * 64), smem, s, a, f, tiles, (BlockSeen*)blocks);
-  if (a.Tk > 0) hipLaunchKernelGGL(range_dkv_f32_k<DHP>, dim3((unsigned)((i64)cdiv(a.Tk, 32) * a.Hkv)), dim3(NW * 64), smem_kv, s, a, (const BlockSeen*)blocks);
+  if (a.Tq > 0)
+    hipLaunchKernelGGL((range_dq_f32_k<DHP, NW, CAP>), dim3((unsigned)(tiles + cdiv(a.Tq, 64 * NW))), dim3(NW * 64), smem, s, a, f, tiles, (BlockSeen*)blocks);
+  if (a.Tk <= 0) return;
+  const int parts = dkv_parts(a);
+  hipLaunchKernelGGL((range_dkv_f32_k<DHP, NW, CAP>), dim3((unsigned)((i64)cdiv(a.Tk, 32) * a.Hkv * parts)), dim3(NW * 64), smem_kv, s, a,
+                     (const BlockSeen*)blocks, sums, parts);
+  sum_parts<float, DHP>(a, sums, parts, s);
 }
+// 8 waves per workgroup; 128 columns take more registers than 8 waves leave each
+#define BY_FORM(call)                                                  \
+  do {                                                                 \
+    if (a.dh <= 64) { if (a.cap > 0.f) call(64, 8, true); else call(64, 8, false); } \
+    else if (a.cap > 0.f) call(128, 4, true);                          \
+    else call(128, 4, false);                                          \
+  } while (0)
 void launch_range_fwd_f32(const RangeAttn& a, float* work, hipStream_t s) {
   if (a.Tq <= 0) return;
-  if (a.dh <= 64) fwd<64>(a, work, s); else fwd<128>(a, work, s);
+#define FWD(D, W, C) fwd<D, W, C>(a, work, s)
+  BY_FORM(FWD);
 }
-void launch_range_bwd_f32(const RangeAttn& a, void* blocks, hipStream_t s) {
-  if (a.dh <= 64) bwd<64>(a, blocks, s); else bwd<128>(a, blocks, s);
+void launch_range_bwd_f32(const RangeAttn& a, void* blocks, float* sums, hipStream_t s) {
+#define BWD(D, W, C) bwd<D, W, C>(a, blocks, sums, s)
+  BY_FORM(BWD);
 }

@@ -193,15 +193,49 @@ template <class T, int DHP> static void join_splits(const RangeAttn& a, const Fe
   else if (f.splits > 1) hipLaunchKernelGGL((range_join_k<T, DHP, 1>), dim3((unsigned)cdiv(n, 4)), dim3(256), 0, s, a, f);
 }
 
-// workgroups that fill the chip twice, of 128 keys (a tile per wave) at least
+// dK and dV from the parts' sums, [part][dk, dv][key row, head][DHP]: one wave per key row and head, DHP / 64 columns per lane
+template <class T, int DHP> __global__ void __launch_bounds__(256) range_dkv_sum_k(RangeAttn a, const float* __restrict__ sums, int parts) {
+  __shared__ float lds[4][2 * DHP];
+  constexpr int C = DHP / 64;
+  const int rows = rows_in_use(a), keys = keys_in_use(a), lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const i64 n = (i64)blockIdx.x * 4 + wv;
+  const int j = (int)(n / a.Hkv), kh = (int)(n - (i64)j * a.Hkv);
+  if (j >= keys) return;
+  float k[C] = {}, v[C] = {};
+  const i64 half = (i64)a.Tk * a.Hkv * DHP;
+  const float* p = sums + n * DHP + lane * C;
+#pragma unroll 4
+  for (int i = 0; i < parts; i++)
+#pragma unroll
+    for (int c = 0; c < C; c++) { k[c] += p[(i64)i * 2 * half + c]; v[c] += p[(i64)i * 2 * half + half + c]; }
+  float z = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; c++) z = __builtin_fmaf(k[c], 0.f, __builtin_fmaf(v[c], 0.f, z));
+  if (!__all(z == 0.f)) {                           // a value that is not finite: seen, or only in a tile with seen ones?
+    range_row_dkv<T>(a, j, kh, rows, keys, lds[wv]);
+    return;
+  }
+  T *dk = (T*)a.dk + (i64)j * a.ldk + (i64)kh * a.dh, *dv = (T*)a.dv + (i64)j * a.ldv + (i64)kh * a.dh;
+#pragma unroll
+  for (int c = 0; c < C; c++)
+    if (lane * C + c < a.dh) { dk[lane * C + c] = from_f<T>(k[c] * a.scale); dv[lane * C + c] = from_f<T>(v[c]); }
+}
+
+template <class T, int DHP> static void sum_parts(const RangeAttn& a, const float* sums, int parts, hipStream_t s) {
+  if (parts > 1) hipLaunchKernelGGL((range_dkv_sum_k<T, DHP>), dim3((unsigned)cdiv((i64)a.Tk * a.Hkv, 4)), dim3(256), 0, s, a, sums, parts);
+}
+
+inline int few_waves(const RangeAttn& a) { return a.dt == 0 && a.dh <= 64 ? 8 : 4; }      // of a workgroup
+// Workgroups that give every CU eight waves, of a tile of keys per wave at least.
 inline FewShape few_shape(const RangeAttn& a, float* work) {
+  const int waves = few_waves(a);
   FewShape f;
   f.gp = a.G < 32 ? a.G : 32;
   f.hb = (a.G + f.gp - 1) / f.gp;
   f.qpt = 32 / f.gp;
   f.tiles = cdiv(a.Tq, f.qpt);
-  const i64 workgroups = (i64)f.tiles * a.Hkv * f.hb, most = cdiv(a.Tk, 128);
-  i64 n = workgroups ? 512 / workgroups : 1;
+  const i64 workgroups = (i64)f.tiles * a.Hkv * f.hb, most = cdiv(a.Tk, 32 * waves);
+  i64 n = workgroups ? 2048 / waves / workgroups : 1;
   if (n > most) n = most;
   if (n > 64) n = 64;
   f.splits = n < 1 ? 1 : (int)n;

@@ -678,34 +678,6 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dkv_k(RangeAttn a, const Blo
     T::store((bf16*)b.dv + (i64)mykv * b.ldv + (i64)kh * b.dh, dvacc, 1.0f, b.dh, g);
   }
 }
-// the sum of the parts, one wave per key row and head: 2 columns per lane (DHP = 64: one)
-template <int DHP> __global__ void __launch_bounds__(256) range_dkv_sum_k(RangeAttn a, const float* __restrict__ sums, int parts) {
-  __shared__ float lds[4][2 * DHP];
-  constexpr int C = DHP / 64;
-  const int rows = rows_in_use(a), keys = keys_in_use(a), lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  const i64 n = (i64)blockIdx.x * 4 + wv;
-  const int j = (int)(n / a.Hkv), kh = (int)(n - (i64)j * a.Hkv);
-  if (j >= keys) return;
-  float k[C] = {}, v[C] = {};
-  const i64 half = (i64)a.Tk * a.Hkv * DHP;
-  const float* p = sums + n * DHP + lane * C;
-#pragma unroll 4
-  for (int i = 0; i < parts; i++)
-#pragma unroll
-    for (int c = 0; c < C; c++) { k[c] += p[(i64)i * 2 * half + c]; v[c] += p[(i64)i * 2 * half + half + c]; }
-  float z = 0.f;
-#pragma unroll
-  for (int c = 0; c < C; c++) z = __builtin_fmaf(k[c], 0.f, __builtin_fmaf(v[c], 0.f, z));
-  if (!__all(z == 0.f)) {                           // a value that is not finite: seen, or only in a tile with seen ones?
-    range_row_dkv<bf16>(a, j, kh, rows, keys, lds[wv]);
-    return;
-  }
-  bf16 *dk = (bf16*)a.dk + (i64)j * a.ldk + (i64)kh * a.dh, *dv = (bf16*)a.dv + (i64)j * a.ldv + (i64)kh * a.dh;
-#pragma unroll
-  for (int c = 0; c < C; c++)
-    if (lane * C + c < a.dh) { dk[lane * C + c] = (bf16)(k[c] * a.scale); dv[lane * C + c] = (bf16)v[c]; }
-}
-
 // ------------------------------------------------------------------------------------
 // Backward for few rows: dQ of 32 rows, then dK/dV of 32 keys per workgroup, the keys (the blocks of 32 queries and the heads that share the
 // key head) shared out to the waves, each with tiles of its own in LDS.
@@ -1041,9 +1013,6 @@ size_t range_flash_sum_floats(const RangeAttn& a) {
   const int n = dkv_parts(a) > dkv_parts_few(a) ? dkv_parts(a) : dkv_parts_few(a);
   return n > 1 ? (size_t)n * 2 * a.Tk * a.Hkv * (a.dh <= 64 ? 64 : 128) : 0;
 }
-template <int DHP> static void sum_parts(const RangeAttn& a, const float* sums, int parts, hipStream_t s) {
-  if (parts > 1) hipLaunchKernelGGL(range_dkv_sum_k<DHP>, dim3((unsigned)cdiv((i64)a.Tk * a.Hkv, 4)), dim3(256), 0, s, a, sums, parts);
-}
 // Which form each kernel takes; form: 0 by the rules, 1 for few rows, 2 for many.  us, many -> few:
 //   forward, query rows x heads   packed documents, 2048 x 16 of 128 (longest 730): 31.6 -> 27.0   2048 x 16, one document: 57.0 -> 57.4
 //     2111 x 12 of 64, behind 4014 keys: 50.4 -> 35.8   4000 x 8 of 64: 47.4 -> 36.4   4096 x 16, 8 documents: 29.0 -> 49.4
@@ -1083,7 +1052,7 @@ template <int DHP, int MOD> static void bwd(const RangeAttn& a, void* blocks, fl
     set_lds(mask, range_bwd_dkv_k<DHP, MOD>, smem);
     hipLaunchKernelGGL((range_bwd_dkv_k<DHP, MOD>), dim3((unsigned)((i64)cdiv(a.Tk, 128) * a.Hkv * parts)), dim3(256), smem, s, a, (const BlockSeen*)blocks, sums, parts);
   }
-  sum_parts<DHP>(a, sums, parts, s);
+  sum_parts<bf16, DHP>(a, sums, parts, s);
 }
 template <int DHP, int MOD> static void fwd(const RangeAttn& a, float* work, int form, hipStream_t s) {
   static std::atomic<unsigned long long> mask{0};

@@ -373,7 +373,8 @@ void launch_range_bwd_flash(const RangeAttn& a, void* blocks, float* sums, int f
 // the same in float32
 bool range_f32_takes(const RangeAttn& a, bool back);
 void launch_range_fwd_f32(const RangeAttn& a, float* work, hipStream_t s);
-void launch_range_bwd_f32(const RangeAttn& a, void* blocks, hipStream_t s);
+size_t range_f32_sum_floats(const RangeAttn& a);
+void launch_range_bwd_f32(const RangeAttn& a, void* blocks, float* sums, hipStream_t s);
 
 // ---- rotary positions, layer norm ---------------------------------------------------------------------------
 #define ROTARY_MAX_DIMS 256
