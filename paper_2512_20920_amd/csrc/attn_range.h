@@ -23,11 +23,15 @@ __device__ __forceinline__ int wave_imin(int v) { return -1 - wave_imax(-1 - v);
 __device__ __forceinline__ int rows_in_use(const RangeAttn& a) { return a.used ? min(max(a.used[0], 0), a.Tq) : a.Tq; }
 __device__ __forceinline__ int keys_in_use(const RangeAttn& a) { return a.used ? min(max(a.used[1], 0), a.Tk) : a.Tk; }
 // clamped; lo = hi = 0 if there is none
-__device__ __forceinline__ int2 key_range(const RangeAttn& a, int i, int keys) {
-  int2 r = make_int2(max(a.lo[i], 0), min(a.hi[i], keys));
+__device__ __forceinline__ int2 clamped(int2 r, int keys) {
+  r = make_int2(max(r.x, 0), min(r.y, keys));
   if (r.x >= r.y) r.x = r.y = 0;
   return r;
 }
+// A workgroup's first loads wait for nothing: ranges (and queries) are read by clamped row number while the rows and keys in use
+// are on their way too.
+__device__ __forceinline__ int2 stored_range(const RangeAttn& a, int i) { i = min(i, a.Tq - 1); return make_int2(a.lo[i], a.hi[i]); }
+__device__ __forceinline__ int2 key_range(const RangeAttn& a, int i, int keys) { return clamped(make_int2(a.lo[i], a.hi[i]), keys); }
 // the score from z = scale q.k, and what a gradient at the score is multiplied by to be one at z
 template <bool CAPPED = true> __device__ __forceinline__ float range_score(float z, float cap, float slope, int at, int j, float* keep) {
   *keep = 1.f;

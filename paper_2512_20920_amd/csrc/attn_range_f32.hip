@@ -63,16 +63,18 @@ template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) 
   extern __shared__ float sm[];                      // NW results [DHP][32], statistics
   int tile, split, head, t0;
   few_place(a, f, (int)blockIdx.x, &tile, &split, &head);
-  const int rows = rows_in_use(a), keys = keys_in_use(a);
-  if (tile * f.qpt >= rows) return;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, kh = head % a.Hkv;
-  const FewRow row = few_row(a, f, tile, head, lane & 31, rows);
-  const FewKeys fk = few_keys(a, f, row, split, keys, &t0);
+  FewRow row = few_row(a, f, tile, head, lane & 31, a.Tq);
+  const int2 stored = stored_range(a, row.i);
   const float slope = a.slopes ? a.slopes[row.h] : 0.f;
   const int at = row.ok && a.at ? a.at[row.i] : row.i;
   const float *k = (const float*)a.k + (i64)kh * a.dh, *v = (const float*)a.v + (i64)kh * a.dh;
   float qf[DHP / 2];
   load_row<DHP>((const float*)a.q + (i64)row.i * a.ldq + (i64)row.h * a.dh, row.ok, a.dh, half, a.scale, qf);
+  const int rows = rows_in_use(a), keys = keys_in_use(a);
+  if (tile * f.qpt >= rows) return;
+  row.ok = row.ok && row.i < rows;
+  const FewKeys fk = few_keys(f, row, stored, split, keys, &t0);
   f32x16 acc[DHP / 32] = {};
   float m = -INFINITY, l = 0.f;
   for (int t = fk.live_from(t0 + wv, NW); t < fk.t1; t = fk.live_from(t + NW, NW)) {
@@ -109,20 +111,18 @@ template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) 
 // some of them see and one past the last.
 template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) range_dq_f32_k(RangeAttn a, FewShape f, int tiles, BlockSeen* __restrict__ blocks) {
   extern __shared__ float sm[];
-  const int rows = rows_in_use(a), keys = keys_in_use(a);
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
   if ((int)blockIdx.x >= tiles) {
     const int b = ((int)blockIdx.x - tiles) * NW + wv;
-    const BlockSeen r = block_seen(a, b, rows, keys, lane);
+    const BlockSeen r = block_seen(a, b, rows_in_use(a), keys_in_use(a), lane);
     if (lane == 0 && b * 64 < a.Tq) blocks[b] = r;
     return;
   }
   int tile, split, head, t0;
   few_place(a, f, (int)blockIdx.x, &tile, &split, &head);
-  if (tile * f.qpt >= rows) return;
   const int kh = head % a.Hkv;
-  const FewRow row = few_row(a, f, tile, head, lane & 31, rows);
-  const FewKeys fk = few_keys(a, f, row, 0, keys, &t0);
+  FewRow row = few_row(a, f, tile, head, lane & 31, a.Tq);
+  const int2 stored = stored_range(a, row.i);
   const float slope = a.slopes ? a.slopes[row.h] : 0.f;
   const int at = row.ok && a.at ? a.at[row.i] : row.i;
   const float *k = (const float*)a.k + (i64)kh * a.dh, *v = (const float*)a.v + (i64)kh * a.dh;
@@ -130,12 +130,16 @@ template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) 
   float qf[DHP / 2], dof[DHP / 2], D = 0.f;
   load_row<DHP>((const float*)a.d_o + orow, row.ok, a.dh, half, 1.f, dof);
   load_row<DHP>((const float*)a.o + orow, row.ok, a.dh, half, 1.f, qf);
+  const float L = row.ok ? a.lse[srow] : -INFINITY;
+  const int rows = rows_in_use(a), keys = keys_in_use(a);
+  if (tile * f.qpt >= rows) return;
+  row.ok = row.ok && row.i < rows;
+  const FewKeys fk = few_keys(f, row, stored, 0, keys, &t0);
 #pragma unroll
   for (int c = 0; c < DHP / 2; c++) D = fmaf(qf[c], dof[c], D);
   D = half_sum(D);
   if (wv == 0 && half == 0 && row.ok) a.dvec[srow] = D;
   load_row<DHP>((const float*)a.q + qrow, row.ok, a.dh, half, a.scale, qf);
-  const float L = row.ok ? a.lse[srow] : -INFINITY;
   f32x16 acc[DHP / 32] = {};
   for (int t = fk.live_from(t0 + wv, NW); t < fk.t1; t = fk.live_from(t + NW, NW)) {
     const int kv = fk.first + t * 32, jc = min(kv + (lane & 31), fk.end - 1);
@@ -165,13 +169,13 @@ template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) 
 template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) range_dkv_f32_k(RangeAttn a, const BlockSeen* __restrict__ blocks, float* __restrict__ sums, int parts) {
   extern __shared__ float sm[];                      // NW results [DHP][32], then 5 x 32 words per wave
   const int per = a.Hkv * parts, kt = (int)blockIdx.x / per, r0 = (int)blockIdx.x - kt * per, kh = r0 % a.Hkv, part = r0 / a.Hkv, k0 = kt * 32;
-  const int rows = rows_in_use(a), keys = keys_in_use(a);
-  if (k0 >= keys) return;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, myk = k0 + (lane & 31);
   float* words = sm + NW * DHP * 32 + wv * 160;
   float kf[DHP / 2], vf[DHP / 2];
-  load_row<DHP>((const float*)a.k + (i64)myk * a.ldk + (i64)kh * a.dh, myk < keys, a.dh, half, a.scale, kf);
-  load_row<DHP>((const float*)a.v + (i64)myk * a.ldv + (i64)kh * a.dh, myk < keys, a.dh, half, 1.f, vf);
+  load_row<DHP>((const float*)a.k + (i64)myk * a.ldk + (i64)kh * a.dh, myk < a.Tk, a.dh, half, a.scale, kf);
+  load_row<DHP>((const float*)a.v + (i64)myk * a.ldv + (i64)kh * a.dh, myk < a.Tk, a.dh, half, 1.f, vf);
+  const int rows = rows_in_use(a), keys = keys_in_use(a);
+  if (k0 >= keys) return;
   f32x16 dka[DHP / 32] = {}, dva[DHP / 32] = {};
   const int nb = (rows + 63) / 64;
   int turn = 0;

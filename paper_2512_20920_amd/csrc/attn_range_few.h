@@ -26,6 +26,7 @@ __device__ __forceinline__ void few_place(const RangeAttn& a, const FewShape& f,
   *head = id - row * heads;
   *tile = row / f.splits;
   *split = row - *tile * f.splits;
+  *tile = f.tiles - 1 - *tile;                       // late queries tend to have the long ranges
 }
 // the keys that the 32 rows see, in tiles of 32 from the first one on
 struct FewKeys {
@@ -43,9 +44,9 @@ struct FewKeys {
     return t;
   }
 };
-__device__ __forceinline__ FewKeys few_keys(const RangeAttn& a, const FewShape& f, const FewRow& row, int split, int keys, int* t0) {
+__device__ __forceinline__ FewKeys few_keys(const FewShape& f, const FewRow& row, int2 stored, int split, int keys, int* t0) {
   FewKeys k;
-  k.r = row.ok ? key_range(a, row.i, keys) : make_int2(0, 0);
+  k.r = row.ok ? clamped(stored, keys) : make_int2(0, 0);
   if (k.r.x == k.r.y) k.r = make_int2(INT_MAX, 0);
   k.first = wave_imin(k.r.x);
   k.end = wave_imax(k.r.y);
@@ -238,7 +239,7 @@ inline FewShape few_shape(const RangeAttn& a, float* work) {
   i64 n = workgroups ? 2048 / waves / workgroups : 1;
   if (n > most) n = most;
   if (n > 64) n = 64;
-  f.splits = n < 1 ? 1 : (int)n;
+  f.splits = n < (a.dt == 0 ? 2 : 4) ? 1 : (int)n;
   f.stats = (float2*)work;
   f.part = work ? work + 2 * (i64)a.Tq * a.H * f.splits : nullptr;
   if ((2 * (i64)a.Tq * a.H * f.splits) % 4) f.part += 2;     // (16-byte aligned)

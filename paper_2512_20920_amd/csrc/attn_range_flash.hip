@@ -23,9 +23,9 @@ struct TwoRanges { int2 r0, r1; };                  // of queries q0 + lane, q0 
 __device__ __forceinline__ TwoRanges two_ranges(const RangeAttn& a, int q0, int rows, int keys) {
   const int lane = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
   TwoRanges t;
-  const int2 none = make_int2(INT_MAX, 0);
-  t.r0 = q0 + lane < rows ? key_range(a, q0 + lane, keys) : none;
-  t.r1 = q0 + 64 + lane < rows ? key_range(a, q0 + 64 + lane, keys) : none;
+  const int2 none = make_int2(INT_MAX, 0), s0 = stored_range(a, q0 + lane), s1 = stored_range(a, q0 + 64 + lane);
+  t.r0 = q0 + lane < rows ? clamped(s0, keys) : none;
+  t.r1 = q0 + 64 + lane < rows ? clamped(s1, keys) : none;
   if (t.r0.x == t.r0.y) t.r0 = none;
   if (t.r1.x == t.r1.y) t.r1 = none;
   return t;
@@ -238,13 +238,17 @@ __global__ void __launch_bounds__(256, 2) range_fwd_few_k(RangeAttn a, FewShape 
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem_raw[];
   int tile, split, head, t0;
   few_place(a, f, (int)blockIdx.x, &tile, &split, &head);
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, kh = head % a.Hkv;
+  FewRow row = few_row(a, f, tile, head, lane & 31, a.Tq);
+  const int2 stored = stored_range(a, row.i);
+  const int at = (MOD & BIASED) && row.ok ? (a.at ? a.at[row.i] : row.i) : 0;
+  bf16x8 qf[T::KK];
+  T::load_frags((const bf16*)a.q + (i64)row.i * a.ldq + (i64)row.h * a.dh, row.ok, a.dh, g, qf);
   const int rows = rows_in_use(a), keys = keys_in_use(a);
   if (tile * f.qpt >= rows) return;
-  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, kh = head % a.Hkv;
-  const FewRow row = few_row(a, f, tile, head, lane & 31, rows);
-  const FewKeys fk = few_keys(a, f, row, split, keys, &t0);
+  row.ok = row.ok && row.i < rows;
+  const FewKeys fk = few_keys(f, row, stored, split, keys, &t0);
   const ScoreForm sf = score_form(a, row.h);
-  const int at = (MOD & BIASED) && row.ok ? (a.at ? a.at[row.i] : row.i) : 0;
   const HeadRows rk = {(const unsigned char*)a.k + (i64)kh * a.dh * 2, a.ldk * 2, a.dh * 2}, rv = {(const unsigned char*)a.v + (i64)kh * a.dh * 2, a.ldv * 2, a.dh * 2};
   unsigned char* tK = smem_raw + wv * T::BYTES;      // 32 rows of K, 32 of V
   const unsigned aK = lds_address(smem_raw) + (unsigned)wv * T::BYTES, aV = aK + T::BYTES / 2;
@@ -257,8 +261,6 @@ __global__ void __launch_bounds__(256, 2) range_fwd_few_k(RangeAttn a, FewShape 
   int t = fk.live_from(t0 + wv, 4);
   issue(rk, t, aK);
   issue(rv, t, aV);
-  bf16x8 qf[T::KK];
-  T::load_frags((const bf16*)a.q + (i64)row.i * a.ldq + (i64)row.h * a.dh, row.ok, a.dh, g, qf);
   T::arrived(qf);
   const unsigned rbase = T::row_base(lane), cbase = T::col_base(lane);
   f32x16 acc[T::DT] = {};
@@ -707,23 +709,30 @@ template <int DHP, int MOD>
 __global__ void __launch_bounds__(256, 2) range_dq_few_k(RangeAttn a, FewShape f, int tiles, BlockSeen* __restrict__ blocks) {
   typedef Tiles<DHP> T;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem_raw[];
-  const int rows = rows_in_use(a), keys = keys_in_use(a);
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
   if ((int)blockIdx.x >= tiles) {
     const int b = ((int)blockIdx.x - tiles) * 4 + wv;
-    const BlockSeen r = block_seen(a, b, rows, keys, lane);
+    const BlockSeen r = block_seen(a, b, rows_in_use(a), keys_in_use(a), lane);
     if (lane == 0 && b * 64 < a.Tq) blocks[b] = r;
     return;
   }
   int tile, split, head, t0;
   few_place(a, f, (int)blockIdx.x, &tile, &split, &head);
-  tile = f.tiles - 1 - tile;                        // late queries tend to have the long ranges
-  if (tile * f.qpt >= rows) return;
   const int kh = head % a.Hkv;
-  const FewRow row = few_row(a, f, tile, head, lane & 31, rows);
-  const FewKeys fk = few_keys(a, f, row, 0, keys, &t0);
-  const ScoreForm sf = score_form(a, row.h);
+  FewRow row = few_row(a, f, tile, head, lane & 31, a.Tq);
+  const int2 stored = stored_range(a, row.i);
   const int at = (MOD & BIASED) && row.ok ? (a.at ? a.at[row.i] : row.i) : 0;
+  const i64 orow = (i64)row.i * a.ldo + (i64)row.h * a.dh, srow = (i64)row.h * a.Tq + row.i;
+  bf16x8 qf[T::KK], dof[T::KK], of[T::KK];
+  float L = row.ok ? a.lse[srow] * LOG2E : 0.f, D = 0.f;
+  T::load_frags((const bf16*)a.d_o + orow, row.ok, a.dh, g, dof);
+  T::load_frags((const bf16*)a.o + orow, row.ok, a.dh, g, of);
+  T::load_frags((const bf16*)a.q + (i64)row.i * a.ldq + (i64)row.h * a.dh, row.ok, a.dh, g, qf);
+  const int rows = rows_in_use(a), keys = keys_in_use(a);
+  if (tile * f.qpt >= rows) return;
+  row.ok = row.ok && row.i < rows;
+  const FewKeys fk = few_keys(f, row, stored, 0, keys, &t0);
+  const ScoreForm sf = score_form(a, row.h);
   const HeadRows rk = {(const unsigned char*)a.k + (i64)kh * a.dh * 2, a.ldk * 2, a.dh * 2}, rv = {(const unsigned char*)a.v + (i64)kh * a.dh * 2, a.ldv * 2, a.dh * 2};
   unsigned char* tK = smem_raw + wv * T::BYTES;      // 32 rows of K, 32 of V
   const unsigned aK = lds_address(smem_raw) + (unsigned)wv * T::BYTES, aV = aK + T::BYTES / 2;
@@ -738,17 +747,11 @@ __global__ void __launch_bounds__(256, 2) range_dq_few_k(RangeAttn a, FewShape f
     issue(rv, t, aV);
     issue(rk, t, aK);
   }
-  const i64 orow = (i64)row.i * a.ldo + (i64)row.h * a.dh, srow = (i64)row.h * a.Tq + row.i;
-  bf16x8 qf[T::KK], dof[T::KK];
-  float L = row.ok ? a.lse[srow] * LOG2E : 0.f, D = 0.f;
-  T::load_frags((const bf16*)a.d_o + orow, row.ok, a.dh, g, dof);
-  T::load_frags((const bf16*)a.o + orow, row.ok, a.dh, g, qf);
 #pragma unroll
   for (int kk = 0; kk < T::KK; kk++)
 #pragma unroll
-    for (int u = 0; u < 8; u++) D = fmaf((float)qf[kk][u], (float)dof[kk][u], D);
+    for (int u = 0; u < 8; u++) D = fmaf((float)of[kk][u], (float)dof[kk][u], D);
   D = both_halves_sum(D);
-  T::load_frags((const bf16*)a.q + (i64)row.i * a.ldq + (i64)row.h * a.dh, row.ok, a.dh, g, qf);
   if (L == -INFINITY) L = 0.f;
   T::arrived(qf);
   T::arrived(dof);
@@ -822,16 +825,22 @@ __global__ void __launch_bounds__(256, 2) range_dkv_few_k(RangeAttn a, const Blo
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem_raw[];
   const int per = a.Hkv * parts, kt = (int)blockIdx.x / per, r0 = (int)blockIdx.x - kt * per, kh = r0 % a.Hkv, part = r0 / a.Hkv;
   const int k0 = kt * 32;                           // early keys are seen by the most queries
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, mykv = k0 + (lane & 31);
+  // (first loads: see stored_range)
+  bf16x8 kf[T::KK], vf[T::KK];
+  const int2 nobody = make_int2(INT_MAX, 0);
+  int2 seen0 = lane * 64 < a.Tq ? *(const int2*)(blocks + lane) : nobody;
+  T::load_frags((const bf16*)a.k + (i64)mykv * a.ldk + (i64)kh * a.dh, mykv < a.Tk, a.dh, g, kf);
+  T::load_frags((const bf16*)a.v + (i64)mykv * a.ldv + (i64)kh * a.dh, mykv < a.Tk, a.dh, g, vf);
   const int rows = rows_in_use(a), keys = keys_in_use(a);
   if (k0 >= keys) return;
-  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, mykv = k0 + (lane & 31);
   unsigned char* tQ = smem_raw + wv * T::BYTES;      // 32 rows of Q, 32 of dO
   const unsigned aQ = lds_address(smem_raw) + (unsigned)wv * T::BYTES, aS = lds_address(smem_raw) + 4 * T::BYTES + (unsigned)wv * 1280u;
   const float* st = (const float*)(smem_raw + 4 * T::BYTES + wv * 1280);      // lse, D, lo, hi, at: 64 words each, of which 32 are used
   // the pairs of a block of 32 queries, in a block of 64 that sees some of the keys, and a head, dealt out to the waves of all parts
   const int nb = (rows + 63) / 64;
-  unsigned long long live = 0;
-  int base = -64, n = 2 * a.G - 1, turn = -1, blk = 0, q0 = -1, h = 0;
+  unsigned long long live = __ballot(lane < nb && seen0.x < k0 + 32 && seen0.y > k0);
+  int base = 0, n = 2 * a.G - 1, turn = -1, blk = 0, q0 = -1, h = 0;
   auto next = [&]() {                               // q0 = -1: none
     do {
       if (++n == 2 * a.G) {
@@ -871,9 +880,6 @@ __global__ void __launch_bounds__(256, 2) range_dkv_few_k(RangeAttn a, const Blo
   };
   next();
   if (q0 >= 0) issue();
-  bf16x8 kf[T::KK], vf[T::KK];
-  T::load_frags((const bf16*)a.k + (i64)mykv * a.ldk + (i64)kh * a.dh, mykv < keys, a.dh, g, kf);
-  T::load_frags((const bf16*)a.v + (i64)mykv * a.ldv + (i64)kh * a.dh, mykv < keys, a.dh, g, vf);
   T::arrived(kf);
   T::arrived(vf);
   f32x16 dka[T::DT] = {}, dva[T::DT] = {};
