@@ -342,7 +342,7 @@ int revffn_op_attention_bwd_noalloc(int32_t dtype, int32_t kernel_mode, const vo
  * None of the calls needs a context; they allocate nothing, only enqueue work on hip_stream and can be captured into a HIP
  * graph.  Device pointers belong to the device that is current at the call, and so does hip_stream.  Scratch memory comes
  * from the caller (16-byte aligned): it needs no initial contents and keeps none for a later call, and two calls that may
- * overlap need two.  A returned REVFFN_EINVAL / ESHAPE / ENULL means that nothing has been enqueued.
+ * overlap need two.  Arrays without rows may be NULL.  A returned REVFFN_EINVAL / ESHAPE / ENULL means that nothing has been enqueued.
  * Arithmetic and sums are float32; with REVFFN_BF16 the attention probabilities and score gradients are rounded to bfloat16 as
  * operands of the matrix cores, and results are rounded once.  No atomics: same inputs, same bits.
  *

@@ -41,7 +41,7 @@ int check_desc(const revffn_attn_desc* d, RangeAttn* a) {
   return 0;
 }
 int check_mask(const revffn_attn_mask* m, RangeAttn* a) {
-  if (!m || !m->lo || !m->hi) return REVFFN_ENULL;
+  if (!m || (a->Tq > 0 && (!m->lo || !m->hi))) return REVFFN_ENULL;
   a->lo = m->lo; a->hi = m->hi; a->at = m->at; a->used = m->used;
   return 0;
 }
@@ -76,7 +76,7 @@ extern "C" {
 
 int revffn_op_attention_ranges(const int32_t* cu_q, const int32_t* cu_k, const int32_t* prefix, int32_t n_docs, int32_t causal,
                                int32_t window, int32_t Tq, int32_t Tk, int32_t* lo, int32_t* hi, int32_t* at, int32_t* used, void* stream) {
-  if (!lo || !hi) return REVFFN_ENULL;
+  if (Tq > 0 && (!lo || !hi)) return REVFFN_ENULL;
   if (n_docs < 1 || n_docs == INT32_MAX || (causal != 0 && causal != 1) || window < 0 || Tq < 0 || Tk < 0 || (prefix && window) || (!causal && (prefix || window)))
     return REVFFN_EINVAL;
   if ((!cu_q && Tq % n_docs) || (!cu_q && !cu_k && Tk % n_docs)) return REVFFN_ESHAPE;
@@ -96,7 +96,7 @@ int revffn_op_attention_masked_fwd(const revffn_attn_desc* desc, const revffn_at
   RangeAttn a;
   TRY(check_desc(desc, &a));
   TRY(check_mask(mask, &a));
-  if (!q || !o || (a.Tk > 0 && (!k || !v))) return REVFFN_ENULL;
+  if ((a.Tq > 0 && (!q || !o)) || (a.Tk > 0 && (!k || !v))) return REVFFN_ENULL;
   const Scratch w = lay_out(a, false, work);
   if (w.bytes && !work) return REVFFN_ENULL;
   if (w.bytes > work_bytes || ((uintptr_t)work & 15)) return REVFFN_EINVAL;
@@ -115,7 +115,7 @@ int revffn_op_attention_masked_bwd(const revffn_attn_desc* desc, const revffn_at
   RangeAttn a;
   TRY(check_desc(desc, &a));
   TRY(check_mask(mask, &a));
-  if (!q || !o || !d_o || !lse || !dq || (a.Tk > 0 && (!k || !v || !dk || !dv))) return REVFFN_ENULL;
+  if ((a.Tq > 0 && (!q || !o || !d_o || !lse || !dq)) || (a.Tk > 0 && (!k || !v || !dk || !dv))) return REVFFN_ENULL;
   const Scratch w = lay_out(a, true, work);
   if (w.bytes && !work) return REVFFN_ENULL;
   if (w.bytes > work_bytes || ((uintptr_t)work & 15)) return REVFFN_EINVAL;
@@ -133,7 +133,7 @@ int revffn_op_rotary_frequencies(const revffn_rotary* r, double* freqs) { return
 int revffn_op_rotary(int32_t dtype, const revffn_rotary* r, const void* x, void* y, const int32_t* pos, int32_t T, int32_t S, int32_t H,
                      int32_t dh, int64_t ldx, int64_t ldy, int32_t transposed, void* stream) {
   RotaryArgs a;
-  if (!r || !x || !y) return REVFFN_ENULL;
+  if (!r || (T > 0 && (!x || !y))) return REVFFN_ENULL;
   if ((dtype != 0 && dtype != 1) || T < 0 || (!pos && S < 1) || H < 1 || dh < 2 || dh > 1024 || H > 65536 || (transposed != 0 && transposed != 1))
     return REVFFN_EINVAL;
   TRY(frequencies(r, a.freq));
@@ -156,7 +156,7 @@ size_t revffn_op_layernorm_workspace(int32_t rows, int32_t cols) {
 
 int revffn_op_layernorm_fwd(int32_t dtype, const void* x, const void* gain, const void* bias, void* y, float* mean, float* rstd, int32_t rows,
                             int32_t cols, int64_t ldx, int64_t ldy, float eps, void* stream) {
-  if (!x || !y) return REVFFN_ENULL;
+  if (rows > 0 && (!x || !y)) return REVFFN_ENULL;
   if ((dtype != 0 && dtype != 1) || rows < 0 || cols < 1 || cols > (1 << 24) || !(eps >= 0.f) || !(eps < INFINITY)) return REVFFN_EINVAL;
   if (ldx < cols || ldy < cols || (x == y && ldx != ldy) || !grid_fits(4 * (i64)rows)) return REVFFN_ESHAPE;
   LayerNorm a = {};
@@ -169,10 +169,10 @@ int revffn_op_layernorm_fwd(int32_t dtype, const void* x, const void* gain, cons
 int revffn_op_layernorm_bwd(int32_t dtype, const void* dy, const void* x, const void* gain, const float* mean, const float* rstd, void* dx,
                             void* dgain, void* dbias, int32_t rows, int32_t cols, int64_t lddy, int64_t ldx, int64_t lddx, int32_t grads_f32,
                             void* work, size_t work_bytes, void* stream) {
-  if (!dy || !x || !mean || !rstd || !dx) return REVFFN_ENULL;
+  if (rows > 0 && (!dy || !x || !mean || !rstd || !dx)) return REVFFN_ENULL;
   if ((dtype != 0 && dtype != 1) || rows < 0 || cols < 1 || cols > (1 << 24) || (grads_f32 != 0 && grads_f32 != 1)) return REVFFN_EINVAL;
   if (ldx < cols || lddy < cols || lddx < cols || (dy == dx && lddy != lddx) || !grid_fits(4 * (i64)rows)) return REVFFN_ESHAPE;
-  if (dx == x) return REVFFN_EINVAL;                // (x is read again for the sums)
+  if (rows > 0 && dx == x) return REVFFN_EINVAL;                // (x is read again for the sums)
   if (dgain || dbias) {
     if (!work) return REVFFN_ENULL;
     if (work_bytes < revffn_op_layernorm_workspace(rows, cols) || ((uintptr_t)work & 15)) return REVFFN_EINVAL;

@@ -237,6 +237,256 @@ def test_attention_ranges():
     assert dl.min() >= 0 and dh.max() <= 21
 
 
+FORMS = pytest.mark.parametrize("dtype,mode", [("bf16", 1), ("bf16", 256), ("bf16", 512), ("f32", 0)])
+
+
+@FORMS
+@pytest.mark.parametrize("scale", [4.0, 40.0])
+def test_attention_peaked(scale, mode, dtype):
+    """Scores of hundreds: one key takes nearly all of a query's weight, and maxima rise late."""
+    lo, hi, at = ref.ranges([150, 70])
+    a = Attention(dtype, 2, 1, 64, 220, 220)
+    a.run(lo, hi, at, mode, scale=scale)
+    a.check(lo, hi, at, scale=scale)
+
+
+@FORMS
+def test_attention_not_finite_where_it_is_seen(mode, dtype):
+    """A NaN that queries see is in their results and in no others (and the call ends)."""
+    lo, hi, at = ref.ranges([100, 200])
+    a = Attention(dtype, 2, 2, 128, 300, 300)
+    a.v[150, :128] = NAN                                    # of the first head
+    a.run(lo, hi, at, mode)
+    o = a.part("o")
+    assert np.isnan(o[150:, 0]).all() and np.isfinite(o[:150]).all() and np.isfinite(o[:, 1]).all()
+    dk = a.part("dk")
+    assert np.isfinite(dk[:100]).all() and np.isfinite(dk[:, 1]).all()
+
+
+@FORMS
+def test_attention_same_bits_again(mode, dtype):
+    lo, hi, at = ref.ranges([300, 211])
+    runs = []
+    for _ in range(2):
+        a = Attention(dtype, 4, 2, 64, 511, 511)
+        a.run(lo, hi, at, mode, slopes=_slopes(4))
+        runs.append([t.clone() for t in (a.o, a.lse, a.dq, a.dk, a.dv)])
+    assert all(torch.equal(x, y) for x, y in zip(*runs))
+
+
+@FORMS
+def test_attention_without_queries_or_keys(mode, dtype):
+    a = Attention(dtype, 2, 1, 64, 0, 40)
+    a.run(np.zeros(0, int), np.zeros(0, int), None, mode)
+    assert (a.part("dk") == 0).all() and (a.part("dv") == 0).all()
+    a = Attention(dtype, 2, 1, 64, 40, 0)
+    a.run(np.zeros(40, int), np.full(40, 9), None, mode)
+    assert (a.part("o") == 0).all() and (a.part("dq") == 0).all() and torch.isneginf(a.lse).all()
+    a = Attention(dtype, 2, 1, 64, 70, 70, extra_rows=5)           # rows there, none in use
+    a.Tq = a.Tk = 0
+    a.run(np.zeros(75, int), np.full(75, 9), None, mode, used=True)
+    assert all(torch.isnan(t).all() for t in (a.o, a.dq, a.dk, a.dv, a.lse))
+
+
+@FORMS
+def test_attention_tensors_that_start_anywhere(mode, dtype):
+    """Rows that start one element after an aligned address go to kernels that take them."""
+    lo, hi, at = ref.ranges([60, 45])
+    a = Attention(dtype, 2, 1, 64, 105, 105, pad=8)
+    for name in ("q", "k", "v", "do", "o", "dq", "dk", "dv"):
+        t = getattr(a, name)
+        room = torch.full((t.numel() + 1,), NAN, dtype=t.dtype, device="cuda")
+        room[1:] = t.reshape(-1)
+        setattr(a, name, room[1:].reshape(t.shape))
+    a.run(lo, hi, at, mode)
+    a.check(lo, hi, at)
+
+
+@pytest.mark.parametrize("dtype,mode", [("bf16", 1), ("bf16", 256), ("bf16", 512), ("f32", 0)])
+def test_attention_offsets_past_32_bits(mode, dtype):
+    """Rows so far apart that keys, values and queries lie more than 2^32 bytes (and elements) behind the first."""
+    n, H, dh, apart = 530, 2, 64, (1 << 23) + 8
+    rng = np.random.default_rng(1)
+    big = {name: torch.empty(n * apart, dtype=TORCH[dtype], device="cuda") for name in ("q", "k", "v", "do", "o", "dq", "dk", "dv")}
+    a = Attention(dtype, H, H, dh, n, n)
+    for name, t in big.items():
+        rows = t.as_strided((n, H * dh), (apart, 1))
+        if name in ("q", "k", "v", "do"):
+            rows.copy_(getattr(a, name))
+        setattr(a, name, rows)
+    lo, hi, at = ref.ranges([100, 430])
+    a.run(lo, hi, at, mode)
+    a.check(lo, hi, at)
+
+
+def test_attention_single_token_far_along_a_cache_past_4_gib():
+    """One query each of two sequences in a cache of 2^22 key rows, 4 GiB a tensor: the last keys count as the first do."""
+    rows, Hkv, H, dh = 1 << 22, 4, 16, 128
+    k = torch.randn(rows, Hkv * dh, dtype=torch.bfloat16, device="cuda")
+    v = torch.randn(rows, Hkv * dh, dtype=torch.bfloat16, device="cuda")
+    q = torch.randn(2, H * dh, dtype=torch.bfloat16, device="cuda")
+    o, lse = torch.empty_like(q), torch.empty(H, 2, device="cuda")
+    d = R.AttnDesc(dtype=1, H=H, Hkv=Hkv, dh=dh, Tq=2, Tk=rows)
+    lo, hi = [rows - 700, 5], [rows, 805]
+    work = torch.empty(R.revffn_op_attention_masked_workspace(d, False), dtype=torch.uint8, device="cuda")
+    R.revffn_op_attention_masked_fwd(d, R.AttnMask(_ints(lo), _ints(hi)), q, k, v, o, lse, work)
+    torch.cuda.synchronize()
+    for i in range(2):
+        part = lambda t: _np(t[lo[i]:hi[i]]).reshape(-1, Hkv, dh)
+        want = ref.attention(_np(q[i:i + 1]).reshape(1, H, dh), part(k), part(v), [0], [hi[i] - lo[i]], dtype="bf16")
+        assert ref.outside(_np(o[i:i + 1]).reshape(1, H, dh), *want["o"]) <= 1.0
+        assert ref.outside(_np(lse[:, i:i + 1]), *want["lse"]) <= 1.0
+
+
+def _graph_of(call):
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    return g
+
+
+class Layer:
+    """An attention layer over packed documents, forward and backward: layer norm, a fused projection, rotary positions on the
+    queries and keys where they lie, attention, the output projection."""
+
+    def __init__(self, lens, d=256, H=4, Hkv=2, dh=64, seed=0, cap=0.0):
+        rng = np.random.default_rng(seed)
+        self.lens, self.d, self.H, self.Hkv, self.dh, self.T = lens, d, H, Hkv, dh, sum(lens)
+        T, self.wide = self.T, (H + 2 * Hkv) * dh
+        bf = lambda *s, sc=1.0: _rand(rng, s, "bf16", sc).cuda()
+        self.x, self.gain, self.bias, self.dout = bf(T, d), bf(d, sc=0.1) + 1, bf(d, sc=0.1), bf(T, d)
+        self.w, self.wo = bf(self.wide, d, sc=d ** -0.5), bf(d, H * dh, sc=(H * dh) ** -0.5)
+        new = lambda *s, t=torch.bfloat16: torch.empty(s, dtype=t, device="cuda")
+        self.n, self.qkv, self.o, self.out = new(T, d), new(T, self.wide), new(T, H * dh), new(T, d)
+        self.dn, self.dqkv, self.do, self.dx = new(T, d), new(T, self.wide), new(T, H * dh), new(T, d)
+        self.dw, self.dwo, self.dgain, self.dbias = new(self.wide, d), new(d, H * dh), new(d), new(d)
+        self.mean, self.rstd, self.lse = new(T, t=torch.float32), new(T, t=torch.float32), new(H, T, t=torch.float32)
+        i32 = torch.int32
+        self.lo, self.hi, self.at, self.used = new(T, t=i32), new(T, t=i32), new(T, t=i32), new(2, t=i32)
+        self.cu = _ints(np.cumsum([0] + lens))
+        self.pos = _ints(np.concatenate([np.arange(n) for n in lens]))
+        self.rotary = R.Rotary(dims=dh, theta=10000.0)
+        self.desc = R.AttnDesc(dtype=1, H=H, Hkv=Hkv, dh=dh, Tq=T, Tk=T, ldq=self.wide, ldk=self.wide, ldv=self.wide, ldo=H * dh, softcap=cap)
+        self.mask = R.AttnMask(self.lo, self.hi, self.at, self.used)
+        n = max(R.revffn_op_attention_masked_workspace(self.desc, True), R.revffn_op_layernorm_workspace(T, d))
+        self.work = new(n, t=torch.uint8)
+
+    def parts(self, t):
+        a, b = self.H * self.dh, (self.H + self.Hkv) * self.dh
+        return t[:, :a], t[:, a:b], t[:, b:]
+
+    def run(self):
+        T, d, w, H, Hkv, dh = self.T, self.d, self.wide, self.H, self.Hkv, self.dh
+        R.revffn_op_attention_ranges(self.cu, None, None, len(self.lens), True, 0, T, T, self.lo, self.hi, self.at, self.used)
+        R.revffn_op_layernorm_fwd(1, self.x, self.gain, self.bias, self.n, self.mean, self.rstd, T, d, d, d, 1e-5)
+        R.revffn_op_gemm(1, 0, self.n, self.w, self.qkv, T, w, d, d, d, w, 0, 0)
+        R.revffn_op_rotary(1, self.rotary, self.qkv, self.qkv, self.pos, T, T, H + Hkv, dh, w, w)
+        R.revffn_op_attention_masked_fwd(self.desc, self.mask, *self.parts(self.qkv), self.o, self.lse, self.work)
+        R.revffn_op_gemm(1, 0, self.o, self.wo, self.out, T, d, H * dh, H * dh, H * dh, d, 0, 0)
+        R.revffn_op_gemm(1, 0, self.dout, self.o, self.dwo, d, H * dh, T, d, H * dh, H * dh, 1, 1)
+        R.revffn_op_gemm(1, 0, self.dout, self.wo, self.do, T, H * dh, d, d, H * dh, H * dh, 0, 1)
+        R.revffn_op_attention_masked_bwd(self.desc, self.mask, *self.parts(self.qkv), self.o, self.do, self.lse, *self.parts(self.dqkv), self.work)
+        R.revffn_op_rotary(1, self.rotary, self.dqkv, self.dqkv, self.pos, T, T, H + Hkv, dh, w, w, True)
+        R.revffn_op_gemm(1, 0, self.dqkv, self.n, self.dw, w, d, T, w, d, d, 1, 1)
+        R.revffn_op_gemm(1, 0, self.dqkv, self.w, self.dn, T, d, w, w, d, d, 0, 1)
+        R.revffn_op_layernorm_bwd(1, self.dn, self.x, self.gain, self.mean, self.rstd, self.dx, self.dgain, self.dbias, T, d, d, d, d, False, self.work)
+
+    def results(self):
+        return {n: getattr(self, n).clone() for n in ("out", "dx", "dw", "dwo", "dgain", "dbias")}
+
+    def reference(self):
+        x, g, b, w, wo, dout = (_np(t) for t in (self.x, self.gain, self.bias, self.w, self.wo, self.dout))
+        T, H, Hkv, dh = self.T, self.H, self.Hkv, self.dh
+        n = ref.layernorm(x, g, b, 1e-5)[0]
+        qkv = (n @ w.T).reshape(T, H + 2 * Hkv, dh)
+        pos, f = self.pos.cpu().numpy(), R.revffn_op_rotary_frequencies(self.rotary)
+        qk = ref.rotary(qkv[:, : H + Hkv], pos, f, False)
+        lo, hi, at = ref.ranges(self.lens)
+        fwd = ref.attention(qk[:, :H], qk[:, H:], qkv[:, H + Hkv:], lo, hi, at)
+        o = fwd["o"][0].reshape(T, H * dh)
+        do = (dout @ wo).reshape(T, H, dh)
+        bwd = ref.attention(qk[:, :H], qk[:, H:], qkv[:, H + Hkv:], lo, hi, at, do=do)
+        dqk = ref.rotary(np.concatenate([bwd["dq"][0], bwd["dk"][0]], 1), pos, f, False, transposed=True)
+        dqkv = np.concatenate([dqk, bwd["dv"][0]], 1).reshape(T, -1)
+        _, _, _, dx, dg, db = ref.layernorm(x, g, b, 1e-5, dqkv @ w)
+        return dict(out=o @ wo.T, dx=dx, dw=dqkv.T @ n, dwo=dout.T @ o, dgain=dg, dbias=db)
+
+
+@pytest.mark.parametrize("lens", [[70, 1, 200, 33], [5], [1, 1, 1]])
+def test_layer_run_together(lens):
+    layer = Layer(lens)
+    layer.run()
+    torch.cuda.synchronize()
+    got, want = layer.results(), layer.reference()
+    # a result passes through at most eight tensors rounded to bf16 (half a step: 2^-8 of each value) and two roundings of matrix
+    # operands; errors of a row's many terms don't line up, so the norm of a result's error stays under that many half steps of its own
+    for name, w in want.items():
+        err = np.linalg.norm(_np(got[name]) - w) / np.linalg.norm(w)
+        assert err < 10 * 2.0 ** -8, (name, err)
+
+
+def test_layer_captured_and_replayed():
+    """One captured graph, replayed with new inputs and eager work between; then a second graph on the same workspace."""
+    layer = Layer([130, 60, 1, 200], seed=1)
+    layer.run()
+    torch.cuda.synchronize()
+    g = _graph_of(layer.run)
+    other = Layer([300, 91], seed=2)
+    other.work = layer.work if layer.work.numel() >= other.work.numel() else other.work
+    g2 = _graph_of(other.run)
+    for seed in range(3):
+        fresh = Layer([130, 60, 1, 200], seed=10 + seed)
+        layer.x.copy_(fresh.x)
+        layer.dout.copy_(fresh.dout)
+        layer.run()
+        torch.cuda.synchronize()
+        want = layer.results()
+        for name in want:
+            getattr(layer, name).fill_(NAN)
+        layer.work.fill_(255)
+        g.replay()
+        g2.replay()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, getattr(layer, n)) for n, a in want.items())
+
+
+def test_calls_on_two_streams_at_once():
+    """Two layers on streams of their own, each with its own workspace, give what each gives alone."""
+    layers = [Layer([300, 200], seed=3, H=8, Hkv=2), Layer([257, 3, 100], seed=4)]
+    want = []
+    for layer in layers:
+        layer.run()
+        torch.cuda.synchronize()
+        want.append(layer.results())
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        for layer, s in zip(layers, streams):
+            with torch.cuda.stream(s):
+                layer.run()
+    torch.cuda.synchronize()
+    for layer, w in zip(layers, want):
+        assert all(torch.equal(a, getattr(layer, n)) for n, a in w.items())
+
+
+def test_tensors_of_another_type_are_refused():
+    b, f = torch.zeros(64, dtype=torch.bfloat16, device="cuda"), torch.zeros(64, device="cuda")
+    with pytest.raises(R.RevffnError, match="bfloat16"):
+        R.revffn_op_layernorm_fwd(1, f, None, None, b, None, None, 1, 64, 64, 64, 1e-5)
+    with pytest.raises(R.RevffnError, match="float32"):
+        R.revffn_op_layernorm_fwd(1, b, None, None, b, b, None, 1, 64, 64, 64, 1e-5)
+    with pytest.raises(R.RevffnError, match="int32"):
+        R.revffn_op_rotary(1, R.Rotary(dims=64, theta=1e4), b, b, torch.zeros(1, dtype=torch.int64, device="cuda"), 1, 1, 1, 64, 64, 64)
+    with pytest.raises(R.RevffnError, match="device"):
+        R.revffn_op_rotary(1, R.Rotary(dims=64, theta=1e4), b, b.cpu(), None, 1, 1, 1, 64, 64, 64)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("interleaved", [False, True])
 # T, H, dh, dims, extra columns in a row, scaling
