@@ -4,14 +4,26 @@
 //   dg = sum over rows of dy xh, db = of dy: every wave (workgroup) keeps the sums of the rows it works on in registers; one
 //   partial sum per workgroup goes to memory, and a second launch adds those in order.
 // Columns of a thread: chunks of 8 neighbours, chunk n at column 8 (thread + n threads): the same whatever the alignment, so the
-// result does not depend on where the rows lie; aligned rows are read 16 bytes at a time, others element by element.
+// result does not depend on where the rows lie; rows are read 16 bytes at a time wherever they start, the last
+// few columns of an odd row one by one.
 #include "kernels.h"
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_v;
+typedef __attribute__((ext_vector_type(8))) float f32x8_v;
+// the same, at any element's address (the hardware takes unaligned 16-byte accesses)
+typedef bf16x8_v bf16x8_any __attribute__((aligned(2)));
+typedef f32x8_v f32x8_any __attribute__((aligned(4)));
+typedef f32x8_v f32x8_16 __attribute__((aligned(16)));
+template <class T, bool ALIGNED> struct Vec8;
+template <> struct Vec8<bf16, true> { typedef bf16x8_v type; };
+template <> struct Vec8<bf16, false> { typedef bf16x8_any type; };
+template <> struct Vec8<float, true> { typedef f32x8_16 type; };
+template <> struct Vec8<float, false> { typedef f32x8_any type; };
 
-template <bool ALIGNED> __device__ __forceinline__ void load8(const bf16* p, int left, float (&r)[8]) {
-  if constexpr (ALIGNED) {
-    const bf16x8_v v = *(const bf16x8_v*)p;
+// 8 columns, of which `left` are there (the others read as 0)
+template <bool ALIGNED, class T> __device__ __forceinline__ void load8(const T* p, int left, float (&r)[8]) {
+  if (ALIGNED || left >= 8) {
+    const auto v = *(const typename Vec8<T, ALIGNED>::type*)p;
 #pragma unroll
     for (int i = 0; i < 8; i++) r[i] = (float)v[i];
   } else {
@@ -19,56 +31,26 @@ template <bool ALIGNED> __device__ __forceinline__ void load8(const bf16* p, int
     for (int i = 0; i < 8; i++) r[i] = i < left ? (float)p[i] : 0.f;
   }
 }
-template <bool ALIGNED> __device__ __forceinline__ void load8(const float* p, int left, float (&r)[8]) {
-  if constexpr (ALIGNED) {
-    const float4 u = *(const float4*)p, v = *(const float4*)(p + 4);
-    r[0] = u.x; r[1] = u.y; r[2] = u.z; r[3] = u.w; r[4] = v.x; r[5] = v.y; r[6] = v.z; r[7] = v.w;
+template <bool ALIGNED, class T> __device__ __forceinline__ void store8(T* p, int left, const float (&r)[8]) {
+  if (ALIGNED || left >= 8) {
+    typename Vec8<T, ALIGNED>::type v;
+#pragma unroll
+    for (int i = 0; i < 8; i++) v[i] = (T)r[i];
+    *(typename Vec8<T, ALIGNED>::type*)p = v;
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; i++) r[i] = i < left ? p[i] : 0.f;
+    for (int i = 0; i < 8; i++) if (i < left) p[i] = (T)r[i];
   }
 }
-template <bool ALIGNED> __device__ __forceinline__ void store8(bf16* p, int left, const float (&r)[8]) {
-  if constexpr (ALIGNED) {
-    bf16x8_v v;
-#pragma unroll
-    for (int i = 0; i < 8; i++) v[i] = (__bf16)r[i];
-    *(bf16x8_v*)p = v;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; i++) if (i < left) p[i] = (__bf16)r[i];
-  }
-}
-template <bool ALIGNED> __device__ __forceinline__ void store8(float* p, int left, const float (&r)[8]) {
-  if constexpr (ALIGNED) {
-    *(float4*)p = make_float4(r[0], r[1], r[2], r[3]);
-    *(float4*)(p + 4) = make_float4(r[4], r[5], r[6], r[7]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; i++) if (i < left) p[i] = r[i];
-  }
-}
-
-// 8 columns as they are in memory: the next row's are on their way while a row is worked on
-template <class T, bool ALIGNED> struct Raw8;
-template <> struct Raw8<bf16, true> {
-  bf16x8_v v;
-  __device__ __forceinline__ void load(const bf16* p, int) { v = *(const bf16x8_v*)p; }
-  __device__ __forceinline__ void get(float (&r)[8]) const {
-#pragma unroll
-    for (int i = 0; i < 8; i++) r[i] = (float)v[i];
-  }
-};
-template <> struct Raw8<float, true> {
-  float4 u, v;
-  __device__ __forceinline__ void load(const float* p, int) { u = *(const float4*)p; v = *(const float4*)(p + 4); }
-  __device__ __forceinline__ void get(float (&r)[8]) const { r[0] = u.x; r[1] = u.y; r[2] = u.z; r[3] = u.w; r[4] = v.x; r[5] = v.y; r[6] = v.z; r[7] = v.w; }
-};
-template <class T> struct Raw8<T, false> {
-  T v[8];
+// the same as they are in memory: the next row's are on their way while a row is worked on
+template <class T, bool ALIGNED> struct Raw8 {
+  typename Vec8<T, true>::type v;
   __device__ __forceinline__ void load(const T* p, int left) {
+    if (ALIGNED || left >= 8) v = *(const typename Vec8<T, ALIGNED>::type*)p;
+    else {
 #pragma unroll
-    for (int i = 0; i < 8; i++) v[i] = i < left ? p[i] : (T)0.f;
+      for (int i = 0; i < 8; i++) v[i] = i < left ? p[i] : (T)0.f;
+    }
   }
   __device__ __forceinline__ void get(float (&r)[8]) const {
 #pragma unroll
@@ -166,13 +148,13 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) layernorm_fwd_k
   }
 }
 
-// Row r of workgroup w: w, w + grid, ..  PARAMS: partial sums of dg and db, [workgroup][2][cols].  CH = 0: rows longer than the registers hold;
+// Row r of workgroup w: w, w + grid, ..  PARAMS: partial sums of dg and db, [workgroup][2][columns].  CH = 0: rows longer than the registers hold;
 // dg and db then come from a kernel of their own.
 template <class T, bool ALIGNED, int WAVES, int CH, bool PARAMS>
 __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) layernorm_bwd_k(LayerNorm a) {
   constexpr int NT = WAVES * 64, ROWS = WAVES == 1 ? 4 : 1, C = CH > 0 ? CH : 1;
   __shared__ float red[4][WAVES];
-  extern __shared__ float sums[];                    // WAVES == 1: [3][2][C * 512]
+  extern __shared__ float sums[];                    // WAVES == 1: [4][C * 512]
   const int wv = threadIdx.x >> 6, tid = ROWS == 4 ? threadIdx.x & 63 : threadIdx.x;
   const T* g = (const T*)a.gain;
   const int cols = a.cols;
@@ -276,32 +258,29 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) layernorm_bwd_k
     turn ^= 2;                                       // (a slow wave may still read the last row's sums)
   }
   if constexpr (PARAMS && CH > 0) {
-    float* out = a.partial + (i64)blockIdx.x * 2 * cols;
+    // In the threads' own order, value i of chunk k at (8 k + i) NT + thread: whole lines to LDS and to memory; the last kernel knows
+    // which column that is.
+    float* out = a.partial + (i64)blockIdx.x * 2 * (C * 8 * NT);
     if constexpr (ROWS == 4) {                       // the four waves' sums, in wave order
-      float* mine = sums + (wv - 1) * 2 * C * 512;
-      if (wv > 0) {
+#pragma unroll
+      for (int w = 0; w < 2; w++) {
+        __syncthreads();
 #pragma unroll
         for (int k = 0; k < C; k++)
 #pragma unroll
-          for (int i = 0; i < 8; i++) { mine[(k * 8 + i) * 64 + tid] = dg[k][i]; mine[C * 512 + (k * 8 + i) * 64 + tid] = db[k][i]; }
+          for (int i = 0; i < 8; i++) sums[(wv * C * 8 + k * 8 + i) * 64 + tid] = w ? db[k][i] : dg[k][i];
+        __syncthreads();
+#pragma unroll
+        for (int p = 0; p < C * 2; p++) {
+          const int at = p * 256 + (int)threadIdx.x;
+          out[w * C * 512 + at] = (sums[at] + sums[C * 512 + at]) + (sums[2 * C * 512 + at] + sums[3 * C * 512 + at]);
+        }
       }
-      __syncthreads();
-      if (wv > 0) return;
+    } else {
 #pragma unroll
-      for (int w = 0; w < 3; w++)
+      for (int k = 0; k < C; k++)
 #pragma unroll
-        for (int k = 0; k < C; k++)
-#pragma unroll
-          for (int i = 0; i < 8; i++) {
-            dg[k][i] += sums[w * 2 * C * 512 + (k * 8 + i) * 64 + tid];
-            db[k][i] += sums[w * 2 * C * 512 + C * 512 + (k * 8 + i) * 64 + tid];
-          }
-    }
-#pragma unroll
-    for (int k = 0; k < C; k++) {
-      const int c = (tid + k * NT) * 8;
-#pragma unroll
-      for (int i = 0; i < 8; i++) if (c + i < cols) { out[c + i] = dg[k][i]; out[cols + c + i] = db[k][i]; }
+        for (int i = 0; i < 8; i++) { out[(k * 8 + i) * NT + tid] = dg[k][i]; out[(C * 8 + k * 8 + i) * NT + tid] = db[k][i]; }
     }
   }
 }
@@ -323,45 +302,63 @@ template <class T> __global__ void __launch_bounds__(256) layernorm_params_k(Lay
   const float* p = &part[w][0][threadIdx.x & 63];
   a.partial[((i64)blockIdx.y * 2 + w) * a.cols + c] = (p[0] + p[64]) + (p[128] + p[192]);
 }
-// 16 columns of one of the two sums per workgroup, 16 threads to a column, each every 16th of the partial sums
-template <class T> __global__ void __launch_bounds__(256) layernorm_reduce_k(const float* __restrict__ partial, int n, int cols, T* dgain, T* dbias) {
+// 16 values of one of the two sums per workgroup, 16 threads to a value, each every 16th of the partial sums.  threads: of the
+// kernel that left them in its threads' order, `padded` values of each; 0: in the order of the columns
+template <class T> __global__ void __launch_bounds__(256) layernorm_reduce_k(const float* __restrict__ partial, int n, int cols, int padded, int threads, T* dgain, T* dbias) {
   __shared__ float part[16][17];
-  const int tc = threadIdx.x & 15, w = threadIdx.x >> 4, c = (int)blockIdx.x * 16 + tc;
+  const int tc = threadIdx.x & 15, w = threadIdx.x >> 4, at = (int)blockIdx.x * 16 + tc;
   T* out = blockIdx.y ? dbias : dgain;
   if (!out) return;
+  int c = at;
+  if (threads) {
+    const int v = at / threads, t = at - v * threads;
+    c = (t + (v >> 3) * threads) * 8 + (v & 7);
+  }
   float s = 0.f;
-  if (c < cols) {
-    const float* p = partial + (i64)blockIdx.y * cols + c;
+  if (at < padded && c < cols) {
+    const float* p = partial + (i64)blockIdx.y * padded + at;
 #pragma unroll 8
-    for (int i = w; i < n; i += 16) s += p[(i64)i * 2 * cols];
+    for (int i = w; i < n; i += 16) s += p[(i64)i * 2 * padded];
   }
   part[w][tc] = s;
   __syncthreads();
-  if (w == 0 && c < cols) {
+  if (w == 0 && at < padded && c < cols) {
 #pragma unroll
     for (int i = 1; i < 16; i++) s += part[i][tc];
     out[c] = from_f<T>(s);
   }
 }
 
-// partial sums: one per workgroup of the backward kernel
-#define MAX_PARTS 512
-size_t layernorm_partial_floats(int rows, int cols) { return (size_t)(rows < 1 ? 1 : rows < MAX_PARTS ? rows : MAX_PARTS) * 2 * cols; }
+// Waves per row, 8-column chunks per thread and (backward) workgroups, each of which leaves partial sums of whole rows: more of them keep
+// more rows in flight, but the sums cost each some 4 KiB (2 KiB CH) of traffic twice and a few microseconds at its end.  8192 x 2048, us with
+// 256, 512, 1024: 27.4, 31.4, 40.1.
+struct Shape { int waves, chunks, parts; };
+static Shape shape_of(int cols) {
+  if (cols <= 512) return {1, 1, 1024};
+  if (cols <= 1024) return {1, 2, 512};
+  if (cols <= 2048) return {1, 4, 256};
+  if (cols <= 4096) return {4, 2, 512};
+  if (cols <= 8192) return {4, 4, 512};
+  if (cols <= 16384) return {16, 2, 256};
+  return {16, 0, 32};
+}
+static int padded_columns(int cols) { const Shape f = shape_of(cols); return f.chunks ? f.waves * f.chunks * 512 : cols; }
+size_t layernorm_partial_floats(int rows, int cols) {
+  const int n = shape_of(cols).parts;
+  return (size_t)(rows < 1 ? 1 : rows < n ? rows : n) * 2 * padded_columns(cols);
+}
 
 static bool aligned(const LayerNorm& a, bool back) {
   const uintptr_t p = (uintptr_t)a.x | (uintptr_t)a.gain | (back ? (uintptr_t)a.dy | (uintptr_t)a.dx : (uintptr_t)a.y | (uintptr_t)a.bias);
   const i64 l = a.cols | a.ldx | (back ? a.lddy | a.lddx : a.ldy);
   return (p & 15) == 0 && (l & 7) == 0;
 }
-// waves per row and 8-column chunks per thread by the row's length
 #define BY_COLS(call)                                   \
   do {                                                  \
-    if (a.cols <= 512) call(1, 1);                      \
-    else if (a.cols <= 1024) call(1, 2);                \
-    else if (a.cols <= 2048) call(1, 4);                \
-    else if (a.cols <= 4096) call(4, 2);                \
-    else if (a.cols <= 8192) call(4, 4);                \
-    else if (a.cols <= 32768) call(16, 4);              \
+    const Shape f = shape_of(a.cols);                   \
+    if (f.waves == 1) { if (f.chunks == 1) call(1, 1); else if (f.chunks == 2) call(1, 2); else call(1, 4); } \
+    else if (f.waves == 4) { if (f.chunks == 2) call(4, 2); else call(4, 4); } \
+    else if (f.chunks) call(16, 2);                     \
     else call(16, 0);                                   \
   } while (0)
 
@@ -382,8 +379,8 @@ template <class T, bool AL, int W, int CH> static int bwd_one(const LayerNorm& a
   int grid = cdiv(a.rows, ROWS);
   if constexpr (CH > 0) {
     if (params) {
-      if (grid > MAX_PARTS) grid = MAX_PARTS;
-      hipLaunchKernelGGL((layernorm_bwd_k<T, AL, W, CH, true>), dim3(grid), block, W == 1 ? (size_t)3 * 2 * CH * 512 * 4 : 0, s, a);
+      if (grid > shape_of(a.cols).parts) grid = shape_of(a.cols).parts;
+      hipLaunchKernelGGL((layernorm_bwd_k<T, AL, W, CH, true>), dim3(grid), block, W == 1 ? (size_t)4 * CH * 512 * 4 : 0, s, a);
       return grid;
     }
   }
@@ -405,7 +402,9 @@ void launch_layernorm_bwd(const LayerNorm& a, hipStream_t s) {
     else n = al ? bwd<bf16, true>(a, params, s) : bwd<bf16, false>(a, params, s);
   }
   if (!params) return;
-  const dim3 grid(cdiv(a.cols, 16), 2);
-  if (a.dt == 0 || a.grads_f32) hipLaunchKernelGGL(layernorm_reduce_k<float>, grid, dim3(256), 0, s, a.partial, n, a.cols, (float*)a.dgain, (float*)a.dbias);
-  else hipLaunchKernelGGL(layernorm_reduce_k<bf16>, grid, dim3(256), 0, s, a.partial, n, a.cols, (bf16*)a.dgain, (bf16*)a.dbias);
+  const Shape f = shape_of(a.cols);
+  const int padded = padded_columns(a.cols), threads = f.chunks ? f.waves * 64 : 0;
+  const dim3 grid(cdiv(padded, 16), 2);
+  if (a.dt == 0 || a.grads_f32) hipLaunchKernelGGL(layernorm_reduce_k<float>, grid, dim3(256), 0, s, a.partial, n, a.cols, padded, threads, (float*)a.dgain, (float*)a.dbias);
+  else hipLaunchKernelGGL(layernorm_reduce_k<bf16>, grid, dim3(256), 0, s, a.partial, n, a.cols, padded, threads, (bf16*)a.dgain, (bf16*)a.dbias);
 }
