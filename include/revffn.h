@@ -369,7 +369,8 @@ typedef struct revffn_attn_desc {
   int64_t ldq, ldk, ldv, ldo; /* row strides in elements of q, dq / k, dk / v, dv / o, d_o (head hh in columns hh*dh ..);
                               0 = dense (H*dh, Hkv*dh)                                               */
   float scale;             /* of q . k; 0 = 1 / sqrt(dh)                                             */
-  float softcap;           /* > 0: scores become softcap * tanh(score / softcap); 0 = not            */
+  float softcap;           /* > 0: scores become softcap * tanh(score / softcap); 0 = not; |scale| / softcap
+                              below 1e30; bfloat16 with one above 4096 goes row by row              */
   const float *slopes;     /* device [H] or NULL: slopes[hh] * |at[i] - j| is subtracted from the (capped) score; no gradient */
 } revffn_attn_desc;
 

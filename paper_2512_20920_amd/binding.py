@@ -417,7 +417,8 @@ def _device():
     if _torch is None:
         import torch
         _torch = torch
-    return _torch, _torch.cuda.current_device() if _torch.cuda.is_available() else -2
+    cuda = _torch.cuda
+    return _torch, cuda.current_device() if cuda.is_initialized() or cuda.is_available() else -2
 
 
 def _refuse(t, want):

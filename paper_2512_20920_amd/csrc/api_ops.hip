@@ -37,6 +37,7 @@ int check_desc(const revffn_attn_desc* d, RangeAttn* a) {
   if (!grid_fits(((i64)d->Tq + 3) / 4 * d->H) || !grid_fits(((i64)d->Tk + 3) / 4 * d->Hkv)) return REVFFN_ESHAPE;
   a->scale = d->scale != 0.f ? d->scale : 1.0f / sqrtf((float)d->dh);
   a->cap = d->softcap;
+  if (a->cap > 0.f && !(fabsf(a->scale) / a->cap < 1e30f)) return REVFFN_EINVAL;      // (q.k scale / cap would overflow)
   a->slopes = d->slopes;
   return 0;
 }
@@ -57,8 +58,12 @@ int frequencies(const revffn_rotary* r, double* f) {
   const int n = r->dims;
   double theta = r->theta;
   if (r->scaling == 2) theta *= pow((double)r->factor, (double)n / (n - 2));
+  // (every call works them out: by products, off by n / 2 half steps of 64 bits at the last, whose angles are the smallest)
+  const double ratio = pow(theta, -2.0 / n);
+  double next = 1.0;
   for (int i = 0; i < n / 2; i++) {
-    double v = pow(theta, -2.0 * i / n);
+    double v = next;
+    next *= ratio;
     if (r->scaling == 1) v /= r->factor;
     if (r->scaling == 3) {
       double g = (r->original * v / (2 * M_PI) - r->few_turns) / ((double)r->many_turns - r->few_turns);

@@ -6,6 +6,7 @@
 
 struct FewShape {
   int gp, hb;              // heads of a workgroup, head blocks per key head (more than one: more than 32 heads to a key head)
+  int inv;                 // r / gp = r inv >> 16 for r < 32
   int qpt, tiles;          // queries of a workgroup, tiles of them
   int splits;              // of the keys
   float2* stats;           // splits > 1: [query row, head][split] maximum (units of log2) and sum
@@ -13,7 +14,7 @@ struct FewShape {
 };
 struct FewRow { int i, h; bool ok; };
 __device__ __forceinline__ FewRow few_row(const RangeAttn& a, const FewShape& f, int tile, int head, int r, int rows) {
-  const int kh = head % a.Hkv, hb = head / a.Hkv, q = r / f.gp, hg = hb * f.gp + r - q * f.gp;
+  const int kh = head % a.Hkv, hb = head / a.Hkv, q = r * f.inv >> 16, hg = hb * f.gp + r - q * f.gp;
   FewRow x;
   x.i = tile * f.qpt + q;
   x.ok = q < f.qpt && hg < a.G && x.i < rows;
@@ -125,15 +126,14 @@ template <class T, int DHP, int NW> __device__ __forceinline__ bool few_store(co
   }
   return !ok || z == 0.f;
 }
-// block of 64 queries: the first key that some of them see and one past the last (none: INT_MAX, 0), and between which keys all of them
-// see (a row in use that sees nothing leaves none)
+// block of 64 queries: the first key that some of them see and one past the last (none: INT_MAX, 0), and between which keys all 64
+// see (one that is not there sees nothing)
 typedef int4 BlockSeen;
 __device__ __forceinline__ BlockSeen block_seen(const RangeAttn& a, int b, int rows, int keys, int lane) {
   const int i = b * 64 + lane;
-  const bool in = i < rows;
-  const int2 r = in ? key_range(a, i, keys) : make_int2(0, 0);
+  const int2 r = i < rows ? key_range(a, i, keys) : make_int2(0, 0);
   const bool sees = r.x < r.y;
-  return make_int4(wave_imin(sees ? r.x : INT_MAX), wave_imax(r.y), wave_imax(sees ? r.x : in ? INT_MAX : INT_MIN), wave_imin(sees ? r.y : in ? 0 : INT_MAX));
+  return make_int4(wave_imin(sees ? r.x : INT_MAX), wave_imax(r.y), wave_imax(sees ? r.x : INT_MAX), wave_imin(r.y));
 }
 // Joins the splits of a (query row, head), W waves each a share of them (16 at most), all their loads in flight at once; DHP / 64
 // columns per lane.  (One wave for all, eight splits in flight: 64 splits of 160 rows 10.8 us, 4.8 like this.)
@@ -234,6 +234,7 @@ inline FewShape few_shape(const RangeAttn& a, float* work) {
   f.gp = a.G < 32 ? a.G : 32;
   f.hb = (a.G + f.gp - 1) / f.gp;
   f.qpt = 32 / f.gp;
+  f.inv = (65536 + f.gp - 1) / f.gp;
   f.tiles = cdiv(a.Tq, f.qpt);
   const i64 workgroups = (i64)f.tiles * a.Hkv * f.hb, most = cdiv(a.Tk, 32 * waves);
   i64 n = workgroups ? 2048 / waves / workgroups : 1;

@@ -282,19 +282,22 @@ __global__ void __launch_bounds__(256, 2) range_fwd_few_k(RangeAttn a, FewShape 
     const float d0 = (float)(at - kv - g * 4);
     const int lo = max(fk.r.x, kv) - kv - g * 4;
     const unsigned n = (unsigned)max(min(fk.r.y, kv + 32) - max(fk.r.x, kv), 0);
-    float mx = -INFINITY;
+    float mx = -INFINITY, keep;
+    if constexpr (MOD != 0) {
 #pragma unroll
-    for (int e = 0; e < 16; e++) {
-      const int c = (e >> 2) * 8 + (e & 3);
-      float keep, y = final_score<MOD>(sf, s[e], d0 - (float)c, &keep);
-      if ((unsigned)(c - lo) >= n) y = -INFINITY;
-      s[e] = y;
-      mx = fmaxf(mx, y);
+      for (int e = 0; e < 16; e++) s[e] = final_score<MOD>(sf, s[e], d0 - (float)((e >> 2) * 8 + (e & 3)), &keep);
     }
-    const float mn = fmaxf(m, both_halves_max(mx)), ms = mn == -INFINITY ? 0.f : mn;
+    if (!__all(!row.ok || (fk.r.x <= kv && fk.r.y >= kv + 32))) {
+#pragma unroll
+      for (int e = 0; e < 16; e++) if ((unsigned)((e >> 2) * 8 + (e & 3) - lo) >= n) s[e] = -INFINITY;
+    }
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) mx = fmaxf(fmaxf(mx, s[e]), s[e + 1]);
+    const float unit = MOD != 0 ? 1.f : sf.f;       // (without MOD the scale is positive and goes into the exponential)
+    const float mn = fmaxf(m, both_halves_max(mx) * unit), ms = mn == -INFINITY ? 0.f : mn;
     float rs = 0.f;
 #pragma unroll
-    for (int e = 0; e < 16; e++) { s[e] = fast_exp2(s[e] - ms); rs += s[e]; }
+    for (int e = 0; e < 16; e++) { s[e] = fast_exp2(MOD != 0 ? s[e] - ms : fmaf(s[e], unit, -ms)); rs += s[e]; }
     if (__any(mn > m)) {
       const float alpha = fast_exp2(m - ms);
       l *= alpha;
@@ -770,26 +773,31 @@ __global__ void __launch_bounds__(256, 2) range_dq_few_k(RangeAttn a, FewShape f
     const float d0 = (float)(at - kv - g * 4);
     const int lo = max(fk.r.x, kv) - kv - g * 4;
     const unsigned n = (unsigned)max(min(fk.r.y, kv + 32) - max(fk.r.x, kv), 0);
-    float keep[16], sum = 0.f;
+    float keep[16];
 #pragma unroll
     for (int e = 0; e < 16; e++) {
-      const int c = (e >> 2) * 8 + (e & 3);
-      if constexpr (MOD != 0) s[e] = fast_exp2(final_score<MOD>(sf, s[e], d0 - (float)c, &keep[e]) - L);
+      if constexpr (MOD != 0) s[e] = fast_exp2(final_score<MOD>(sf, s[e], d0 - (float)((e >> 2) * 8 + (e & 3)), &keep[e]) - L);
       else { s[e] = fast_exp2(fmaf(s[e], sf.f, -L)); keep[e] = 1.f; }
-      if ((unsigned)(c - lo) >= n) s[e] = dp[e] = 0.f;
-      sum = fmaf(s[e], dp[e], sum);
+    }
+    const bool masked = !__all(!row.ok || (fk.r.x <= kv && fk.r.y >= kv + 32));
+    if (masked) {
+#pragma unroll
+      for (int e = 0; e < 16; e++) if ((unsigned)((e >> 2) * 8 + (e & 3) - lo) >= n) s[e] = dp[e] = 0.f;
     }
     // (as in the other form: D of a row whose keys are all in this tile)
     const bool alone = fk.r.x >= kv && fk.r.y <= kv + 32 && fk.r.x < fk.r.y;
     if (__any(alone)) {
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; e++) sum = fmaf(s[e], dp[e], sum);
       sum = both_halves_sum(sum);
       if (alone) { D = sum; own = true; }
     }
 #pragma unroll
     for (int e = 0; e < 16; e++) s[e] *= (dp[e] - D) * keep[e];
-    if (!__all(fk.r.x <= kv && fk.r.y >= kv + 32)) {
+    if (masked) {                                   // (D may be no number)
 #pragma unroll
-      for (int e = 0; e < 16; e++) if ((unsigned)((e >> 2) * 8 + (e & 3) - lo) >= n) s[e] = 0.f;      // (D may be no number)
+      for (int e = 0; e < 16; e++) if ((unsigned)((e >> 2) * 8 + (e & 3) - lo) >= n) s[e] = 0.f;
     }
     bf16x8 ds[2], first[T::DT];
     ds[0] = acc_to_frag(s, 0);
@@ -972,7 +980,8 @@ __global__ void __launch_bounds__(256, 2) range_dkv_few_k(RangeAttn a, const Blo
 
 // ---- launchers ----
 static bool takes(const RangeAttn& a, bool back) {
-  if (a.dt != 1 || a.dh > 128 || a.dh % 8) return false;
+  // (the tanh of these kernels is off by up to 2^-22, so a capped score by that of the cap: 2^-10 at most here)
+  if (a.dt != 1 || a.dh > 128 || a.dh % 8 || a.cap > 4096.f) return false;
   uintptr_t p = (uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v;
   p |= back ? (uintptr_t)a.o | (uintptr_t)a.d_o | (uintptr_t)a.dq | (uintptr_t)a.dk | (uintptr_t)a.dv : (uintptr_t)a.out;
   const i64 l = a.ldq | a.ldk | a.ldv | a.ldo;

@@ -68,12 +68,13 @@ template <int DHP> struct Tiles {
   // 16 rows of a buffer, from row0 on, to LDS at dst
   static __device__ __forceinline__ void load16(__amdgpu_buffer_rsrc_t rs, unsigned ldb, int width, int row0, unsigned dst) {
     const int lane = lane_now();
-    const unsigned a = (unsigned)(lane / CPR), c = (unsigned)((lane % CPR) ^ swz<DHP>(lane / CPR));
+    const unsigned c = (unsigned)((lane % CPR) ^ swz<DHP>(lane / CPR)), mine = (unsigned)(lane / CPR) * ldb;      // (one multiplication per lane)
 #pragma unroll
     for (unsigned i = 0; i < LOADS; i++) {
       const unsigned chunk = c ^ (i * (DHP == 128 ? 1u : 2u));              // swz(RPL i + a) = swz(a) ^ ..
-      const unsigned off = (a + row0 + i * RPL) * ldb + chunk * 16u;
-      load_lds_b128(rs, __builtin_amdgcn_readfirstlane(dst + i * 1024u), (int)(chunk * 16u) < width ? off : OOB);
+      unsigned off = mine + chunk * 16u + __builtin_amdgcn_readfirstlane((unsigned)(row0 + (int)i * RPL) * ldb);
+      if (width < ROW) off = (int)(chunk * 16u) < width ? off : OOB;
+      load_lds_b128(rs, __builtin_amdgcn_readfirstlane(dst + i * 1024u), off);
     }
   }
   // per-lane byte offsets: fragments of rows lane & 31 (step kk: ^ kk * 32), transposed ones (column block: ^ dtile * 64)

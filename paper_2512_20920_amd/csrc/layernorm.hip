@@ -384,11 +384,10 @@ template <class T, bool AL, int W, int CH> static int bwd_one(const LayerNorm& a
       return grid;
     }
   }
+  const int n = a.rows < 4 * 32 ? cdiv(a.rows, 4) : 32;
+  if (params) hipLaunchKernelGGL(layernorm_params_k<T>, dim3(cdiv(a.cols, 64), n), dim3(256), 0, s, a);      // (first: dx may be dy)
   hipLaunchKernelGGL((layernorm_bwd_k<T, AL, W, CH, false>), dim3(grid), block, 0, s, a);
-  if (!params) return 0;
-  grid = a.rows < 4 * 32 ? cdiv(a.rows, 4) : 32;
-  hipLaunchKernelGGL(layernorm_params_k<T>, dim3(cdiv(a.cols, 64), grid), dim3(256), 0, s, a);
-  return grid;
+  return params ? n : 0;
 }
 template <class T, bool AL> static int bwd(const LayerNorm& a, bool params, hipStream_t s) {
 #define BWD(W, CH) return bwd_one<T, AL, W, CH>(a, params, s)

@@ -2,7 +2,7 @@
 kernels document (not collected by pytest).
 
 Bounds.  u is half a step of the storage type (bf16 2^-8, float32 2^-24), e = 2^-24.  A score is a float32 sum of dh products: it
-is off by at most (dh + 8) e sum |q k| scale, its cap by cap 2^-21 more (a float32 tanh), its bias by 2 e slope distance.
+is off by at most (dh + 8) e sum |q k| scale, its cap by cap 2^-21 more (the bf16 kernels' tanh; the full one: 8 e of the score), its bias by 2 e slope distance.
 A probability is off by twice that (its own score, the row's sum), by (n + 16) e for the exponential and the sum of n
 terms, and in bf16 by u as an operand of the matrix cores: rel.  Hence o: rel sum p |v| and u |o| for its own
 rounding; dv likewise over the queries.  D = <o, dO> inherits the error of o; ds = p (dP - D) is off by rel |ds|
@@ -58,7 +58,7 @@ def attention(q, k, v, lo, hi, at=None, scale=None, cap=0.0, slopes=None, do=Non
         t = np.tanh(z / cap) if cap else 0.0
         s = t * cap if cap else z
         if cap:
-            e_s = e_s + cap * 2.0 ** -21
+            e_s = e_s + (cap * 2.0 ** -21 if dtype == "bf16" and cap <= 4096 else 8 * E32 * np.abs(s))
         if slopes is not None:
             d = np.abs(np.asarray(at)[:, None] - j) * slopes[h]
             s = s - d

@@ -251,6 +251,26 @@ def test_attention_peaked(scale, mode, dtype):
 
 
 @FORMS
+@pytest.mark.parametrize("cap", [1.0, 3000.0, 1e6])
+def test_attention_caps(cap, mode, dtype):
+    lo, hi, at = ref.ranges([60, 45])
+    a = Attention(dtype, 2, 1, 64, 105, 105)
+    a.run(lo, hi, at, mode, cap=cap)
+    a.check(lo, hi, at, cap=cap)
+
+
+@FORMS
+@pytest.mark.parametrize("dh", [64, 128])
+def test_attention_bias_that_grows_with_the_distance(dh, mode, dtype):
+    """Negative slopes: scores rise to hundreds away from the query, also where no query is (the rows behind the last one)."""
+    lens = [3, 430, 8]
+    lo, hi, at = ref.ranges(lens)
+    a = Attention(dtype, 2, 1, dh, sum(lens), sum(lens), extra_rows=20)
+    a.run(lo, hi, at, mode, slopes=[-1.0, -0.5], used=True)
+    a.check(lo, hi, at, slopes=[-1.0, -0.5])
+
+
+@FORMS
 def test_attention_not_finite_where_it_is_seen(mode, dtype):
     """A NaN that queries see is in their results and in no others (and the call ends)."""
     lo, hi, at = ref.ranges([100, 200])
@@ -581,7 +601,13 @@ def test_layernorm(rows, cols, pad, params, dtype):
         assert ref.outside(_np(dbias), rdb, (rows + 16) * e * np.abs(dyn).sum(0) + ug * np.abs(rdb)) <= 1.0
     if pad:
         assert torch.isnan(y[:, cols:]).all() and torch.isnan(dx[:, cols:]).all()
-    # in place: the same bits
+    # in place, with the sums: the same bits
+    dy3, g3, b3 = dy.clone(), None if dgain is None else torch.empty_like(dgain), None if dbias is None else torch.empty_like(dbias)
+    work.fill_(255)
+    R.revffn_op_layernorm_bwd(dt, dy3, x, gain, mean, rstd, dy3, g3, b3, rows, cols, ld, ld, ld, params == "gain_f32", work)
+    torch.cuda.synchronize()
+    assert torch.equal(dy3[:, :cols], dx[:, :cols]) and (g3 is None or torch.equal(g3, dgain)) and (b3 is None or torch.equal(b3, dbias))
+    # without them
     x2, dy2 = x.clone(), dy.clone()
     R.revffn_op_layernorm_bwd(dt, dy2, x2, gain, mean, rstd, dy2, None, None, rows, cols, ld, ld, ld)
     R.revffn_op_layernorm_fwd(dt, x2, gain, bias, x2, None, None, rows, cols, ld, ld, 1e-5)
