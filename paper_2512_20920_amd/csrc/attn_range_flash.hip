@@ -400,6 +400,10 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen*
       __builtin_amdgcn_sched_barrier(0);
     }
   };
+  // With a bias that falls with the distance every query has few keys of weight, and D's error is as large as all roundings together
+  // in every row.  There dS keeps 16 bits (a fourth product), and part 2 gets D with what the row's dS, which should add up to nothing,
+  // add up to: dq's and dk's errors 1.6 times that of a gradient rounded once -> 1.3, 1.4.
+  float rest = 0.f;
   // dS in place of S.  D = <o, dO> carries the rounding of o, which for a query of few keys counts as much as all other roundings: where
   // one tile holds all keys of a query, its D is summed from the tile's own products instead, D = sum P dP.
   auto gradients = [&](int kv) {
@@ -430,7 +434,12 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen*
       for (int e = 0; e < 16; e++) {
         float keep;
         const float p = prob(j, e, &keep);
-        s[j][e] = p * (dp[j][e] - myD) * keep;
+        float x = p * (dp[j][e] - myD);
+        if constexpr (MOD & BIASED) {
+          if (masked && !seen(j, e)) x = 0.f;
+          rest += x;
+        }
+        s[j][e] = x * keep;
       }
     if (masked) {
 #pragma unroll
@@ -439,8 +448,14 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen*
         for (int e = 0; e < 16; e++)
           if (!seen(j, e)) s[j][e] = 0.f;
     }
+    if constexpr (!(MOD & BIASED)) {
 #pragma unroll
-    for (int c = 0; c < 4; c++) dsf[c] = acc_to_frag(s[c >> 1], c & 1);
+      for (int c = 0; c < 4; c++) dsf[c] = acc_to_frag(s[c >> 1], c & 1);
+    }
+  };
+  auto times_k = [&](const unsigned char* tile) {   // dQ^T += K^T dS^T
+    if constexpr (MOD & BIASED) T::template cols_times_split<64>(acc, tile, cbase, s, first);
+    else T::template cols_times<64>(acc, tile, cbase, dsf, first);
   };
   if (qr.first < qr.end) {
     int kv = qr.first, kv1 = live_from(qr, kv + 64, q0, rows, keys), kv2;
@@ -472,7 +487,7 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen*
       probabilities();
       __builtin_amdgcn_s_setprio(1);
       read_kv(fr[0], now, sv, 0);
-      T::template cols_times<64>(acc, smem_raw + before * T::BYTES, cbase, dsf, first);
+      times_k(smem_raw + before * T::BYTES);
       times_q(now, sv);
       __builtin_amdgcn_s_setprio(0);
       phase_end();
@@ -480,11 +495,12 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen*
       kv1 = kv2;
     }
     probabilities();
-    T::template cols_times<64>(acc, smem_raw + before * T::BYTES, cbase, dsf, first);
+    times_k(smem_raw + before * T::BYTES);
     wait_vmcnt<0>();                                // the zero-filled loads past the last tile
     phase_end();
   }
   const RangeAttn b = args_again();
+  if constexpr (MOD & BIASED) myD += both_halves_sum(rest);
   if (g == 0 && myq < rows) b.dvec[(i64)h * b.Tq + myq] = myD;
   if (partly && !T::finite(acc)) {
     for (int r = 0; r < 32 && q0 + wv * 32 + r < rows; r++) range_row_dq<bf16>(args_again(), q0 + wv * 32 + r, h, keys, (float*)smem_raw + wv * 2 * DHP);
@@ -762,6 +778,7 @@ __global__ void __launch_bounds__(256, 2) range_dq_few_k(RangeAttn a, FewShape f
   const unsigned rbase = T::row_base(lane), cbase = T::col_base(lane);
   f32x16 acc[T::DT] = {};
   bool own = wv == 0;                               // this wave has the row's D
+  float rest = 0.f;
   while (t < fk.t1) {
     const int kv = fk.first + t * 32, next = fk.live_from(t + 4, 4);
     wait_vmcnt<0>();
@@ -794,23 +811,32 @@ __global__ void __launch_bounds__(256, 2) range_dq_few_k(RangeAttn a, FewShape f
       if (alone) { D = sum; own = true; }
     }
 #pragma unroll
-    for (int e = 0; e < 16; e++) s[e] *= (dp[e] - D) * keep[e];
+    for (int e = 0; e < 16; e++) s[e] *= dp[e] - D;
     if (masked) {                                   // (D may be no number)
 #pragma unroll
       for (int e = 0; e < 16; e++) if ((unsigned)((e >> 2) * 8 + (e & 3) - lo) >= n) s[e] = 0.f;
     }
-    bf16x8 ds[2], first[T::DT];
-    ds[0] = acc_to_frag(s, 0);
-    ds[1] = acc_to_frag(s, 1);
+    if constexpr (MOD & BIASED) {                   // (as in the other form)
+#pragma unroll
+      for (int e = 0; e < 16; e++) rest += s[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 16; e++) s[e] *= keep[e];
+    bf16x8 first[T::DT];
     T::read_cols(first, tK, cbase, 0);
-    T::template cols_times<32>(acc, tK, cbase, ds, first);
+    if constexpr (MOD & BIASED) T::template cols_times_split<32>(acc, tK, cbase, &s, first);
+    else {
+      const bf16x8 ds[2] = {acc_to_frag(s, 0), acc_to_frag(s, 1)};
+      T::template cols_times<32>(acc, tK, cbase, ds, first);
+    }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
     if (next < fk.t1) issue(rk, next, aK);
     t = next;
   }
-  float2* found = (float2*)(smem_raw + 4 * T::BYTES);      // [wave][row]: D, and whether it is the one
-  if (g == 0) found[wv * 32 + lane] = make_float2(D, own ? 1.f : 0.f);
+  float4* found = (float4*)(smem_raw + 4 * T::BYTES);      // [wave][row]: D, whether it is the one, the sum of dS
+  rest = both_halves_sum(rest);
+  if (g == 0) found[wv * 32 + lane] = make_float4(D, own ? 1.f : 0.f, rest, 0.f);
   put_partial<T::DT>((float*)tK, acc, lane);
   __syncthreads();
   const FewRow mine = few_row(a, f, tile, head, threadIdx.x & 31, rows);
@@ -818,6 +844,10 @@ __global__ void __launch_bounds__(256, 2) range_dq_few_k(RangeAttn a, FewShape f
     float d = found[threadIdx.x].x;
 #pragma unroll
     for (int w = 1; w < 4; w++) if (found[w * 32 + threadIdx.x].y != 0.f) d = found[w * 32 + threadIdx.x].x;
+    if constexpr (MOD & BIASED) {
+#pragma unroll
+      for (int w = 0; w < 4; w++) d += found[w * 32 + threadIdx.x].z;
+    }
     a.dvec[(i64)mine.h * a.Tq + mine.i] = d;
   }
   const bool fine = few_store<bf16, DHP, 4>((const float*)smem_raw, (bf16*)a.dq + (i64)mine.i * a.ldq + (i64)mine.h * a.dh, mine.ok, a.dh, a.scale);
@@ -1042,7 +1072,7 @@ template <int DHP, int MOD> static void bwd(const RangeAttn& a, void* blocks, fl
   const bool fq = few_dq(a, form), fkv = few_dkv(a, form);
   if (a.Tq > 0 && fq) {
     static std::atomic<unsigned long long> mask{0};
-    constexpr unsigned smem = 4 * Tiles<DHP>::BYTES + 4 * 256;
+    constexpr unsigned smem = 4 * Tiles<DHP>::BYTES + 4 * 512;
     set_lds(mask, range_dq_few_k<DHP, MOD>, smem);
     FewShape f = few_shape(a, nullptr);
     f.splits = 1;

@@ -121,6 +121,26 @@ template <int DHP> struct Tiles {
       __builtin_amdgcn_sched_barrier(0);
     }
   }
+  // the same with p as two bf16 numbers, which hold 16 bits of it: a is the accumulator layout's tiles of 32 rows
+  template <int N> static __device__ __forceinline__ void cols_times_split(f32x16 (&acc)[DT], const unsigned char* tile, unsigned cbase, const f32x16* a, bf16x8 (&first)[DT]) {
+    bf16x8 f[2][DT];
+#pragma unroll
+    for (int d = 0; d < DT; d++) f[0][d] = first[d];
+#pragma unroll
+    for (int c = 0; c < N / 16; c++) {
+      if (c < N / 16 - 1) read_cols(f[(c + 1) & 1], tile, cbase, c + 1);
+      const bf16x8 hi = acc_to_frag(a[c >> 1], c & 1);
+      bf16x8 lo;
+#pragma unroll
+      for (int u = 0; u < 8; u++) lo[u] = (__bf16)(a[c >> 1][8 * (c & 1) + u] - (float)hi[u]);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int d = 0; d < DT; d++) acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[c & 1][d], hi, acc[d], 0, 0, 0);
+#pragma unroll
+      for (int d = 0; d < DT; d++) acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[c & 1][d], lo, acc[d], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
   // one row times f; the lanes of a half hold 4 of 8 columns
   static __device__ __forceinline__ void store(bf16* row, const f32x16 (&acc)[DT], float f, int dh, int g) {
 #pragma unroll
