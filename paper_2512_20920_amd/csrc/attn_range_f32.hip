@@ -178,16 +178,16 @@ template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) 
   if (k0 >= keys) return;
   f32x16 dka[DHP / 32] = {}, dva[DHP / 32] = {};
   const int nb = (rows + 63) / 64;
-  int turn = 0;
+  int n = part * NW + wv;                            // this wave's next one of the pairs of a block, 2 G to a block
   for (int b0 = 0; b0 < nb; b0 += 64) {
     const int2 r = b0 + lane < nb ? *(const int2*)(blocks + b0 + lane) : make_int2(INT_MAX, 0);
     unsigned long long live = __ballot(r.x < k0 + 32 && r.y > k0);
     while (live) {
       const int b = b0 + __builtin_ctzll(live);
       live &= live - 1;
-      for (int n = 0; n < 2 * a.G; n++, turn++) {
+      for (; n < 2 * a.G; n += NW * parts) {
         const int q0 = b * 64 + (n & 1) * 32, h = kh * a.G + (n >> 1), i = q0 + (lane & 31);
-        if (turn % (NW * parts) != part * NW + wv || q0 >= rows) continue;
+        if (q0 >= rows) continue;
         const int2 see = i < rows ? key_range(a, i, keys) : make_int2(0, 0);
         if (!__any(see.x < k0 + 32 && see.y > k0)) continue;
         const int ic = min(i, rows - 1);
@@ -218,6 +218,7 @@ template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) 
         accumulate<DHP>(dva, d_o, a.ldo, a.dh, q0, rows - 1, s, lane);
         accumulate<DHP>(dka, q, a.ldq, a.dh, q0, rows - 1, dp, lane);
       }
+      n -= 2 * a.G;
     }
   }
   const int r = k0 + (int)(threadIdx.x & 31);

@@ -542,23 +542,23 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dkv_k(RangeAttn a, const Blo
   b0 = wave_imin(b0);
   b1 = wave_imax(b1);
   unsigned long long live = 0;
-  int base = b0 - 64, pair = -1, blk = -1, hg = a.G - 1;
+  int base = b0 - 64, blk = -1, hg = part - parts;  // hg: head of the pairs of block blk
+  bool first = true;
   auto next = [&]() {                               // the next (block, head) of this part; blk = -1: none
-    do {
-      if (++hg == a.G) {
-        hg = 0;
-        while (!live) {
-          base += 64;
-          if (base > b1 || b1 < 0) { blk = -1; return; }
-          const int b = base + lane_now();
-          const int2 t = b <= b1 ? seen2[2 * (i64)b] : make_int2(INT_MAX, 0);
-          live = __ballot(t.x < k0 + 128 && t.y > k0);
-        }
-        blk = base + __builtin_ctzll(live);
-        live &= live - 1;
+    hg += parts;
+    while (first || hg >= a.G) {
+      while (!live) {
+        base += 64;
+        if (base > b1 || b1 < 0) { blk = -1; return; }
+        const int b = base + lane_now();
+        const int2 t = b <= b1 ? seen2[2 * (i64)b] : make_int2(INT_MAX, 0);
+        live = __ballot(t.x < k0 + 128 && t.y > k0);
       }
-      pair++;
-    } while (pair % parts != part);
+      if (!first) hg -= a.G;
+      first = false;
+      blk = base + __builtin_ctzll(live);
+      live &= live - 1;
+    }
   };
   f32x16 dkacc[T::DT] = {}, dvacc[T::DT] = {};
   const unsigned lds0 = lds_address(smem_raw);
@@ -878,11 +878,10 @@ __global__ void __launch_bounds__(256, 2) range_dkv_few_k(RangeAttn a, const Blo
   // the pairs of a block of 32 queries, in a block of 64 that sees some of the keys, and a head, dealt out to the waves of all parts
   const int nb = (rows + 63) / 64;
   unsigned long long live = __ballot(lane < nb && seen0.x < k0 + 32 && seen0.y > k0);
-  int base = 0, n = 2 * a.G - 1, turn = -1, blk = 0, q0 = -1, h = 0;
+  int base = 0, blk = -1, n = part * 4 + wv, q0 = -1, h = 0;      // n: of the pairs of block blk, 2 G to a block
   auto next = [&]() {                               // q0 = -1: none
     do {
-      if (++n == 2 * a.G) {
-        n = 0;
+      while (blk < 0 || n >= 2 * a.G) {
         while (!live) {
           base += 64;
           if (base >= nb) { q0 = -1; return; }
@@ -890,13 +889,14 @@ __global__ void __launch_bounds__(256, 2) range_dkv_few_k(RangeAttn a, const Blo
           const int2 r = b < nb ? *(const int2*)(blocks + b) : make_int2(INT_MAX, 0);
           live = __ballot(r.x < k0 + 32 && r.y > k0);
         }
+        if (blk >= 0) n -= 2 * a.G;
         blk = base + __builtin_ctzll(live);
         live &= live - 1;
       }
-      turn++;
       q0 = blk * 64 + (n & 1) * 32;
       h = kh * a.G + (n >> 1);
-    } while (turn % (4 * parts) != part * 4 + wv || q0 >= rows);
+      n += 4 * parts;
+    } while (q0 >= rows);
   };
   auto issue = [&]() {
     const int m = min(32, rows - q0);
@@ -1061,10 +1061,11 @@ size_t range_flash_sum_floats(const RangeAttn& a) {
 // Which form each kernel takes; form: 0 by the rules, 1 for few rows, 2 for many.  us, many -> few:
 //   forward, query rows x heads   packed documents, 2048 x 16 of 128 (longest 730): 31.6 -> 27.0   2048 x 16, one document: 57.0 -> 57.4
 //     2111 x 12 of 64, behind 4014 keys: 50.4 -> 35.8   4000 x 8 of 64: 47.4 -> 36.4   4096 x 16, 8 documents: 29.0 -> 49.4
+//     4095 x 16 of 64, capped: 54.2 -> 49.7   2000 x 32 of 64, capped: 49.8 -> 41.6
 //   dQ   the same: 40.2 -> 33.4, 69.9 -> 61.8   4000 x 8 of 64: 54.3 -> 32.4   2000 x 32 of 64: 59.1 -> 50.7   4096 x 16 of 128: 37.5 -> 59.6
 //   dK/dV 2048 x 16 of 128: 58.0 -> 39.3, 99.5 -> 73.2   4095 x 16 (8 key heads) of 64: 85 -> 75   4096 x 16 of 128: 47.8 -> 66
 // At 32 k rows x heads the form for many has one workgroup per CU.
-static bool few_fwd(const RangeAttn& a, int form) { return form ? form == 1 : (i64)a.Tq * a.H <= 32 * 1024; }
+static bool few_fwd(const RangeAttn& a, int form) { return form ? form == 1 : (i64)a.Tq * a.H <= (a.dh <= 64 ? 64 : 32) * 1024; }
 static bool few_dq(const RangeAttn& a, int form) { return form ? form == 1 : (i64)a.Tq * a.H <= (a.dh <= 64 ? 64 : 32) * 1024; }
 static bool few_dkv(const RangeAttn& a, int form) { return form ? form == 1 : (a.G <= 2 || (i64)a.Tk * a.Hkv <= 4 * 1024) && (i64)a.Tk * a.H <= (a.G == 1 ? 32 : 64) * 1024; }
 
