@@ -106,6 +106,8 @@ __global__ void __launch_bounds__(256, 2) range_fwd_k(RangeAttn a) {
     if constexpr (MOD != 0) {
       const float d0 = (float)(at - kv - g * 4);
       float keep;
+      tanh_scores<MOD, true>(sf, s[0]);
+      tanh_scores<MOD, true>(sf, s[1]);
 #pragma unroll
       for (int j = 0; j < 2; j++)
 #pragma unroll
@@ -284,6 +286,7 @@ __global__ void __launch_bounds__(256, 2) range_fwd_few_k(RangeAttn a, FewShape 
     const unsigned n = (unsigned)max(min(fk.r.y, kv + 32) - max(fk.r.x, kv), 0);
     float mx = -INFINITY, keep;
     if constexpr (MOD != 0) {
+      tanh_scores<MOD, true>(sf, s);
 #pragma unroll
       for (int e = 0; e < 16; e++) s[e] = final_score<MOD>(sf, s[e], d0 - (float)((e >> 2) * 8 + (e & 3)), &keep);
     }
@@ -409,6 +412,8 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen*
   auto gradients = [&](int kv) {
     const bool masked = kv < all_from || kv + 64 > all_to, alone = mine.x >= kv && mine.y <= kv + 64;
     if (masked) partly = true;
+    tanh_scores<MOD, false>(sf, s[0]);
+    tanh_scores<MOD, false>(sf, s[1]);
     float d0 = (float)(at - kv - g * 4);
     int lo = max(mine.x, kv) - kv - g * 4;
     const unsigned n = (unsigned)max(min(mine.y, kv + 64) - max(mine.x, kv), 0);
@@ -617,6 +622,7 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dkv_k(RangeAttn a, const Blo
           dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[kk & 1][1], vf[kk], dp, 0, 0, 0);
           __builtin_amdgcn_sched_barrier(0);
         }
+        tanh_scores<MOD, false>(sf, s);
         // element e is query j * 32 + (e >> 2) * 8 + g * 4 + (e & 3) of the block
 #pragma unroll
         for (int eb = 0; eb < 4; eb++) {
@@ -791,6 +797,7 @@ __global__ void __launch_bounds__(256, 2) range_dq_few_k(RangeAttn a, FewShape f
     const int lo = max(fk.r.x, kv) - kv - g * 4;
     const unsigned n = (unsigned)max(min(fk.r.y, kv + 32) - max(fk.r.x, kv), 0);
     float keep[16];
+    tanh_scores<MOD, false>(sf, s);
 #pragma unroll
     for (int e = 0; e < 16; e++) {
       if constexpr (MOD != 0) s[e] = fast_exp2(final_score<MOD>(sf, s[e], d0 - (float)((e >> 2) * 8 + (e & 3)), &keep[e]) - L);
@@ -928,6 +935,7 @@ __global__ void __launch_bounds__(256, 2) range_dkv_few_k(RangeAttn a, const Blo
     const unsigned rbase = T::row_base(lane), cbase = T::col_base(lane);
     f32x16 s, dp;
     rows_times2<DHP>(s, dp, tQ, tQ + T::BYTES / 2, rbase, kf, vf);
+    tanh_scores<MOD, false>(sf, s);
     const int2 lo_hi = make_int2(((const int*)st)[128 + (lane & 31)], ((const int*)st)[192 + (lane & 31)]);
 #pragma unroll
     for (int eb = 0; eb < 4; eb++) {
@@ -1010,7 +1018,7 @@ __global__ void __launch_bounds__(256, 2) range_dkv_few_k(RangeAttn a, const Blo
 
 // ---- launchers ----
 static bool takes(const RangeAttn& a, bool back) {
-  // (the tanh of these kernels is off by up to 2^-22, so a capped score by that of the cap: 2^-10 at most here)
+  // (the tanh of these kernels is off by up to 2^-22 where a wave has large scores, a capped score by that of the cap: 2^-10 at most here)
   if (a.dt != 1 || a.dh > 128 || a.dh % 8 || a.cap > 4096.f) return false;
   uintptr_t p = (uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v;
   p |= back ? (uintptr_t)a.o | (uintptr_t)a.d_o | (uintptr_t)a.dq | (uintptr_t)a.dk | (uintptr_t)a.dv : (uintptr_t)a.out;
