@@ -392,7 +392,8 @@ int revffn_op_attention_ranges(const int32_t *cu_q, const int32_t *cu_k, const i
  * dk and dv are summed over the query heads that share a key head.
  * REVFFN_EINVAL: a bad field, work_bytes too small.  REVFFN_ESHAPE: a row stride below the row's width, or more rows
  * times heads than a launch can have (2^26).  REVFFN_EUNSUPPORTED: kernel_mode 2 and a shape that the matrix-core kernels
- * don't take (float32: dh a multiple of 4 up to 128; bfloat16: of 8; strides and pointers aligned to 16 bytes). */
+ * don't take (float32: dh a multiple of 4 up to 128; bfloat16: of 8, softcap up to 4096, strides below 2^24; strides and
+ * pointers aligned to 16 bytes). */
 size_t revffn_op_attention_masked_workspace(const revffn_attn_desc *desc, int32_t backward);
 int revffn_op_attention_masked_fwd(const revffn_attn_desc *desc, const revffn_attn_mask *mask, const void *q, const void *k,
                                    const void *v, void *o, float *lse, void *work, size_t work_bytes, void *hip_stream);
@@ -426,7 +427,8 @@ int revffn_op_rotary(int32_t dtype, const revffn_rotary *r, const void *x, void 
 /* LayerNorm of `rows` rows (fewer than 2^22) of `cols` (<= 2^24) columns: y = (x - mean) * rstd * gain + bias, rstd = 1 / sqrt(variance + eps).  gain and
  * bias (dtype, [cols]) may be NULL (1 and 0).  mean, rstd (float32 [rows]) may be NULL; the backward pass needs them.  y may be
  * x with the same stride.  Backward: dx, and the sums dgain, dbias over the rows (either may be NULL: not wanted), in
- * dtype, or float32 with grads_f32; dx may be dy with the same stride.  All are overwritten.  work: revffn_op_layernorm_workspace bytes,
+ * dtype, or float32 with grads_f32; dx may be dy with the same stride, but not x
+ * (REVFFN_EINVAL).  All are overwritten.  work: revffn_op_layernorm_workspace bytes,
  * read only if dgain or dbias is wanted.  rows = 0 is allowed (dgain = dbias = 0). */
 size_t revffn_op_layernorm_workspace(int32_t rows, int32_t cols);
 int revffn_op_layernorm_fwd(int32_t dtype, const void *x, const void *gain, const void *bias, void *y, float *mean,

@@ -55,7 +55,8 @@ __global__ void __launch_bounds__(256) attn_ranges_k(const int* __restrict__ cu_
 }
 void launch_attn_ranges(const int* cu_q, const int* cu_k, const int* prefix, int n_docs, int causal, int window, int Tq, int Tk,
                         int* lo, int* hi, int* at, int* used, hipStream_t s) {
-  hipLaunchKernelGGL(attn_ranges_k, dim3(cdiv(Tq, 256)), dim3(256), 0, s, cu_q, cu_k, prefix, n_docs, causal, window, Tq, Tk, lo, hi, at, used);
+  const int grid = Tq > 0 ? cdiv(Tq, 256) : 1;      // (without rows: `used` alone)
+  hipLaunchKernelGGL(attn_ranges_k, dim3(grid), dim3(256), 0, s, cu_q, cu_k, prefix, n_docs, causal, window, Tq, Tk, lo, hi, at, used);
 }
 
 // a workgroup is four rows of one head, a wave each

@@ -237,6 +237,16 @@ def test_attention_ranges():
     assert dl.min() >= 0 and dh.max() <= 21
 
 
+def test_attention_ranges_of_no_queries():
+    used = torch.full((2,), -7, dtype=torch.int32, device="cuda")
+    nothing = torch.empty(0, dtype=torch.int32, device="cuda")
+    for cu_q, cu_k, Tk, want in [(_ints([0, 0, 0]), _ints([0, 3, 5]), 9, [0, 5]), (None, None, 8, [0, 8]), (_ints([0, 0, 0]), None, 9, [0, 0])]:
+        used.fill_(-7)
+        R.revffn_op_attention_ranges(cu_q, cu_k, None, 2, True, 0, 0, Tk, nothing, nothing, nothing, used)
+        torch.cuda.synchronize()
+        assert used.tolist() == want
+
+
 FORMS = pytest.mark.parametrize("dtype,mode", [("bf16", 1), ("bf16", 256), ("bf16", 512), ("f32", 0)])
 
 
