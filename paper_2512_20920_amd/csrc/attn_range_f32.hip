@@ -5,11 +5,12 @@
 // the two halves of the wave hold in element e.  So probabilities stay in the registers they were computed in, at full
 // precision, and keys and values are read from memory as operands directly: K 16 bytes of its own row per lane, V a row of 32
 // consecutive columns per half.  32 rows (keys) per workgroup, tiles of 32 shared out to the waves.
+// Bound by the matrix pipe's 64 clocks per instruction and, in small calls, the chain of loads around them: 2048 rows x 16 heads of 128
+// (documents of 1500 and 548) 201, 302 and 416 us, 50 to 52 of the 154 TFLOP/s of a large float32 product; 751 x 4 of 64: 13, 19, 24.
 #include "attn_range_few.h"
 
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
-
 
 __device__ __forceinline__ int elem_row(int e, int half) { return (e >> 2) * 8 + half * 4 + (e & 3); }
 __device__ __forceinline__ float half_sum(float v) { return v + __shfl_xor(v, 32, WAVE); }
@@ -107,7 +108,8 @@ template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) 
   few_finish<float, DHP, NW>(a, f, tile, split, head, rows, keys, sm, stats, sm);
 }
 
-// dQ of 32 rows, and D = <o, dO>.  The last workgroups of the launch (from `tiles` on) note instead, a wave per block of 64 queries, the first key that
+// dQ of 32 rows, and D = <o, dO>; where there are few workgroups the keys are split as in the forward pass (751 rows x 4 heads of
+// 64: 28 us, 19 + 4.6 split in two; 1000 x 4: all passes 116 -> 99).  The last workgroups of the launch (from `tiles` on) note instead, a wave per block of 64 queries, the first key that
 // some of them see and one past the last.
 template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) range_dq_f32_k(RangeAttn a, FewShape f, int tiles, BlockSeen* __restrict__ blocks) {
   extern __shared__ float sm[];
@@ -134,11 +136,11 @@ template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) 
   const int rows = rows_in_use(a), keys = keys_in_use(a);
   if (tile * f.qpt >= rows) return;
   row.ok = row.ok && row.i < rows;
-  const FewKeys fk = few_keys(f, row, stored, 0, keys, &t0);
+  const FewKeys fk = few_keys(f, row, stored, split, keys, &t0);
 #pragma unroll
   for (int c = 0; c < DHP / 2; c++) D = fmaf(qf[c], dof[c], D);
   D = half_sum(D);
-  if (wv == 0 && half == 0 && row.ok) a.dvec[srow] = D;
+  if (split == 0 && wv == 0 && half == 0 && row.ok) a.dvec[srow] = D;
   load_row<DHP>((const float*)a.q + qrow, row.ok, a.dh, half, a.scale, qf);
   f32x16 acc[DHP / 32] = {};
   for (int t = fk.live_from(t0 + wv, NW); t < fk.t1; t = fk.live_from(t + NW, NW)) {
@@ -157,6 +159,10 @@ template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) 
   spill<DHP>(sm + wv * DHP * 32, acc, lane);
   __syncthreads();
   const FewRow mine = few_row(a, f, tile, head, threadIdx.x & 31, rows);
+  if (f.splits > 1) {                               // (the launch below adds them)
+    (void)few_store<float, DHP, NW>(sm, f.part + (((i64)mine.i * a.H + mine.h) * f.splits + split) * DHP, mine.ok, DHP, 1.f);
+    return;
+  }
   const bool fine = few_store<float, DHP, NW>(sm, (float*)a.dq + (i64)mine.i * a.ldq + (i64)mine.h * a.dh, mine.ok, a.dh, a.scale);
   if (__syncthreads_or(!fine))
     for (int x = wv; x < 32; x += NW) {
@@ -165,6 +171,30 @@ template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) 
     }
 }
 
+// dQ from the splits' sums, a wave per query row and head
+template <int DHP> __global__ void __launch_bounds__(256) range_dq_sum_f32_k(RangeAttn a, FewShape f) {
+  __shared__ float lds[4][2 * DHP];
+  constexpr int C = DHP / 64;
+  const int rows = rows_in_use(a), lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const i64 n = (i64)blockIdx.x * 4 + wv;
+  const int i = (int)(n / a.H), h = (int)(n - (i64)i * a.H);
+  if (i >= rows) return;
+  float v[C] = {}, z = 0.f;
+  const float* p = f.part + n * f.splits * DHP + lane * C;
+#pragma unroll 4
+  for (int x = 0; x < f.splits; x++)
+#pragma unroll
+    for (int c = 0; c < C; c++) v[c] += p[x * DHP + c];
+#pragma unroll
+  for (int c = 0; c < C; c++) z = fmaf(v[c], 0.f, z);
+  if (!__all(z == 0.f)) {                           // a value that is not finite: seen, or only in a tile with seen ones?
+    range_row_dq<float>(a, i, h, keys_in_use(a), lds[wv]);
+    return;
+  }
+  float* dq = (float*)a.dq + (i64)i * a.ldq + (i64)h * a.dh;
+#pragma unroll
+  for (int c = 0; c < C; c++) if (lane * C + c < a.dh) dq[lane * C + c] = v[c] * a.scale;
+}
 // dK, dV of 32 keys of a key head: the waves share out the blocks of 32 queries that see some of them, of every head that shares it.
 template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) range_dkv_f32_k(RangeAttn a, const BlockSeen* __restrict__ blocks, float* __restrict__ sums, int parts) {
   extern __shared__ float sm[];                      // NW results [DHP][32], then 5 x 32 words per wave
@@ -273,9 +303,11 @@ static int dkv_parts(const RangeAttn& a) {
   while (n < 8 && workgroups * n * 2 * waves <= 2048 && pairs >= 2 * n * waves) n *= 2;
   return n;
 }
+// the sums of dQ's splits or of dK's and dV's parts, one after the other in the same memory
 size_t range_f32_sum_floats(const RangeAttn& a) {
   const int n = dkv_parts(a);
-  return n > 1 ? (size_t)n * 2 * a.Tk * a.Hkv * (a.dh <= 64 ? 64 : 128) : 0;
+  const size_t kv = n > 1 ? (size_t)n * 2 * a.Tk * a.Hkv * (a.dh <= 64 ? 64 : 128) : 0, q = few_floats(a);
+  return kv > q ? kv : q;
 }
 template <int DHP, int NW, bool CAP> static void bwd(const RangeAttn& a, void* blocks, float* sums, hipStream_t s) {
   constexpr size_t smem = (size_t)NW * DHP * 32 * 4, smem_kv = smem + NW * 160 * 4;
@@ -283,10 +315,11 @@ template <int DHP, int NW, bool CAP> static void bwd(const RangeAttn& a, void* b
   set_lds(mask_q, range_dq_f32_k<DHP, NW, CAP>, smem);
   set_lds(mask_kv, range_dkv_f32_k<DHP, NW, CAP>, smem_kv);
   FewShape f = few_shape(a, nullptr);
-  f.splits = 1;
-  const int tiles = f.tiles * a.Hkv * f.hb;
+  f.part = sums;
+  const int tiles = f.tiles * f.splits * a.Hkv * f.hb;
   if (a.Tq > 0)
     hipLaunchKernelGGL((range_dq_f32_k<DHP, NW, CAP>), dim3((unsigned)(tiles + cdiv(a.Tq, 64 * NW))), dim3(NW * 64), smem, s, a, f, tiles, (BlockSeen*)blocks);
+  if (f.splits > 1) hipLaunchKernelGGL((range_dq_sum_f32_k<DHP>), dim3((unsigned)cdiv((i64)a.Tq * a.H, 4)), dim3(256), 0, s, a, f);
   if (a.Tk <= 0) return;
   const int parts = dkv_parts(a);
   hipLaunchKernelGGL((range_dkv_f32_k<DHP, NW, CAP>), dim3((unsigned)((i64)cdiv(a.Tk, 32) * a.Hkv * parts)), dim3(NW * 64), smem_kv, s, a,

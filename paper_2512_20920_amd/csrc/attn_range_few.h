@@ -227,7 +227,9 @@ template <class T, int DHP> static void sum_parts(const RangeAttn& a, const floa
 }
 
 inline int few_waves(const RangeAttn& a) { return a.dt == 0 && a.dh <= 64 ? 8 : 4; }      // of a workgroup
-// Workgroups that give every CU eight waves, of a tile of keys per wave at least.
+// Workgroups that give every CU eight waves, of a tile of keys per wave at least.  A second launch costs 4 us and more, so few splits
+// don't pay in bfloat16: 600 rows x 12 heads of 128 whole 13.2 us, in two 15.9 + 5.7; 1000 x 8 of 64 10.6, 11 + 4.9.  Float32, whose products take
+// eight times as long: 751 x 4 of 64 whole 19.4, in two 13.4 + 4.1.
 inline FewShape few_shape(const RangeAttn& a, float* work) {
   const int waves = few_waves(a);
   FewShape f;

@@ -56,6 +56,8 @@ __device__ __forceinline__ int live_from(const QueryRanges& q, int kv, int q0, i
 // that some query sees to the last, tiles that none sees left out; K two tiles ahead and V one.  An iteration is two phases with a
 // barrier behind each: in the first a wave takes the maximum and half of the exponentials and reads the next tile's key
 // fragments, in the second it multiplies those and P V of this tile, with the other half of the exponentials between.
+// Bound by the matrix pipe and the exponentials by turns, 1.2 us per tile of 128 x 64 on a full CU, 1.8 alone: one document of 8192 rows, 16
+// heads of 128: 303 us, 0.9 PFLOP/s; 16 documents of 512: 56 us.
 // ------------------------------------------------------------------------------------
 template <int DHP, int MOD>
 __global__ void __launch_bounds__(256, 2) range_fwd_k(RangeAttn a) {
@@ -224,7 +226,8 @@ __global__ void __launch_bounds__(256, 2) range_fwd_k(RangeAttn a) {
 // ------------------------------------------------------------------------------------
 // Forward for few rows: 32 rows per workgroup, tiles of 32 keys shared out to the waves, each in LDS of its own that no other wave
 // touches, so nothing waits at a barrier until the partial results meet.  A single token's query against a long run of keys
-// reads every key and value once, for all heads that share them: that reading bounds it.
+// reads every key and value once, for all heads that share them: that reading bounds it (92800 keys of five sequences, 8 key heads of
+// 128: 70 us, 5.4 TB/s, and 4.8 to join).
 // ------------------------------------------------------------------------------------
 // a wave's result to its part of LDS, [column][32 rows]
 template <int DT> __device__ __forceinline__ void put_partial(float* mine, const f32x16 (&acc)[DT], int lane) {
@@ -333,6 +336,7 @@ __global__ void __launch_bounds__(256, 2) range_fwd_few_k(RangeAttn a, FewShape 
 // Backward, part 1: dQ, D = <o, dO> of the rows, and per block of 64 queries which keys some and all of them see, for part 2.
 //   S^T = K Q^T,  P^T = exp(S^T - lse),  dP^T = V dO^T,  dS^T = P^T (dP^T - D),  dQ^T += K^T dS^T,  times scale at the end.
 // The forward kernel's tiles and phases; the keys of a tile are read once more in the phase after, so they have three stages.
+// One document of 8192 rows, 16 heads of 128: 378 us, 1.1 PFLOP/s, the matrix pipe 65 % busy.
 // ------------------------------------------------------------------------------------
 template <int DHP, int MOD>
 __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen* __restrict__ blocks) {
@@ -518,8 +522,9 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen*
 // Backward, part 2: dK and dV.  Workgroup = 128 keys of one key head, wave = 32 keys (one per lane column).  It goes over the blocks of
 // 64 queries that see some of its keys, and in each over the query heads that share the key head:
 //   S = Q K^T,  P = exp(S - lse),  dP = dO V^T,  dS = P (dP - D),  dV^T += dO^T P,  dK^T += Q^T dS, times scale at the end.
-// parts > 1: workgroup `part` of a tile takes every parts-th of those (block, head) pairs and leaves its sums in float32 for the
-// kernel below.
+// parts > 1: workgroup `part` of a tile takes every parts-th of those (block, head) pairs and leaves its sums in float32 for a second
+// launch.  One document of 8192 rows, 16 heads of 128 to 4, 1, 2, 4 parts: 1258 us, 761 + 17, 612 + 28 (0.9 PFLOP/s); the longest chains
+// of (block, head) pairs bound the first, registers (two waves per SIMD) the last.
 // ------------------------------------------------------------------------------------
 template <int DHP> constexpr unsigned DKV_STAGE = 2 * Tiles<DHP>::BYTES + 5 * 256;      // Q, dO, lse, D, lo, hi, at
 template <int DHP, int MOD>
@@ -707,7 +712,8 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dkv_k(RangeAttn a, const Blo
 }
 // ------------------------------------------------------------------------------------
 // Backward for few rows: dQ of 32 rows, then dK/dV of 32 keys per workgroup, the keys (the blocks of 32 queries and the heads that share the
-// key head) shared out to the waves, each with tiles of its own in LDS.
+// key head) shared out to the waves, each with tiles of its own in LDS.  A workgroup's first loads and last sums are half of its time where
+// documents are short (2048 rows x 16 heads of 128, longest 730: 33 and 39 us).
 // ------------------------------------------------------------------------------------
 // a^T[row, lane] = tile a's rows x fa, the same for b; the next fragments are read while these are multiplied
 template <int DHP> __device__ __forceinline__ void rows_times2(f32x16& a, f32x16& b, const unsigned char* ta, const unsigned char* tb, unsigned rbase,
@@ -1049,7 +1055,7 @@ template <class K> static void set_lds(std::atomic<unsigned long long>& mask, K 
   }
 }
 // Parts of a key tile's (query block, head) pairs in dK/dV, for 128 keys per workgroup and for 32: workgroups enough to fill the chip twice, where
-// several heads that share a key head make the pairs many (and the float32 sums that a part costs few).
+// several heads that share a key head make the pairs many (and the float32 sums that a part costs few).  For 1 to 8 parts: see range_bwd_dkv_k.
 static int dkv_parts(const RangeAttn& a) {
   const i64 workgroups = (i64)cdiv(a.Tk, 128) * a.Hkv;
   int n = 1;

@@ -2,6 +2,7 @@
 // head, the rest copied.  A workgroup takes a few rows: it works out the (cos, sin) of their pairs once, into LDS, and streams all
 // heads of the rows past them, so that reading x and writing y is what bounds it and the angle may cost what it needs:
 // position * frequency in float64, reduced to a fraction of a turn there, and a full-precision sine and cosine of that.
+// bf16, 8192 rows of 40 heads of 128: 37 us (4.5 TB/s); float32, 4096 rows of 32 heads: 29 us (4.6).
 #include "kernels.h"
 
 template <class T, int V> struct Vec { typedef __attribute__((ext_vector_type(V))) T type; };
