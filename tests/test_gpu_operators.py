@@ -281,6 +281,25 @@ def test_attention_bias_that_grows_with_the_distance(dh, mode, dtype):
 
 
 @FORMS
+@pytest.mark.parametrize("where,value", [("k", NAN), ("q", float("inf")), ("v", float("-inf"))])
+def test_attention_not_finite_beside_long_documents(where, value, mode, dtype):
+    """A short document's value that is not finite between two whose keys (or queries) are split over workgroups, rows behind the last."""
+    lens = [333, 40, 500]
+    lo, hi, at = ref.ranges(lens)
+    inside = np.zeros(sum(lens), bool)
+    inside[333:373] = True
+    a, clean = (Attention(dtype, 4, 2, 64, sum(lens), sum(lens), extra_rows=40) for _ in range(2))
+    getattr(a, where)[350] = value
+    a.run(lo, hi, at, mode, used=True)
+    clean.run(lo, hi, at, mode, used=True)
+    clean.check(lo, hi, at)
+    bounds = ref.attention(clean.part("q"), clean.part("k"), clean.part("v"), lo, hi, at, do=clean.part("do"), dtype=dtype)
+    for name in ("o", "dq", "dk", "dv"):
+        assert ref.outside(a.part(name)[~inside], clean.part(name)[~inside], 2 * bounds[name][1][~inside]) <= 1.0, name
+    assert torch.isnan(a.dq[sum(lens):]).all() and torch.isnan(a.dk[sum(lens):]).all()
+
+
+@FORMS
 def test_attention_not_finite_where_it_is_seen(mode, dtype):
     """A NaN that queries see is in their results and in no others (and the call ends)."""
     lo, hi, at = ref.ranges([100, 200])
