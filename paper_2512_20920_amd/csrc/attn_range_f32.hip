@@ -24,33 +24,84 @@ template <int DHP> __device__ __forceinline__ void load_row(const float* row, bo
     for (int i = 0; i < 4; i++) r[c * 4 + i] = v[i] * f;
   }
 }
-template <int DHP> __device__ __forceinline__ f32x16 scores(const float* row, int dh, int half, const float (&r)[DHP / 2]) {
+// Products of a tile's rows, read from memory, go in groups of 16 instructions (128 columns; about 1000 clocks), the next group's loads on
+// their way meanwhile.
+template <int DHP> struct Chunks {                   // a group of a row's chunks of 4 columns: c = 4 n .. 4 n + 3
+  f32x4 v[4];
+  __device__ __forceinline__ void load(const float* row, int dh, int half, int n) {
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+      const int col = (n * 4 + c) * 8 + half * 4;
+      v[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (col < dh) v[c] = *(const f32x4*)(row + col);
+    }
+  }
+  template <class F> __device__ __forceinline__ void times(f32x16& a, int n, F other) const {      // other(c): 4 columns of the other operand
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+      const f32x4 o = other(n * 4 + c);
+#pragma unroll
+      for (int i = 0; i < 4; i++) a = __builtin_amdgcn_mfma_f32_32x32x2f32(v[c][i], o[i], a, 0, 0, 0);
+    }
+  }
+};
+template <int DHP> __device__ __forceinline__ f32x4 piece(const float (&r)[DHP / 2], int c) { return f32x4{r[c * 4], r[c * 4 + 1], r[c * 4 + 2], r[c * 4 + 3]}; }
+template <int DHP, class F> __device__ __forceinline__ f32x16 scores(const float* row, int dh, int half, F other) {
+  constexpr int N = DHP / 32;
+  Chunks<DHP> x[2];
   f32x16 a = {};
+  x[0].load(row, dh, half, 0);
 #pragma unroll
-  for (int c = 0; c < DHP / 8; c++) {
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if (c * 8 + half * 4 < dh) v = *(const f32x4*)(row + c * 8 + half * 4);
-#pragma unroll
-    for (int i = 0; i < 4; i++) a = __builtin_amdgcn_mfma_f32_32x32x2f32(v[i], r[c * 4 + i], a, 0, 0, 0);
+  for (int n = 0; n < N; n++) {
+    if (n < N - 1) x[(n + 1) & 1].load(row, dh, half, n + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    x[n & 1].times(a, n, other);
+    __builtin_amdgcn_sched_barrier(0);
   }
   return a;
 }
-// acc^T[column, lane] += X^T[column, row] p[row, lane] over the 32 rows of X from r0 on (rows past the last one are that one: p is
-// zero there); all loads in flight before the first product
-template <int DHP> __device__ __forceinline__ void accumulate(f32x16 (&acc)[DHP / 32], const float* x, i64 ld, int dh, int r0, int last, const f32x16& p, int lane) {
-  constexpr int DT = DHP / 32;
-  float v[16][DT];
+// two products of that kind one after the other
+template <int DHP, class F, class G> __device__ __forceinline__ void scores2(f32x16& a, f32x16& b, const float* ra, const float* rb, int dh, int half, F fa, G fb) {
+  constexpr int N = DHP / 32;
+  Chunks<DHP> x[2];
+  a = f32x16{};
+  b = f32x16{};
+  x[0].load(ra, dh, half, 0);
 #pragma unroll
-  for (int e = 0; e < 16; e++) {
-    const float* row = x + (i64)min(r0 + elem_row(e, lane >> 5), last) * ld + (lane & 31);
-#pragma unroll
-    for (int i = 0; i < DT; i++) v[e][i] = (lane & 31) + i * 32 < dh ? row[i * 32] : 0.f;
+  for (int n = 0; n < 2 * N; n++) {
+    if (n < 2 * N - 1) x[(n + 1) & 1].load(n + 1 < N ? ra : rb, dh, half, (n + 1) % N);
+    __builtin_amdgcn_sched_barrier(0);
+    if (n < N) x[n & 1].times(a, n, fa);
+    else x[n & 1].times(b, n - N, fb);
+    __builtin_amdgcn_sched_barrier(0);
   }
-  __builtin_amdgcn_sched_barrier(0);
+}
+// acc^T[column, lane] += X^T[column, row] p[row, lane] over the 32 rows of X from r0 on (rows past the last one are that one: p is
+// zero there); group n: elements 4 n .. 4 n + 3.  The first group is loaded ahead.
+template <int DHP> struct Columns {
+  float v[4][DHP / 32];
+  __device__ __forceinline__ void load(const float* x, i64 ld, int dh, int r0, int last, int lane, int n) {
 #pragma unroll
-  for (int e = 0; e < 16; e++)
+    for (int e = 0; e < 4; e++) {
+      const float* row = x + (i64)min(r0 + elem_row(n * 4 + e, lane >> 5), last) * ld + (lane & 31);
 #pragma unroll
-    for (int i = 0; i < DT; i++) acc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[e][i], p[e], acc[i], 0, 0, 0);
+      for (int i = 0; i < DHP / 32; i++) v[e][i] = (lane & 31) + i * 32 < dh ? row[i * 32] : 0.f;
+    }
+  }
+};
+template <int DHP> __device__ __forceinline__ void accumulate(f32x16 (&acc)[DHP / 32], const Columns<DHP>& first, const float* x, i64 ld, int dh, int r0, int last, const f32x16& p, int lane) {
+  Columns<DHP> c[2];
+  c[0] = first;
+#pragma unroll
+  for (int n = 0; n < 4; n++) {
+    if (n < 3) c[(n + 1) & 1].load(x, ld, dh, r0, last, lane, n + 1);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int e = 0; e < 4; e++)
+#pragma unroll
+      for (int i = 0; i < DHP / 32; i++) acc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(c[n & 1].v[e][i], p[n * 4 + e], acc[i], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  }
 }
 // a wave's accumulators to LDS, [column][32 rows]
 template <int DHP> __device__ __forceinline__ void spill(float* t, const f32x16 (&acc)[DHP / 32], int lane) {
@@ -60,7 +111,7 @@ template <int DHP> __device__ __forceinline__ void spill(float* t, const f32x16 
     for (int e = 0; e < 16; e++) t[(i * 32 + elem_row(e, lane >> 5)) * 32 + (lane & 31)] = acc[i][e];
 }
 // CAP: with the tanh, whose code the other calls would fetch for nothing
-template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) range_fwd_f32_k(RangeAttn a, FewShape f) {
+template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64, 2) range_fwd_f32_k(RangeAttn a, FewShape f) {
   extern __shared__ float sm[];                      // NW results [DHP][32], statistics
   int tile, split, head, t0;
   few_place(a, f, (int)blockIdx.x, &tile, &split, &head);
@@ -80,7 +131,9 @@ template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) 
   float m = -INFINITY, l = 0.f;
   for (int t = fk.live_from(t0 + wv, NW); t < fk.t1; t = fk.live_from(t + NW, NW)) {
     const int kv = fk.first + t * 32;
-    f32x16 s = scores<DHP>(k + (i64)min(kv + (lane & 31), fk.end - 1) * a.ldk, a.dh, half, qf);
+    f32x16 s = scores<DHP>(k + (i64)min(kv + (lane & 31), fk.end - 1) * a.ldk, a.dh, half, [&](int c) { return piece<DHP>(qf, c); });
+    Columns<DHP> first;
+    first.load(v, a.ldv, a.dh, kv, fk.end - 1, lane, 0);
     float mx = -INFINITY;
 #pragma unroll
     for (int e = 0; e < 16; e++) {
@@ -98,7 +151,7 @@ template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) 
     m = mn;
 #pragma unroll
     for (int i = 0; i < DHP / 32; i++) acc[i] *= alpha;
-    accumulate<DHP>(acc, v, a.ldv, a.dh, kv, fk.end - 1, s, lane);
+    accumulate<DHP>(acc, first, v, a.ldv, a.dh, kv, fk.end - 1, s, lane);
   }
   l = half_sum(l);
   float* stats = sm + NW * DHP * 32;
@@ -111,8 +164,8 @@ template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) 
 // dQ of 32 rows, and D = <o, dO>; where there are few workgroups the keys are split as in the forward pass (751 rows x 4 heads of
 // 64: 28 us, 19 + 4.6 split in two; 1000 x 4: all passes 116 -> 99).  The last workgroups of the launch (from `tiles` on) note instead, a wave per block of 64 queries, the first key that
 // some of them see and one past the last.
-template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) range_dq_f32_k(RangeAttn a, FewShape f, int tiles, BlockSeen* __restrict__ blocks) {
-  extern __shared__ float sm[];
+template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64, 2) range_dq_f32_k(RangeAttn a, FewShape f, int tiles, BlockSeen* __restrict__ blocks) {
+  extern __shared__ float sm[];                      // Q and dO of the rows, later NW results [DHP][32]
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
   if ((int)blockIdx.x >= tiles) {
     const int b = ((int)blockIdx.x - tiles) * NW + wv;
@@ -129,24 +182,40 @@ template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) 
   const int at = row.ok && a.at ? a.at[row.i] : row.i;
   const float *k = (const float*)a.k + (i64)kh * a.dh, *v = (const float*)a.v + (i64)kh * a.dh;
   const i64 orow = (i64)row.i * a.ldo + (i64)row.h * a.dh, qrow = (i64)row.i * a.ldq + (i64)row.h * a.dh, srow = (i64)row.h * a.Tq + row.i;
-  float qf[DHP / 2], dof[DHP / 2], D = 0.f;
-  load_row<DHP>((const float*)a.d_o + orow, row.ok, a.dh, half, 1.f, dof);
-  load_row<DHP>((const float*)a.o + orow, row.ok, a.dh, half, 1.f, qf);
+  // the rows' operands, the same for all waves, in LDS as in the kernel below
+  f32x4 *qf = (f32x4*)sm, *dof = qf + DHP / 8 * 64;
+  float D = 0.f;
+#pragma unroll
+  for (int c = 0; c < DHP / 8; c++) {
+    const int col = c * 8 + half * 4;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x, z = x;
+    if (row.ok && col < a.dh) {
+      if (c % NW == wv) x = *(const f32x4*)((const float*)a.q + qrow + col);
+      y = *(const f32x4*)((const float*)a.d_o + orow + col);
+      z = *(const f32x4*)((const float*)a.o + orow + col);
+    }
+    if (c % NW == wv) {
+      qf[c * 64 + lane] = x * a.scale;
+      dof[c * 64 + lane] = y;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; u++) D = fmaf(y[u], z[u], D);
+  }
   const float L = row.ok ? a.lse[srow] : -INFINITY;
   const int rows = rows_in_use(a), keys = keys_in_use(a);
   if (tile * f.qpt >= rows) return;
   row.ok = row.ok && row.i < rows;
   const FewKeys fk = few_keys(f, row, stored, split, keys, &t0);
-#pragma unroll
-  for (int c = 0; c < DHP / 2; c++) D = fmaf(qf[c], dof[c], D);
   D = half_sum(D);
   if (split == 0 && wv == 0 && half == 0 && row.ok) a.dvec[srow] = D;
-  load_row<DHP>((const float*)a.q + qrow, row.ok, a.dh, half, a.scale, qf);
+  __syncthreads();
   f32x16 acc[DHP / 32] = {};
   for (int t = fk.live_from(t0 + wv, NW); t < fk.t1; t = fk.live_from(t + NW, NW)) {
     const int kv = fk.first + t * 32, jc = min(kv + (lane & 31), fk.end - 1);
-    f32x16 s = scores<DHP>(k + (i64)jc * a.ldk, a.dh, half, qf);
-    const f32x16 dp = scores<DHP>(v + (i64)jc * a.ldv, a.dh, half, dof);
+    f32x16 s, dp;
+    scores2<DHP>(s, dp, k + (i64)jc * a.ldk, v + (i64)jc * a.ldv, a.dh, half, [&](int c) { return qf[c * 64 + lane]; }, [&](int c) { return dof[c * 64 + lane]; });
+    Columns<DHP> first;
+    first.load(k, a.ldk, a.dh, kv, fk.end - 1, lane, 0);
 #pragma unroll
     for (int e = 0; e < 16; e++) {
       const int j = kv + elem_row(e, half);
@@ -154,8 +223,9 @@ template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) 
       const float x = range_score<CAP>(s[e], a.cap, slope, at, j, &keep);
       s[e] = j >= fk.r.x && j < fk.r.y && L != -INFINITY ? expf(x - L) * (dp[e] - D) * keep : 0.f;
     }
-    accumulate<DHP>(acc, k, a.ldk, a.dh, kv, fk.end - 1, s, lane);
+    accumulate<DHP>(acc, first, k, a.ldk, a.dh, kv, fk.end - 1, s, lane);
   }
+  __syncthreads();                                   // (the results lie where the operands were)
   spill<DHP>(sm + wv * DHP * 32, acc, lane);
   __syncthreads();
   const FewRow mine = few_row(a, f, tile, head, threadIdx.x & 31, rows);
@@ -196,16 +266,27 @@ template <int DHP> __global__ void __launch_bounds__(256) range_dq_sum_f32_k(Ran
   for (int c = 0; c < C; c++) if (lane * C + c < a.dh) dq[lane * C + c] = v[c] * a.scale;
 }
 // dK, dV of 32 keys of a key head: the waves share out the blocks of 32 queries that see some of them, of every head that shares it.
-template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) range_dkv_f32_k(RangeAttn a, const BlockSeen* __restrict__ blocks, float* __restrict__ sums, int parts) {
-  extern __shared__ float sm[];                      // NW results [DHP][32], then 5 x 32 words per wave
+template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64, 2) range_dkv_f32_k(RangeAttn a, const BlockSeen* __restrict__ blocks, float* __restrict__ sums, int parts) {
+  extern __shared__ float sm[];                      // K and V of the keys, later NW results [DHP][32]; then 5 x 32 words per wave
   const int per = a.Hkv * parts, kt = (int)blockIdx.x / per, r0 = (int)blockIdx.x - kt * per, kh = r0 % a.Hkv, part = r0 / a.Hkv, k0 = kt * 32;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, myk = k0 + (lane & 31);
   float* words = sm + NW * DHP * 32 + wv * 160;
-  float kf[DHP / 2], vf[DHP / 2];
-  load_row<DHP>((const float*)a.k + (i64)myk * a.ldk + (i64)kh * a.dh, myk < a.Tk, a.dh, half, a.scale, kf);
-  load_row<DHP>((const float*)a.v + (i64)myk * a.ldv + (i64)kh * a.dh, myk < a.Tk, a.dh, half, 1.f, vf);
+  // the keys' operands, the same for all waves: chunk c of lane l at [c][l], which costs LDS reads but the registers of two waves per SIMD
+  f32x4 *kf = (f32x4*)sm, *vf = kf + DHP / 8 * 64;
+#pragma unroll
+  for (int c = wv; c < DHP / 8; c += NW) {
+    const int col = c * 8 + half * 4;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
+    if (myk < a.Tk && col < a.dh) {
+      x = *(const f32x4*)((const float*)a.k + (i64)myk * a.ldk + (i64)kh * a.dh + col);
+      y = *(const f32x4*)((const float*)a.v + (i64)myk * a.ldv + (i64)kh * a.dh + col);
+    }
+    kf[c * 64 + lane] = x * a.scale;
+    vf[c * 64 + lane] = y;
+  }
   const int rows = rows_in_use(a), keys = keys_in_use(a);
   if (k0 >= keys) return;
+  __syncthreads();
   f32x16 dka[DHP / 32] = {}, dva[DHP / 32] = {};
   const int nb = (rows + 63) / 64;
   int n = part * NW + wv;                            // this wave's next one of the pairs of a block, 2 G to a block
@@ -232,8 +313,10 @@ template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) 
         }
         wave_lds_fence();
         const float *q = (const float*)a.q + (i64)h * a.dh, *d_o = (const float*)a.d_o + (i64)h * a.dh;
-        f32x16 s = scores<DHP>(q + (i64)ic * a.ldq, a.dh, half, kf);
-        f32x16 dp = scores<DHP>(d_o + (i64)ic * a.ldo, a.dh, half, vf);
+        f32x16 s, dp;
+        scores2<DHP>(s, dp, q + (i64)ic * a.ldq, d_o + (i64)ic * a.ldo, a.dh, half, [&](int c) { return kf[c * 64 + lane]; }, [&](int c) { return vf[c * 64 + lane]; });
+        Columns<DHP> first;
+        first.load(d_o, a.ldo, a.dh, q0, rows - 1, lane, 0);
         const float slope = a.slopes ? a.slopes[h] : 0.f;
 #pragma unroll
         for (int e = 0; e < 16; e++) {
@@ -245,12 +328,14 @@ template <int DHP, int NW, bool CAP> __global__ void __launch_bounds__(NW * 64) 
           dp[e] = sees ? p * (dp[e] - words[32 + x]) * keep : 0.f;
           s[e] = sees ? p : 0.f;
         }
-        accumulate<DHP>(dva, d_o, a.ldo, a.dh, q0, rows - 1, s, lane);
-        accumulate<DHP>(dka, q, a.ldq, a.dh, q0, rows - 1, dp, lane);
+        accumulate<DHP>(dva, first, d_o, a.ldo, a.dh, q0, rows - 1, s, lane);
+        first.load(q, a.ldq, a.dh, q0, rows - 1, lane, 0);
+        accumulate<DHP>(dka, first, q, a.ldq, a.dh, q0, rows - 1, dp, lane);
       }
       n -= 2 * a.G;
     }
   }
+  __syncthreads();                                   // (the results lie where the keys were)
   const int r = k0 + (int)(threadIdx.x & 31);
   if (parts > 1) {
     float* row = sums + ((((i64)part * 2) * a.Tk + r) * a.Hkv + kh) * DHP;
