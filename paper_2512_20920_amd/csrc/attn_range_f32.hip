@@ -6,7 +6,7 @@
 // precision, and keys and values are read from memory as operands directly: K 16 bytes of its own row per lane, V a row of 32
 // consecutive columns per half.  32 rows (keys) per workgroup, tiles of 32 shared out to the waves.
 // Bound by the matrix pipe's 64 clocks per instruction and, in small calls, the chain of loads around them: 2048 rows x 16 heads of 128
-// (documents of 1500 and 548) 201, 302 and 416 us, 50 to 52 of the 154 TFLOP/s of a large float32 product; 751 x 4 of 64: 13, 19, 24.
+// (documents of 1500 and 548) 167, 229 and 328 us, 62 to 68 of the 154 TFLOP/s of a large float32 product; 751 x 4 of 64: 13, 19, 23.
 #include "attn_range_few.h"
 
 typedef __attribute__((ext_vector_type(16))) float f32x16;
@@ -411,10 +411,10 @@ template <int DHP, int NW, bool CAP> static void bwd(const RangeAttn& a, void* b
                      (const BlockSeen*)blocks, sums, parts);
   sum_parts<float, DHP>(a, sums, parts, s);
 }
-// 8 waves per workgroup; 128 columns take more registers than 8 waves leave each
 #define BY_FORM(call)                                                  \
   do {                                                                 \
-    if (a.dh <= 64) { if (a.cap > 0.f) call(64, 8, true); else call(64, 8, false); } \
+    if (a.dh <= 64 && few_waves(a) == 8) { if (a.cap > 0.f) call(64, 8, true); else call(64, 8, false); } \
+    else if (a.dh <= 64) { if (a.cap > 0.f) call(64, 4, true); else call(64, 4, false); } \
     else if (a.cap > 0.f) call(128, 4, true);                          \
     else call(128, 4, false);                                          \
   } while (0)

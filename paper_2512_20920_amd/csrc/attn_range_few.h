@@ -226,7 +226,23 @@ template <class T, int DHP> static void sum_parts(const RangeAttn& a, const floa
   if (parts > 1) hipLaunchKernelGGL((range_dkv_sum_k<T, DHP>), dim3((unsigned)cdiv((i64)a.Tk * a.Hkv, 4)), dim3(256), 0, s, a, sums, parts);
 }
 
-inline int few_waves(const RangeAttn& a) { return a.dt == 0 && a.dh <= 64 ? 8 : 4; }      // of a workgroup
+// Waves of a workgroup: four; eight in float32 with heads of 64, whose registers allow it, unless even the splits of the keys leave half of
+// the CUs without a workgroup: then the work had better go to more CUs' matrix pipes.  Training step of float32, four -> eight, us: 250 rows x 4
+// heads (32 workgroups) 47 -> 56, 400 x 4 (52, in two) 57 -> 70, 751 x 4 (94, in two) 67 -> 64, 1000 x 4 (126, in two) 87 -> 97, 1500 x 8 281 -> 201,
+// 4000 x 4 752 -> 537; five single tokens against 16500 keys 20.8 -> 19.3.
+inline i64 few_splits(const RangeAttn& a, i64 workgroups, int waves) {
+  const i64 most = cdiv(a.Tk, 32 * waves), n = workgroups ? 2048 / waves / workgroups : 1;
+  return n < most ? (n < 64 ? n : 64) : (most < 64 ? most : 64);
+}
+inline i64 few_workgroups(const RangeAttn& a) {
+  const int gp = a.G < 32 ? a.G : 32;
+  return (i64)cdiv(a.Tq, 32 / gp) * a.Hkv * cdiv(a.G, gp);
+}
+inline int few_waves(const RangeAttn& a) {
+  if (a.dt != 0 || a.dh > 64) return 4;
+  const i64 workgroups = few_workgroups(a), n = few_splits(a, workgroups, 8);
+  return workgroups * (n < 1 ? 1 : n) < 128 ? 4 : 8;
+}
 // Workgroups that give every CU eight waves, of a tile of keys per wave at least.  A second launch costs 4 us and more, so few splits
 // don't pay in bfloat16: 600 rows x 12 heads of 128 whole 13.2 us, in two 15.9 + 5.7; 1000 x 8 of 64 10.6, 11 + 4.9.  Float32, whose products take
 // eight times as long: 751 x 4 of 64 whole 19.4, in two 13.4 + 4.1.
@@ -234,14 +250,11 @@ inline FewShape few_shape(const RangeAttn& a, float* work) {
   const int waves = few_waves(a);
   FewShape f;
   f.gp = a.G < 32 ? a.G : 32;
-  f.hb = (a.G + f.gp - 1) / f.gp;
+  f.hb = cdiv(a.G, f.gp);
   f.qpt = 32 / f.gp;
   f.inv = (65536 + f.gp - 1) / f.gp;
   f.tiles = cdiv(a.Tq, f.qpt);
-  const i64 workgroups = (i64)f.tiles * a.Hkv * f.hb, most = cdiv(a.Tk, 32 * waves);
-  i64 n = workgroups ? 2048 / waves / workgroups : 1;
-  if (n > most) n = most;
-  if (n > 64) n = 64;
+  const i64 n = few_splits(a, few_workgroups(a), waves);
   f.splits = n < (a.dt == 0 ? 2 : 4) ? 1 : (int)n;
   f.stats = (float2*)work;
   f.part = work ? work + 2 * (i64)a.Tq * a.H * f.splits : nullptr;
