@@ -348,8 +348,8 @@ int revffn_op_attention_bwd_noalloc(int32_t dtype, int32_t kernel_mode, const vo
  *
  * Which keys a query sees.  Query row i sees the key rows lo[i] <= j < hi[i] (clamped to 0 .. Tk; lo >= hi: none).  Documents
  * that lie one behind the other, causal order, a prefix that everybody sees and a sliding window are all such ranges;
- * revffn_op_attention_ranges writes them, or the caller does.  A query that sees nothing gets o = 0, lse = -inf and dq = 0;
- * a key that nobody sees gets dk = dv = 0.  What lies outside a query's range never reaches its results, not even an
+ * revffn_op_attention_ranges writes them, or the caller does.  A query that sees nothing, or whose scores are all -infinity,
+ * gets o = 0, lse = -inf and dq = 0 and adds nothing to dk and dv; a key that nobody sees gets dk = dv = 0.  What lies outside a query's range never reaches its results, not even an
  * infinity or a NaN (a tile that holds one is then worked out again row by row, which is slow). */
 typedef struct revffn_attn_mask {
   const int32_t *lo, *hi;  /* device [Tq]                                                            */

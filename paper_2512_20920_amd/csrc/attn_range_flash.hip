@@ -365,7 +365,9 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen*
   T::load_frags((const bf16*)a.q + (i64)myq * a.ldq + (i64)h * a.dh, myq < rows, a.dh, g, qf);
   T::load_frags((const bf16*)a.d_o + (i64)myq * a.ldo + (i64)h * a.dh, myq < rows, a.dh, g, dof);
   float mylse = myq < rows ? a.lse[(i64)h * a.Tq + myq] * LOG2E : 0.f;
-  if (mylse == -INFINITY) mylse = 0.f;              // (sees nothing: every score is -infinity)
+  // no sum: it sees nothing, or every score is -infinity, from keys that may hold infinities themselves (times a zero probability)
+  bool partly = __any(mylse == -INFINITY && mine.x < mine.y);
+  if (mylse == -INFINITY) mylse = 0.f;
   float myD = 0.f;
   {
     bf16x8 of[T::KK];
@@ -385,7 +387,6 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dq_k(RangeAttn a, BlockSeen*
   f32x16 acc[T::DT] = {}, s[2], dp[2];
   bf16x8 dsf[4], first[T::DT];
   bf16x8 fr[2][4];
-  bool partly = false;
   auto read_kv = [&](bf16x8 (&f)[4], unsigned sk, unsigned sv, int kk) {
     const unsigned char *cK = smem_raw + sk * T::BYTES, *cV = smem_raw + sv * T::BYTES;
     const unsigned w = rbase ^ (unsigned)(kk * 32);
@@ -605,10 +606,10 @@ __global__ void __launch_bounds__(256, 2) range_bwd_dkv_k(RangeAttn a, const Blo
     if (blk >= 0) issue(blk, hg, cur ^ 1);
     if (seen.x < kw + 32 && seen.y > kw) {          // some query of the block sees some key of this wave
       const bool whole = seen.z <= kw && seen.w >= kw + 32;
-      if (!whole) partly = true;
       const ScoreForm sf = score_form(a, h);
       const unsigned char *cQ = smem_raw + cur * DKV_STAGE<DHP>, *cO = cQ + T::BYTES;
       const float *cL = (const float*)(cO + T::BYTES), *cD = cL + 64;
+      if (!whole || __any(cL[lane_now()] == -INFINITY)) partly = true;      // (a query whose scores are all -infinity: exp(-inf + inf) here)
       const int *cLo = (const int*)(cD + 64), *cHi = cLo + 64, *cAt = cHi + 64;
 #pragma unroll 1
       for (int j = 0; j < 2; j++) {

@@ -313,6 +313,30 @@ def test_attention_not_finite_where_it_is_seen(mode, dtype):
 
 
 @FORMS
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("where", ["q", "k"])
+def test_attention_queries_whose_scores_are_all_minus_infinity(where, dh, mode, dtype):
+    """Such a query counts as one that sees nothing, whole tiles of keys (queries) among them: the results are those of empty ranges."""
+    lens = [128, 320, 64]                                   # (so that blocks of queries see the tiles of keys whole)
+    lo, hi, at = ref.ranges(lens, causal=False)
+    T = sum(lens)
+    a = Attention(dtype, 4, 4, dh, T, T)
+    for h in range(4):                                      # column 0 of every head is positive: an infinity there makes no 0 * infinity
+        a.q[:, h * dh] = a.q[:, h * dh].abs() + 0.5
+        a.k[:, h * dh] = a.k[:, h * dh].abs() + 0.5
+    none = np.zeros(T, bool)
+    if where == "q":
+        none[[0, 127, 170, 300, 447, 500]] = True
+        a.q[torch.from_numpy(none).cuda(), ::dh] = float("-inf")
+    else:
+        none[128:448] = True
+        a.k[128:448, ::dh] = float("-inf")
+    a.run(lo, hi, at, mode)
+    a.check(np.where(none, 0, lo), np.where(none, 0, hi))
+    assert torch.isneginf(a.lse[:, torch.from_numpy(none).cuda()]).all()
+
+
+@FORMS
 def test_attention_same_bits_again(mode, dtype):
     lo, hi, at = ref.ranges([300, 211])
     runs = []
