@@ -31,8 +31,8 @@ template <class T, int V> __device__ __forceinline__ void store_vec(T* p, const 
 template <class T, int V, bool INTER>
 __global__ void __launch_bounds__(256) rotary_k(RotaryArgs a, int rows_wg, int units, unsigned magic) {
   extern __shared__ float2 turn[];                   // [rows_wg][dims / 2]
-  const T* __restrict__ x = (const T*)a.x;
-  T* __restrict__ y = (T*)a.y;
+  const T* x = (const T*)a.x;                        // (may be y: each thread reads what it writes before it writes it)
+  T* y = (T*)a.y;
   const int half = a.dims / 2, t0 = (int)blockIdx.x * rows_wg, nt = min(rows_wg, a.T - t0);
   for (int e = threadIdx.x; e < nt * half; e += 256) {
     const int t = e / half, c = e - t * half, row = t0 + t;
