@@ -387,7 +387,8 @@ int revffn_op_attention_ranges(const int32_t *cu_q, const int32_t *cu_k, const i
 
 /* o = softmax(scores) v over each query's range; lse[H, Tq] = log of the sum of exponentials (NULL if not wanted; the
  * backward pass needs it).  q, k, v are not changed and overlap no result.  work: revffn_op_attention_masked_workspace
- * bytes.  A call of few query rows, a single token each for instance, is split along its keys and joined.
+ * bytes of this very desc: they do not grow with it, a call of fewer rows may need more (its keys are split further), so a program
+ * with several shapes asks for each and keeps the largest.  A call of few query rows, a single token each for instance, is split along its keys and joined.
  * The backward pass takes o and lse of the forward pass with the same desc and mask, and d_o; dq, dk, dv are overwritten.
  * dk and dv are summed over the query heads that share a key head.
  * REVFFN_EINVAL: a bad field, work_bytes too small.  REVFFN_ESHAPE: a row stride below the row's width, or more rows
@@ -428,7 +429,8 @@ int revffn_op_rotary(int32_t dtype, const revffn_rotary *r, const void *x, void 
  * bias (dtype, [cols]) may be NULL (1 and 0).  mean, rstd (float32 [rows]) may be NULL; the backward pass needs them.  y may be
  * x with the same stride.  Backward: dx, and the sums dgain, dbias over the rows (either may be NULL: not wanted), in
  * dtype, or float32 with grads_f32; dx may be dy with the same stride, but not x
- * (REVFFN_EINVAL).  All are overwritten.  work: revffn_op_layernorm_workspace bytes,
+ * (REVFFN_EINVAL).  All are overwritten.  work: revffn_op_layernorm_workspace bytes
+ * (of these rows and columns: more columns may need less),
  * read only if dgain or dbias is wanted.  rows = 0 is allowed (dgain = dbias = 0). */
 size_t revffn_op_layernorm_workspace(int32_t rows, int32_t cols);
 int revffn_op_layernorm_fwd(int32_t dtype, const void *x, const void *gain, const void *bias, void *y, float *mean,

@@ -462,7 +462,7 @@ def revffn_op_attention_ranges(cu_q, cu_k, prefix, n_docs, causal, window, Tq, T
 
 
 def revffn_op_attention_masked_workspace(desc, backward):
-    """Bytes of scratch memory for a forward pass, or for both (0 also for a desc that the calls refuse)."""
+    """Bytes of scratch memory for a forward pass, or for both (0 also for a desc that the calls refuse).  A desc of fewer rows may need more."""
     return load_library().revffn_op_attention_masked_workspace(ctypes.byref(desc), int(backward))
 
 

@@ -91,6 +91,21 @@ def test_attention_refuses_missing_and_small(lib):
     assert fwd(ctypes.byref(desc(kernel_mode=2)), bm, P + 2, P, P, P, P, P, 1 << 30) == EUNSUPPORTED
 
 
+def test_attention_scratch_memory_is_each_descs_own(lib):
+    """A call of fewer rows may need more of it, and a workspace that is too small for it is refused, whatever larger call it was made for."""
+    size = lambda backward, **kw: lib.revffn_op_attention_masked_workspace(ctypes.byref(desc(**kw)), backward)
+    shape = dict(H=16, Hkv=4, dh=128, Tk=32768)
+    big, small = size(0, Tq=4096, **shape), size(0, Tq=64, **shape)
+    assert big < small
+    f32 = dict(dtype=0, H=4, Hkv=2, dh=64)
+    big_b, small_b = size(1, Tq=8192, Tk=8192, **f32), size(1, Tq=2048, Tk=2048, **f32)
+    assert big_b < small_b
+    bm = ctypes.byref(R.AttnMask(P, P))
+    assert lib.revffn_op_attention_masked_fwd(ctypes.byref(desc(Tq=64, **shape)), bm, P, P, P, P, P, P, big, None) == EINVAL
+    assert lib.revffn_op_attention_masked_bwd(ctypes.byref(desc(Tq=2048, Tk=2048, **f32)), bm, *[P] * 10, big_b, None) == EINVAL
+    assert lib.revffn_op_layernorm_workspace(300, 20000) < lib.revffn_op_layernorm_workspace(300, 16384)
+
+
 def test_attention_ranges_refuses(lib):
     f = lambda *a: lib.revffn_op_attention_ranges(*a, None)
     assert f(P, P, None, 2, 1, 0, 10, 10, None, P, None, None) == ENULL and f(P, P, None, 2, 1, 0, 10, 10, P, None, None, None) == ENULL
