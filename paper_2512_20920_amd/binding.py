@@ -54,6 +54,20 @@ class Merged(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in MERGED_FIELDS]
 
 
+def _run_of(count, *tensors):
+    """Refuses tensors whose elements don't lie one behind the other, or fewer than count of them; returns the shortest's number."""
+    least = 1 << 62
+    for t in tensors:
+        if t is None or type(t) is int:
+            continue
+        if not t.is_contiguous():
+            raise RevffnError(f"strides {t.stride()} of an array that is read as one run of elements")
+        least = min(least, t.numel())
+    if least < count:
+        raise RevffnError(f"an array of {least} elements, of which {count} are used")
+    return least
+
+
 class AttnDesc(ctypes.Structure):
     """revffn_attn_desc; slopes: a float32 tensor (kept alive by this object), an address or None."""
     _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "kernel_mode", "H", "Hkv", "dh", "Tq", "Tk")] + [
@@ -62,6 +76,7 @@ class AttnDesc(ctypes.Structure):
 
     def __init__(self, slopes=None, **fields):
         super().__init__(slopes=_ptr(slopes), **fields)
+        _run_of(self.H, slopes)
         self.kept = slopes
 
 
@@ -71,6 +86,8 @@ class AttnMask(ctypes.Structure):
 
     def __init__(self, lo, hi, at=None, used=None):
         super().__init__(_ptr(lo), _ptr(hi), _ptr(at), _ptr(used))
+        _run_of(2, used)
+        self.rows = _run_of(0, lo, hi, at)          # query rows that the arrays have entries for
         self.kept = (lo, hi, at, used)
 
 
@@ -408,17 +425,20 @@ def revffn_inverse_merged(ctx, weights, merged, y1, y2, x1, x2, B, S, ld, residu
 
 
 # ---- attention over key ranges, rotary positions, layer norm ----------------------------------------------------------
-_torch = None
+_current = _stream_of = None
 
 
 def _device():
-    """torch and the current device.  (Small calls are bound by what the host does for them, so these functions look things up once.)"""
-    global _torch
-    if _torch is None:
+    """The current device.  (Small calls are bound by what the host does for them, so these functions look things up once.)"""
+    global _current, _stream_of, _I32, _F32, _BF16
+    if _current is None:
         import torch
-        _torch = torch
-    cuda = _torch.cuda
-    return _torch, cuda.current_device() if cuda.is_initialized() or cuda.is_available() else -2
+        _I32, _F32, _BF16 = torch.int32, torch.float32, torch.bfloat16
+        if not torch.cuda.is_available():
+            return -2
+        torch.cuda.init()
+        _current, _stream_of = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+    return _current()
 
 
 def _refuse(t, want):
@@ -441,10 +461,25 @@ def _addresses(device, want, *tensors):
     return out
 
 
-def _on(stream, torch, device):
+def _dense(device, want, count, *tensors):
+    """The same for arrays whose elements the call takes to lie one behind the other, `count` of them."""
+    out = []
+    for t in tensors:
+        if t is None or type(t) is int:
+            out.append(t)
+        elif t.get_device() != device or t.dtype is not want:
+            _refuse(t, want)
+        else:
+            if not t.is_contiguous() or t.numel() < count:
+                _run_of(count, t)
+            out.append(t.data_ptr())
+    return out
+
+
+def _on(stream, device):
     """The stream's handle; None: the current one of the current device."""
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(device)
+        return _stream_of(device)
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -452,13 +487,18 @@ def _work(device, work):
     """(address, bytes) of a workspace tensor or None."""
     if work is None:
         return None, 0
+    if not work.is_contiguous():
+        _run_of(0, work)
     return _addresses(device, None, work)[0], work.numel() * work.element_size()
 
 
 def revffn_op_attention_ranges(cu_q, cu_k, prefix, n_docs, causal, window, Tq, Tk, lo, hi, at=None, used=None, stream=None):
-    torch, dev = _device()
-    q, k, p, l, h, a, u = _addresses(dev, torch.int32, cu_q, cu_k, prefix, lo, hi, at, used)
-    _check(load_library().revffn_op_attention_ranges(q, k, p, n_docs, int(causal), window, Tq, Tk, l, h, a, u, _on(stream, torch, dev)))
+    dev = _device()
+    q, k = _dense(dev, _I32, n_docs + 1, cu_q, cu_k)
+    p, = _dense(dev, _I32, n_docs, prefix)
+    l, h, a = _dense(dev, _I32, Tq, lo, hi, at)
+    u, = _dense(dev, _I32, 2, used)
+    _check(load_library().revffn_op_attention_ranges(q, k, p, n_docs, int(causal), window, Tq, Tk, l, h, a, u, _on(stream, dev)))
 
 
 def revffn_op_attention_masked_workspace(desc, backward):
@@ -466,27 +506,25 @@ def revffn_op_attention_masked_workspace(desc, backward):
     return load_library().revffn_op_attention_masked_workspace(ctypes.byref(desc), int(backward))
 
 
-def _element(torch, dtype):
-    return torch.bfloat16 if dtype == 1 else torch.float32
-
-
 def _attention_operands(desc, mask, *typed):
-    torch, dev = _device()
-    _addresses(dev, torch.float32, desc.kept)
-    _addresses(dev, torch.int32, *mask.kept)
-    return torch, dev, _addresses(dev, _element(torch, desc.dtype), *typed)
+    dev = _device()
+    _addresses(dev, _F32, desc.kept)
+    _addresses(dev, _I32, *mask.kept)
+    if mask.rows < desc.Tq:
+        raise RevffnError(f"a mask of {mask.rows} query rows, of which {desc.Tq} are used")
+    return dev, _addresses(dev, _BF16 if desc.dtype == 1 else _F32, *typed)
 
 
 def revffn_op_attention_masked_fwd(desc, mask, q, k, v, o, lse, work=None, stream=None):
-    torch, dev, p = _attention_operands(desc, mask, q, k, v, o)
-    _check(load_library().revffn_op_attention_masked_fwd(ctypes.byref(desc), ctypes.byref(mask), *p, *_addresses(dev, torch.float32, lse),
-                                                         *_work(dev, work), _on(stream, torch, dev)))
+    dev, p = _attention_operands(desc, mask, q, k, v, o)
+    _check(load_library().revffn_op_attention_masked_fwd(ctypes.byref(desc), ctypes.byref(mask), *p, *_dense(dev, _F32, desc.H * desc.Tq, lse),
+                                                         *_work(dev, work), _on(stream, dev)))
 
 
 def revffn_op_attention_masked_bwd(desc, mask, q, k, v, o, d_o, lse, dq, dk, dv, work=None, stream=None):
-    torch, dev, p = _attention_operands(desc, mask, q, k, v, o, d_o, dq, dk, dv)
-    _check(load_library().revffn_op_attention_masked_bwd(ctypes.byref(desc), ctypes.byref(mask), *p[:5], *_addresses(dev, torch.float32, lse),
-                                                         *p[5:], *_work(dev, work), _on(stream, torch, dev)))
+    dev, p = _attention_operands(desc, mask, q, k, v, o, d_o, dq, dk, dv)
+    _check(load_library().revffn_op_attention_masked_bwd(ctypes.byref(desc), ctypes.byref(mask), *p[:5], *_dense(dev, _F32, desc.H * desc.Tq, lse),
+                                                         *p[5:], *_work(dev, work), _on(stream, dev)))
 
 
 def revffn_op_rotary_frequencies(rotary):
@@ -498,10 +536,10 @@ def revffn_op_rotary_frequencies(rotary):
 
 
 def revffn_op_rotary(dtype, rotary, x, y, pos, T, S, H, dh, ldx, ldy, transposed=False, stream=None):
-    torch, dev = _device()
-    px, py = _addresses(dev, _element(torch, dtype), x, y)
-    _check(load_library().revffn_op_rotary(dtype, ctypes.byref(rotary), px, py, *_addresses(dev, torch.int32, pos), T, S, H, dh, ldx, ldy,
-                                           int(transposed), _on(stream, torch, dev)))
+    dev = _device()
+    px, py = _addresses(dev, _BF16 if dtype == 1 else _F32, x, y)
+    _check(load_library().revffn_op_rotary(dtype, ctypes.byref(rotary), px, py, *_dense(dev, _I32, T, pos), T, S, H, dh, ldx, ldy,
+                                           int(transposed), _on(stream, dev)))
 
 
 def revffn_op_layernorm_workspace(rows, cols):
@@ -509,16 +547,20 @@ def revffn_op_layernorm_workspace(rows, cols):
 
 
 def revffn_op_layernorm_fwd(dtype, x, gain, bias, y, mean, rstd, rows, cols, ldx, ldy, eps, stream=None):
-    torch, dev = _device()
-    _check(load_library().revffn_op_layernorm_fwd(dtype, *_addresses(dev, _element(torch, dtype), x, gain, bias, y),
-                                                  *_addresses(dev, torch.float32, mean, rstd), rows, cols, ldx, ldy, eps,
-                                                  _on(stream, torch, dev)))
+    dev = _device()
+    t = _BF16 if dtype == 1 else _F32
+    px, py = _addresses(dev, t, x, y)
+    _check(load_library().revffn_op_layernorm_fwd(dtype, px, *_dense(dev, t, cols, gain, bias), py,
+                                                  *_dense(dev, _F32, rows, mean, rstd), rows, cols, ldx, ldy, eps,
+                                                  _on(stream, dev)))
 
 
 def revffn_op_layernorm_bwd(dtype, dy, x, gain, mean, rstd, dx, dgain, dbias, rows, cols, lddy, ldx, lddx, grads_f32=False, work=None,
                             stream=None):
-    torch, dev = _device()
-    dyp, xp, gp, dxp = _addresses(dev, _element(torch, dtype), dy, x, gain, dx)
-    grads = _addresses(dev, torch.float32 if grads_f32 else _element(torch, dtype), dgain, dbias)
-    _check(load_library().revffn_op_layernorm_bwd(dtype, dyp, xp, gp, *_addresses(dev, torch.float32, mean, rstd), dxp, *grads, rows, cols,
-                                                  lddy, ldx, lddx, int(grads_f32), *_work(dev, work), _on(stream, torch, dev)))
+    dev = _device()
+    t = _BF16 if dtype == 1 else _F32
+    dyp, xp, dxp = _addresses(dev, t, dy, x, dx)
+    gp, = _dense(dev, t, cols, gain)
+    grads = _dense(dev, _F32 if grads_f32 else t, cols, dgain, dbias)
+    _check(load_library().revffn_op_layernorm_bwd(dtype, dyp, xp, gp, *_dense(dev, _F32, rows, mean, rstd), dxp, *grads, rows, cols,
+                                                  lddy, ldx, lddx, int(grads_f32), *_work(dev, work), _on(stream, dev)))

@@ -560,6 +560,40 @@ def test_tensors_of_another_type_are_refused():
         R.revffn_op_rotary(1, R.Rotary(dims=64, theta=1e4), b, b.cpu(), None, 1, 1, 1, 64, 64, 64)
 
 
+def test_arrays_with_strides_or_too_few_elements_are_refused():
+    """Ranges as columns of one table, for instance, would be read as something else; every array that has no stride argument."""
+    T, H, dh = 6, 2, 64
+    bf, f32 = (lambda *s: torch.zeros(s, dtype=torch.bfloat16, device="cuda")), (lambda *s: torch.zeros(s, device="cuda"))
+    ints = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")
+    q, lse, work = bf(T, H * dh), f32(H, T), torch.zeros(1 << 20, dtype=torch.uint8, device="cuda")
+    r = R.Rotary(dims=64, theta=1e4)
+
+    def ranges(cu=ints(3), pre=ints(2), lo=ints(T), hi=ints(T), at=ints(T), used=ints(2)):
+        R.revffn_op_attention_ranges(cu, cu, pre, 2, True, 0, T, T, lo, hi, at, used)
+
+    def attention(lo=ints(T), hi=ints(T), at=ints(T), used=ints(2), slopes=f32(H), lse=lse, work=work):
+        d, m = R.AttnDesc(dtype=1, H=H, Hkv=H, dh=dh, Tq=T, Tk=T, slopes=slopes), R.AttnMask(lo, hi, at, used)
+        R.revffn_op_attention_masked_fwd(d, m, q, q, q, bf(T, H * dh), lse, work)
+        R.revffn_op_attention_masked_bwd(d, m, q, q, q, q, q, lse, bf(T, H * dh), bf(T, H * dh), bf(T, H * dh), work)
+
+    def rotary(pos=ints(T)):
+        R.revffn_op_rotary(1, r, q, bf(T, H * dh), pos, T, T, H, dh, H * dh, H * dh)
+
+    def norm(gain=bf(H * dh), bias=bf(H * dh), mean=f32(T), rstd=f32(T), dgain=bf(H * dh), dbias=bf(H * dh), work=work):
+        R.revffn_op_layernorm_fwd(1, q, gain, bias, bf(T, H * dh), mean, rstd, T, H * dh, H * dh, H * dh, 1e-5)
+        R.revffn_op_layernorm_bwd(1, q, q, gain, mean, rstd, bf(T, H * dh), dgain, dbias, T, H * dh, H * dh, H * dh, H * dh, False, work)
+    for call in (ranges, attention, rotary, norm):
+        call()
+        torch.cuda.synchronize()
+        for name, t in zip(call.__code__.co_varnames, call.__defaults__):
+            wide = torch.zeros(*t.shape, 2, dtype=t.dtype, device="cuda")[..., 0]
+            with pytest.raises(R.RevffnError, match="strides"):
+                call(**{name: wide})
+            with pytest.raises(R.RevffnError):
+                call(**{name: t.flatten()[:1]})
+    torch.cuda.synchronize()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("interleaved", [False, True])
 # T, H, dh, dims, extra columns in a row, scaling

@@ -181,6 +181,23 @@ def test_tensors_that_no_gpu_may_read_are_refused():
         R.binding._refuse(t, torch.float32)
 
 
+def test_arrays_with_strides_or_too_few_elements_are_refused():
+    torch = pytest.importorskip("torch")
+    dense = R.binding._dense
+    table = torch.zeros(6, 2, dtype=torch.int32)
+    assert dense(-1, torch.int32, 12, table, None, 4096) == [table.data_ptr(), None, 4096]
+    with pytest.raises(R.RevffnError, match="strides"):
+        dense(-1, torch.int32, 6, table[:, 0])
+    with pytest.raises(R.RevffnError, match="12 elements"):
+        dense(-1, torch.int32, 13, table)
+    with pytest.raises(R.RevffnError, match="float32"):
+        dense(-1, torch.float32, 1, table)
+    with pytest.raises(R.RevffnError, match="device"):
+        dense(0, torch.int32, 1, table)
+    with pytest.raises(R.RevffnError, match="strides"):
+        R.binding._work(-1, torch.zeros(8, 8, dtype=torch.uint8)[:, :4])
+
+
 @pytest.mark.parametrize("cap,bias", [(0.0, False), (2.0, False), (0.0, True), (3.0, True)])
 def test_reference_gradients_are_differences(cap, bias):
     """The gradients that the kernels are compared with, against central differences of the forward reference."""
