@@ -312,6 +312,64 @@ def test_attention_not_finite_where_it_is_seen(mode, dtype):
     assert np.isfinite(dk[:100]).all() and np.isfinite(dk[:, 1]).all()
 
 
+def _check_in_parts(a, lo, hi, at=None, cap=0.0, slopes=None, rows=64):
+    """Attention.check for many rows: `rows` queries at a time against the keys that they see.  (Errors of dk's and dv's parts add up.)"""
+    lo, hi, at = np.asarray(lo), np.asarray(hi), np.arange(len(lo)) if at is None else np.asarray(at)
+    q, k, v, do = (a.part(x) for x in ("q", "k", "v", "do"))
+    want = {n: [np.zeros(shape), np.zeros(shape)] for n, shape in (("o", q.shape), ("dq", q.shape), ("dk", k.shape), ("dv", k.shape))}
+    want["lse"] = [np.full((a.H, a.Tq), -np.inf), np.zeros((a.H, a.Tq))]
+    for i in range(0, a.Tq, rows):
+        r = slice(i, min(i + rows, a.Tq))
+        some = lo[r] < hi[r]
+        if not some.any():
+            continue
+        c = slice(lo[r][some].min(), hi[r][some].max())
+        part = ref.attention(q[r], k[c], v[c], np.maximum(lo[r] - c.start, 0), hi[r] - c.start, at[r] - c.start, cap=cap, slopes=slopes, do=do[r], dtype=a.dtype)
+        for j in range(2):
+            for name in ("o", "dq"):
+                want[name][j][r] = part[name][j]
+            want["lse"][j][:, r] = part["lse"][j]
+            for name in ("dk", "dv"):
+                want[name][j][c] += part[name][j]
+    got = {n: a.part(n) for n in ("o", "dq", "dk", "dv")} | {"lse": _np(a.lse[:, : a.Tq])}
+    worst = {name: ref.outside(got[name], *want[name]) for name in got}
+    assert max(worst.values()) <= 1.0, worst
+
+
+BY_SIZE = pytest.mark.parametrize("dtype,mode", [("bf16", 0), ("bf16", 256), ("bf16", 512), ("f32", 0)])
+
+
+@BY_SIZE
+@pytest.mark.parametrize("H,Hkv,dh,cap", [(2, 2, 64, 0.0), (3, 1, 64, 0.0), (4, 1, 128, 0.0), (6, 2, 128, 20.0)])
+def test_attention_keys_seen_from_far_apart_blocks(H, Hkv, dh, cap, mode, dtype):
+    """More than 64 blocks of 64 queries.  Each query sees some hundred keys, its own neighbours or, a few whole blocks of queries, the first ones: a block
+    that is left out or taken twice is a large part of a key's gradients."""
+    n = 4700
+    i = np.arange(n)
+    lo, hi = np.maximum(i - 100, 0), i + 1
+    first = np.isin(i // 64, [30, 63, 64, 66, 70, 73])
+    lo[first], hi[first] = 0, 50 + i[first] % 13
+    a = Attention(dtype, H, Hkv, dh, n, n)
+    a.run(lo, hi, None, mode, cap=cap)
+    _check_in_parts(a, lo, hi, cap=cap)
+
+
+# rows, heads, key heads, width: which form each kernel takes goes by these, on both sides of each line and with the forms of dq and of dk, dv apart;
+# 1500 x 32: between 256 and 512 workgroups in the form for many rows, whose second 256 take their tiles in the other order
+@BY_SIZE
+@pytest.mark.parametrize("T,H,Hkv,dh", [(1500, 32, 32, 64), (1500, 32, 32, 128), (2048, 16, 16, 128), (2049, 16, 16, 128), (3000, 16, 8, 128), (2000, 16, 4, 64),
+                                        (4500, 16, 16, 64), (3000, 24, 8, 64)])
+def test_attention_sizes_around_the_lines(T, H, Hkv, dh, mode, dtype):
+    rng = np.random.default_rng(T + H)
+    lens = []
+    while sum(lens) < T:
+        lens.append(min(int(rng.integers(1, 200)), T - sum(lens)))
+    lo, hi, at = ref.ranges(lens)
+    a = Attention(dtype, H, Hkv, dh, T, T)
+    a.run(lo, hi, at, mode)
+    _check_in_parts(a, lo, hi, at)
+
+
 @FORMS
 @pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("where", ["q", "k"])
@@ -700,6 +758,41 @@ def test_layernorm(rows, cols, pad, params, dtype):
     R.revffn_op_layernorm_fwd(dt, x2, gain, bias, x2, None, None, rows, cols, ld, ld, 1e-5)
     torch.cuda.synchronize()
     assert torch.equal(x2[:, :cols], y[:, :cols]) and torch.equal(dy2[:, :cols], dx[:, :cols])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+# rows, columns, extra columns in a row: three rows and more for a workgroup (wave), not as many for each; a line of columns per form of the kernel
+@pytest.mark.parametrize("rows,cols,pad", [(9001, 256, 0), (12301, 509, 0), (4500, 1000, 0), (6601, 777, 1), (2600, 2048, 0), (3333, 1500, 4), (2600, 2047, 0),
+                                           (1100, 4096, 0), (1600, 2300, 0), (1100, 4001, 0), (1100, 4104, 0), (1030, 8190, 2), (530, 8200, 0), (800, 16001, 0),
+                                           (70, 16392, 0), (131, 20001, 3)])
+def test_layernorm_backward_of_many_rows(rows, cols, pad, dtype):
+    """x and dy whole numbers, mean 0 and rstd 1: the sums over the rows are whole numbers below 2^24, which float32 adds without error in any order, so a
+    row that is left out, taken twice or mixed up with the next one shows.  In place as well."""
+    rng = np.random.default_rng(rows + cols)
+    whole = lambda top: torch.from_numpy(rng.integers(-top, top + 1, (rows, cols + pad)).astype(np.float32)).to(TORCH[dtype]).cuda()
+    x, dy = whole(8), whole(6)
+    mean, rstd = torch.zeros(rows, device="cuda"), torch.ones(rows, device="cuda")
+    xn, d = _np(x[:, :cols]), _np(dy[:, :cols])
+    s, q = d.mean(1, keepdims=True), (d * xn).mean(1, keepdims=True)
+    want = d - s - xn * q
+    # s and q are exact sums divided once: half a step of each, of x q and of the two differences
+    e = 2.0 ** -24
+    bound = 4 * e * (np.abs(d) + np.abs(s) + np.abs(xn * q)) + HALF_STEP[dtype] * np.abs(want)
+    dt, ld = (1 if dtype == "bf16" else 0), cols + pad
+    results = []
+    for in_place in (False, True):
+        dx = dy.clone() if in_place else torch.full_like(dy, NAN)
+        dgain, dbias = (torch.full((cols,), NAN, device="cuda") for _ in range(2))
+        work = torch.full((R.revffn_op_layernorm_workspace(rows, cols),), 255, dtype=torch.uint8, device="cuda")
+        R.revffn_op_layernorm_bwd(dt, dx if in_place else dy, x, None, mean, rstd, dx, dgain, dbias, rows, cols, ld, ld, ld, True, work)
+        torch.cuda.synchronize()
+        assert (_np(dgain) == (d * xn).sum(0)).all() and (_np(dbias) == d.sum(0)).all()
+        assert ref.outside(_np(dx[:, :cols]), want, bound) <= 1.0
+        results.append(dx[:, :cols].clone())
+    dx = torch.full_like(dy, NAN)
+    R.revffn_op_layernorm_bwd(dt, dy, x, None, mean, rstd, dx, None, None, rows, cols, ld, ld, ld)
+    torch.cuda.synchronize()
+    assert all(torch.equal(dx[:, :cols], r) for r in results) and (pad == 0 or torch.isnan(dx[:, cols:]).all())
 
 
 def test_layernorm_without_rows():
