@@ -312,6 +312,28 @@ def test_attention_not_finite_where_it_is_seen(mode, dtype):
     assert np.isfinite(dk[:100]).all() and np.isfinite(dk[:, 1]).all()
 
 
+@pytest.mark.parametrize("mode", [256, 512])
+@pytest.mark.parametrize("dh", [64, 128])
+# root mean square errors as multiples of those of the float64 result rounded once to its type; the lines lie between what three seeds of these
+# inputs give with a correction and without it:
+#   biased: 16 bits of dS and the sum of dS in D: dq 1.08..1.14, 1.48..1.52 without
+#   short: D summed from the tile that holds all keys of a query: dq, dk 1.39..1.50, 1.63..1.76 without
+#   capped: the forward pass's tanh from a polynomial (float32 lse): 1.67..1.90, 3.99..4.56 without
+@pytest.mark.parametrize("kind,names,most", [("biased", ("dq",), 1.3), ("short", ("dq", "dk"), 1.57), ("capped", ("lse",), 2.75)])
+def test_attention_errors_stay_near_a_single_rounding(kind, names, most, dh, mode):
+    H, Hkv, lens, opt = {"biased": (4, 2, [140, 61, 300], dict(slopes=_slopes(4))), "capped": (2, 2, [140, 61], dict(cap=30.0)),
+                         "short": (4, 2, [30, 17, 1, 25, 9, 3, 31, 12, 28, 5, 22, 16, 2, 30, 19], {})}[kind]
+    lo, hi, at = ref.ranges(lens)
+    a = Attention("bf16", H, Hkv, dh, sum(lens), sum(lens))
+    a.run(lo, hi, at, mode, **opt)
+    want = ref.attention(a.part("q"), a.part("k"), a.part("v"), lo, hi, at, cap=opt.get("cap", 0.0), slopes=opt.get("slopes"), do=a.part("do"))
+    for name in names:
+        x = want[name][0]
+        once = x.astype(np.float32) if name == "lse" else _np(torch.from_numpy(x).to(torch.bfloat16))
+        got = _np(a.lse) if name == "lse" else a.part(name)
+        assert np.sqrt(((got - x) ** 2).mean()) <= most * np.sqrt(((once - x) ** 2).mean()), name
+
+
 def _check_in_parts(a, lo, hi, at=None, cap=0.0, slopes=None, rows=64):
     """Attention.check for many rows: `rows` queries at a time against the keys that they see.  (Errors of dk's and dv's parts add up.)"""
     lo, hi, at = np.asarray(lo), np.asarray(hi), np.arange(len(lo)) if at is None else np.asarray(at)
