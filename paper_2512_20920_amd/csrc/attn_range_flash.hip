@@ -1075,19 +1075,31 @@ size_t range_flash_sum_floats(const RangeAttn& a) {
   const int n = dkv_parts(a) > dkv_parts_few(a) ? dkv_parts(a) : dkv_parts_few(a);
   return n > 1 ? (size_t)n * 2 * a.Tk * a.Hkv * (a.dh <= 64 ? 64 : 128) : 0;
 }
-// Which form each kernel takes; form: 0 by the rules, 1 for few rows, 2 for many.  us, many -> few:
-//   forward, query rows x heads   packed documents, 2048 x 16 of 128 (longest 730): 31.6 -> 27.0   2048 x 16, one document: 57.0 -> 57.4
-//     2111 x 12 of 64, behind 4014 keys: 50.4 -> 35.8   4000 x 8 of 64: 47.4 -> 36.4   4096 x 16, 8 documents: 29.0 -> 49.4
-//     4095 x 16 of 64, capped: 54.2 -> 49.7   2000 x 32 of 64, capped: 49.8 -> 41.6
-//   dQ   the same: 40.2 -> 33.4, 69.9 -> 61.8   4000 x 8 of 64: 54.3 -> 32.4   2000 x 32 of 64: 59.1 -> 50.7   4096 x 16 of 128: 37.5 -> 59.6
-//   dK/dV 2048 x 16 of 128: 58.0 -> 39.3, 99.5 -> 73.2   4095 x 16 (8 key heads) of 64: 85 -> 75   4096 x 16 of 128: 47.8 -> 66
-// At 32 k rows x heads the form for many has one workgroup per CU.
-static bool few_fwd(const RangeAttn& a, int form) { return form ? form == 1 : (i64)a.Tq * a.H <= (a.dh <= 64 ? 64 : 32) * 1024; }
-static bool few_dq(const RangeAttn& a, int form) { return form ? form == 1 : (i64)a.Tq * a.H <= (a.dh <= 64 ? 64 : 32) * 1024; }
-static bool few_dkv(const RangeAttn& a, int form) { return form ? form == 1 : (a.G <= 2 || (i64)a.Tk * a.Hkv <= 4 * 1024) && (i64)a.Tk * a.H <= (a.G == 1 ? 32 : 64) * 1024; }
+// Which form each kernel takes; form: 0 by the rules, 1 for few rows, 2 for many.  The lengths of the documents, which the host does not know, count as
+// much as the sizes: documents of 512 are at home in tiles of 128 at half of a line, long ones only above it.  The lines lie where the geometric mean over
+// three kinds of batch crosses 1: many / few (above 1: few rows are faster), documents of 30 to 730 rows, one document, documents of 512, heads of 128
+//   forward  1024 x 32 rows x heads 1.08 1.12 0.92   2304 x 16 1.12 1.16 0.81   5000 x 8 1.00 1.23 0.82   2560 x 16 1.02 1.10 0.84   1400 x 32 1.00 0.92 0.75
+//   dQ                              1.04 1.04 0.85             1.05 1.14 0.79            1.00 1.19 0.81             0.97 1.08 0.84             0.97 0.89 0.77
+//   dK/dV    1400 x 32 1.16 1.08 0.87   3300 x 16 1.21 1.07 0.87   6500 x 8 1.09 1.15 0.84   3700 x 16 1.07 1.02 0.85   2048 x 32 0.96 0.88 0.72
+// and of 64
+//   forward  3300 x 16 1.00 1.22 0.89   2048 x 32 1.10 0.99 0.82   4096 x 16 1.08 1.06 0.77   5400 x 16 1.18 0.91 0.90   8192 x 16 0.96 0.73 0.78
+//   dQ                 1.00 1.10 0.84             0.94 0.92 0.74             0.99 0.99 0.70             1.05 0.86 0.84             0.91 0.74 0.75
+//   (capped, the documents of 30 to 730 rows: 4095 x 16 1.33, dQ 1.20; 5400 x 16 1.45, 1.28)
+//   dK/dV    5000 x 8 1.46 1.60 0.98    2048 x 32 1.15 1.06 0.83   4096 x 16 1.18 1.13 0.79   5400 x 16 1.07 0.98 0.87   8192 x 16 0.90 0.77 0.79
+// dK/dV with heads that share a key head (128, then 64): query rows x heads / key heads
+//   2048 x 16/8 1.17 1.05 1.04, 1.14 1.10 0.95   3300 x 16/8 1.13 0.85 1.04, 1.01 0.92 1.05   4096 x 16/8 1.57 0.99, 1.28 0.92   8192 x 16/8 of 64 1.32 0.82
+//   2048 x 16/4 1.19 1.05 1.04, 1.19 1.13 1.01   1024 x 32/8 1.07 1.00, 1.04 0.98   1400 x 32/8 1.03 0.93 1.04, 1.17 0.95 1.06   6000 x 8/2 1.13 0.80, 1.14 0.86
+//   4096 x 16/1 1.66 1.70, 1.65 2.04   6000 x 16/1 1.31 1.27 1.04, 1.38 1.39 1.13   8192 x 16/1 0.94 0.94 0.75, 0.96 1.03 0.81
+static bool few_queries(const RangeAttn& a, int form) { return form ? form == 1 : (i64)a.Tq * a.H <= (a.dh <= 64 ? 64 : 36) * 1024; }
+static bool few_dkv(const RangeAttn& a, int form) {
+  if (form) return form == 1;
+  const i64 rows = (i64)a.Tk * a.H;
+  if (a.G <= 2) return rows <= (a.G == 2 || a.dh <= 64 ? 64 : 48) * 1024;
+  return (i64)a.Tk * a.Hkv <= 8 * 1024 && rows <= 96 * 1024;
+}
 
 template <int DHP, int MOD> static void bwd(const RangeAttn& a, void* blocks, float* sums, int form, hipStream_t s) {
-  const bool fq = few_dq(a, form), fkv = few_dkv(a, form);
+  const bool fq = few_queries(a, form), fkv = few_dkv(a, form);
   if (a.Tq > 0 && fq) {
     static std::atomic<unsigned long long> mask{0};
     constexpr unsigned smem = 4 * Tiles<DHP>::BYTES + 4 * 512;
@@ -1119,7 +1131,7 @@ template <int DHP, int MOD> static void bwd(const RangeAttn& a, void* blocks, fl
 }
 template <int DHP, int MOD> static void fwd(const RangeAttn& a, float* work, int form, hipStream_t s) {
   static std::atomic<unsigned long long> mask{0};
-  if (few_fwd(a, form)) {
+  if (few_queries(a, form)) {
     set_lds(mask, range_fwd_few_k<DHP, MOD>, FEW_SMEM<DHP>);
     const FewShape f = few_shape(a, work);
     hipLaunchKernelGGL((range_fwd_few_k<DHP, MOD>), dim3((unsigned)((i64)f.tiles * f.splits * a.Hkv * f.hb)), dim3(256), FEW_SMEM<DHP>, s, a, f);

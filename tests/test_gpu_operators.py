@@ -380,7 +380,7 @@ def test_attention_keys_seen_from_far_apart_blocks(H, Hkv, dh, cap, mode, dtype)
 # 1500 x 32: between 256 and 512 workgroups in the form for many rows, whose second 256 take their tiles in the other order
 @BY_SIZE
 @pytest.mark.parametrize("T,H,Hkv,dh", [(1500, 32, 32, 64), (1500, 32, 32, 128), (2048, 16, 16, 128), (2049, 16, 16, 128), (3000, 16, 8, 128), (2000, 16, 4, 64),
-                                        (4500, 16, 16, 64), (3000, 24, 8, 64)])
+                                        (4500, 16, 16, 64), (3000, 24, 8, 64), (1500, 24, 8, 64), (2600, 16, 16, 128), (1900, 9, 3, 64)])
 def test_attention_sizes_around_the_lines(T, H, Hkv, dh, mode, dtype):
     rng = np.random.default_rng(T + H)
     lens = []
