@@ -1,5 +1,5 @@
 // The forms of attention over key ranges for few rows: a workgroup takes 32 rows, which are queries of all (at most 32) heads that share
-// a key head, so that its keys are read once for all of them, and its four waves share the keys out in tiles of 32.  The keys may
+// a key head, so that its keys are read once for all of them, and its four or eight waves (few_waves) share the keys out in tiles of 32.  The keys may
 // be split further over several workgroups, whose results a second launch joins.
 #pragma once
 #include "attn_range.h"

@@ -2,9 +2,10 @@
 // with float32 arithmetic.  It serves what the matrix-core kernels don't take.  Also the ranges themselves.
 #include "attn_range.h"
 
-// One thread per query row; a document's rows are found by bisection of cu_q, of which LDS holds as much as fits, so that one load's
-// latency is paid and not one per step (7 documents, 2048 rows: 4.8 us without).
-#define CU_LDS 2048
+// One thread per query row; a document's rows are found by bisection of cu_q, from a copy in LDS where that is shorter than a bisection's loads in
+// memory: documents, rows, us with and without it, launches back to back: 7, 2048: 2.22 2.34; 100, 8192: 2.47 2.70; 1000, 65536: 3.10 3.17; 2000, 65536: 3.56
+// 3.33.  (A launch of its own between others: 4.8.)
+#define CU_LDS 1024
 __global__ void __launch_bounds__(256) attn_ranges_k(const int* __restrict__ cu_q, const int* __restrict__ cu_k, const int* __restrict__ prefix,
                                                      int n_docs, int causal, int window, int Tq, int Tk, int* __restrict__ lo, int* __restrict__ hi,
                                                      int* __restrict__ at, int* __restrict__ used) {

@@ -331,8 +331,15 @@ template <class T> __global__ void __launch_bounds__(256) layernorm_reduce_k(con
 }
 
 // Waves per row, 8-column chunks per thread and (backward) workgroups, each of which leaves partial sums of whole rows: more of them keep
-// more rows in flight, but the sums cost each some 4 KiB (2 KiB CH) of traffic twice and a few microseconds at its end.  8192 x 2048, us with
-// 256, 512, 1024: 27.4, 31.4, 40.1.
+// more rows in flight, but the sums cost each 4 KiB per wave of a row and chunk of traffic twice and a few microseconds at its end.  Backward with its sums, us,
+// by workgroups (bf16 unless said; w4: with four waves to a row instead, w16: sixteen):
+//   8192 x 512   256, 512, 1024, 2048: 14.0 13.3 14.9 19.2, w4 20.7   32768 x 256: 45.9 31.4 24.8 29.8, w4 52.9
+//   8192 x 1024  256, 512, 1024: 21.0 19.6 20.7, w4 33.0 and more     2000 x 1024: 11.3 13.2 13.2
+//   8192 x 2048  128, 256, 512: 48.7 32.8 31.1, w4 33.0               2000 x 2048: 16.1 14.5 17.6   float32 67.5 49.2 51.0, w4 45.7
+//   8192 x 4096  256, 512, 1024: 82.8 60.0 56.8, w16 68.4             2000 x 4096: 27.6 23.9 29.1   float32 98.8 86.8 98.3
+//   8192 x 8192  256, 512, 1024: 135.5 102.0 116.6, w16 109.3         2000 x 8192: 43.2 40.6 55.5   float32 184.4 174.1 199.2, w16 164.1
+//   2000 x 16384 128, 256, 512: 73.4 59.9 78.9, from memory for every pass 90.5                     float32 152.8 114.4 130.4
+// Longer rows, which are read for every pass: 1000 x 32768 forward 38.8 (3.4 TB/s), backward 98.7; float32 84, 160.
 struct Shape { int waves, chunks, parts; };
 static Shape shape_of(int cols) {
   if (cols <= 512) return {1, 1, 1024};

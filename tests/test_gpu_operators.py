@@ -237,6 +237,21 @@ def test_attention_ranges():
     assert dl.min() >= 0 and dh.max() <= 21
 
 
+@pytest.mark.parametrize("docs", [1022, 1023, 1024, 1025, 5000])
+def test_attention_ranges_of_many_documents(docs):
+    rng = np.random.default_rng(docs)
+    q_lens, more = rng.integers(0, 5, docs), rng.integers(0, 3, docs)
+    cum = lambda l: _ints(np.cumsum(np.concatenate([[0], l])))
+    for k_lens, kw in ((q_lens, {}), (q_lens + more, {}), (q_lens, dict(window=2)), (q_lens + more, dict(prefix=rng.integers(0, 4, docs).tolist()))):
+        n, m = int(q_lens.sum()), int(k_lens.sum())
+        lo, hi, at = ref.ranges(q_lens.tolist(), k_lens.tolist(), **kw)
+        dl, dh, da, du = (torch.full((k,), -7, dtype=torch.int32, device="cuda") for k in (n, n, n, 2))
+        R.revffn_op_attention_ranges(cum(q_lens), None if k_lens is q_lens else cum(k_lens), _ints(kw["prefix"]) if "prefix" in kw else None, docs, True,
+                                     kw.get("window", 0), n, m, dl, dh, da, du)
+        torch.cuda.synchronize()
+        assert dl.tolist() == list(lo) and dh.tolist() == list(hi) and da.tolist() == list(at) and du.tolist() == [n, m]
+
+
 def test_attention_ranges_of_no_queries():
     used = torch.full((2,), -7, dtype=torch.int32, device="cuda")
     nothing = torch.empty(0, dtype=torch.int32, device="cuda")
