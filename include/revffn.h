@@ -386,13 +386,14 @@ int revffn_op_attention_ranges(const int32_t *cu_q, const int32_t *cu_k, const i
                                int32_t *at, int32_t *used, void *hip_stream);
 
 /* o = softmax(scores) v over each query's range; lse[H, Tq] = log of the sum of exponentials (NULL if not wanted; the
- * backward pass needs it).  q, k, v are not changed and overlap no result.  work: revffn_op_attention_masked_workspace
- * bytes of this very desc: they do not grow with it, a call of fewer rows may need more (its keys are split further), so a program
- * with several shapes asks for each and keeps the largest.  A call of few query rows, a single token each for instance, is split along its keys and joined.
+ * backward pass needs it).  q, k, v are not changed; no result shares elements with an input or another result.
+ * work: revffn_op_attention_masked_workspace bytes of this very desc: they do not grow with it, a call of fewer rows may need
+ * more (its keys are split further), so a program with several shapes asks for each and keeps the largest.  A call of few query
+ * rows, a single token each for instance, is split along its keys and joined.
  * The backward pass takes o and lse of the forward pass with the same desc and mask, and d_o; dq, dk, dv are overwritten.
  * dk and dv are summed over the query heads that share a key head.
- * REVFFN_EINVAL: a bad field, work_bytes too small.  REVFFN_ESHAPE: a row stride below the row's width, or more rows
- * times heads than a launch can have (2^26).  REVFFN_EUNSUPPORTED: kernel_mode 2 and a shape that the matrix-core kernels
+ * REVFFN_EINVAL: a bad field, work_bytes too small, a result that starts where an input or another result does.  REVFFN_ESHAPE:
+ * a row stride below the row's width, or more rows times heads than a launch can have (2^26).  REVFFN_EUNSUPPORTED: kernel_mode 2 and a shape that the matrix-core kernels
  * don't take (float32: dh a multiple of 4 up to 128; bfloat16: of 8, softcap up to 4096, strides below 2^24; strides and
  * pointers aligned to 16 bytes). */
 size_t revffn_op_attention_masked_workspace(const revffn_attn_desc *desc, int32_t backward);

@@ -3,6 +3,7 @@
 #include "kernels.h"
 #include "../../include/revffn.h"
 #include <math.h>
+#include <initializer_list>
 
 #define TRY(x) do { int e_ = (x); if (e_) return e_; } while (0)
 
@@ -45,6 +46,14 @@ int check_mask(const revffn_attn_mask* m, RangeAttn* a) {
   if (!m || (a->Tq > 0 && (!m->lo || !m->hi))) return REVFFN_ENULL;
   a->lo = m->lo; a->hi = m->hi; a->at = m->at; a->used = m->used;
   return 0;
+}
+// whether a result starts where an input or another result does (results first, rows > 0 of them)
+bool same_place(std::initializer_list<const void*> results, std::initializer_list<const void*> inputs) {
+  for (auto r = results.begin(); r != results.end(); r++) {
+    for (auto other = r + 1; other != results.end(); other++) if (*r && *r == *other) return true;
+    for (const void* in : inputs) if (*r && *r == in) return true;
+  }
+  return false;
 }
 int frequencies(const revffn_rotary* r, double* f) {
   if (!r || !f) return REVFFN_ENULL;
@@ -107,9 +116,11 @@ int revffn_op_attention_masked_fwd(const revffn_attn_desc* desc, const revffn_at
   if (w.bytes > work_bytes || ((uintptr_t)work & 15)) return REVFFN_EINVAL;
   a.q = q; a.k = k; a.v = v; a.out = o; a.lse = lse;
   const int mode = desc->kernel_mode & 0xff, form = desc->kernel_mode >> 8;
-  if (mode != 1 && range_flash_takes(a, false)) launch_range_fwd_flash(a, w.parts, form, (hipStream_t)stream);
-  else if (mode != 1 && range_f32_takes(a, false)) launch_range_fwd_f32(a, w.parts, (hipStream_t)stream);
-  else if (mode == 2) return REVFFN_EUNSUPPORTED;
+  const bool flash = mode != 1 && range_flash_takes(a, false), f32 = mode != 1 && range_f32_takes(a, false);
+  if (mode == 2 && !flash && !f32) return REVFFN_EUNSUPPORTED;
+  if (a.Tq > 0 && same_place({o, lse}, {q, k, v})) return REVFFN_EINVAL;
+  if (flash) launch_range_fwd_flash(a, w.parts, form, (hipStream_t)stream);
+  else if (f32) launch_range_fwd_f32(a, w.parts, (hipStream_t)stream);
   else launch_range_fwd_rows(a, (hipStream_t)stream);
   return 0;
 }
@@ -126,9 +137,12 @@ int revffn_op_attention_masked_bwd(const revffn_attn_desc* desc, const revffn_at
   if (w.bytes > work_bytes || ((uintptr_t)work & 15)) return REVFFN_EINVAL;
   a.q = q; a.k = k; a.v = v; a.o = o; a.d_o = d_o; a.lse = (float*)lse; a.dq = dq; a.dk = dk; a.dv = dv; a.dvec = w.dvec;
   const int mode = desc->kernel_mode & 0xff, form = desc->kernel_mode >> 8;
-  if (mode != 1 && range_flash_takes(a, true)) launch_range_bwd_flash(a, w.blocks, w.sums, form, (hipStream_t)stream);
-  else if (mode != 1 && range_f32_takes(a, true)) launch_range_bwd_f32(a, w.blocks, w.sums, (hipStream_t)stream);
-  else if (mode == 2) return REVFFN_EUNSUPPORTED;
+  const bool flash = mode != 1 && range_flash_takes(a, true), f32 = mode != 1 && range_f32_takes(a, true);
+  if (mode == 2 && !flash && !f32) return REVFFN_EUNSUPPORTED;
+  // (dk and dv are worked out after dq, from q, o's D, d_o and lse)
+  if (same_place({a.Tq > 0 ? dq : nullptr, a.Tk > 0 ? dk : nullptr, a.Tk > 0 ? dv : nullptr}, {q, k, v, o, d_o, lse})) return REVFFN_EINVAL;
+  if (flash) launch_range_bwd_flash(a, w.blocks, w.sums, form, (hipStream_t)stream);
+  else if (f32) launch_range_bwd_f32(a, w.blocks, w.sums, (hipStream_t)stream);
   else launch_range_bwd_rows(a, (hipStream_t)stream);
   return 0;
 }

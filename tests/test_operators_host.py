@@ -91,6 +91,22 @@ def test_attention_refuses_missing_and_small(lib):
     assert fwd(ctypes.byref(desc(kernel_mode=2)), bm, P + 2, P, P, P, P, P, 1 << 30) == EUNSUPPORTED
 
 
+def test_attention_refuses_results_in_the_place_of_inputs(lib):
+    """A gradient written over d_o, for instance, which the second half of the backward pass reads again."""
+    bd, bm, n = ctypes.byref(desc()), ctypes.byref(R.AttnMask(P, P)), 1 << 30
+    apart = [P * (i + 1) for i in range(9)]                 # q, k, v, o, (d_o, lse, dq, dk, dv or lse)
+    for into in (3, 4):
+        for other in range(into):
+            a = apart[:5]
+            a[into] = a[other]
+            assert lib.revffn_op_attention_masked_fwd(bd, bm, *a, P, n, None) == EINVAL, (into, other)
+    for into in (6, 7, 8):
+        for other in range(into):
+            a = apart[:9]
+            a[into] = a[other]
+            assert lib.revffn_op_attention_masked_bwd(bd, bm, *a, P, n, None) == EINVAL, (into, other)
+
+
 def test_attention_scratch_memory_is_each_descs_own(lib):
     """A call of fewer rows may need more of it, and a workspace that is too small for it is refused, whatever larger call it was made for."""
     size = lambda backward, **kw: lib.revffn_op_attention_masked_workspace(ctypes.byref(desc(**kw)), backward)
