@@ -437,7 +437,8 @@ def _device():
         if not torch.cuda.is_available():
             return -2
         torch.cuda.init()
-        _current, _stream_of = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+        _stream_of = torch._C._cuda_getCurrentRawStream
+        _current = torch._C._cuda_getDevice              # (last: another thread that finds it finds the others)
     return _current()
 
 
