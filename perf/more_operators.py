@@ -255,7 +255,7 @@ def _product(st):
         import paper_2512_20920_amd as R
         dt, ld = 1 if st["dtype"] == "bf16" else 0, st["w"].stride(0)
         R.revffn_op_quantize_rows(dt, st["x"], st["codes"], st["scale"], M, K, K, ld)
-        R.revffn_op_gemm_i8(dt, 0, st["codes"], st["scale"], st["w"], st["wscale"], st["bias"], st["y"], M, N, K, ld, ld, N)
+        R.revffn_op_gemm_int(dt, 0, st["codes"], st["scale"], st["w"], st["wscale"], st["bias"], st["y"], M, N, K, ld, ld, N)
         return st["y"]
     x = st["x"].float()
     scale = (x.abs().amax(1, keepdim=True).double() / 127.0).float()
