@@ -442,6 +442,67 @@ int revffn_op_layernorm_bwd(int32_t dtype, const void *dy, const void *x, const 
                             int64_t lddy, int64_t ldx, int64_t lddx, int32_t grads_f32, void *work, size_t work_bytes,
                             void *hip_stream);
 
+/* ---- a layer that answers in 8 bits: paged cache, its attention, integer products -----------------------------------
+ * The parts of a layer of a program that serves requests: new keys and values go into a cache held in 8 bits, attention reads it, and
+ * the projections around it are products of 8-bit integers.  What is said above about contexts, streams, graphs, devices, scratch memory
+ * and errors holds here too.
+ *
+ * The cache.  Memory comes in pages of `page` tokens; table[s][p] names the page that holds tokens p * page .. of sequence s.  A page holds,
+ * per key head, numbers of 8 bits (e4m3: 4 bits of exponent, 3 of mantissa, largest 448, no infinity) in units of a power of two, one for the head's
+ * keys of the page and one for its values:
+ *   k [pages][Hkv][page][dh]      v [pages][Hkv][page / 16][dh][16]  (16 tokens of a column side by side)      k_scale, v_scale [pages][Hkv]
+ * Nothing of it needs initial contents: a page is begun when its first token is appended.
+ * Rows of a call: sequence s owns rows cu[s] .. cu[s + 1] - 1 of it, which are the last of its len[s] tokens, so row r of n stands at token
+ * len[s] - n + r (cu NULL: one row each).  Numbers are clamped to their range; a table entry outside 0 .. pages - 1 is no page: what would
+ * stand there is not written, and nobody sees it.  So are tokens from max_pages * page on, and rows that would stand before token 0.  Rows that no
+ * sequence owns are left as they were. */
+typedef struct revffn_cache {
+  void *k, *v;             /* device, 16-byte aligned                                                */
+  float *k_scale, *v_scale; /* device [pages][Hkv]                                                   */
+  const int32_t *table;    /* device [n_seqs][max_pages]                                             */
+  const int32_t *len;      /* device [n_seqs]: tokens of each sequence, those of this call among them */
+  const int32_t *cu;       /* device [n_seqs + 1], ascending, or NULL                                */
+  int32_t pages, page;     /* pages of the memory; tokens of one: 16, 32, 64 or 128                  */
+  int32_t max_pages;       /* row length of table; max_pages * page <= 2^30                          */
+  int32_t n_seqs;          /* up to 2^20                                                             */
+  int32_t Hkv, dh;         /* key heads; head width, a multiple of 16 up to 256, page * dh <= 16384  */
+} revffn_cache;
+
+/* New keys and values (T rows of Hkv heads, row strides ldk, ldv) into the cache, keys turned to their positions on the way, as revffn_op_rotary
+ * turns them (r NULL: not), and with them the queries of the same rows (q to q_out, H heads; q NULL: none; q_out = q with ldqo = ldq turns in
+ * place).  pos: device [T], or NULL: a row's token in its sequence.  r->dims has to be a multiple of 16.
+ * A key is rounded to dtype, as revffn_op_rotary would store it, then to 8 bits; rounding is to nearest, ties to even.  The unit of a page and head is the
+ * least power of two (2^-96 .. 2^119) that brings its largest value within 448; if a page that holds tokens already needs a larger one, they are
+ * rounded again to it (which changes only numbers below 2^-6 of the new unit).  A value that is not finite is stored as NaN and does not count
+ * for the unit.  Only the pages and heads that get rows are written, and of those only the rows and what is rounded again.  A page that gets rows
+ * must not be named by another entry of the table that gets rows too: shared pages are for reading. */
+int revffn_op_cache_append(int32_t dtype, const revffn_cache *cache, const revffn_rotary *r, const int32_t *pos, const void *q, void *q_out,
+                           const void *k, const void *v, int32_t T, int32_t H, int64_t ldq, int64_t ldqo, int64_t ldk, int64_t ldv,
+                           void *hip_stream);
+
+/* Attention of the call's rows (desc->Tq of them) over the cache, which holds their own tokens already.  Of desc, Tk, ldk and ldv are not read; Hkv and dh
+ * must be the cache's; slopes count from the row's token; kernel_mode 0, 1 or 2.  causal: a row sees its sequence's tokens up to its own, with
+ * window > 0 the last `window` of them only; not causal: all len[s].  o and lse as of revffn_op_attention_masked_fwd, and as there nothing that a row does not
+ * see reaches it.  Single tokens' and short prompts' keys are split over workgroups, by the lengths on the device, and joined: the bits of a row
+ * depend on the other sequences of its call, and are the same whenever the call is.  work: revffn_op_attention_cached_workspace bytes of
+ * this very desc and cache's sizes.  The matrix-core kernels take rows aligned to 16 bytes, in float32 heads of up to 128 columns; others go row
+ * by row (kernel_mode 2: REVFFN_EUNSUPPORTED). */
+size_t revffn_op_attention_cached_workspace(const revffn_attn_desc *desc, const revffn_cache *cache);
+int revffn_op_attention_cached(const revffn_attn_desc *desc, const revffn_cache *cache, int32_t causal, int32_t window, const void *q, void *o,
+                               float *lse, void *work, size_t work_bytes, void *hip_stream);
+
+/* Rows of x (dtype, `cols` columns, <= 2^24) to 8-bit integers: scale[row] = max |x| / 127 (float32), codes = x / scale rounded to the nearest integer, ties to
+ * even, as if the quotient were exact.  A row whose scale would be below 2^-126 is zeros with scale 0; one with a value that is not finite is zeros with
+ * scale NaN, which poisons its products.  For a layer's tokens before each product, and for its weights (rows = output channels), once. */
+int revffn_op_quantize_rows(int32_t dtype, const void *x, int8_t *codes, float *scale, int32_t rows, int32_t cols, int64_t ldx, int64_t ldc,
+                            void *hip_stream);
+/* c[m, n] = (sum_k a[m, k] b[n, k]) a_scale[m] b_scale[n] + bias[n]: a [M, K] and b [N, K] 8-bit integers, c and bias (NULL: none) in dtype.  The sum is
+ * exact (K <= 131071).  c shares no elements with the others.  lda, ldb multiples of 16 and a, b aligned to 16 bytes go to the matrix cores (K may be
+ * any), others to a slow kernel (kernel_mode 2: REVFFN_EUNSUPPORTED; 1: the slow kernel always; + 256 * t forces one of the matrix-core kernel's
+ * shapes, t = 1 ..).  All give the same bits. */
+int revffn_op_gemm_int(int32_t dtype, int32_t kernel_mode, const int8_t *a, const float *a_scale, const int8_t *b, const float *b_scale,
+                      const void *bias, void *c, int32_t M, int32_t N, int32_t K, int64_t lda, int64_t ldb, int64_t ldc, void *hip_stream);
+
 /* Host-only check hook (no GPU work): where the MFMA GEMM's XCD-aware launch places its workgroups.
  * Workgroups reach the 8 XCDs round-robin by linear id; the kernel maps workgroup `i` back to a tile so that
  * each XCD works on tiles that share operands.  This call runs the same index function on the host for every

@@ -14,7 +14,9 @@ from .binding import (Config, Weights, Grads, Context, load_library, library_pat
                       Merged, MERGED_FIELDS, revffn_merge_adapters, revffn_forward_merged, revffn_inverse_merged,
                       AttnDesc, AttnMask, Rotary, revffn_op_attention_ranges, revffn_op_attention_masked_workspace,
                       revffn_op_attention_masked_fwd, revffn_op_attention_masked_bwd, revffn_op_rotary_frequencies,
-                      revffn_op_rotary, revffn_op_layernorm_workspace, revffn_op_layernorm_fwd, revffn_op_layernorm_bwd)
+                      revffn_op_rotary, revffn_op_layernorm_workspace, revffn_op_layernorm_fwd, revffn_op_layernorm_bwd,
+                      Cache, revffn_op_cache_append, revffn_op_attention_cached_workspace, revffn_op_attention_cached,
+                      revffn_op_quantize_rows, revffn_op_gemm_int)
 
 __all__ = ["Config", "Weights", "Grads", "Context", "load_library", "library_path",
            "revffn_forward", "revffn_inverse", "revffn_backward", "revffn_backward_stored", "revffn_inverse_backward",
@@ -26,4 +28,5 @@ __all__ = ["Config", "Weights", "Grads", "Context", "load_library", "library_pat
            "revffn_inverse_merged", "AttnDesc", "AttnMask", "Rotary", "revffn_op_attention_ranges",
            "revffn_op_attention_masked_workspace", "revffn_op_attention_masked_fwd", "revffn_op_attention_masked_bwd",
            "revffn_op_rotary_frequencies", "revffn_op_rotary", "revffn_op_layernorm_workspace", "revffn_op_layernorm_fwd",
-           "revffn_op_layernorm_bwd"]
+           "revffn_op_layernorm_bwd", "Cache", "revffn_op_cache_append", "revffn_op_attention_cached_workspace",
+           "revffn_op_attention_cached", "revffn_op_quantize_rows", "revffn_op_gemm_int"]

@@ -18,6 +18,8 @@ EXPORTED_SYMBOLS = (
     "revffn_op_attention_ranges", "revffn_op_attention_masked_workspace", "revffn_op_attention_masked_fwd",
     "revffn_op_attention_masked_bwd", "revffn_op_rotary_frequencies", "revffn_op_rotary", "revffn_op_layernorm_workspace",
     "revffn_op_layernorm_fwd", "revffn_op_layernorm_bwd",
+    "revffn_op_cache_append", "revffn_op_attention_cached_workspace", "revffn_op_attention_cached", "revffn_op_quantize_rows",
+    "revffn_op_gemm_int",
 )
 
 WEIGHT_FIELDS = (
@@ -97,6 +99,25 @@ class Rotary(ctypes.Structure):
         (n, ctypes.c_float) for n in ("theta", "factor", "few_turns", "many_turns", "magnitude")]
 
 
+class Cache(ctypes.Structure):
+    """revffn_cache.  k, v: tensors of one byte per element; k_scale, v_scale float32; table, len, cu int32 (all kept alive by this
+    object), addresses or, for cu, None."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "table", "len", "cu")] + [
+        (n, ctypes.c_int32) for n in ("pages", "page", "max_pages", "n_seqs", "Hkv", "dh")]
+
+    def __init__(self, k, v, k_scale, v_scale, table, len, cu=None, **sizes):
+        super().__init__(*(_ptr(t) for t in (k, v, k_scale, v_scale, table, len, cu)), **sizes)
+        for t in (k, v):
+            if t is not None and type(t) is not int and t.element_size() != 1:
+                raise RevffnError(f"a tensor of {t.dtype} where numbers of 8 bits are held")
+        _run_of(self.pages * self.Hkv * self.page * self.dh, k, v)
+        _run_of(self.pages * self.Hkv, k_scale, v_scale)
+        _run_of(self.n_seqs * self.max_pages, table)
+        _run_of(self.n_seqs, len)
+        _run_of(self.n_seqs + 1, cu)
+        self.kept = ((k, v), (k_scale, v_scale), (table, len, cu))
+
+
 def library_path():
     return os.path.join(_HERE, "librevffn.so")
 
@@ -160,6 +181,13 @@ def load_library():
     lib.revffn_op_layernorm_workspace.restype = size
     lib.revffn_op_layernorm_fwd.argtypes = [i32, vp, vp, vp, vp, vp, vp, i32, i32, i64, i64, ctypes.c_float, vp]
     lib.revffn_op_layernorm_bwd.argtypes = [i32, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i64, i64, i64, i32, vp, size, vp]
+    cache = ctypes.POINTER(Cache)
+    lib.revffn_op_cache_append.argtypes = [i32, cache, rot, vp, vp, vp, vp, vp, i32, i32, i64, i64, i64, i64, vp]
+    lib.revffn_op_attention_cached_workspace.argtypes = [desc, cache]
+    lib.revffn_op_attention_cached_workspace.restype = size
+    lib.revffn_op_attention_cached.argtypes = [desc, cache, i32, i32, vp, vp, vp, vp, size, vp]
+    lib.revffn_op_quantize_rows.argtypes = [i32, vp, vp, vp, i32, i32, i64, i64, vp]
+    lib.revffn_op_gemm_int.argtypes = [i32, i32, vp, vp, vp, vp, vp, vp, i32, i32, i32, i64, i64, i64, vp]
     lib.revffn_profile_enable.argtypes = [vp, i32]
     lib.revffn_profile_read.argtypes = [vp, i32, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int64),
                                         ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double)]
@@ -169,7 +197,7 @@ def load_library():
     lib.revffn_strerror.argtypes = [ctypes.c_int]
     for name in EXPORTED_SYMBOLS:
         if name not in ("revffn_workspace_bytes", "revffn_destroy", "revffn_strerror", "revffn_profile_kernel_name",
-                        "revffn_op_attention_masked_workspace", "revffn_op_layernorm_workspace"):
+                        "revffn_op_attention_masked_workspace", "revffn_op_layernorm_workspace", "revffn_op_attention_cached_workspace"):
             getattr(lib, name).restype = ctypes.c_int
     _LIB = lib
     return lib
@@ -430,10 +458,10 @@ _current = _stream_of = None
 
 def _device():
     """The current device.  (Small calls are bound by what the host does for them, so these functions look things up once.)"""
-    global _current, _stream_of, _I32, _F32, _BF16
+    global _current, _stream_of, _I32, _F32, _BF16, _I8
     if _current is None:
         import torch
-        _I32, _F32, _BF16 = torch.int32, torch.float32, torch.bfloat16
+        _I32, _F32, _BF16, _I8 = torch.int32, torch.float32, torch.bfloat16, torch.int8
         if not torch.cuda.is_available():
             return -2
         torch.cuda.init()
@@ -565,3 +593,52 @@ def revffn_op_layernorm_bwd(dtype, dy, x, gain, mean, rstd, dx, dgain, dbias, ro
     grads = _dense(dev, _F32 if grads_f32 else t, cols, dgain, dbias)
     _check(load_library().revffn_op_layernorm_bwd(dtype, dyp, xp, gp, *_dense(dev, _F32, rows, mean, rstd), dxp, *grads, rows, cols,
                                                   lddy, ldx, lddx, int(grads_f32), *_work(dev, work), _on(stream, dev)))
+
+
+# ---- a layer that answers in 8 bits: paged cache, its attention, integer products ----------------------------------------
+def _cache(device, cache):
+    numbers, scales, lists = cache.kept
+    _addresses(device, None, *numbers)
+    _addresses(device, _F32, *scales)
+    _addresses(device, _I32, *lists)
+    return ctypes.byref(cache)
+
+
+def revffn_op_cache_append(dtype, cache, rotary, pos, q, q_out, k, v, T, H, ldq, ldqo, ldk, ldv, stream=None):
+    dev = _device()
+    c = _cache(dev, cache)
+    p = _addresses(dev, _BF16 if dtype == 1 else _F32, q, q_out, k, v)
+    _check(load_library().revffn_op_cache_append(dtype, c, None if rotary is None else ctypes.byref(rotary), *_dense(dev, _I32, T, pos), *p, T, H, ldq,
+                                                 ldqo, ldk, ldv, _on(stream, dev)))
+
+
+def revffn_op_attention_cached_workspace(desc, cache):
+    """Bytes of scratch memory (0 also for what the call refuses)."""
+    return load_library().revffn_op_attention_cached_workspace(ctypes.byref(desc), ctypes.byref(cache))
+
+
+def revffn_op_attention_cached(desc, cache, causal, window, q, o, lse, work=None, stream=None):
+    dev = _device()
+    c = _cache(dev, cache)
+    _addresses(dev, _F32, desc.kept)
+    p = _addresses(dev, _BF16 if desc.dtype == 1 else _F32, q, o)
+    _check(load_library().revffn_op_attention_cached(ctypes.byref(desc), c, int(causal), window, *p, *_dense(dev, _F32, desc.H * desc.Tq, lse),
+                                                     *_work(dev, work), _on(stream, dev)))
+
+
+def revffn_op_quantize_rows(dtype, x, codes, scale, rows, cols, ldx, ldc, stream=None):
+    dev = _device()
+    px, = _addresses(dev, _BF16 if dtype == 1 else _F32, x)
+    pc, = _addresses(dev, _I8, codes)
+    _check(load_library().revffn_op_quantize_rows(dtype, px, pc, *_dense(dev, _F32, rows, scale), rows, cols, ldx, ldc, _on(stream, dev)))
+
+
+def revffn_op_gemm_int(dtype, kernel_mode, a, a_scale, b, b_scale, bias, c, M, N, K, lda, ldb, ldc, stream=None):
+    dev = _device()
+    t = _BF16 if dtype == 1 else _F32
+    pa, pb = _addresses(dev, _I8, a, b)
+    sa, = _dense(dev, _F32, M, a_scale)
+    sb, = _dense(dev, _F32, N, b_scale)
+    pbias, = _dense(dev, t, N, bias)
+    pc, = _addresses(dev, t, c)
+    _check(load_library().revffn_op_gemm_int(dtype, kernel_mode, pa, sa, pb, sb, pbias, pc, M, N, K, lda, ldb, ldc, _on(stream, dev)))

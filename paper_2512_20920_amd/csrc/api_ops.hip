@@ -1,4 +1,5 @@
-// C entry points of the operators for attention layers: attention over key ranges, rotary positions, layer norm.  They check
+// C entry points of the operators for attention layers: attention over key ranges, rotary positions, layer norm, a paged cache of
+// 8-bit numbers and the attention that reads it, products of 8-bit integers.  They check
 // their arguments, lay out the caller's scratch memory and enqueue; nothing here allocates or waits.
 #include "kernels.h"
 #include "../../include/revffn.h"
@@ -81,6 +82,31 @@ int frequencies(const revffn_rotary* r, double* f) {
     }
     f[i] = v;
   }
+  return 0;
+}
+
+// (a page's rows of a head have to fit a workgroup's registers: page * dh <= 16384)
+int check_cache(const revffn_cache* c, CacheView* v) {
+  if (!c) return REVFFN_ENULL;
+  if ((c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) || c->pages < 1 || c->max_pages < 1 || c->max_pages > (1 << 30) / c->page ||
+      c->n_seqs < 0 || c->n_seqs > (1 << 20) || c->Hkv < 1 || c->Hkv > 65536 || c->dh < 16 || c->dh > 256 || c->dh % 16)
+    return REVFFN_EINVAL;
+  if (c->page * c->dh > 16384 || (i64)c->pages * c->Hkv > INT32_MAX) return REVFFN_ESHAPE;
+  if (!c->k || !c->v || !c->k_scale || !c->v_scale || (c->n_seqs > 0 && (!c->table || !c->len))) return REVFFN_ENULL;
+  if (((uintptr_t)c->k | (uintptr_t)c->v) & 15 || c->k == c->v || c->k_scale == c->v_scale) return REVFFN_EINVAL;
+  *v = CacheView{(unsigned char*)c->k, (unsigned char*)c->v, c->k_scale, c->v_scale, c->table, c->len, c->cu, c->pages, __builtin_ctz(c->page),
+                 c->max_pages, c->n_seqs, c->Hkv, c->dh};
+  return 0;
+}
+int check_cached(const revffn_attn_desc* d, const revffn_cache* c, CachedAttn* a) {
+  RangeAttn r;
+  TRY(check_desc(d, &r));
+  *a = CachedAttn{};
+  TRY(check_cache(c, &a->c));
+  if (d->kernel_mode >> 8 || d->Hkv != c->Hkv || d->dh != c->dh) return REVFFN_EINVAL;
+  if (!grid_fits((i64)d->Tq * d->H + 4 * (i64)c->n_seqs * c->Hkv)) return REVFFN_ESHAPE;
+  a->slopes = r.slopes; a->dt = r.dt; a->H = r.H; a->G = r.G; a->T = r.Tq; a->ldq = r.ldq; a->ldo = r.ldo; a->scale = r.scale; a->cap = r.cap;
+  cached_attn_plan(a);
   return 0;
 }
 
@@ -200,6 +226,73 @@ int revffn_op_layernorm_bwd(int32_t dtype, const void* dy, const void* x, const 
   a.dy = dy; a.x = x; a.gain = gain; a.mean = (float*)mean; a.rstd = (float*)rstd; a.dx = dx; a.dgain = dgain; a.dbias = dbias; a.dt = dtype;
   a.rows = rows; a.cols = cols; a.lddy = lddy; a.ldx = ldx; a.lddx = lddx; a.grads_f32 = grads_f32; a.partial = (float*)work;
   launch_layernorm_bwd(a, (hipStream_t)stream);
+  return 0;
+}
+
+int revffn_op_cache_append(int32_t dtype, const revffn_cache* cache, const revffn_rotary* r, const int32_t* pos, const void* q, void* q_out,
+                           const void* k, const void* v, int32_t T, int32_t H, int64_t ldq, int64_t ldqo, int64_t ldk, int64_t ldv, void* stream) {
+  CacheAppend a = {};
+  TRY(check_cache(cache, &a.c));
+  if ((dtype != 0 && dtype != 1) || T < 0 || (q && (H < 1 || H > 65536))) return REVFFN_EINVAL;
+  if (T > 0 && (!k || !v || (q && !q_out))) return REVFFN_ENULL;
+  if (r) {
+    TRY(frequencies(r, a.freq));
+    if (r->dims > cache->dh || r->dims % 16) return REVFFN_EINVAL;
+    a.dims = r->dims;
+    a.interleaved = r->interleaved;
+    for (int i = 0; i < r->dims / 2; i++) a.freq[i] /= 2 * M_PI;
+  }
+  a.mag = r && r->magnitude != 0.f ? r->magnitude : 1.f;
+  const i64 wq = (i64)H * cache->dh, wk = (i64)cache->Hkv * cache->dh;
+  if (ldk < wk || ldv < wk || (q && (ldq < wq || ldqo < wq || (q == q_out && ldq != ldqo)))) return REVFFN_ESHAPE;
+  if (!grid_fits(((i64)T / cache->page + 2 * (i64)cache->n_seqs) * 4)) return REVFFN_ESHAPE;
+  if (T > 0 && same_place({cache->k, cache->v, cache->k_scale, cache->v_scale, q ? q_out : nullptr}, {k, v})) return REVFFN_EINVAL;
+  a.q = q; a.q_out = q_out; a.k = k; a.v = v; a.pos = pos; a.dt = dtype; a.T = T; a.H = H; a.ldq = ldq; a.ldqo = ldqo; a.ldk = ldk; a.ldv = ldv;
+  if (T > 0 && cache->n_seqs > 0) launch_cache_append(a, (hipStream_t)stream);
+  return 0;
+}
+
+size_t revffn_op_attention_cached_workspace(const revffn_attn_desc* desc, const revffn_cache* cache) {
+  CachedAttn a;
+  return check_cached(desc, cache, &a) ? 0 : cached_attn_bytes(a);
+}
+
+int revffn_op_attention_cached(const revffn_attn_desc* desc, const revffn_cache* cache, int32_t causal, int32_t window, const void* q, void* o,
+                               float* lse, void* work, size_t work_bytes, void* stream) {
+  CachedAttn a;
+  TRY(check_cached(desc, cache, &a));
+  if ((causal != 0 && causal != 1) || window < 0 || (window && !causal)) return REVFFN_EINVAL;
+  if (a.T > 0 && (!q || !o || !work)) return REVFFN_ENULL;
+  if (a.T > 0 && (work_bytes < cached_attn_bytes(a) || ((uintptr_t)work & 15))) return REVFFN_EINVAL;
+  if (a.T > 0 && same_place({o, lse}, {q, cache->k, cache->v, cache->k_scale, cache->v_scale})) return REVFFN_EINVAL;
+  a.causal = causal; a.window = window; a.q = q; a.out = o; a.lse = lse;
+  const bool fits = cached_attn_takes(a);
+  if (desc->kernel_mode == 2 && !fits) return REVFFN_EUNSUPPORTED;
+  if (a.T > 0 && cache->n_seqs > 0) launch_cached_attn(a, work, desc->kernel_mode == 1 || !fits, (hipStream_t)stream);
+  return 0;
+}
+
+int revffn_op_quantize_rows(int32_t dtype, const void* x, int8_t* codes, float* scale, int32_t rows, int32_t cols, int64_t ldx, int64_t ldc, void* stream) {
+  if (rows > 0 && (!x || !codes || !scale)) return REVFFN_ENULL;
+  if ((dtype != 0 && dtype != 1) || rows < 0 || cols < 1 || cols > (1 << 24) || (rows > 0 && ((const void*)codes == x || (const void*)scale == x))) return REVFFN_EINVAL;
+  if (ldx < cols || ldc < cols || !grid_fits(rows)) return REVFFN_ESHAPE;
+  launch_quantize_rows(dtype, x, (signed char*)codes, scale, rows, cols, ldx, ldc, (hipStream_t)stream);
+  return 0;
+}
+
+int revffn_op_gemm_int(int32_t dtype, int32_t kernel_mode, const int8_t* a, const float* a_scale, const int8_t* b, const float* b_scale, const void* bias,
+                      void* c, int32_t M, int32_t N, int32_t K, int64_t lda, int64_t ldb, int64_t ldc, void* stream) {
+  if ((M > 0 && (!a || !a_scale)) || (N > 0 && (!b || !b_scale)) || (M > 0 && N > 0 && !c)) return REVFFN_ENULL;
+  if ((dtype != 0 && dtype != 1) || kernel_mode < 0 || (kernel_mode & 0xff) > 2 || (kernel_mode >> 8 && (kernel_mode & 0xff) == 1) ||
+      kernel_mode >> 8 > GEMM_I8_FORMS || M < 0 || N < 0 || K < 1)
+    return REVFFN_EINVAL;
+  if (M > 0 && N > 0 && same_place({c}, {a, b, a_scale, b_scale, bias})) return REVFFN_EINVAL;
+  // (128 * 128 * K has to stay below 2^31)
+  if (K > 131071 || lda < K || ldb < K || ldc < N || !grid_fits(((i64)M + 31) / 32 * (((i64)N + 31) / 32) * 4)) return REVFFN_ESHAPE;
+  GemmI8 g = {(const signed char*)a, (const signed char*)b, a_scale, b_scale, bias, c, dtype, M, N, K, lda, ldb, ldc};
+  const bool fits = gemm_i8_takes(g);
+  if (((kernel_mode & 0xff) == 2 || kernel_mode >> 8) && !fits) return REVFFN_EUNSUPPORTED;
+  launch_gemm_i8(g, kernel_mode >> 8 ? 1 + (kernel_mode >> 8) : (kernel_mode == 1 || !fits ? 1 : 0), (hipStream_t)stream);
   return 0;
 }
 

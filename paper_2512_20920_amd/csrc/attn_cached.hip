@@ -1,0 +1,551 @@
+// Attention over a paged cache of 8-bit numbers (cache.h) on the matrix cores.
+//
+// A wave owns 32 rows, which are (query, head) pairs that share a key head, and walks over the keys in tiles of 32.  It works on transposed scores
+// S^T[key, row] = K Q^T, as the kernels over key ranges do, but nothing goes through LDS: both operands that come from the cache lie in it as a lane
+// needs them, 16 bytes at a time, and turn into bfloat16, their power of two included, without a rounding (v_cvt_scalef32_pk_bf16_fp8).
+//  * K: row m of the operand is the tile's token 16 ((m >> 2) & 1) + 4 (m >> 3) + (m & 3), so that the 16 scores that a lane gets (rows
+//    8 (e >> 2) + 4 g + (e & 3) of the result, g = lane >> 5) are tokens 16 g + e, in order.  The head's columns are contracted in the order in which
+//    16 bytes of a row hold them: step 2 t takes columns 32 t + 16 g + 0..7, step 2 t + 1 the next eight; Q is loaded alike.
+//  * V: a lane's 16 probabilities are those of 16 tokens in a row, which are the 16 bytes of one column that the cache keeps together.
+// Scores, maxima, sums and accumulators are float32.  bfloat16 calls round the probabilities to bfloat16 as operands; float32 calls take queries
+// and probabilities as three bfloat16 numbers each (24 bits; the cache's numbers need no more than one), so they are float32 throughout.
+#include "attn_range_tiles.h"
+#include "cache.h"
+
+namespace {
+
+constexpr int FEW_ROWS = 96;             // of a sequence and key head: up to here a workgroup's four waves share 32 rows' keys, beyond each has 32 rows
+constexpr int TARGET = 1024;             // workgroups that a call's keys are split for
+
+// What a call does with a sequence.  Keys begin .. end - 1 are seen by some row; cost: tiles of keys for a wave of a workgroup (a group) of rows.
+struct SeqWork { int row0, n, start, begin, end, groups, cost; bool few; };
+__device__ __forceinline__ SeqWork work_of(const CachedAttn& a, int s) {
+  SeqWork w;
+  const int2 rows = cache_rows(a.c, s, a.T);
+  const int len = cache_len(a.c, s);
+  w.row0 = rows.x; w.n = rows.y;
+  w.start = len - rows.y;                            // where the first row stands
+  w.end = min(len, cache_room(a.c));
+  w.begin = a.window ? max(w.start + 1 - a.window, 0) : 0;
+  const i64 R = (i64)rows.y * a.G;
+  w.few = R <= FEW_ROWS;
+  w.groups = (int)(w.few ? (R + 31) >> 5 : (R + 127) >> 7);
+  const int tiles = w.end > w.begin ? ((w.end - 1) >> 5) - (w.begin >> 5) + 1 : 0;
+  w.cost = w.few ? (tiles + 3) >> 2 : tiles;
+  return w;
+}
+// Into how many parts a group's keys go, if `per` tiles per wave are the aim: up to 64
+__device__ __forceinline__ int splits_of(const CachedAttn& a, const SeqWork& w, int per) {
+  if (!w.few && !a.split_many) return 1;
+  return min(max((w.cost + per - 1) / per, 1), 64);
+}
+// tiles per wave that make TARGET workgroups of everything
+__device__ __forceinline__ int tiles_per(const CachedAttn& a) {
+  float sum = 0.f;
+  for (int s0 = 0; s0 < a.c.n_seqs; s0 += 64) {
+    const int s = s0 + (int)(threadIdx.x & 63);
+    if (s < a.c.n_seqs) { const SeqWork w = work_of(a, s); if (w.few || a.split_many) sum += (float)w.groups * (float)w.cost; }
+  }
+  return max((int)(wave_sum(sum) * ((float)a.c.Hkv / TARGET)) + 1, 1);
+}
+// A call's list of workgroups: sequence by sequence, and in it (split, group, key head), key heads fastest (one stays on one XCD if there are eight).
+// Parts of split groups lie in the scratch memory in the same order, one of 32 rows (few) or four per workgroup: slot.
+struct Item { int s, at, splits; i64 slot; SeqWork w; };
+template <bool JOIN> __device__ __forceinline__ bool find(const CachedAttn& a, int id, Item* x) {
+  const int per = tiles_per(a), lane = threadIdx.x & 63;
+  int before = 0;
+  i64 slots = 0;
+  for (int s0 = 0; s0 < a.c.n_seqs; s0 += 64) {
+    int mine = 0, room = 0;
+    if (s0 + lane < a.c.n_seqs) {
+      const SeqWork w = work_of(a, s0 + lane);
+      const int k = splits_of(a, w, per);
+      // (first rows that are out of order can ask for more than there are: no sum overflows, and whoever is past the scratch memory stays out of it)
+      mine = min(JOIN ? (k > 1 ? w.groups * a.c.Hkv : 0) : w.groups * a.c.Hkv * k, 1 << 24);
+      room = min(k > 1 ? w.groups * a.c.Hkv * k * (w.few ? 1 : 4) : 0, 1 << 24);
+    }
+    const int running = wave_running(mine), all = __builtin_amdgcn_readlane(running, 63), rooms = wave_running(room);
+    if (id < before + all) {
+      const int l = __builtin_ctzll(__ballot(before + running > id));
+      x->s = s0 + l;
+      x->at = id - before - (__builtin_amdgcn_readlane(running, l) - __builtin_amdgcn_readlane(mine, l));
+      x->slot = slots + __builtin_amdgcn_readlane(rooms, l) - __builtin_amdgcn_readlane(room, l);
+      x->w = work_of(a, x->s);
+      x->splits = splits_of(a, x->w, per);
+      return true;
+    }
+    before += all;
+    slots += __builtin_amdgcn_readlane(rooms, 63);
+  }
+  return false;
+}
+
+// Keys that the query at `pos` sees
+__device__ __forceinline__ int2 seen_from(const CachedAttn& a, int pos, int end) {
+  int2 r = make_int2(a.window ? max(pos + 1 - a.window, 0) : 0, a.causal ? min(pos + 1, end) : end);
+  if (r.x >= r.y) r = make_int2(0, 0);
+  return r;
+}
+
+// One row by a wave of its own, which touches only what the row sees: 64 keys at a time, then the columns.  lds: dh floats of this wave's own.
+template <class T> __device__ void cached_row(const CachedAttn& a, int s, int i, int h, int pos, int end, float* lds) {
+  const CacheView& c = a.c;
+  const int lane = threadIdx.x & 63, dh = c.dh, kh = h / a.G, P1 = (1 << c.lg) - 1;
+  const int2 r = seen_from(a, pos, end);
+  const T* q = (const T*)a.q + (i64)i * a.ldq + (i64)h * dh;
+  wave_lds_fence();
+  for (int d = lane; d < dh; d += 64) lds[d] = to_f(q[d]);
+  wave_lds_fence();
+  const float slope = a.slopes ? a.slopes[h] : 0.f;
+  float acc[4] = {}, m = -INFINITY, l = 0.f;
+  for (int j0 = r.x; j0 < r.y; j0 += 64) {
+    const int j = j0 + lane, page = j < r.y ? cache_page(c, s, j >> c.lg) : -1;
+    const bool sees = page >= 0;
+    const i64 block = cache_block(c, max(page, 0), kh);
+    float x = -INFINITY, keep, unit = 0.f;
+    if (sees) {
+      const unsigned* k = (const unsigned*)(c.k + ((block << c.lg) + (j & P1)) * dh);
+      float s0 = 0.f, s1 = 0.f;
+      for (int d = 0; d < dh; d += 4) {
+        const int w = (int)k[d >> 2];
+        s0 = fmaf(__builtin_amdgcn_cvt_f32_fp8(w, 0), lds[d], s0); s1 = fmaf(__builtin_amdgcn_cvt_f32_fp8(w, 1), lds[d + 1], s1);
+        s0 = fmaf(__builtin_amdgcn_cvt_f32_fp8(w, 2), lds[d + 2], s0); s1 = fmaf(__builtin_amdgcn_cvt_f32_fp8(w, 3), lds[d + 3], s1);
+      }
+      x = range_score((s0 + s1) * c.ks[block] * a.scale, a.cap, slope, pos, j, &keep);
+      unit = c.vs[block];
+    }
+    const float mn = fmaxf(m, wave_max(x)), ms = mn == -INFINITY ? 0.f : mn;
+    const float p = sees ? expf(x - ms) : 0.f, alpha = expf(m - ms);
+    l = l * alpha + wave_sum(p);
+#pragma unroll
+    for (int u = 0; u < 4; u++) acc[u] *= alpha;
+    m = mn;
+    unsigned long long live = __ballot(sees);
+    while (live) {
+      const int b = __builtin_ctzll(live);
+      live &= live - 1;
+      const float f = __shfl(p * unit, b, WAVE);
+      const int jb = (j0 + b) & P1, pg = __shfl(page, b, WAVE);
+      const unsigned char* v = c.v + ((cache_block(c, pg, kh) << c.lg) + (jb & ~15)) * dh + (jb & 15);
+#pragma unroll
+      for (int u = 0; u < 4; u++) if (lane + 64 * u < dh) acc[u] = fmaf(f, e4m3_value(v[(lane + 64 * u) * 16]), acc[u]);
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  T* o = (T*)a.out + (i64)i * a.ldo + (i64)h * dh;
+#pragma unroll
+  for (int u = 0; u < 4; u++) if (lane + 64 * u < dh) o[lane + 64 * u] = from_f<T>(acc[u] * inv);
+  if (lane == 0 && a.lse) a.lse[(i64)h * a.T + i] = l == 0.f ? -INFINITY : m + logf(l);
+}
+
+template <class T> __global__ void __launch_bounds__(256) cached_rows_k(CachedAttn a) {
+  __shared__ float lds[4][256];
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const i64 id = (i64)blockIdx.x * 4 + wv;
+  const int i = (int)(id / a.H), h = (int)(id - (i64)i * a.H);
+  if (i >= a.T) return;
+  for (int s0 = 0; s0 < a.c.n_seqs; s0 += 64) {
+    int2 r = make_int2(0, 0);
+    if (s0 + lane < a.c.n_seqs) r = cache_rows(a.c, s0 + lane, a.T);
+    const unsigned long long hit = __ballot(i >= r.x && i < r.x + r.y);
+    if (hit) {
+      const int s = s0 + __builtin_ctzll(hit);
+      const SeqWork w = work_of(a, s);
+      cached_row<T>(a, s, i, h, w.start + (i - w.row0), w.end, lds[wv]);
+      return;
+    }
+  }
+}
+
+__device__ __forceinline__ float lane_f(float v, int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), l)); }
+
+// ---- the matrix-core kernel ----
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+// 8 numbers of the cache times a power of two
+__device__ __forceinline__ bf16x8 eight(unsigned lo, unsigned hi, float scale) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+  const uint4 r = make_uint4(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), __builtin_bit_cast(unsigned, c), __builtin_bit_cast(unsigned, d));
+  return __builtin_bit_cast(bf16x8, r);
+}
+__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+
+// DHP: head width rounded up to 64, 128 or 256.  WHOLE: it is the width.  F32: float32 queries and results.
+template <int DHP, bool WHOLE, bool F32, int MOD>
+__global__ void __launch_bounds__(256, DHP == 256 || F32 ? 1 : 2) cached_attn_k(CachedAttn a) {
+  typedef typename std::conditional<F32, float, bf16>::type T;
+  constexpr int KT = DHP / 32, DT = DHP / 32, Q = F32 ? 3 : 1;
+  constexpr bool AHEAD = DHP <= 128;                 // the next tile is on its way while one is worked on (wider heads have no registers for it)
+  extern __shared__ __attribute__((aligned(16))) float smem[];        // two waves' partial results and statistics
+  Item x;
+  if (!find<false>(a, (int)blockIdx.x, &x)) return;
+  const CacheView& c = a.c;
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, col = lane & 31, lg = c.lg, P1 = (1 << lg) - 1;
+  const int dh = WHOLE ? DHP : c.dh;
+  const int rest = x.at / c.Hkv, kh = x.at - rest * c.Hkv, split = rest / x.w.groups;
+  const bool few = x.w.few;
+  const int group = x.w.groups - 1 - (rest - split * x.w.groups);      // (late rows see most)
+  const int blk = few ? group : group * 4 + wv;
+
+  // this lane's row
+  const int r = blk * 32 + col, qi = r / a.G, i = x.w.row0 + qi, h = kh * a.G + (r - qi * a.G), pos = x.w.start + qi;
+  const bool ok = qi < x.w.n;
+  bf16x8 qf[Q][2 * KT];
+#pragma unroll
+  for (int t = 0; t < KT; t++) {
+    float v[16];
+#pragma unroll
+    for (int u = 0; u < 16; u++) v[u] = 0.f;
+    if (ok && (WHOLE || 32 * t + 16 * g < dh)) {
+      const T* q = (const T*)a.q + (i64)i * a.ldq + (i64)h * dh + 32 * t + 16 * g;
+      if constexpr (F32) {
+#pragma unroll
+        for (int u = 0; u < 16; u += 4) { const float4 w = *(const float4*)(q + u); v[u] = w.x; v[u + 1] = w.y; v[u + 2] = w.z; v[u + 3] = w.w; }
+      } else {
+#pragma unroll
+        for (int u = 0; u < 16; u += 8) {
+          const bf16x8 w = *(const bf16x8*)(q + u);
+#pragma unroll
+          for (int k = 0; k < 8; k++) v[u + k] = (float)w[k];
+        }
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < Q; p++)
+#pragma unroll
+      for (int u = 0; u < 16; u++) {
+        const bf16 b = (bf16)v[u];
+        qf[p][2 * t + (u >> 3)][u & 7] = b;
+        v[u] -= (float)b;
+      }
+  }
+  int2 sees = ok ? seen_from(a, pos, x.w.end) : make_int2(0, 0);
+  if (sees.x == sees.y) sees = make_int2(INT_MAX, 0);
+  const int first = wave_imin(sees.x), last = wave_imax(sees.y);
+  const int all_from = wave_imax(ok ? sees.x : 0), all_to = wave_imin(ok ? sees.y : INT_MAX);
+  // this wave's tiles: t0, t0 + step, .. below t1 (of 32 keys, counted from the sequence's first)
+  int t0 = 0, t1 = 0, step = few ? 4 : 1;
+  if (first < last) {
+    const int a0 = first >> 5, n = ((last - 1) >> 5) - a0 + 1, per = (n + x.splits - 1) / x.splits;
+    t0 = a0 + min(split * per, n);
+    t1 = min(t0 + per, a0 + n);
+    if (few) t0 += wv;
+  }
+  const int count = t1 > t0 ? (t1 - t0 + step - 1) / step : 0;
+
+  ScoreForm sf;
+  sf.f = a.scale * LOG2E;
+  sf.x1 = a.cap > 0.f ? a.scale / a.cap : 0.f;
+  sf.cap2 = a.cap * LOG2E;
+  sf.slope2 = a.slopes && ok ? a.slopes[h] * LOG2E : 0.f;
+  const float unit = MOD != 0 ? 1.f : sf.f;
+
+  // pages and scales of 64 tiles at a time, one tile per lane: of its first 16 tokens and of its second
+  int page0 = 0, page1 = 0;
+  float ks0 = 0.f, ks1 = 0.f, vs0 = 0.f, vs1 = 0.f;
+  auto look_up = [&](int n) {
+    const int kv = (t0 + (n + lane) * step) * 32;
+    const bool there = n + lane < count;
+    page0 = there ? cache_page(c, x.s, kv >> lg) : -1;
+    page1 = there ? cache_page(c, x.s, (kv + 16) >> lg) : -1;
+    const i64 b0 = cache_block(c, max(page0, 0), kh), b1 = cache_block(c, max(page1, 0), kh);
+    ks0 = c.ks[b0]; ks1 = c.ks[b1]; vs0 = c.vs[b0]; vs1 = c.vs[b1];
+  };
+  const int tok = 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3);
+  struct Tile { uint4 k[KT], v[DT]; float ks, vs; bool bad; };
+  auto fetch = [&](int n, Tile& t) {                 // the n-th tile; its pages have been looked up
+    const int l = n & 63, kv = (t0 + n * step) * 32;
+    const int p0 = __builtin_amdgcn_readlane(page0, l), p1 = __builtin_amdgcn_readlane(page1, l);
+    const i64 s0 = (cache_block(c, max(p0, 0), kh) << lg) + (kv & P1), s1 = (cache_block(c, max(p1, 0), kh) << lg) + ((kv + 16) & P1);
+    t.bad = g ? p1 < 0 : p0 < 0;
+    t.ks = tok & 16 ? lane_f(ks1, l) : lane_f(ks0, l);
+    t.vs = g ? lane_f(vs1, l) : lane_f(vs0, l);
+    const unsigned char* k = c.k + ((tok & 16 ? s1 : s0) + (tok & 15)) * dh;
+    const unsigned char* v = c.v + (g ? s1 : s0) * dh;
+    // (columns past the width: K reads other columns' numbers, which meet zeros of q; results of V's are not stored)
+#pragma unroll
+    for (int u = 0; u < KT; u++) t.k[u] = *(const uint4*)(k + (WHOLE || 32 * u + 16 * g < dh ? 32 * u + 16 * g : 0));
+#pragma unroll
+    for (int u = 0; u < DT; u++) t.v[u] = *(const uint4*)(v + 16 * (WHOLE || 32 * u + col < dh ? 32 * u + col : 0));
+  };
+
+  f32x16 acc[DT];
+#pragma unroll
+  for (int d = 0; d < DT; d++) acc[d] = f32x16{};
+  float m = -INFINITY, l = 0.f;
+  Tile cur, next;
+  if (count > 0) {
+    look_up(0);
+    if (AHEAD) fetch(0, cur);
+  }
+  for (int n = 0; n < count; n++) {
+    const int kv = (t0 + n * step) * 32;
+    if constexpr (AHEAD) {
+      if (n + 1 < count) {
+        if (((n + 1) & 63) == 0) look_up(n + 1);
+        fetch(n + 1, next);
+      }
+    } else {
+      if (n > 0 && (n & 63) == 0) look_up(n);
+      fetch(n, cur);
+    }
+    f32x16 s = {};
+#pragma unroll
+    for (int t = 0; t < KT; t++) {
+      const bf16x8 k0 = eight(cur.k[t].x, cur.k[t].y, cur.ks), k1 = eight(cur.k[t].z, cur.k[t].w, cur.ks);
+#pragma unroll
+      for (int p = 0; p < Q; p++) { s = mfma(k0, qf[p][2 * t], s); s = mfma(k1, qf[p][2 * t + 1], s); }
+    }
+    if constexpr (MOD != 0) {
+      const float d0 = (float)(pos - kv - 16 * g);
+      float keep;
+      if constexpr (F32 && (MOD & CAPPED)) {
+        if (a.cap > 0.f)
+#pragma unroll
+          for (int e = 0; e < 16; e++) s[e] = tanhf(s[e] * sf.x1) * (a.cap / a.scale);      // (back to units of q.k)
+#pragma unroll
+        for (int e = 0; e < 16; e++) s[e] = final_score<MOD & BIASED>(sf, s[e], d0 - (float)e, &keep);
+      } else {
+        tanh_scores<MOD, true>(sf, s);
+#pragma unroll
+        for (int e = 0; e < 16; e++) s[e] = final_score<MOD>(sf, s[e], d0 - (float)e, &keep);
+      }
+    }
+    const bool any_bad = __any(cur.bad);
+    if (kv < all_from || kv + 32 > all_to || any_bad) {
+      const int lo = max(sees.x, kv) - kv - 16 * g;
+      const unsigned cnt = (unsigned)max(min(sees.y, kv + 32) - max(sees.x, kv), 0);
+#pragma unroll
+      for (int e = 0; e < 16; e++) if ((unsigned)(e - lo) >= cnt || cur.bad) s[e] = -INFINITY;
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) mx = fmaxf(fmaxf(mx, s[e]), s[e + 1]);
+    const float mn = fmaxf(m, both_halves_max(mx) * unit), ms = mn == -INFINITY ? 0.f : mn;
+    if (__any(mn > m)) {
+      const float alpha = fast_exp2(m - ms);
+      l *= alpha;
+#pragma unroll
+      for (int d = 0; d < DT; d++) acc[d] *= alpha;
+    }
+    m = mn;
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; e++) { s[e] = fast_exp2(MOD != 0 ? s[e] - ms : fmaf(s[e], unit, -ms)); sum += s[e]; }
+    l += sum;
+    bf16x8 pf[Q][2];
+#pragma unroll
+    for (int p = 0; p < Q; p++) {
+      pf[p][0] = acc_to_frag(s, 0);
+      pf[p][1] = acc_to_frag(s, 1);
+#pragma unroll
+      for (int e = 0; e < 16; e++) s[e] -= (float)pf[p][e >> 3][e & 7];
+    }
+    if (kv + 32 > x.w.end || any_bad) {              // what lies behind the last token, or on no page, may be anything: zeros
+      const int keep = cur.bad ? 0 : x.w.end - kv - 16 * g;
+#pragma unroll
+      for (int d = 0; d < DT; d++) {
+        unsigned* w = (unsigned*)&cur.v[d];
+#pragma unroll
+        for (int u = 0; u < 4; u++) { const int b = min(max(keep - 4 * u, 0), 4); w[u] &= b == 4 ? ~0u : (1u << (8 * b)) - 1u; }
+      }
+    }
+#pragma unroll
+    for (int d = 0; d < DT; d++) {
+      const bf16x8 v0 = eight(cur.v[d].x, cur.v[d].y, cur.vs), v1 = eight(cur.v[d].z, cur.v[d].w, cur.vs);
+#pragma unroll
+      for (int p = 0; p < Q; p++) { acc[d] = mfma(v0, pf[p][0], acc[d]); acc[d] = mfma(v1, pf[p][1], acc[d]); }
+    }
+    if constexpr (AHEAD) cur = next;
+  }
+  l = both_halves_sum(l);
+
+  // ---- a few rows' waves put their results together: waves 2 and 3 give theirs to 0 and 1, then 1 to 0 ----
+  if (few) {
+    constexpr int FLOATS = DT * 16 * 64;
+    auto give = [&](int to) {
+      float* p = smem + to * (FLOATS + 128);
+#pragma unroll
+      for (int d = 0; d < DT; d++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) p[(d * 16 + e) * 64 + lane] = acc[d][e];
+      p[FLOATS + lane] = m;
+      p[FLOATS + 64 + lane] = l;
+    };
+    auto take = [&](int from) {
+      const float* p = smem + from * (FLOATS + 128);
+      const float m2 = p[FLOATS + lane], l2 = p[FLOATS + 64 + lane], mn = fmaxf(m, m2), ms = mn == -INFINITY ? 0.f : mn;
+      const float w = fast_exp2(m - ms), w2 = fast_exp2(m2 - ms);
+#pragma unroll
+      for (int d = 0; d < DT; d++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) acc[d][e] = fmaf(acc[d][e], w, p[(d * 16 + e) * 64 + lane] * w2);
+      l = l * w + l2 * w2;
+      m = mn;
+    };
+    if (wv >= 2) give(wv - 2);
+    __syncthreads();
+    if (wv < 2) take(wv);
+    __syncthreads();
+    if (wv == 1) give(0);
+    __syncthreads();
+    if (wv > 0) return;
+    take(0);
+  }
+  if (x.splits > 1) {
+    const i64 slot = x.slot + (few ? (i64)x.at : (i64)x.at * 4 + wv);
+    if (!ok || slot >= a.slots) return;
+    if (g == 0) a.stats[slot * 32 + col] = make_float2(m, l);
+    float* p = a.parts + (slot * 32 + col) * DHP;
+#pragma unroll
+    for (int d = 0; d < DT; d++)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        *(float4*)(p + d * 32 + 2 * e + 4 * g) = make_float4(acc[d][e], acc[d][e + 1], acc[d][e + 2], acc[d][e + 3]);
+    return;
+  }
+  // a value that is not finite: seen by its row, or only multiplied by zero in a tile that it sees a part of?
+  float z = 0.f;
+#pragma unroll
+  for (int d = 0; d < DT; d++)
+#pragma unroll
+    for (int e = 0; e < 16; e++) z = fmaf(acc[d][e], 0.f, z);
+  unsigned long long odd = __ballot(ok && z != 0.f);
+  const unsigned again = (unsigned)odd | (unsigned)(odd >> 32);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if (ok) {
+    T* o = (T*)a.out + (i64)i * a.ldo + (i64)h * dh;
+#pragma unroll
+    for (int d = 0; d < DT; d++)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        if (WHOLE || d * 32 + 2 * e + 4 * g < dh) {
+          typedef __attribute__((ext_vector_type(4))) T V4;
+          V4 v;
+#pragma unroll
+          for (int u = 0; u < 4; u++) v[u] = from_f<T>(acc[d][e + u] * inv);
+          *(V4*)(o + d * 32 + 2 * e + 4 * g) = v;
+        }
+    if (g == 0 && a.lse) a.lse[(i64)h * a.T + i] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+  }
+  if (again)
+    for (int b = 0; b < 32; b++)
+      if ((again >> b) & 1) {
+        const int rr = blk * 32 + b, qr = rr / a.G;
+        cached_row<T>(a, x.s, x.w.row0 + qr, kh * a.G + (rr - qr * a.G), x.w.start + qr, x.w.end, smem + wv * DHP);
+      }
+}
+
+// Joins the parts of split groups, a wave per row
+template <class T, int DHP> __global__ void __launch_bounds__(256) cached_join_k(CachedAttn a) {
+  __shared__ float lds[4][DHP];
+  constexpr int C = DHP / 64;
+  Item x;
+  if (!find<true>(a, (int)blockIdx.x, &x)) return;
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), Hkv = a.c.Hkv, dh = a.c.dh;
+  const int group = x.at / Hkv, kh = x.at - group * Hkv, blocks = x.w.few ? 1 : 4;      // (of the list of groups; the parts' order is turned)
+  if (x.slot + (i64)x.splits * x.w.groups * Hkv * blocks > a.slots) return;
+  for (int r = wv; r < blocks * 32; r += 4) {
+    const int rr = group * blocks * 32 + r, qi = rr / a.G;
+    if (qi >= x.w.n) return;
+    const int i = x.w.row0 + qi, h = kh * a.G + (rr - qi * a.G);
+    auto part = [&](int split) {                     // first row of the part's 32
+      const i64 at = ((i64)split * x.w.groups + (x.w.groups - 1 - group)) * Hkv + kh;
+      return ((x.slot + at * blocks + (r >> 5)) * 32 + (r & 31));
+    };
+    const float2 st = lane < x.splits ? a.stats[part(lane)] : make_float2(-INFINITY, 0.f);
+    const float M = wave_max(st.x), Ms = M == -INFINITY ? 0.f : M;
+    const float w = st.y == 0.f ? 0.f : exp2f(st.x - Ms);
+    const float tot = wave_sum(w * st.y);
+    float v[C] = {};
+    for (int k0 = 0; k0 < x.splits; k0 += 16) {
+      float p[16][C];
+#pragma unroll
+      for (int k = 0; k < 16; k++)
+#pragma unroll
+        for (int u = 0; u < C; u++) p[k][u] = k0 + k < x.splits ? a.parts[part(k0 + k) * DHP + lane * C + u] : 0.f;
+#pragma unroll
+      for (int k = 0; k < 16; k++) {
+        const float f = lane_f(w, (k0 + k) & 63);
+#pragma unroll
+        for (int u = 0; u < C; u++) v[u] = fmaf(k0 + k < x.splits ? f : 0.f, p[k][u], v[u]);
+      }
+    }
+    float z = 0.f;
+#pragma unroll
+    for (int u = 0; u < C; u++) z = fmaf(v[u], 0.f, z);
+    if (!__all(z == 0.f)) {
+      cached_row<T>(a, x.s, i, h, x.w.start + qi, x.w.end, lds[wv]);
+      continue;
+    }
+    const float inv = tot == 0.f ? 0.f : 1.f / tot;
+    T* o = (T*)a.out + (i64)i * a.ldo + (i64)h * dh;
+#pragma unroll
+    for (int u = 0; u < C; u++) if (lane * C + u < dh) o[lane * C + u] = from_f<T>(v[u] * inv);
+    if (lane == 0 && a.lse) a.lse[(i64)h * a.T + i] = tot == 0.f ? -INFINITY : (M + log2f(tot)) * LN2;
+  }
+}
+
+// Most groups that a call can have: sequences of up to 96 rows per key head make one per 32, others one per 128
+i64 most_groups(const CachedAttn& a) {
+  const i64 rows = (i64)a.T * a.G, seqs = a.c.n_seqs < a.T ? a.c.n_seqs : a.T;
+  const i64 by_row = rows / 32 + seqs, by_seq = rows / 128 + 3 * seqs;
+  return by_row < by_seq ? by_row : by_seq;
+}
+int padded(int dh) { return dh <= 64 ? 64 : dh <= 128 ? 128 : 256; }
+i64 most_slots(const CachedAttn& a) {
+  const i64 heads = most_groups(a) * a.c.Hkv;
+  return (heads + TARGET) * (a.split_many && (i64)a.T * a.G > FEW_ROWS ? 4 : 1);
+}
+
+template <int DHP, bool WHOLE, bool F32, int MOD> void go(const CachedAttn& a, hipStream_t s) {
+  constexpr size_t smem = 2 * (DHP / 32 * 16 * 64 + 128) * sizeof(float);
+  const i64 heads = most_groups(a) * a.c.Hkv;
+  if (smem > 65536) {
+    static std::atomic<unsigned long long> attr_mask{0};
+    if (attr_needed(attr_mask)) {
+      (void)hipFuncSetAttribute((const void*)cached_attn_k<DHP, WHOLE, F32, MOD>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+      attr_done(attr_mask);
+    }
+  }
+  hipLaunchKernelGGL((cached_attn_k<DHP, WHOLE, F32, MOD>), dim3((unsigned)(heads + TARGET)), dim3(256), smem, s, a);
+  typedef typename std::conditional<F32, float, bf16>::type T;
+  hipLaunchKernelGGL((cached_join_k<T, DHP>), dim3((unsigned)heads), dim3(256), 0, s, a);
+}
+template <int DHP, bool F32> void go(const CachedAttn& a, hipStream_t s) {
+  // (without a part of the score's form its kernel has no instructions of it; a scale that is not positive is multiplied, not put into the exponential)
+  const int mod = (a.cap > 0.f ? CAPPED : 0) | (a.slopes || !(a.scale > 0.f) ? BIASED : 0);
+  auto pick = [&](auto whole) {
+    constexpr bool WHOLE = decltype(whole)::value;
+    if (mod == 0) go<DHP, WHOLE, F32, 0>(a, s);
+    else if (mod == CAPPED) go<DHP, WHOLE, F32, CAPPED>(a, s);
+    else if (mod == BIASED) go<DHP, WHOLE, F32, BIASED>(a, s);
+    else go<DHP, WHOLE, F32, CAPPED | BIASED>(a, s);
+  };
+  if (a.c.dh == DHP) pick(std::true_type{}); else pick(std::false_type{});
+}
+
+}  // namespace
+
+// prompts fill the chip by themselves from TARGET groups on
+void cached_attn_plan(CachedAttn* a) { a->split_many = most_groups(*a) * a->c.Hkv < TARGET; }
+size_t cached_attn_bytes(const CachedAttn& a) { return (size_t)most_slots(a) * 32 * (padded(a.c.dh) * 4 + 8); }
+bool cached_attn_takes(const CachedAttn& a) {
+  const int es = a.dt == 0 ? 4 : 2;
+  return (a.dt == 1 || a.c.dh <= 128) && (a.ldq | a.ldo) * es % 16 == 0 && ((uintptr_t)a.q | (uintptr_t)a.out) % 16 == 0;
+}
+void launch_cached_attn(CachedAttn a, void* work, bool rows, hipStream_t s) {
+  if (a.T < 1 || a.c.n_seqs < 1) return;
+  if (rows) {
+    const dim3 grid((unsigned)cdiv((i64)a.T * a.H, 4));
+    if (a.dt == 0) hipLaunchKernelGGL((cached_rows_k<float>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((cached_rows_k<bf16>), grid, dim3(256), 0, s, a);
+    return;
+  }
+  a.slots = most_slots(a);
+  a.parts = (float*)work;
+  a.stats = (float2*)(a.parts + a.slots * 32 * padded(a.c.dh));
+  const int w = padded(a.c.dh);
+  if (a.dt == 0) { if (w == 64) go<64, true>(a, s); else go<128, true>(a, s); }
+  else { if (w == 64) go<64, false>(a, s); else if (w == 128) go<128, false>(a, s); else go<256, false>(a, s); }
+}

@@ -396,3 +396,47 @@ struct LayerNorm {
 size_t layernorm_partial_floats(int rows, int cols);
 void launch_layernorm_fwd(const LayerNorm& a, hipStream_t s);
 void launch_layernorm_bwd(const LayerNorm& a, hipStream_t s);
+
+// ---- a paged cache of 8-bit numbers -------------------------------------------------------------------------
+struct CacheView {                       // (cache.h says how numbers and scales lie)
+  unsigned char *k, *v;
+  float *ks, *vs;
+  const int *table, *len, *cu;
+  int pages, lg, max_pages, n_seqs, Hkv, dh;      // lg: log2 of a page's tokens
+};
+struct CacheAppend {
+  CacheView c;
+  const void *q, *k, *v; void* q_out; const int* pos;
+  int dt, T, H, dims, interleaved;       // dims 0: nothing is turned
+  i64 ldq, ldqo, ldk, ldv;
+  float mag;
+  double freq[ROTARY_MAX_DIMS / 2];      // in turns
+};
+void launch_cache_append(const CacheAppend& a, hipStream_t s);
+struct CachedAttn {
+  CacheView c;
+  const void* q; void* out; float* lse; const float* slopes;
+  int dt, H, G, T, causal, window;
+  i64 ldq, ldo;
+  float scale, cap;
+  float* parts; float2* stats;           // scratch of split calls: `slots` parts of 32 rows
+  i64 slots;
+  int split_many;                        // whether prompts may be split along their keys
+};
+void cached_attn_plan(CachedAttn* a);               // split_many, from the sizes alone
+size_t cached_attn_bytes(const CachedAttn& a);
+bool cached_attn_takes(const CachedAttn& a);        // whether the matrix-core kernels do (else row by row)
+void launch_cached_attn(CachedAttn a, void* work, bool rows, hipStream_t s);
+
+// ---- products of 8-bit integers -----------------------------------------------------------------------------
+void launch_quantize_rows(int dt, const void* x, signed char* codes, float* scale, int rows, int cols, i64 ldx, i64 ldc, hipStream_t s);
+struct GemmI8 {
+  const signed char *a, *b;
+  const float *sa, *sb;
+  const void* bias; void* c;
+  int dt, M, N, K;
+  i64 lda, ldb, ldc;
+};
+#define GEMM_I8_FORMS 1
+bool gemm_i8_takes(const GemmI8& g);                // whether the matrix-core kernels do
+void launch_gemm_i8(const GemmI8& g, int form, hipStream_t s);      // form: 0 by size, 1 any shape and alignment (slow), 2.. forced, see gemm_i8.hip

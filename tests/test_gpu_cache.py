@@ -1,0 +1,630 @@
+"""The paged cache of 8-bit numbers, its attention and the integer products through the C ABI, against 64 bits: what is stored bit for bit, what is
+computed within bounds from the arithmetic."""
+import numpy as np
+import pytest
+import torch
+
+import cache_reference as ref
+from operators_reference import outside
+
+pytestmark = pytest.mark.gpu
+
+if torch.cuda.is_available():
+    import paper_2512_20920_amd as R
+
+TORCH = {"bf16": torch.bfloat16, "f32": torch.float32}
+NAN = float("nan")
+
+
+def _np(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def _ints(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).to("cuda", torch.int32)
+
+
+def _normal(rng, dtype, *shape, scale=1.0):
+    return torch.from_numpy((scale * rng.standard_normal(shape)).astype(np.float32)).to(TORCH[dtype]).cuda()
+
+
+class Paged:
+    """A cache on the GPU beside the reference's.  Its memory starts out as NaNs throughout."""
+
+    def __init__(self, dtype, Hkv, dh, page, tables, pages=None, seed=0):
+        self.dtype, self.Hkv, self.dh, self.page = dtype, Hkv, dh, page
+        self.table = np.asarray(tables)
+        self.pages = int(self.table.max()) + 2 if pages is None else pages
+        one = lambda *s: torch.full(s, 255, dtype=torch.uint8, device="cuda")
+        self.k, self.v = one(self.pages, Hkv, page, dh), one(self.pages, Hkv, page // 16, dh, 16)
+        self.ks, self.vs = (torch.full((self.pages, Hkv), NAN, dtype=torch.float32, device="cuda") for _ in range(2))
+        self.model = ref.Cache(self.pages, page, Hkv, dh)
+        self.rng = np.random.default_rng(seed)
+
+    def cache(self, held, cu):
+        self.lists = (_ints(self.table), _ints(held), None if cu is None else _ints(cu))
+        return R.Cache(self.k, self.v, self.ks, self.vs, *self.lists, pages=self.pages, page=self.page, max_pages=self.table.shape[1],
+                       n_seqs=self.table.shape[0], Hkv=self.Hkv, dh=self.dh)
+
+    def values(self):
+        """{name: [pages, Hkv, page, dh]} of what the memory stands for, in units of its scales."""
+        v = ref.decode(self.v.cpu().numpy()).transpose(0, 1, 2, 4, 3).reshape(self.model.numbers["v"].shape)
+        return {"k": ref.decode(self.k.cpu().numpy()), "v": v}
+
+    def check(self):
+        got = self.values()
+        for name, scale in (("k", self.ks), ("v", self.vs)):
+            assert np.array_equal(_np(scale), self.model.scale[name], equal_nan=True), name
+            assert np.array_equal(got[name], self.model.numbers[name], equal_nan=True), name
+
+    def append(self, held, new, H=2, rotary=None, pos=None, pad=0, k=None, v=None, in_place=False, no_q=False, stream=None, single=False, extra=3):
+        """Rows of a projection [T + extra, H + 2 Hkv heads + pad]; checks the cache and the queries against the rotation alone."""
+        T, dh, Hkv, dtype = sum(new), self.dh, self.Hkv, self.dtype
+        rows = T + extra
+        wide = torch.full((rows, (H + 2 * Hkv) * dh + pad), NAN, dtype=TORCH[dtype], device="cuda")
+        wide[:T, :(H + 2 * Hkv) * dh] = _normal(self.rng, dtype, T, (H + 2 * Hkv) * dh)
+        q, kk, vv = wide[:, :H * dh], wide[:, H * dh:(H + Hkv) * dh], wide[:, (H + Hkv) * dh:(H + 2 * Hkv) * dh]
+        if k is not None:
+            kk[:T], vv[:T] = k.reshape(T, -1), v.reshape(T, -1)
+        if pos is None:
+            at = np.concatenate([np.arange(h - n, h) for h, n in zip(held, new)] + [np.zeros(extra, int)])
+        else:
+            at = np.concatenate([pos, np.zeros(extra, int)])
+        before, ld, dt = wide.clone(), wide.stride(0), 1 if dtype == "bf16" else 0
+        out = q if in_place else torch.full((rows, H * dh), NAN, dtype=TORCH[dtype], device="cuda")
+        want_q, want_k = before[:, :H * dh].clone(), before[:, H * dh:(H + Hkv) * dh].clone()
+        if rotary is not None:
+            for t, heads in ((want_q, H), (want_k, Hkv)):
+                R.revffn_op_rotary(dt, rotary, t[:T], t[:T], _ints(at[:T]), T, max(T, 1), heads, dh, heads * dh, heads * dh, stream=stream)
+        c = self.cache(held, None if single else np.cumsum([0] + list(new)))
+        R.revffn_op_cache_append(dt, c, rotary, None if pos is None else _ints(at), None if no_q else q, None if no_q else out, kk, vv, T if single else rows, H, ld,
+                                 out.stride(0), ld, ld, stream=stream)
+        torch.cuda.synchronize()
+        owned = np.concatenate([(np.arange(h - n, h) >= 0) & (np.arange(h - n, h) < self.page * self.table.shape[1]) for h, n in zip(held, new)])
+        if not no_q:
+            mine = torch.from_numpy(owned).cuda()
+            assert torch.equal(out[:T][mine], want_q[:T][mine])
+            rest = before[:, :H * dh] if in_place else torch.full_like(want_q, NAN)
+            assert torch.equal(out[:T][~mine].nan_to_num(7.0), rest[:T][~mine].nan_to_num(7.0)) and torch.isnan(out[T:]).all()
+        if not in_place:
+            assert torch.equal(wide.nan_to_num(7.0), before.nan_to_num(7.0))       # the inputs are as they were
+        heads = lambda t: _np(t[:T]).reshape(T, Hkv, dh)
+        self.model.append(self.table, held, new, heads(want_k), heads(before[:, (H + Hkv) * dh:(H + 2 * Hkv) * dh]))
+        self.check()
+
+
+def _tables(rng, lens, page, spare=1):
+    need = [-(-n // page) for n in lens]
+    order = rng.permutation(sum(need) + 2)
+    t = np.full((len(lens), max(max(need), 1) + spare), -1)
+    for s in range(len(lens)):
+        t[s, :need[s]] = order[sum(need[:s]):sum(need[:s + 1])]
+    return t
+
+
+def _rotary(dims, interleaved=False, **kw):
+    return R.Rotary(dims=dims, interleaved=interleaved, theta=1e4, **kw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hkv,dh,page,H,dims,interleaved", [
+    (2, 64, 16, 4, 64, False), (1, 128, 64, 2, 128, False), (2, 128, 128, 2, 64, True), (3, 16, 16, 3, 16, False), (1, 256, 64, 1, 256, False),
+    (2, 80, 32, 6, 32, True), (2, 96, 128, 2, 96, False), (5, 48, 64, 5, 16, False), (1, 144, 32, 2, 144, True), (8, 64, 128, 16, 64, False)])
+def test_append(Hkv, dh, page, H, dims, interleaved, dtype):
+    """A prompt each, pieces that end inside pages, single tokens, a sequence that gets nothing."""
+    rng = np.random.default_rng(page + dh)
+    c = Paged(dtype, Hkv, dh, page, _tables(rng, [150, 3 * page + 2, 40, 9], page))
+    r = _rotary(dims, interleaved)
+    held = np.zeros(4, int)
+    for new in ([37, 3 * page, 0, 1], [1, 1, 0, 0], [page, 0, 17, 3], [1, 1, 1, 1], [30, 0, 1, 0]):
+        held = held + new
+        c.append(list(held), new, H, r)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kw", [dict(pad=8), dict(pad=3), dict(pad=1, in_place=True), dict(in_place=True), dict(no_q=True), dict(no_q=True, pad=5)])
+def test_append_strides_and_places(kw, dtype):
+    c = Paged(dtype, 2, 64, 32, [[1, 0, 3], [4, 2, -1]])
+    c.append([70, 33], [70, 33], 3, _rotary(64), **kw)
+    c.append([71, 40], [1, 7], 3, None, **kw)
+    c.append([75, 41], [4, 1], 3, _rotary(32, True, scaling=1, factor=4.0, magnitude=1.2), pos=np.array([90000, 5, 0, 7, 2 ** 30]), **kw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 63, 64, 65, 200])
+def test_append_single_tokens(n, dtype):
+    """One row each, with and without a list of first rows, around the number of sequences that a wave looks at at once."""
+    rng = np.random.default_rng(n)
+    lens = rng.integers(1, 40, n)
+    for single in (False, True):
+        c = Paged(dtype, 1, 16, 16, _tables(rng, lens + 1, 16), seed=n)
+        c.append(list(lens), list(lens), 1, _rotary(16))
+        c.append(list(lens + 1), [1] * n, 1, _rotary(16), single=single, extra=0 if single else 3)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_append_values(dtype):
+    """Zeros, values that are not finite, far apart in size, around powers of two, and pages whose unit grows with each token."""
+    dh, t = 32, TORCH[dtype]
+    c = Paged(dtype, 2, dh, 16, [[0, 1, 2, 3, 4]])
+    rng = np.random.default_rng(3)
+    k = rng.standard_normal((16, 2, dh)) * 2.0 ** rng.integers(-30, 30, (16, 2, 1))
+    k[0] = 0
+    k[1, 0, ::3], k[1, 1, 1], k[2, :, 5] = np.inf, np.nan, -np.inf
+    v = rng.standard_normal((16, 2, dh))
+    v[:, 1] = 0
+    v[3, 0] = np.nan
+    up = lambda x: torch.from_numpy(x.astype(np.float32)).to(t).cuda()
+    c.append([16], [16], 1, None, k=up(k), v=up(v))
+    c.append([18], [2], 1, None, k=up(np.full((2, 2, dh), np.nan)), v=up(np.zeros((2, 2, dh))))      # a page begun with nothing finite
+    for j in range(14):
+        size = 2.0 ** (3 * j - 20)
+        c.append([19 + j], [1], 1, None, k=up(rng.standard_normal((1, 2, dh)) * size), v=up(rng.standard_normal((1, 2, dh)) / size))
+    edge = np.array([448.0, 449, 447, 464, 480, 1e30, 3e38, 2.0 ** -100, 1e-38, 2.0 ** -9, 2.0 ** -10, 1.0, 240.0, 232, 248, 17.0] * 2).reshape(1, 1, dh) * np.ones((3, 2, 1))
+    edge[1] *= 2.0 ** -20
+    edge[2, 1] = 2.0 ** -130
+    c.append([35], [3], 1, None, k=up(edge), v=up(-edge))
+    if dtype == "f32":
+        low = np.full((1, 2, dh), 1e-42)
+        c.append([36], [1], 1, None, k=up(low), v=up(low))
+
+
+def test_append_pages_that_are_none():
+    """Entries of the table out of range, tokens behind its end, rows that would stand before token 0, more rows than the sequences own,
+    numbers out of range: what has no place is left out, everything else is as it should be."""
+    c = Paged("bf16", 2, 64, 16, [[0, -1, 2, 99], [3, 4, 5, -2 ** 31], [1, 2 ** 31 - 1, 6, 7]], pages=8)
+    c.append([64, 40, 17], [64, 20, 17], 2, _rotary(64))
+    c.append([70, 100, 18], [6, 60, 1], 2, _rotary(64))          # behind the table's end
+    c.append([70, 3, 18], [0, 9, 0], 2, _rotary(64))             # six rows before token 0
+    # first rows and lengths out of range
+    T = 4
+    x = torch.zeros(T, 4 * 64, dtype=torch.bfloat16, device="cuda")
+    before = [t.clone() for t in (c.k, c.v, c.ks, c.vs)]
+    out = torch.full((T, 128), NAN, dtype=torch.bfloat16, device="cuda")
+    for held, cu in (([-5, -2 ** 31, 0], [0, 1, 2, 3]), ([5, 6, 7], [9, 4, 100, 4]), ([5, 6, 7], [-7, -3, 0, 0])):
+        cache = c.cache(held, cu)
+        R.revffn_op_cache_append(1, cache, _rotary(64), None, x[:, :128], out, x[:, 128:], x[:, 128:].clone(), T, 2, 256, 128, 256, 128)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a.nan_to_num(9.0) if a.is_floating_point() else a, b.nan_to_num(9.0) if b.is_floating_point() else b) for a, b in zip((c.k, c.v, c.ks, c.vs), before))
+
+
+# name: heads, key heads, width, page, tokens held, new ones, options
+SHAPES = {
+    "one_token": (2, 2, 64, 16, [1], [1], {}),
+    "next_tokens": (8, 2, 128, 64, [212, 37, 1001, 1, 128, 300], [1] * 6, {}),
+    "next_tokens_small_pages": (4, 4, 64, 16, [15, 16, 17, 32, 33, 100], [1] * 6, {}),
+    "next_tokens_large_pages": (16, 1, 128, 128, [127, 128, 129, 500], [1] * 4, {}),
+    "forty_heads_to_one": (40, 1, 64, 32, [70, 200], [1, 1], {}),
+    "hundred_heads_to_one": (100, 1, 16, 16, [50], [1], {}),
+    "three_heads_to_one": (6, 2, 128, 32, [30, 90, 5], [12, 3, 5], {}),
+    "prompt": (4, 2, 128, 64, [150], [150], {}),
+    "prompt_behind_a_cache": (4, 1, 64, 16, [333], [70], {}),
+    "mixed": (4, 2, 64, 32, [200, 77, 260, 1, 5], [130, 1, 40, 1, 0], {}),
+    "window": (4, 2, 64, 16, [300, 77, 40], [100, 1, 40], dict(window=33)),
+    "window_of_one": (2, 2, 64, 16, [100, 33], [40, 1], dict(window=1)),
+    "not_causal": (2, 1, 64, 32, [100, 33], [40, 33], dict(causal=False)),
+    "capped": (4, 4, 64, 16, [140, 61], [100, 1], dict(cap=5.0)),
+    "biased": (4, 2, 128, 32, [140, 61], [100, 1], dict(bias=True)),
+    "capped_biased": (4, 2, 64, 32, [140, 61], [100, 1], dict(cap=5.0, bias=True)),
+    "capped_wide": (2, 2, 128, 16, [140, 61], [20, 1], dict(cap=3.0)),
+    "width_16": (2, 1, 16, 16, [70, 65], [70, 1], {}),
+    "width_32": (2, 1, 32, 64, [70, 65], [33, 1], {}),
+    "width_80": (3, 1, 80, 32, [70, 65], [40, 1], dict(cap=20.0)),
+    "width_96": (2, 2, 96, 128, [150], [60], {}),
+    "width_112": (2, 2, 112, 16, [150], [60], dict(bias=True)),
+    "width_144": (2, 1, 144, 16, [50, 40], [20, 1], {}),
+    "width_256": (2, 1, 256, 64, [100, 40], [35, 1], {}),
+    "width_256_capped": (2, 2, 256, 16, [60, 40], [5, 1], dict(cap=4.0)),
+    "more_rows_than_tokens": (2, 2, 64, 16, [5, 0, 20], [9, 3, 1], {}),
+    "nothing_held": (2, 2, 64, 16, [0, 0], [2, 1], dict(causal=False)),
+}
+MODES = pytest.mark.parametrize("dtype,mode", [("bf16", 2), ("bf16", 1), ("f32", 2), ("f32", 1)])
+
+
+def _slopes(H):
+    return 2.0 ** (-8.0 * (np.arange(H) + 1) / H)
+
+
+def _fill(c, held, k=None, v=None):
+    """All tokens of all sequences into the cache at once (written by the reference: the append has tests of its own)."""
+    n = int(np.sum(held))
+    k = c.rng.standard_normal((n, c.Hkv, c.dh)) if k is None else k
+    v = c.rng.standard_normal((n, c.Hkv, c.dh)) if v is None else v
+    c.model.append(c.table, list(held), list(held), k, v)
+    for name, codes, scale in (("k", c.k, c.ks), ("v", c.v, c.vs)):
+        x = torch.from_numpy(c.model.numbers[name]).float().to(torch.float8_e4m3fn).view(torch.uint8)
+        if name == "v":
+            x = x.reshape(c.pages, c.Hkv, c.page // 16, 16, c.dh).transpose(3, 4)
+        codes.copy_(x.contiguous())
+        scale.copy_(torch.from_numpy(c.model.scale[name]).float())
+
+
+class Attend:
+    def __init__(self, c, held, new, H, mode=0, pad=0, extra=2, scale=0.0, cap=0.0, slopes=None, cu=True, qscale=1.0):
+        self.c, self.held, self.new, self.H = c, held, new, H
+        T, dh = sum(new), c.dh
+        self.T = T
+        self.q = torch.full((T + extra, H * dh + pad), NAN, dtype=TORCH[c.dtype], device="cuda")
+        self.q[:T, :H * dh] = _normal(c.rng, c.dtype, T, H * dh, scale=qscale)
+        self.o = torch.full_like(self.q, NAN)
+        self.lse = torch.full((H, T + extra), NAN, dtype=torch.float32, device="cuda")
+        self.scale, self.cap, self.slopes = scale, cap, slopes
+        self.cache = c.cache(held, np.cumsum([0] + list(new)) if cu else None)
+        self.slope_t = None if slopes is None else torch.tensor(slopes, dtype=torch.float32, device="cuda")
+        self.desc = R.AttnDesc(dtype=1 if c.dtype == "bf16" else 0, kernel_mode=mode, H=H, Hkv=c.Hkv, dh=dh, Tq=T + extra, ldq=self.q.stride(0), ldo=self.o.stride(0),
+                               scale=scale, softcap=cap, slopes=self.slope_t)
+        n = R.revffn_op_attention_cached_workspace(self.desc, self.cache)
+        self.work = torch.full((n,), 255, dtype=torch.uint8, device="cuda")         # NaN patterns throughout
+
+    def run(self, causal=True, window=0, stream=None):
+        self.how = dict(causal=causal, window=window)
+        R.revffn_op_attention_cached(self.desc, self.cache, causal, window, self.q, self.o, self.lse, self.work, stream=stream)
+
+    def queries(self):
+        return _np(self.q[:self.T, :self.H * self.c.dh]).reshape(self.T, self.H, self.c.dh)
+
+    def results(self):
+        torch.cuda.synchronize()
+        return _np(self.o[:self.T, :self.H * self.c.dh]).reshape(self.T, self.H, self.c.dh), _np(self.lse[:, :self.T])
+
+    def check(self):
+        o, lse = self.results()
+        sl = None if self.slopes is None else np.asarray(self.slopes, np.float32).astype(np.float64)
+        want = ref.attention(self.c.model, self.c.table, self.held, self.new, self.queries(), scale=self.scale or None, cap=self.cap, slopes=sl, dtype=self.c.dtype, **self.how)
+        worst = outside(o, *want["o"]), outside(lse, *want["lse"])
+        assert max(worst) <= 1.0, worst
+        assert torch.isnan(self.o[self.T:]).all() and torch.isnan(self.o[:, self.H * self.c.dh:]).all() and torch.isnan(self.lse[:, self.T:]).all()
+
+
+def _attend(name, dtype, mode, **kw):
+    H, Hkv, dh, page, held, new, opt = SHAPES[name]
+    if dtype == "f32" and dh > 128 and mode == 2:
+        mode = 0                                             # (refused on the matrix cores: see the host's tests)
+    opt = dict(opt)
+    c = Paged(dtype, Hkv, dh, page, _tables(np.random.default_rng(len(name)), held, page), seed=len(name))
+    _fill(c, held)
+    a = Attend(c, held, new, H, mode, cap=opt.pop("cap", 0.0), slopes=_slopes(H) if opt.pop("bias", False) else None, **kw)
+    a.run(**opt)
+    return a
+
+
+@MODES
+@pytest.mark.parametrize("name", list(SHAPES))
+def test_attention(name, dtype, mode):
+    _attend(name, dtype, mode).check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pad,mode", [(8, 2), (64, 0), (3, 0), (1, 1)])
+def test_attention_strides(pad, mode, dtype):
+    _attend("mixed", dtype, mode, pad=pad).check()
+
+
+@MODES
+def test_attention_without_a_list_of_first_rows(dtype, mode):
+    _attend("next_tokens", dtype, mode, cu=False, extra=0).check()
+
+
+@MODES
+@pytest.mark.parametrize("scale,cap", [(0.3, 0.0), (-0.2, 0.0), (-0.2, 3.0), (1e-3, 0.5), (4.0, 0.0), (0.1, 1e6)])
+def test_attention_scales(scale, cap, dtype, mode):
+    """Scores of hundreds among them: one key takes nearly all of a query's weight, and maxima rise late."""
+    c = Paged(dtype, 1, 64, 32, [[2, 0, 1, 4, 3, 5], [7, 6, 8, 9, 10, 11]])
+    _fill(c, [150, 70])
+    a = Attend(c, [150, 70], [110, 1], 2, mode, scale=scale, cap=cap)
+    a.run()
+    a.check()
+
+
+@MODES
+def test_attention_holes_and_ends(dtype, mode):
+    """Pages that are none in the middle and at the end, lengths behind the table's end, a sequence all of whose pages are none."""
+    table = np.array([[0, -1, 2, 99, 4], [-1, -1, -1, -1, -1], [5, 6, 7, 8, -3], [9, 2 ** 31 - 1, 10, 11, 12]])
+    for page in (16, 32):
+        c = Paged(dtype, 2, 64, page, table, pages=13)
+        held = [5 * page, 40, 4 * page - 3, 5 * page + 9]
+        _fill(c, held)
+        a = Attend(c, held, [3, 2, 50, 30], 4, mode)
+        a.run()
+        a.check()
+        o, lse = a.results()
+        assert (o[3:5] == 0).all() and np.isneginf(lse[:, 3:5]).all()
+
+
+@MODES
+def test_attention_lists_out_of_range(dtype, mode):
+    """Lengths and first rows out of range end the call in order, and nobody's rows but the owned ones are written."""
+    c = Paged(dtype, 2, 64, 16, [[0, 1, 2], [3, 4, 5], [6, 7, 8]])
+    _fill(c, [48, 48, 48])
+    a = Attend(c, [48, 48, 48], [1, 2, 3], 4, mode)
+    for held, cu in (([-4, -2 ** 31, 2 ** 31 - 1], [0, 1, 3, 6]), ([48, 48, 48], [100, -7, 2 ** 31 - 1, -1]), ([48, 48, 48], [5, 4, 3, 2]), ([0, 0, 0], [0, 0, 0, 0])):
+        a.cache = c.cache(held, cu)
+        a.run()
+        a.results()
+        assert torch.isnan(a.o[a.T:]).all()
+
+
+@MODES
+@pytest.mark.parametrize("held,new", [([70, 300, 45, 200], [60, 1, 5, 200]), ([1000, 40], [1, 1])])
+def test_attention_values_that_are_not_finite(held, new, dtype, mode):
+    """A NaN among one sequence's values (keys, queries): who sees it gets it, everybody else's results are what they are without, rows of the same
+    tile that may not see it yet among them."""
+    for where in ("k", "v", "q"):
+        c, clean = (Paged(dtype, 1, 64, 16, _tables(np.random.default_rng(7), held, 16), seed=5) for _ in range(2))
+        n = int(np.sum(held))
+        k, v = np.random.default_rng(6).standard_normal((2, n, 1, 64))
+        _fill(clean, held, k, v)
+        token = held[0] - 2                                  # of the first sequence: its last query but one sees it first, if it has so many
+        if where != "q":
+            (k if where == "k" else v)[token, 0, 3] = np.nan
+        _fill(c, held, k, v)
+        a, b = Attend(c, held, new, 2, mode), Attend(clean, held, new, 2, mode)
+        a.q.copy_(b.q)
+        if where == "q":
+            a.q[0, 5] = NAN
+        a.run()
+        b.run()
+        b.check()
+        o, lse = a.results()
+        o2, lse2 = b.results()
+        want = ref.attention(clean.model, clean.table, held, new, b.queries(), dtype=dtype)
+        at = held[0] - new[0] + np.arange(new[0])
+        sees = np.zeros((a.T, 2), bool)
+        if where == "q":
+            sees[0, 0] = True
+        else:
+            sees[:new[0]][at >= token] = True
+        assert np.isnan(o[sees]).any(axis=-1).all() and sees.any()
+        # (rows worked out again add in another order: both are within the bounds, so at most two of them apart)
+        assert outside(o[~sees], o2[~sees], 2 * want["o"][1][~sees]) <= 1.0, where
+        assert outside(lse[~sees.T], lse2[~sees.T], 2 * want["lse"][1][~sees.T]) <= 1.0
+
+
+@pytest.mark.parametrize("dtype,rows,keys", [("bf16", 1, 9000), ("bf16", 33, 5000), ("f32", 1, 9000), ("bf16", 1, 40000)])
+def test_attention_of_long_sequences(dtype, rows, keys):
+    """Keys split over many workgroups, their pages far apart in a large memory; spot rows against the reference."""
+    page = 64
+    n = -(-keys // page)
+    rng = np.random.default_rng(keys)
+    c = Paged(dtype, 1, 128, page, rng.permutation(n + 3)[None, :n + 1], pages=n + 3)
+    _fill(c, [keys])
+    a = Attend(c, [keys], [rows], 4, 0)
+    a.run()
+    a.check()
+
+
+def test_attention_far_into_memory():
+    """A memory of more than 2^32 bytes of keys: the last pages are where they should be, for both operators."""
+    page, Hkv, dh = 128, 8, 128
+    pages = (1 << 32) // (page * Hkv * dh) + 40
+    k, v = (torch.empty(pages, Hkv, page * dh, dtype=torch.uint8, device="cuda") for _ in range(2))
+    ks, vs = (torch.empty(pages, Hkv, dtype=torch.float32, device="cuda") for _ in range(2))
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rows = torch.randn(200, 10, dh, generator=g, device="cuda").to(torch.bfloat16)
+    out = []
+    for first in (0, pages - 2):
+        table, held, cu = _ints([[first + 1, first]]), _ints([200]), _ints([0, 200])
+        cache = R.Cache(k, v, ks, vs, table, held, cu, pages=pages, page=page, max_pages=2, n_seqs=1, Hkv=Hkv, dh=dh)
+        kk, vv = (torch.randn(200, Hkv, dh, generator=torch.Generator(device="cuda").manual_seed(s), device="cuda").to(torch.bfloat16) for s in (1, 2))
+        R.revffn_op_cache_append(1, cache, None, None, None, None, kk, vv, 200, 0, 0, 0, Hkv * dh, Hkv * dh)
+        q = rows[:, :8].contiguous()
+        o, lse = torch.empty_like(q), torch.empty(8, 200, dtype=torch.float32, device="cuda")
+        desc = R.AttnDesc(dtype=1, H=8, Hkv=Hkv, dh=dh, Tq=200)
+        work = torch.empty(R.revffn_op_attention_cached_workspace(desc, cache), dtype=torch.uint8, device="cuda")
+        R.revffn_op_attention_cached(desc, cache, True, 0, q, o, lse, work)
+        torch.cuda.synchronize()
+        out.append((o, lse, k[first:first + 2].clone(), v[first:first + 2].clone(), ks[first:first + 2].clone(), vs[first:first + 2].clone()))
+    assert all(torch.equal(x, y) for x, y in zip(*out)) and torch.isfinite(out[0][0]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_graph_replays_follow_the_lists(dtype):
+    """A step of append and attention captured once and replayed as the sequences grow: every replay equals the same calls made eagerly on a cache of
+    its own, with eager work between the replays."""
+    page, Hkv, H, dh, S = 16, 2, 4, 64, 3
+    table = [[0, 1, 2, 3], [4, 5, 6, 7], [8, 9, 10, 11]]
+    held0 = np.array([5, 15, 31])
+    rng = np.random.default_rng(8)
+    a, b = Paged(dtype, Hkv, dh, page, table), Paged(dtype, Hkv, dh, page, table)
+    k, v = rng.standard_normal((2, held0.sum(), Hkv, dh))
+    _fill(a, held0, k, v)
+    _fill(b, held0, k, v)
+    dt, r = 1 if dtype == "bf16" else 0, _rotary(dh)
+    x = torch.zeros(S, (H + 2 * Hkv) * dh, dtype=TORCH[dtype], device="cuda")
+    desc = R.AttnDesc(dtype=dt, H=H, Hkv=Hkv, dh=dh, Tq=S)
+
+    def state(c):
+        cache = c.cache(held0, None)
+        return cache, c.lists[1], torch.empty(S, H * dh, dtype=TORCH[dtype], device="cuda"), torch.empty(S, H * dh, dtype=TORCH[dtype], device="cuda"), \
+            torch.empty(H, S, dtype=torch.float32, device="cuda"), torch.empty(R.revffn_op_attention_cached_workspace(desc, cache), dtype=torch.uint8, device="cuda")
+
+    def step(st):
+        cache, _, q, o, lse, work = st
+        w = x.stride(0)
+        R.revffn_op_cache_append(dt, cache, r, None, x, q, x[:, H * dh:], x[:, (H + Hkv) * dh:], S, H, w, H * dh, w, w)
+        R.revffn_op_attention_cached(desc, cache, True, 0, q, o, lse, work)
+    sa, sb = state(a), state(b)
+    graph = torch.cuda.CUDAGraph()
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        with torch.cuda.graph(graph, stream=stream):
+            step(sa)
+    torch.cuda.synchronize()
+    for n in range(6):
+        x.copy_(_normal(rng, dtype, *x.shape))
+        for st in (sa, sb):
+            st[1].add_(1)
+        graph.replay()
+        step(sb)
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in ((a.k, b.k), (a.v, b.v), (sa[2], sb[2]), (sa[3], sb[3]), (sa[4], sb[4])))
+        assert torch.isfinite(sa[3]).all() and torch.equal(a.ks.nan_to_num(0), b.ks.nan_to_num(0))
+        torch.randn(1000, device="cuda").sum().item()
+
+
+def test_another_stream():
+    a = _attend("mixed", "bf16", 2)
+    torch.cuda.synchronize()
+    want = a.o.clone()
+    a.o.fill_(NAN)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    a.run(stream=s)
+    s.synchronize()
+    assert torch.equal(a.o.nan_to_num(3.0), want.nan_to_num(3.0))
+
+
+def test_two_calls_at_once():
+    """Two layers' attention on two streams, a workspace each, over and over: the bits of each alone."""
+    calls = [_attend("next_tokens", "bf16", 2), _attend("mixed", "bf16", 2)]
+    torch.cuda.synchronize()
+    want = [a.o.clone() for a in calls]
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(20):
+        for a, s in zip(calls, streams):
+            a.run(stream=s)
+    torch.cuda.synchronize()
+    for a, w in zip(calls, want):
+        assert torch.equal(a.o.nan_to_num(3.0), w.nan_to_num(3.0))
+
+
+# ---- integer products ------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols,pad", [(1, 1, 0), (5, 64, 0), (7, 63, 1), (300, 1000, 8), (3, 1024, 0), (2, 1025, 7), (9, 4096, 16), (4, 5000, 3), (2, 40000, 0)])
+def test_quantize_rows(rows, cols, pad, dtype):
+    rng = np.random.default_rng(rows + cols)
+    x = torch.full((rows, cols + pad), 1e30, dtype=TORCH[dtype], device="cuda")
+    x[:, :cols] = _normal(rng, dtype, rows, cols) * (2.0 ** torch.from_numpy(rng.integers(-20, 20, (rows, 1))).float().cuda()).to(TORCH[dtype])
+    if rows > 2:
+        x[1, :cols] = 0
+        x[2, :cols] = torch.arange(cols, device="cuda").remainder(255) / 2 - 63.5        # with a value of 63.5: every half a tie
+        x[2, 0] = 63.5
+    if rows > 6:
+        x[3, cols // 2], x[4, 0], x[5, :cols] = NAN, float("-inf"), 1e-39 if dtype == "f32" else 1e-38
+    codes = torch.full((rows, cols + pad), 99, dtype=torch.int8, device="cuda")
+    scale = torch.full((rows + 1,), 5.0, dtype=torch.float32, device="cuda")
+    R.revffn_op_quantize_rows(1 if dtype == "bf16" else 0, x, codes, scale, rows, cols, cols + pad, cols + pad)
+    torch.cuda.synchronize()
+    want, unit = ref.quantized(_np(x[:, :cols]))
+    assert np.array_equal(_np(scale[:rows]), unit, equal_nan=True) and scale[rows] == 5.0
+    assert np.array_equal(codes[:, :cols].cpu().numpy(), want) and (codes[:, cols:] == 99).all()
+
+
+def _product(dtype, M, N, K, mode, pad=0, bias=True, seed=0, off=0):
+    """Codes of all sizes; what lies in a row behind K is not zero."""
+    rng = np.random.default_rng(seed + M + 3 * N + 7 * K)
+    ld = (K + 15) // 16 * 16 + pad if off == 0 else K + pad
+    ints = lambda n: torch.from_numpy(rng.integers(-128, 128, (n, ld)).astype(np.int8)).cuda()
+    a, b = ints(M), ints(N)
+    sa, sb = (torch.from_numpy(rng.uniform(0.001, 0.1, n).astype(np.float32)).cuda() for n in (M, N))
+    z = _normal(rng, dtype, N) if bias else None
+    c = torch.full((M + 1, N + 3), NAN, dtype=TORCH[dtype], device="cuda")
+    R.revffn_op_gemm_int(1 if dtype == "bf16" else 0, mode, a, sa, b, sb, z, c, M, N, K, ld, ld, N + 3)
+    torch.cuda.synchronize()
+    exact = a[:, :K].cpu().numpy().astype(np.int64) @ b[:, :K].cpu().numpy().astype(np.int64).T
+    want = exact * _np(sa)[:, None] * _np(sb) + (_np(z) if bias else 0.0)
+    # the sum to float32, times one scale, times the other and the bias added: half a step each, then half a step of the type
+    size = np.abs(exact * _np(sa)[:, None] * _np(sb))
+    bound = 3 * 2.0 ** -24 * size + 2.0 ** -24 * np.abs(want) + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * np.abs(want)
+    assert outside(_np(c[:M, :N]), want, bound * 1.001) <= 1.0
+    assert torch.isnan(c[M]).all() and torch.isnan(c[:, N:]).all()
+    return c
+
+
+FORMS = [0, 1] + [256 * t for t in range(1, 2)]
+
+
+@pytest.mark.parametrize("mode", FORMS)
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 64, 16), (3, 5, 100), (8, 200, 333), (33, 129, 128), (64, 64, 129), (70, 300, 640), (130, 257, 1000), (300, 520, 2049), (257, 1024, 4096)])
+def test_product(M, N, K, mode):
+    for dtype in ("bf16", "f32"):
+        _product(dtype, M, N, K, mode)
+
+
+@pytest.mark.parametrize("mode", [0, 1])
+def test_product_rows_that_are_not_aligned(mode):
+    _product("bf16", 40, 70, 333, mode, off=1)
+    _product("bf16", 40, 70, 200, mode, off=1, pad=5, bias=False)
+
+
+def test_product_forms_agree():
+    """One answer, bit for bit, whatever kernel gives it."""
+    got = [_product("f32", 200, 300, 777, mode) for mode in FORMS]
+    for c in got[1:]:
+        assert torch.equal(c.nan_to_num(1.0), got[0].nan_to_num(1.0))
+
+
+def test_product_of_the_largest_sums():
+    """128 * 128 * 131071: the last k's that a 32-bit sum holds."""
+    K = 131071
+    a = torch.full((2, 131072), -128, dtype=torch.int8, device="cuda")
+    one = torch.ones(2, dtype=torch.float32, device="cuda")
+    for mode in FORMS:
+        c = torch.empty(2, 2, dtype=torch.float32, device="cuda")
+        R.revffn_op_gemm_int(0, mode, a, one, a.clone(), one, None, c, 2, 2, K, 131072, 131072, 2)
+        torch.cuda.synchronize()
+        assert (c == float(128 * 128 * K)).all()
+
+
+def test_product_of_a_poisoned_row():
+    x = torch.randn(5, 256, device="cuda")
+    x[2, 17] = float("inf")
+    codes, scale = torch.empty(5, 256, dtype=torch.int8, device="cuda"), torch.empty(5, dtype=torch.float32, device="cuda")
+    R.revffn_op_quantize_rows(0, x, codes, scale, 5, 256, 256, 256)
+    w, ws = torch.ones(40, 256, dtype=torch.int8, device="cuda"), torch.ones(40, dtype=torch.float32, device="cuda")
+    c = torch.empty(5, 40, dtype=torch.float32, device="cuda")
+    R.revffn_op_gemm_int(0, 0, codes, scale, w, ws, None, c, 5, 40, 256, 256, 256, 40)
+    torch.cuda.synchronize()
+    assert torch.isnan(c[2]).all() and torch.isfinite(c[[0, 1, 3, 4]]).all()
+
+
+# ---- together --------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_served_layer(dtype):
+    """Projections as integer products, rotation and append, attention over the cache, the output projection: a prompt and then tokens, against
+    the same layer in 64 bits.  Each step's own rounding is tested above; here the parts have to fit together, so what is compared is the
+    layer's result with the reference fed by the stored numbers."""
+    d, H, Hkv, dh, page = 256, 4, 2, 64, 32
+    dt, t = 1 if dtype == "bf16" else 0, TORCH[dtype]
+    rng = np.random.default_rng(4)
+    width = (H + 2 * Hkv) * dh
+
+    def weights(n, k):
+        w = _normal(rng, "f32", n, k, scale=k ** -0.5)
+        codes, scale = torch.empty(n, k, dtype=torch.int8, device="cuda"), torch.empty(n, dtype=torch.float32, device="cuda")
+        R.revffn_op_quantize_rows(0, w, codes, scale, n, k, k, k)
+        return codes, scale
+    wqkv, sqkv = weights(width, d)
+    wo, so = weights(d, H * dh)
+    c = Paged(dtype, Hkv, dh, page, _tables(rng, [120, 75, 40], page))
+    held = np.array([0, 0, 0])
+    for new in ([90, 33, 1], [1, 1, 1], [20, 1, 30], [1, 1, 1]):
+        held, T = held + new, sum(new)
+        x = _normal(rng, dtype, T, d)
+
+        def product(x, w, ws, n, k):
+            codes, scale = torch.empty(T, k, dtype=torch.int8, device="cuda"), torch.empty(T, dtype=torch.float32, device="cuda")
+            y = torch.empty(T, n, dtype=t, device="cuda")
+            R.revffn_op_quantize_rows(dt, x, codes, scale, T, k, x.stride(0), k)
+            R.revffn_op_gemm_int(dt, 0, codes, scale, w, ws, None, y, T, n, k, k, k, n)
+            exact = (codes.double() @ w.double().t()) * scale.double()[:, None] * ws.double()
+            assert (y.double() - exact).abs().max() <= exact.abs().max() * (2.0 ** -8 if dtype == "bf16" else 2.0 ** -21)
+            return y
+        qkv = product(x, wqkv, sqkv, width, d)
+        cache = c.cache(held, np.cumsum([0] + new))
+        at = np.concatenate([np.arange(h - n, h) for h, n in zip(held, new)])
+        key = qkv[:, H * dh:(H + Hkv) * dh].contiguous()
+        R.revffn_op_rotary(dt, _rotary(dh), key, key, _ints(at), T, T, Hkv, dh, Hkv * dh, Hkv * dh)
+        value = qkv[:, (H + Hkv) * dh:]
+        R.revffn_op_cache_append(dt, cache, _rotary(dh), None, qkv, qkv, qkv[:, H * dh:], value, T, H, width, width, width, width)
+        c.model.append(c.table, list(held), new, _np(key).reshape(T, Hkv, dh), _np(value).reshape(T, Hkv, dh))
+        o, lse = torch.empty(T, H * dh, dtype=t, device="cuda"), torch.empty(H, T, dtype=torch.float32, device="cuda")
+        desc = R.AttnDesc(dtype=dt, H=H, Hkv=Hkv, dh=dh, Tq=T, ldq=width)
+        work = torch.empty(R.revffn_op_attention_cached_workspace(desc, cache), dtype=torch.uint8, device="cuda")
+        R.revffn_op_attention_cached(desc, cache, True, 0, qkv, o, lse, work)
+        torch.cuda.synchronize()
+        c.check()
+        want = ref.attention(c.model, c.table, list(held), new, _np(qkv[:, :H * dh]).reshape(T, H, dh), dtype=dtype)
+        assert outside(_np(o).reshape(T, H, dh), *want["o"]) <= 1.0 and outside(_np(lse), *want["lse"]) <= 1.0
+        y = product(o, wo, so, d, H * dh)
+        assert torch.isfinite(y).all()
