@@ -1,10 +1,29 @@
 // New keys and values into the pages of a cache, keys and queries turned to their positions on the way.
 //
-// A workgroup takes the new rows of one page (a sequence's pages one after the other: find_item) and a share of the heads: the
-// angles of its rows stay in registers from head to head.  For a key head it takes the largest value of all its rows' keys and
-// of their values, two numbers that meet in LDS, before the first number is written.
+// A workgroup takes the new rows of one page (a sequence's pages one after the other: find_item) and one head's values, one head's keys or a few
+// heads' queries (several heads where a page's rows of one are too few): each reads its rows once, into registers, and writes them once.  For keys
+// and values the largest of all comes between, from the waves' maxima in LDS.
+//
+// Keys are turned in float64: sines, cosines and products, so that a key differs from the exact one by its rounding alone.  In float32 one
+// in some 10^6 keys ends up on the other side of a border between two 8-bit numbers, half a step of 2^-4 of its value.  It costs no more: the series below
+// are 15 multiply-adds, and the vector units do those at the rate of float32.
 #include "cache.h"
-#include "rotary.h"
+
+// cosine and sine of a part of a turn, both within 3e-14: the nearest quarter is taken off, and the series summed for what is left, at most pi / 4
+__device__ __forceinline__ double2 turn_of(double turns) {
+  turns -= rint(turns);
+  const double quarter = rint(4.0 * turns), x = (turns - 0.25 * quarter) * 6.283185307179586, u = x * x;
+  double s = fma(u, 1.0 / 6227020800.0, -1.0 / 39916800.0), c = fma(u, -1.0 / 87178291200.0, 1.0 / 479001600.0);
+  s = fma(u, s, 1.0 / 362880.0);   c = fma(u, c, -1.0 / 3628800.0);
+  s = fma(u, s, -1.0 / 5040.0);    c = fma(u, c, 1.0 / 40320.0);
+  s = fma(u, s, 1.0 / 120.0);      c = fma(u, c, -1.0 / 720.0);
+  s = fma(u, s, -1.0 / 6.0);       c = fma(u, c, 1.0 / 24.0);
+  s = fma(u * x, s, x);            c = fma(u, c, -0.5);
+  c = fma(u, c, 1.0);
+  const int q = (int)quarter & 3;
+  const double a = q & 1 ? s : c, b = q & 1 ? c : s;
+  return make_double2(q == 1 || q == 2 ? -a : a, q >= 2 ? -b : b);
+}
 
 // Eight columns of a row.  WIDE: 16 bytes at a time.
 template <class T, bool WIDE> __device__ __forceinline__ void load8(const T* p, float* x) {
@@ -61,12 +80,21 @@ __device__ __forceinline__ unsigned byte_mask(int t, int lo, int hi) {
   return below_b & ~below_a;
 }
 
-// UN: units of 16 columns per thread that a page's rows of a head make (a page times a head's width is at most 16384)
-template <class T, int UN, bool INTER, bool WIDE>
-__global__ void __launch_bounds__(256) cache_append_k(CacheAppend a) {
-  __shared__ float tops[2][2][4];
+// float64 to float32.  What is rounded again, to fewer bits, goes by these 32 (the compiler may not make one rounding of the two).
+__device__ __forceinline__ float to_f32(double d) {
+  float f = (float)d;
+  asm("" : "+v"(f));
+  return f;
+}
+// A head's rows of a page are `units` of 16 columns: UN per lane of WPH waves.  A workgroup has WPH waves if those are more than four, else four, and
+// 4 / WPH heads.  Roles by blockIdx.y: values, keys (vblocks workgroups each), queries (qloop times as many heads one after the other).
+template <class T, int UN, int WPH, bool INTER, bool WIDE>
+__global__ void __launch_bounds__(WPH > 4 ? WPH * 64 : 256) cache_append_k(CacheAppend a, int vblocks, int qloop) {
+  constexpr int WAVES = WPH > 4 ? WPH : 4, HEADS = WAVES / WPH, LANES = 64 * WPH;
+  __shared__ float tops[WAVES];
   const CacheView& c = a.c;
-  const int tid = threadIdx.x, wv = tid >> 6, P = 1 << c.lg, room = cache_room(c), dh = c.dh;
+  const int wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), hw = wv / WPH, tid = (int)threadIdx.x - hw * LANES;
+  const int P = 1 << c.lg, room = cache_room(c), dh = c.dh;
   int s, nth;
   auto pages_of = [&](int s) {
     const int n = cache_rows(c, s, a.T).y, len = cache_len(c, s), first = max(len - n, 0), end = min(len, room);
@@ -77,14 +105,79 @@ __global__ void __launch_bounds__(256) cache_append_k(CacheAppend a) {
   const int len = cache_len(c, s), start = len - rows.y, first = max(start, 0), p = (first >> c.lg) + nth, at0 = p << c.lg;
   const int page = cache_page(c, s, p), r0 = max(first - at0, 0), r1 = min(min(len, room) - at0, P);      // rows r0 .. r1 - 1 of the page
   const i64 token0 = (i64)rows.x + (at0 - start);    // row 0 of the page, as a row of the call (may lie before the first)
+  const int role = (int)blockIdx.y < vblocks ? 0 : (int)blockIdx.y < 2 * vblocks ? 1 : 2;
+  if (role < 2 && page < 0) return;
+
+  // the unit to use: the least that brings `top` of all the head's waves within 448, and not less than the page's (where it holds rows already)
+  auto unit_for = [&](float top, float old) {
+    top = wave_max(top);
+    if constexpr (WPH > 1) {
+      if ((threadIdx.x & 63) == 0) tops[wv] = top;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < WPH; w++) top = fmaxf(top, tops[hw * WPH + w]);
+    }
+    const float now = power_for(top);
+    return r0 > 0 ? fmaxf(now, old) : now;
+  };
+
+  if (role == 0) {                                   // values: 16 tokens of two columns per lane, which are 16 bytes of each column
+    const int h = (int)blockIdx.y * HEADS + hw;
+    const bool live = h < c.Hkv;
+    const i64 block = cache_block(c, page, live ? h : 0);
+    unsigned char* vp = c.v + (block << c.lg) * dh;
+    const float old = c.vs[block];
+    static_assert(UN <= 2, "a lane's 32 values are two units");
+    const int u = tid, g = u / (dh >> 1), col = 2 * (u - g * (dh >> 1)), t0 = 16 * g;
+    float x[2][16], top = 0.f;
+#pragma unroll
+    for (int t = 0; t < 16; t++) {
+      x[0][t] = x[1][t] = 0.f;
+      const int r = t0 + t;
+      if (live && r >= r0 && r < r1) {
+        const T* v = (const T*)a.v + (token0 + r) * a.ldv + (i64)h * dh + col;
+        if constexpr (WIDE) {
+          typedef __attribute__((ext_vector_type(2))) T V;
+          const V w = *(const V*)v;
+          x[0][t] = to_f(w[0]); x[1][t] = to_f(w[1]);
+        } else { x[0][t] = to_f(v[0]); x[1][t] = to_f(v[1]); }
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 16; t++) top = larger_finite(larger_finite(top, x[0][t]), x[1][t]);
+    const float now = unit_for(top, old), inv = 1.f / now, again = old * inv;
+    const bool more = r0 > 0 && now > old;
+    if (!live) return;
+    if (tid == 0) c.vs[block] = now;
+    if (t0 >= P || t0 >= r1 || (t0 + 16 <= r0 && !more)) return;
+    const bool whole = t0 >= r0 && t0 + 16 <= r1;
+#pragma unroll
+    for (int k = 0; k < 2; k++) {
+      uint4* at = (uint4*)(vp + (i64)(t0 * dh + 16 * (col + k)));
+      uint4 held = make_uint4(0, 0, 0, 0);
+      if (!whole) held = *at;
+      unsigned w[4] = {held.x, held.y, held.z, held.w};
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        const float* y = x[k] + 4 * i;
+        const unsigned mine = byte_mask(t0 + 4 * i, r0, r1), below = byte_mask(t0 + 4 * i, 0, r0);
+        unsigned keep = w[i];
+        if (more) keep = (rescaled(keep, again) & below) | (keep & ~below);
+        const unsigned fresh = four_e4m3(in_units(y[0], inv), in_units(y[1], inv), in_units(y[2], inv), in_units(y[3], inv));
+        w[i] = (fresh & mine) | (keep & ~mine);
+      }
+      *at = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    return;
+  }
 
   const int upr = dh >> 4, turned = a.dims >> 4;
   int row[UN], ca[UN], cb[UN];
   bool in[UN], turn[UN];
-  float2 cs[UN][8];
+  double2 cs[UN][8];
 #pragma unroll
   for (int j = 0; j < UN; j++) {
-    const int u = tid + 256 * j, r = u / upr, cu = u - r * upr;
+    const int u = tid + LANES * j, r = u / upr, cu = u - r * upr;
     row[j] = r0 + r;
     in[j] = row[j] < r1;
     turn[j] = cu < turned;
@@ -93,7 +186,10 @@ __global__ void __launch_bounds__(256) cache_append_k(CacheAppend a) {
     if (in[j] && turn[j]) {
       const int pos = a.pos ? a.pos[token0 + row[j]] : at0 + row[j];
 #pragma unroll
-      for (int i = 0; i < 8; i++) cs[j][i] = rotary_turn(a.freq[8 * cu + i], pos, a.mag, 1.f);
+      for (int i = 0; i < 8; i++) {
+        cs[j][i] = turn_of((double)pos * a.freq[8 * cu + i]);
+        cs[j][i].x *= a.mag; cs[j][i].y *= a.mag;
+      }
     }
   }
   auto load_turned = [&](const T* x, int j, float* v) {
@@ -101,145 +197,99 @@ __global__ void __launch_bounds__(256) cache_append_k(CacheAppend a) {
     load8<T, WIDE>(x + cb[j], v + 8);
     if (turn[j]) {
 #pragma unroll
-      for (int i = 0; i < 8; i++)
-        if constexpr (INTER) rotary_pair(v[2 * i], v[2 * i + 1], cs[j][i]);
-        else rotary_pair(v[i], v[8 + i], cs[j][i]);
+      for (int i = 0; i < 8; i++) {
+        float &p = v[INTER ? 2 * i : i], &q = v[INTER ? 2 * i + 1 : 8 + i];
+        const double dp = p, dq = q;
+        const double tp = fma(dp, cs[j][i].x, -(dq * cs[j][i].y)), tq = fma(dq, cs[j][i].x, dp * cs[j][i].y);
+        p = to_f32(tp);
+        q = to_f32(tq);
+      }
     }
   };
-
-  const int chunks = gridDim.y, y = blockIdx.y;
-  if (page >= 0)
-    for (int h = y * c.Hkv / chunks; h < (y + 1) * c.Hkv / chunks; h++) {
-      const i64 block = cache_block(c, page, h);
-      unsigned char *kp = c.k + (block << c.lg) * dh, *vp = c.v + (block << c.lg) * dh;
-      const float old_k = c.ks[block], old_v = c.vs[block];
-      float kx[UN][16], top_k = 0.f, top_v = 0.f;
+  if (role == 1) {
+    const int h = ((int)blockIdx.y - vblocks) * HEADS + hw;
+    const bool live = h < c.Hkv;
+    const i64 block = cache_block(c, page, live ? h : 0);
+    unsigned char* kp = c.k + (block << c.lg) * dh;
+    const float old = c.ks[block];
+    float x[UN][16], top = 0.f;
 #pragma unroll
-      for (int j = 0; j < UN; j++)
-        if (in[j]) {
-          load_turned((const T*)a.k + (token0 + row[j]) * a.ldk + (i64)h * dh, j, kx[j]);
+    for (int j = 0; j < UN; j++)
+      if (live && in[j]) {
+        load_turned((const T*)a.k + (token0 + row[j]) * a.ldk + (i64)h * dh, j, x[j]);
 #pragma unroll
-          for (int i = 0; i < 16; i++) {
-            kx[j][i] = to_f(from_f<T>(kx[j][i]));    // (a key is what the rotation alone would store, then in 8 bits)
-            top_k = larger_finite(top_k, kx[j][i]);
-          }
-        }
-      // values: 16 tokens of two columns per thread, which are 16 bytes of each column
-      constexpr int VN = UN > 1 ? UN / 2 : 1;
-      float vx[VN][2][16];
-#pragma unroll
-      for (int j = 0; j < VN; j++) {
-        const int u = tid + 256 * j, g = u / (dh >> 1), col = 2 * (u - g * (dh >> 1));
-#pragma unroll
-        for (int t = 0; t < 16; t++) {
-          vx[j][0][t] = vx[j][1][t] = 0.f;
-          const int r = 16 * g + t;
-          if (r >= r0 && r < r1) {
-            const T* x = (const T*)a.v + (token0 + r) * a.ldv + (i64)h * dh + col;
-            if constexpr (WIDE) {
-              typedef __attribute__((ext_vector_type(2))) T V;
-              const V v = *(const V*)x;
-              vx[j][0][t] = to_f(v[0]); vx[j][1][t] = to_f(v[1]);
-            } else { vx[j][0][t] = to_f(x[0]); vx[j][1][t] = to_f(x[1]); }
-            top_v = larger_finite(larger_finite(top_v, vx[j][0][t]), vx[j][1][t]);
-          }
+        for (int i = 0; i < 16; i++) {
+          x[j][i] = to_f(from_f<T>(x[j][i]));        // (a key is rounded to float32, to its type, and then to 8 bits)
+          top = larger_finite(top, x[j][i]);
         }
       }
-      top_k = wave_max(top_k);
-      top_v = wave_max(top_v);
-      if ((tid & 63) == 0) { tops[h & 1][0][wv] = top_k; tops[h & 1][1][wv] = top_v; }
-      __syncthreads();                               // (the next head's go to the other half: one barrier per head is enough)
-      float now_k = 0.f, now_v = 0.f;
-#pragma unroll
-      for (int w = 0; w < 4; w++) { now_k = fmaxf(now_k, tops[h & 1][0][w]); now_v = fmaxf(now_v, tops[h & 1][1][w]); }
-      now_k = power_for(now_k);
-      now_v = power_for(now_v);
-      if (r0 > 0) { now_k = fmaxf(now_k, old_k); now_v = fmaxf(now_v, old_v); }
-      const bool more_k = r0 > 0 && now_k > old_k, more_v = r0 > 0 && now_v > old_v;
-      const float inv_k = 1.f / now_k, inv_v = 1.f / now_v, again_k = old_k * inv_k, again_v = old_v * inv_v;
-      if (tid == 0) { c.ks[block] = now_k; c.vs[block] = now_v; }
-      if (more_k)                                    // what the page holds already, in the new unit
-        for (int o = tid * 16; o < r0 * dh; o += 4096) {
-          uint4 w = *(uint4*)(kp + o);
-          w.x = rescaled(w.x, again_k); w.y = rescaled(w.y, again_k); w.z = rescaled(w.z, again_k); w.w = rescaled(w.w, again_k);
-          *(uint4*)(kp + o) = w;
-        }
-#pragma unroll
-      for (int j = 0; j < UN; j++)
-        if (in[j]) {
-          float* x = kx[j];
-#pragma unroll
-          for (int i = 0; i < 16; i++) x[i] = in_units(x[i], inv_k);
-          *(uint2*)(kp + row[j] * dh + ca[j]) = make_uint2(four_e4m3(x[0], x[1], x[2], x[3]), four_e4m3(x[4], x[5], x[6], x[7]));
-          *(uint2*)(kp + row[j] * dh + cb[j]) = make_uint2(four_e4m3(x[8], x[9], x[10], x[11]), four_e4m3(x[12], x[13], x[14], x[15]));
-        }
-#pragma unroll
-      for (int j = 0; j < VN; j++) {
-        const int u = tid + 256 * j, g = u / (dh >> 1), col = 2 * (u - g * (dh >> 1)), t0 = 16 * g;
-        if (t0 >= P || t0 >= r1 || (t0 + 16 <= r0 && !more_v)) continue;
-        const bool whole = t0 >= r0 && t0 + 16 <= r1;
-#pragma unroll
-        for (int k = 0; k < 2; k++) {
-          uint4* at = (uint4*)(vp + (i64)(t0 * dh + 16 * (col + k)));
-          uint4 held = make_uint4(0, 0, 0, 0);
-          if (!whole) held = *at;
-          unsigned w[4] = {held.x, held.y, held.z, held.w};
-#pragma unroll
-          for (int i = 0; i < 4; i++) {
-            const float* x = vx[j][k] + 4 * i;
-            const unsigned mine = byte_mask(t0 + 4 * i, r0, r1), below = byte_mask(t0 + 4 * i, 0, r0);
-            unsigned keep = w[i];
-            if (more_v) keep = (rescaled(keep, again_v) & below) | (keep & ~below);
-            const unsigned fresh = four_e4m3(in_units(x[0], inv_v), in_units(x[1], inv_v), in_units(x[2], inv_v), in_units(x[3], inv_v));
-            w[i] = (fresh & mine) | (keep & ~mine);
-          }
-          *at = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+    const float now = unit_for(top, old), inv = 1.f / now, again = old * inv;
+    if (!live) return;
+    if (tid == 0) c.ks[block] = now;
+    if (r0 > 0 && now > old)                         // what the page holds already, in the new unit
+      for (int o = tid * 16; o < r0 * dh; o += LANES * 16) {
+        uint4 w = *(uint4*)(kp + o);
+        w.x = rescaled(w.x, again); w.y = rescaled(w.y, again); w.z = rescaled(w.z, again); w.w = rescaled(w.w, again);
+        *(uint4*)(kp + o) = w;
       }
-    }
-  if (a.q)
-    for (int h = y * a.H / chunks; h < (y + 1) * a.H / chunks; h++)
 #pragma unroll
-      for (int j = 0; j < UN; j++)
-        if (in[j]) {
-          float v[16];
-          load_turned((const T*)a.q + (token0 + row[j]) * a.ldq + (i64)h * dh, j, v);
-          T* o = (T*)a.q_out + (token0 + row[j]) * a.ldqo + (i64)h * dh;
-          store8<T, WIDE>(o + ca[j], v);
-          store8<T, WIDE>(o + cb[j], v + 8);
-        }
-}
-
-template <class T, int UN, bool INTER> static void launch(const CacheAppend& a, dim3 grid, bool wide, hipStream_t s) {
-  if (wide) hipLaunchKernelGGL((cache_append_k<T, UN, INTER, true>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((cache_append_k<T, UN, INTER, false>), grid, dim3(256), 0, s, a);
-}
-template <class T> static void launch(const CacheAppend& a, dim3 grid, bool wide, hipStream_t s) {
-  const int un = cdiv((i64)a.c.dh << a.c.lg, 4096);
-  if (a.interleaved) {
-    if (un <= 1) launch<T, 1, true>(a, grid, wide, s);
-    else if (un <= 2) launch<T, 2, true>(a, grid, wide, s);
-    else launch<T, 4, true>(a, grid, wide, s);
-  } else {
-    if (un <= 1) launch<T, 1, false>(a, grid, wide, s);
-    else if (un <= 2) launch<T, 2, false>(a, grid, wide, s);
-    else launch<T, 4, false>(a, grid, wide, s);
+    for (int j = 0; j < UN; j++)
+      if (in[j]) {
+        float* y = x[j];
+#pragma unroll
+        for (int i = 0; i < 16; i++) y[i] = in_units(y[i], inv);
+        *(uint2*)(kp + row[j] * dh + ca[j]) = make_uint2(four_e4m3(y[0], y[1], y[2], y[3]), four_e4m3(y[4], y[5], y[6], y[7]));
+        *(uint2*)(kp + row[j] * dh + cb[j]) = make_uint2(four_e4m3(y[8], y[9], y[10], y[11]), four_e4m3(y[12], y[13], y[14], y[15]));
+      }
+    return;
   }
+  for (int n = 0; n < qloop; n++) {
+    const int h = (((int)blockIdx.y - 2 * vblocks) * qloop + n) * HEADS + hw;
+    if (h >= a.H) return;
+#pragma unroll
+    for (int j = 0; j < UN; j++)
+      if (in[j]) {
+        float v[16];
+        load_turned((const T*)a.q + (token0 + row[j]) * a.ldq + (i64)h * dh, j, v);
+        T* o = (T*)a.q_out + (token0 + row[j]) * a.ldqo + (i64)h * dh;
+        store8<T, WIDE>(o + ca[j], v);
+        store8<T, WIDE>(o + cb[j], v + 8);
+      }
+  }
+}
+
+template <class T, int UN, int WPH> static void launch(const CacheAppend& a, i64 visits, bool wide, hipStream_t s) {
+  constexpr int WAVES = WPH > 4 ? WPH : 4, HEADS = WAVES / WPH;
+  const int vblocks = cdiv(a.c.Hkv, HEADS), groups = a.q ? cdiv(a.H, HEADS) : 0;
+  // heads of queries one after the other where that leaves workgroups enough: their angles are worked out once
+  int qloop = (int)(visits * groups / 1024);
+  qloop = qloop < 1 ? 1 : qloop > 4 ? 4 : qloop;
+  const dim3 grid((unsigned)visits, 2 * vblocks + (groups ? cdiv(groups, qloop) : 0)), block(WAVES * 64);
+  if (a.interleaved) {
+    if (wide) hipLaunchKernelGGL((cache_append_k<T, UN, WPH, true, true>), grid, block, 0, s, a, vblocks, qloop);
+    else hipLaunchKernelGGL((cache_append_k<T, UN, WPH, true, false>), grid, block, 0, s, a, vblocks, qloop);
+  } else {
+    if (wide) hipLaunchKernelGGL((cache_append_k<T, UN, WPH, false, true>), grid, block, 0, s, a, vblocks, qloop);
+    else hipLaunchKernelGGL((cache_append_k<T, UN, WPH, false, false>), grid, block, 0, s, a, vblocks, qloop);
+  }
+}
+template <class T> static void launch(const CacheAppend& a, i64 visits, bool wide, hipStream_t s) {
+  const int units = (a.c.dh << a.c.lg) >> 4;
+  if (units <= 64) launch<T, 1, 1>(a, visits, wide, s);
+  else if (units <= 128) launch<T, 1, 2>(a, visits, wide, s);
+  else if (units <= 256) launch<T, 1, 4>(a, visits, wide, s);
+  else if (units <= 512) launch<T, 2, 4>(a, visits, wide, s);
+  else launch<T, 2, 8>(a, visits, wide, s);
 }
 void launch_cache_append(const CacheAppend& a, hipStream_t s) {
   const CacheView& c = a.c;
   // a sequence's n new rows meet at most (n - 1) / page + 2 pages
   const i64 visits = c.cu ? ((i64)a.T >> c.lg) + 2 * (i64)(c.n_seqs < a.T ? c.n_seqs : a.T) : (a.T < c.n_seqs ? a.T : c.n_seqs);
   if (visits == 0) return;
-  const int heads = a.q && a.H > c.Hkv ? a.H : c.Hkv;
-  i64 chunks = 1024 / visits;
-  if (chunks < 1) chunks = 1;
-  if (chunks > heads) chunks = heads;
   const int es = a.dt == 0 ? 4 : 2;
   const i64 strides = a.ldk | a.ldv | (a.q ? a.ldq | a.ldqo : 0);
   const uintptr_t at = (uintptr_t)a.k | (uintptr_t)a.v | (a.q ? (uintptr_t)a.q | (uintptr_t)a.q_out : 0);
   const bool wide = strides * es % 16 == 0 && at % 16 == 0;
-  const dim3 grid((unsigned)visits, (unsigned)chunks);
-  if (a.dt == 0) launch<float>(a, grid, wide, s);
-  else launch<bf16>(a, grid, wide, s);
+  if (a.dt == 0) launch<float>(a, visits, wide, s);
+  else launch<bf16>(a, visits, wide, s);
 }

@@ -3,7 +3,7 @@
 // heads of the rows past them, so that reading x and writing y is what bounds it and the angle may cost what it needs:
 // position * frequency in float64, reduced to a fraction of a turn there, and a full-precision sine and cosine of that.
 // bf16, 8192 rows of 40 heads of 128: 37 us (4.5 TB/s); float32, 4096 rows of 32 heads: 29 us (4.6).
-#include "rotary.h"
+#include "kernels.h"
 
 template <class T, int V> struct Vec { typedef __attribute__((ext_vector_type(V))) T type; };
 template <class T> struct Vec<T, 1> { typedef T type; };
@@ -36,7 +36,10 @@ __global__ void __launch_bounds__(256) rotary_k(RotaryArgs a, int rows_wg, int u
   const int half = a.dims / 2, t0 = (int)blockIdx.x * rows_wg, nt = min(rows_wg, a.T - t0);
   for (int e = threadIdx.x; e < nt * half; e += 256) {
     const int t = e / half, c = e - t * half, row = t0 + t;
-    turn[e] = rotary_turn(a.freq[c], a.pos ? a.pos[row] : row % a.S, a.mag, a.sign);
+    const double turns = (double)(a.pos ? a.pos[row] : row % a.S) * a.freq[c];
+    float s, co;
+    sincospif(2.f * (float)(turns - rint(turns)), &s, &co);
+    turn[e] = make_float2(co * a.mag, s * a.mag * a.sign);
   }
   __syncthreads();
   constexpr int P = INTER ? (V == 1 ? 1 : V / 2) : V;                       // pairs per unit
@@ -58,7 +61,10 @@ __global__ void __launch_bounds__(256) rotary_k(RotaryArgs a, int rows_wg, int u
           else load_vec<T, V>(xh + u * V, v);
 #pragma unroll
           for (int i = 0; i < P; i++) {
-            rotary_pair(v[2 * i], v[2 * i + 1], cs[u * P + i]);
+            const float2 r = cs[u * P + i];
+            const float p = v[2 * i], q = v[2 * i + 1];
+            v[2 * i] = p * r.x - q * r.y;
+            v[2 * i + 1] = p * r.y + q * r.x;
           }
           if constexpr (V == 1) { yh[2 * u] = from_f<T>(v[0]); yh[2 * u + 1] = from_f<T>(v[1]); }
           else store_vec<T, V>(yh + u * V, v);
@@ -68,7 +74,10 @@ __global__ void __launch_bounds__(256) rotary_k(RotaryArgs a, int rows_wg, int u
           load_vec<T, V>(xh + half + u * V, q);
 #pragma unroll
           for (int i = 0; i < V; i++) {
-            rotary_pair(p[i], q[i], cs[u * V + i]);
+            const float2 r = cs[u * V + i];
+            const float w = p[i];
+            p[i] = w * r.x - q[i] * r.y;
+            q[i] = w * r.y + q[i] * r.x;
           }
           store_vec<T, V>(yh + u * V, p);
           store_vec<T, V>(yh + half + u * V, q);

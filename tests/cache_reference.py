@@ -37,6 +37,18 @@ def power_for(m):
     return 2.0 ** min(max(e, -96), 119)
 
 
+def turned(x, at, frequencies, interleaved=False, magnitude=1.0):
+    """x [rows, heads, dh] at positions, the angle reduced to a turn in extended precision, as positions may be far."""
+    y, n = np.array(x, np.float64), len(frequencies)
+    turns = np.asarray(at, np.longdouble)[:, None] * (np.asarray(frequencies) / (2 * np.pi)).astype(np.longdouble)
+    angle = (2 * np.pi * (turns - np.rint(turns)).astype(np.float64))[:, None]
+    c, s = np.cos(angle) * magnitude, np.sin(angle) * magnitude
+    first, second = (slice(0, 2 * n, 2), slice(1, 2 * n, 2)) if interleaved else (slice(0, n), slice(n, 2 * n))
+    u, w = np.array(x[..., first], np.float64), np.array(x[..., second], np.float64)
+    y[..., first], y[..., second] = u * c - w * s, u * s + w * c
+    return y
+
+
 class Cache:
     """numbers[page][head][row] in units of scale[page][head], values (not codes); NaN where nothing is known."""
 

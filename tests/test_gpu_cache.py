@@ -72,10 +72,11 @@ class Paged:
             at = np.concatenate([pos, np.zeros(extra, int)])
         before, ld, dt = wide.clone(), wide.stride(0), 1 if dtype == "bf16" else 0
         out = q if in_place else torch.full((rows, H * dh), NAN, dtype=TORCH[dtype], device="cuda")
-        want_q, want_k = before[:, :H * dh].clone(), before[:, H * dh:(H + Hkv) * dh].clone()
+        heads = lambda t, n: _np(t[:T]).reshape(T, n, dh)
+        want_q, want_k = heads(before[:, :H * dh], H), heads(before[:, H * dh:(H + Hkv) * dh], Hkv)
         if rotary is not None:
-            for t, heads in ((want_q, H), (want_k, Hkv)):
-                R.revffn_op_rotary(dt, rotary, t[:T], t[:T], _ints(at[:T]), T, max(T, 1), heads, dh, heads * dh, heads * dh, stream=stream)
+            want_q, want_k = (ref.turned(x, at[:T], R.revffn_op_rotary_frequencies(rotary), rotary.interleaved, rotary.magnitude or 1.0) for x in (want_q, want_k))
+            want_k = _np(torch.from_numpy(want_k).float().to(TORCH[dtype]))
         c = self.cache(held, None if single else np.cumsum([0] + list(new)))
         R.revffn_op_cache_append(dt, c, rotary, None if pos is None else _ints(at), None if no_q else q, None if no_q else out, kk, vv, T if single else rows, H, ld,
                                  out.stride(0), ld, ld, stream=stream)
@@ -83,13 +84,14 @@ class Paged:
         owned = np.concatenate([(np.arange(h - n, h) >= 0) & (np.arange(h - n, h) < self.page * self.table.shape[1]) for h, n in zip(held, new)])
         if not no_q:
             mine = torch.from_numpy(owned).cuda()
-            assert torch.equal(out[:T][mine], want_q[:T][mine])
-            rest = before[:, :H * dh] if in_place else torch.full_like(want_q, NAN)
+            # one rounding to float32 and one to the type
+            got = _np(out[:T]).reshape(T, H, dh)[owned]
+            assert (np.abs(got - want_q[owned]) <= (np.abs(want_q[owned]) + 2.0 ** -126) * (2.0 ** -24 + (2.0 ** -8 if dtype == "bf16" else 0)) * (1 + 2.0 ** -8)).all()
+            rest = before[:, :H * dh] if in_place else torch.full_like(before[:, :H * dh], NAN)
             assert torch.equal(out[:T][~mine].nan_to_num(7.0), rest[:T][~mine].nan_to_num(7.0)) and torch.isnan(out[T:]).all()
         if not in_place:
             assert torch.equal(wide.nan_to_num(7.0), before.nan_to_num(7.0))       # the inputs are as they were
-        heads = lambda t: _np(t[:T]).reshape(T, Hkv, dh)
-        self.model.append(self.table, held, new, heads(want_k), heads(before[:, (H + Hkv) * dh:(H + 2 * Hkv) * dh]))
+        self.model.append(self.table, held, new, want_k, heads(before[:, (H + Hkv) * dh:(H + 2 * Hkv) * dh], Hkv))
         self.check()
 
 
@@ -613,17 +615,18 @@ def test_a_served_layer(dtype):
         qkv = product(x, wqkv, sqkv, width, d)
         cache = c.cache(held, np.cumsum([0] + new))
         at = np.concatenate([np.arange(h - n, h) for h, n in zip(held, new)])
-        key = qkv[:, H * dh:(H + Hkv) * dh].contiguous()
-        R.revffn_op_rotary(dt, _rotary(dh), key, key, _ints(at), T, T, Hkv, dh, Hkv * dh, Hkv * dh)
+        key = ref.turned(_np(qkv[:, H * dh:(H + Hkv) * dh]).reshape(T, Hkv, dh), at, R.revffn_op_rotary_frequencies(_rotary(dh)))
+        query = ref.turned(_np(qkv[:, :H * dh]).reshape(T, H, dh), at, R.revffn_op_rotary_frequencies(_rotary(dh)))
         value = qkv[:, (H + Hkv) * dh:]
         R.revffn_op_cache_append(dt, cache, _rotary(dh), None, qkv, qkv, qkv[:, H * dh:], value, T, H, width, width, width, width)
-        c.model.append(c.table, list(held), new, _np(key).reshape(T, Hkv, dh), _np(value).reshape(T, Hkv, dh))
+        c.model.append(c.table, list(held), new, _np(torch.from_numpy(key).float().to(t)), _np(value).reshape(T, Hkv, dh))
         o, lse = torch.empty(T, H * dh, dtype=t, device="cuda"), torch.empty(H, T, dtype=torch.float32, device="cuda")
         desc = R.AttnDesc(dtype=dt, H=H, Hkv=Hkv, dh=dh, Tq=T, ldq=width)
         work = torch.empty(R.revffn_op_attention_cached_workspace(desc, cache), dtype=torch.uint8, device="cuda")
         R.revffn_op_attention_cached(desc, cache, True, 0, qkv, o, lse, work)
         torch.cuda.synchronize()
         c.check()
+        assert np.abs(_np(qkv[:, :H * dh]).reshape(T, H, dh) - query).max() <= np.abs(query).max() * (2.0 ** -8 if dtype == "bf16" else 2.0 ** -23)
         want = ref.attention(c.model, c.table, list(held), new, _np(qkv[:, :H * dh]).reshape(T, H, dh), dtype=dtype)
         assert outside(_np(o).reshape(T, H, dh), *want["o"]) <= 1.0 and outside(_np(lse), *want["lse"]) <= 1.0
         y = product(o, wo, so, d, H * dh)
