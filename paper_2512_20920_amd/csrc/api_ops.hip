@@ -263,8 +263,9 @@ int revffn_op_attention_cached(const revffn_attn_desc* desc, const revffn_cache*
   CachedAttn a;
   TRY(check_cached(desc, cache, &a));
   if ((causal != 0 && causal != 1) || window < 0 || (window && !causal)) return REVFFN_EINVAL;
-  if (a.T > 0 && (!q || !o || !work)) return REVFFN_ENULL;
-  if (a.T > 0 && (work_bytes < cached_attn_bytes(a) || ((uintptr_t)work & 15))) return REVFFN_EINVAL;
+  const size_t need = cached_attn_bytes(a);
+  if (a.T > 0 && (!q || !o || (need && !work))) return REVFFN_ENULL;
+  if (a.T > 0 && (work_bytes < need || ((uintptr_t)work & 15))) return REVFFN_EINVAL;
   if (a.T > 0 && same_place({o, lse}, {q, cache->k, cache->v, cache->k_scale, cache->v_scale})) return REVFFN_EINVAL;
   a.causal = causal; a.window = window; a.q = q; a.out = o; a.lse = lse;
   const bool fits = cached_attn_takes(a);

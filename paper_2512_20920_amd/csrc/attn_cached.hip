@@ -1,12 +1,14 @@
 // Attention over a paged cache of 8-bit numbers (cache.h) on the matrix cores.
 //
-// A wave owns 32 rows, which are (query, head) pairs that share a key head, and walks over the keys in tiles of 32.  It works on transposed scores
-// S^T[key, row] = K Q^T, as the kernels over key ranges do, but nothing goes through LDS: both operands that come from the cache lie in it as a lane
-// needs them, 16 bytes at a time, and turn into bfloat16, their power of two included, without a rounding (v_cvt_scalef32_pk_bf16_fp8).
+// Rows are (query, head) pairs that share a key head.  A wave works on transposed scores S^T[key, row] = K Q^T, as the kernels over key ranges do, but
+// nothing of the cache goes through LDS: both operands that come from it lie there as a lane needs them, 16 bytes at a time, and turn into bfloat16, their
+// power of two included, without a rounding (v_cvt_scalef32_pk_bf16_fp8).  In the form for many rows (32 per wave, tiles of 32 keys, 32x32x16):
 //  * K: row m of the operand is the tile's token 16 ((m >> 2) & 1) + 4 (m >> 3) + (m & 3), so that the 16 scores that a lane gets (rows
 //    8 (e >> 2) + 4 g + (e & 3) of the result, g = lane >> 5) are tokens 16 g + e, in order.  The head's columns are contracted in the order in which
 //    16 bytes of a row hold them: step 2 t takes columns 32 t + 16 g + 0..7, step 2 t + 1 the next eight; Q is loaded alike.
 //  * V: a lane's 16 probabilities are those of 16 tokens in a row, which are the 16 bytes of one column that the cache keeps together.
+// In the form for few rows (16 per workgroup, whose waves share the keys out in tiles of 64, 16x16x32) the same with g = lane >> 4: four runs of 16 tokens,
+// four blocks b of 16 keys whose row m is token 16 (m >> 2) + 4 b + (m & 3).
 // Scores, maxima, sums and accumulators are float32.  bfloat16 calls round the probabilities to bfloat16 as operands; float32 calls take queries
 // and probabilities as three bfloat16 numbers each (24 bits; the cache's numbers need no more than one), so they are float32 throughout.
 #include "attn_range_tiles.h"
@@ -14,10 +16,10 @@
 
 namespace {
 
-constexpr int FEW_ROWS = 96;             // of a sequence and key head: up to here a workgroup's four waves share 32 rows' keys, beyond each has 32 rows
+constexpr int FEW_ROWS = 64;             // of a sequence and key head: up to here groups of 16 rows, beyond groups of 128, 32 for each of four waves
 constexpr int TARGET = 1024;             // workgroups that a call's keys are split for
 
-// What a call does with a sequence.  Keys begin .. end - 1 are seen by some row; cost: tiles of keys for a wave of a workgroup (a group) of rows.
+// What a call does with a sequence.  Keys begin .. end - 1 are seen by some row; cost: tiles of 32 keys for a wave of a workgroup (a group) of rows.
 struct SeqWork { int row0, n, start, begin, end, groups, cost; bool few; };
 __device__ __forceinline__ SeqWork work_of(const CachedAttn& a, int s) {
   SeqWork w;
@@ -28,50 +30,54 @@ __device__ __forceinline__ SeqWork work_of(const CachedAttn& a, int s) {
   w.end = min(len, cache_room(a.c));
   w.begin = a.window ? max(w.start + 1 - a.window, 0) : 0;
   const i64 R = (i64)rows.y * a.G;
-  w.few = R <= FEW_ROWS;
-  w.groups = (int)(w.few ? (R + 31) >> 5 : (R + 127) >> 7);
+  w.few = a.few_only || R <= FEW_ROWS;
+  w.groups = (int)(w.few ? (R + 15) >> 4 : (R + 127) >> 7);
   const int tiles = w.end > w.begin ? ((w.end - 1) >> 5) - (w.begin >> 5) + 1 : 0;
   w.cost = w.few ? (tiles + 3) >> 2 : tiles;
   return w;
 }
 // Into how many parts a group's keys go, if `per` tiles per wave are the aim: up to 64
 __device__ __forceinline__ int splits_of(const CachedAttn& a, const SeqWork& w, int per) {
-  if (!w.few && !a.split_many) return 1;
+  if (a.split == 0 || (!w.few && a.split == 1)) return 1;
+  if (!w.few) per = max(per, 8);                     // (128 rows' parts are work to join)
   return min(max((w.cost + per - 1) / per, 1), 64);
 }
-// tiles per wave that make TARGET workgroups of everything
-__device__ __forceinline__ int tiles_per(const CachedAttn& a) {
-  float sum = 0.f;
-  for (int s0 = 0; s0 < a.c.n_seqs; s0 += 64) {
-    const int s = s0 + (int)(threadIdx.x & 63);
-    if (s < a.c.n_seqs) { const SeqWork w = work_of(a, s); if (w.few || a.split_many) sum += (float)w.groups * (float)w.cost; }
-  }
-  return max((int)(wave_sum(sum) * ((float)a.c.Hkv / TARGET)) + 1, 1);
-}
 // A call's list of workgroups: sequence by sequence, and in it (split, group, key head), key heads fastest (one stays on one XCD if there are eight).
-// Parts of split groups lie in the scratch memory in the same order, one of 32 rows (few) or four per workgroup: slot.
+// Parts of split groups lie in the scratch memory in the same order, in slots of 16 rows: one per workgroup (few) or eight.
+// JOIN: the list of four rows each of the split groups instead.
 struct Item { int s, at, splits; i64 slot; SeqWork w; };
 template <bool JOIN> __device__ __forceinline__ bool find(const CachedAttn& a, int id, Item* x) {
-  const int per = tiles_per(a), lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, n = a.c.n_seqs;
+  SeqWork first = {};
+  if (lane < n) first = work_of(a, lane);
+  int per = 1;                                       // tiles per wave that make TARGET workgroups of everything
+  if (a.split) {
+    float sum = 0.f;
+    for (int s0 = 0; s0 < n; s0 += 64) {
+      const SeqWork w = s0 == 0 ? first : s0 + lane < n ? work_of(a, s0 + lane) : SeqWork{};
+      sum += (float)w.groups * (float)w.cost;
+    }
+    per = max((int)(wave_sum(sum) * ((float)a.c.Hkv / TARGET)) + 1, 1);
+  }
   int before = 0;
   i64 slots = 0;
-  for (int s0 = 0; s0 < a.c.n_seqs; s0 += 64) {
-    int mine = 0, room = 0;
-    if (s0 + lane < a.c.n_seqs) {
-      const SeqWork w = work_of(a, s0 + lane);
-      const int k = splits_of(a, w, per);
-      // (first rows that are out of order can ask for more than there are: no sum overflows, and whoever is past the scratch memory stays out of it)
-      mine = min(JOIN ? (k > 1 ? w.groups * a.c.Hkv : 0) : w.groups * a.c.Hkv * k, 1 << 24);
-      room = min(k > 1 ? w.groups * a.c.Hkv * k * (w.few ? 1 : 4) : 0, 1 << 24);
-    }
+  for (int s0 = 0; s0 < n; s0 += 64) {
+    const SeqWork w = s0 == 0 ? first : s0 + lane < n ? work_of(a, s0 + lane) : SeqWork{};
+    const int k = splits_of(a, w, per);
+    // (first rows that are out of order can ask for more than there are: no sum overflows, and whoever is past the scratch memory stays out of it)
+    const int groups = min(w.groups, 1 << 20) * a.c.Hkv, quads = (int)(((i64)w.n * a.G + 3) >> 2) * a.c.Hkv;
+    const int mine = min(JOIN ? (k > 1 ? quads : 0) : groups * k, 1 << 24);
+    const int room = min(k > 1 ? groups * k * (w.few ? 1 : 8) : 0, 1 << 24);
     const int running = wave_running(mine), all = __builtin_amdgcn_readlane(running, 63), rooms = wave_running(room);
     if (id < before + all) {
       const int l = __builtin_ctzll(__ballot(before + running > id));
       x->s = s0 + l;
       x->at = id - before - (__builtin_amdgcn_readlane(running, l) - __builtin_amdgcn_readlane(mine, l));
       x->slot = slots + __builtin_amdgcn_readlane(rooms, l) - __builtin_amdgcn_readlane(room, l);
-      x->w = work_of(a, x->s);
-      x->splits = splits_of(a, x->w, per);
+      x->splits = __builtin_amdgcn_readlane(k, l);
+      x->w.row0 = __builtin_amdgcn_readlane(w.row0, l); x->w.n = __builtin_amdgcn_readlane(w.n, l); x->w.start = __builtin_amdgcn_readlane(w.start, l);
+      x->w.begin = __builtin_amdgcn_readlane(w.begin, l); x->w.end = __builtin_amdgcn_readlane(w.end, l);
+      x->w.groups = __builtin_amdgcn_readlane(w.groups, l); x->w.cost = __builtin_amdgcn_readlane(w.cost, l); x->w.few = __builtin_amdgcn_readlane((int)w.few, l);
       return true;
     }
     before += all;
@@ -161,6 +167,7 @@ __device__ __forceinline__ float lane_f(float v, int l) { return __builtin_bit_c
 
 // ---- the matrix-core kernel ----
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
 // 8 numbers of the cache times a power of two
 __device__ __forceinline__ bf16x8 eight(unsigned lo, unsigned hi, float scale) {
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
@@ -170,81 +177,298 @@ __device__ __forceinline__ bf16x8 eight(unsigned lo, unsigned hi, float scale) {
 }
 __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 
-// DHP: head width rounded up to 64, 128 or 256.  WHOLE: it is the width.  F32: float32 queries and results.
-template <int DHP, bool WHOLE, bool F32, int MOD>
-__global__ void __launch_bounds__(256, DHP == 256 || F32 ? 1 : 2) cached_attn_k(CachedAttn a) {
-  typedef typename std::conditional<F32, float, bf16>::type T;
-  constexpr int KT = DHP / 32, DT = DHP / 32, Q = F32 ? 3 : 1;
-  constexpr bool AHEAD = DHP <= 128;                 // the next tile is on its way while one is worked on (wider heads have no registers for it)
-  extern __shared__ __attribute__((aligned(16))) float smem[];        // two waves' partial results and statistics
-  Item x;
-  if (!find<false>(a, (int)blockIdx.x, &x)) return;
-  const CacheView& c = a.c;
-  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, col = lane & 31, lg = c.lg, P1 = (1 << lg) - 1;
-  const int dh = WHOLE ? DHP : c.dh;
-  const int rest = x.at / c.Hkv, kh = x.at - rest * c.Hkv, split = rest / x.w.groups;
-  const bool few = x.w.few;
-  const int group = x.w.groups - 1 - (rest - split * x.w.groups);      // (late rows see most)
-  const int blk = few ? group : group * 4 + wv;
-
-  // this lane's row
-  const int r = blk * 32 + col, qi = r / a.G, i = x.w.row0 + qi, h = kh * a.G + (r - qi * a.G), pos = x.w.start + qi;
-  const bool ok = qi < x.w.n;
-  bf16x8 qf[Q][2 * KT];
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+// over the lanes l, l ^ 16, l ^ 32, l ^ 48
+__device__ __forceinline__ float quarters_max(float x) {
+  const unsigned b = __builtin_bit_cast(unsigned, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+  return both_halves_max(fmaxf(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1])));
+}
+__device__ __forceinline__ float quarters_sum(float x) {
+  const unsigned b = __builtin_bit_cast(unsigned, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+  return both_halves_sum(__builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]));
+}
+// 16 columns of a row of queries, as Q numbers each (zeros for a row that is not there)
+template <class T, int Q> __device__ __forceinline__ void load_q16(const T* q, bool ok, bf16x8 (*f)[2]) {
+  float v[16];
 #pragma unroll
-  for (int t = 0; t < KT; t++) {
-    float v[16];
+  for (int u = 0; u < 16; u++) v[u] = 0.f;
+  if (ok) {
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int u = 0; u < 16; u++) v[u] = 0.f;
-    if (ok && (WHOLE || 32 * t + 16 * g < dh)) {
-      const T* q = (const T*)a.q + (i64)i * a.ldq + (i64)h * dh + 32 * t + 16 * g;
-      if constexpr (F32) {
+      for (int u = 0; u < 16; u += 4) { const float4 w = *(const float4*)(q + u); v[u] = w.x; v[u + 1] = w.y; v[u + 2] = w.z; v[u + 3] = w.w; }
+    } else {
 #pragma unroll
-        for (int u = 0; u < 16; u += 4) { const float4 w = *(const float4*)(q + u); v[u] = w.x; v[u + 1] = w.y; v[u + 2] = w.z; v[u + 3] = w.w; }
-      } else {
+      for (int u = 0; u < 16; u += 8) {
+        const bf16x8 w = *(const bf16x8*)(q + u);
 #pragma unroll
-        for (int u = 0; u < 16; u += 8) {
-          const bf16x8 w = *(const bf16x8*)(q + u);
-#pragma unroll
-          for (int k = 0; k < 8; k++) v[u + k] = (float)w[k];
-        }
+        for (int k = 0; k < 8; k++) v[u + k] = (float)w[k];
       }
     }
-#pragma unroll
-    for (int p = 0; p < Q; p++)
-#pragma unroll
-      for (int u = 0; u < 16; u++) {
-        const bf16 b = (bf16)v[u];
-        qf[p][2 * t + (u >> 3)][u & 7] = b;
-        v[u] -= (float)b;
-      }
   }
-  int2 sees = ok ? seen_from(a, pos, x.w.end) : make_int2(0, 0);
-  if (sees.x == sees.y) sees = make_int2(INT_MAX, 0);
-  const int first = wave_imin(sees.x), last = wave_imax(sees.y);
-  const int all_from = wave_imax(ok ? sees.x : 0), all_to = wave_imin(ok ? sees.y : INT_MAX);
-  // this wave's tiles: t0, t0 + step, .. below t1 (of 32 keys, counted from the sequence's first)
-  int t0 = 0, t1 = 0, step = few ? 4 : 1;
-  if (first < last) {
-    const int a0 = first >> 5, n = ((last - 1) >> 5) - a0 + 1, per = (n + x.splits - 1) / x.splits;
-    t0 = a0 + min(split * per, n);
-    t1 = min(t0 + per, a0 + n);
-    if (few) t0 += wv;
+#pragma unroll
+  for (int p = 0; p < Q; p++)
+#pragma unroll
+    for (int u = 0; u < 16; u++) {
+      const bf16 b = (bf16)v[u];
+      f[p][u >> 3][u & 7] = b;
+      v[u] -= (float)b;
+    }
+}
+// the scores' final form (MOD), in units of log2 where there is one; first: distance of the lane's first key
+template <bool F32, int MOD, class S> __device__ __forceinline__ void final_scores(const CachedAttn& a, const ScoreForm& sf, float first, S& s) {
+  if constexpr (MOD != 0) {
+    float keep;
+    if constexpr (F32 && (MOD & CAPPED)) {
+#pragma unroll
+      for (int e = 0; e < 16; e++) s[e] = final_score<MOD & BIASED>(sf, tanhf(s[e] * sf.x1) * (a.cap / a.scale), first - (float)e, &keep);      // (back to units of q.k)
+    } else {
+      tanh_scores<MOD, true>(sf, s);
+#pragma unroll
+      for (int e = 0; e < 16; e++) s[e] = final_score<MOD>(sf, s[e], first - (float)e, &keep);
+    }
   }
-  const int count = t1 > t0 ? (t1 - t0 + step - 1) / step : 0;
-
+}
+__device__ __forceinline__ ScoreForm form_of(const CachedAttn& a, int h, bool ok) {
   ScoreForm sf;
   sf.f = a.scale * LOG2E;
   sf.x1 = a.cap > 0.f ? a.scale / a.cap : 0.f;
   sf.cap2 = a.cap * LOG2E;
   sf.slope2 = a.slopes && ok ? a.slopes[h] * LOG2E : 0.f;
+  return sf;
+}
+// a column's numbers of 16 tokens, of which `keep` are there: what lies behind the last token, or on no page, may be anything
+__device__ __forceinline__ uint4 first_tokens(uint4 v, int keep) {
+  unsigned w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int u = 0; u < 4; u++) { const int b = min(max(keep - 4 * u, 0), 4); w[u] &= b == 4 ? ~0u : (1u << (8 * b)) - 1u; }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// ---- few rows: 16 per workgroup, NW waves share the keys out in tiles of 64, and put their results together in LDS ----
+// Bound by reading the cache, where it is long.  A tile's keys are asked for when the last one's have been multiplied, its values likewise, and the
+// pages two tiles ahead; three waves per SIMD hide the rest.
+template <int DHP, int NW> constexpr unsigned FEW_SMEM = NW * (DHP * 16 + 32) * 4 + 16;
+template <int DHP, bool WHOLE, bool F32, int MOD, int NW>
+__device__ __forceinline__ void few_rows(const CachedAttn& a, const Item& x, float* smem) {
+  typedef typename std::conditional<F32, float, bf16>::type T;
+  constexpr int KT = DHP / 64, DT = DHP / 16, Q = F32 ? 3 : 1;
+  const CacheView& c = a.c;
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, col = lane & 15, lg = c.lg, P1 = (1 << lg) - 1;
+  const int dh = WHOLE ? DHP : c.dh;
+  const int rest = x.at / c.Hkv, kh = x.at - rest * c.Hkv, split = rest / x.w.groups, group = rest - split * x.w.groups;
+
+  const int r = group * 16 + col, qi = r / a.G, i = x.w.row0 + qi, h = kh * a.G + (r - qi * a.G), pos = x.w.start + qi;
+  const bool ok = qi < x.w.n;
+  int2 sees = ok ? seen_from(a, pos, x.w.end) : make_int2(0, 0);
+  if (sees.x == sees.y) sees = make_int2(INT_MAX, 0);
+  const int first = wave_imin(sees.x), last = wave_imax(sees.y);
+  const int all_from = wave_imax(ok ? sees.x : 0), all_to = wave_imin(ok ? sees.y : INT_MAX);
+  // this wave's tiles: t0, t0 + NW, .. below t1 (of 64 keys, counted from the sequence's first)
+  int t0 = 0, t1 = 0;
+  if (first < last) {
+    const int a0 = first >> 6, n = ((last - 1) >> 6) - a0 + 1, per = (n + x.splits - 1) / x.splits;
+    t0 = a0 + min(split * per, n);
+    t1 = min(t0 + per, a0 + n);
+  }
+  t0 += wv;
+
+  // where a lane's keys and values of a tile lie: token 16 gk + .. of the keys, 16 g + .. of the values
+  const int gk = col >> 2;
+  auto page_of = [&](int t, int group) { return t < t1 ? cache_page(c, x.s, (t * 64 + group * 16) >> lg) : -1; };
+  int pk = page_of(t0, gk), pv = page_of(t0, g);
+  uint4 k[4][KT], v[DT];
+  float ks, vs;
+  auto fetch_k = [&](int t, int page) {
+    const i64 block = cache_block(c, max(page, 0), kh);
+    ks = c.ks[block];
+    const unsigned char* p = c.k + ((block << lg) + ((t * 64 + gk * 16) & P1) + (col & 3)) * dh;
+    // (columns past the width read others, which meet zeros of q)
+#pragma unroll
+    for (int b = 0; b < 4; b++)
+#pragma unroll
+      for (int u = 0; u < KT; u++) k[b][u] = *(const uint4*)(p + 4 * b * dh + (WHOLE || 64 * u + 16 * g < dh ? 64 * u + 16 * g : 0));
+  };
+  auto fetch_v = [&](int t, int page) {
+    const i64 block = cache_block(c, max(page, 0), kh);
+    vs = c.vs[block];
+    const unsigned char* p = c.v + ((block << lg) + ((t * 64 + g * 16) & P1)) * dh;
+#pragma unroll
+    for (int d = 0; d < DT; d++) v[d] = *(const uint4*)(p + 16 * (WHOLE || 16 * d + col < dh ? 16 * d + col : 0));
+  };
+  bf16x8 qf[KT][Q][2];
+#pragma unroll
+  for (int t = 0; t < KT; t++) load_q16<T, Q>((const T*)a.q + (i64)i * a.ldq + (i64)h * dh + 64 * t + 16 * g, ok && (WHOLE || 64 * t + 16 * g < dh), qf[t]);
+  const ScoreForm sf = form_of(a, h, ok);
+  const float unit = MOD != 0 ? 1.f : sf.f;
+
+  f32x4 acc[DT];
+#pragma unroll
+  for (int d = 0; d < DT; d++) acc[d] = f32x4{};
+  float m = -INFINITY, l = 0.f;
+  if (t0 < t1) { fetch_k(t0, pk); fetch_v(t0, pv); }
+  int nk = page_of(t0 + NW, gk), nv = page_of(t0 + NW, g);
+  for (int t = t0; t < t1; t += NW) {
+    const int kv = t * 64;
+    f32x16 s;
+#pragma unroll
+    for (int b = 0; b < 4; b++) {
+      f32x4 z = {};
+#pragma unroll
+      for (int u = 0; u < KT; u++) {
+        const bf16x8 k0 = eight(k[b][u].x, k[b][u].y, ks), k1 = eight(k[b][u].z, k[b][u].w, ks);
+#pragma unroll
+        for (int p = 0; p < Q; p++) { z = mfma16(k0, qf[u][p][0], z); z = mfma16(k1, qf[u][p][1], z); }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; e++) s[4 * b + e] = z[e];
+    }
+    const bool more = t + NW < t1;
+    const int vp = pv;
+    if (more) fetch_k(t + NW, nk);
+    final_scores<F32, MOD>(a, sf, (float)(pos - kv - 16 * g), s);
+    const bool bad = vp < 0, any_bad = __any(bad);
+    if (kv < all_from || kv + 64 > all_to || any_bad) {
+      const int lo = max(sees.x, kv) - kv - 16 * g;
+      const unsigned n = (unsigned)max(min(sees.y, kv + 64) - max(sees.x, kv), 0);
+#pragma unroll
+      for (int e = 0; e < 16; e++) if ((unsigned)(e - lo) >= n || bad) s[e] = -INFINITY;
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) mx = fmaxf(fmaxf(mx, s[e]), s[e + 1]);
+    const float mn = fmaxf(m, quarters_max(mx) * unit), ms = mn == -INFINITY ? 0.f : mn;
+    if (__any(mn > m)) {
+      const float alpha = fast_exp2(m - ms);
+      l *= alpha;
+#pragma unroll
+      for (int d = 0; d < DT; d++) acc[d] *= alpha;
+    }
+    m = mn;
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; e++) { s[e] = fast_exp2(MOD != 0 ? s[e] - ms : fmaf(s[e], unit, -ms)); sum += s[e]; }
+    l += sum;
+    bf16x8 pf[Q][2];
+#pragma unroll
+    for (int p = 0; p < Q; p++) {
+      pf[p][0] = acc_to_frag(s, 0);
+      pf[p][1] = acc_to_frag(s, 1);
+#pragma unroll
+      for (int e = 0; e < 16; e++) s[e] -= (float)pf[p][e >> 3][e & 7];
+    }
+    if (kv + 64 > x.w.end || any_bad) {
+      const int keep = bad ? 0 : x.w.end - kv - 16 * g;
+#pragma unroll
+      for (int d = 0; d < DT; d++) v[d] = first_tokens(v[d], keep);
+    }
+#pragma unroll
+    for (int d = 0; d < DT; d++) {
+      const bf16x8 v0 = eight(v[d].x, v[d].y, vs), v1 = eight(v[d].z, v[d].w, vs);
+#pragma unroll
+      for (int p = 0; p < Q; p++) { acc[d] = mfma16(v0, pf[p][0], acc[d]); acc[d] = mfma16(v1, pf[p][1], acc[d]); }
+    }
+    if (more) fetch_v(t + NW, nv);
+    pv = nv;
+    nk = page_of(t + 2 * NW, gk);
+    nv = page_of(t + 2 * NW, g);
+  }
+  l = quarters_sum(l);
+
+  // the waves' maxima and sums, then their results in units of the common maximum: [wave][16 columns' block][lane]
+  float* ml = smem + NW * DHP * 16;                  // [wave][maximum, sum][16 rows]
+  unsigned* odd = (unsigned*)(ml + NW * 32);
+  if (lane < 16) { ml[wv * 32 + lane] = m; ml[wv * 32 + 16 + lane] = l; }
+  if (threadIdx.x == 0) *odd = 0;
+  __syncthreads();
+  float M = -INFINITY, tot = 0.f;
+#pragma unroll
+  for (int w = 0; w < NW; w++) M = fmaxf(M, ml[w * 32 + col]);
+  const float Ms = M == -INFINITY ? 0.f : M, mine = fast_exp2(m - Ms);
+#pragma unroll
+  for (int w = 0; w < NW; w++) tot = fmaf(fast_exp2(ml[w * 32 + col] - Ms), ml[w * 32 + 16 + col], tot);
+  float4* part = (float4*)smem;
+#pragma unroll
+  for (int d = 0; d < DT; d++) part[(wv * DT + d) * 64 + lane] = make_float4(acc[d][0] * mine, acc[d][1] * mine, acc[d][2] * mine, acc[d][3] * mine);
+  __syncthreads();
+  const float inv = tot == 0.f ? 0.f : 1.f / tot;
+  const i64 slot = x.slot + x.at;
+  bool bad = false;
+#pragma unroll
+  for (int d = wv; d < DT; d += NW) {                // (a thread's row is its lane's)
+    float4 z = part[d * 64 + lane];
+#pragma unroll
+    for (int w = 1; w < NW; w++) { const float4 y = part[(w * DT + d) * 64 + lane]; z.x += y.x; z.y += y.y; z.z += y.z; z.w += y.w; }
+    const int at = 16 * d + 4 * g;
+    if (x.splits > 1) {
+      if (ok && slot < a.slots) *(float4*)(a.parts + (slot * 16 + col) * DHP + at) = z;
+    } else if (ok && (WHOLE || at < dh)) {
+      bad = bad || !(fmaf(z.x, 0.f, fmaf(z.y, 0.f, fmaf(z.z, 0.f, z.w * 0.f))) == 0.f);
+      typedef __attribute__((ext_vector_type(4))) T V4;
+      V4 o;
+      o[0] = from_f<T>(z.x * inv); o[1] = from_f<T>(z.y * inv); o[2] = from_f<T>(z.z * inv); o[3] = from_f<T>(z.w * inv);
+      *(V4*)((T*)a.out + (i64)i * a.ldo + (i64)h * dh + at) = o;
+    }
+  }
+  if (x.splits > 1) {
+    if (threadIdx.x < 16 && ok && slot < a.slots) a.stats[slot * 16 + col] = make_float2(M, tot);
+    return;
+  }
+  if (threadIdx.x < 16 && ok && a.lse) a.lse[(i64)h * a.T + i] = tot == 0.f ? -INFINITY : (M + log2f(tot)) * LN2;
+  // a value that is not finite: seen by its row, or only multiplied by zero in a tile that it sees a part of?
+  unsigned long long b = __ballot(bad);
+  if (b) { b |= b >> 32; b |= b >> 16; if (lane == 0) atomicOr(odd, (unsigned)b & 0xffffu); }
+  __syncthreads();
+  const unsigned again = *odd;
+  if (again)
+    for (int n = wv; n < 16; n += NW)
+      if ((again >> n) & 1) {
+        const int rr = group * 16 + n, qr = rr / a.G;
+        cached_row<T>(a, x.s, x.w.row0 + qr, kh * a.G + (rr - qr * a.G), x.w.start + qr, x.w.end, smem + wv * DHP);
+      }
+}
+
+// ---- many rows: 32 per wave, tiles of 32 keys ----
+// DHP: head width rounded up to 64, 128 or 256.  WHOLE: it is the width.  F32: float32 queries and results.
+template <int DHP, bool WHOLE, bool F32, int MOD>
+__device__ __forceinline__ void many_rows(const CachedAttn& a, const Item& x, float* smem) {
+  typedef typename std::conditional<F32, float, bf16>::type T;
+  constexpr int KT = DHP / 32, DT = DHP / 32, Q = F32 ? 3 : 1;
+  constexpr bool AHEAD = DHP <= 128;                 // the next tile is on its way while one is worked on (wider heads have no registers for it)
+  const CacheView& c = a.c;
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, col = lane & 31, lg = c.lg, P1 = (1 << lg) - 1;
+  const int dh = WHOLE ? DHP : c.dh;
+  const int rest = x.at / c.Hkv, kh = x.at - rest * c.Hkv, split = rest / x.w.groups;
+  const int group = x.w.groups - 1 - (rest - split * x.w.groups);      // (late rows see most)
+  const int blk = group * 4 + wv;
+
+  // this lane's row
+  const int r = blk * 32 + col, qi = r / a.G, i = x.w.row0 + qi, h = kh * a.G + (r - qi * a.G), pos = x.w.start + qi;
+  const bool ok = qi < x.w.n;
+  bf16x8 qf[KT][Q][2];
+#pragma unroll
+  for (int t = 0; t < KT; t++) load_q16<T, Q>((const T*)a.q + (i64)i * a.ldq + (i64)h * dh + 32 * t + 16 * g, ok && (WHOLE || 32 * t + 16 * g < dh), qf[t]);
+  int2 sees = ok ? seen_from(a, pos, x.w.end) : make_int2(0, 0);
+  if (sees.x == sees.y) sees = make_int2(INT_MAX, 0);
+  const int first = wave_imin(sees.x), last = wave_imax(sees.y);
+  const int all_from = wave_imax(ok ? sees.x : 0), all_to = wave_imin(ok ? sees.y : INT_MAX);
+  // this wave's tiles: t0 .. t1 - 1 (of 32 keys, counted from the sequence's first)
+  int t0 = 0, t1 = 0;
+  if (first < last) {
+    const int a0 = first >> 5, n = ((last - 1) >> 5) - a0 + 1, per = (n + x.splits - 1) / x.splits;
+    t0 = a0 + min(split * per, n);
+    t1 = min(t0 + per, a0 + n);
+  }
+  const int count = max(t1 - t0, 0);
+  const ScoreForm sf = form_of(a, h, ok);
   const float unit = MOD != 0 ? 1.f : sf.f;
 
   // pages and scales of 64 tiles at a time, one tile per lane: of its first 16 tokens and of its second
   int page0 = 0, page1 = 0;
   float ks0 = 0.f, ks1 = 0.f, vs0 = 0.f, vs1 = 0.f;
   auto look_up = [&](int n) {
-    const int kv = (t0 + (n + lane) * step) * 32;
+    const int kv = (t0 + n + lane) * 32;
     const bool there = n + lane < count;
     page0 = there ? cache_page(c, x.s, kv >> lg) : -1;
     page1 = there ? cache_page(c, x.s, (kv + 16) >> lg) : -1;
@@ -254,12 +478,14 @@ __global__ void __launch_bounds__(256, DHP == 256 || F32 ? 1 : 2) cached_attn_k(
   const int tok = 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3);
   struct Tile { uint4 k[KT], v[DT]; float ks, vs; bool bad; };
   auto fetch = [&](int n, Tile& t) {                 // the n-th tile; its pages have been looked up
-    const int l = n & 63, kv = (t0 + n * step) * 32;
+    const int l = n & 63, kv = (t0 + n) * 32;
     const int p0 = __builtin_amdgcn_readlane(page0, l), p1 = __builtin_amdgcn_readlane(page1, l);
     const i64 s0 = (cache_block(c, max(p0, 0), kh) << lg) + (kv & P1), s1 = (cache_block(c, max(p1, 0), kh) << lg) + ((kv + 16) & P1);
     t.bad = g ? p1 < 0 : p0 < 0;
-    t.ks = tok & 16 ? lane_f(ks1, l) : lane_f(ks0, l);
-    t.vs = g ? lane_f(vs1, l) : lane_f(vs0, l);
+    // (read by all lanes before any chooses: in a branch, a lane that is not in it may be the one that is read)
+    const float k0 = lane_f(ks0, l), k1 = lane_f(ks1, l), v0 = lane_f(vs0, l), v1 = lane_f(vs1, l);
+    t.ks = tok & 16 ? k1 : k0;
+    t.vs = g ? v1 : v0;
     const unsigned char* k = c.k + ((tok & 16 ? s1 : s0) + (tok & 15)) * dh;
     const unsigned char* v = c.v + (g ? s1 : s0) * dh;
     // (columns past the width: K reads other columns' numbers, which meet zeros of q; results of V's are not stored)
@@ -279,7 +505,7 @@ __global__ void __launch_bounds__(256, DHP == 256 || F32 ? 1 : 2) cached_attn_k(
     if (AHEAD) fetch(0, cur);
   }
   for (int n = 0; n < count; n++) {
-    const int kv = (t0 + n * step) * 32;
+    const int kv = (t0 + n) * 32;
     if constexpr (AHEAD) {
       if (n + 1 < count) {
         if (((n + 1) & 63) == 0) look_up(n + 1);
@@ -294,23 +520,9 @@ __global__ void __launch_bounds__(256, DHP == 256 || F32 ? 1 : 2) cached_attn_k(
     for (int t = 0; t < KT; t++) {
       const bf16x8 k0 = eight(cur.k[t].x, cur.k[t].y, cur.ks), k1 = eight(cur.k[t].z, cur.k[t].w, cur.ks);
 #pragma unroll
-      for (int p = 0; p < Q; p++) { s = mfma(k0, qf[p][2 * t], s); s = mfma(k1, qf[p][2 * t + 1], s); }
+      for (int p = 0; p < Q; p++) { s = mfma(k0, qf[t][p][0], s); s = mfma(k1, qf[t][p][1], s); }
     }
-    if constexpr (MOD != 0) {
-      const float d0 = (float)(pos - kv - 16 * g);
-      float keep;
-      if constexpr (F32 && (MOD & CAPPED)) {
-        if (a.cap > 0.f)
-#pragma unroll
-          for (int e = 0; e < 16; e++) s[e] = tanhf(s[e] * sf.x1) * (a.cap / a.scale);      // (back to units of q.k)
-#pragma unroll
-        for (int e = 0; e < 16; e++) s[e] = final_score<MOD & BIASED>(sf, s[e], d0 - (float)e, &keep);
-      } else {
-        tanh_scores<MOD, true>(sf, s);
-#pragma unroll
-        for (int e = 0; e < 16; e++) s[e] = final_score<MOD>(sf, s[e], d0 - (float)e, &keep);
-      }
-    }
+    final_scores<F32, MOD>(a, sf, (float)(pos - kv - 16 * g), s);
     const bool any_bad = __any(cur.bad);
     if (kv < all_from || kv + 32 > all_to || any_bad) {
       const int lo = max(sees.x, kv) - kv - 16 * g;
@@ -341,14 +553,10 @@ __global__ void __launch_bounds__(256, DHP == 256 || F32 ? 1 : 2) cached_attn_k(
 #pragma unroll
       for (int e = 0; e < 16; e++) s[e] -= (float)pf[p][e >> 3][e & 7];
     }
-    if (kv + 32 > x.w.end || any_bad) {              // what lies behind the last token, or on no page, may be anything: zeros
+    if (kv + 32 > x.w.end || any_bad) {
       const int keep = cur.bad ? 0 : x.w.end - kv - 16 * g;
 #pragma unroll
-      for (int d = 0; d < DT; d++) {
-        unsigned* w = (unsigned*)&cur.v[d];
-#pragma unroll
-        for (int u = 0; u < 4; u++) { const int b = min(max(keep - 4 * u, 0), 4); w[u] &= b == 4 ? ~0u : (1u << (8 * b)) - 1u; }
-      }
+      for (int d = 0; d < DT; d++) cur.v[d] = first_tokens(cur.v[d], keep);
     }
 #pragma unroll
     for (int d = 0; d < DT; d++) {
@@ -360,43 +568,11 @@ __global__ void __launch_bounds__(256, DHP == 256 || F32 ? 1 : 2) cached_attn_k(
   }
   l = both_halves_sum(l);
 
-  // ---- a few rows' waves put their results together: waves 2 and 3 give theirs to 0 and 1, then 1 to 0 ----
-  if (few) {
-    constexpr int FLOATS = DT * 16 * 64;
-    auto give = [&](int to) {
-      float* p = smem + to * (FLOATS + 128);
-#pragma unroll
-      for (int d = 0; d < DT; d++)
-#pragma unroll
-        for (int e = 0; e < 16; e++) p[(d * 16 + e) * 64 + lane] = acc[d][e];
-      p[FLOATS + lane] = m;
-      p[FLOATS + 64 + lane] = l;
-    };
-    auto take = [&](int from) {
-      const float* p = smem + from * (FLOATS + 128);
-      const float m2 = p[FLOATS + lane], l2 = p[FLOATS + 64 + lane], mn = fmaxf(m, m2), ms = mn == -INFINITY ? 0.f : mn;
-      const float w = fast_exp2(m - ms), w2 = fast_exp2(m2 - ms);
-#pragma unroll
-      for (int d = 0; d < DT; d++)
-#pragma unroll
-        for (int e = 0; e < 16; e++) acc[d][e] = fmaf(acc[d][e], w, p[(d * 16 + e) * 64 + lane] * w2);
-      l = l * w + l2 * w2;
-      m = mn;
-    };
-    if (wv >= 2) give(wv - 2);
-    __syncthreads();
-    if (wv < 2) take(wv);
-    __syncthreads();
-    if (wv == 1) give(0);
-    __syncthreads();
-    if (wv > 0) return;
-    take(0);
-  }
   if (x.splits > 1) {
-    const i64 slot = x.slot + (few ? (i64)x.at : (i64)x.at * 4 + wv);
-    if (!ok || slot >= a.slots) return;
-    if (g == 0) a.stats[slot * 32 + col] = make_float2(m, l);
-    float* p = a.parts + (slot * 32 + col) * DHP;
+    const i64 slot = x.slot + (i64)x.at * 8 + wv * 2;                 // (two of 16 rows each, one behind the other)
+    if (!ok || slot + 1 >= a.slots) return;
+    if (g == 0) a.stats[slot * 16 + col] = make_float2(m, l);
+    float* p = a.parts + (slot * 16 + col) * DHP;
 #pragma unroll
     for (int d = 0; d < DT; d++)
 #pragma unroll
@@ -436,6 +612,21 @@ __global__ void __launch_bounds__(256, DHP == 256 || F32 ? 1 : 2) cached_attn_k(
       }
 }
 
+template <int DHP, bool WHOLE, bool F32, int MOD>
+__global__ void __launch_bounds__(256, DHP == 256 || F32 ? 1 : 2) cached_attn_k(CachedAttn a) {
+  extern __shared__ __attribute__((aligned(16))) float smem[];
+  Item x;
+  if (!find<false>(a, (int)blockIdx.x, &x)) return;
+  if (x.w.few) few_rows<DHP, WHOLE, F32, MOD, 4>(a, x, smem);
+  else many_rows<DHP, WHOLE, F32, MOD>(a, x, smem);
+}
+template <int DHP, bool WHOLE, bool F32, int MOD, int NW>
+__global__ void __launch_bounds__(NW * 64, DHP == 256 || F32 ? 1 : DHP == 64 ? 3 : 2) cached_few_k(CachedAttn a) {
+  extern __shared__ __attribute__((aligned(16))) float smem[];
+  Item x;
+  if (find<false>(a, (int)blockIdx.x, &x)) few_rows<DHP, WHOLE, F32, MOD, NW>(a, x, smem);
+}
+
 // Joins the parts of split groups, a wave per row
 template <class T, int DHP> __global__ void __launch_bounds__(256) cached_join_k(CachedAttn a) {
   __shared__ float lds[4][DHP];
@@ -443,15 +634,16 @@ template <class T, int DHP> __global__ void __launch_bounds__(256) cached_join_k
   Item x;
   if (!find<true>(a, (int)blockIdx.x, &x)) return;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), Hkv = a.c.Hkv, dh = a.c.dh;
-  const int group = x.at / Hkv, kh = x.at - group * Hkv, blocks = x.w.few ? 1 : 4;      // (of the list of groups; the parts' order is turned)
-  if (x.slot + (i64)x.splits * x.w.groups * Hkv * blocks > a.slots) return;
-  for (int r = wv; r < blocks * 32; r += 4) {
-    const int rr = group * blocks * 32 + r, qi = rr / a.G;
-    if (qi >= x.w.n) return;
-    const int i = x.w.row0 + qi, h = kh * a.G + (rr - qi * a.G);
-    auto part = [&](int split) {                     // first row of the part's 32
-      const i64 at = ((i64)split * x.w.groups + (x.w.groups - 1 - group)) * Hkv + kh;
-      return ((x.slot + at * blocks + (r >> 5)) * 32 + (r & 31));
+  const int quad = x.at / Hkv, kh = x.at - quad * Hkv, rr = quad * 4 + wv, qi = rr / a.G;
+  if (qi >= x.w.n) return;
+  // of the list of workgroups that made the parts: the row's group, and which of its slots and rows
+  const int lrows = x.w.few ? 4 : 7, slots = x.w.few ? 1 : 8, g0 = rr >> lrows, group = x.w.few ? g0 : x.w.groups - 1 - g0, in = rr & ((1 << lrows) - 1);
+  if (x.slot + (i64)x.splits * x.w.groups * Hkv * slots > a.slots) return;
+  const int i = x.w.row0 + qi, h = kh * a.G + (rr - qi * a.G);
+  {
+    auto part = [&](int split) {
+      const i64 at = ((i64)split * x.w.groups + group) * Hkv + kh;
+      return (x.slot + at * slots) * 16 + in;
     };
     const float2 st = lane < x.splits ? a.stats[part(lane)] : make_float2(-INFINITY, 0.f);
     const float M = wave_max(st.x), Ms = M == -INFINITY ? 0.f : M;
@@ -476,7 +668,7 @@ template <class T, int DHP> __global__ void __launch_bounds__(256) cached_join_k
     for (int u = 0; u < C; u++) z = fmaf(v[u], 0.f, z);
     if (!__all(z == 0.f)) {
       cached_row<T>(a, x.s, i, h, x.w.start + qi, x.w.end, lds[wv]);
-      continue;
+      return;
     }
     const float inv = tot == 0.f ? 0.f : 1.f / tot;
     T* o = (T*)a.out + (i64)i * a.ldo + (i64)h * dh;
@@ -486,31 +678,39 @@ template <class T, int DHP> __global__ void __launch_bounds__(256) cached_join_k
   }
 }
 
-// Most groups that a call can have: sequences of up to 96 rows per key head make one per 32, others one per 128
+// Most groups that a call can have
 i64 most_groups(const CachedAttn& a) {
   const i64 rows = (i64)a.T * a.G, seqs = a.c.n_seqs < a.T ? a.c.n_seqs : a.T;
-  const i64 by_row = rows / 32 + seqs, by_seq = rows / 128 + 3 * seqs;
-  return by_row < by_seq ? by_row : by_seq;
+  const i64 by_row = rows / 16 + seqs, by_seq = rows / 128 + (FEW_ROWS / 16) * seqs;
+  return a.few_only || by_row < by_seq ? by_row : by_seq;
 }
 int padded(int dh) { return dh <= 64 ? 64 : dh <= 128 ? 128 : 256; }
 i64 most_slots(const CachedAttn& a) {
-  const i64 heads = most_groups(a) * a.c.Hkv;
-  return (heads + TARGET) * (a.split_many && (i64)a.T * a.G > FEW_ROWS ? 4 : 1);
+  return a.split ? (most_groups(a) * a.c.Hkv + TARGET) * (a.split == 2 && !a.few_only ? 8 : 1) : 0;
 }
 
-template <int DHP, bool WHOLE, bool F32, int MOD> void go(const CachedAttn& a, hipStream_t s) {
-  constexpr size_t smem = 2 * (DHP / 32 * 16 * 64 + 128) * sizeof(float);
-  const i64 heads = most_groups(a) * a.c.Hkv;
-  if (smem > 65536) {
-    static std::atomic<unsigned long long> attr_mask{0};
-    if (attr_needed(attr_mask)) {
-      (void)hipFuncSetAttribute((const void*)cached_attn_k<DHP, WHOLE, F32, MOD>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-      attr_done(attr_mask);
-    }
+template <class K> void launch(K kernel, std::atomic<unsigned long long>& attr_mask, i64 grid, int block, unsigned smem, const CachedAttn& a, hipStream_t s) {
+  if (smem > 65536 && attr_needed(attr_mask)) {
+    (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    attr_done(attr_mask);
   }
-  hipLaunchKernelGGL((cached_attn_k<DHP, WHOLE, F32, MOD>), dim3((unsigned)(heads + TARGET)), dim3(256), smem, s, a);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(block), smem, s, a);
+}
+template <int DHP, bool WHOLE, bool F32, int MOD> void go(const CachedAttn& a, hipStream_t s) {
+  static std::atomic<unsigned long long> mask[3];
+  const i64 grid = most_groups(a) * a.c.Hkv + (a.split ? TARGET : 0);
+  if (!a.few_only) launch(cached_attn_k<DHP, WHOLE, F32, MOD>, mask[0], grid, 256, FEW_SMEM<DHP, 4>, a, s);
+  else {
+    // eight waves where nothing is split, if their registers allow it
+    constexpr int NW = DHP == 256 || F32 ? 4 : 8;
+    if (a.split) launch(cached_few_k<DHP, WHOLE, F32, MOD, 4>, mask[1], grid, 256, FEW_SMEM<DHP, 4>, a, s);
+    else launch(cached_few_k<DHP, WHOLE, F32, MOD, NW>, mask[2], grid, NW * 64, FEW_SMEM<DHP, NW>, a, s);
+  }
+  if (!a.split) return;
+  const i64 rows = (i64)a.T * a.G, seqs = a.c.n_seqs < a.T ? a.c.n_seqs : a.T, few = (i64)FEW_ROWS * seqs;
+  const i64 joined = a.few_only || a.split == 2 || rows < few ? rows : few;      // rows that may have been split
   typedef typename std::conditional<F32, float, bf16>::type T;
-  hipLaunchKernelGGL((cached_join_k<T, DHP>), dim3((unsigned)heads), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((cached_join_k<T, DHP>), dim3((unsigned)((joined / 4 + seqs) * a.c.Hkv)), dim3(256), 0, s, a);
 }
 template <int DHP, bool F32> void go(const CachedAttn& a, hipStream_t s) {
   // (without a part of the score's form its kernel has no instructions of it; a scale that is not positive is multiplied, not put into the exponential)
@@ -527,9 +727,14 @@ template <int DHP, bool F32> void go(const CachedAttn& a, hipStream_t s) {
 
 }  // namespace
 
-// prompts fill the chip by themselves from TARGET groups on
-void cached_attn_plan(CachedAttn* a) { a->split_many = most_groups(*a) * a->c.Hkv < TARGET; }
-size_t cached_attn_bytes(const CachedAttn& a) { return (size_t)most_slots(a) * 32 * (padded(a.c.dh) * 4 + 8); }
+// What the sizes alone say.  One row per sequence, or few in all: the form for few rows throughout.  Its keys need no splitting up to what eight waves
+// do in some 5 us, and then there is no second launch.  Prompts' keys are split where there is not a workgroup of theirs for every CU.
+void cached_attn_plan(CachedAttn* a) {
+  const i64 room = (i64)a->c.max_pages << a->c.lg;
+  a->few_only = (i64)a->T * a->G <= FEW_ROWS || a->T <= a->c.n_seqs;
+  a->split = a->few_only && room <= 2048 ? 0 : most_groups(*a) * a->c.Hkv < 256 ? 2 : 1;
+}
+size_t cached_attn_bytes(const CachedAttn& a) { return (size_t)most_slots(a) * 16 * (padded(a.c.dh) * 4 + 8); }
 bool cached_attn_takes(const CachedAttn& a) {
   const int es = a.dt == 0 ? 4 : 2;
   return (a.dt == 1 || a.c.dh <= 128) && (a.ldq | a.ldo) * es % 16 == 0 && ((uintptr_t)a.q | (uintptr_t)a.out) % 16 == 0;
@@ -544,7 +749,7 @@ void launch_cached_attn(CachedAttn a, void* work, bool rows, hipStream_t s) {
   }
   a.slots = most_slots(a);
   a.parts = (float*)work;
-  a.stats = (float2*)(a.parts + a.slots * 32 * padded(a.c.dh));
+  a.stats = (float2*)(a.parts + a.slots * 16 * padded(a.c.dh));
   const int w = padded(a.c.dh);
   if (a.dt == 0) { if (w == 64) go<64, true>(a, s); else go<128, true>(a, s); }
   else { if (w == 64) go<64, false>(a, s); else if (w == 128) go<128, false>(a, s); else go<256, false>(a, s); }

@@ -419,11 +419,12 @@ struct CachedAttn {
   int dt, H, G, T, causal, window;
   i64 ldq, ldo;
   float scale, cap;
-  float* parts; float2* stats;           // scratch of split calls: `slots` parts of 32 rows
+  float* parts; float2* stats;           // scratch of split calls: `slots` parts of 16 rows
   i64 slots;
-  int split_many;                        // whether prompts may be split along their keys
+  int few_only;                          // every sequence in the form for few rows
+  int split;                             // whose keys may be split: 0 nobody's, 1 few rows', 2 prompts' too
 };
-void cached_attn_plan(CachedAttn* a);               // split_many, from the sizes alone
+void cached_attn_plan(CachedAttn* a);               // few_only and split, from the sizes alone
 size_t cached_attn_bytes(const CachedAttn& a);
 bool cached_attn_takes(const CachedAttn& a);        // whether the matrix-core kernels do (else row by row)
 void launch_cached_attn(CachedAttn a, void* work, bool rows, hipStream_t s);

@@ -87,7 +87,7 @@ def test_append_refuses(lib):
 
 
 def test_attention_refuses(lib):
-    c, d = cache(), desc()
+    c, d = cache(max_pages=400), desc()
     assert attend(lib, None, c) == ENULL and attend(lib, d, None) == ENULL
     for kw in (dict(q=None), dict(o=None), dict(work=None)):
         assert attend(lib, d, c, **kw) == ENULL
@@ -107,8 +107,10 @@ def test_attention_refuses(lib):
 
 def test_workspaces_do_not_depend_on_addresses(lib):
     d = desc(Tq=300)
-    sizes = {lib.revffn_op_attention_cached_workspace(ctypes.byref(d), ctypes.byref(cache(**kw))) for kw in (dict(), dict(k=16 * P), dict(table=9 * P))}
-    assert len(sizes) == 1
+    sizes = {lib.revffn_op_attention_cached_workspace(ctypes.byref(d), ctypes.byref(cache(max_pages=99, **kw))) for kw in (dict(), dict(k=16 * P), dict(table=9 * P))}
+    assert len(sizes) == 1 and min(sizes) > 0
+    short = desc(Tq=3)                                       # (single tokens of short sequences need none)
+    assert lib.revffn_op_attention_cached_workspace(ctypes.byref(short), ctypes.byref(cache())) == 0
 
 
 def test_integer_products_refuse(lib):

@@ -217,6 +217,8 @@ SHAPES = {
     "width_144": (2, 1, 144, 16, [50, 40], [20, 1], {}),
     "width_256": (2, 1, 256, 64, [100, 40], [35, 1], {}),
     "width_256_capped": (2, 2, 256, 16, [60, 40], [5, 1], dict(cap=4.0)),
+    "width_208_prompt": (2, 1, 208, 32, [170], [100], {}),
+    "width_256_prompt": (2, 2, 256, 16, [170, 5], [150, 5], dict(cap=4.0, bias=True)),
     "more_rows_than_tokens": (2, 2, 64, 16, [5, 0, 20], [9, 3, 1], {}),
     "nothing_held": (2, 2, 64, 16, [0, 0], [2, 1], dict(causal=False)),
 }
