@@ -6,6 +6,7 @@
 // by loads straight from memory.  Rows past the end, and chunks past k, are loaded as zeros; the bytes of the last chunk that lie past k are
 // cleared in a's fragments.
 #include "lds_load.h"
+#include <math.h>
 
 typedef __attribute__((ext_vector_type(4))) int i32x4;
 typedef __attribute__((ext_vector_type(16))) int i32x16;
@@ -153,6 +154,106 @@ __global__ void __launch_bounds__(NW * 64) gemm_i8_k(GemmI8 g) {
       if (m0 + wm + i * 32 < g.M && n0 + wn + j * 32 < g.N) put_block<T>(g, m0 + wm + i * 32, n0 + wn + j * 32, acc[i][j]);
 }
 
+// ---- 256 x 256 in phases ----
+// A k-tile is two phases over half tiles, each half tile refilled as soon as it has been read, and the two waves of a SIMD are half a phase apart: one
+// multiplies while the other reads its fragments and asks for loads (the scheme of gemm_mfma.hip's tile, whose barriers and counts these are):
+//   phase 0: read A0 B0 B1, multiply A0 x (B0 B1), ask for A1 of k-tile t + 1
+//   phase 1: read A1,       multiply A1 x (B0 B1), ask for A0 B0 B1 of k-tile t + 2
+// 8 waves as 2 x 4, a wave owns 64 rows x 2 x 32 columns of each half.  At the end of a read segment a wave waits for all but its youngest 8
+// loads, which covers the half tiles that the next phase reads; fragments are in registers when it ends, so a half tile is overwritten only after
+// everybody has read it.
+template <class T> __global__ void __launch_bounds__(512) gemm_i8_phased_k(GemmI8 g) {
+  constexpr unsigned HALF = 128 * KB, STAGE = 4 * HALF;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  int by, bx;
+  if (!place((g.M + 255) / 256, (g.N + 255) / 256, &by, &bx)) return;
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m0 = by * 256, n0 = bx * 256;
+  const int wm = (wv >> 2) * 64, wn = (wv & 3) * 32;  // inside a half
+  const u32x4 da = rows_desc(g.a, g.lda, m0, g.M, g.K), db = rows_desc(g.b, g.ldb, n0, g.N, g.K);
+  const int nk = (g.K + KB - 1) / KB, whole = g.K / KB;
+  unsigned base[4][2];
+  int chunk[2];
+#pragma unroll
+  for (int i = 0; i < 2; i++) {
+    const int pos = (wv * 2 + i) * 64 + lane, r = pos >> 3, c = (pos & 7) ^ ((r >> 1) & 7);
+    chunk[i] = c * 16;
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+      base[h][i] = m0 + h * 128 + r < g.M ? (unsigned)(h * 128 + r) * (unsigned)g.lda + c * 16u : OOB;
+      base[2 + h][i] = n0 + h * 128 + r < g.N ? (unsigned)(h * 128 + r) * (unsigned)g.ldb + c * 16u : OOB;
+    }
+  }
+  const unsigned lw = __builtin_amdgcn_readfirstlane(lds_address(smem) + (unsigned)wv * 2048u);
+  auto issue = [&](int kt, int hf) {                 // this wave's part of half tile hf (A0 A1 B0 B1) of k-tile kt
+    const unsigned dst = lw + (unsigned)(kt & 1) * STAGE + hf * HALF, soff = (unsigned)kt * KB;
+#pragma unroll
+    for (int i = 0; i < 2; i++)
+      load_lds_b128_s(hf < 2 ? da : db, dst + i * 1024u, kt < whole || kt * KB + chunk[i] < g.K ? base[hf][i] : OOB, soff);
+  };
+  i32x16 acc[4][2];
+#pragma unroll
+  for (int i = 0; i < 4; i++)
+#pragma unroll
+    for (int j = 0; j < 2; j++) acc[i][j] = i32x16{};
+  auto issue3 = [&](int kt) { issue(kt, 0); issue(kt, 2); issue(kt, 3); };
+  issue3(0); issue(0, 1);
+  issue3(1);
+  wait_vmcnt<8>();                                   // A0 B0 B1 of k-tile 0
+  __builtin_amdgcn_s_barrier();
+  if (wv >= 4) __builtin_amdgcn_s_barrier();         // waves 4-7 half a phase behind
+  const bool lower = g.M - m0 > 128;
+  i32x4 fa[2][4], fb[2][4];
+  for (int kt = 0; kt < nk; kt++) {
+    const unsigned char* st = smem + (unsigned)(kt & 1) * STAGE;
+    const bool ragged = kt == whole && (g.K & 15);
+#pragma unroll
+    for (int p = 0; p < 2; p++) {
+      if (p == 0 || lower) {
+#pragma unroll
+        for (int kk = 0; kk < 4; kk++) {
+#pragma unroll
+          for (int i = 0; i < 2; i++) fa[i][kk] = fragment(st + p * HALF, wm + i * 32 + (lane & 31), kk, lane);
+          if (p == 0)
+#pragma unroll
+            for (int j = 0; j < 2; j++) fb[j][kk] = fragment(st + (2 + j) * HALF, wn + (lane & 31), kk, lane);
+        }
+        if (ragged) {
+#pragma unroll
+          for (int kk = 0; kk < 4; kk++)
+#pragma unroll
+            for (int i = 0; i < 2; i++) fa[i][kk] = first_bytes(fa[i][kk], g.K - kt * KB - kk * 32 - (lane >> 5) * 16);
+        }
+      }
+      if (p == 0) issue(kt + 1, 1); else issue3(kt + 2);
+      wait_vmcnt<8>();
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
+      if (p == 0 || lower)
+#pragma unroll
+      for (int kk = 0; kk < 4; kk++)
+#pragma unroll
+        for (int i = 0; i < 2; i++)
+#pragma unroll
+          for (int j = 0; j < 2; j++) acc[p * 2 + i][j] = mfma(fa[i][kk], fb[j][kk], acc[p * 2 + i][j]);
+      __builtin_amdgcn_s_setprio(0);
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+    }
+  }
+  if (wv < 4) __builtin_amdgcn_s_barrier();
+  wait_vmcnt<0>();                                   // the zero-filled loads past the last k-tile
+#pragma unroll
+  for (int i = 0; i < 4; i++)
+#pragma unroll
+    for (int j = 0; j < 2; j++) {
+      const int m = m0 + (i >> 1) * 128 + wm + (i & 1) * 32, n = n0 + j * 128 + wn;
+      if (m < g.M && n < g.N) put_block<T>(g, m, n, acc[i][j]);
+    }
+}
+
 // ---- any shape and alignment: a thread per result ----
 template <class T> __global__ void __launch_bounds__(256) gemm_i8_any_k(GemmI8 g) {
   const int n = blockIdx.x * 256 + threadIdx.x;
@@ -167,19 +268,43 @@ template <class T> __global__ void __launch_bounds__(256) gemm_i8_any_k(GemmI8 g
   }
 }
 
-template <class T, int BM, int BN, int WGM, int NW, int NS> void go(const GemmI8& g, hipStream_t s) {
-  constexpr size_t smem = (size_t)NS * (BM + BN) * KB;
-  static std::atomic<unsigned long long> attr_mask{0};
+template <class K> void launch(K kernel, std::atomic<unsigned long long>& attr_mask, int BM, int BN, int threads, size_t smem, const GemmI8& g, hipStream_t s) {
   if (attr_needed(attr_mask)) {
-    (void)hipFuncSetAttribute((const void*)gemm_i8_k<T, BM, BN, WGM, NW, NS>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     attr_done(attr_mask);
   }
   const i64 tiles = (i64)cdiv(g.M, BM) * cdiv(g.N, BN);
-  hipLaunchKernelGGL((gemm_i8_k<T, BM, BN, WGM, NW, NS>), dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(NW * 64), smem, s, g);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(threads), smem, s, g);
+}
+template <class T, int BM, int BN, int WGM, int NW, int NS> void go(const GemmI8& g, hipStream_t s) {
+  static std::atomic<unsigned long long> mask{0};
+  launch(gemm_i8_k<T, BM, BN, WGM, NW, NS>, mask, BM, BN, NW * 64, (size_t)NS * (BM + BN) * KB, g, s);
+}
+// Which shape a product gets: the one with the least rounds of workgroups times what a round takes per 128 k's (us, measured with every CU busy):
+//   256 x 256 in phases 1.93, 128 x 256 1.20, 128 x 128 0.72, 64 x 64 (two per CU) 0.49.
+// Measured, bfloat16 results, us for these four: 8192 x 14336, k 4096: 437 541 648 886 (2.2 * 10^15 multiplications and additions a second); 8192 x 2048,
+// k 2048: 39 45 50 71; 2048 x 11264, k 2048: 66 63 73 96; 611 x 11264, k 2048: 30 22 25 33; 2048 x 2048, k 2048: 29 19 15 19; 611 x 2048, k 2048:
+// 28 18 12 11; 256 x 4096, k 4096: 44 28 19 15; 8 x 6144, k 2048: 20 15 11 8.
+int form_for(const GemmI8& g) {
+  const struct { int form, bm, bn, round; float us; } shapes[] = {{2, 256, 256, 256, 1.93f}, {3, 128, 256, 256, 1.20f}, {4, 128, 128, 256, 0.72f}, {5, 64, 64, 512, 0.49f}};
+  int best = 5;
+  float least = INFINITY;
+  for (const auto& x : shapes) {
+    const i64 tiles = (i64)cdiv(g.M, x.bm) * cdiv(g.N, x.bn);
+    const float cost = (float)((tiles + x.round - 1) / x.round) * x.us;
+    if (cost < least) { least = cost; best = x.form; }
+  }
+  return best;
 }
 template <class T> void go(const GemmI8& g, int form, hipStream_t s) {
-  if (form == 1) hipLaunchKernelGGL((gemm_i8_any_k<T>), dim3(cdiv(g.N, 256), g.M < 4096 ? g.M : 4096), dim3(256), 0, s, g);
-  else go<T, 128, 128, 4, 8, 4>(g, s);
+  static std::atomic<unsigned long long> mask{0};
+  switch (form ? form : form_for(g)) {
+    case 1: hipLaunchKernelGGL((gemm_i8_any_k<T>), dim3(cdiv(g.N, 256), g.M < 4096 ? g.M : 4096), dim3(256), 0, s, g); break;
+    case 2: launch(gemm_i8_phased_k<T>, mask, 256, 256, 512, 2 * 512 * KB, g, s); break;
+    case 3: go<T, 128, 256, 2, 8, 3>(g, s); break;
+    case 4: go<T, 128, 128, 4, 8, 4>(g, s); break;
+    default: go<T, 64, 64, 2, 4, 4>(g, s);
+  }
 }
 
 }  // namespace
