@@ -1,8 +1,8 @@
 // New keys and values into the pages of a cache, keys and queries turned to their positions on the way.
 //
-// A workgroup takes the new rows of one page (a sequence's pages one after the other: find_item) and one head's values, one head's keys or a few
-// heads' queries (several heads where a page's rows of one are too few): each reads its rows once, into registers, and writes them once.  For keys
-// and values the largest of all comes between, from the waves' maxima in LDS.
+// A workgroup takes the new rows of one page (a sequence's pages one after the other: find_item) and a head's or two's keys or values (several heads at a
+// time where a page's rows of one are too few): it reads them once, into registers, and writes them once, the largest of all of a head's in between, from
+// the waves' maxima in LDS.  Other workgroups take four or eight rows' queries, which nothing but the launch has in common with these.
 //
 // Keys are turned in float64: sines, cosines and products, so that a key differs from the exact one by its rounding alone.  In float32 one
 // in some 10^6 keys ends up on the other side of a border between two 8-bit numbers, half a step of 2^-4 of its value.  It costs no more: the series below
@@ -25,20 +25,19 @@ __device__ __forceinline__ double2 turn_of(double turns) {
   return make_double2(q == 1 || q == 2 ? -a : a, q >= 2 ? -b : b);
 }
 
-// Eight columns of a row.  WIDE: 16 bytes at a time.
-template <class T, bool WIDE> __device__ __forceinline__ void load8(const T* p, float* x) {
-  if constexpr (WIDE && sizeof(T) == 2) {
-    typedef __attribute__((ext_vector_type(8))) T V;
-    const V v = *(const V*)p;
-#pragma unroll
-    for (int i = 0; i < 8; i++) x[i] = to_f(v[i]);
-  } else if constexpr (WIDE) {
+// Eight columns of a row as they lie (WIDE: 16 bytes at a time), and as numbers
+template <class T> struct Raw8 { __attribute__((ext_vector_type(8))) T v; };
+template <class T, bool WIDE> __device__ __forceinline__ Raw8<T> load8(const T* p) {
+  Raw8<T> r;
+  if constexpr (WIDE && sizeof(T) == 2) r.v = *(const decltype(r.v)*)p;
+  else if constexpr (WIDE) {
     const float4 u = *(const float4*)p, w = *(const float4*)(p + 4);
-    x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = w.x; x[5] = w.y; x[6] = w.z; x[7] = w.w;
+    r.v[0] = u.x; r.v[1] = u.y; r.v[2] = u.z; r.v[3] = u.w; r.v[4] = w.x; r.v[5] = w.y; r.v[6] = w.z; r.v[7] = w.w;
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; i++) x[i] = to_f(p[i]);
+    for (int i = 0; i < 8; i++) r.v[i] = p[i];
   }
+  return r;
 }
 template <class T, bool WIDE> __device__ __forceinline__ void store8(T* p, const float* x) {
   if constexpr (WIDE && sizeof(T) == 2) {
@@ -86,145 +85,235 @@ __device__ __forceinline__ float to_f32(double d) {
   asm("" : "+v"(f));
   return f;
 }
+// Where the two halves of unit cu of a head lie: 16 columns, which are 8 pairs where they are turned (cu < dims / 16)
+template <bool INTER> __device__ __forceinline__ int first_half(const CacheAppend& a, int cu) { return INTER || cu >= a.dims >> 4 ? 16 * cu : 8 * cu; }
+template <bool INTER> __device__ __forceinline__ int second_half(const CacheAppend& a, int cu) { return INTER || cu >= a.dims >> 4 ? 16 * cu + 8 : a.dims / 2 + 8 * cu; }
+// the unit's 16 numbers, turned (turn: where its 8 cosines and sines are)
+template <class T, bool INTER> __device__ __forceinline__ void turned(const Raw8<T>& first, const Raw8<T>& second, bool turn, const double2* cs, float* v) {
+#pragma unroll
+  for (int i = 0; i < 8; i++) { v[i] = to_f(first.v[i]); v[8 + i] = to_f(second.v[i]); }
+  if (turn) {
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      float &p = v[INTER ? 2 * i : i], &q = v[INTER ? 2 * i + 1 : 8 + i];
+      const double dp = p, dq = q;
+      p = to_f32(fma(dp, cs[i].x, -(dq * cs[i].y)));
+      q = to_f32(fma(dq, cs[i].x, dp * cs[i].y));
+    }
+  }
+}
+__device__ __forceinline__ double2 angle(const CacheAppend& a, int pos, int pair) {
+  double2 r = turn_of((double)pos * a.freq[pair]);
+  r.x *= a.mag; r.y *= a.mag;
+  return r;
+}
+
+// Queries: a wave per row, whose angles it works out once, into LDS, and streams all heads past them
+template <class T, bool INTER, bool WIDE> __device__ __forceinline__ void turn_queries(const CacheAppend& a, i64 i, double2* cs) {
+  const CacheView& c = a.c;
+  const int lane = threadIdx.x & 63;
+  if (i >= a.T) return;
+  for (int s0 = 0; s0 < c.n_seqs; s0 += 64) {
+    int2 r = make_int2(0, 0);
+    if (s0 + lane < c.n_seqs) r = cache_rows(c, s0 + lane, a.T);
+    const unsigned long long hit = __ballot(i >= r.x && i < r.x + r.y);
+    if (!hit) continue;
+    const int l = __builtin_ctzll(hit), at = cache_len(c, s0 + l) - __builtin_amdgcn_readlane(r.y, l) + (int)(i - __builtin_amdgcn_readlane(r.x, l));
+    if (at < 0 || at >= cache_room(c)) return;       // (a row without a place)
+    const int pos = a.pos ? a.pos[i] : at, upr = c.dh >> 4, units = a.H * upr;
+    const T* q = (const T*)a.q + i * a.ldq;
+    T* o = (T*)a.q_out + i * a.ldqo;
+    constexpr int N = 4;                             // units whose loads are on their way together
+    for (int u0 = lane; u0 - lane < units; u0 += 64 * N) {
+      Raw8<T> x[N], y[N];
+      int cu[N], at[N];
+#pragma unroll
+      for (int n = 0; n < N; n++) {
+        const int u = min(u0 + 64 * n, units - 1), h = u / upr;
+        cu[n] = u - h * upr;
+        at[n] = h * c.dh;
+        x[n] = load8<T, WIDE>(q + at[n] + first_half<INTER>(a, cu[n]));
+        y[n] = load8<T, WIDE>(q + at[n] + second_half<INTER>(a, cu[n]));
+      }
+      if (u0 == lane) {
+        for (int p = lane; p < a.dims >> 1; p += 64) cs[p] = angle(a, pos, p);
+        wave_lds_fence();
+      }
+#pragma unroll
+      for (int n = 0; n < N; n++) {
+        float v[16];
+        turned<T, INTER>(x[n], y[n], cu[n] < a.dims >> 4, cs + 8 * cu[n], v);
+        if (u0 + 64 * n < units) {
+          store8<T, WIDE>(o + at[n] + first_half<INTER>(a, cu[n]), v);
+          store8<T, WIDE>(o + at[n] + second_half<INTER>(a, cu[n]), v + 8);
+        }
+      }
+    }
+    return;
+  }
+}
+
 // A head's rows of a page are `units` of 16 columns: UN per lane of WPH waves.  A workgroup has WPH waves if those are more than four, else four, and
-// 4 / WPH heads.  Roles by blockIdx.y: values, keys (vblocks workgroups each), queries (qloop times as many heads one after the other).
+// 4 / WPH heads at a time, `loop` (1 or 2) of them one after the other, all of whose loads are asked for first.  Roles by blockIdx.x: the pages' values
+// and keys (vblocks workgroups of each role for each of `visits` pages), then the queries.
 template <class T, int UN, int WPH, bool INTER, bool WIDE>
-__global__ void __launch_bounds__(WPH > 4 ? WPH * 64 : 256) cache_append_k(CacheAppend a, int vblocks, int qloop) {
+__global__ void __launch_bounds__(WPH > 4 ? WPH * 64 : 256) cache_append_k(CacheAppend a, int visits, int vblocks, int loop) {
   constexpr int WAVES = WPH > 4 ? WPH : 4, HEADS = WAVES / WPH, LANES = 64 * WPH;
-  __shared__ float tops[WAVES];
+  __shared__ float tops[2][WAVES];
+  __shared__ double2 turns[WAVES][ROTARY_MAX_DIMS / 2];
   const CacheView& c = a.c;
   const int wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), hw = wv / WPH, tid = (int)threadIdx.x - hw * LANES;
+  const int role = (int)blockIdx.x / visits, visit = (int)blockIdx.x - role * visits;
+  if (role >= 2 * vblocks) {                         // (queries: beyond the pages' workgroups)
+    turn_queries<T, INTER, WIDE>(a, (i64)((int)blockIdx.x - 2 * vblocks * visits) * WAVES + wv, turns[wv]);
+    return;
+  }
   const int P = 1 << c.lg, room = cache_room(c), dh = c.dh;
   int s, nth;
   auto pages_of = [&](int s) {
     const int n = cache_rows(c, s, a.T).y, len = cache_len(c, s), first = max(len - n, 0), end = min(len, room);
     return end > first ? ((end - 1) >> c.lg) - (first >> c.lg) + 1 : 0;
   };
-  if (!find_item(c.n_seqs, (int)blockIdx.x, pages_of, &s, &nth)) return;
+  if (!find_item(c.n_seqs, visit, pages_of, &s, &nth)) return;
   const int2 rows = cache_rows(c, s, a.T);
   const int len = cache_len(c, s), start = len - rows.y, first = max(start, 0), p = (first >> c.lg) + nth, at0 = p << c.lg;
   const int page = cache_page(c, s, p), r0 = max(first - at0, 0), r1 = min(min(len, room) - at0, P);      // rows r0 .. r1 - 1 of the page
   const i64 token0 = (i64)rows.x + (at0 - start);    // row 0 of the page, as a row of the call (may lie before the first)
-  const int role = (int)blockIdx.y < vblocks ? 0 : (int)blockIdx.y < 2 * vblocks ? 1 : 2;
-  if (role < 2 && page < 0) return;
+  if (page < 0) return;
+  const bool keys = role >= vblocks;
+  const int h0 = (keys ? role - vblocks : role) * loop * HEADS + hw;           // then h0 + HEADS
 
   // the unit to use: the least that brings `top` of all the head's waves within 448, and not less than the page's (where it holds rows already)
-  auto unit_for = [&](float top, float old) {
+  auto unit_for = [&](float top, float old, int n) {
     top = wave_max(top);
     if constexpr (WPH > 1) {
-      if ((threadIdx.x & 63) == 0) tops[wv] = top;
+      if ((threadIdx.x & 63) == 0) tops[n][wv] = top;
       __syncthreads();
 #pragma unroll
-      for (int w = 0; w < WPH; w++) top = fmaxf(top, tops[hw * WPH + w]);
+      for (int w = 0; w < WPH; w++) top = fmaxf(top, tops[n][hw * WPH + w]);
     }
     const float now = power_for(top);
     return r0 > 0 ? fmaxf(now, old) : now;
   };
 
-  if (role == 0) {                                   // values: 16 tokens of two columns per lane, which are 16 bytes of each column
-    const int h = (int)blockIdx.y * HEADS + hw;
-    const bool live = h < c.Hkv;
-    const i64 block = cache_block(c, page, live ? h : 0);
-    unsigned char* vp = c.v + (block << c.lg) * dh;
-    const float old = c.vs[block];
+  if (!keys) {                                       // values: 16 tokens of two columns per lane, which are 16 bytes of each column
     static_assert(UN <= 2, "a lane's 32 values are two units");
+    typedef __attribute__((ext_vector_type(2))) T V2;
     const int u = tid, g = u / (dh >> 1), col = 2 * (u - g * (dh >> 1)), t0 = 16 * g;
-    float x[2][16], top = 0.f;
+    V2 raw[2][16];
+    float olds[2];
 #pragma unroll
-    for (int t = 0; t < 16; t++) {
-      x[0][t] = x[1][t] = 0.f;
-      const int r = t0 + t;
-      if (live && r >= r0 && r < r1) {
-        const T* v = (const T*)a.v + (token0 + r) * a.ldv + (i64)h * dh + col;
-        if constexpr (WIDE) {
-          typedef __attribute__((ext_vector_type(2))) T V;
-          const V w = *(const V*)v;
-          x[0][t] = to_f(w[0]); x[1][t] = to_f(w[1]);
-        } else { x[0][t] = to_f(v[0]); x[1][t] = to_f(v[1]); }
+    for (int n = 0; n < 2; n++) {
+      const int h = h0 + n * HEADS;
+      const bool live = n < loop && h < c.Hkv;
+      olds[n] = live ? c.vs[cache_block(c, page, h)] : 0.f;
+#pragma unroll
+      for (int t = 0; t < 16; t++) {
+        raw[n][t] = V2{};
+        const int r = t0 + t;
+        if (live && r >= r0 && r < r1) {
+          const T* v = (const T*)a.v + (token0 + r) * a.ldv + (i64)h * dh + col;
+          if constexpr (WIDE) raw[n][t] = *(const V2*)v;
+          else { raw[n][t][0] = v[0]; raw[n][t][1] = v[1]; }
+        }
       }
     }
 #pragma unroll
-    for (int t = 0; t < 16; t++) top = larger_finite(larger_finite(top, x[0][t]), x[1][t]);
-    const float now = unit_for(top, old), inv = 1.f / now, again = old * inv;
-    const bool more = r0 > 0 && now > old;
-    if (!live) return;
-    if (tid == 0) c.vs[block] = now;
-    if (t0 >= P || t0 >= r1 || (t0 + 16 <= r0 && !more)) return;
-    const bool whole = t0 >= r0 && t0 + 16 <= r1;
+    for (int n = 0; n < 2; n++) {
+      if (n >= loop) break;
+      const int h = h0 + n * HEADS;
+      const bool live = h < c.Hkv;
+      const float old = olds[n];
+      float x[2][16], top = 0.f;
 #pragma unroll
-    for (int k = 0; k < 2; k++) {
-      uint4* at = (uint4*)(vp + (i64)(t0 * dh + 16 * (col + k)));
-      uint4 held = make_uint4(0, 0, 0, 0);
-      if (!whole) held = *at;
-      unsigned w[4] = {held.x, held.y, held.z, held.w};
-#pragma unroll
-      for (int i = 0; i < 4; i++) {
-        const float* y = x[k] + 4 * i;
-        const unsigned mine = byte_mask(t0 + 4 * i, r0, r1), below = byte_mask(t0 + 4 * i, 0, r0);
-        unsigned keep = w[i];
-        if (more) keep = (rescaled(keep, again) & below) | (keep & ~below);
-        const unsigned fresh = four_e4m3(in_units(y[0], inv), in_units(y[1], inv), in_units(y[2], inv), in_units(y[3], inv));
-        w[i] = (fresh & mine) | (keep & ~mine);
+      for (int t = 0; t < 16; t++) {
+        x[0][t] = to_f(raw[n][t][0]);
+        x[1][t] = to_f(raw[n][t][1]);
+        top = larger_finite(larger_finite(top, x[0][t]), x[1][t]);
       }
-      *at = make_uint4(w[0], w[1], w[2], w[3]);
+      const float now = unit_for(top, old, n), inv = 1.f / now, again = old * inv;
+      const bool more = r0 > 0 && now > old;
+      if (!live || t0 >= P || t0 >= r1) continue;
+      const i64 block = cache_block(c, page, h);
+      unsigned char* vp = c.v + (block << c.lg) * dh;
+      if (tid == 0) c.vs[block] = now;
+      if (t0 + 16 <= r0 && !more) continue;
+      const bool whole = t0 >= r0 && t0 + 16 <= r1;
+#pragma unroll
+      for (int k = 0; k < 2; k++) {
+        uint4* at = (uint4*)(vp + (i64)(t0 * dh + 16 * (col + k)));
+        uint4 held = make_uint4(0, 0, 0, 0);
+        if (!whole) held = *at;
+        unsigned w[4] = {held.x, held.y, held.z, held.w};
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+          const float* y = x[k] + 4 * i;
+          const unsigned mine = byte_mask(t0 + 4 * i, r0, r1), below = byte_mask(t0 + 4 * i, 0, r0);
+          unsigned keep = w[i];
+          if (more) keep = (rescaled(keep, again) & below) | (keep & ~below);
+          const unsigned fresh = four_e4m3(in_units(y[0], inv), in_units(y[1], inv), in_units(y[2], inv), in_units(y[3], inv));
+          w[i] = (fresh & mine) | (keep & ~mine);
+        }
+        *at = make_uint4(w[0], w[1], w[2], w[3]);
+      }
     }
     return;
   }
 
-  const int upr = dh >> 4, turned = a.dims >> 4;
-  int row[UN], ca[UN], cb[UN];
-  bool in[UN], turn[UN];
-  double2 cs[UN][8];
+  const int upr = dh >> 4;
+  int row[UN], cu[UN];
+  bool in[UN];
+  Raw8<T> xa[2][UN], xb[2][UN];
+  float olds[2];
 #pragma unroll
   for (int j = 0; j < UN; j++) {
-    const int u = tid + LANES * j, r = u / upr, cu = u - r * upr;
+    const int u = tid + LANES * j, r = u / upr;
+    cu[j] = u - r * upr;
     row[j] = r0 + r;
     in[j] = row[j] < r1;
-    turn[j] = cu < turned;
-    ca[j] = INTER || !turn[j] ? 16 * cu : 8 * cu;
-    cb[j] = INTER || !turn[j] ? 16 * cu + 8 : a.dims / 2 + 8 * cu;
-    if (in[j] && turn[j]) {
+  }
+#pragma unroll
+  for (int n = 0; n < 2; n++) {
+    const int h = h0 + n * HEADS;
+    const bool live = n < loop && h < c.Hkv;
+    olds[n] = live ? c.ks[cache_block(c, page, h)] : 0.f;
+#pragma unroll
+    for (int j = 0; j < UN; j++)
+      if (live && in[j]) {
+        const T* k = (const T*)a.k + (token0 + row[j]) * a.ldk + (i64)h * dh;
+        xa[n][j] = load8<T, WIDE>(k + first_half<INTER>(a, cu[j]));
+        xb[n][j] = load8<T, WIDE>(k + second_half<INTER>(a, cu[j]));
+      }
+  }
+  double2 cs[UN][8];
+#pragma unroll
+  for (int j = 0; j < UN; j++)
+    if (in[j] && cu[j] < a.dims >> 4) {
       const int pos = a.pos ? a.pos[token0 + row[j]] : at0 + row[j];
 #pragma unroll
-      for (int i = 0; i < 8; i++) {
-        cs[j][i] = turn_of((double)pos * a.freq[8 * cu + i]);
-        cs[j][i].x *= a.mag; cs[j][i].y *= a.mag;
-      }
+      for (int i = 0; i < 8; i++) cs[j][i] = angle(a, pos, 8 * cu[j] + i);
     }
-  }
-  auto load_turned = [&](const T* x, int j, float* v) {
-    load8<T, WIDE>(x + ca[j], v);
-    load8<T, WIDE>(x + cb[j], v + 8);
-    if (turn[j]) {
 #pragma unroll
-      for (int i = 0; i < 8; i++) {
-        float &p = v[INTER ? 2 * i : i], &q = v[INTER ? 2 * i + 1 : 8 + i];
-        const double dp = p, dq = q;
-        const double tp = fma(dp, cs[j][i].x, -(dq * cs[j][i].y)), tq = fma(dq, cs[j][i].x, dp * cs[j][i].y);
-        p = to_f32(tp);
-        q = to_f32(tq);
-      }
-    }
-  };
-  if (role == 1) {
-    const int h = ((int)blockIdx.y - vblocks) * HEADS + hw;
+  for (int n = 0; n < 2; n++) {
+    if (n >= loop) break;
+    const int h = h0 + n * HEADS;
     const bool live = h < c.Hkv;
-    const i64 block = cache_block(c, page, live ? h : 0);
-    unsigned char* kp = c.k + (block << c.lg) * dh;
-    const float old = c.ks[block];
+    const float old = olds[n];
     float x[UN][16], top = 0.f;
 #pragma unroll
     for (int j = 0; j < UN; j++)
       if (live && in[j]) {
-        load_turned((const T*)a.k + (token0 + row[j]) * a.ldk + (i64)h * dh, j, x[j]);
+        turned<T, INTER>(xa[n][j], xb[n][j], cu[j] < a.dims >> 4, cs[j], x[j]);
 #pragma unroll
         for (int i = 0; i < 16; i++) {
           x[j][i] = to_f(from_f<T>(x[j][i]));        // (a key is rounded to float32, to its type, and then to 8 bits)
           top = larger_finite(top, x[j][i]);
         }
       }
-    const float now = unit_for(top, old), inv = 1.f / now, again = old * inv;
-    if (!live) return;
+    const float now = unit_for(top, old, n), inv = 1.f / now, again = old * inv;
+    if (!live) continue;
+    const i64 block = cache_block(c, page, h);
+    unsigned char* kp = c.k + (block << c.lg) * dh;
     if (tid == 0) c.ks[block] = now;
     if (r0 > 0 && now > old)                         // what the page holds already, in the new unit
       for (int o = tid * 16; o < r0 * dh; o += LANES * 16) {
@@ -238,39 +327,22 @@ __global__ void __launch_bounds__(WPH > 4 ? WPH * 64 : 256) cache_append_k(Cache
         float* y = x[j];
 #pragma unroll
         for (int i = 0; i < 16; i++) y[i] = in_units(y[i], inv);
-        *(uint2*)(kp + row[j] * dh + ca[j]) = make_uint2(four_e4m3(y[0], y[1], y[2], y[3]), four_e4m3(y[4], y[5], y[6], y[7]));
-        *(uint2*)(kp + row[j] * dh + cb[j]) = make_uint2(four_e4m3(y[8], y[9], y[10], y[11]), four_e4m3(y[12], y[13], y[14], y[15]));
-      }
-    return;
-  }
-  for (int n = 0; n < qloop; n++) {
-    const int h = (((int)blockIdx.y - 2 * vblocks) * qloop + n) * HEADS + hw;
-    if (h >= a.H) return;
-#pragma unroll
-    for (int j = 0; j < UN; j++)
-      if (in[j]) {
-        float v[16];
-        load_turned((const T*)a.q + (token0 + row[j]) * a.ldq + (i64)h * dh, j, v);
-        T* o = (T*)a.q_out + (token0 + row[j]) * a.ldqo + (i64)h * dh;
-        store8<T, WIDE>(o + ca[j], v);
-        store8<T, WIDE>(o + cb[j], v + 8);
+        *(uint2*)(kp + row[j] * dh + first_half<INTER>(a, cu[j])) = make_uint2(four_e4m3(y[0], y[1], y[2], y[3]), four_e4m3(y[4], y[5], y[6], y[7]));
+        *(uint2*)(kp + row[j] * dh + second_half<INTER>(a, cu[j])) = make_uint2(four_e4m3(y[8], y[9], y[10], y[11]), four_e4m3(y[12], y[13], y[14], y[15]));
       }
   }
 }
 
 template <class T, int UN, int WPH> static void launch(const CacheAppend& a, i64 visits, bool wide, hipStream_t s) {
   constexpr int WAVES = WPH > 4 ? WPH : 4, HEADS = WAVES / WPH;
-  const int vblocks = cdiv(a.c.Hkv, HEADS), groups = a.q ? cdiv(a.H, HEADS) : 0;
-  // heads of queries one after the other where that leaves workgroups enough: their angles are worked out once
-  int qloop = (int)(visits * groups / 1024);
-  qloop = qloop < 1 ? 1 : qloop > 4 ? 4 : qloop;
-  const dim3 grid((unsigned)visits, 2 * vblocks + (groups ? cdiv(groups, qloop) : 0)), block(WAVES * 64);
+  const int loop = visits * cdiv(a.c.Hkv, HEADS) >= 512 ? 2 : 1, vblocks = cdiv(a.c.Hkv, HEADS * loop);
+  const dim3 grid((unsigned)(visits * 2 * vblocks + (a.q ? cdiv(a.T, WAVES) : 0))), block(WAVES * 64);
   if (a.interleaved) {
-    if (wide) hipLaunchKernelGGL((cache_append_k<T, UN, WPH, true, true>), grid, block, 0, s, a, vblocks, qloop);
-    else hipLaunchKernelGGL((cache_append_k<T, UN, WPH, true, false>), grid, block, 0, s, a, vblocks, qloop);
+    if (wide) hipLaunchKernelGGL((cache_append_k<T, UN, WPH, true, true>), grid, block, 0, s, a, (int)visits, vblocks, loop);
+    else hipLaunchKernelGGL((cache_append_k<T, UN, WPH, true, false>), grid, block, 0, s, a, (int)visits, vblocks, loop);
   } else {
-    if (wide) hipLaunchKernelGGL((cache_append_k<T, UN, WPH, false, true>), grid, block, 0, s, a, vblocks, qloop);
-    else hipLaunchKernelGGL((cache_append_k<T, UN, WPH, false, false>), grid, block, 0, s, a, vblocks, qloop);
+    if (wide) hipLaunchKernelGGL((cache_append_k<T, UN, WPH, false, true>), grid, block, 0, s, a, (int)visits, vblocks, loop);
+    else hipLaunchKernelGGL((cache_append_k<T, UN, WPH, false, false>), grid, block, 0, s, a, (int)visits, vblocks, loop);
   }
 }
 template <class T> static void launch(const CacheAppend& a, i64 visits, bool wide, hipStream_t s) {
