@@ -17,7 +17,6 @@
 namespace {
 
 constexpr int FEW_ROWS = 64;             // of a sequence and key head: up to here groups of 16 rows, beyond groups of 128, 32 for each of four waves
-constexpr int TARGET = 1024;             // workgroups that a call's keys are split for
 
 // What a call does with a sequence.  Keys begin .. end - 1 are seen by some row; cost: tiles of 32 keys for a wave of a workgroup (a group) of rows.
 struct SeqWork { int row0, n, start, begin, end, groups, cost; bool few; };
@@ -50,14 +49,26 @@ template <bool JOIN> __device__ __forceinline__ bool find(const CachedAttn& a, i
   const int lane = threadIdx.x & 63, n = a.c.n_seqs;
   SeqWork first = {};
   if (lane < n) first = work_of(a, lane);
-  int per = 1;                                       // tiles per wave that make TARGET workgroups of everything
+  int per = 1;                                       // tiles per wave
   if (a.split) {
-    float sum = 0.f;
+    // as many as make a.target workgroups of everything: with one more, those and one for each group are always enough.  Rounded up to whole workgroups
+    // for each group that may be some too many to be on the CUs together, and then per grows until they are (lists of up to 64 sequences).
+    float sum = 0.f, groups = 0.f;
     for (int s0 = 0; s0 < n; s0 += 64) {
       const SeqWork w = s0 == 0 ? first : s0 + lane < n ? work_of(a, s0 + lane) : SeqWork{};
       sum += (float)w.groups * (float)w.cost;
+      groups += (float)w.groups;
     }
-    per = max((int)(wave_sum(sum) * ((float)a.c.Hkv / TARGET)) + 1, 1);
+    const float heads = (float)a.c.Hkv;
+    per = max((int)(wave_sum(sum) * (heads / (float)a.target)) + 1, 1);
+    if (per > 1 && n <= 64) {
+      const float most = fmaxf((float)a.target, wave_sum(groups) * heads);
+      for (int i = 0; i < 8; i++) {
+        const float all = wave_sum((float)first.groups * (float)splits_of(a, first, per)) * heads;
+        if (all <= most) break;
+        per = max(per + 1, (int)((float)per * all / most));
+      }
+    }
   }
   int before = 0;
   i64 slots = 0;
@@ -646,21 +657,25 @@ template <class T, int DHP> __global__ void __launch_bounds__(256) cached_join_k
       return (x.slot + at * slots) * 16 + in;
     };
     const float2 st = lane < x.splits ? a.stats[part(lane)] : make_float2(-INFINITY, 0.f);
+    float p[16][C];
+    auto load = [&](int k0) {
+#pragma unroll
+      for (int k = 0; k < 16; k++)
+#pragma unroll
+        for (int u = 0; u < C; u++) p[k][u] = k0 + k < x.splits ? a.parts[part(k0 + k) * DHP + lane * C + u] : 0.f;
+    };
+    load(0);                                         // (on their way with the statistics)
     const float M = wave_max(st.x), Ms = M == -INFINITY ? 0.f : M;
     const float w = st.y == 0.f ? 0.f : exp2f(st.x - Ms);
     const float tot = wave_sum(w * st.y);
     float v[C] = {};
     for (int k0 = 0; k0 < x.splits; k0 += 16) {
-      float p[16][C];
-#pragma unroll
-      for (int k = 0; k < 16; k++)
-#pragma unroll
-        for (int u = 0; u < C; u++) p[k][u] = k0 + k < x.splits ? a.parts[part(k0 + k) * DHP + lane * C + u] : 0.f;
+      if (k0) load(k0);
 #pragma unroll
       for (int k = 0; k < 16; k++) {
-        const float f = lane_f(w, (k0 + k) & 63);
+        const float f = lane_f(w, (k0 + k) & 63);    // (0 behind the last)
 #pragma unroll
-        for (int u = 0; u < C; u++) v[u] = fmaf(k0 + k < x.splits ? f : 0.f, p[k][u], v[u]);
+        for (int u = 0; u < C; u++) v[u] = fmaf(f, p[k][u], v[u]);
       }
     }
     float z = 0.f;
@@ -686,7 +701,7 @@ i64 most_groups(const CachedAttn& a) {
 }
 int padded(int dh) { return dh <= 64 ? 64 : dh <= 128 ? 128 : 256; }
 i64 most_slots(const CachedAttn& a) {
-  return a.split ? (most_groups(a) * a.c.Hkv + TARGET) * (a.split == 2 && !a.few_only ? 8 : 1) : 0;
+  return a.split ? (most_groups(a) * a.c.Hkv + a.target) * (a.split == 2 && !a.few_only ? 8 : 1) : 0;
 }
 
 template <class K> void launch(K kernel, std::atomic<unsigned long long>& attr_mask, i64 grid, int block, unsigned smem, const CachedAttn& a, hipStream_t s) {
@@ -698,12 +713,12 @@ template <class K> void launch(K kernel, std::atomic<unsigned long long>& attr_m
 }
 template <int DHP, bool WHOLE, bool F32, int MOD> void go(const CachedAttn& a, hipStream_t s) {
   static std::atomic<unsigned long long> mask[3];
-  const i64 grid = most_groups(a) * a.c.Hkv + (a.split ? TARGET : 0);
+  const i64 grid = most_groups(a) * a.c.Hkv + (a.split ? a.target : 0);
   if (!a.few_only) launch(cached_attn_k<DHP, WHOLE, F32, MOD>, mask[0], grid, 256, FEW_SMEM<DHP, 4>, a, s);
   else {
     // eight waves where nothing is split, if their registers allow it
     constexpr int NW = DHP == 256 || F32 ? 4 : 8;
-    if (a.split) launch(cached_few_k<DHP, WHOLE, F32, MOD, 4>, mask[1], grid, 256, FEW_SMEM<DHP, 4>, a, s);
+    if (a.split || most_groups(a) * a.c.Hkv >= 256) launch(cached_few_k<DHP, WHOLE, F32, MOD, 4>, mask[1], grid, 256, FEW_SMEM<DHP, 4>, a, s);
     else launch(cached_few_k<DHP, WHOLE, F32, MOD, NW>, mask[2], grid, NW * 64, FEW_SMEM<DHP, NW>, a, s);
   }
   if (!a.split) return;
@@ -727,12 +742,15 @@ template <int DHP, bool F32> void go(const CachedAttn& a, hipStream_t s) {
 
 }  // namespace
 
-// What the sizes alone say.  One row per sequence, or few in all: the form for few rows throughout.  Its keys need no splitting up to what eight waves
-// do in some 5 us, and then there is no second launch.  Prompts' keys are split where there is not a workgroup of theirs for every CU.
+// What the sizes alone say.  One row per sequence, or few in all: the form for few rows throughout.  Splitting its keys takes a second launch (4 us and
+// more), and gives work to CUs that have none: a workgroup with a CU to itself takes 3 us for 512 tokens.  Without, with, 8 sequences of 4 key heads of 128, us:
+// 512 tokens 8.2, 10.6; 1024 10.9, 10.1; 2048 17.8, 12.5.  Where there is a workgroup for every CU anyway it only evens out lengths.  Prompts' keys are split
+// where there are fewer.
 void cached_attn_plan(CachedAttn* a) {
-  const i64 room = (i64)a->c.max_pages << a->c.lg;
+  a->target = a->c.dh <= 64 ? 1024 : a->c.dh <= 128 ? 512 : 256;      // workgroups that are on the CUs together
   a->few_only = (i64)a->T * a->G <= FEW_ROWS || a->T <= a->c.n_seqs;
-  a->split = a->few_only && room <= 2048 ? 0 : most_groups(*a) * a->c.Hkv < 256 ? 2 : 1;
+  const i64 room = (i64)a->c.max_pages << a->c.lg, groups = most_groups(*a) * a->c.Hkv;
+  a->split = a->few_only && room <= (groups < 256 ? 768 : 2048) ? 0 : groups < 256 ? 2 : 1;
 }
 size_t cached_attn_bytes(const CachedAttn& a) { return (size_t)most_slots(a) * 16 * (padded(a.c.dh) * 4 + 8); }
 bool cached_attn_takes(const CachedAttn& a) {

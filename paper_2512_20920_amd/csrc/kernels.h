@@ -423,6 +423,7 @@ struct CachedAttn {
   i64 slots;
   int few_only;                          // every sequence in the form for few rows
   int split;                             // whose keys may be split: 0 nobody's, 1 few rows', 2 prompts' too
+  int target;                            // into how many workgroups all keys are split
 };
 void cached_attn_plan(CachedAttn* a);               // few_only and split, from the sizes alone
 size_t cached_attn_bytes(const CachedAttn& a);
