@@ -18,6 +18,10 @@ namespace {
 
 constexpr int FEW_ROWS = 64;             // of a sequence and key head: up to here groups of 16 rows, beyond groups of 128, 32 for each of four waves
 
+// A row's reference for its exponentials is a maximum that may be this much behind, in units of log2: then results are rescaled in a few tiles instead of
+// in more than half of them, and no exponential is past 2^8, of which bfloat16 and float32 hold as many bits as of one below 1.
+constexpr float HEADROOM = 8.f;
+
 // What a call does with a sequence.  Keys begin .. end - 1 are seen by some row; cost: tiles of 32 keys for a wave of a workgroup (a group) of rows.
 struct SeqWork { int row0, n, start, begin, end, groups, cost; bool few; };
 __device__ __forceinline__ SeqWork work_of(const CachedAttn& a, int s) {
@@ -38,7 +42,7 @@ __device__ __forceinline__ SeqWork work_of(const CachedAttn& a, int s) {
 // Into how many parts a group's keys go, if `per` tiles per wave are the aim: up to 64
 __device__ __forceinline__ int splits_of(const CachedAttn& a, const SeqWork& w, int per) {
   if (a.split == 0 || (!w.few && a.split == 1)) return 1;
-  if (!w.few) per = max(per, 8);                     // (128 rows' parts are work to join)
+  if (!w.few) per = max(per, a.dt == 0 ? 4 : 8);     // (128 rows' parts are work to join; float32 tiles take three times the products: 20.8 -> 18.5 us with 4 at 256 tokens)
   return min(max((w.cost + per - 1) / per, 1), 64);
 }
 // A call's list of workgroups: sequence by sequence, and in it (split, group, key head), key heads fastest (one stays on one XCD if there are eight).
@@ -287,7 +291,7 @@ __device__ __forceinline__ void few_rows(const CachedAttn& a, const Item& x, flo
 
   // where a lane's keys and values of a tile lie: token 16 gk + .. of the keys, 16 g + .. of the values
   const int gk = col >> 2;
-  auto page_of = [&](int t, int group) { return t < t1 ? cache_page(c, x.s, (t * 64 + group * 16) >> lg) : -1; };
+  auto page_of = [&](int t, int group) { return cache_page(c, x.s, (t * 64 + group * 16) >> lg); };      // (of any t: a place outside the table is no page)
   int pk = page_of(t0, gk), pv = page_of(t0, g);
   uint4 k[4][KT], v[DT];
   float ks, vs;
@@ -349,14 +353,15 @@ __device__ __forceinline__ void few_rows(const CachedAttn& a, const Item& x, flo
     float mx = -INFINITY;
 #pragma unroll
     for (int e = 0; e < 16; e += 2) mx = fmaxf(fmaxf(mx, s[e]), s[e + 1]);
-    const float mn = fmaxf(m, quarters_max(mx) * unit), ms = mn == -INFINITY ? 0.f : mn;
-    if (__any(mn > m)) {
-      const float alpha = fast_exp2(m - ms);
+    const float top = quarters_max(mx) * unit;
+    if (__any(top > m + HEADROOM)) {
+      const float mn = fmaxf(m, top), alpha = fast_exp2(m - (mn == -INFINITY ? 0.f : mn));
       l *= alpha;
 #pragma unroll
       for (int d = 0; d < DT; d++) acc[d] *= alpha;
+      m = mn;
     }
-    m = mn;
+    const float ms = m == -INFINITY ? 0.f : m;
     float sum = 0.f;
 #pragma unroll
     for (int e = 0; e < 16; e++) { s[e] = fast_exp2(MOD != 0 ? s[e] - ms : fmaf(s[e], unit, -ms)); sum += s[e]; }
@@ -446,7 +451,6 @@ template <int DHP, bool WHOLE, bool F32, int MOD>
 __device__ __forceinline__ void many_rows(const CachedAttn& a, const Item& x, float* smem) {
   typedef typename std::conditional<F32, float, bf16>::type T;
   constexpr int KT = DHP / 32, DT = DHP / 32, Q = F32 ? 3 : 1;
-  constexpr bool AHEAD = DHP <= 128;                 // the next tile is on its way while one is worked on (wider heads have no registers for it)
   const CacheView& c = a.c;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, col = lane & 31, lg = c.lg, P1 = (1 << lg) - 1;
   const int dh = WHOLE ? DHP : c.dh;
@@ -487,71 +491,77 @@ __device__ __forceinline__ void many_rows(const CachedAttn& a, const Item& x, fl
     ks0 = c.ks[b0]; ks1 = c.ks[b1]; vs0 = c.vs[b0]; vs1 = c.vs[b1];
   };
   const int tok = 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3);
-  struct Tile { uint4 k[KT], v[DT]; float ks, vs; bool bad; };
-  auto fetch = [&](int n, Tile& t) {                 // the n-th tile; its pages have been looked up
+  uint4 k[KT], v[DT];
+  float ks, vs;
+  bool bad;
+  // the n-th tile's keys, values; its pages have been looked up.  (Read by all lanes before any chooses: in a branch, a lane that is not in it may be the one
+  // that is read.)
+  auto fetch_k = [&](int n) {
     const int l = n & 63, kv = (t0 + n) * 32;
     const int p0 = __builtin_amdgcn_readlane(page0, l), p1 = __builtin_amdgcn_readlane(page1, l);
+    const float k0 = lane_f(ks0, l), k1 = lane_f(ks1, l);
     const i64 s0 = (cache_block(c, max(p0, 0), kh) << lg) + (kv & P1), s1 = (cache_block(c, max(p1, 0), kh) << lg) + ((kv + 16) & P1);
-    t.bad = g ? p1 < 0 : p0 < 0;
-    // (read by all lanes before any chooses: in a branch, a lane that is not in it may be the one that is read)
-    const float k0 = lane_f(ks0, l), k1 = lane_f(ks1, l), v0 = lane_f(vs0, l), v1 = lane_f(vs1, l);
-    t.ks = tok & 16 ? k1 : k0;
-    t.vs = g ? v1 : v0;
-    const unsigned char* k = c.k + ((tok & 16 ? s1 : s0) + (tok & 15)) * dh;
-    const unsigned char* v = c.v + (g ? s1 : s0) * dh;
-    // (columns past the width: K reads other columns' numbers, which meet zeros of q; results of V's are not stored)
+    ks = tok & 16 ? k1 : k0;
+    const unsigned char* p = c.k + ((tok & 16 ? s1 : s0) + (tok & 15)) * dh;
+    // (columns past the width read others, which meet zeros of q)
 #pragma unroll
-    for (int u = 0; u < KT; u++) t.k[u] = *(const uint4*)(k + (WHOLE || 32 * u + 16 * g < dh ? 32 * u + 16 * g : 0));
+    for (int u = 0; u < KT; u++) k[u] = *(const uint4*)(p + (WHOLE || 32 * u + 16 * g < dh ? 32 * u + 16 * g : 0));
+  };
+  auto fetch_v = [&](int n) {
+    const int l = n & 63, kv = (t0 + n) * 32;
+    const int p0 = __builtin_amdgcn_readlane(page0, l), p1 = __builtin_amdgcn_readlane(page1, l);
+    const float v0 = lane_f(vs0, l), v1 = lane_f(vs1, l);
+    const i64 s0 = (cache_block(c, max(p0, 0), kh) << lg) + (kv & P1), s1 = (cache_block(c, max(p1, 0), kh) << lg) + ((kv + 16) & P1);
+    bad = g ? p1 < 0 : p0 < 0;
+    vs = g ? v1 : v0;
+    const unsigned char* p = c.v + (g ? s1 : s0) * dh;
 #pragma unroll
-    for (int u = 0; u < DT; u++) t.v[u] = *(const uint4*)(v + 16 * (WHOLE || 32 * u + col < dh ? 32 * u + col : 0));
+    for (int u = 0; u < DT; u++) v[u] = *(const uint4*)(p + 16 * (WHOLE || 32 * u + col < dh ? 32 * u + col : 0));
   };
 
   f32x16 acc[DT];
 #pragma unroll
   for (int d = 0; d < DT; d++) acc[d] = f32x16{};
   float m = -INFINITY, l = 0.f;
-  Tile cur, next;
   if (count > 0) {
     look_up(0);
-    if (AHEAD) fetch(0, cur);
+    fetch_k(0);
+    fetch_v(0);
   }
   for (int n = 0; n < count; n++) {
     const int kv = (t0 + n) * 32;
-    if constexpr (AHEAD) {
-      if (n + 1 < count) {
-        if (((n + 1) & 63) == 0) look_up(n + 1);
-        fetch(n + 1, next);
-      }
-    } else {
-      if (n > 0 && (n & 63) == 0) look_up(n);
-      fetch(n, cur);
-    }
     f32x16 s = {};
 #pragma unroll
     for (int t = 0; t < KT; t++) {
-      const bf16x8 k0 = eight(cur.k[t].x, cur.k[t].y, cur.ks), k1 = eight(cur.k[t].z, cur.k[t].w, cur.ks);
+      const bf16x8 k0 = eight(k[t].x, k[t].y, ks), k1 = eight(k[t].z, k[t].w, ks);
 #pragma unroll
       for (int p = 0; p < Q; p++) { s = mfma(k0, qf[t][p][0], s); s = mfma(k1, qf[t][p][1], s); }
     }
+    // (a 64th tile's pages are looked up when its keys are asked for: its values come behind them, this tile's are here already)
+    if (n + 1 < count) {
+      if (((n + 1) & 63) == 0) look_up(n + 1);
+      fetch_k(n + 1);
+    }
     final_scores<F32, MOD>(a, sf, (float)(pos - kv - 16 * g), s);
-    const bool any_bad = __any(cur.bad);
+    const bool any_bad = __any(bad);
     if (kv < all_from || kv + 32 > all_to || any_bad) {
       const int lo = max(sees.x, kv) - kv - 16 * g;
       const unsigned cnt = (unsigned)max(min(sees.y, kv + 32) - max(sees.x, kv), 0);
 #pragma unroll
-      for (int e = 0; e < 16; e++) if ((unsigned)(e - lo) >= cnt || cur.bad) s[e] = -INFINITY;
+      for (int e = 0; e < 16; e++) if ((unsigned)(e - lo) >= cnt || bad) s[e] = -INFINITY;
     }
     float mx = -INFINITY;
 #pragma unroll
     for (int e = 0; e < 16; e += 2) mx = fmaxf(fmaxf(mx, s[e]), s[e + 1]);
-    const float mn = fmaxf(m, both_halves_max(mx) * unit), ms = mn == -INFINITY ? 0.f : mn;
-    if (__any(mn > m)) {
-      const float alpha = fast_exp2(m - ms);
+    const float top = both_halves_max(mx) * unit;
+    if (__any(top > m + HEADROOM)) {
+      const float mn = fmaxf(m, top), alpha = fast_exp2(m - (mn == -INFINITY ? 0.f : mn));
       l *= alpha;
 #pragma unroll
       for (int d = 0; d < DT; d++) acc[d] *= alpha;
+      m = mn;
     }
-    m = mn;
+    const float ms = m == -INFINITY ? 0.f : m;
     float sum = 0.f;
 #pragma unroll
     for (int e = 0; e < 16; e++) { s[e] = fast_exp2(MOD != 0 ? s[e] - ms : fmaf(s[e], unit, -ms)); sum += s[e]; }
@@ -565,17 +575,17 @@ __device__ __forceinline__ void many_rows(const CachedAttn& a, const Item& x, fl
       for (int e = 0; e < 16; e++) s[e] -= (float)pf[p][e >> 3][e & 7];
     }
     if (kv + 32 > x.w.end || any_bad) {
-      const int keep = cur.bad ? 0 : x.w.end - kv - 16 * g;
+      const int keep = bad ? 0 : x.w.end - kv - 16 * g;
 #pragma unroll
-      for (int d = 0; d < DT; d++) cur.v[d] = first_tokens(cur.v[d], keep);
+      for (int d = 0; d < DT; d++) v[d] = first_tokens(v[d], keep);
     }
 #pragma unroll
     for (int d = 0; d < DT; d++) {
-      const bf16x8 v0 = eight(cur.v[d].x, cur.v[d].y, cur.vs), v1 = eight(cur.v[d].z, cur.v[d].w, cur.vs);
+      const bf16x8 v0 = eight(v[d].x, v[d].y, vs), v1 = eight(v[d].z, v[d].w, vs);
 #pragma unroll
       for (int p = 0; p < Q; p++) { acc[d] = mfma(v0, pf[p][0], acc[d]); acc[d] = mfma(v1, pf[p][1], acc[d]); }
     }
-    if constexpr (AHEAD) cur = next;
+    if (n + 1 < count) fetch_v(n + 1);
   }
   l = both_halves_sum(l);
 
@@ -624,7 +634,7 @@ __device__ __forceinline__ void many_rows(const CachedAttn& a, const Item& x, fl
 }
 
 template <int DHP, bool WHOLE, bool F32, int MOD>
-__global__ void __launch_bounds__(256, DHP == 256 || F32 ? 1 : 2) cached_attn_k(CachedAttn a) {
+__global__ void __launch_bounds__(256, DHP == 256 || F32 ? 1 : DHP == 128 ? 2 : 3) cached_attn_k(CachedAttn a) {
   extern __shared__ __attribute__((aligned(16))) float smem[];
   Item x;
   if (!find<false>(a, (int)blockIdx.x, &x)) return;
