@@ -16,7 +16,7 @@
 
 namespace {
 
-constexpr int FEW_ROWS = 64;             // of a sequence and key head: up to here groups of 16 rows, beyond groups of 128, 32 for each of four waves
+constexpr int FEW_ROWS = 64;             // of a sequence and key head: up to here groups of 16 rows, beyond groups of 1 << lr, 32 for each of the waves
 
 // A row's reference for its exponentials is a maximum that may be this much behind, in units of log2: then results are rescaled in a few tiles instead of
 // in more than half of them, and no exponential is past 2^8, of which bfloat16 and float32 hold as many bits as of one below 1.
@@ -34,9 +34,9 @@ __device__ __forceinline__ SeqWork work_of(const CachedAttn& a, int s) {
   w.begin = a.window ? max(w.start + 1 - a.window, 0) : 0;
   const i64 R = (i64)rows.y * a.G;
   w.few = a.few_only || R <= FEW_ROWS;
-  w.groups = (int)(w.few ? (R + 15) >> 4 : (R + 127) >> 7);
+  w.groups = (int)(w.few ? (R + 15) >> 4 : (R + (1 << a.lr) - 1) >> a.lr);
   const int tiles = w.end > w.begin ? ((w.end - 1) >> 5) - (w.begin >> 5) + 1 : 0;
-  w.cost = w.few ? (tiles + 3) >> 2 : tiles;
+  w.cost = w.few ? (tiles + 3) >> 2 : (tiles + (128 >> a.lr) - 1) >> (7 - a.lr);
   return w;
 }
 // Into how many parts a group's keys go, if `per` tiles per wave are the aim: up to 64
@@ -46,7 +46,7 @@ __device__ __forceinline__ int splits_of(const CachedAttn& a, const SeqWork& w, 
   return min(max((w.cost + per - 1) / per, 1), 64);
 }
 // A call's list of workgroups: sequence by sequence, and in it (split, group, key head), key heads fastest (one stays on one XCD if there are eight).
-// Parts of split groups lie in the scratch memory in the same order, in slots of 16 rows: one per workgroup (few) or eight.
+// Parts of split groups lie in the scratch memory in the same order, in slots of 16 rows: one per workgroup (few) or as many as its rows fill.
 // JOIN: the list of four rows each of the split groups instead.
 struct Item { int s, at, splits; i64 slot; SeqWork w; };
 template <bool JOIN> __device__ __forceinline__ bool find(const CachedAttn& a, int id, Item* x) {
@@ -82,7 +82,7 @@ template <bool JOIN> __device__ __forceinline__ bool find(const CachedAttn& a, i
     // (first rows that are out of order can ask for more than there are: no sum overflows, and whoever is past the scratch memory stays out of it)
     const int groups = min(w.groups, 1 << 20) * a.c.Hkv, quads = (int)(((i64)w.n * a.G + 3) >> 2) * a.c.Hkv;
     const int mine = min(JOIN ? (k > 1 ? quads : 0) : groups * k, 1 << 24);
-    const int room = min(k > 1 ? groups * k * (w.few ? 1 : 8) : 0, 1 << 24);
+    const int room = min(k > 1 ? groups * k * (w.few ? 1 : 1 << (a.lr - 4)) : 0, 1 << 24);
     const int running = wave_running(mine), all = __builtin_amdgcn_readlane(running, 63), rooms = wave_running(room);
     if (id < before + all) {
       const int l = __builtin_ctzll(__ballot(before + running > id));
@@ -446,6 +446,9 @@ __device__ __forceinline__ void few_rows(const CachedAttn& a, const Item& x, flo
 }
 
 // ---- many rows: 32 per wave, tiles of 32 keys ----
+// LDS: the parts of three waves, then a row of floats for each
+template <int DHP> constexpr int ROWS_AT = 3 * 64 * (DHP / 2 + 2);
+template <int DHP> constexpr unsigned MANY_SMEM = (ROWS_AT<DHP> + 4 * DHP) * 4;
 // DHP: head width rounded up to 64, 128 or 256.  WHOLE: it is the width.  F32: float32 queries and results.
 template <int DHP, bool WHOLE, bool F32, int MOD>
 __device__ __forceinline__ void many_rows(const CachedAttn& a, const Item& x, float* smem) {
@@ -456,7 +459,8 @@ __device__ __forceinline__ void many_rows(const CachedAttn& a, const Item& x, fl
   const int dh = WHOLE ? DHP : c.dh;
   const int rest = x.at / c.Hkv, kh = x.at - rest * c.Hkv, split = rest / x.w.groups;
   const int group = x.w.groups - 1 - (rest - split * x.w.groups);      // (late rows see most)
-  const int blk = group * 4 + wv;
+  // of the workgroup's waves those of one block of 32 rows share its keys out
+  const int nb = a.lr - 5, kparts = 4 >> nb, kp = wv >> nb, blk = (group << nb) + (wv & ((1 << nb) - 1));
 
   // this lane's row
   const int r = blk * 32 + col, qi = r / a.G, i = x.w.row0 + qi, h = kh * a.G + (r - qi * a.G), pos = x.w.start + qi;
@@ -471,8 +475,8 @@ __device__ __forceinline__ void many_rows(const CachedAttn& a, const Item& x, fl
   // this wave's tiles: t0 .. t1 - 1 (of 32 keys, counted from the sequence's first)
   int t0 = 0, t1 = 0;
   if (first < last) {
-    const int a0 = first >> 5, n = ((last - 1) >> 5) - a0 + 1, per = (n + x.splits - 1) / x.splits;
-    t0 = a0 + min(split * per, n);
+    const int a0 = first >> 5, n = ((last - 1) >> 5) - a0 + 1, all = x.splits * kparts, per = (n + all - 1) / all;
+    t0 = a0 + min((split * kparts + kp) * per, n);
     t1 = min(t0 + per, a0 + n);
   }
   const int count = max(t1 - t0, 0);
@@ -589,8 +593,33 @@ __device__ __forceinline__ void many_rows(const CachedAttn& a, const Item& x, fl
   }
   l = both_halves_sum(l);
 
+  if (kparts > 1) {
+    // the waves of a block put their results together
+    constexpr int P = DT * 16 + 2;
+    float* mine = smem + (wv - (1 << nb)) * (P * 64) + lane;
+    if (kp) {
+#pragma unroll
+      for (int d = 0; d < DT; d++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) mine[(d * 16 + e) * 64] = acc[d][e];
+      mine[(P - 2) * 64] = m;
+      mine[(P - 1) * 64] = l;
+    }
+    __syncthreads();
+    if (kp) return;
+    for (int k = 1; k < kparts; k++) {
+      const float* p = smem + (((k - 1) << nb) + wv) * (P * 64) + lane;
+      const float m1 = p[(P - 2) * 64], mn = fmaxf(m, m1), ms = mn == -INFINITY ? 0.f : mn, f0 = fast_exp2(m - ms), f1 = fast_exp2(m1 - ms);
+      l = l * f0 + p[(P - 1) * 64] * f1;
+      m = mn;
+#pragma unroll
+      for (int d = 0; d < DT; d++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) acc[d][e] = fmaf(p[(d * 16 + e) * 64], f1, acc[d][e] * f0);
+    }
+  }
   if (x.splits > 1) {
-    const i64 slot = x.slot + (i64)x.at * 8 + wv * 2;                 // (two of 16 rows each, one behind the other)
+    const i64 slot = x.slot + ((i64)x.at << (a.lr - 4)) + wv * 2;                 // (two of 16 rows each, one behind the other)
     if (!ok || slot + 1 >= a.slots) return;
     if (g == 0) a.stats[slot * 16 + col] = make_float2(m, l);
     float* p = a.parts + (slot * 16 + col) * DHP;
@@ -629,12 +658,12 @@ __device__ __forceinline__ void many_rows(const CachedAttn& a, const Item& x, fl
     for (int b = 0; b < 32; b++)
       if ((again >> b) & 1) {
         const int rr = blk * 32 + b, qr = rr / a.G;
-        cached_row<T>(a, x.s, x.w.row0 + qr, kh * a.G + (rr - qr * a.G), x.w.start + qr, x.w.end, smem + wv * DHP);
+        cached_row<T>(a, x.s, x.w.row0 + qr, kh * a.G + (rr - qr * a.G), x.w.start + qr, x.w.end, smem + ROWS_AT<DHP> + wv * DHP);
       }
 }
 
 template <int DHP, bool WHOLE, bool F32, int MOD>
-__global__ void __launch_bounds__(256, DHP == 256 || F32 ? 1 : DHP == 128 ? 2 : 3) cached_attn_k(CachedAttn a) {
+__global__ void __launch_bounds__(256, DHP == 256 || F32 ? 1 : DHP == 128 ? 2 : 4) cached_attn_k(CachedAttn a) {
   extern __shared__ __attribute__((aligned(16))) float smem[];
   Item x;
   if (!find<false>(a, (int)blockIdx.x, &x)) return;
@@ -658,7 +687,7 @@ template <class T, int DHP> __global__ void __launch_bounds__(256) cached_join_k
   const int quad = x.at / Hkv, kh = x.at - quad * Hkv, rr = quad * 4 + wv, qi = rr / a.G;
   if (qi >= x.w.n) return;
   // of the list of workgroups that made the parts: the row's group, and which of its slots and rows
-  const int lrows = x.w.few ? 4 : 7, slots = x.w.few ? 1 : 8, g0 = rr >> lrows, group = x.w.few ? g0 : x.w.groups - 1 - g0, in = rr & ((1 << lrows) - 1);
+  const int lrows = x.w.few ? 4 : a.lr, slots = 1 << (lrows - 4), g0 = rr >> lrows, group = x.w.few ? g0 : x.w.groups - 1 - g0, in = rr & ((1 << lrows) - 1);
   if (x.slot + (i64)x.splits * x.w.groups * Hkv * slots > a.slots) return;
   const int i = x.w.row0 + qi, h = kh * a.G + (rr - qi * a.G);
   {
@@ -706,12 +735,12 @@ template <class T, int DHP> __global__ void __launch_bounds__(256) cached_join_k
 // Most groups that a call can have
 i64 most_groups(const CachedAttn& a) {
   const i64 rows = (i64)a.T * a.G, seqs = a.c.n_seqs < a.T ? a.c.n_seqs : a.T;
-  const i64 by_row = rows / 16 + seqs, by_seq = rows / 128 + (FEW_ROWS / 16) * seqs;
+  const i64 by_row = rows / 16 + seqs, by_seq = (rows >> a.lr) + (FEW_ROWS / 16) * seqs;
   return a.few_only || by_row < by_seq ? by_row : by_seq;
 }
 int padded(int dh) { return dh <= 64 ? 64 : dh <= 128 ? 128 : 256; }
 i64 most_slots(const CachedAttn& a) {
-  return a.split ? (most_groups(a) * a.c.Hkv + a.target) * (a.split == 2 && !a.few_only ? 8 : 1) : 0;
+  return a.split ? (most_groups(a) * a.c.Hkv + a.target) * (a.split == 2 && !a.few_only ? 1 << (a.lr - 4) : 1) : 0;
 }
 
 template <class K> void launch(K kernel, std::atomic<unsigned long long>& attr_mask, i64 grid, int block, unsigned smem, const CachedAttn& a, hipStream_t s) {
@@ -724,7 +753,7 @@ template <class K> void launch(K kernel, std::atomic<unsigned long long>& attr_m
 template <int DHP, bool WHOLE, bool F32, int MOD> void go(const CachedAttn& a, hipStream_t s) {
   static std::atomic<unsigned long long> mask[3];
   const i64 grid = most_groups(a) * a.c.Hkv + (a.split ? a.target : 0);
-  if (!a.few_only) launch(cached_attn_k<DHP, WHOLE, F32, MOD>, mask[0], grid, 256, FEW_SMEM<DHP, 4>, a, s);
+  if (!a.few_only) launch(cached_attn_k<DHP, WHOLE, F32, MOD>, mask[0], grid, 256, MANY_SMEM<DHP>, a, s);      // (more than the form for few rows takes)
   else {
     // eight waves where nothing is split, if their registers allow it
     constexpr int NW = DHP == 256 || F32 ? 4 : 8;
@@ -756,8 +785,13 @@ template <int DHP, bool F32> void go(const CachedAttn& a, hipStream_t s) {
 // more), and gives work to CUs that have none: a workgroup with a CU to itself takes 3 us for 512 tokens.  Without, with, 8 sequences of 4 key heads of 128, us:
 // 512 tokens 8.2, 10.6; 1024 10.9, 10.1; 2048 17.8, 12.5.  Where there is a workgroup for every CU anyway it only evens out lengths.  Prompts' keys are split
 // where there are fewer.
+// A prompt's workgroup takes 32, 64 or 128 rows, and its four waves a quarter, half or all of their keys each: the fewer rows there are, the more workgroups
+// they make.  32 heads of 128 over 8, 32, 64, 128 rows, us: 512 tokens 15.8, 16.3, 31.1; 512 behind 3000 46.8, 53.7, 63.5; 2048 behind 3000 184, 173, 182;
+// 4096 behind 3000 426, 404, 396.  The same of 64: 11.5, 13.4, 24.9; 34.3, 46.4, 51.1; 109, 111, 131; 249, 241, 258.
 void cached_attn_plan(CachedAttn* a) {
   a->target = a->c.dh <= 64 ? 1024 : a->c.dh <= 128 ? 512 : 256;      // workgroups that are on the CUs together
+  const i64 blocks = ((i64)a->T * a->H) >> 7;        // workgroups of 128 rows
+  a->lr = 4 * blocks <= a->target ? 5 : 2 * blocks <= 3 * (i64)a->target ? 6 : 7;
   a->few_only = (i64)a->T * a->G <= FEW_ROWS || a->T <= a->c.n_seqs;
   const i64 room = (i64)a->c.max_pages << a->c.lg, groups = most_groups(*a) * a->c.Hkv;
   a->split = a->few_only && room <= (groups < 256 ? 768 : 2048) ? 0 : groups < 256 ? 2 : 1;

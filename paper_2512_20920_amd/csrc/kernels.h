@@ -421,6 +421,7 @@ struct CachedAttn {
   float scale, cap;
   float* parts; float2* stats;           // scratch of split calls: `slots` parts of 16 rows
   i64 slots;
+  int lr;                                // log2 of the rows of a workgroup in the form for many
   int few_only;                          // every sequence in the form for few rows
   int split;                             // whose keys may be split: 0 nobody's, 1 few rows', 2 prompts' too
   int target;                            // into how many workgroups all keys are split
