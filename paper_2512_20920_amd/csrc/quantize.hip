@@ -5,11 +5,25 @@
 // step of scale, of at most 25 bits of which the last is zero where the first is not), so one comparison with scale / 2 tells which.
 #include "kernels.h"
 
-__device__ __forceinline__ int code_of(float x, float scale, float inv) {
-  float k = rintf(x * inv);
-  const float r = fmaf(-k, scale, x), half = 0.5f * scale;
-  if (fabsf(r) > half || (fabsf(r) == half && ((int)k & 1))) k += r > 0.f ? 1.f : -1.f;
-  return (int)k;
+// V codes in the low bytes of k.  x / scale + 1.5 2^23 has the nearest integer in its low bits; where no lane's remainder is half a step or more, as in
+// nearly every wavefront, there is nothing to choose.
+template <int V> __device__ __forceinline__ void codes_of(const float (&x)[V], float scale, float inv, unsigned (&k)[V]) {
+  constexpr float BIG = 12582912.f;
+  const float half = 0.5f * scale;
+  float worst = 0.f;
+#pragma unroll
+  for (int i = 0; i < V; i++) {
+    const float z = fmaf(x[i], inv, BIG);
+    k[i] = __builtin_bit_cast(unsigned, z);
+    worst = fmaxf(worst, fabsf(fmaf(BIG - z, scale, x[i])));
+  }
+  if (__any(worst >= half)) {
+#pragma unroll
+    for (int i = 0; i < V; i++) {
+      const float r = fmaf(BIG - __builtin_bit_cast(float, k[i]), scale, x[i]);
+      if (fabsf(r) > half || (fabsf(r) == half && (k[i] & 1))) k[i] += r > 0.f ? 1 : -1;
+    }
+  }
 }
 template <class T, int V> struct Vec { typedef __attribute__((ext_vector_type(V))) T type; };
 
@@ -24,8 +38,8 @@ __global__ void __launch_bounds__(256) quantize_rows_k(const T* __restrict__ x, 
   if (row >= rows) return;                           // (W = 1: no barrier below)
   const T* xr = x + (i64)row * ldx;
   signed char* cr = codes + (i64)row * ldc;
-  float v[N][V], top = 0.f;
-  bool fine = true;
+  float v[N][V];
+  unsigned most = 0;                                 // the largest |x|, as bits: what is not finite is above all that is
   auto load = [&](int c, float (&o)[V]) {
     if constexpr (V == 1) o[0] = c < cols ? to_f(xr[c]) : 0.f;
     else {
@@ -43,15 +57,14 @@ __global__ void __launch_bounds__(256) quantize_rows_k(const T* __restrict__ x, 
   };
   auto look = [&](const float (&o)[V]) {
 #pragma unroll
-    for (int i = 0; i < V; i++) { const float a = fabsf(o[i]); fine = fine && a < INFINITY; top = fmaxf(top, a); }
+    for (int i = 0; i < V; i++) most = max(most, __builtin_bit_cast(unsigned, o[i]) & 0x7fffffffu);
   };
 #pragma unroll
   for (int n = 0; n < N; n++) load(n * STEP + t * V, v[n]);
 #pragma unroll
   for (int n = 0; n < N; n++) look(v[n]);
   for (int c = N * STEP + t * V; c < cols; c += STEP) { float o[V]; load(c, o); look(o); }
-  if (!fine) top = INFINITY;
-  top = wave_max(top);
+  float top = wave_max(most < 0x7f800000u ? __builtin_bit_cast(float, most) : INFINITY);
   if constexpr (W == 4) {
     if (lane == 0) red[wv] = top;
     __syncthreads();
@@ -64,18 +77,21 @@ __global__ void __launch_bounds__(256) quantize_rows_k(const T* __restrict__ x, 
   if (t == 0) scales[row] = scale < INFINITY ? scale : __builtin_nanf("");
   auto put = [&](int c, const float (&o)[V]) {
     if (c >= cols) return;
-    signed char k[V];
+    unsigned k[V];
+    codes_of<V>(o, scale, inv, k);
+    if (!live)
 #pragma unroll
-    for (int i = 0; i < V; i++) k[i] = live ? (signed char)code_of(o[i], scale, inv) : 0;
-    if constexpr (V == 1) cr[c] = k[0];
+      for (int i = 0; i < V; i++) k[i] = 0;
+    if constexpr (V == 1) cr[c] = (signed char)k[0];
     else if (c + V <= cols) {
-      typename Vec<signed char, V>::type w;
+      unsigned w[V / 4];
 #pragma unroll
-      for (int i = 0; i < V; i++) w[i] = k[i];
-      *(typename Vec<signed char, V>::type*)(cr + c) = w;
+      for (int i = 0; i < V / 4; i++)                // the four low bytes
+        w[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(k[4 * i + 3], k[4 * i + 2], 0x0c0c0400), __builtin_amdgcn_perm(k[4 * i + 1], k[4 * i], 0x0c0c0400), 0x05040100);
+      *(uint2*)(cr + c) = make_uint2(w[0], w[1]);
     } else {
 #pragma unroll
-      for (int i = 0; i < V; i++) if (c + i < cols) cr[c + i] = k[i];
+      for (int i = 0; i < V; i++) if (c + i < cols) cr[c + i] = (signed char)k[i];
     }
   };
 #pragma unroll
