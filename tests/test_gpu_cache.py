@@ -384,6 +384,19 @@ def test_attention_values_that_are_not_finite(held, new, dtype, mode):
         assert outside(lse[~sees.T], lse2[~sees.T], 2 * want["lse"][1][~sees.T]) <= 1.0
 
 
+@pytest.mark.parametrize("H,dh,rows,dtype", [(64, 256, 140, "bf16"), (128, 256, 390, "bf16"), (64, 128, 260, "bf16"), (256, 128, 390, "bf16"),
+                                             (128, 64, 260, "bf16"), (512, 64, 390, "bf16"), (128, 64, 260, "f32"), (256, 128, 390, "f32")])
+def test_attention_of_many_rows(H, dh, rows, dtype):
+    """So many that a workgroup takes 64 of them, or 128, not 32 as with the shapes above; tokens, a few rows and nobody beside them."""
+    held, new = [rows + 37, 90, 33, 0, 20], [rows, 1, 3, 0, 20]
+    page = 16 if dh == 64 else 64
+    c = Paged(dtype, H // 4, dh, page, _tables(np.random.default_rng(rows), held, page), seed=rows)
+    _fill(c, held)
+    a = Attend(c, held, new, H, 0)
+    a.run(window=(200 if rows == 390 else 0))
+    a.check()
+
+
 @pytest.mark.parametrize("dtype,rows,keys", [("bf16", 1, 9000), ("bf16", 33, 5000), ("f32", 1, 9000), ("bf16", 1, 40000)])
 def test_attention_of_long_sequences(dtype, rows, keys):
     """Keys split over many workgroups, their pages far apart in a large memory; spot rows against the reference."""
