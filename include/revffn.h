@@ -470,7 +470,7 @@ typedef struct revffn_cache {
 
 /* New keys and values (T rows of Hkv heads, row strides ldk, ldv) into the cache, keys turned to their positions on the way (r NULL: not), and with
  * them the queries of the same rows (q to q_out, H heads; q NULL: none; q_out = q with ldqo = ldq turns in place).  pos: device [T], or NULL: a row's
- * token in its sequence.  r->dims has to be a multiple of 16; 2 Hkv + H <= 65535.  The turn is that of revffn_op_rotary, here in float64 throughout.
+ * token in its sequence.  r->dims has to be a multiple of 16; H <= 65536.  The turn is that of revffn_op_rotary, here in float64 throughout.
  * A key is rounded to float32, to dtype, then to 8 bits, each to nearest, ties to even.  The unit of a page and head is the
  * least power of two (2^-96 .. 2^119) that brings its largest value within 448; if a page that holds tokens already needs a larger one, they are
  * rounded again to it (which changes only numbers below 2^-6 of the new unit).  A value that is not finite is stored as NaN and does not count

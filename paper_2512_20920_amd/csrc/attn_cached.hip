@@ -231,18 +231,17 @@ template <class T, int Q> __device__ __forceinline__ void load_q16(const T* q, b
       v[u] -= (float)b;
     }
 }
-// the scores' final form (MOD), in units of log2 where there is one; first: distance of the lane's first key
+// The scores' final form (MOD), but for a last factor that the exponential takes with it (unit_of), in units of log2; first: distance of the lane's first key
+template <int MOD> __device__ __forceinline__ float unit_of(const ScoreForm& sf) { return MOD == 0 ? sf.f : MOD == CAPPED ? sf.cap2 : 1.f; }
 template <bool F32, int MOD, class S> __device__ __forceinline__ void final_scores(const CachedAttn& a, const ScoreForm& sf, float first, S& s) {
-  if constexpr (MOD != 0) {
+  if constexpr (F32 && (MOD & CAPPED)) {
+#pragma unroll
+    for (int e = 0; e < 16; e++) s[e] = tanhf(s[e] * sf.x1);
+  } else tanh_scores<MOD, true>(sf, s);
+  if constexpr (MOD & BIASED) {
     float keep;
-    if constexpr (F32 && (MOD & CAPPED)) {
 #pragma unroll
-      for (int e = 0; e < 16; e++) s[e] = final_score<MOD & BIASED>(sf, tanhf(s[e] * sf.x1) * (a.cap / a.scale), first - (float)e, &keep);      // (back to units of q.k)
-    } else {
-      tanh_scores<MOD, true>(sf, s);
-#pragma unroll
-      for (int e = 0; e < 16; e++) s[e] = final_score<MOD>(sf, s[e], first - (float)e, &keep);
-    }
+    for (int e = 0; e < 16; e++) s[e] = final_score<MOD>(sf, s[e], first - (float)e, &keep);
   }
 }
 __device__ __forceinline__ ScoreForm form_of(const CachedAttn& a, int h, bool ok) {
@@ -263,7 +262,8 @@ __device__ __forceinline__ uint4 first_tokens(uint4 v, int keep) {
 
 // ---- few rows: 16 per workgroup, NW waves share the keys out in tiles of 64, and put their results together in LDS ----
 // Bound by reading the cache, where it is long.  A tile's keys are asked for when the last one's have been multiplied, its values likewise, and the
-// pages two tiles ahead; three waves per SIMD hide the rest.
+// pages two tiles ahead; the SIMD's other waves (two of them up to 64 columns, one up to 128) hide the rest.  Tiles of 64 keys rather than 32: a wave's
+// softmax statistics, reductions over lanes and waits come half as often.
 template <int DHP, int NW> constexpr unsigned FEW_SMEM = NW * (DHP * 16 + 32) * 4 + 16;
 template <int DHP, bool WHOLE, bool F32, int MOD, int NW>
 __device__ __forceinline__ void few_rows(const CachedAttn& a, const Item& x, float* smem) {
@@ -316,7 +316,7 @@ __device__ __forceinline__ void few_rows(const CachedAttn& a, const Item& x, flo
 #pragma unroll
   for (int t = 0; t < KT; t++) load_q16<T, Q>((const T*)a.q + (i64)i * a.ldq + (i64)h * dh + 64 * t + 16 * g, ok && (WHOLE || 64 * t + 16 * g < dh), qf[t]);
   const ScoreForm sf = form_of(a, h, ok);
-  const float unit = MOD != 0 ? 1.f : sf.f;
+  const float unit = unit_of<MOD>(sf);
 
   f32x4 acc[DT];
 #pragma unroll
@@ -364,7 +364,7 @@ __device__ __forceinline__ void few_rows(const CachedAttn& a, const Item& x, flo
     const float ms = m == -INFINITY ? 0.f : m;
     float sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < 16; e++) { s[e] = fast_exp2(MOD != 0 ? s[e] - ms : fmaf(s[e], unit, -ms)); sum += s[e]; }
+    for (int e = 0; e < 16; e++) { s[e] = fast_exp2(MOD & BIASED ? s[e] - ms : fmaf(s[e], unit, -ms)); sum += s[e]; }
     l += sum;
     bf16x8 pf[Q][2];
 #pragma unroll
@@ -446,6 +446,10 @@ __device__ __forceinline__ void few_rows(const CachedAttn& a, const Item& x, flo
 }
 
 // ---- many rows: 32 per wave, tiles of 32 keys ----
+// Bound by the vector instructions of the softmax and the conversions, and by how many waves a SIMD has to take them from: two at 128 columns (195
+// registers), three at 64.  4096 rows of 32 heads to 8 of 128 columns behind 4096 tokens: 486 us, 0.85 PFLOP/s.  Each wave converts its tiles for itself: converted
+// once for the workgroup, in LDS, 553 us, with the reads a tile ahead 510; queries in LDS, which leaves registers for three waves, 547 us (502 with two):
+// more waves find less of each other's tiles in the L1 cache.  A tile's registers are filled again as soon as they are used up; with a second set 525.
 // LDS: the parts of three waves, then a row of floats for each
 template <int DHP> constexpr int ROWS_AT = 3 * 64 * (DHP / 2 + 2);
 template <int DHP> constexpr unsigned MANY_SMEM = (ROWS_AT<DHP> + 4 * DHP) * 4;
@@ -481,7 +485,7 @@ __device__ __forceinline__ void many_rows(const CachedAttn& a, const Item& x, fl
   }
   const int count = max(t1 - t0, 0);
   const ScoreForm sf = form_of(a, h, ok);
-  const float unit = MOD != 0 ? 1.f : sf.f;
+  const float unit = unit_of<MOD>(sf);
 
   // pages and scales of 64 tiles at a time, one tile per lane: of its first 16 tokens and of its second
   int page0 = 0, page1 = 0;
@@ -568,7 +572,7 @@ __device__ __forceinline__ void many_rows(const CachedAttn& a, const Item& x, fl
     const float ms = m == -INFINITY ? 0.f : m;
     float sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < 16; e++) { s[e] = fast_exp2(MOD != 0 ? s[e] - ms : fmaf(s[e], unit, -ms)); sum += s[e]; }
+    for (int e = 0; e < 16; e++) { s[e] = fast_exp2(MOD & BIASED ? s[e] - ms : fmaf(s[e], unit, -ms)); sum += s[e]; }
     l += sum;
     bf16x8 pf[Q][2];
 #pragma unroll
@@ -663,7 +667,7 @@ __device__ __forceinline__ void many_rows(const CachedAttn& a, const Item& x, fl
 }
 
 template <int DHP, bool WHOLE, bool F32, int MOD>
-__global__ void __launch_bounds__(256, DHP == 256 || F32 ? 1 : DHP == 128 ? 2 : 4) cached_attn_k(CachedAttn a) {
+__global__ void __launch_bounds__(256, DHP == 256 || F32 ? 1 : DHP == 128 ? 2 : 3) cached_attn_k(CachedAttn a) {
   extern __shared__ __attribute__((aligned(16))) float smem[];
   Item x;
   if (!find<false>(a, (int)blockIdx.x, &x)) return;

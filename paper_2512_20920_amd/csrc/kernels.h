@@ -426,7 +426,7 @@ struct CachedAttn {
   int split;                             // whose keys may be split: 0 nobody's, 1 few rows', 2 prompts' too
   int target;                            // into how many workgroups all keys are split
 };
-void cached_attn_plan(CachedAttn* a);               // few_only and split, from the sizes alone
+void cached_attn_plan(CachedAttn* a);               // few_only, split, lr and target, from the sizes alone
 size_t cached_attn_bytes(const CachedAttn& a);
 bool cached_attn_takes(const CachedAttn& a);        // whether the matrix-core kernels do (else row by row)
 void launch_cached_attn(CachedAttn a, void* work, bool rows, hipStream_t s);
