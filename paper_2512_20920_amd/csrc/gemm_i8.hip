@@ -23,6 +23,10 @@ __device__ __forceinline__ u32x4 rows_desc(const signed char* p, i64 ld, int row
              (unsigned)__builtin_amdgcn_readfirstlane((int)(n < (i64)OOB ? n : (i64)OOB)), 0x00020000u};
   return d;
 }
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const signed char* p, i64 ld, int row0, int rows, int K) {
+  const i64 n = rows > row0 ? ((i64)(rows - row0 - 1) * ld + K + 3) & ~3ll : 0;
+  return __builtin_amdgcn_make_buffer_rsrc((void*)(p + (i64)row0 * ld), (short)0, (int)(n < (i64)OOB ? n : (i64)OOB), 0x00020000);
+}
 __device__ __forceinline__ i32x4 fragment(const unsigned char* tile, int r, int kk, int lane) {
   return *(const i32x4*)(tile + r * KB + (((kk * 2 + (lane >> 5)) ^ ((r >> 1) & 7)) << 4));
 }
@@ -254,6 +258,51 @@ template <class T> __global__ void __launch_bounds__(512) gemm_i8_phased_k(GemmI
     }
 }
 
+// ---- a few rows: tiles of 32 x 32, whose k-tiles the eight waves share out ----
+// Reading b bounds it, of which every workgroup asks for all that it needs at once, or nearly: no k-tile waits for another one's place in LDS.
+// Fragments come from memory as they are, a row's 128 bytes by four loads; the waves' sums meet in LDS.
+template <class T> __global__ void __launch_bounds__(512) gemm_i8_few_k(GemmI8 g) {
+  constexpr int NW = 8;
+  __shared__ int part[NW][1024];
+  const int tiles_n = (g.N + 31) / 32, by = (int)blockIdx.x / tiles_n, m0 = by * 32, n0 = ((int)blockIdx.x - by * tiles_n) * 32;
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, c = (lane >> 5) * 16;
+  const __amdgpu_buffer_rsrc_t ra = rows_of(g.a, g.lda, m0, g.M, g.K), rb = rows_of(g.b, g.ldb, n0, g.N, g.K);
+  const unsigned ba = m0 + r < g.M ? (unsigned)r * (unsigned)g.lda + c : OOB, bb = n0 + r < g.N ? (unsigned)r * (unsigned)g.ldb + c : OOB;
+  i32x16 acc = {};
+  for (int kt = wv; kt * KB < g.K; kt += 2 * NW) {
+    i32x4 fa[2][4], fb[2][4];
+#pragma unroll
+    for (int u = 0; u < 2; u++)
+#pragma unroll
+      for (int kk = 0; kk < 4; kk++) {
+        const int k = (kt + u * NW) * KB + kk * 32;
+        const bool in = k + c < g.K;
+        fb[u][kk] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rb, in ? bb + k : OOB, 0, 0));
+        fa[u][kk] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(ra, in ? ba + k : OOB, 0, 0));
+      }
+#pragma unroll
+    for (int u = 0; u < 2; u++)
+#pragma unroll
+      for (int kk = 0; kk < 4; kk++) {
+        const int k = (kt + u * NW) * KB + kk * 32;
+        if (k + 32 > g.K && (g.K & 15)) fa[u][kk] = first_bytes(fa[u][kk], g.K - k - c);
+        acc = mfma(fa[u][kk], fb[u][kk], acc);
+      }
+  }
+#pragma unroll
+  for (int e = 0; e < 16; e++) part[wv][e * 64 + lane] = acc[e];
+  __syncthreads();
+  for (int j = threadIdx.x; j < 1024; j += NW * 64) {
+    const int e = j >> 6, l = j & 63, m = m0 + 8 * (e >> 2) + 4 * (l >> 5) + (e & 3), n = n0 + (l & 31);
+    if (m >= g.M || n >= g.N) continue;
+    int s = 0;
+#pragma unroll
+    for (int w = 0; w < NW; w++) s += part[w][j];
+    const float bias = g.bias ? to_f(((const T*)g.bias)[n]) : 0.f;
+    ((T*)g.c)[(i64)m * g.ldc + n] = from_f<T>(fmaf((float)s * g.sa[m], g.sb[n], bias));
+  }
+}
+
 // ---- any shape and alignment: a thread per result ----
 template <class T> __global__ void __launch_bounds__(256) gemm_i8_any_k(GemmI8 g) {
   const int n = blockIdx.x * 256 + threadIdx.x;
@@ -285,7 +334,10 @@ template <class T, int BM, int BN, int WGM, int NW, int NS> void go(const GemmI8
 // Measured, bfloat16 results, us for these four: 8192 x 14336, k 4096: 437 541 648 886 (2.2 * 10^15 multiplications and additions a second); 8192 x 2048,
 // k 2048: 39 45 50 71; 2048 x 11264, k 2048: 66 63 73 96; 611 x 11264, k 2048: 30 22 25 33; 2048 x 2048, k 2048: 29 19 15 19; 611 x 2048, k 2048:
 // 28 18 12 11; 256 x 4096, k 4096: 44 28 19 15; 8 x 6144, k 2048: 20 15 11 8.
+// A tile of 32 x 32 each, where no CU gets two (us, then the best of the others): 8 x 6144, k 2048: 5.2, 8.1; 48 x 4096, k 14336: 27, 39; 128 x 2048, k 5632:
+// 12.9, 17.3; beyond, 48 x 6144, k 2048: 8.9, 8.5; 8 x 14336, k 4096: 14.5, 13.6; 128 x 4096, k 14336: 52, 39.
 int form_for(const GemmI8& g) {
+  if ((i64)cdiv(g.M, 32) * cdiv(g.N, 32) <= 256) return 6;
   const struct { int form, bm, bn, round; float us; } shapes[] = {{2, 256, 256, 256, 1.93f}, {3, 128, 256, 256, 1.20f}, {4, 128, 128, 256, 0.72f}, {5, 64, 64, 512, 0.49f}};
   int best = 5;
   float least = INFINITY;
@@ -303,6 +355,7 @@ template <class T> void go(const GemmI8& g, int form, hipStream_t s) {
     case 2: launch(gemm_i8_phased_k<T>, mask, 256, 256, 512, 2 * 512 * KB, g, s); break;
     case 3: go<T, 128, 256, 2, 8, 3>(g, s); break;
     case 4: go<T, 128, 128, 4, 8, 4>(g, s); break;
+    case 6: hipLaunchKernelGGL((gemm_i8_few_k<T>), dim3((unsigned)cdiv(g.M, 32) * (unsigned)cdiv(g.N, 32)), dim3(512), 0, s, g); break;
     default: go<T, 64, 64, 2, 4, 4>(g, s);
   }
 }

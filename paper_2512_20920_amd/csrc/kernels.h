@@ -440,6 +440,6 @@ struct GemmI8 {
   int dt, M, N, K;
   i64 lda, ldb, ldc;
 };
-#define GEMM_I8_FORMS 4
+#define GEMM_I8_FORMS 5
 bool gemm_i8_takes(const GemmI8& g);                // whether the matrix-core kernels do
 void launch_gemm_i8(const GemmI8& g, int form, hipStream_t s);      // form: 0 by size, 1 any shape and alignment (slow), 2.. forced, see gemm_i8.hip

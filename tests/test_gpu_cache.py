@@ -548,7 +548,7 @@ def _product(dtype, M, N, K, mode, pad=0, bias=True, seed=0, off=0):
     return c
 
 
-FORMS = [0, 1] + [256 * t for t in range(1, 5)]
+FORMS = [0, 1] + [256 * t for t in range(1, 6)]
 
 
 @pytest.mark.parametrize("mode", FORMS)
