@@ -145,6 +145,19 @@ def test_append_single_tokens(n, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_append_of_many_sequences(dtype):
+    """Prompts, pieces, single tokens and nothing, in a list longer than a wave looks at at once."""
+    rng = np.random.default_rng(8)
+    n = 150
+    new = rng.integers(0, 3, n) * rng.integers(0, 30, n)
+    more = rng.integers(0, 2, n)
+    more[[2, 70, 149]] = 100, 33, 64
+    c = Paged(dtype, 2, 32, 16, _tables(rng, new + more, 16), seed=9)
+    c.append([int(x) for x in new], [int(x) for x in new], 2, _rotary(32))
+    c.append([int(x) for x in new + more], [int(x) for x in more], 2, _rotary(32))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_append_values(dtype):
     """Zeros, values that are not finite, far apart in size, around powers of two, and pages whose unit grows with each token."""
     dh, t = 32, TORCH[dtype]
@@ -394,6 +407,37 @@ def test_attention_of_many_rows(H, dh, rows, dtype):
     _fill(c, held)
     a = Attend(c, held, new, H, 0)
     a.run(window=(200 if rows == 390 else 0))
+    a.check()
+
+
+@MODES
+@pytest.mark.parametrize("n,prompts", [(64, 0), (65, 0), (65, 3), (150, 0), (150, 5), (300, 2)])
+def test_attention_of_many_sequences(n, prompts, dtype, mode):
+    """Lists longer than a wave looks at at once, long sequences and prompts among them, so that some keys are split and most are not."""
+    rng = np.random.default_rng(n + prompts)
+    held, new = rng.integers(0, 90, n), rng.integers(0, 2, n)
+    held[[3, n // 2, n - 1]] = 2600, 700, 1500
+    for s in rng.permutation(n)[:prompts]:
+        new[s] = min(held[s], 75)
+    held, new = [int(x) for x in held], [int(x) for x in new]
+    c = Paged(dtype, 2, 64, 16, _tables(rng, held, 16), seed=n)
+    _fill(c, held)
+    a = Attend(c, held, new, 8, mode)
+    a.run()
+    a.check()
+
+
+@MODES
+def test_attention_over_shared_pages(dtype, mode):
+    """Two sequences that begin alike name the same pages for it."""
+    table = np.array([[4, 1, 5, 0, -1], [4, 1, 5, 2, 3]])
+    held, new = [120, 155], [60, 2]
+    k, v = np.random.default_rng(3).standard_normal((2, sum(held), 2, 64))
+    k[120:216], v[120:216] = k[:96], v[:96]
+    c = Paged(dtype, 2, 64, 32, table)
+    _fill(c, held, k, v)
+    a = Attend(c, held, new, 4, mode)
+    a.run()
     a.check()
 
 
