@@ -291,7 +291,8 @@ __device__ __forceinline__ void few_rows(const CachedAttn& a, const Item& x, flo
 
   // where a lane's keys and values of a tile lie: token 16 gk + .. of the keys, 16 g + .. of the values
   const int gk = col >> 2;
-  auto page_of = [&](int t, int group) { return cache_page(c, x.s, (t * 64 + group * 16) >> lg); };      // (of any t: a place outside the table is no page)
+  // (of any t; what lies behind the last token is no page, whatever its unit may be)
+  auto page_of = [&](int t, int group) { const int j = t * 64 + group * 16, p = cache_page(c, x.s, j >> lg); return j < x.w.end ? p : -1; };
   int pk = page_of(t0, gk), pv = page_of(t0, g);
   uint4 k[4][KT], v[DT];
   float ks, vs;
@@ -376,6 +377,7 @@ __device__ __forceinline__ void few_rows(const CachedAttn& a, const Item& x, flo
     }
     if (kv + 64 > x.w.end || any_bad) {
       const int keep = bad ? 0 : x.w.end - kv - 16 * g;
+      vs = bad ? 1.f : vs;
 #pragma unroll
       for (int d = 0; d < DT; d++) v[d] = first_tokens(v[d], keep);
     }
@@ -494,7 +496,7 @@ __device__ __forceinline__ void many_rows(const CachedAttn& a, const Item& x, fl
     const int kv = (t0 + n + lane) * 32;
     const bool there = n + lane < count;
     page0 = there ? cache_page(c, x.s, kv >> lg) : -1;
-    page1 = there ? cache_page(c, x.s, (kv + 16) >> lg) : -1;
+    page1 = there && kv + 16 < x.w.end ? cache_page(c, x.s, (kv + 16) >> lg) : -1;      // (behind the last token there is none)
     const i64 b0 = cache_block(c, max(page0, 0), kh), b1 = cache_block(c, max(page1, 0), kh);
     ks0 = c.ks[b0]; ks1 = c.ks[b1]; vs0 = c.vs[b0]; vs1 = c.vs[b1];
   };
@@ -584,6 +586,7 @@ __device__ __forceinline__ void many_rows(const CachedAttn& a, const Item& x, fl
     }
     if (kv + 32 > x.w.end || any_bad) {
       const int keep = bad ? 0 : x.w.end - kv - 16 * g;
+      vs = bad ? 1.f : vs;
 #pragma unroll
       for (int d = 0; d < DT; d++) v[d] = first_tokens(v[d], keep);
     }

@@ -428,6 +428,26 @@ def test_attention_of_many_sequences(n, prompts, dtype, mode):
 
 
 @MODES
+@pytest.mark.parametrize("held,new", [([70, 300, 45, 17], [60, 1, 5, 17]), ([1000, 33], [1, 1]), ([150, 3000], [150, 1])])
+def test_attention_beside_pages_not_begun(held, new, dtype, mode):
+    """Entries behind a sequence's last token may name pages that nothing was appended to, whose units are NaN: the bits are those without them."""
+    table = _tables(np.random.default_rng(2), held, 16, spare=4)
+    out = []
+    for behind in (-1, table.max() + 1):
+        c = Paged(dtype, 1, 64, 16, np.where(table < 0, behind, table), pages=int(table.max()) + 2, seed=4)
+        _fill(c, held)
+        for s, n in enumerate(held):                         # nor is there anything in a last page's other places
+            if n % 16:
+                c.k[table[s, n // 16], :, n % 16:] = 255
+                c.v[table[s, n // 16], :, 0, :, n % 16:] = 255
+        a = Attend(c, held, new, 2, mode)
+        a.run()
+        a.check()
+        out.append((a.o, a.lse))
+    assert all(torch.equal(x.nan_to_num(5.0), y.nan_to_num(5.0)) for x, y in zip(*out))
+
+
+@MODES
 def test_attention_over_shared_pages(dtype, mode):
     """Two sequences that begin alike name the same pages for it."""
     table = np.array([[4, 1, 5, 0, -1], [4, 1, 5, 2, 3]])
