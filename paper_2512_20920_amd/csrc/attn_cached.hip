@@ -237,7 +237,11 @@ template <bool F32, int MOD, class S> __device__ __forceinline__ void final_scor
   if constexpr (F32 && (MOD & CAPPED)) {
 #pragma unroll
     for (int e = 0; e < 16; e++) s[e] = tanhf(s[e] * sf.x1);
-  } else tanh_scores<MOD, true>(sf, s);
+  } else {
+    // The second way of tanh_scores is off by 2^-22 of the CAP: a quarter of a unit at 10^6, in a tile's scores of order one as well.  Past 4096, of which that
+    // is 2^-10, only scores of at least 0.66 of the cap go it, so that errors are within 2^-21 of each score.
+    tanh_scores<MOD, true, true>(sf, s, a.cap > 4096.f);
+  }
   if constexpr (MOD & BIASED) {
     float keep;
 #pragma unroll

@@ -188,29 +188,35 @@ __device__ __forceinline__ ScoreForm score_form(const RangeAttn& a, int h) {
   s.slope2 = a.slopes ? a.slopes[h] * LOG2E : 0.f;
   return s;
 }
+// tanh up to |x| = 0.8: x times a polynomial in x^2, fitted to the least relative error there (6e-8)
+__device__ __forceinline__ float tanh_near(float x) {
+  const float u = x * x;
+  float p = fmaf(u, -4.355297423899174e-3f, 1.909329742193222e-2f);
+  p = fmaf(u, p, -5.311431363224983e-2f);
+  p = fmaf(u, p, 1.3321048021316528e-1f);
+  p = fmaf(u, p, -3.333267569541931e-1f);
+  p = fmaf(u, p, 9.999999403953552e-1f);
+  return p * x;
+}
 // q.k to tanh(q.k x1) where the kernel caps.  Forward (SERIES), up to |x| = 0.8, which the scores of a wave hardly ever pass (a cap is
-// there for the ones that do): x times a polynomial in x^2, fitted to the least relative error there (6e-8).  Beyond, and in the
+// there for the ones that do): tanh_near.  Beyond, and in the
 // backward kernels, 1 - 2 / (e^2x + 1), off by some 2^-22, which for a cap of 30 made the error of lse four times as large.  Eight
 // multiplications and additions take as long as an exponential and a reciprocal: within 2 % of each other at 4095 x 16 of 64.
-template <int MOD, bool SERIES> __device__ __forceinline__ void tanh_scores(const ScoreForm& sf, f32x16& a) {
+// EACH, each: every score by its own size, tanh_near up to 0.8.
+template <int MOD, bool SERIES, bool EACH = false> __device__ __forceinline__ void tanh_scores(const ScoreForm& sf, f32x16& a, bool each = false) {
   if constexpr (MOD & CAPPED) {
     float big = 0.f;
 #pragma unroll
     for (int e = 0; e < 16; e += 2) big = fmaxf(fmaxf(big, fabsf(a[e])), fabsf(a[e + 1]));
     if (!SERIES || __any(big * fabsf(sf.x1) > 0.8f)) {
 #pragma unroll
-      for (int e = 0; e < 16; e++) a[e] = fmaf(-2.f, __builtin_amdgcn_rcpf(fast_exp2(a[e] * (sf.x1 * (2.f * LOG2E))) + 1.f), 1.f);
+      for (int e = 0; e < 16; e++) {
+        const float far = fmaf(-2.f, __builtin_amdgcn_rcpf(fast_exp2(a[e] * (sf.x1 * (2.f * LOG2E))) + 1.f), 1.f);
+        a[e] = EACH && each && fabsf(a[e] * sf.x1) <= 0.8f ? tanh_near(a[e] * sf.x1) : far;
+      }
     } else {
 #pragma unroll
-      for (int e = 0; e < 16; e++) {
-        const float x = a[e] * sf.x1, u = x * x;
-        float p = fmaf(u, -4.355297423899174e-3f, 1.909329742193222e-2f);
-        p = fmaf(u, p, -5.311431363224983e-2f);
-        p = fmaf(u, p, 1.3321048021316528e-1f);
-        p = fmaf(u, p, -3.333267569541931e-1f);
-        p = fmaf(u, p, 9.999999403953552e-1f);
-        a[e] = p * x;
-      }
+      for (int e = 0; e < 16; e++) a[e] = tanh_near(a[e] * sf.x1);
     }
   }
 }

@@ -710,3 +710,17 @@ def test_a_served_layer(dtype):
         assert outside(_np(o).reshape(T, H, dh), *want["o"]) <= 1.0 and outside(_np(lse), *want["lse"]) <= 1.0
         y = product(o, wo, so, d, H * dh)
         assert torch.isfinite(y).all()
+
+
+# ---- calls at the ends of what is allowed ----------------------------------------------------------------------------
+@MODES
+@pytest.mark.parametrize("cap,bias", [(5000.0, False), (1e5, True), (1e6, False)])
+def test_attention_caps_above_some_rows_scores(cap, bias, dtype, mode):
+    """Rows whose scores are of order one beside rows whose scores reach a cap of thousands and more, in the same tiles: a score's error goes by its own
+    size, not by the cap (the bounds' 8 half steps of each score)."""
+    c = Paged(dtype, 1, 64, 32, [[2, 0, 1, 4, 3, 5], [7, 6, 8, 9, 10, 11]])
+    _fill(c, [150, 70])
+    a = Attend(c, [150, 70], [110, 2], 2, mode, scale=cap / 8, cap=cap, slopes=_slopes(2) if bias else None)
+    a.q[1:112:2] *= 2.0 ** -round(np.log2(cap))
+    a.run()
+    a.check()
