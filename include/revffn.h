@@ -481,7 +481,7 @@ int revffn_op_cache_append(int32_t dtype, const revffn_cache *cache, const revff
                            void *hip_stream);
 
 /* Attention of the call's rows (desc->Tq of them) over the cache, which holds their own tokens already.  Of desc, Tk, ldk and ldv are not read; Hkv and dh
- * must be the cache's; slopes count from the row's token; kernel_mode 0, 1 or 2.  (A bfloat16 softcap above 4096 stays on the matrix cores here.)  causal: a row sees its sequence's tokens up to its own, with
+ * must be the cache's; slopes count from the row's token; kernel_mode 0, 1 or 2.  (A bfloat16 softcap above 4096 stays on the matrix cores here; one above 10^30 is none.)  causal: a row sees its sequence's tokens up to its own, with
  * window > 0 the last `window` of them only; not causal: all len[s].  o and lse as of revffn_op_attention_masked_fwd, and as there nothing that a row does not
  * see reaches it.  Single tokens' and short prompts' keys are split over workgroups, by the lengths on the device, and joined: the bits of a row
  * depend on the other sequences of its call, and are the same whenever the call is.  work: revffn_op_attention_cached_workspace bytes of

@@ -105,7 +105,9 @@ int check_cached(const revffn_attn_desc* d, const revffn_cache* c, CachedAttn* a
   TRY(check_cache(c, &a->c));
   if (d->kernel_mode >> 8 || d->Hkv != c->Hkv || d->dh != c->dh) return REVFFN_EINVAL;
   if (!grid_fits((i64)d->Tq * d->H + 4 * (i64)c->n_seqs * c->Hkv)) return REVFFN_ESHAPE;
-  a->slopes = r.slopes; a->dt = r.dt; a->H = r.H; a->G = r.G; a->T = r.Tq; a->ldq = r.ldq; a->ldo = r.ldo; a->scale = r.scale; a->cap = r.cap;
+  a->slopes = r.slopes; a->dt = r.dt; a->H = r.H; a->G = r.G; a->T = r.Tq; a->ldq = r.ldq; a->ldo = r.ldo; a->scale = r.scale;
+  // (from 2.4 * 10^38 on a cap in units of log2 is no float.  One above 10^30 changes no score z up to 10^26 by half a step: by z^3 / 3 cap^2.)
+  a->cap = r.cap > 1e30f ? 0.f : r.cap;
   cached_attn_plan(a);
   return 0;
 }

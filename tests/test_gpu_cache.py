@@ -724,3 +724,15 @@ def test_attention_caps_above_some_rows_scores(cap, bias, dtype, mode):
     a.q[1:112:2] *= 2.0 ** -round(np.log2(cap))
     a.run()
     a.check()
+
+
+@MODES
+@pytest.mark.parametrize("cap", [1e31, 3.4e38])
+def test_attention_caps_without_end(cap, dtype, mode):
+    """A cap near the type's largest value changes no score: the results are those without, single keys with negative scores among them."""
+    held, new = [1, 1, 1, 1, 1, 40, 90], [1, 1, 1, 1, 1, 1, 60]
+    c = Paged(dtype, 2, 64, 32, _tables(np.random.default_rng(1), held, 32))
+    _fill(c, held)
+    a = Attend(c, held, new, 4, mode, scale=0.3, cap=cap)
+    a.run()
+    a.check()
