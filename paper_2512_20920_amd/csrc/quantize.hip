@@ -2,14 +2,14 @@
 // One pass over memory, which bounds it: a row's values wait in registers for its maximum (8192 x 4096 bfloat16: 23 us, 4.4 TB/s; 8 rows: a launch's 3).
 //
 // The quotient is rounded as if it were exact.  k = rint(x (1 / scale)) is right or next to it; x - k scale is a float (a multiple of half a
-// step of scale, of at most 25 bits of which the last is zero where the first is not), so one comparison with scale / 2 tells which.
+// step of scale, of at most 25 bits of which the last is zero where the first is not), so one comparison of twice that with scale tells which
+// (scale / 2 itself need be no float: below 2^-125 scale may be an odd number of 2^-149).
 #include "kernels.h"
 
 // V codes in the low bytes of k.  x / scale + 1.5 2^23 has the nearest integer in its low bits; where no lane's remainder is half a step or more, as in
 // nearly every wavefront, there is nothing to choose.
 template <int V> __device__ __forceinline__ void codes_of(const float (&x)[V], float scale, float inv, unsigned (&k)[V]) {
   constexpr float BIG = 12582912.f;
-  const float half = 0.5f * scale;
   float worst = 0.f;
 #pragma unroll
   for (int i = 0; i < V; i++) {
@@ -17,11 +17,11 @@ template <int V> __device__ __forceinline__ void codes_of(const float (&x)[V], f
     k[i] = __builtin_bit_cast(unsigned, z);
     worst = fmaxf(worst, fabsf(fmaf(BIG - z, scale, x[i])));
   }
-  if (__any(worst >= half)) {
+  if (__any(2.f * worst >= scale)) {
 #pragma unroll
     for (int i = 0; i < V; i++) {
-      const float r = fmaf(BIG - __builtin_bit_cast(float, k[i]), scale, x[i]);
-      if (fabsf(r) > half || (fabsf(r) == half && (k[i] & 1))) k[i] += r > 0.f ? 1 : -1;
+      const float r = 2.f * fmaf(BIG - __builtin_bit_cast(float, k[i]), scale, x[i]);
+      if (fabsf(r) > scale || (fabsf(r) == scale && (k[i] & 1))) k[i] += r > 0.f ? 1 : -1;
     }
   }
 }

@@ -736,3 +736,21 @@ def test_attention_caps_without_end(cap, dtype, mode):
     a = Attend(c, held, new, 4, mode, scale=0.3, cap=cap)
     a.run()
     a.check()
+
+
+def test_quantize_rows_of_the_smallest_scales():
+    """Scales just above 2^-126, where half of one may lie between two numbers: values a 2^-149 to both sides of each half."""
+    rng = np.random.default_rng(11)
+    unit, rows = 2.0 ** -149, 3000
+    steps = 2 ** 23 + 2 * rng.integers(0, 2 ** 20, rows) + 1         # the scale: an odd number of 2^-149
+    x = np.zeros((rows, 16))
+    x[:, 0] = np.float32(127 * steps * unit)
+    for i in range(7):
+        for side in range(2):                                # (the two numbers around a half of the scale, or one and a half: exact, below 2^24 units)
+            x[:, 1 + 2 * i + side] = ((steps * (1 + 2 * (i % 2)) // 2) + side) * unit * (-1) ** i
+    x = torch.from_numpy(x.astype(np.float32)).cuda()
+    codes, scale = torch.empty(rows, 16, dtype=torch.int8, device="cuda"), torch.empty(rows, dtype=torch.float32, device="cuda")
+    R.revffn_op_quantize_rows(0, x, codes, scale, rows, 16, 16, 16)
+    torch.cuda.synchronize()
+    want, unit = ref.quantized(_np(x))
+    assert np.array_equal(_np(scale), unit) and np.array_equal(codes.cpu().numpy(), want)
