@@ -277,7 +277,7 @@ int revffn_op_attention_cached(const revffn_attn_desc* desc, const revffn_cache*
 
 int revffn_op_quantize_rows(int32_t dtype, const void* x, int8_t* codes, float* scale, int32_t rows, int32_t cols, int64_t ldx, int64_t ldc, void* stream) {
   if (rows > 0 && (!x || !codes || !scale)) return REVFFN_ENULL;
-  if ((dtype != 0 && dtype != 1) || rows < 0 || cols < 1 || cols > (1 << 24) || (rows > 0 && ((const void*)codes == x || (const void*)scale == x))) return REVFFN_EINVAL;
+  if ((dtype != 0 && dtype != 1) || rows < 0 || cols < 1 || cols > (1 << 24) || (rows > 0 && same_place({codes, scale}, {x}))) return REVFFN_EINVAL;
   if (ldx < cols || ldc < cols || !grid_fits(rows)) return REVFFN_ESHAPE;
   launch_quantize_rows(dtype, x, (signed char*)codes, scale, rows, cols, ldx, ldc, (hipStream_t)stream);
   return 0;

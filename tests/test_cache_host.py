@@ -199,3 +199,8 @@ def test_integers_of_the_reference():
     x = np.array([[1.0, -127.0, 63.5, 2.5, -0.5], [0, 0, 0, 0, 0], [1e-40, 0, 0, 0, 0], [np.inf, 1, 1, 1, 1], [np.nan, 0, 0, 0, 0]])
     codes, scale = ref.quantized(x)
     assert codes[0].tolist() == [1, -127, 64, 2, 0] and scale[0] == 1.0 and scale[1] == scale[2] == 0 and np.isnan(scale[3:]).all() and not codes[1:].any()
+
+
+# ---- results in the place of results, and calls at the ends of what is allowed -----------------------------------------
+def test_rows_to_integers_refuse_codes_in_the_place_of_scales(lib):
+    assert lib.revffn_op_quantize_rows(1, P, 3 * P, 3 * P, 5, 64, 64, 64, None) == EINVAL
