@@ -99,8 +99,12 @@ int check_cache(const revffn_cache* c, CacheView* v) {
   return 0;
 }
 int check_cached(const revffn_attn_desc* d, const revffn_cache* c, CachedAttn* a) {
+  if (!d) return REVFFN_ENULL;
+  revffn_attn_desc rows = *d;
+  rows.Tk = 0;
+  rows.ldk = rows.ldv = 0;                           // (keys are the cache's)
   RangeAttn r;
-  TRY(check_desc(d, &r));
+  TRY(check_desc(&rows, &r));
   *a = CachedAttn{};
   TRY(check_cache(c, &a->c));
   if (d->kernel_mode >> 8 || d->Hkv != c->Hkv || d->dh != c->dh) return REVFFN_EINVAL;

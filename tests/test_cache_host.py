@@ -204,3 +204,12 @@ def test_integers_of_the_reference():
 # ---- results in the place of results, and calls at the ends of what is allowed -----------------------------------------
 def test_rows_to_integers_refuse_codes_in_the_place_of_scales(lib):
     assert lib.revffn_op_quantize_rows(1, P, 3 * P, 3 * P, 5, 64, 64, 64, None) == EINVAL
+
+
+@pytest.mark.parametrize("kw", [dict(Tk=-1), dict(Tk=2 ** 26), dict(ldk=64), dict(ldk=-5, ldv=1), dict(ldv=1)])
+def test_attention_does_not_read_the_keys_fields(lib, kw):
+    """The cache says where keys are: whatever the desc holds of them, it is the same call."""
+    c = cache(max_pages=400)
+    need = lib.revffn_op_attention_cached_workspace(ctypes.byref(desc()), ctypes.byref(c))
+    assert lib.revffn_op_attention_cached_workspace(ctypes.byref(desc(**kw)), ctypes.byref(c)) == need > 0
+    assert attend(lib, desc(Tq=0, **kw), c, q=None, o=None, lse=None, work=None, size=0) == 0
