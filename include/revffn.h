@@ -486,7 +486,7 @@ int revffn_op_cache_append(int32_t dtype, const revffn_cache *cache, const revff
  * see reaches it.  Single tokens' and short prompts' keys are split over workgroups, by the lengths on the device, and joined: the bits of a row
  * depend on the other sequences of its call, and are the same whenever the call is.  work: revffn_op_attention_cached_workspace bytes of
  * this very desc and cache's sizes.  The matrix-core kernels take rows aligned to 16 bytes, in float32 heads of up to 128 columns; others go row
- * by row (kernel_mode 2: REVFFN_EUNSUPPORTED). */
+ * by row (kernel_mode 2: REVFFN_EUNSUPPORTED).  (Tq + 3) / 4 * H + min(n_seqs, Tq) * Hkv has to stay below 2^24 (REVFFN_ESHAPE). */
 size_t revffn_op_attention_cached_workspace(const revffn_attn_desc *desc, const revffn_cache *cache);
 int revffn_op_attention_cached(const revffn_attn_desc *desc, const revffn_cache *cache, int32_t causal, int32_t window, const void *q, void *o,
                                float *lse, void *work, size_t work_bytes, void *hip_stream);

@@ -108,7 +108,9 @@ int check_cached(const revffn_attn_desc* d, const revffn_cache* c, CachedAttn* a
   *a = CachedAttn{};
   TRY(check_cache(c, &a->c));
   if (d->kernel_mode >> 8 || d->Hkv != c->Hkv || d->dh != c->dh) return REVFFN_EINVAL;
-  if (!grid_fits((i64)d->Tq * d->H + 4 * (i64)c->n_seqs * c->Hkv)) return REVFFN_ESHAPE;
+  // (a wave per row of the join, and up to a workgroup per sequence and key head that is not full: the largest grid that a call can have)
+  const i64 seqs = c->n_seqs < d->Tq ? c->n_seqs : d->Tq;
+  if (!grid_fits(((i64)d->Tq + 3) / 4 * d->H + seqs * c->Hkv)) return REVFFN_ESHAPE;
   a->slopes = r.slopes; a->dt = r.dt; a->H = r.H; a->G = r.G; a->T = r.Tq; a->ldq = r.ldq; a->ldo = r.ldo; a->scale = r.scale;
   // (from 2.4 * 10^38 on a cap in units of log2 is no float.  One above 10^30 changes no score z up to 10^26 by half a step: by z^3 / 3 cap^2.)
   a->cap = r.cap > 1e30f ? 0.f : r.cap;

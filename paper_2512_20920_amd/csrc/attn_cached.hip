@@ -64,7 +64,7 @@ template <bool JOIN> __device__ __forceinline__ bool find(const CachedAttn& a, i
       groups += (float)w.groups;
     }
     const float heads = (float)a.c.Hkv;
-    per = max((int)(wave_sum(sum) * (heads / (float)a.target)) + 1, 1);
+    per = (int)fminf(wave_sum(sum) * (heads / (float)a.target), 0x1p30f) + 1;
     if (per > 1 && n <= 64) {
       const float most = fmaxf((float)a.target, wave_sum(groups) * heads);
       for (int i = 0; i < 8; i++) {
@@ -79,8 +79,9 @@ template <bool JOIN> __device__ __forceinline__ bool find(const CachedAttn& a, i
   for (int s0 = 0; s0 < n; s0 += 64) {
     const SeqWork w = s0 == 0 ? first : s0 + lane < n ? work_of(a, s0 + lane) : SeqWork{};
     const int k = splits_of(a, w, per);
-    // (first rows that are out of order can ask for more than there are: no sum overflows, and whoever is past the scratch memory stays out of it)
-    const int groups = min(w.groups, 1 << 20) * a.c.Hkv, quads = (int)(((i64)w.n * a.G + 3) >> 2) * a.c.Hkv;
+    // (first rows that are out of order can ask for more than there are: a sequence has at most all T of them, with T * H < 2^26 no sum of 64 overflows, and
+    // whoever is past the scratch memory stays out of it)
+    const int groups = w.groups * a.c.Hkv, quads = (int)(((i64)w.n * a.G + 3) >> 2) * a.c.Hkv;
     const int mine = min(JOIN ? (k > 1 ? quads : 0) : groups * k, 1 << 24);
     const int room = min(k > 1 ? groups * k * (w.few ? 1 : 1 << (a.lr - 4)) : 0, 1 << 24);
     const int running = wave_running(mine), all = __builtin_amdgcn_readlane(running, 63), rooms = wave_running(room);

@@ -213,3 +213,15 @@ def test_attention_does_not_read_the_keys_fields(lib, kw):
     need = lib.revffn_op_attention_cached_workspace(ctypes.byref(desc()), ctypes.byref(c))
     assert lib.revffn_op_attention_cached_workspace(ctypes.byref(desc(**kw)), ctypes.byref(c)) == need > 0
     assert attend(lib, desc(Tq=0, **kw), c, q=None, o=None, lse=None, work=None, size=0) == 0
+
+
+def test_attention_takes_every_call_that_a_launch_can_hold(lib):
+    """Rows times heads, and sequences that have rows times key heads: as the header says, whatever the number of sequences without."""
+    size = lambda d, c: lib.revffn_op_attention_cached_workspace(ctypes.byref(d), ctypes.byref(c))
+    wide = cache(max_pages=400)
+    assert size(desc(Tq=131072, H=128), wide) > 0 and size(desc(Tq=2 ** 19 - 100, H=128), wide) > 0
+    many = dict(n_seqs=2 ** 20, Hkv=8, max_pages=400)
+    assert size(desc(H=8, Hkv=8), cache(**many)) > 0 and size(desc(Tq=2 ** 20, H=8, Hkv=8), cache(**many)) > 0
+    assert size(desc(Tq=2 ** 20, H=16, Hkv=16), cache(**many | dict(Hkv=16))) == 0
+    assert attend(lib, desc(Tq=2 ** 20, H=16, Hkv=16), cache(**many | dict(Hkv=16))) == ESHAPE
+    assert attend(lib, desc(Tq=2 ** 19, H=128), wide) == ESHAPE

@@ -754,3 +754,65 @@ def test_quantize_rows_of_the_smallest_scales():
     torch.cuda.synchronize()
     want, unit = ref.quantized(_np(x))
     assert np.array_equal(_np(scale), unit) and np.array_equal(codes.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("mode", [2, 1])
+def test_attention_of_more_than_two_to_the_24_rows(mode):
+    """131075 rows of 128 heads: one sequence with nearly all, two with a few; every row against float32, spot rows against 64 bits."""
+    H, Hkv, dh, page, held, new = 128, 2, 16, 16, [20, 40, 33], [1, 131072, 2]
+    T, G = sum(new), H // Hkv
+    c = Paged("bf16", Hkv, dh, page, _tables(np.random.default_rng(2), held, page), seed=12)
+    _fill(c, held)
+    q = torch.randn(T, H, dh, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(torch.bfloat16)
+    o, lse = torch.full_like(q, NAN), torch.full((H, T), NAN, dtype=torch.float32, device="cuda")
+    cache = c.cache(held, np.cumsum([0] + new))
+    desc = R.AttnDesc(dtype=1, kernel_mode=mode, H=H, Hkv=Hkv, dh=dh, Tq=T)
+    work = torch.empty(R.revffn_op_attention_cached_workspace(desc, cache), dtype=torch.uint8, device="cuda")
+    R.revffn_op_attention_cached(desc, cache, False, 0, q, o, lse, work)
+    torch.cuda.synchronize()
+    row = 0
+    for s, n in enumerate(new):
+        k, v = (torch.from_numpy(c.model.rows(x, c.table, s, held[s])).float().cuda() for x in "kv")
+        for at in range(row, row + n, 16384):
+            end = min(at + 16384, row + n)
+            for h in range(Hkv):
+                qq = q[at:end, h * G:(h + 1) * G].float().reshape(-1, dh)
+                x = qq @ k[:, h].T.contiguous() / 4
+                p = torch.softmax(x, -1)
+                want, size = p @ v[:, h], p @ v[:, h].abs()
+                # half a step of bfloat16 for the probabilities, one for the result; then float32's on both sides, scores (24 half steps of sums up to 6) and sums (56)
+                bound = 2.0 ** -8 * (size + want.abs()) + 2.0 ** -14 * size
+                got = o[at:end, h * G:(h + 1) * G].float().reshape(-1, dh)
+                assert ((got - want).abs() <= bound).all(), (s, at, h)
+                l = lse[h * G:(h + 1) * G, at:end].T.reshape(-1)
+                assert ((l - torch.logsumexp(x, -1)).abs() <= 2.0 ** -14).all()
+        row += n
+    for i, s in ((0, 0), (1, 1), (77777, 1), (131072, 1), (131073, 2), (131074, 2)):
+        want = ref.attention(c.model, c.table[s:s + 1], held[s:s + 1], [1], _np(q[i:i + 1]), causal=False)
+        assert outside(_np(o[i:i + 1]), *want["o"]) <= 1.0 and outside(_np(lse[:, i:i + 1]), *want["lse"]) <= 1.0
+
+
+def _among_many(at, n, held, new, table):
+    """Lists of n sequences that hold nothing and get nothing, but for those at `at`."""
+    many = np.full((n, table.shape[1]), -1)
+    many[at] = table
+    h, r = np.zeros(n, int), np.zeros(n, int)
+    h[at], r[at] = held, new
+    return _ints(many), _ints(h), _ints(np.concatenate([[0], np.cumsum(r)]))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_among_a_million_sequences(dtype):
+    """As many sequences as there may be, four of them with rows."""
+    held, new, n = [20, 100, 5, 64], [1, 2, 1, 30], 2 ** 20
+    c = Paged(dtype, 4, 64, 16, _tables(np.random.default_rng(3), held, 16))
+    _fill(c, held)
+    a = Attend(c, held, new, 8, 2)
+    lists = _among_many([0, 77, 2 ** 19, n - 1], n, held, new, c.table)
+    cache = R.Cache(c.k, c.v, c.ks, c.vs, *lists, pages=c.pages, page=16, max_pages=c.table.shape[1], n_seqs=n, Hkv=4, dh=64)
+    work = torch.empty(R.revffn_op_attention_cached_workspace(a.desc, cache), dtype=torch.uint8, device="cuda")
+    R.revffn_op_attention_cached(a.desc, cache, True, 0, a.q, a.o, a.lse, work)
+    b = ref.attention(c.model, c.table, held, new, a.queries(), dtype=dtype)
+    o, lse = a.results()
+    assert torch.isnan(a.o[a.T:]).all() and torch.isnan(a.lse[:, a.T:]).all()
+    assert outside(o, *b["o"]) <= 1.0 and outside(lse, *b["lse"]) <= 1.0
