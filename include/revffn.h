@@ -475,7 +475,9 @@ typedef struct revffn_cache {
  * least power of two (2^-96 .. 2^119) that brings its largest value within 448; if a page that holds tokens already needs a larger one, they are
  * rounded again to it (which changes only numbers below 2^-6 of the new unit).  A value that is not finite is stored as NaN and does not count
  * for the unit.  Only the pages and heads that get rows are written, and of those only the rows and what is rounded again.  A page that gets rows
- * must not be named by another entry of the table that gets rows too: shared pages are for reading. */
+ * must not be named by another entry of the table that gets rows too: shared pages are for reading.  Queries of rows that stand before token 0
+ * or from max_pages * page on are left as they were.  REVFFN_ESHAPE: a stride below the rows' width, or a launch of 2^32 threads and more: a row's
+ * queries take 64, a page's new rows of a key head up to 512, and a call is taken to meet T / page + 2 min(n_seqs, T) pages. */
 int revffn_op_cache_append(int32_t dtype, const revffn_cache *cache, const revffn_rotary *r, const int32_t *pos, const void *q, void *q_out,
                            const void *k, const void *v, int32_t T, int32_t H, int64_t ldq, int64_t ldqo, int64_t ldk, int64_t ldv,
                            void *hip_stream);

@@ -253,9 +253,10 @@ int revffn_op_cache_append(int32_t dtype, const revffn_cache* cache, const revff
   a.mag = r && r->magnitude != 0.f ? r->magnitude : 1.f;
   const i64 wq = (i64)H * cache->dh, wk = (i64)cache->Hkv * cache->dh;
   if (ldk < wk || ldv < wk || (q && (ldq < wq || ldqo < wq || (q == q_out && ldq != ldqo)))) return REVFFN_ESHAPE;
-  if (!grid_fits(((i64)T / cache->page + 2 * (i64)cache->n_seqs) * 2 * cache->Hkv + T) || (q && wq > INT32_MAX)) return REVFFN_ESHAPE;
+  if (q && wq > INT32_MAX) return REVFFN_ESHAPE;
   if (T > 0 && same_place({cache->k, cache->v, cache->k_scale, cache->v_scale, q ? q_out : nullptr}, {k, v})) return REVFFN_EINVAL;
   a.q = q; a.q_out = q_out; a.k = k; a.v = v; a.pos = pos; a.dt = dtype; a.T = T; a.H = H; a.ldq = ldq; a.ldqo = ldqo; a.ldk = ldk; a.ldv = ldv;
+  if (!cache_append_fits(a)) return REVFFN_ESHAPE;
   if (T > 0 && cache->n_seqs > 0) launch_cache_append(a, (hipStream_t)stream);
   return 0;
 }

@@ -334,35 +334,52 @@ __global__ void __launch_bounds__(WPH > 4 ? WPH * 64 : 256) cache_append_k(Cache
   }
 }
 
-template <class T, int UN, int WPH> static void launch(const CacheAppend& a, i64 visits, bool wide, hipStream_t s) {
-  constexpr int WAVES = WPH > 4 ? WPH : 4, HEADS = WAVES / WPH;
-  const int loop = visits * cdiv(a.c.Hkv, HEADS) >= 512 ? 2 : 1, vblocks = cdiv(a.c.Hkv, HEADS * loop);
-  const dim3 grid((unsigned)(visits * 2 * vblocks + (a.q ? cdiv(a.T, WAVES) : 0))), block(WAVES * 64);
+// Waves per head of a page, and what follows from them: a launch's grid
+struct AppendShape { int wph, waves, loop, vblocks; i64 visits, grid; };
+static AppendShape shape_of(const CacheAppend& a) {
+  const CacheView& c = a.c;
+  const int units = (c.dh << c.lg) >> 4;
+  AppendShape r;
+  r.wph = units <= 64 ? 1 : units <= 128 ? 2 : units <= 512 ? 4 : 8;
+  r.waves = r.wph > 4 ? r.wph : 4;
+  // a sequence's n new rows meet at most (n - 1) / page + 2 pages
+  r.visits = c.cu ? ((i64)a.T >> c.lg) + 2 * (i64)(c.n_seqs < a.T ? c.n_seqs : a.T) : (a.T < c.n_seqs ? a.T : c.n_seqs);
+  const int heads = r.waves / r.wph;
+  r.loop = r.visits * cdiv(c.Hkv, heads) >= 512 ? 2 : 1;
+  r.vblocks = cdiv(c.Hkv, heads * r.loop);
+  r.grid = r.visits * 2 * r.vblocks + (a.q ? cdiv(a.T, r.waves) : 0);
+  return r;
+}
+bool cache_append_fits(const CacheAppend& a) {
+  const AppendShape r = shape_of(a);
+  return r.grid * (r.waves * 64) < (i64)1 << 32;
+}
+template <class T, int UN, int WPH> static void launch(const CacheAppend& a, const AppendShape& r, bool wide, hipStream_t s) {
+  const dim3 grid((unsigned)r.grid), block(r.waves * 64);
+  const int visits = (int)r.visits;
   if (a.interleaved) {
-    if (wide) hipLaunchKernelGGL((cache_append_k<T, UN, WPH, true, true>), grid, block, 0, s, a, (int)visits, vblocks, loop);
-    else hipLaunchKernelGGL((cache_append_k<T, UN, WPH, true, false>), grid, block, 0, s, a, (int)visits, vblocks, loop);
+    if (wide) hipLaunchKernelGGL((cache_append_k<T, UN, WPH, true, true>), grid, block, 0, s, a, visits, r.vblocks, r.loop);
+    else hipLaunchKernelGGL((cache_append_k<T, UN, WPH, true, false>), grid, block, 0, s, a, visits, r.vblocks, r.loop);
   } else {
-    if (wide) hipLaunchKernelGGL((cache_append_k<T, UN, WPH, false, true>), grid, block, 0, s, a, (int)visits, vblocks, loop);
-    else hipLaunchKernelGGL((cache_append_k<T, UN, WPH, false, false>), grid, block, 0, s, a, (int)visits, vblocks, loop);
+    if (wide) hipLaunchKernelGGL((cache_append_k<T, UN, WPH, false, true>), grid, block, 0, s, a, visits, r.vblocks, r.loop);
+    else hipLaunchKernelGGL((cache_append_k<T, UN, WPH, false, false>), grid, block, 0, s, a, visits, r.vblocks, r.loop);
   }
 }
-template <class T> static void launch(const CacheAppend& a, i64 visits, bool wide, hipStream_t s) {
-  const int units = (a.c.dh << a.c.lg) >> 4;
-  if (units <= 64) launch<T, 1, 1>(a, visits, wide, s);
-  else if (units <= 128) launch<T, 1, 2>(a, visits, wide, s);
-  else if (units <= 256) launch<T, 1, 4>(a, visits, wide, s);
-  else if (units <= 512) launch<T, 2, 4>(a, visits, wide, s);
-  else launch<T, 2, 8>(a, visits, wide, s);
+template <class T> static void launch(const CacheAppend& a, const AppendShape& r, bool wide, hipStream_t s) {
+  switch (r.wph) {
+    case 1: launch<T, 1, 1>(a, r, wide, s); break;
+    case 2: launch<T, 1, 2>(a, r, wide, s); break;
+    case 4: if ((a.c.dh << a.c.lg) >> 4 <= 256) launch<T, 1, 4>(a, r, wide, s); else launch<T, 2, 4>(a, r, wide, s); break;
+    default: launch<T, 2, 8>(a, r, wide, s);
+  }
 }
 void launch_cache_append(const CacheAppend& a, hipStream_t s) {
-  const CacheView& c = a.c;
-  // a sequence's n new rows meet at most (n - 1) / page + 2 pages
-  const i64 visits = c.cu ? ((i64)a.T >> c.lg) + 2 * (i64)(c.n_seqs < a.T ? c.n_seqs : a.T) : (a.T < c.n_seqs ? a.T : c.n_seqs);
-  if (visits == 0) return;
+  const AppendShape r = shape_of(a);
+  if (r.visits == 0) return;
   const int es = a.dt == 0 ? 4 : 2;
   const i64 strides = a.ldk | a.ldv | (a.q ? a.ldq | a.ldqo : 0);
   const uintptr_t at = (uintptr_t)a.k | (uintptr_t)a.v | (a.q ? (uintptr_t)a.q | (uintptr_t)a.q_out : 0);
   const bool wide = strides * es % 16 == 0 && at % 16 == 0;
-  if (a.dt == 0) launch<float>(a, visits, wide, s);
-  else launch<bf16>(a, visits, wide, s);
+  if (a.dt == 0) launch<float>(a, r, wide, s);
+  else launch<bf16>(a, r, wide, s);
 }

@@ -412,6 +412,7 @@ struct CacheAppend {
   float mag;
   double freq[ROTARY_MAX_DIMS / 2];      // in turns
 };
+bool cache_append_fits(const CacheAppend& a);       // whether one launch can hold it
 void launch_cache_append(const CacheAppend& a, hipStream_t s);
 struct CachedAttn {
   CacheView c;

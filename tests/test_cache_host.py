@@ -225,3 +225,10 @@ def test_attention_takes_every_call_that_a_launch_can_hold(lib):
     assert size(desc(Tq=2 ** 20, H=16, Hkv=16), cache(**many | dict(Hkv=16))) == 0
     assert attend(lib, desc(Tq=2 ** 20, H=16, Hkv=16), cache(**many | dict(Hkv=16))) == ESHAPE
     assert attend(lib, desc(Tq=2 ** 19, H=128), wide) == ESHAPE
+
+
+def test_append_refuses_more_than_a_launch_can_hold(lib):
+    """2^32 threads and more: for pages that get rows times key heads, for queries; of eight waves per page and head (and odd numbers of heads) too."""
+    c = cache(n_seqs=2 ** 20, Hkv=64)
+    assert append(lib, c, T=2 ** 20, ldk=4096, ldv=4096) == ESHAPE and append(lib, cache(), T=2 ** 26) == ESHAPE
+    assert append(lib, cache(n_seqs=2 ** 20, Hkv=3, dh=128, page=128), T=2 ** 20, q=None, q_out=None, ldk=384, ldv=384) == ESHAPE

@@ -816,3 +816,27 @@ def test_attention_among_a_million_sequences(dtype):
     o, lse = a.results()
     assert torch.isnan(a.o[a.T:]).all() and torch.isnan(a.lse[:, a.T:]).all()
     assert outside(o, *b["o"]) <= 1.0 and outside(lse, *b["lse"]) <= 1.0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_append_among_a_million_sequences(dtype):
+    """As many sequences as there may be, four of them with rows: the cache and the queries of a call of those alone."""
+    held, new, n, Hkv, H, dh = [20, 100, 5, 64], [1, 2, 1, 30], 2 ** 20, 4, 8, 64
+    table, T = _tables(np.random.default_rng(4), held, 16), 34
+    x = _normal(np.random.default_rng(5), dtype, T, (H + 2 * Hkv) * dh)
+    w, out = x.stride(0), []
+    for many in (False, True):
+        c = Paged(dtype, Hkv, dh, 16, table, seed=6)
+        _fill(c, [19, 98, 4, 34])                            # what is there already
+        for t in (c.ks, c.vs):
+            t.nan_to_num_(0)
+        cache = c.cache(held, np.cumsum([0] + new))
+        if many:
+            lists = _among_many([0, 77, 2 ** 19, n - 1], n, held, new, table)
+            cache = R.Cache(c.k, c.v, c.ks, c.vs, *lists, pages=c.pages, page=16, max_pages=table.shape[1], n_seqs=n, Hkv=Hkv, dh=dh)
+        q = torch.full((T + 1, H * dh), NAN, dtype=TORCH[dtype], device="cuda")
+        R.revffn_op_cache_append(1 if dtype == "bf16" else 0, cache, _rotary(dh), None, x, q, x[:, H * dh:], x[:, (H + Hkv) * dh:], T, H, w, H * dh, w, w)
+        torch.cuda.synchronize()
+        assert torch.isfinite(q[:T]).all() and torch.isnan(q[T:]).all()
+        out.append((c.k, c.v, c.ks, c.vs, q[:T]))
+    assert all(torch.equal(a, b) for a, b in zip(*out))
