@@ -495,13 +495,14 @@ int revffn_op_attention_cached(const revffn_attn_desc *desc, const revffn_cache 
 
 /* Rows of x (dtype, `cols` columns, <= 2^24) to 8-bit integers: scale[row] = max |x| / 127 (float32), codes = x / scale rounded to the nearest integer, ties to
  * even, as if the quotient were exact.  A row whose scale would be below 2^-126 is zeros with scale 0; one with a value that is not finite is zeros with
- * scale NaN, which poisons its products.  For a layer's tokens before each product, and for its weights (rows = output channels), once. */
+ * scale NaN, which poisons its products.  For a layer's tokens before each product, and for its weights (rows = output channels), once.  Fewer than 2^24 rows. */
 int revffn_op_quantize_rows(int32_t dtype, const void *x, int8_t *codes, float *scale, int32_t rows, int32_t cols, int64_t ldx, int64_t ldc,
                             void *hip_stream);
 /* c[m, n] = (sum_k a[m, k] b[n, k]) a_scale[m] b_scale[n] + bias[n]: a [M, K] and b [N, K] 8-bit integers, c and bias (NULL: none) in dtype.  The sum is
  * exact (K <= 131071).  c shares no elements with the others.  lda, ldb multiples of 16 and a, b aligned to 16 bytes go to the matrix cores (K may be
  * any), others to a slow kernel (kernel_mode 2: REVFFN_EUNSUPPORTED; 1: the slow kernel always; + 256 * t forces one of the matrix-core kernel's
- * shapes, t = 1 ..).  All give the same bits. */
+ * shapes, t = 1 ..).  All give the same bits.  lda, ldb below 2^22 for the matrix cores; REVFFN_ESHAPE: M or N of 2^30 and more, M * N of 2^36 and more (a
+ * forced shape: more tiles than a launch can have), a stride below the row's width. */
 int revffn_op_gemm_int(int32_t dtype, int32_t kernel_mode, const int8_t *a, const float *a_scale, const int8_t *b, const float *b_scale,
                       const void *bias, void *c, int32_t M, int32_t N, int32_t K, int64_t lda, int64_t ldb, int64_t ldc, void *hip_stream);
 

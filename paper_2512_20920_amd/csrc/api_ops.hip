@@ -298,11 +298,13 @@ int revffn_op_gemm_int(int32_t dtype, int32_t kernel_mode, const int8_t* a, cons
     return REVFFN_EINVAL;
   if (M > 0 && N > 0 && same_place({c}, {a, b, a_scale, b_scale, bias})) return REVFFN_EINVAL;
   // (128 * 128 * K has to stay below 2^31)
-  if (K > 131071 || lda < K || ldb < K || ldc < N || !grid_fits(((i64)M + 31) / 32 * (((i64)N + 31) / 32) * 4)) return REVFFN_ESHAPE;
+  if (K > 131071 || lda < K || ldb < K || ldc < N) return REVFFN_ESHAPE;
   GemmI8 g = {(const signed char*)a, (const signed char*)b, a_scale, b_scale, bias, c, dtype, M, N, K, lda, ldb, ldc};
   const bool fits = gemm_i8_takes(g);
   if (((kernel_mode & 0xff) == 2 || kernel_mode >> 8) && !fits) return REVFFN_EUNSUPPORTED;
-  launch_gemm_i8(g, kernel_mode >> 8 ? 1 + (kernel_mode >> 8) : (kernel_mode == 1 || !fits ? 1 : 0), (hipStream_t)stream);
+  const int form = kernel_mode >> 8 ? 1 + (kernel_mode >> 8) : (kernel_mode == 1 || !fits ? 1 : 0);
+  if (!gemm_i8_launches(g, form)) return REVFFN_ESHAPE;
+  launch_gemm_i8(g, form, (hipStream_t)stream);
   return 0;
 }
 

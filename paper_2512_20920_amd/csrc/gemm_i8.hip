@@ -317,17 +317,26 @@ template <class T> __global__ void __launch_bounds__(256) gemm_i8_any_k(GemmI8 g
   }
 }
 
-template <class K> void launch(K kernel, std::atomic<unsigned long long>& attr_mask, int BM, int BN, int threads, size_t smem, const GemmI8& g, hipStream_t s) {
+// The matrix-core shapes: rows and columns of a tile, threads, workgroups that all CUs hold at once, and what a round of those takes per 128 k's
+struct Shape { int bm, bn, threads, round; float us; };
+constexpr Shape SHAPES[] = {{256, 256, 512, 256, 1.93f}, {128, 256, 512, 256, 1.20f}, {128, 128, 512, 256, 0.72f}, {64, 64, 256, 512, 0.49f}, {32, 32, 512, 0, 0.f}};
+constexpr int FIRST = 2, FEW = 6;                    // forms of the first shape and of the last, which splits k instead
+static_assert(sizeof(SHAPES) / sizeof(Shape) == GEMM_I8_FORMS && FIRST + GEMM_I8_FORMS - 1 == FEW, "forms 2 .. are the shapes in order");
+i64 tiles_of(const GemmI8& g, const Shape& x) { return ((i64)g.M + x.bm - 1) / x.bm * (((i64)g.N + x.bn - 1) / x.bn); }
+bool launches(const GemmI8& g, const Shape& x) { return (tiles_of(g, x) + 7) / 8 * 8 * x.threads < (i64)1 << 32; }
+
+template <class K> void launch(K kernel, std::atomic<unsigned long long>& attr_mask, int form, size_t smem, const GemmI8& g, hipStream_t s) {
   if (attr_needed(attr_mask)) {
     (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     attr_done(attr_mask);
   }
-  const i64 tiles = (i64)cdiv(g.M, BM) * cdiv(g.N, BN);
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(threads), smem, s, g);
+  const Shape& x = SHAPES[form - FIRST];
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((tiles_of(g, x) + 7) / 8 * 8)), dim3(x.threads), smem, s, g);
 }
-template <class T, int BM, int BN, int WGM, int NW, int NS> void go(const GemmI8& g, hipStream_t s) {
+template <class T, int FORM, int WGM, int NS> void go(const GemmI8& g, hipStream_t s) {
   static std::atomic<unsigned long long> mask{0};
-  launch(gemm_i8_k<T, BM, BN, WGM, NW, NS>, mask, BM, BN, NW * 64, (size_t)NS * (BM + BN) * KB, g, s);
+  constexpr Shape X = SHAPES[FORM - FIRST];
+  launch(gemm_i8_k<T, X.bm, X.bn, WGM, X.threads / 64, NS>, mask, FORM, (size_t)NS * (X.bm + X.bn) * KB, g, s);
 }
 // Which shape a product gets: the one with the least rounds of workgroups times what a round takes per 128 k's (us, measured with every CU busy):
 //   256 x 256 in phases 1.93, 128 x 256 1.20, 128 x 128 0.72, 64 x 64 (two per CU) 0.49.
@@ -337,26 +346,29 @@ template <class T, int BM, int BN, int WGM, int NW, int NS> void go(const GemmI8
 // A tile of 32 x 32 each, where no CU gets two (us, then the best of the others): 8 x 6144, k 2048: 5.2, 8.1; 48 x 4096, k 14336: 27, 39; 128 x 2048, k 5632:
 // 12.9, 17.3; beyond, 48 x 6144, k 2048: 8.9, 8.5; 8 x 14336, k 4096: 14.5, 13.6; 128 x 4096, k 14336: 52, 39.
 int form_for(const GemmI8& g) {
-  if ((i64)cdiv(g.M, 32) * cdiv(g.N, 32) <= 256) return 6;
-  const struct { int form, bm, bn, round; float us; } shapes[] = {{2, 256, 256, 256, 1.93f}, {3, 128, 256, 256, 1.20f}, {4, 128, 128, 256, 0.72f}, {5, 64, 64, 512, 0.49f}};
-  int best = 5;
+  if (tiles_of(g, SHAPES[FEW - FIRST]) <= 256) return FEW;
+  int best = FIRST;
   float least = INFINITY;
-  for (const auto& x : shapes) {
-    const i64 tiles = (i64)cdiv(g.M, x.bm) * cdiv(g.N, x.bn);
-    const float cost = (float)((tiles + x.round - 1) / x.round) * x.us;
-    if (cost < least) { least = cost; best = x.form; }
+  for (int form = FIRST; form < FEW; form++) {
+    const Shape& x = SHAPES[form - FIRST];
+    const float cost = (float)((tiles_of(g, x) + x.round - 1) / x.round) * x.us;
+    if (cost < least && launches(g, x)) { least = cost; best = form; }
   }
   return best;
 }
 template <class T> void go(const GemmI8& g, int form, hipStream_t s) {
   static std::atomic<unsigned long long> mask{0};
   switch (form ? form : form_for(g)) {
-    case 1: hipLaunchKernelGGL((gemm_i8_any_k<T>), dim3(cdiv(g.N, 256), g.M < 4096 ? g.M : 4096), dim3(256), 0, s, g); break;
-    case 2: launch(gemm_i8_phased_k<T>, mask, 256, 256, 512, 2 * 512 * KB, g, s); break;
-    case 3: go<T, 128, 256, 2, 8, 3>(g, s); break;
-    case 4: go<T, 128, 128, 4, 8, 4>(g, s); break;
-    case 6: hipLaunchKernelGGL((gemm_i8_few_k<T>), dim3((unsigned)cdiv(g.M, 32) * (unsigned)cdiv(g.N, 32)), dim3(512), 0, s, g); break;
-    default: go<T, 64, 64, 2, 4, 4>(g, s);
+    case 1: {                                        // (2^31 threads at most)
+      const int blocks = cdiv(g.N, 256), most = (1 << 23) / blocks;
+      hipLaunchKernelGGL((gemm_i8_any_k<T>), dim3(blocks, g.M < 4096 ? (g.M < most ? g.M : most) : (most < 4096 ? most : 4096)), dim3(256), 0, s, g);
+      break;
+    }
+    case 2: launch(gemm_i8_phased_k<T>, mask, 2, 2 * 512 * KB, g, s); break;
+    case 3: go<T, 3, 2, 3>(g, s); break;
+    case 4: go<T, 4, 4, 4>(g, s); break;
+    case FEW: hipLaunchKernelGGL((gemm_i8_few_k<T>), dim3((unsigned)tiles_of(g, SHAPES[FEW - FIRST])), dim3(512), 0, s, g); break;
+    default: go<T, 5, 2, 4>(g, s);
   }
 }
 
@@ -364,6 +376,10 @@ template <class T> void go(const GemmI8& g, int form, hipStream_t s) {
 
 bool gemm_i8_takes(const GemmI8& g) {
   return (g.lda | g.ldb) % 16 == 0 && ((uintptr_t)g.a | (uintptr_t)g.b) % 16 == 0 && g.lda < (1 << 22) && g.ldb < (1 << 22);
+}
+// M, N below 2^30 and fewer than 2^36 results: 256 x 256 always does, and the slow kernel
+bool gemm_i8_launches(const GemmI8& g, int form) {
+  return g.M < 1 << 30 && g.N < 1 << 30 && (i64)g.M * g.N < (i64)1 << 36 && (form < FIRST || launches(g, SHAPES[form - FIRST]));
 }
 void launch_gemm_i8(const GemmI8& g, int form, hipStream_t s) {
   if (g.M < 1 || g.N < 1) return;

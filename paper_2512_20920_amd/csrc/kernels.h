@@ -443,4 +443,5 @@ struct GemmI8 {
 };
 #define GEMM_I8_FORMS 5
 bool gemm_i8_takes(const GemmI8& g);                // whether the matrix-core kernels do
+bool gemm_i8_launches(const GemmI8& g, int form);   // whether a launch can hold it
 void launch_gemm_i8(const GemmI8& g, int form, hipStream_t s);      // form: 0 by size, 1 any shape and alignment (slow), 2.. forced, see gemm_i8.hip

@@ -232,3 +232,12 @@ def test_append_refuses_more_than_a_launch_can_hold(lib):
     c = cache(n_seqs=2 ** 20, Hkv=64)
     assert append(lib, c, T=2 ** 20, ldk=4096, ldv=4096) == ESHAPE and append(lib, cache(), T=2 ** 26) == ESHAPE
     assert append(lib, cache(n_seqs=2 ** 20, Hkv=3, dh=128, page=128), T=2 ** 20, q=None, q_out=None, ldk=384, ldv=384) == ESHAPE
+
+
+def test_integer_products_refuse_more_than_a_launch_can_hold(lib):
+    def product(M, N, mode=0, lda=16):
+        return lib.revffn_op_gemm_int(1, mode, P, 2 * P, 3 * P, 4 * P, None, 6 * P, M, N, 16, lda, lda, N, None)
+    for M, N in ((2 ** 30, 1), (1, 2 ** 30), (2 ** 18, 2 ** 18), (2 ** 31 - 1, 2 ** 31 - 1)):
+        for mode in (0, 1, 2, 256, 256 * 5):
+            assert product(M, N, mode) == ESHAPE and (mode >= 2 or product(M, N, mode, lda=17) == ESHAPE)
+    assert product(2 ** 17, 2 ** 17, 256 * 5) == ESHAPE and product(1, 2 ** 30 - 1, 256 * 4) == ESHAPE      # (more tiles than a launch can have)

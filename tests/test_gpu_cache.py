@@ -840,3 +840,21 @@ def test_append_among_a_million_sequences(dtype):
         assert torch.isfinite(q[:T]).all() and torch.isnan(q[T:]).all()
         out.append((c.k, c.v, c.ks, c.vs, q[:T]))
     assert all(torch.equal(a, b) for a, b in zip(*out))
+
+
+@pytest.mark.parametrize("M,N,K,mode", [(32768, 151936, 16, 0), (32768, 151936, 16, 256 * 4), (5000, 2 ** 20 + 7, 3, 1), (1, 2 ** 27 + 3, 16, 0), (3, 2 ** 27 + 1, 16, 2), (2 ** 27 + 33, 1, 16, 0)])
+def test_product_of_more_than_two_to_the_32_results(M, N, K, mode):
+    """Many rows by many columns, or one of them beyond what 32 by 32 tiles of a launch reach; every result: sums and scales are such that only the last rounding is one."""
+    g = torch.Generator(device="cuda").manual_seed(M + K)
+    ints = lambda n: torch.randint(-128, 128, (n, 16), generator=g, device="cuda", dtype=torch.int8)
+    units = lambda n: torch.exp2(-torch.randint(0, 9, (n,), generator=g, device="cuda").float())
+    a, b, sa, sb = ints(M), ints(N), units(M), units(N)
+    c = torch.full((M, N), NAN, dtype=torch.bfloat16, device="cuda")
+    R.revffn_op_gemm_int(1, mode, a, sa, b, sb, None, c, M, N, K, 16, 16, N)
+    torch.cuda.synchronize()
+    m = min(M, 1024)
+    n = (1 << 27) // m
+    for i in range(0, M, m):
+        for j in range(0, N, n):
+            x, y = a[i:i + m, :K].float() * sa[i:i + m, None], b[j:j + n, :K].float() * sb[j:j + n, None]
+            assert torch.equal(c[i:i + m, j:j + n], (x @ y.T.contiguous()).to(torch.bfloat16)), (i, j)
