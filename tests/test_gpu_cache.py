@@ -858,3 +858,104 @@ def test_product_of_more_than_two_to_the_32_results(M, N, K, mode):
         for j in range(0, N, n):
             x, y = a[i:i + m, :K].float() * sa[i:i + m, None], b[j:j + n, :K].float() * sb[j:j + n, None]
             assert torch.equal(c[i:i + m, j:j + n], (x @ y.T.contiguous()).to(torch.bfloat16)), (i, j)
+
+
+# ---- whose rows are written, and the four calls in a graph -------------------------------------------------------------
+# lengths, first rows of eight rows in a call, and (sequence, first row, rows) of those that are owned after numbers have been clamped
+LISTS = [([-4, -2 ** 31, 2 ** 31 - 1], [0, 1, 3, 6], [(0, 0, 1), (1, 1, 2), (2, 3, 3)]), ([48, 48, 48], [100, -7, 2 ** 31 - 1, -1], [(1, 0, 8)]),
+         ([48, 48, 48], [5, 4, 3, 2], []), ([0, 0, 0], [0, 0, 0, 0], []), ([30, 48, 20], [2, 2, 5, 2 ** 31 - 1], [(1, 2, 3), (2, 5, 3)])]
+
+
+@MODES
+@pytest.mark.parametrize("held,cu,owned", LISTS)
+def test_attention_writes_the_rows_of_its_sequences(held, cu, owned, dtype, mode):
+    """Exactly those, whatever the lists hold, and what they should be: lengths past the table see all of it, none sees nothing."""
+    c = Paged(dtype, 2, 64, 16, [[0, 1, 2], [3, 4, 5], [6, 7, 8]])
+    _fill(c, [48, 48, 48])
+    a = Attend(c, [48, 48, 48], [2, 3, 3], 4, mode, extra=0)
+    a.cache = c.cache(held, cu)
+    a.run()
+    o, lse = a.results()
+    mine = np.zeros(8, bool)
+    for s, first, n in owned:
+        length = min(max(held[s], 0), 2 ** 30)
+        want = ref.attention(c.model, c.table[s:s + 1], [length], [n], a.queries()[first:first + n], dtype=dtype)
+        assert outside(o[first:first + n], *want["o"]) <= 1.0 and outside(lse[:, first:first + n], *want["lse"]) <= 1.0
+        mine[first:first + n] = True
+    assert np.isnan(o[~mine]).all() and np.isnan(lse[:, ~mine]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("held,cu,owned", LISTS)
+def test_append_writes_the_rows_of_its_sequences(held, cu, owned, dtype):
+    """Their queries, keys and values where they have a place, and nothing else."""
+    Hkv, H, dh = 2, 4, 64
+    c = Paged(dtype, Hkv, dh, 16, [[0, 1, 2], [3, 4, 5], [6, 7, 8]])
+    _fill(c, [48, 48, 48])
+    x = _normal(np.random.default_rng(9), dtype, 8, (H + 2 * Hkv) * dh)
+    out = torch.full((8, H * dh), NAN, dtype=TORCH[dtype], device="cuda")
+    w = x.stride(0)
+    R.revffn_op_cache_append(1 if dtype == "bf16" else 0, c.cache(held, cu), None, None, x, out, x[:, H * dh:], x[:, (H + Hkv) * dh:], 8, H, w, H * dh, w, w)
+    torch.cuda.synchronize()
+    mine = np.zeros(8, bool)
+    k, v = (_np(x[:, n * dh:(n + Hkv) * dh]).reshape(8, Hkv, dh) for n in (H, H + Hkv))
+    for s, first, n in owned:
+        length = min(max(held[s], 0), 2 ** 30)
+        at = length - n + np.arange(n)
+        mine[first:first + n] = (at >= 0) & (at < 48)
+        c.model.append(c.table[s:s + 1], [length], [n], k[first:first + n], v[first:first + n])
+    c.check()
+    mine = torch.from_numpy(mine).cuda()
+    assert torch.equal(out[mine], x[mine][:, :H * dh]) and torch.isnan(out[~mine]).all()
+
+
+@pytest.mark.parametrize("mode", [0] + FORMS[2:])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_graph_replays_of_a_layer(dtype, mode):
+    """All four calls captured once and replayed as the sequences grow: every replay equals the same calls made eagerly on a cache of its own, with eager
+    work between the replays."""
+    d, page, Hkv, H, dh, S = 256, 16, 2, 4, 64, 3
+    table, held0 = [[0, 1, 2, 3], [4, 5, 6, 7], [8, 9, 10, 11]], np.array([5, 15, 31])
+    rng, t, dt, width = np.random.default_rng(10), TORCH[dtype], 1 if dtype == "bf16" else 0, (H + 2 * Hkv) * dh
+    new = lambda *s, ty=t: torch.full(s, 1, dtype=ty, device="cuda")
+    ints = lambda n, k: (torch.from_numpy(rng.integers(-127, 128, (n, k)).astype(np.int8)).cuda(), torch.from_numpy(rng.uniform(1e-4, 1e-3, n).astype(np.float32)).cuda())
+    (wqkv, sqkv), (wo, so) = ints(width, d), ints(d, H * dh)
+    x, r, desc = new(S, d), _rotary(dh), R.AttnDesc(dtype=dt, H=H, Hkv=Hkv, dh=dh, Tq=S, ldq=width)
+    k, v = rng.standard_normal((2, held0.sum(), Hkv, dh))
+
+    class Layer:
+        def __init__(self):
+            self.c = Paged(dtype, Hkv, dh, page, table)
+            _fill(self.c, held0, k, v)
+            self.cache, self.held = self.c.cache(held0, None), self.c.lists[1]
+            self.work = torch.empty(R.revffn_op_attention_cached_workspace(desc, self.cache), dtype=torch.uint8, device="cuda")
+            self.codes, self.scale, self.qkv, self.o, self.y = new(S, d, ty=torch.int8), new(S, ty=torch.float32), new(S, width), new(S, H * dh), new(S, d)
+            self.lse = new(H, S, ty=torch.float32)
+
+        def step(self):
+            qkv = self.qkv
+            R.revffn_op_quantize_rows(dt, x, self.codes, self.scale, S, d, d, d)
+            R.revffn_op_gemm_int(dt, mode, self.codes, self.scale, wqkv, sqkv, None, qkv, S, width, d, d, d, width)
+            R.revffn_op_cache_append(dt, self.cache, r, None, qkv, qkv, qkv[:, H * dh:], qkv[:, (H + Hkv) * dh:], S, H, width, width, width, width)
+            R.revffn_op_attention_cached(desc, self.cache, True, 0, qkv, self.o, self.lse, self.work)
+            R.revffn_op_quantize_rows(dt, self.o, self.codes, self.scale, S, H * dh, H * dh, d)
+            R.revffn_op_gemm_int(dt, mode, self.codes, self.scale, wo, so, None, self.y, S, d, H * dh, d, H * dh, d)
+    a, b = Layer(), Layer()
+    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        with torch.cuda.graph(graph, stream=stream):
+            a.step()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        x.copy_(_normal(rng, dtype, S, d))
+        for layer in (a, b):
+            layer.held.add_(1)
+        graph.replay()
+        b.step()
+        torch.cuda.synchronize()
+        for n in ("codes", "scale", "qkv", "o", "lse", "y"):
+            p, q = getattr(a, n), getattr(b, n)
+            assert torch.equal(p, q) and torch.isfinite(p.float()).all(), n
+        assert torch.equal(a.c.k, b.c.k) and torch.equal(a.c.v, b.c.v) and torch.equal(a.c.ks.nan_to_num(0), b.c.ks.nan_to_num(0))
+        torch.randn(1000, device="cuda").sum().item()
