@@ -3,6 +3,9 @@ layout of the cache's struct; and the references in 64 bits against independent 
 import ctypes
 import os
 import re
+import struct
+import subprocess
+import tempfile
 
 import numpy as np
 import pytest
@@ -241,3 +244,30 @@ def test_integer_products_refuse_more_than_a_launch_can_hold(lib):
         for mode in (0, 1, 2, 256, 256 * 5):
             assert product(M, N, mode) == ESHAPE and (mode >= 2 or product(M, N, mode, lda=17) == ESHAPE)
     assert product(2 ** 17, 2 ** 17, 256 * 5) == ESHAPE and product(1, 2 ** 30 - 1, 256 * 4) == ESHAPE      # (more tiles than a launch can have)
+
+
+def _kernels(path):
+    """{name: (registers spilled, bytes of private memory)} of every kernel in a library built here."""
+    data, out = open(path, "rb").read(), {}
+    for m in re.finditer(b"__CLANG_OFFLOAD_BUNDLE__", data):
+        at = m.end() + 8
+        for _ in range(struct.unpack_from("<Q", data, m.end())[0]):
+            offset, size, length = struct.unpack_from("<3Q", data, at)
+            target = data[at + 24:at + 24 + length]
+            at += 24 + length
+            if not target.endswith(b"gfx950"):
+                continue
+            with tempfile.NamedTemporaryFile(suffix=".elf") as f:
+                f.write(data[m.start() + offset:m.start() + offset + size])
+                f.flush()
+                notes = subprocess.run(["/opt/rocm/llvm/bin/llvm-readelf", "--notes", f.name], capture_output=True, text=True, check=True).stdout
+            for block in notes.split("  - .agpr_count:")[1:]:
+                field = lambda n: re.search(rf"^ +\.{n}: +(\S+)", block, re.M).group(1)
+                out[field("name")] = (int(field("vgpr_spill_count")), int(field("private_segment_fixed_size")))
+    return out
+
+
+def test_no_kernel_of_the_cache_spills_registers(lib):
+    """A rule of those kernels: the first ones that spilled gave wrong results, and spills in their loops would cost more than the forms that do without."""
+    kernels = {n: x for n, x in _kernels(R.library_path()).items() if "cached_" in n or "cache_append" in n or "gemm_i8" in n or "quantize_rows" in n}
+    assert len(kernels) > 100 and not {n for n, x in kernels.items() if x != (0, 0)}
