@@ -462,7 +462,7 @@ typedef struct revffn_cache {
   const int32_t *table;    /* device [n_seqs][max_pages]                                             */
   const int32_t *len;      /* device [n_seqs]: tokens of each sequence, those of this call among them */
   const int32_t *cu;       /* device [n_seqs + 1], ascending, or NULL                                */
-  int32_t pages, page;     /* pages of the memory; tokens of one: 16, 32, 64 or 128                  */
+  int32_t pages, page;     /* pages of the memory (pages * Hkv below 2^31); tokens of one: 16, 32, 64 or 128 */
   int32_t max_pages;       /* row length of table; max_pages * page <= 2^30                          */
   int32_t n_seqs;          /* up to 2^20                                                             */
   int32_t Hkv, dh;         /* key heads; head width, a multiple of 16 up to 256, page * dh <= 16384  */

@@ -454,7 +454,7 @@ __device__ __forceinline__ void few_rows(const CachedAttn& a, const Item& x, flo
 
 // ---- many rows: 32 per wave, tiles of 32 keys ----
 // Bound by the vector instructions of the softmax and the conversions, and by how many waves a SIMD has to take them from: two at 128 columns (195
-// registers), three at 64.  4096 rows of 32 heads to 8 of 128 columns behind 4096 tokens: 486 us, 0.85 PFLOP/s.  Each wave converts its tiles for itself: converted
+// registers), three at 64.  4096 rows of 32 heads to 8 of 128 columns behind 4096 tokens: 486 to 499 us, 0.85 to 0.83 PFLOP/s.  Each wave converts its tiles for itself: converted
 // once for the workgroup, in LDS, 553 us, with the reads a tile ahead 510; queries in LDS, which leaves registers for three waves, 547 us (502 with two):
 // more waves find less of each other's tiles in the L1 cache.  A tile's registers are filled again as soon as they are used up; with a second set 525.
 // LDS: the parts of three waves, then a row of floats for each
@@ -801,7 +801,9 @@ template <int DHP, bool F32> void go(const CachedAttn& a, hipStream_t s) {
 // they make.  32 heads of 128 over 8, 32, 64, 128 rows, us: 512 tokens 15.8, 16.3, 31.1; 512 behind 3000 46.8, 53.7, 63.5; 2048 behind 3000 184, 173, 182;
 // 4096 behind 3000 426, 404, 396.  The same of 64: 11.5, 13.4, 24.9; 34.3, 46.4, 51.1; 109, 111, 131; 249, 241, 258.
 void cached_attn_plan(CachedAttn* a) {
-  a->target = a->c.dh <= 64 ? 1024 : a->c.dh <= 128 ? 512 : 256;      // workgroups that are on the CUs together
+  // the workgroups that bfloat16's form for few rows has on the CUs together: four, two, one on each.  (Of those with fewer, three for
+  // most for many rows at 64 columns, in float32 half as many, some wait for others to end.)
+  a->target = a->c.dh <= 64 ? 1024 : a->c.dh <= 128 ? 512 : 256;
   const i64 blocks = ((i64)a->T * a->H) >> 7;        // workgroups of 128 rows
   a->lr = 4 * blocks <= a->target ? 5 : 2 * blocks <= 3 * (i64)a->target ? 6 : 7;
   a->few_only = (i64)a->T * a->G <= FEW_ROWS || a->T <= a->c.n_seqs;

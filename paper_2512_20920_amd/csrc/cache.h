@@ -9,8 +9,6 @@
 #pragma once
 #include "attn_range.h"
 
-#define E4M3_NAN 0x7f7f7f7fu
-
 __device__ __forceinline__ int cache_len(const CacheView& c, int s) { return min(max(c.len[s], 0), 1 << 30); }
 // rows of this call that belong to a sequence: the first, and how many
 __device__ __forceinline__ int2 cache_rows(const CacheView& c, int s, int T) {

@@ -15,17 +15,20 @@ namespace {
 
 constexpr int KB = 128;                  // bytes of k per tile
 
-// rows row0 .. of an operand as a buffer: offsets count from row0, what lies behind the last row reads as zeros
+// rows row0 .. of an operand as a buffer: offsets count from row0, what lies behind the last row reads as zeros.  As the four words that loads into LDS take,
+// and as what loads into registers do.
+__device__ __forceinline__ unsigned rows_bytes(i64 ld, int row0, int rows, int K) {
+  const i64 n = rows > row0 ? ((i64)(rows - row0 - 1) * ld + K + 3) & ~3ll : 0;
+  return (unsigned)(n < (i64)OOB ? n : (i64)OOB);
+}
 __device__ __forceinline__ u32x4 rows_desc(const signed char* p, i64 ld, int row0, int rows, int K) {
   const unsigned long long at = (unsigned long long)(p + (i64)row0 * ld);
-  const i64 n = rows > row0 ? ((i64)(rows - row0 - 1) * ld + K + 3) & ~3ll : 0;
   u32x4 d = {(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)at), (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(at >> 32)),
-             (unsigned)__builtin_amdgcn_readfirstlane((int)(n < (i64)OOB ? n : (i64)OOB)), 0x00020000u};
+             (unsigned)__builtin_amdgcn_readfirstlane((int)rows_bytes(ld, row0, rows, K)), 0x00020000u};
   return d;
 }
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const signed char* p, i64 ld, int row0, int rows, int K) {
-  const i64 n = rows > row0 ? ((i64)(rows - row0 - 1) * ld + K + 3) & ~3ll : 0;
-  return __builtin_amdgcn_make_buffer_rsrc((void*)(p + (i64)row0 * ld), (short)0, (int)(n < (i64)OOB ? n : (i64)OOB), 0x00020000);
+  return __builtin_amdgcn_make_buffer_rsrc((void*)(p + (i64)row0 * ld), (short)0, (int)rows_bytes(ld, row0, rows, K), 0x00020000);
 }
 __device__ __forceinline__ i32x4 fragment(const unsigned char* tile, int r, int kk, int lane) {
   return *(const i32x4*)(tile + r * KB + (((kk * 2 + (lane >> 5)) ^ ((r >> 1) & 7)) << 4));
