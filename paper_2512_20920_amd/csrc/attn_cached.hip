@@ -9,7 +9,8 @@
 //  * V: a lane's 16 probabilities are those of 16 tokens in a row, which are the 16 bytes of one column that the cache keeps together.
 // In the form for few rows (16 per workgroup, whose waves share the keys out in tiles of 64, 16x16x32) the same with g = lane >> 4: four runs of 16 tokens,
 // four blocks b of 16 keys whose row m is token 16 (m >> 2) + 4 b + (m & 3).
-// Scores, maxima, sums and accumulators are float32.  bfloat16 calls round the probabilities to bfloat16 as operands; float32 calls take queries
+// Scores, maxima, sums and accumulators are float32.  bfloat16 calls round the probabilities to bfloat16 as operands (results are
+// then 1.1 to 1.4 times as far from 64 bits, relative error 0.0023 for a prompt's piece, as with probabilities that would take three products); float32 calls take queries
 // and probabilities as three bfloat16 numbers each (24 bits; the cache's numbers need no more than one), so they are float32 throughout.
 #include "attn_range_tiles.h"
 #include "cache.h"
